@@ -10,7 +10,9 @@
  *   4. column-wise OBS sweep with b-bit asymmetric grids      (kq_obs_quantize)
  * with the GPTAQ drift correction as an option (kq_accum_drift, kq_gptaq_p, and the Pt
  * argument of kq_obs_quantize), inference with the quantized layer (kq_pack_codes,
- * kq_infer), plus two check-only calls (kq_dequant_revert, kq_proxy_loss).
+ * kq_infer), decoding with a 4-bit key/value cache (kq_kv_append, kq_kv_attend, kq_kv_evict,
+ * kq_kv_read), scoring (kq_token_logprobs and its gradient), plus two check-only calls
+ * (kq_dequant_revert, kq_proxy_loss).
  *
  * Conventions shared by every call
  *   - Tokens are rows: X is [T x d_in], G is [T x d_out]; the paper stacks tokens as
@@ -106,7 +108,8 @@ KQ_API kq_status kq_selftest_timeout(int* info, int64_t limit_us, kq_stream_t st
  * checker on machines where none may run.
  * kq_debug_build: 1 for the debug build, 0 otherwise.
  * kq_debug_status: synchronizes the device, then *unit = the first source file (0 api,
- *   1 syrk, 2 biip, 3 chol, 4 obs, 5 trail_tc, 6 gptaq, 7 infer, 8 check) whose checks
+ *   1 syrk, 2 biip, 3 chol, 4 obs, 5 trail_tc, 6 gptaq, 7 infer, 8 check, 9 kv_store,
+ *   10 kv_attend, 11 kv_evict, 12 logprob) whose checks
  *   failed and *line = its first failing line, or *unit = -1 and *line = 0 when none did
  *   (always so in the normal build); reset clears the recorded lines.
  * kq_selftest_bounds: writes buf[i] = i for i = 0 .. n under a check against n; buf must
@@ -405,6 +408,130 @@ KQ_API kq_status kq_infer(const uint32_t* packed, const float* scale, const int3
                           int64_t d_in, int bits, int group, const float* s_x, const float* s_g,
                           const int8_t* sign_u, const int8_t* sign_v, const float* x, int64_t B, float* y,
                           int* info, void* ws, size_t ws_bytes, kq_stream_t stream);
+
+/* ------------------------------------------------------------------------------------
+ * Decoding with a 4-bit key/value cache (serving a quantized model; no counterpart in the
+ * paper, whose inference ends at the layer products of kq_infer).
+ *
+ * The cache is a pool of pages that the caller owns. Keys and values are held in 4 bits, each
+ * row (one token, one head, `dim` values) on a grid of its own: offset = the row's minimum
+ * rounded down to bf16, scale = (maximum - offset) / 15 rounded up to bf16, code =
+ * clamp(rint((x - offset) / scale), 0, 15) (float32 operations, IEEE division, ties to even),
+ * value = scale * code + offset. A constant row that bf16 holds has scale 0. A row with a NaN or
+ * an infinity, or whose range has no finite bf16 grid, gets scale = offset = NaN: it reads back
+ * as NaN, and so does every attention output that sees it.
+ *
+ * kq_kv_cache: data [pages][kv_heads][page * (dim + 8)] bytes, 16-byte aligned; a page and
+ *   head is page / 16 granules of 16 tokens, each [16][dim / 2] bytes of key codes (dimension
+ *   2 j in the low half of byte j), the same of value codes, 16 (scale, offset) bf16 pairs
+ *   of the keys and 16 of the values. table [batch][table_ld] int32: the page of slots
+ *   p * page .. of a sequence. dim is 64 or 128, page a multiple of 16 up to 1024, kv_heads and
+ *   batch up to 65535, table_ld * page < 2^31. Two sequences may share pages that neither
+ *   writes. The structure itself is read on the host during the call.
+ *
+ * Tokens of several sequences are packed: token i belongs to the sequence b with
+ * start[b] <= i < start[b + 1] (start [batch + 1] int32, not decreasing). lens [batch] int32 is
+ * the number of occupied slots of each sequence. Device arrays are checked by the kernels: a
+ * length or a page out of range, or a token without a slot, is skipped or clamped and recorded
+ * in info (nullable, device int) as -KQ_ERR_INVALID_ARG, and nothing outside the buffers is
+ * touched. dtype is KQ_BF16 or KQ_F32.
+ *
+ * kq_kv_append: quantizes k, v [T][kv_heads][dim] (token and head strides in elements,
+ *   unit stride in dim) into slots lens[b], lens[b] + 1, ... of each sequence. lens_out
+ *   (nullable) receives the new lengths. acc (nullable, [batch][kv_heads][S] fp32) gets 0 and pos
+ *   (nullable, int32, same shape) the token's position seen[b] + its index in the call at the
+ *   slots written (seen [batch] int32: tokens the sequence has had so far, evicted ones among
+ *   them; seen = NULL counts from lens); seen_out (nullable) receives seen plus the new tokens.
+ *   lens_out and seen_out must not be lens or seen.
+ * kq_kv_read: the values of cached tokens, k, v [T][kv_heads][dim] contiguous: token i of
+ *   sequence b is slot first[b] + i - start[b] (first = NULL: 0). Slots at or beyond lens[b] (lens =
+ *   NULL: the capacity) and tokens of no sequence read 0.
+ * ---------------------------------------------------------------------------------- */
+#define KQ_BF16 0
+#define KQ_F32 1
+typedef struct kq_kv_cache {
+    uint8_t* data;
+    const int32_t* table;
+    int64_t pages, page, kv_heads, dim, batch, table_ld;
+} kq_kv_cache;
+KQ_API kq_status kq_kv_append(const kq_kv_cache* cache, const void* k, const void* v, int dtype, int64_t T,
+                              int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride,
+                              int64_t v_head_stride, const int32_t* start, const int32_t* lens, int32_t* lens_out,
+                              float* acc, int32_t* pos, int64_t S, const int32_t* seen, int32_t* seen_out,
+                              int* info, kq_stream_t stream);
+KQ_API kq_status kq_kv_read(const kq_kv_cache* cache, const int32_t* start, const int32_t* first,
+                            const int32_t* lens, int dtype, int64_t T, void* k, void* v, int* info,
+                            kq_stream_t stream);
+
+/* kq_kv_attend: attention of q [T][q_heads][dim] (token and head strides in elements) over the
+ *   cache, q_heads / kv_heads query heads to a key/value head (head h reads h / (q_heads /
+ *   kv_heads)). The T tokens' own keys are expected in the cache already, as the last slots of
+ *   their sequence: token i of sequence b sees the slots below lens[b] - (start[b + 1] - 1 - i).
+ *     s_j = scale <q, k_j>,  out = sum_j e^(s_j) v_j / sum_j e^(s_j),  lse = ln sum_j e^(s_j)
+ *   out [T][q_heads][dim] contiguous in q's type, lse (nullable) [T][q_heads] fp32. A token that
+ *   sees no slot gives out = 0, lse = -infinity. Sums and softmax are fp32 over exact codes.
+ *   acc (nullable, [batch][kv_heads][S] fp32): each slot's weight e^(s_j - lse), summed over the
+ *   query heads of its head and over the sequence's tokens of this call, is added to it; then
+ *   lens <= S. Results do not depend on the order in which blocks run.
+ *   ws: kq_kv_attend_workspace(T, q_heads, kv_heads, dim, S) bytes (S = 0 without acc), 256-byte
+ *   aligned, contents of no interest before or after.
+ */
+KQ_API size_t kq_kv_attend_workspace(int64_t T, int64_t q_heads, int64_t kv_heads, int64_t dim, int64_t S);
+KQ_API kq_status kq_kv_attend(const kq_kv_cache* cache, const void* q, int dtype, int64_t T, int64_t q_heads,
+                              int64_t q_token_stride, int64_t q_head_stride, const int32_t* start,
+                              const int32_t* lens, float scale, void* out, float* lse, float* acc, int64_t S,
+                              int* info, void* ws, size_t ws_bytes, kq_stream_t stream);
+
+/* kq_kv_evict: cuts every sequence and head with more than `budget` slots back to `budget`
+ *   slots, each head on its own. Kept are the slots whose position is among the last `recent`
+ *   (pos >= seen[b] - recent) or the first `sink` (pos < sink), then those of the largest
+ *   accumulated weight acc; equal weights, and more protected slots than the budget holds, go to
+ *   the lowest slot first; a NaN weight ranks below every number. Kept slots below the budget stay
+ *   where they are; kept slots beyond it move, in order, into the free slots, in order (keys are
+ *   cached with their rotary position applied, so the order of slots carries no meaning beyond
+ *   pos). Only what moves is read and written.
+ *   acc_out, pos_out ([batch][kv_heads][S], S as acc and pos) receive the weights and
+ *   positions of the slots kept; they may be acc and pos themselves. Entries beyond the new length
+ *   are left as they are. lens_out (not lens) receives min(lens, budget). Slots at and beyond
+ *   the new length keep stale contents. Pages must not be shared. recent + sink <= budget, budget >= 1.
+ *   ws: kq_kv_evict_workspace(batch, kv_heads, S, budget) bytes, 256-byte aligned.
+ */
+KQ_API size_t kq_kv_evict_workspace(int64_t batch, int64_t kv_heads, int64_t S, int64_t budget);
+KQ_API kq_status kq_kv_evict(const kq_kv_cache* cache, const int32_t* lens, const float* acc, const int32_t* pos,
+                             const int32_t* seen, int64_t S, int64_t budget, int64_t recent, int64_t sink,
+                             int32_t* lens_out, float* acc_out, int32_t* pos_out, int* info, void* ws,
+                             size_t ws_bytes, kq_stream_t stream);
+
+/* ------------------------------------------------------------------------------------
+ * Log probabilities of given tokens (scoring a quantized model, and the loss its calibration
+ * gradients start from; Sec. 5 of the paper evaluates by perplexity).
+ *
+ * kq_token_logprobs: for each row x of logits [T][V] (row stride ld elements, dtype KQ_BF16 or
+ *   KQ_F32): lse = ln sum_v e^(x_v), logp = x_target - lse, entropy = -sum_v p_v ln p_v, and the
+ *   `top` largest p_v (0 <= top <= 32, top <= V) as top_id [T][top] int32 and top_logp [T][top]
+ *   fp32, largest first, equal logits in the order of their index. lse, entropy nullable; top_id
+ *   and top_logp are NULL when top = 0. -infinity marks a token that cannot occur (p = 0, no share
+ *   in the entropy). target [T] int64: a negative target is not scored (logp = 0); a target >= V is
+ *   recorded in info as -KQ_ERR_INVALID_ARG, with logp = NaN. A row of -infinity only has lse =
+ *   logp = top_logp = -infinity and entropy 0. A row with a NaN or +infinity has NaN results
+ *   (top_id then ranks NaN above every number).
+ *   V <= 2^20. fp32 arithmetic; no workspace.
+ * kq_token_logprobs_grad: the gradient of sum_t (g_logp_t logp_t + g_entropy_t entropy_t):
+ *     grad_v = g_logp (delta(v, target) - p_v) - g_entropy p_v (ln p_v + entropy)
+ *   with lse and entropy from kq_token_logprobs (entropy and g_entropy may both be NULL). grad
+ *   [T][V] in the logits' type, row stride ld_grad; it may be logits itself (same stride). A row
+ *   with a negative target has no g_logp part, a row of -infinity only has grad 0. A target >= V
+ *   is recorded in info, its row's g_logp part left out.
+ * ---------------------------------------------------------------------------------- */
+#define KQ_LOGPROBS_MAX_TOP 32
+#define KQ_LOGPROBS_MAX_V (1 << 20)
+KQ_API kq_status kq_token_logprobs(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld,
+                                   const int64_t* target, int top, float* logp, float* entropy, float* lse,
+                                   int32_t* top_id, float* top_logp, int* info, kq_stream_t stream);
+KQ_API kq_status kq_token_logprobs_grad(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld,
+                                        const int64_t* target, const float* lse, const float* entropy,
+                                        const float* g_logp, const float* g_entropy, void* grad, int64_t ld_grad,
+                                        int* info, kq_stream_t stream);
 
 /* ------------------------------------------------------------------------------------
  * Check-only calls (not part of the timed path).

@@ -229,6 +229,10 @@ int debug_read_trail_tc(int);
 int debug_read_gptaq(int);
 int debug_read_infer(int);
 int debug_read_check(int);
+int debug_read_kv_store(int);
+int debug_read_kv_attend(int);
+int debug_read_kv_evict(int);
+int debug_read_logprob(int);
 }  // namespace kq
 
 extern "C" int kq_debug_build(void) {
@@ -243,7 +247,9 @@ extern "C" kq_status kq_debug_status(int* unit, int* line, int reset) {
     using Reader = int (*)(int);
     static const Reader readers[] = {kq::debug_read_api,      kq::debug_read_syrk,  kq::debug_read_biip,
                                      kq::debug_read_chol,     kq::debug_read_obs,   kq::debug_read_trail_tc,
-                                     kq::debug_read_gptaq,    kq::debug_read_infer, kq::debug_read_check};
+                                     kq::debug_read_gptaq,    kq::debug_read_infer, kq::debug_read_check,
+                                     kq::debug_read_kv_store, kq::debug_read_kv_attend, kq::debug_read_kv_evict,
+                                     kq::debug_read_logprob};
     KQ_CUDA(cudaDeviceSynchronize());
     int u = -1, l = 0;
     for (int k = 0; k < static_cast<int>(sizeof(readers) / sizeof(readers[0])); ++k) {

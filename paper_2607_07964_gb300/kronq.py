@@ -20,6 +20,8 @@ KQ_ERR_CUDA, KQ_ERR_TIMEOUT, KQ_ERR_WORKSPACE, KQ_ERR_NONFINITE = 4, 5, 6, 7
 KQ_FWD, KQ_INV, KQ_FWD_SYM = 0, 1, 2
 KQ_TRAIL_FP32, KQ_TRAIL_3XTF32 = 0, 1
 KQ_SYRK_CHUNK_TOKENS = 512
+KQ_BF16, KQ_F32 = 0, 1
+KQ_LOGPROBS_MAX_TOP = 32
 
 _lib = None
 
@@ -79,6 +81,14 @@ def lib() -> ctypes.CDLL:
             "kq_gptaq_p_workspace": ([I64], SZ),
             "kq_gptaq_p": ([P, P, I64, F, P, P, P, SZ, P], I),
             "kq_dequant_revert": ([P, P, P, I64, I64, I, P, P, P, P, P, P], I),
+            "kq_kv_append": ([P, P, P, I, I64, I64, I64, I64, I64, P, P, P, P, P, I64, P, P, P, P], I),
+            "kq_kv_read": ([P, P, P, P, I, I64, P, P, P, P], I),
+            "kq_kv_attend_workspace": ([I64, I64, I64, I64, I64], SZ),
+            "kq_kv_attend": ([P, P, I, I64, I64, I64, I64, P, P, F, P, P, P, I64, P, P, SZ, P], I),
+            "kq_kv_evict_workspace": ([I64, I64, I64, I64], SZ),
+            "kq_kv_evict": ([P, P, P, P, P, I64, I64, I64, I64, P, P, P, P, P, SZ, P], I),
+            "kq_token_logprobs": ([P, I, I64, I64, I64, P, I, P, P, P, P, P, P, P], I),
+            "kq_token_logprobs_grad": ([P, I, I64, I64, I64, P, P, P, P, P, P, I64, P, P], I),
             "kq_proxy_loss_workspace": ([I64, I64], SZ),
             "kq_proxy_loss": ([P, P, I64, I64, P, P, P, P, SZ, P], I),
         }
@@ -145,7 +155,8 @@ def kq_debug_build() -> bool:
     return bool(lib().kq_debug_build())
 
 
-DEBUG_UNITS = ("api", "syrk", "biip", "chol", "obs", "trail_tc", "gptaq", "infer", "check")
+DEBUG_UNITS = ("api", "syrk", "biip", "chol", "obs", "trail_tc", "gptaq", "infer", "check", "kv_store",
+               "kv_attend", "kv_evict", "logprob")
 
 
 def kq_debug_status(reset: bool = True) -> tuple[str | None, int]:
@@ -452,6 +463,191 @@ def kq_infer(packed, scale, zero, d_out: int, d_in: int, bits: int, group: int, 
     _ok(lib().kq_infer(_ptr(packed), _ptr(scale), _ptr(zero), d_out, d_in, bits, group, _ptr(s_x), _ptr(s_g),
                        _ptr(sign_u), _ptr(sign_v), _ptr(x), B, _ptr(y), _ptr(info), _ptr(ws),
                        0 if ws is None else ws.numel(), _stream(stream)), "kq_infer")
+
+
+class _KvCache(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("table", ctypes.c_void_p)] + [
+        (n, ctypes.c_int64) for n in ("pages", "page", "kv_heads", "dim", "batch", "table_ld")]
+
+
+def kq_kv_cache_bytes(page: int, dim: int) -> int:
+    """Bytes of one page and head of the 4-bit cache: a cache is uint8 [pages, kv_heads, this]."""
+    return page * (dim + 8)
+
+
+def _cache(cache, table, dim: int) -> _KvCache:
+    _need(cache, "cache", torch.uint8)
+    _need(table, "table", torch.int32)
+    if cache.dim() != 3 or table.dim() != 2:
+        raise ValueError("cache must be [pages, kv_heads, page * (dim + 8)], table [batch, pages of a sequence]")
+    if cache.shape[2] % (dim + 8):
+        raise ValueError(f"cache's last dimension must be page * (dim + 8) with dim = {dim}, got {cache.shape[2]}")
+    return _KvCache(cache.data_ptr(), table.data_ptr(), cache.shape[0], cache.shape[2] // (dim + 8), cache.shape[1], dim,
+                    table.shape[0], table.shape[1])
+
+
+_DTYPES = {torch.bfloat16: KQ_BF16, torch.float32: KQ_F32}
+
+
+def _dtype(t, name):
+    d = _DTYPES.get(t.dtype)
+    if d is None:
+        raise ValueError(f"{name} must be bfloat16 or float32, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    return d
+
+
+def _rows3(t, name, heads=None, dim=None):
+    if t.dim() != 3 or (t.stride(2) != 1 and t.numel()):
+        raise ValueError(f"{name} must be [tokens, heads, dim] with unit stride in dim")
+    if (heads is not None and t.shape[1] != heads) or (dim is not None and t.shape[2] != dim):
+        raise ValueError(f"{name} must have {heads} heads of {dim}, got {tuple(t.shape)}")
+
+
+def kq_kv_append(k, v, start, lens, cache, table, lens_out=None, acc=None, pos=None, seen=None, seen_out=None, info=None,
+                 stream=None) -> None:
+    """k, v [T, kv_heads, dim] (bf16 or fp32, any token and head strides) into the 4-bit cache at the
+    slots that follow lens [batch]; start [batch + 1] gives each sequence's tokens. acc, pos [batch,
+    kv_heads, S]: weight 0 and position seen + index at the new slots."""
+    dtype = _dtype(k, "k")
+    _rows3(k, "k", cache.shape[1])
+    _rows3(v, "v", cache.shape[1], k.shape[2])
+    if v.dtype != k.dtype or v.shape != k.shape:
+        raise ValueError("k and v must have one shape and type")
+    _need(v, "v", k.dtype, contiguous=False)
+    c = _cache(cache, table, k.shape[2])
+    B, S = c.batch, 0
+    _need(start, "start", torch.int32, (B + 1,))
+    for t, name in ((lens, "lens"), (lens_out, "lens_out"), (seen, "seen"), (seen_out, "seen_out")):
+        _need(t, name, torch.int32, (B,))
+    for t, name, ty in ((acc, "acc", torch.float32), (pos, "pos", torch.int32)):
+        if t is not None:
+            S = t.shape[-1]
+            _need(t, name, ty, (B, c.kv_heads, S))
+    if acc is not None and pos is not None and acc.shape != pos.shape:
+        raise ValueError("acc and pos must have one shape")
+    _need(info, "info", torch.int32)
+    _ok(lib().kq_kv_append(ctypes.byref(c), _ptr(k), _ptr(v), dtype, k.shape[0], k.stride(0), k.stride(1), v.stride(0),
+                           v.stride(1), _ptr(start), _ptr(lens), _ptr(lens_out), _ptr(acc), _ptr(pos), S, _ptr(seen),
+                           _ptr(seen_out), _ptr(info), _stream(stream)), "kq_kv_append")
+
+
+def kq_kv_read(cache, table, start, first, lens, k, v, info=None, stream=None) -> None:
+    """k, v [T, kv_heads, dim] (bf16 or fp32, contiguous) = the values of cached tokens: token i of
+    sequence b is slot first[b] + i - start[b] (first None: 0); at or beyond lens[b] it reads 0."""
+    dtype = _dtype(k, "k")
+    _rows3(k, "k", cache.shape[1])
+    _need(k, "k", k.dtype)
+    _need(v, "v", k.dtype, tuple(k.shape))
+    c = _cache(cache, table, k.shape[2])
+    _need(start, "start", torch.int32, (c.batch + 1,))
+    _need(first, "first", torch.int32, (c.batch,))
+    _need(lens, "lens", torch.int32, (c.batch,))
+    _need(info, "info", torch.int32)
+    _ok(lib().kq_kv_read(ctypes.byref(c), _ptr(start), _ptr(first), _ptr(lens), dtype, k.shape[0], _ptr(k), _ptr(v),
+                         _ptr(info), _stream(stream)), "kq_kv_read")
+
+
+def kq_kv_attend_workspace(q, cache, table, acc=None) -> int:
+    """Bytes of kq_kv_attend's workspace for these tensors."""
+    return int(lib().kq_kv_attend_workspace(q.shape[0], q.shape[1], cache.shape[1], q.shape[2],
+                                            0 if acc is None else acc.shape[-1]))
+
+
+def kq_kv_attend(q, start, lens, cache, table, out, ws, scale: float, lse=None, acc=None, info=None, stream=None) -> None:
+    """out [T, q_heads, dim] = attention of q over the cached slots of each token's sequence (the
+    tokens' own keys are its last slots; token i sees what was cached up to itself). lse [T, q_heads]:
+    the log-sums. acc [batch, kv_heads, S] += each slot's weight summed over heads and tokens."""
+    dtype = _dtype(q, "q")
+    _rows3(q, "q")
+    T, heads, dim = q.shape
+    c = _cache(cache, table, dim)
+    _need(out, "out", q.dtype, (T, heads, dim))
+    _need(lse, "lse", torch.float32, (T, heads))
+    _need(start, "start", torch.int32, (c.batch + 1,))
+    _need(lens, "lens", torch.int32, (c.batch,))
+    S = 0
+    if acc is not None:
+        S = acc.shape[-1]
+        _need(acc, "acc", torch.float32, (c.batch, c.kv_heads, S))
+    _need(ws, "ws", torch.uint8)
+    _need(info, "info", torch.int32)
+    _ok(lib().kq_kv_attend(ctypes.byref(c), _ptr(q), dtype, T, heads, q.stride(0), q.stride(1), _ptr(start), _ptr(lens),
+                           float(scale), _ptr(out), _ptr(lse), _ptr(acc), S, _ptr(info), _ptr(ws),
+                           0 if ws is None else ws.numel(), _stream(stream)), "kq_kv_attend")
+
+
+def kq_kv_evict_workspace(acc, budget: int) -> int:
+    """Bytes of kq_kv_evict's workspace for weights acc [batch, kv_heads, S]."""
+    return int(lib().kq_kv_evict_workspace(acc.shape[0], acc.shape[1], acc.shape[2], int(budget)))
+
+
+def kq_kv_evict(cache, table, lens, acc, pos, seen, dim: int, budget: int, recent: int, sink: int, lens_out, acc_out,
+                pos_out, ws, info=None, stream=None) -> None:
+    """Cuts each sequence and head back to `budget` slots: the last `recent` and first `sink`
+    positions and the slots of the largest acc stay; kept slots beyond the budget move into the
+    freed ones. acc_out, pos_out may be acc, pos; lens_out = min(lens, budget) may not be lens."""
+    c = _cache(cache, table, dim)
+    S = acc.shape[-1]
+    shape = (c.batch, c.kv_heads, S)
+    for t, name, ty in ((acc, "acc", torch.float32), (pos, "pos", torch.int32), (acc_out, "acc_out", torch.float32),
+                        (pos_out, "pos_out", torch.int32)):
+        _need(t, name, ty, shape)
+    for t, name in ((lens, "lens"), (seen, "seen"), (lens_out, "lens_out")):
+        _need(t, name, torch.int32, (c.batch,))
+    _need(ws, "ws", torch.uint8)
+    _need(info, "info", torch.int32)
+    _ok(lib().kq_kv_evict(ctypes.byref(c), _ptr(lens), _ptr(acc), _ptr(pos), _ptr(seen), S, int(budget), int(recent),
+                          int(sink), _ptr(lens_out), _ptr(acc_out), _ptr(pos_out), _ptr(info), _ptr(ws),
+                          0 if ws is None else ws.numel(), _stream(stream)), "kq_kv_evict")
+
+
+def _logits(t, name):
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1 and t.numel()):
+        raise ValueError(f"{name} must be [T, V] with unit column stride")
+    return _dtype(t, name)
+
+
+def _row_stride(t):
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def kq_token_logprobs(logits, target, logp, entropy=None, lse=None, top_id=None, top_logp=None, info=None,
+                      stream=None) -> None:
+    """logp [T] of the target tokens [T] int64 (negative: not scored), with the entropy and log-sum
+    of each row of logits [T, V] (bf16 or fp32) and its top_id.shape[1] most likely tokens."""
+    dtype = _logits(logits, "logits")
+    T, V = logits.shape
+    top = 0 if top_id is None else top_id.shape[-1]
+    _need(target, "target", torch.int64, (T,))
+    for t, name in ((logp, "logp"), (entropy, "entropy"), (lse, "lse")):
+        _need(t, name, torch.float32, (T,))
+    _need(top_id, "top_id", torch.int32, (T, top))
+    if (top_id is None) != (top_logp is None):
+        raise ValueError("top_id and top_logp go together")
+    _need(top_logp, "top_logp", torch.float32, (T, top))
+    _need(info, "info", torch.int32)
+    _ok(lib().kq_token_logprobs(_ptr(logits), dtype, T, V, _row_stride(logits), _ptr(target), top, _ptr(logp),
+                                _ptr(entropy), _ptr(lse), _ptr(top_id), _ptr(top_logp), _ptr(info), _stream(stream)),
+        "kq_token_logprobs")
+
+
+def kq_token_logprobs_grad(logits, target, lse, g_logp, grad, entropy=None, g_entropy=None, info=None,
+                           stream=None) -> None:
+    """grad [T, V] = the gradient of sum(g_logp * logp + g_entropy * entropy) with respect to logits;
+    lse and entropy from kq_token_logprobs. grad may be logits."""
+    dtype = _logits(logits, "logits")
+    T, V = logits.shape
+    if _logits(grad, "grad") != dtype or grad.shape != logits.shape:
+        raise ValueError("grad must have the shape and type of logits")
+    _need(target, "target", torch.int64, (T,))
+    for t, name in ((lse, "lse"), (g_logp, "g_logp"), (entropy, "entropy"), (g_entropy, "g_entropy")):
+        _need(t, name, torch.float32, (T,))
+    _need(info, "info", torch.int32)
+    _ok(lib().kq_token_logprobs_grad(_ptr(logits), dtype, T, V, _row_stride(logits), _ptr(target), _ptr(lse),
+                                     _ptr(entropy), _ptr(g_logp), _ptr(g_entropy), _ptr(grad), _row_stride(grad),
+                                     _ptr(info), _stream(stream)), "kq_token_logprobs_grad")
 
 
 def kq_dequant_revert(codes, scale, zero, group: int, s_x, s_g, sign_u, sign_v, W_hat, stream=None):
