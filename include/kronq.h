@@ -426,7 +426,7 @@ KQ_API kq_status kq_infer(const uint32_t* packed, const float* scale, const int3
  *   2 j in the low half of byte j), the same of value codes, 16 (scale, offset) bf16 pairs
  *   of the keys and 16 of the values. table [batch][table_ld] int32: the page of slots
  *   p * page .. of a sequence. dim is 64 or 128, page a multiple of 16 up to 1024, kv_heads and
- *   batch up to 65535, table_ld * page < 2^31. Two sequences may share pages that neither
+ *   batch up to 65535 (their product up to 2^24), table_ld * page < 2^31. Two sequences may share pages that neither
  *   writes. The structure itself is read on the host during the call.
  *
  * Tokens of several sequences are packed: token i belongs to the sequence b with

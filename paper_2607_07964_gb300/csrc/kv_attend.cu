@@ -1,103 +1,741 @@
-// kq_kv_attend: attention over the 4-bit cache. One block for a token and query head: tiles of
-// 128 slots, a thread a slot for the scores, a thread a dimension for the sum of values, with the
-// running maximum and sum of an online softmax. The weights of the slots come from the stored
-// scores and the finished log-sum in a second kernel.
+// kq_kv_attend: attention of a few query rows over the 4-bit cache, one pass over the cached bytes.
+//
+// Mathematics. With a key k_j = s_j c_j + o_j (codes c in 0 .. 15) the score is
+//     <q, k_j> = s_j <q, c_j> + o_j sum(q),
+// so the tensor cores multiply q with the codes themselves and the grid enters as two numbers a
+// row. The values likewise: sum_j p_j v_j = sum_j (p_j s'_j) c'_j + sum_j p_j o'_j. A nibble masked
+// out of a word in place is the fp16 subnormal c 2^-24 (or 16 c 2^-24 four bits up), which
+// mma.sync multiplies exactly, so a code costs about half an integer instruction and no conversion.
+//   * q is scaled by a power of two into fp16: exact for bf16; fp32 is split into two fp16 halves
+//     (22 bits), as are the weights p s' when the output is fp32. All sums are fp32.
+//   * Codes enter about their middle, c - 8, so that the sums stay of the size of what they sum to: with
+//     codes all positive the tensor cores' truncation adds up in one direction. For bf16 outputs the
+//     scores' accumulators start at -8 sum(q) and the values' take -8 times the weights' sum (one more
+//     product, with a constant) along with the rescaling that a new maximum needs. fp32 outputs
+//     make c - 8 itself (two more instructions for four codes), and round each tile's sum into the running one: 1e-6
+//     of the output instead of 1e-4 over 2600 slots.
+//   * p_j s'_j is scaled by a power of two that follows the largest s' seen, up to 2^14: fp16 then
+//     holds it to 11 bits over 28 binades below the largest, whatever the values' range.
+//
+// What bounds it: the cache is read once, D + 8 bytes for each token and head; with D = 128 that
+// leaves an SM 5.8 cycles a token at 6.8 TB/s, against ~3 issue slots and 1 to 2 tensor cycles, so
+// the kernel is laid out to keep bulk copies in flight. A row of 16-byte units per token lets each
+// lane take its operands straight from the staged bytes in the mma layout (a lane's 16 bytes of a
+// key row are its share of every k step; the order of the dimensions inside a product is free).
+//
+// Split. The work is the list of 64-token tiles of every (sequence, head, group of query rows), and
+// each CTA takes an equal, contiguous part of it, so ragged lengths, few sequences and long ones
+// all fill the GPU evenly, without the host knowing the lengths. A CTA that covers a whole
+// (sequence, head) writes its output, parts of one are joined by kv_combine_kernel from at most two
+// partial results a CTA. One producer warp streams tiles through a ring of bulk copies; four
+// consumer warps take 16 tokens of a tile each, with their own running maximum and sums, joined at
+// the end of a segment. Accumulated weights need the finished log-sum, so the scores are kept
+// (they mostly stay in L2) and kv_weight_kernel turns them into weights.
 #include <algorithm>
+#include <atomic>
 
 #include "kv_common.cuh"
 
 namespace kq {
 namespace {
 
-constexpr int kTile = 128;
+constexpr int kTile = 64;                        // tokens of a tile
+constexpr int kWarps = kTile / kGranule;         // consumer warps, a granule each
+constexpr int kThreads = 32 * (kWarps + 1);      // and the producer
+constexpr int kMaxCtas = 640;                    // the workspace holds two partial results of each
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
-__device__ __forceinline__ int64_t visible(const int32_t* start, int b, int64_t i, int64_t n) {
-    const int64_t m = n - (start[b + 1] - 1 - i);
-    return m < 0 ? 0 : m;
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                        uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    uint32_t y;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(hi), "f"(lo));
+    return y;
+}
+__device__ __forceinline__ float2 unpack_f16(uint32_t x) { return __half22float2(*reinterpret_cast<const __half2*>(&x)); }
+// Two codes of a word, nibbles 0 and 4 of x (ODD: 1 and 5), as the A operand. Plain: the masked
+// bits, subnormals c 2^-24 (ODD: 16 c 2^-24). CENTRED: c - 8, through 1024 + c (ODD: 1024 + 16 c, over 16).
+template <bool CENTRED, bool ODD>
+__device__ __forceinline__ uint32_t codes(uint32_t x) {
+    constexpr uint32_t mask = ODD ? 0x00F000F0u : 0x000F000Fu;
+    if constexpr (!CENTRED) return x & mask;
+    uint32_t y = (x & mask) | 0x64006400u;
+    if constexpr (ODD) asm("fma.rn.f16x2 %0, %0, %1, %2;" : "+r"(y) : "r"(0x2C002C00u), "r"(0xD480D480u));   // / 16 - 72
+    else asm("sub.rn.f16x2 %0, %0, %1;" : "+r"(y) : "r"(0x64086408u));                                      // - 1032
+    return y;
+}
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
+                 "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(smem_u32(bar))
+                 : "memory");
+}
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+struct Attend {
+    KvView c;
+    const void* q;
+    int64_t tokens, q_token, q_head;   // strides in elements
+    int32_t q_heads, group;            // query heads in all, and of a key/value head
+    bool q_vec;                        // rows of q can be read 16 bytes at a time
+    const int32_t* start;
+    const int32_t* lens;
+    float scale;
+    void* out;
+    float* lse;                        // [T][q_heads]
+    float* scores;                     // [T][kv_heads][S][group], in units of ln 2, or nullptr
+    int64_t S;
+    int64_t cap;                       // slots a sequence may have: the table's, and S with weights
+    int64_t* base;                     // [batch + 1] first tile of each sequence in the list of work, then the CTAs
+    float* part;                       // [2 CTAs][rows][D + 2]: sums, maximum, sum of weights
+    int* info;
+};
+
+// Sequence b's share of the work.
+struct Seq {
+    int32_t nq, rows_tiles, tiles;   // queries, groups of ROWS query rows, 64-token tiles (at least 1)
+    int32_t n;                       // length
+    int32_t first;                   // its first token
+};
+template <int ROWS>
+__device__ __forceinline__ Seq sequence(const Attend& p, int b, int* info) {
+    Seq s;
+    const int64_t s0 = p.start[b], s1 = p.start[b + 1];
+    s.n = static_cast<int32_t>(kv_length(p.lens, b, p.cap, info));
+    s.first = static_cast<int32_t>(s0);
+    s.nq = static_cast<int32_t>(s1 - s0);
+    if (s0 < 0 || s1 < s0 || s1 > p.tokens) {
+        record_error(info, -KQ_ERR_INVALID_ARG);
+        s.nq = 0;
+    }
+    s.rows_tiles = static_cast<int32_t>((static_cast<int64_t>(s.nq) * p.group + ROWS - 1) / ROWS);
+    s.tiles = max(1, (s.n + kTile - 1) / kTile);
+    return s;
+}
+__device__ __forceinline__ int64_t work_of(const Attend& p, const Seq& s) {
+    return static_cast<int64_t>(s.rows_tiles) * s.tiles * p.c.kv_heads;
+}
+// The slots that query token i (of nq) of a sequence with n slots sees.
+__device__ __forceinline__ int32_t visible(int32_t n, int32_t nq, int32_t i) { return max(0, n - (nq - 1 - i)); }
+// CTA c of C takes tiles W c / C .. W (c + 1) / C - 1 of W; the CTA that takes tile w.
+__device__ __forceinline__ int64_t first_tile(int64_t W, int64_t c, int64_t C) { return W * c / C; }
+__device__ __forceinline__ int64_t cta_of(int64_t W, int64_t w, int64_t C) { return ((w + 1) * C - 1) / W; }
+
+// A position in the list of work: tile `tile` of row group `rt` of head h of sequence b.
+struct Place {
+    int b, h, rt, tile;
+    Seq s;
+};
+template <int ROWS>
+__device__ __forceinline__ void next_sequence(const Attend& p, Place& at) {
+    do {
+        ++at.b;
+        if (at.b >= p.c.batch) return;
+        at.s = sequence<ROWS>(p, at.b, nullptr);
+    } while (at.s.rows_tiles == 0);
+}
+// Past the rest of this row group.
+template <int ROWS>
+__device__ __forceinline__ void next_item(const Attend& p, Place& at) {
+    at.tile = 0;
+    if (++at.rt < at.s.rows_tiles) return;
+    at.rt = 0;
+    if (++at.h < p.c.kv_heads) return;
+    at.h = 0;
+    next_sequence<ROWS>(p, at);
 }
 
-template <typename T, int D>
-__global__ void __launch_bounds__(kTile) kv_attend_kernel(KvView c, const T* __restrict__ q, int64_t tokens, int q_heads,
-                                                          int64_t ts, int64_t hs, const int32_t* __restrict__ start,
-                                                          const int32_t* __restrict__ lens, float scale, T* __restrict__ out,
-                                                          float* __restrict__ lse, float* __restrict__ scores, int64_t S,
-                                                          int* info) {
-    __shared__ float qs[D], p[kTile], red[4];
-    __shared__ const uint8_t* gran[kTile / kGranule];
-    if (blockIdx.x == 0 && threadIdx.x == 0 && (start[0] != 0 || start[c.batch] != tokens)) record_error(info, -KQ_ERR_INVALID_ARG);
-    const int64_t i = blockIdx.x / q_heads;
-    const int hq = static_cast<int>(blockIdx.x % q_heads);
-    const int group = q_heads / c.kv_heads, h = hq / group, tid = threadIdx.x;
-    const int b = kv_sequence_of(start, c.batch, i);
-    if (b < 0) {
-        record_error(info, -KQ_ERR_INVALID_ARG);
+template <int D, int NT>
+struct Shape {
+    static constexpr int kRows = 8 * NT;
+    static constexpr int kGranuleBytes = kGranule * (D + 8);
+    static constexpr int kStageBytes = kWarps * kGranuleBytes;
+    static constexpr int kMergeFloats = kWarps * kRows * D;
+    static constexpr int kStages = D == 128 ? 5 : 8;
+    static constexpr size_t kSmem = kStages * kStageBytes + kMergeFloats * sizeof(float);
+};
+
+template <typename T, int D, int NT>
+__global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) kv_attend_kernel(const Attend p, const int min_tiles) {
+    using Sh = Shape<D, NT>;
+    constexpr int kRows = Sh::kRows, kStages = Sh::kStages;
+    constexpr bool kSplit = sizeof(T) == 4;      // fp32: two fp16 halves of q and of the weights
+    constexpr int kWords = D / 32;               // code words of a row that a lane of a quad takes
+    extern __shared__ __align__(128) uint8_t smem[];
+    float* const merge = reinterpret_cast<float*>(smem + kStages * Sh::kStageBytes);
+    __shared__ uint64_t full[kStages], empty[kStages];
+    __shared__ int abort_flag;
+    __shared__ int64_t scan_tmp[kThreads / 32], found_base;
+    __shared__ int found_b;
+    __shared__ float sm_m[kWarps][kRows], sm_l[kWarps][kRows], sm_o[kWarps][kRows];
+    __shared__ int sm_e[kWarps];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const KvView& c = p.c;
+
+    // ---- this CTA's part of the work
+    if (tid == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(&full[i], 1);
+            mbar_init(&empty[i], kWarps);
+        }
+        abort_flag = 0;
+        found_b = -1;
+        fence_mbar_init();
+        if (blockIdx.x == 0 && (p.start[0] != 0 || p.start[c.batch] != p.tokens)) record_error(p.info, -KQ_ERR_INVALID_ARG);
+    }
+    int64_t W = 0;
+    {
+        int64_t mine = 0;
+        for (int b = tid; b < c.batch; b += kThreads) mine += work_of(p, sequence<kRows>(p, b, blockIdx.x ? nullptr : p.info));
+        for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+        if (lane == 0) scan_tmp[warp] = mine;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kThreads / 32; ++i) W += scan_tmp[i];
+    }
+    const int64_t C = max(static_cast<int64_t>(1), min(static_cast<int64_t>(gridDim.x), (W + min_tiles - 1) / min_tiles));
+    const int64_t w0 = first_tile(W, blockIdx.x, C), w1 = blockIdx.x < C ? first_tile(W, blockIdx.x + 1, C) : w0;
+    if (blockIdx.x != 0 && w0 >= w1) return;
+    int64_t before = 0;
+    for (int b0 = 0; b0 < c.batch; b0 += kThreads) {
+        const int b = b0 + tid;
+        const int64_t v = b < c.batch ? work_of(p, sequence<kRows>(p, b, nullptr)) : 0;
+        int64_t x = v;
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += y;
+        }
+        __syncthreads();
+        if (lane == 31) scan_tmp[warp] = x;
+        __syncthreads();
+        int64_t lead = before, all = before;
+#pragma unroll
+        for (int i = 0; i < kThreads / 32; ++i) {
+            if (i < warp) lead += scan_tmp[i];
+            all += scan_tmp[i];
+        }
+        const int64_t at = lead + x - v;
+        if (b < c.batch && v > 0 && at <= w0 && w0 < at + v) {
+            found_b = b;
+            found_base = at;
+        }
+        if (blockIdx.x == 0 && b < c.batch) p.base[b] = at;
+        before = all;
+    }
+    if (blockIdx.x == 0 && tid == 0) {
+        p.base[c.batch] = W;
+        p.base[c.batch + 1] = C;
+    }
+    __syncthreads();
+    if (w0 >= w1 || found_b < 0) return;   // uniform: an empty list of work
+    pdl_launch_dependents();
+    Place at;
+    at.b = found_b;
+    at.s = sequence<kRows>(p, at.b, nullptr);
+    {
+        const int64_t rem = w0 - found_base, head = static_cast<int64_t>(at.s.rows_tiles) * at.s.tiles;
+        at.h = static_cast<int>(rem / head);
+        at.rt = static_cast<int>(rem % head / at.s.tiles);
+        at.tile = static_cast<int>(rem % at.s.tiles);
+    }
+
+    if (warp == kWarps) {
+        // ---- producer: tiles into the ring; lane l holds the page of the l-th page ahead
+        int it = 0;
+        bool ok = true;
+        int page_b = -1, page_at = 0, page_id = 0;
+        for (int64_t w = w0; w < w1 && ok; ++w, ++it) {
+            const int slot0 = at.tile * kTile, grans = (min(kTile, at.s.n - slot0) + kGranule - 1) / kGranule;
+            const int stage = it % kStages;
+            if (it >= kStages) {
+                ok = lane != 0 || mbar_wait(&empty[stage], ((it / kStages) & 1) ^ 1, &abort_flag);
+                ok = __shfl_sync(0xffffffffu, ok, 0);
+                if (!ok) break;
+            }
+            if (lane == 0) {
+                if (grans > 0) mbar_arrive_expect_tx(&full[stage], grans * Sh::kGranuleBytes);
+                else mbar_arrive(&full[stage]);
+            }
+            for (int g = 0; g < grans;) {
+                const int slot = slot0 + g * kGranule, pg = slot / c.page;
+                if (page_b != at.b || pg < page_at || pg >= page_at + 32) {
+                    page_b = at.b;
+                    page_at = pg;
+                    page_id = 0;
+                    if (pg + lane <= (at.s.n - 1) / c.page) {
+                        page_id = c.table[static_cast<int64_t>(at.b) * c.table_ld + pg + lane];
+                        if (page_id < 0 || page_id >= c.pages) {
+                            record_error(p.info, -KQ_ERR_INVALID_ARG);
+                            page_id = 0;
+                        }
+                    }
+                }
+                const int id = __shfl_sync(0xffffffffu, page_id, pg - page_at);
+                const int in_page = slot - pg * c.page;
+                const int run = min(grans - g, (c.page - in_page) / kGranule);
+                if (lane == 0)
+                    bulk_load(smem + stage * Sh::kStageBytes + g * Sh::kGranuleBytes,
+                              c.data + (static_cast<int64_t>(id) * c.kv_heads + at.h) * kv_head_bytes(c) + in_page * (D + 8),
+                              run * Sh::kGranuleBytes, &full[stage]);
+                g += run;
+            }
+            if (++at.tile == at.s.tiles) next_item<kRows>(p, at);
+        }
+        // a wait gave up somewhere: leave only when this CTA's copies have landed
+        __syncthreads();
+        if (abort_flag && lane == 0) {
+            record_error(p.info, -KQ_ERR_TIMEOUT);
+            int none = 0;
+            for (int i = max(0, it - kStages); i < it; ++i) mbar_wait(&full[i % kStages], (i / kStages) & 1, &none);
+        }
         return;
     }
-    const int64_t cap = scores ? min(kv_capacity(c), S) : kv_capacity(c);
-    const int64_t n = visible(start, b, i, kv_length(lens, b, cap, info));
-    for (int d = tid; d < D; d += kTile) qs[d] = static_cast<float>(q[i * ts + hq * hs + d]) * scale;
-    float m = -INFINITY, z = 0.0f, o = 0.0f;
-    for (int64_t base = 0; base < n; base += kTile) {
-        __syncthreads();
-        if (tid < kTile / kGranule) {
-            const int64_t s0 = base + tid * kGranule;
-            const uint8_t* g = s0 < n ? kv_granule(c, b, h, s0) : c.data;
-            if (!g) record_error(info, -KQ_ERR_INVALID_ARG);
-            gran[tid] = g ? g : c.data;
-        }
-        __syncthreads();
-        float s = -INFINITY;
-        if (base + tid < n) {
-            const uint8_t* g = gran[tid / kGranule];
-            const uint8_t* row = g + kv_code_at(D, 0, tid % kGranule);
-            const uint32_t prm = *reinterpret_cast<const uint32_t*>(g + kv_param_at(D, 0, tid % kGranule));
-            s = 0.0f;
-            for (int d = 0; d < D; ++d)
-                s = fmaf(qs[d], fmaf(kv_scale(prm), static_cast<float>((row[d / 2] >> (4 * (d & 1))) & 15), kv_offset(prm)), s);
-            if (scores) scores[((i * c.kv_heads + h) * S + base + tid) * group + hq % group] = s;
-        }
-        float w = s;
-        for (int off = 16; off > 0; off >>= 1) w = fmaxf(w, __shfl_xor_sync(0xffffffffu, w, off));
-        if (isnan(s)) w = s;
-        if ((tid & 31) == 0) red[tid >> 5] = w;
-        __syncthreads();
-        const float mn = fmaxf(m, fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
-        p[tid] = s == -INFINITY ? 0.0f : expf(s - mn);
-        __syncthreads();
-        const float r = m == -INFINITY ? 0.0f : expf(m - mn);
-        m = mn;
-        z *= r;
-        o *= r;
-        const int many = static_cast<int>(min(static_cast<int64_t>(kTile), n - base));
-        for (int t = 0; t < many; ++t) {
-            z += p[t];
-            if (tid < D) {
-                const uint8_t* g = gran[t / kGranule];
-                const uint32_t prm = *reinterpret_cast<const uint32_t*>(g + kv_param_at(D, 1, t % kGranule));
-                const int code = (g[kv_code_at(D, 1, t % kGranule) + tid / 2] >> (4 * (tid & 1))) & 15;
-                o = fmaf(p[t], fmaf(kv_scale(prm), static_cast<float>(code), kv_offset(prm)), o);
+
+    // ---- consumers
+    const int g8 = lane >> 2, t4 = lane & 3;
+    // the token of A row g8 (and 8 more of row g8 + 8), chosen so that the tokens 2 t4, 2 t4 + 1, 2 t4 + 8 and 2 t4 + 9
+    // of the weights' fragment are rows t4, 7 - t4, 8 + t4, 15 - t4: neighbouring lanes then read
+    // neighbouring rows of codes
+    const int tok = (g8 & 1) ? 7 - (g8 >> 1) : (g8 >> 1);
+    int it = 0;
+    // After a wait that gave up the warps go on through the same steps without waiting (the result is
+    // reported as failed), so that none of them is left alone at a barrier.
+    for (int64_t w = w0; w < w1;) {
+        const int64_t seg = min(w1 - w, static_cast<int64_t>(at.s.tiles - at.tile));
+        const int rows = min(kRows, at.s.nq * p.group - at.rt * kRows);
+        // q: lane (g8, t4) holds dimensions t4 D / 4 .. of row g8, each word of 8 as two k steps: (0, 4 | 1, 5) and
+        // (2, 6 | 3, 7), the odd ones divided by 16 because their nibbles sit four bits up
+        uint32_t bq[NT][kWords][4], bl[NT][kWords][4];
+        float alpha[NT][2], beta[NT][2], zero[NT][2];   // zero: -8 sum(q) in the accumulator's units
+        int32_t lim[NT][2];
+        int64_t put[NT][2];   // where a row's scores go
+        int32_t least = at.s.n;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int r = nt * 8 + g8, row = at.rt * kRows + r;
+            float x[D / 4];
+            if (r < rows) {
+                const T* src = static_cast<const T*>(p.q) + (at.s.first + row / p.group) * p.q_token +
+                               (static_cast<int64_t>(at.h) * p.group + row % p.group) * p.q_head + t4 * (D / 4);
+                if (p.q_vec) {
+#pragma unroll
+                    for (int i = 0; i < static_cast<int>(D / 4 * sizeof(T) / 16); ++i) {
+                        const uint4 u = reinterpret_cast<const uint4*>(src)[i];
+                        const uint32_t v[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            if constexpr (kSplit) {
+                                x[4 * i + j] = __uint_as_float(v[j]);
+                            } else {
+                                x[8 * i + 2 * j] = __uint_as_float(v[j] << 16);
+                                x[8 * i + 2 * j + 1] = __uint_as_float(v[j] & 0xFFFF0000u);
+                            }
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < D / 4; ++i) x[i] = static_cast<float>(src[i]);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < D / 4; ++i) x[i] = 0.0f;
+            }
+            float top = 0.0f, sum = 0.0f;
+            bool fine = true;
+#pragma unroll
+            for (int i = 0; i < D / 4; ++i) {
+                top = fmaxf(top, fabsf(x[i]));
+                sum += x[i];
+                fine &= fabsf(x[i]) <= 3.402823466e38f;
+            }
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+            int bad = !fine;
+            bad |= __shfl_xor_sync(0xffffffffu, bad, 1);
+            bad |= __shfl_xor_sync(0xffffffffu, bad, 2);
+            // 2^e brings the largest below 2^14; both powers stay normal
+            const int e = min(100, max(-113, 13 - static_cast<int>((__float_as_uint(top) >> 23) & 255) + 127));
+            const float up = bad ? 0.0f : __uint_as_float(static_cast<uint32_t>(e + 127) << 23);
+            const float f = p.scale * kLog2e;
+            const float a = bad ? NAN : (kSplit ? f : f * 0x1p24f) * __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+            const float bt = bad ? NAN : f * sum;
+            const float zr = bad ? 0.0f : sum * (up * -0x1p-21f);   // of no use to centred codes
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {   // nibbles j and j + 4
+                    const float s = up * (!kSplit && (j & 1) ? 0.0625f : 1.0f);
+                    const float x0 = bad ? 0.0f : x[8 * i + j] * s, x1 = bad ? 0.0f : x[8 * i + j + 4] * s;
+                    bq[nt][i][j] = pack_f16(x0, x1);
+                    if constexpr (kSplit) {
+                        const float2 h = unpack_f16(bq[nt][i][j]);
+                        bl[nt][i][j] = pack_f16(x0 - h.x, x1 - h.y);
+                    }
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {   // the accumulator's columns 2 t4 + k
+                const int col = nt * 8 + 2 * t4 + k, crow = at.rt * kRows + col;
+                alpha[nt][k] = __shfl_sync(0xffffffffu, a, (2 * t4 + k) * 4);
+                beta[nt][k] = __shfl_sync(0xffffffffu, bt, (2 * t4 + k) * 4);
+                zero[nt][k] = __shfl_sync(0xffffffffu, zr, (2 * t4 + k) * 4);
+                const int i = crow / p.group;
+                lim[nt][k] = col < rows ? visible(at.s.n, at.s.nq, i) : 0;
+                put[nt][k] = ((static_cast<int64_t>(at.s.first + i) * c.kv_heads + at.h) * p.S) * p.group + crow % p.group;
             }
         }
+        float o[NT][D / 16][4], m[NT][2], l[NT][2], off[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[nt][i][j] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) m[nt][k] = -INFINITY, l[nt][k] = 0.0f, off[nt][k] = 0.0f;
+        }
+        least = visible(at.s.n, at.s.nq, at.rt * kRows / p.group);   // what the first row sees, the others see
+        int ev = 20;   // biased exponent of the largest value scale so far
+
+        for (int64_t k = 0; k < seg; ++k, ++it) {
+            const int stage = it % kStages;
+            const bool ok = __all_sync(0xffffffffu, mbar_wait(&full[stage], (it / kStages) & 1, &abort_flag));
+            const int slot = (at.tile + static_cast<int>(k)) * kTile + warp * kGranule;
+            if (ok && slot < at.s.n) {   // uniform over the warp
+                const uint8_t* gr = smem + stage * Sh::kStageBytes + warp * Sh::kGranuleBytes;
+                // scores; fp32: the two halves of the dimensions and the low part of q apart, as the tensor
+                // cores truncate each sum to its own size
+                float s[NT][4], s2[NT][kSplit ? 2 : 1][4];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        s[nt][j] = kSplit ? 0.0f : zero[nt][j & 1];
+                        s2[nt][0][j] = 0.0f;
+                        if constexpr (kSplit) s2[nt][1][j] = 0.0f;
+                    }
+                {
+                    uint32_t ka[kWords], kb[kWords];
+                    if constexpr (D == 128) {
+                        const uint4 u = *reinterpret_cast<const uint4*>(gr + tok * 64 + t4 * 16);
+                        const uint4 v = *reinterpret_cast<const uint4*>(gr + (tok + 8) * 64 + t4 * 16);
+                        ka[0] = u.x, ka[1] = u.y, ka[2] = u.z, ka[3] = u.w;
+                        kb[0] = v.x, kb[1] = v.y, kb[2] = v.z, kb[3] = v.w;
+                    } else {
+                        const uint2 u = *reinterpret_cast<const uint2*>(gr + tok * 32 + t4 * 8);
+                        const uint2 v = *reinterpret_cast<const uint2*>(gr + (tok + 8) * 32 + t4 * 8);
+                        ka[0] = u.x, ka[1] = u.y;
+                        kb[0] = v.x, kb[1] = v.y;
+                    }
+#pragma unroll
+                    for (int i = 0; i < kWords; ++i) {
+#pragma unroll
+                        for (int hf = 0; hf < 2; ++hf) {
+                            const uint32_t x = hf ? ka[i] >> 8 : ka[i], y = hf ? kb[i] >> 8 : kb[i];
+                            const uint32_t a0 = codes<kSplit, false>(x), a1 = codes<kSplit, false>(y);
+                            const uint32_t a2 = codes<kSplit, true>(x), a3 = codes<kSplit, true>(y);
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                if constexpr (kSplit) {
+                                    mma_f16(2 * i < kWords ? s[nt] : s2[nt][0], a0, a1, a2, a3, bq[nt][i][2 * hf],
+                                            bq[nt][i][2 * hf + 1]);
+                                    mma_f16(s2[nt][1], a0, a1, a2, a3, bl[nt][i][2 * hf], bl[nt][i][2 * hf + 1]);
+                                } else {
+                                    mma_f16(s[nt], a0, a1, a2, a3, bq[nt][i][2 * hf], bq[nt][i][2 * hf + 1]);
+                                }
+                            }
+                        }
+                    }
+                }
+                const uint32_t* prm = reinterpret_cast<const uint32_t*>(gr + kGranule * D);
+                const uint32_t kp[2] = {prm[tok], prm[tok + 8]}, vp[2] = {prm[16 + tok], prm[24 + tok]};
+                // the grid about its middle code: x = s (c - 8) + (o + 8 s)
+                const float ks[2] = {kv_scale(kp[0]), kv_scale(kp[1])}, vs[2] = {kv_scale(vp[0]), kv_scale(vp[1])};
+                const float ko[2] = {fmaf(8.0f, ks[0], kv_offset(kp[0])), fmaf(8.0f, ks[1], kv_offset(kp[1]))};
+                const float vo[2] = {fmaf(8.0f, vs[0], kv_offset(vp[0])), fmaf(8.0f, vs[1], kv_offset(vp[1]))};
+                const int at0 = slot + tok, at1 = at0 + 8;
+                // the largest value scale so far, as an exponent (a NaN or a slot past the end has no say)
+                uint32_t big = 0;
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf) {
+                    const uint32_t sb = vp[hf] << 16;
+                    if (sb < 0x7F800000u && (hf ? at1 : at0) < at.s.n) big = max(big, sb);
+                }
+                const int en = max(ev, static_cast<int>(__reduce_max_sync(0xffffffffu, big) >> 23));
+                const float drop = __uint_as_float(static_cast<uint32_t>(max(0, 127 + ev - en)) << 23);
+                ev = en;
+                const float inv = __uint_as_float(static_cast<uint32_t>(267 - en) << 23);   // 2^14 / 2^(en + 1 - 127)
+                const bool all_seen = slot + kGranule <= least;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    float wgt[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {   // j = 2 (row half) + column
+                        const int hf = j >> 1, k2 = j & 1;
+                        if constexpr (kSplit) s[nt][j] += s2[nt][0][j] + s2[nt][1][j];
+                        const float x = fmaf(ks[hf], alpha[nt][k2] * s[nt][j], ko[hf] * beta[nt][k2]);
+                        s[nt][j] = all_seen || (hf ? at1 : at0) < lim[nt][k2] ? x : -INFINITY;
+                    }
+                    if (p.scores) {
+#pragma unroll
+                        for (int hf = 0; hf < 2; ++hf) {
+                            const int64_t sl = hf ? at1 : at0;
+                            if (!(p.group & 1)) {   // two columns are neighbours of one token
+                                if (sl < lim[nt][0])
+                                    *reinterpret_cast<float2*>(p.scores + put[nt][0] + sl * p.group) =
+                                        make_float2(s[nt][2 * hf], s[nt][2 * hf + 1]);
+                            } else {
+                                if (sl < lim[nt][0]) p.scores[put[nt][0] + sl * p.group] = s[nt][2 * hf];
+                                if (sl < lim[nt][1]) p.scores[put[nt][1] + sl * p.group] = s[nt][2 * hf + 1];
+                            }
+                        }
+                    }
+                    float corr[2];
+#pragma unroll
+                    for (int k2 = 0; k2 < 2; ++k2) {
+                        float mx = fmaxf(s[nt][k2], s[nt][2 + k2]);
+#pragma unroll
+                        for (int sh = 4; sh < 32; sh <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, sh));
+                        const float mn = fmaxf(m[nt][k2], mx), ms = mn == -INFINITY ? 0.0f : mn;
+                        corr[k2] = ex2(m[nt][k2] - ms);
+                        m[nt][k2] = mn;
+                        l[nt][k2] *= corr[k2];
+                        off[nt][k2] *= corr[k2];
+                        corr[k2] *= drop;
+#pragma unroll
+                        for (int hf = 0; hf < 2; ++hf) {
+                            const float pr = ex2(s[nt][2 * hf + k2] - ms);
+                            const bool in = all_seen || (hf ? at1 : at0) < lim[nt][k2];
+                            l[nt][k2] += pr;
+                            off[nt][k2] += in ? pr * vo[hf] : 0.0f;
+                            wgt[2 * hf + k2] = in ? pr * (vs[hf] * inv) : 0.0f;
+                        }
+                    }
+                    // weights of 16 tokens by 8 rows into the B fragment: token pairs along a lane
+                    const uint32_t h0 = pack_f16(wgt[0], wgt[1]), h1 = pack_f16(wgt[2], wgt[3]);
+                    uint32_t e0 = 0, e1 = 0;
+                    if constexpr (kSplit) {
+                        const float2 f0 = unpack_f16(h0), f1 = unpack_f16(h1);
+                        e0 = transpose8(pack_f16(wgt[0] - f0.x, wgt[1] - f0.y));
+                        e1 = transpose8(pack_f16(wgt[2] - f1.x, wgt[3] - f1.y));
+                    }
+                    const uint32_t b0 = transpose8(h0), b1 = transpose8(h1);
+                    if constexpr (!kSplit) {
+                        // 8 times the weights' sum, in every row of the accumulator's layout
+                        float mid[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                        mma_f16(mid, 0x00080008u, 0x00080008u, 0x00080008u, 0x00080008u, b0, b1);
+#pragma unroll
+                        for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                o[nt][i][j] = fmaf(o[nt][i][j], corr[j & 1], (j < 2 ? -1.0f : -16.0f) * mid[j & 1]);
+                    }
+                    // values: words of dimensions 16 g8 .. (D = 128) or 8 g8 .. (D = 64) of four tokens
+                    const uint8_t* vr = gr + kGranule * (D / 2) + g8 * (D / 16);
+                    uint32_t v[4][D / 64];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int tk = (i >> 1) * 8 + (i & 1 ? 7 - t4 : t4);
+                        if constexpr (D == 128) {
+                            const uint2 u = *reinterpret_cast<const uint2*>(vr + tk * 64);
+                            v[i][0] = u.x, v[i][1] = u.y;
+                        } else {
+                            v[i][0] = *reinterpret_cast<const uint32_t*>(vr + tk * 32);
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < D / 64; ++j)
+#pragma unroll
+                        for (int qd = 0; qd < 4; ++qd) {   // dimensions 2 qd and 2 qd + 1 of the word
+                            const uint32_t sel = qd < 2 ? 0x5410u : 0x7632u;
+                            uint32_t x = __byte_perm(v[0][j], v[1][j], sel), y = __byte_perm(v[2][j], v[3][j], sel);
+                            if (qd & 1) x >>= 8, y >>= 8;
+                            const uint32_t a0 = codes<kSplit, false>(x), a1 = codes<kSplit, true>(x);
+                            const uint32_t a2 = codes<kSplit, false>(y), a3 = codes<kSplit, true>(y);
+                            if constexpr (kSplit) {   // a tile's sum by itself, then rounded into the running one
+                                float u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                                mma_f16(u, a0, a1, a2, a3, e0, e1);
+                                mma_f16(u, a0, a1, a2, a3, b0, b1);
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) o[nt][4 * j + qd][r] = fmaf(o[nt][4 * j + qd][r], corr[r & 1], u[r]);
+                            } else {
+                                mma_f16(o[nt][4 * j + qd], a0, a1, a2, a3, b0, b1);
+                            }
+                        }
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&empty[stage]);
+        }
+
+        // ---- join the warps' sums
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int k2 = 0; k2 < 2; ++k2) {
+#pragma unroll
+                for (int sh = 4; sh < 32; sh <<= 1) {
+                    l[nt][k2] += __shfl_xor_sync(0xffffffffu, l[nt][k2], sh);
+                    off[nt][k2] += __shfl_xor_sync(0xffffffffu, off[nt][k2], sh);
+                }
+                const int col = nt * 8 + 2 * t4 + k2;
+                if (g8 == 0) {
+                    sm_m[warp][col] = m[nt][k2];
+                    sm_l[warp][col] = l[nt][k2];
+                    sm_o[warp][col] = off[nt][k2];
+                }
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i)
+                    *reinterpret_cast<float2*>(merge + (warp * kRows + col) * D + g8 * (D / 8) + 2 * i) =
+                        make_float2(o[nt][i][k2], o[nt][i][2 + k2] * (kSplit ? 1.0f : 0.0625f));
+            }
+        if (lane == 0) sm_e[warp] = ev - (kSplit ? 140 : 116);   // 2^24 of subnormal codes, 2^-14 2^(ev + 1 - 127) of the weights
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        const bool whole = seg == at.s.tiles;
+        float* part = p.part + (2 * static_cast<int64_t>(blockIdx.x) + (at.tile == 0 && w > w0 ? 1 : 0)) * (kRows * (D + 2));
+        for (int col = tid / D; col < rows; col += 128 / D) {
+            const int d = tid % D;
+            float M = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < kWarps; ++i) M = fmaxf(M, sm_m[i][col]);
+            const float ms = M == -INFINITY ? 0.0f : M;
+            float L = 0.0f, O = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kWarps; ++i) {
+                const float f = ex2(sm_m[i][col] - ms);
+                L = fmaf(f, sm_l[i][col], L);
+                O = fmaf(f, ldexpf(merge[(i * kRows + col) * D + d], sm_e[i]) + sm_o[i][col], O);
+            }
+            if (whole) {
+                const int row = at.rt * kRows + col;
+                const int64_t r = (static_cast<int64_t>(at.s.first) + row / p.group) * p.q_heads + at.h * p.group + row % p.group;
+                static_cast<T*>(p.out)[r * D + d] = static_cast<T>(L == 0.0f ? 0.0f : O / L);
+                if (d == 0 && p.lse) p.lse[r] = L == 0.0f ? -INFINITY : (ms + log2f(L)) * kLn2;
+            } else {
+                part[col * D + d] = O;
+                if (d == 0) {
+                    part[kRows * D + col] = M;
+                    part[kRows * (D + 1) + col] = L;
+                }
+            }
+        }
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        w += seg;
+        at.tile += static_cast<int>(seg) - 1;
+        if (++at.tile == at.s.tiles) next_item<kRows>(p, at);
     }
-    if (tid < D) out[(i * q_heads + hq) * D + tid] = static_cast<T>(n > 0 ? o / z : 0.0f);
-    if (tid == 0 && lse) lse[i * q_heads + hq] = n > 0 ? m + logf(z) : -INFINITY;
+    __syncthreads();
 }
 
-__global__ void kv_weight_kernel(KvView c, int q_heads, const int32_t* __restrict__ start, const int32_t* __restrict__ lens,
-                                 const float* __restrict__ scores, const float* __restrict__ lse, float* __restrict__ acc,
-                                 int64_t S) {
-    const int b = blockIdx.y / c.kv_heads, h = blockIdx.y % c.kv_heads, group = q_heads / c.kv_heads;
-    const int64_t slot = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
-    const int64_t n = kv_length(lens, b, min(kv_capacity(c), S), nullptr);
-    if (slot >= n) return;
-    float sum = 0.0f;
-    for (int64_t i = start[b]; i < start[b + 1]; ++i) {
-        if (slot >= visible(start, b, i, n)) continue;
-        for (int g = 0; g < group; ++g)
-            sum += expf(scores[((i * c.kv_heads + h) * S + slot) * group + g] - lse[i * q_heads + h * group + g]);
+// Joins the partial results of rows that more than one CTA worked on. One block for a token and
+// key/value head, a thread for each dimension.
+template <typename T, int D, int NT>
+__global__ void __launch_bounds__(D) kv_combine_kernel(const Attend p) {
+    constexpr int kRows = 8 * NT;
+    pdl_wait();
+    pdl_launch_dependents();
+    const int64_t i = blockIdx.x / p.c.kv_heads;
+    const int h = static_cast<int>(blockIdx.x % p.c.kv_heads), d = threadIdx.x;
+    const int b = kv_sequence_of(p.start, p.c.batch, i);
+    if (b < 0) return;
+    const Seq s = sequence<kRows>(p, b, nullptr);
+    if (s.nq == 0) return;
+    const int64_t W = p.base[p.c.batch], C = p.base[p.c.batch + 1];
+    for (int g = 0; g < p.group; ++g) {
+        const int64_t row = (i - s.first) * p.group + g;
+        const int64_t a = p.base[b] + (static_cast<int64_t>(h) * s.rows_tiles + row / kRows) * s.tiles;
+        const int64_t c0 = cta_of(W, a, C), c1 = cta_of(W, a + s.tiles - 1, C);
+        if (c0 == c1) continue;
+        const int col = static_cast<int>(row % kRows);
+        const float* first = p.part + (2 * c0 + (a > first_tile(W, c0, C) ? 1 : 0)) * (kRows * (D + 2));
+        const float* rest = p.part + 2 * (c0 + 1) * (kRows * (D + 2));   // later CTAs begin with this item
+        const int64_t step = 2 * (kRows * (D + 2));
+        float M = first[kRows * D + col];
+        for (int64_t k = 0; k < c1 - c0; ++k) M = fmaxf(M, rest[k * step + kRows * D + col]);
+        const float ms = M == -INFINITY ? 0.0f : M;
+        float f = ex2(first[kRows * D + col] - ms);
+        float L = f * first[kRows * (D + 1) + col], O = f * first[col * D + d];
+#pragma unroll 4
+        for (int64_t k = 0; k < c1 - c0; ++k) {
+            f = ex2(rest[k * step + kRows * D + col] - ms);
+            L = fmaf(f, rest[k * step + kRows * (D + 1) + col], L);
+            O = fmaf(f, rest[k * step + col * D + d], O);
+        }
+        const int64_t r = i * p.q_heads + h * p.group + g;
+        static_cast<T*>(p.out)[r * D + d] = static_cast<T>(L == 0.0f ? 0.0f : O / L);
+        if (d == 0 && p.lse) p.lse[r] = L == 0.0f ? -INFINITY : (ms + log2f(L)) * kLn2;
     }
-    acc[(static_cast<int64_t>(b) * c.kv_heads + h) * S + slot] += sum;
 }
+
+// acc += the weights of the slots: a thread a slot, the rows of its sequence and head in order.
+__global__ void __launch_bounds__(256) kv_weight_kernel(const Attend p, float* __restrict__ acc) {
+    pdl_wait();
+    const int b = blockIdx.x / p.c.kv_heads, h = blockIdx.x % p.c.kv_heads;
+    const Seq s = sequence<8>(p, b, nullptr);
+    if (s.nq == 0) return;
+    for (int slot = blockIdx.y * 256 + threadIdx.x; slot < s.n; slot += gridDim.y * 256) {
+        float sum = 0.0f;
+        for (int i = 0; i < s.nq; ++i) {
+            if (slot >= visible(s.n, s.nq, i)) continue;
+            const int64_t tk = s.first + i;
+            const float* sc = p.scores + ((tk * p.c.kv_heads + h) * p.S + slot) * p.group;
+            const float* ls = p.lse + tk * p.q_heads + h * p.group;
+            for (int g = 0; g < p.group; ++g) sum += ex2(sc[g] - ls[g] * kLog2e);
+        }
+        acc[(static_cast<int64_t>(b) * p.c.kv_heads + h) * p.S + slot] += sum;
+    }
+}
+
+template <typename... Params, typename... Args>
+cudaError_t launch_after(void (*kern)(Params...), dim3 grid, dim3 block, cudaStream_t st, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kern, static_cast<Params>(args)...);
+}
+
+template <typename T, int D, int NT>
+kq_status run_attend(const Attend& p, cudaStream_t stream) {
+    using Sh = Shape<D, NT>;
+    static std::atomic<uint64_t> done{0};
+    KQ_TRY(once_per_device(done, [] {
+        KQ_CUDA(cudaFuncSetAttribute(kv_attend_kernel<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     static_cast<int>(Sh::kSmem)));
+        return KQ_OK;
+    }));
+    const int grid = std::min(kMaxCtas, num_sms() * (NT == 1 ? 3 : 2));
+    kv_attend_kernel<T, D, NT><<<grid, kThreads, Sh::kSmem, stream>>>(p, 2);
+    KQ_LAUNCH_CHECK("kv_attend_kernel");
+    KQ_CUDA(launch_after(kv_combine_kernel<T, D, NT>, dim3(static_cast<unsigned>(p.tokens * p.c.kv_heads)), dim3(D), stream, p));
+    count_launch();
+    return KQ_OK;
+}
+
+size_t al256(size_t b) { return (b + 255) & ~static_cast<size_t>(255); }
+constexpr size_t kBaseBytes = (65536 + 2) * sizeof(int64_t);
+size_t part_bytes(int64_t dim) { return al256(2ull * kMaxCtas * 16 * (dim + 2) * sizeof(float)); }
 
 }  // namespace
 
@@ -108,7 +746,8 @@ using namespace kq;
 
 extern "C" size_t kq_kv_attend_workspace(int64_t T, int64_t q_heads, int64_t kv_heads, int64_t dim, int64_t S) {
     if (T < 1 || q_heads < 1 || kv_heads < 1 || q_heads % kv_heads || dim < 1 || S < 0) return 0;
-    return S ? static_cast<size_t>(T) * q_heads * (S + 64) * sizeof(float) : 0;
+    return al256(kBaseBytes) + part_bytes(dim) + al256(static_cast<size_t>(T) * q_heads * sizeof(float)) +
+           static_cast<size_t>(T) * q_heads * S * sizeof(float);
 }
 
 extern "C" kq_status kq_kv_attend(const kq_kv_cache* cache, const void* q, int dtype, int64_t T, int64_t q_heads,
@@ -122,37 +761,59 @@ extern "C" kq_status kq_kv_attend(const kq_kv_cache* cache, const void* q, int d
         return KQ_ERR_UNSUPPORTED;
     }
     const uintptr_t es = dtype == KQ_BF16 ? 2 : 4;
-    if (T < 0 || T > 0x7fffffffll || q_heads < 1 || q_heads % c.kv_heads || !start || !lens || (T > 0 && (!q || !out)) ||
-        (acc && S < 1) || !(scale - scale == 0.0f) ||
+    if (T < 0 || T > 0x7fffffffll || q_heads < 1 || q_heads > 0x7fffffffll || q_heads % c.kv_heads || !start || !lens ||
+        (T > 0 && (!q || !out)) || (acc && S < 1) || S > 0x7fffffffll || !(scale - scale == 0.0f) ||
+        T * q_heads > 0x7fffffffll ||
         ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & (es - 1))) {
-        set_error("kq_kv_attend: q, out, start, lens must not be NULL, q_heads a multiple of kv_heads, scale finite, "
-                  "S >= 1 with acc");
+        set_error("kq_kv_attend: q, out, start, lens must not be NULL, q_heads a multiple of kv_heads, T q_heads < 2^31, "
+                  "scale finite, S >= 1 with acc");
         return KQ_ERR_INVALID_ARG;
     }
     if (T == 0) return KQ_OK;
     const size_t need = kq_kv_attend_workspace(T, q_heads, c.kv_heads, c.dim, acc ? S : 0);
-    if (need && (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 255u))) {
+    if (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 255u)) {
         set_error("kq_kv_attend: workspace must be 256-byte aligned and hold %zu bytes", need);
         return KQ_ERR_WORKSPACE;
     }
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
-    float* scores = acc ? static_cast<float*>(ws) : nullptr;
-    float* sums = lse;
-    if (acc && !lse) sums = scores + static_cast<size_t>(T) * q_heads * S;
-    const unsigned grid = static_cast<unsigned>(T * q_heads);
-#define KQ_ATTEND(TY, DIM)                                                                                         \
-    kv_attend_kernel<TY, DIM><<<grid, kTile, 0, stream>>>(c, static_cast<const TY*>(q), T, static_cast<int>(q_heads), \
-                                                          q_token_stride, q_head_stride, start, lens, scale,       \
-                                                          static_cast<TY*>(out), sums, scores, S, info)
-    if (dtype == KQ_BF16) c.dim == 128 ? KQ_ATTEND(__nv_bfloat16, 128) : KQ_ATTEND(__nv_bfloat16, 64);
-    else c.dim == 128 ? KQ_ATTEND(float, 128) : KQ_ATTEND(float, 64);
-#undef KQ_ATTEND
-    KQ_LAUNCH_CHECK("kv_attend_kernel");
+    uint8_t* w = static_cast<uint8_t*>(ws);
+    Attend p;
+    p.c = c;
+    p.q = q;
+    p.tokens = T;
+    p.q_token = q_token_stride;
+    p.q_head = q_head_stride;
+    p.q_heads = static_cast<int32_t>(q_heads);
+    p.group = static_cast<int32_t>(q_heads / c.kv_heads);
+    p.q_vec = !(reinterpret_cast<uintptr_t>(q) & 15u) && !((q_token_stride * es) & 15u) && !((q_head_stride * es) & 15u);
+    p.start = start;
+    p.lens = lens;
+    p.scale = scale;
+    p.out = out;
+    p.base = reinterpret_cast<int64_t*>(w);
+    p.part = reinterpret_cast<float*>(w + al256(kBaseBytes));
+    float* sums = reinterpret_cast<float*>(w + al256(kBaseBytes) + part_bytes(c.dim));
+    p.lse = lse ? lse : acc ? sums : nullptr;
+    p.scores = acc ? sums + al256(static_cast<size_t>(T) * q_heads * sizeof(float)) / sizeof(float) : nullptr;
+    p.S = S;
+    p.cap = acc ? std::min(S, kv_capacity(c)) : kv_capacity(c);
+    p.info = info;
+    // Up to 8 rows of a key/value head fill one accumulator tile; more take two, so that the cache is
+    // read half as often (a tensor-core column costs the same whether a row fills it or not).
+    const bool wide = p.group > 8 || T > c.batch;
+    kq_status st;
+    if (dtype == KQ_BF16)
+        st = c.dim == 128 ? (wide ? run_attend<__nv_bfloat16, 128, 2>(p, stream) : run_attend<__nv_bfloat16, 128, 1>(p, stream))
+                          : (wide ? run_attend<__nv_bfloat16, 64, 2>(p, stream) : run_attend<__nv_bfloat16, 64, 1>(p, stream));
+    else
+        st = c.dim == 128 ? (wide ? run_attend<float, 128, 2>(p, stream) : run_attend<float, 128, 1>(p, stream))
+                          : (wide ? run_attend<float, 64, 2>(p, stream) : run_attend<float, 64, 1>(p, stream));
+    KQ_TRY(st);
     if (acc) {
-        const dim3 wg(static_cast<unsigned>(cdiv(std::min<int64_t>(S, kv_capacity(c)), 256)),
-                      static_cast<unsigned>(c.batch * c.kv_heads));
-        kv_weight_kernel<<<wg, 256, 0, stream>>>(c, static_cast<int>(q_heads), start, lens, scores, sums, acc, S);
-        KQ_LAUNCH_CHECK("kv_weight_kernel");
+        const dim3 wg(static_cast<unsigned>(c.batch * c.kv_heads),
+                      static_cast<unsigned>(std::min<int64_t>(cdiv(p.cap, 256), 65535)));
+        KQ_CUDA(launch_after(kv_weight_kernel, wg, dim3(256), stream, p, acc));
+        count_launch();
     }
     return KQ_OK;
 }

@@ -26,7 +26,8 @@ kq_status kv_view(const kq_kv_cache* c, const char* who, KvView* v) {
         return KQ_ERR_UNSUPPORTED;
     }
     if (c->page < kGranule || c->page > 1024 || c->page % kGranule || c->pages < 1 || c->pages > 0x7fffffffll ||
-        c->kv_heads < 1 || c->kv_heads > 65535 || c->batch < 1 || c->batch > 65535 || c->table_ld < 1 ||
+        c->kv_heads < 1 || c->kv_heads > 65535 || c->batch < 1 || c->batch > 65535 || c->batch * c->kv_heads > (1 << 24) ||
+        c->table_ld < 1 || c->table_ld > 0x7fffffffll ||
         c->table_ld * c->page > 0x7fffffffll - 1024 || (reinterpret_cast<uintptr_t>(c->data) & 15u)) {
         set_error("%s: page must be a multiple of 16 up to 1024, pages, kv_heads, batch and table_ld in range, data "
                   "16-byte aligned", who);

@@ -404,7 +404,7 @@ def test_attend_records_bad_lengths_pages_and_tokens():
     dc, dt = _to_dev(cache)
     q = torch.randn(2, 2, 64, device=DEV)
     out, info = torch.zeros_like(q), _i32([0])
-    ws = torch.empty(1 << 20, dtype=torch.uint8, device=DEV)
+    ws = torch.empty(K().kq_kv_attend_workspace(q, dc, dt, torch.empty(2, 1, 32)), dtype=torch.uint8, device=DEV)
 
     def status(start, lens, table, acc=None):
         K().kq_kv_attend(q, _i32(start), _i32(lens), dc, table, out, ws, 0.1, acc=acc, info=info)
