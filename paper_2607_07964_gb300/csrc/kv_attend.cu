@@ -23,12 +23,12 @@
 // lane take its operands straight from the staged bytes in the mma layout (a lane's 16 bytes of a
 // key row are its share of every k step; the order of the dimensions inside a product is free).
 //
-// Split. The work is the list of 64-token tiles of every (sequence, head, group of query rows), and
+// Split. The work is the list of 128-token tiles of every (sequence, head, group of query rows), and
 // each CTA takes an equal, contiguous part of it, so ragged lengths, few sequences and long ones
 // all fill the GPU evenly, without the host knowing the lengths. A CTA that covers a whole
 // (sequence, head) writes its output, parts of one are joined by kv_combine_kernel from at most two
 // partial results a CTA. One producer warp streams tiles through a ring of bulk copies; four
-// consumer warps take 16 tokens of a tile each, with their own running maximum and sums, joined at
+// consumer warps take 32 tokens of a tile each, with their own running maximum and sums, joined at
 // the end of a segment. Accumulated weights need the finished log-sum, so the scores are kept
 // (they mostly stay in L2) and kv_weight_kernel turns them into weights.
 #include <algorithm>
@@ -39,10 +39,11 @@
 namespace kq {
 namespace {
 
-constexpr int kTile = 64;                        // tokens of a tile
-constexpr int kWarps = kTile / kGranule;         // consumer warps, a granule each
+constexpr int kWarps = 4;                        // consumer warps
+constexpr int kTile = kWarps * 2 * kGranule;     // tokens of a tile: two granules to a warp
 constexpr int kThreads = 32 * (kWarps + 1);      // and the producer
 constexpr int kMaxCtas = 640;                    // the workspace holds two partial results of each
+constexpr float kSlack = 8.0f;                   // how far, in powers of two, a weight may pass 1
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 __device__ __forceinline__ float ex2(float x) {
@@ -86,6 +87,31 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
+// 8 consecutive values; vec: they can be read 16 bytes at a time.
+__device__ __forceinline__ void load8(const float* p, bool vec, float (&x)[8]) {
+    if (vec) {
+        const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = p[i];
+    }
+}
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, bool vec, float (&x)[8]) {
+    if (vec) {
+        const uint4 u = *reinterpret_cast<const uint4*>(p);
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __bfloat162float(p[i]);
+    }
+}
+
 struct Attend {
     KvView c;
     const void* q;
@@ -107,7 +133,7 @@ struct Attend {
 
 // Sequence b's share of the work.
 struct Seq {
-    int32_t nq, rows_tiles, tiles;   // queries, groups of ROWS query rows, 64-token tiles (at least 1)
+    int32_t nq, rows_tiles, tiles;   // queries, groups of ROWS query rows, tiles (at least 1)
     int32_t n;                       // length
     int32_t first;                   // its first token
 };
@@ -163,18 +189,251 @@ template <int D, int NT>
 struct Shape {
     static constexpr int kRows = 8 * NT;
     static constexpr int kGranuleBytes = kGranule * (D + 8);
-    static constexpr int kStageBytes = kWarps * kGranuleBytes;
+    static constexpr int kStageBytes = kTile / kGranule * kGranuleBytes;
     static constexpr int kMergeFloats = kWarps * kRows * D;
-    static constexpr int kStages = D == 128 ? 5 : 8;
+    static constexpr int kStages = D == 128 ? 3 : 5;
     static constexpr size_t kSmem = kStages * kStageBytes + kMergeFloats * sizeof(float);
+};
+
+// A consumer warp's state for a group of NT x 8 query rows. A lane (g8, t4) has columns 2 t4 and
+// 2 t4 + 1 of each 8 rows.
+template <typename T, int D, int NT>
+struct Rows {
+    static constexpr bool kSplit = sizeof(T) == 4;   // fp32: two fp16 halves of q and of the weights
+    static constexpr int kWords = D / 32;            // code words of a row that a lane of a quad takes
+    uint32_t bq[NT][kWords][4], bl[NT][kSplit ? kWords : 1][4];   // q, and what fp16 left of it
+    float alpha[NT][2], gamma[NT][2];                // score = alpha (s S + o gamma), S from the tensor cores
+    int32_t lim[NT][2];                              // slots seen
+    int64_t put[NT][2];                              // where scores go
+    float o[NT][D / 16][4], m[NT][2], l[NT][2], off[NT][2];
+    int ev;                                          // biased exponent that the value scales are held to
+
+    // Two granules: 32 tokens from slot `slot`, staged at gr. MASK: some slot may be unseen by some row.
+    template <bool MASK>
+    __device__ __forceinline__ void step(const uint8_t* gr, int slot, int n, int g8, int t4, float* scores, int group) {
+        // the token of A row g8 (and 8 more of row g8 + 8), chosen so that the tokens 2 t4, 2 t4 + 1, 2 t4 + 8 and
+        // 2 t4 + 9 of the weights' fragment are rows t4, 7 - t4, 8 + t4, 15 - t4: neighbouring lanes
+        // then read neighbouring rows of codes
+        const int tok = (g8 & 1) ? 7 - (g8 >> 1) : (g8 >> 1);
+        constexpr int kBytes = kGranule * (D + 8);
+        float s[2][NT][4], vs[2][2], vo[2][2];
+#pragma unroll
+        for (int gi = 0; gi < 2; ++gi) {
+            const uint8_t* g = gr + gi * kBytes;
+            // fp32: the two halves of the dimensions and the low part of q apart, as the tensor cores
+            // truncate each sum to its own size
+            float s2[NT][kSplit ? 2 : 1][4];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    s[gi][nt][j] = kSplit ? 0.0f : -8.0f * gamma[nt][j & 1];
+                    s2[nt][0][j] = 0.0f;
+                    if constexpr (kSplit) s2[nt][1][j] = 0.0f;
+                }
+            uint32_t ka[kWords], kb[kWords];
+            if constexpr (D == 128) {
+                const uint4 u = *reinterpret_cast<const uint4*>(g + tok * 64 + t4 * 16);
+                const uint4 v = *reinterpret_cast<const uint4*>(g + (tok + 8) * 64 + t4 * 16);
+                ka[0] = u.x, ka[1] = u.y, ka[2] = u.z, ka[3] = u.w;
+                kb[0] = v.x, kb[1] = v.y, kb[2] = v.z, kb[3] = v.w;
+            } else {
+                const uint2 u = *reinterpret_cast<const uint2*>(g + tok * 32 + t4 * 8);
+                const uint2 v = *reinterpret_cast<const uint2*>(g + (tok + 8) * 32 + t4 * 8);
+                ka[0] = u.x, ka[1] = u.y;
+                kb[0] = v.x, kb[1] = v.y;
+            }
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) {
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf) {
+                    const uint32_t x = hf ? ka[i] >> 8 : ka[i], y = hf ? kb[i] >> 8 : kb[i];
+                    const uint32_t a0 = codes<kSplit, false>(x), a1 = codes<kSplit, false>(y);
+                    const uint32_t a2 = codes<kSplit, true>(x), a3 = codes<kSplit, true>(y);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        if constexpr (kSplit) {
+                            mma_f16(2 * i < kWords ? s[gi][nt] : s2[nt][0], a0, a1, a2, a3, bq[nt][i][2 * hf], bq[nt][i][2 * hf + 1]);
+                            mma_f16(s2[nt][1], a0, a1, a2, a3, bl[nt][i][2 * hf], bl[nt][i][2 * hf + 1]);
+                        } else {
+                            mma_f16(s[gi][nt], a0, a1, a2, a3, bq[nt][i][2 * hf], bq[nt][i][2 * hf + 1]);
+                        }
+                    }
+                }
+            }
+            const uint32_t* prm = reinterpret_cast<const uint32_t*>(g + kGranule * D);
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+                // the grid about its middle code: x = s (c - 8) + (o + 8 s)
+                const uint32_t kp = prm[tok + 8 * hf], vp = prm[16 + tok + 8 * hf];
+                const float ks = kv_scale(kp), ko = fmaf(8.0f, ks, kv_offset(kp));
+                vs[gi][hf] = kv_scale(vp);
+                vo[gi][hf] = fmaf(8.0f, vs[gi][hf], kv_offset(vp));
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        float& x = s[gi][nt][2 * hf + k];
+                        if constexpr (kSplit) x += s2[nt][0][2 * hf + k] + s2[nt][1][2 * hf + k];
+                        x = fmaf(ks, x, ko * gamma[nt][k]);
+                        if (MASK && slot + 16 * gi + tok + 8 * hf >= lim[nt][k]) x = -INFINITY;
+                    }
+            }
+        }
+        if (scores) {
+#pragma unroll
+            for (int gi = 0; gi < 2; ++gi)
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        const int64_t sl = slot + 16 * gi + tok + 8 * hf;
+                        const float x0 = alpha[nt][0] * s[gi][nt][2 * hf], x1 = alpha[nt][1] * s[gi][nt][2 * hf + 1];
+                        if (!(group & 1)) {   // two columns are neighbours of one token
+                            if (sl < lim[nt][0]) *reinterpret_cast<float2*>(scores + put[nt][0] + sl * group) = make_float2(x0, x1);
+                        } else {
+                            if (sl < lim[nt][0]) scores[put[nt][0] + sl * group] = x0;
+                            if (sl < lim[nt][1]) scores[put[nt][1] + sl * group] = x1;
+                        }
+                    }
+        }
+        // The maximum that the weights are taken against moves only when a score passes it by 2^kSlack,
+        // and the values' exponent only when a scale passes it: both are rare after the first tiles.
+        float mx[NT][2], vmax = 0.0f;
+        bool move = false;
+#pragma unroll
+        for (int gi = 0; gi < 2; ++gi)
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf)
+                if (!MASK || slot + 16 * gi + tok + 8 * hf < n) vmax = fmaxf(vmax, vs[gi][hf]);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                mx[nt][k] = fmaxf(fmaxf(s[0][nt][k], s[0][nt][2 + k]), fmaxf(s[1][nt][k], s[1][nt][2 + k])) * alpha[nt][k];
+                move |= mx[nt][k] > m[nt][k] + kSlack;
+            }
+        move |= static_cast<int>(__float_as_uint(vmax) >> 23) > ev;
+        float corr[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) corr[nt][0] = corr[nt][1] = 1.0f;
+        if (__any_sync(0xffffffffu, move)) {
+            const uint32_t vb = vmax < INFINITY ? __float_as_uint(vmax) : 0u;
+            const int en = max(ev, static_cast<int>(__reduce_max_sync(0xffffffffu, vb) >> 23));
+            const float drop = __uint_as_float(static_cast<uint32_t>(max(0, 127 + ev - en)) << 23);
+            ev = en;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    float x = mx[nt][k];
+#pragma unroll
+                    for (int sh = 4; sh < 32; sh <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, sh));
+                    const float mn = fmaxf(m[nt][k], x);
+                    const float r = mn == -INFINITY ? 1.0f : ex2(m[nt][k] - mn);
+                    m[nt][k] = mn;
+                    l[nt][k] *= r;
+                    off[nt][k] *= r;
+                    corr[nt][k] = r * drop;
+                }
+        }
+        const float inv = __uint_as_float(static_cast<uint32_t>(259 - ev) << 23);   // 2^6 / 2^(ev + 1 - 127)
+        uint32_t b[2][NT][2], e[2][NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            float ms[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) ms[k] = m[nt][k] == -INFINITY ? 0.0f : m[nt][k];
+#pragma unroll
+            for (int gi = 0; gi < 2; ++gi)
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf) {
+                    const float va = vs[gi][hf] * inv;
+                    float w[2];
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const float x = s[gi][nt][2 * hf + k];
+                        const float pr = ex2(fmaf(alpha[nt][k], x, -ms[k]));
+                        l[nt][k] += pr;
+                        if (MASK) {
+                            const bool in = slot + 16 * gi + tok + 8 * hf < lim[nt][k];
+                            off[nt][k] += in ? pr * vo[gi][hf] : 0.0f;
+                            w[k] = in ? pr * va : 0.0f;
+                        } else {
+                            off[nt][k] = fmaf(pr, vo[gi][hf], off[nt][k]);
+                            w[k] = pr * va;
+                        }
+                    }
+                    // weights of 16 tokens by 8 rows into the B fragment: token pairs along a lane
+                    const uint32_t h = pack_f16(w[0], w[1]);
+                    if constexpr (kSplit) {
+                        const float2 f = unpack_f16(h);
+                        e[gi][nt][hf] = transpose8(pack_f16(w[0] - f.x, w[1] - f.y));
+                    }
+                    b[gi][nt][hf] = transpose8(h);
+                }
+            if constexpr (!kSplit) {
+                // 8 times the weights' sum, in every row of the accumulator's layout
+                float mid[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int gi = 0; gi < 2; ++gi)
+                    mma_f16(mid, 0x00080008u, 0x00080008u, 0x00080008u, 0x00080008u, b[gi][nt][0], b[gi][nt][1]);
+                const float m16[2] = {16.0f * mid[0], 16.0f * mid[1]};
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        o[nt][i][j] = fmaf(o[nt][i][j], corr[nt][j & 1], j < 2 ? -mid[j] : -m16[j & 1]);
+            }
+        }
+        // values: words of dimensions 16 g8 .. (D = 128) or 8 g8 .. (D = 64) of four tokens
+#pragma unroll
+        for (int gi = 0; gi < 2; ++gi) {
+            const uint8_t* vr = gr + gi * kBytes + kGranule * (D / 2) + g8 * (D / 16);
+            uint32_t v[4][D / 64];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int tk = (i >> 1) * 8 + (i & 1 ? 7 - t4 : t4);
+                if constexpr (D == 128) {
+                    const uint2 u = *reinterpret_cast<const uint2*>(vr + tk * 64);
+                    v[i][0] = u.x, v[i][1] = u.y;
+                } else {
+                    v[i][0] = *reinterpret_cast<const uint32_t*>(vr + tk * 32);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < D / 64; ++j)
+#pragma unroll
+                for (int qd = 0; qd < 4; ++qd) {   // dimensions 2 qd and 2 qd + 1 of the word
+                    const uint32_t sel = qd < 2 ? 0x5410u : 0x7632u;
+                    uint32_t x = __byte_perm(v[0][j], v[1][j], sel), y = __byte_perm(v[2][j], v[3][j], sel);
+                    if (qd & 1) x >>= 8, y >>= 8;
+                    const uint32_t a0 = codes<kSplit, false>(x), a1 = codes<kSplit, true>(x);
+                    const uint32_t a2 = codes<kSplit, false>(y), a3 = codes<kSplit, true>(y);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        float(&ac)[4] = o[nt][4 * j + qd];
+                        if constexpr (kSplit) {   // 16 tokens' sum by itself, then rounded into the running one
+                            float u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                            mma_f16(u, a0, a1, a2, a3, e[gi][nt][0], e[gi][nt][1]);
+                            mma_f16(u, a0, a1, a2, a3, b[gi][nt][0], b[gi][nt][1]);
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) ac[r] = gi == 0 ? fmaf(ac[r], corr[nt][r & 1], u[r]) : ac[r] + u[r];
+                        } else {
+                            mma_f16(ac, a0, a1, a2, a3, b[gi][nt][0], b[gi][nt][1]);
+                        }
+                    }
+                }
+        }
+    }
 };
 
 template <typename T, int D, int NT>
 __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) kv_attend_kernel(const Attend p, const int min_tiles) {
     using Sh = Shape<D, NT>;
     constexpr int kRows = Sh::kRows, kStages = Sh::kStages;
-    constexpr bool kSplit = sizeof(T) == 4;      // fp32: two fp16 halves of q and of the weights
-    constexpr int kWords = D / 32;               // code words of a row that a lane of a quad takes
+    constexpr bool kSplit = Rows<T, D, NT>::kSplit;
+    constexpr int kWords = Rows<T, D, NT>::kWords;
     extern __shared__ __align__(128) uint8_t smem[];
     float* const merge = reinterpret_cast<float*>(smem + kStages * Sh::kStageBytes);
     __shared__ uint64_t full[kStages], empty[kStages];
@@ -307,10 +566,6 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) kv_attend_kernel(co
 
     // ---- consumers
     const int g8 = lane >> 2, t4 = lane & 3;
-    // the token of A row g8 (and 8 more of row g8 + 8), chosen so that the tokens 2 t4, 2 t4 + 1, 2 t4 + 8 and 2 t4 + 9
-    // of the weights' fragment are rows t4, 7 - t4, 8 + t4, 15 - t4: neighbouring lanes then read
-    // neighbouring rows of codes
-    const int tok = (g8 & 1) ? 7 - (g8 >> 1) : (g8 >> 1);
     int it = 0;
     // After a wait that gave up the warps go on through the same steps without waiting (the result is
     // reported as failed), so that none of them is left alone at a barrier.
@@ -318,49 +573,26 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) kv_attend_kernel(co
         const int64_t seg = min(w1 - w, static_cast<int64_t>(at.s.tiles - at.tile));
         const int rows = min(kRows, at.s.nq * p.group - at.rt * kRows);
         // q: lane (g8, t4) holds dimensions t4 D / 4 .. of row g8, each word of 8 as two k steps: (0, 4 | 1, 5) and
-        // (2, 6 | 3, 7), the odd ones divided by 16 because their nibbles sit four bits up
-        uint32_t bq[NT][kWords][4], bl[NT][kWords][4];
-        float alpha[NT][2], beta[NT][2], zero[NT][2];   // zero: -8 sum(q) in the accumulator's units
-        int32_t lim[NT][2];
-        int64_t put[NT][2];   // where a row's scores go
-        int32_t least = at.s.n;
+        // (2, 6 | 3, 7); the odd ones are divided by 16 where their nibbles sit four bits up
+        Rows<T, D, NT> R;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int r = nt * 8 + g8, row = at.rt * kRows + r;
-            float x[D / 4];
-            if (r < rows) {
-                const T* src = static_cast<const T*>(p.q) + (at.s.first + row / p.group) * p.q_token +
-                               (static_cast<int64_t>(at.h) * p.group + row % p.group) * p.q_head + t4 * (D / 4);
-                if (p.q_vec) {
-#pragma unroll
-                    for (int i = 0; i < static_cast<int>(D / 4 * sizeof(T) / 16); ++i) {
-                        const uint4 u = reinterpret_cast<const uint4*>(src)[i];
-                        const uint32_t v[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            if constexpr (kSplit) {
-                                x[4 * i + j] = __uint_as_float(v[j]);
-                            } else {
-                                x[8 * i + 2 * j] = __uint_as_float(v[j] << 16);
-                                x[8 * i + 2 * j + 1] = __uint_as_float(v[j] & 0xFFFF0000u);
-                            }
-                        }
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < D / 4; ++i) x[i] = static_cast<float>(src[i]);
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < D / 4; ++i) x[i] = 0.0f;
-            }
+            const int row = at.rt * kRows + nt * 8 + g8;
+            const bool real = nt * 8 + g8 < rows;
+            const T* src = static_cast<const T*>(p.q) + (at.s.first + (real ? row / p.group : 0)) * p.q_token +
+                           (static_cast<int64_t>(at.h) * p.group + (real ? row % p.group : 0)) * p.q_head + t4 * (D / 4);
             float top = 0.0f, sum = 0.0f;
             bool fine = true;
 #pragma unroll
-            for (int i = 0; i < D / 4; ++i) {
-                top = fmaxf(top, fabsf(x[i]));
-                sum += x[i];
-                fine &= fabsf(x[i]) <= 3.402823466e38f;
+            for (int i = 0; i < kWords; ++i) {
+                float x[8];
+                load8(src + 8 * i, p.q_vec, x);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    top = fmaxf(top, fabsf(x[j]));
+                    sum += x[j];
+                    fine &= fabsf(x[j]) <= 3.402823466e38f;
+                }
             }
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
@@ -369,216 +601,56 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) kv_attend_kernel(co
             int bad = !fine;
             bad |= __shfl_xor_sync(0xffffffffu, bad, 1);
             bad |= __shfl_xor_sync(0xffffffffu, bad, 2);
-            // 2^e brings the largest below 2^14; both powers stay normal
+            // 2^e brings the largest below 2^14; both powers stay normal. The sign of the scale goes to q, so that
+            // alpha > 0 and scores compare before they are scaled.
             const int e = min(100, max(-113, 13 - static_cast<int>((__float_as_uint(top) >> 23) & 255) + 127));
-            const float up = bad ? 0.0f : __uint_as_float(static_cast<uint32_t>(e + 127) << 23);
-            const float f = p.scale * kLog2e;
-            const float a = bad ? NAN : (kSplit ? f : f * 0x1p24f) * __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-            const float bt = bad ? NAN : f * sum;
-            const float zr = bad ? 0.0f : sum * (up * -0x1p-21f);   // of no use to centred codes
+            const float up = copysignf(__uint_as_float(static_cast<uint32_t>(e + 127) << 23), p.scale);
+            const float f = fmaxf(fabsf(p.scale) * kLog2e, 0x1p-126f);
+            // score / ln 2 = f (s sum(q c) + o sum(q)) with sum(q c) = S / unit
+            const float unit = kSplit ? up : up * 0x1p-24f;
+            const float a = bad ? NAN : fmaxf((kSplit ? f : f * 0x1p24f) * __uint_as_float(static_cast<uint32_t>(127 - e) << 23), 0x1p-126f);
+            const float gm = bad ? 0.0f : sum * unit;
 #pragma unroll
             for (int i = 0; i < kWords; ++i) {
+                float x[8];
+                load8(src + 8 * i, p.q_vec, x);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {   // nibbles j and j + 4
                     const float s = up * (!kSplit && (j & 1) ? 0.0625f : 1.0f);
-                    const float x0 = bad ? 0.0f : x[8 * i + j] * s, x1 = bad ? 0.0f : x[8 * i + j + 4] * s;
-                    bq[nt][i][j] = pack_f16(x0, x1);
+                    const float x0 = real && !bad ? x[j] * s : 0.0f, x1 = real && !bad ? x[j + 4] * s : 0.0f;
+                    R.bq[nt][i][j] = pack_f16(x0, x1);
                     if constexpr (kSplit) {
-                        const float2 h = unpack_f16(bq[nt][i][j]);
-                        bl[nt][i][j] = pack_f16(x0 - h.x, x1 - h.y);
+                        const float2 h = unpack_f16(R.bq[nt][i][j]);
+                        R.bl[nt][i][j] = pack_f16(x0 - h.x, x1 - h.y);
                     }
                 }
             }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {   // the accumulator's columns 2 t4 + k
                 const int col = nt * 8 + 2 * t4 + k, crow = at.rt * kRows + col;
-                alpha[nt][k] = __shfl_sync(0xffffffffu, a, (2 * t4 + k) * 4);
-                beta[nt][k] = __shfl_sync(0xffffffffu, bt, (2 * t4 + k) * 4);
-                zero[nt][k] = __shfl_sync(0xffffffffu, zr, (2 * t4 + k) * 4);
+                R.alpha[nt][k] = __shfl_sync(0xffffffffu, a, (2 * t4 + k) * 4);
+                R.gamma[nt][k] = __shfl_sync(0xffffffffu, gm, (2 * t4 + k) * 4);
                 const int i = crow / p.group;
-                lim[nt][k] = col < rows ? visible(at.s.n, at.s.nq, i) : 0;
-                put[nt][k] = ((static_cast<int64_t>(at.s.first + i) * c.kv_heads + at.h) * p.S) * p.group + crow % p.group;
+                R.lim[nt][k] = col < rows ? visible(at.s.n, at.s.nq, i) : 0;
+                R.put[nt][k] = ((static_cast<int64_t>(at.s.first + i) * c.kv_heads + at.h) * p.S) * p.group + crow % p.group;
+                R.m[nt][k] = -INFINITY, R.l[nt][k] = 0.0f, R.off[nt][k] = 0.0f;
             }
-        }
-        float o[NT][D / 16][4], m[NT][2], l[NT][2], off[NT][2];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) o[nt][i][j] = 0.0f;
-#pragma unroll
-            for (int k = 0; k < 2; ++k) m[nt][k] = -INFINITY, l[nt][k] = 0.0f, off[nt][k] = 0.0f;
+                for (int j = 0; j < 4; ++j) R.o[nt][i][j] = 0.0f;
         }
-        least = visible(at.s.n, at.s.nq, at.rt * kRows / p.group);   // what the first row sees, the others see
-        int ev = 20;   // biased exponent of the largest value scale so far
+        R.ev = 20;
+        const int least = visible(at.s.n, at.s.nq, at.rt * kRows / p.group);   // what the first row sees, the others see
 
         for (int64_t k = 0; k < seg; ++k, ++it) {
             const int stage = it % kStages;
             const bool ok = __all_sync(0xffffffffu, mbar_wait(&full[stage], (it / kStages) & 1, &abort_flag));
-            const int slot = (at.tile + static_cast<int>(k)) * kTile + warp * kGranule;
+            const int slot = (at.tile + static_cast<int>(k)) * kTile + warp * 2 * kGranule;
+            const uint8_t* gr = smem + stage * Sh::kStageBytes + warp * 2 * Sh::kGranuleBytes;
             if (ok && slot < at.s.n) {   // uniform over the warp
-                const uint8_t* gr = smem + stage * Sh::kStageBytes + warp * Sh::kGranuleBytes;
-                // scores; fp32: the two halves of the dimensions and the low part of q apart, as the tensor
-                // cores truncate each sum to its own size
-                float s[NT][4], s2[NT][kSplit ? 2 : 1][4];
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        s[nt][j] = kSplit ? 0.0f : zero[nt][j & 1];
-                        s2[nt][0][j] = 0.0f;
-                        if constexpr (kSplit) s2[nt][1][j] = 0.0f;
-                    }
-                {
-                    uint32_t ka[kWords], kb[kWords];
-                    if constexpr (D == 128) {
-                        const uint4 u = *reinterpret_cast<const uint4*>(gr + tok * 64 + t4 * 16);
-                        const uint4 v = *reinterpret_cast<const uint4*>(gr + (tok + 8) * 64 + t4 * 16);
-                        ka[0] = u.x, ka[1] = u.y, ka[2] = u.z, ka[3] = u.w;
-                        kb[0] = v.x, kb[1] = v.y, kb[2] = v.z, kb[3] = v.w;
-                    } else {
-                        const uint2 u = *reinterpret_cast<const uint2*>(gr + tok * 32 + t4 * 8);
-                        const uint2 v = *reinterpret_cast<const uint2*>(gr + (tok + 8) * 32 + t4 * 8);
-                        ka[0] = u.x, ka[1] = u.y;
-                        kb[0] = v.x, kb[1] = v.y;
-                    }
-#pragma unroll
-                    for (int i = 0; i < kWords; ++i) {
-#pragma unroll
-                        for (int hf = 0; hf < 2; ++hf) {
-                            const uint32_t x = hf ? ka[i] >> 8 : ka[i], y = hf ? kb[i] >> 8 : kb[i];
-                            const uint32_t a0 = codes<kSplit, false>(x), a1 = codes<kSplit, false>(y);
-                            const uint32_t a2 = codes<kSplit, true>(x), a3 = codes<kSplit, true>(y);
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) {
-                                if constexpr (kSplit) {
-                                    mma_f16(2 * i < kWords ? s[nt] : s2[nt][0], a0, a1, a2, a3, bq[nt][i][2 * hf],
-                                            bq[nt][i][2 * hf + 1]);
-                                    mma_f16(s2[nt][1], a0, a1, a2, a3, bl[nt][i][2 * hf], bl[nt][i][2 * hf + 1]);
-                                } else {
-                                    mma_f16(s[nt], a0, a1, a2, a3, bq[nt][i][2 * hf], bq[nt][i][2 * hf + 1]);
-                                }
-                            }
-                        }
-                    }
-                }
-                const uint32_t* prm = reinterpret_cast<const uint32_t*>(gr + kGranule * D);
-                const uint32_t kp[2] = {prm[tok], prm[tok + 8]}, vp[2] = {prm[16 + tok], prm[24 + tok]};
-                // the grid about its middle code: x = s (c - 8) + (o + 8 s)
-                const float ks[2] = {kv_scale(kp[0]), kv_scale(kp[1])}, vs[2] = {kv_scale(vp[0]), kv_scale(vp[1])};
-                const float ko[2] = {fmaf(8.0f, ks[0], kv_offset(kp[0])), fmaf(8.0f, ks[1], kv_offset(kp[1]))};
-                const float vo[2] = {fmaf(8.0f, vs[0], kv_offset(vp[0])), fmaf(8.0f, vs[1], kv_offset(vp[1]))};
-                const int at0 = slot + tok, at1 = at0 + 8;
-                // the largest value scale so far, as an exponent (a NaN or a slot past the end has no say)
-                uint32_t big = 0;
-#pragma unroll
-                for (int hf = 0; hf < 2; ++hf) {
-                    const uint32_t sb = vp[hf] << 16;
-                    if (sb < 0x7F800000u && (hf ? at1 : at0) < at.s.n) big = max(big, sb);
-                }
-                const int en = max(ev, static_cast<int>(__reduce_max_sync(0xffffffffu, big) >> 23));
-                const float drop = __uint_as_float(static_cast<uint32_t>(max(0, 127 + ev - en)) << 23);
-                ev = en;
-                const float inv = __uint_as_float(static_cast<uint32_t>(267 - en) << 23);   // 2^14 / 2^(en + 1 - 127)
-                const bool all_seen = slot + kGranule <= least;
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    float wgt[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {   // j = 2 (row half) + column
-                        const int hf = j >> 1, k2 = j & 1;
-                        if constexpr (kSplit) s[nt][j] += s2[nt][0][j] + s2[nt][1][j];
-                        const float x = fmaf(ks[hf], alpha[nt][k2] * s[nt][j], ko[hf] * beta[nt][k2]);
-                        s[nt][j] = all_seen || (hf ? at1 : at0) < lim[nt][k2] ? x : -INFINITY;
-                    }
-                    if (p.scores) {
-#pragma unroll
-                        for (int hf = 0; hf < 2; ++hf) {
-                            const int64_t sl = hf ? at1 : at0;
-                            if (!(p.group & 1)) {   // two columns are neighbours of one token
-                                if (sl < lim[nt][0])
-                                    *reinterpret_cast<float2*>(p.scores + put[nt][0] + sl * p.group) =
-                                        make_float2(s[nt][2 * hf], s[nt][2 * hf + 1]);
-                            } else {
-                                if (sl < lim[nt][0]) p.scores[put[nt][0] + sl * p.group] = s[nt][2 * hf];
-                                if (sl < lim[nt][1]) p.scores[put[nt][1] + sl * p.group] = s[nt][2 * hf + 1];
-                            }
-                        }
-                    }
-                    float corr[2];
-#pragma unroll
-                    for (int k2 = 0; k2 < 2; ++k2) {
-                        float mx = fmaxf(s[nt][k2], s[nt][2 + k2]);
-#pragma unroll
-                        for (int sh = 4; sh < 32; sh <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, sh));
-                        const float mn = fmaxf(m[nt][k2], mx), ms = mn == -INFINITY ? 0.0f : mn;
-                        corr[k2] = ex2(m[nt][k2] - ms);
-                        m[nt][k2] = mn;
-                        l[nt][k2] *= corr[k2];
-                        off[nt][k2] *= corr[k2];
-                        corr[k2] *= drop;
-#pragma unroll
-                        for (int hf = 0; hf < 2; ++hf) {
-                            const float pr = ex2(s[nt][2 * hf + k2] - ms);
-                            const bool in = all_seen || (hf ? at1 : at0) < lim[nt][k2];
-                            l[nt][k2] += pr;
-                            off[nt][k2] += in ? pr * vo[hf] : 0.0f;
-                            wgt[2 * hf + k2] = in ? pr * (vs[hf] * inv) : 0.0f;
-                        }
-                    }
-                    // weights of 16 tokens by 8 rows into the B fragment: token pairs along a lane
-                    const uint32_t h0 = pack_f16(wgt[0], wgt[1]), h1 = pack_f16(wgt[2], wgt[3]);
-                    uint32_t e0 = 0, e1 = 0;
-                    if constexpr (kSplit) {
-                        const float2 f0 = unpack_f16(h0), f1 = unpack_f16(h1);
-                        e0 = transpose8(pack_f16(wgt[0] - f0.x, wgt[1] - f0.y));
-                        e1 = transpose8(pack_f16(wgt[2] - f1.x, wgt[3] - f1.y));
-                    }
-                    const uint32_t b0 = transpose8(h0), b1 = transpose8(h1);
-                    if constexpr (!kSplit) {
-                        // 8 times the weights' sum, in every row of the accumulator's layout
-                        float mid[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                        mma_f16(mid, 0x00080008u, 0x00080008u, 0x00080008u, 0x00080008u, b0, b1);
-#pragma unroll
-                        for (int i = 0; i < D / 16; ++i)
-#pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                o[nt][i][j] = fmaf(o[nt][i][j], corr[j & 1], (j < 2 ? -1.0f : -16.0f) * mid[j & 1]);
-                    }
-                    // values: words of dimensions 16 g8 .. (D = 128) or 8 g8 .. (D = 64) of four tokens
-                    const uint8_t* vr = gr + kGranule * (D / 2) + g8 * (D / 16);
-                    uint32_t v[4][D / 64];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int tk = (i >> 1) * 8 + (i & 1 ? 7 - t4 : t4);
-                        if constexpr (D == 128) {
-                            const uint2 u = *reinterpret_cast<const uint2*>(vr + tk * 64);
-                            v[i][0] = u.x, v[i][1] = u.y;
-                        } else {
-                            v[i][0] = *reinterpret_cast<const uint32_t*>(vr + tk * 32);
-                        }
-                    }
-#pragma unroll
-                    for (int j = 0; j < D / 64; ++j)
-#pragma unroll
-                        for (int qd = 0; qd < 4; ++qd) {   // dimensions 2 qd and 2 qd + 1 of the word
-                            const uint32_t sel = qd < 2 ? 0x5410u : 0x7632u;
-                            uint32_t x = __byte_perm(v[0][j], v[1][j], sel), y = __byte_perm(v[2][j], v[3][j], sel);
-                            if (qd & 1) x >>= 8, y >>= 8;
-                            const uint32_t a0 = codes<kSplit, false>(x), a1 = codes<kSplit, true>(x);
-                            const uint32_t a2 = codes<kSplit, false>(y), a3 = codes<kSplit, true>(y);
-                            if constexpr (kSplit) {   // a tile's sum by itself, then rounded into the running one
-                                float u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                                mma_f16(u, a0, a1, a2, a3, e0, e1);
-                                mma_f16(u, a0, a1, a2, a3, b0, b1);
-#pragma unroll
-                                for (int r = 0; r < 4; ++r) o[nt][4 * j + qd][r] = fmaf(o[nt][4 * j + qd][r], corr[r & 1], u[r]);
-                            } else {
-                                mma_f16(o[nt][4 * j + qd], a0, a1, a2, a3, b0, b1);
-                            }
-                        }
-                }
+                if (slot + 2 * kGranule <= least) R.template step<false>(gr, slot, at.s.n, g8, t4, p.scores, p.group);
+                else R.template step<true>(gr, slot, at.s.n, g8, t4, p.scores, p.group);
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(&empty[stage]);
@@ -588,24 +660,24 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) kv_attend_kernel(co
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int k2 = 0; k2 < 2; ++k2) {
+            for (int k = 0; k < 2; ++k) {
 #pragma unroll
                 for (int sh = 4; sh < 32; sh <<= 1) {
-                    l[nt][k2] += __shfl_xor_sync(0xffffffffu, l[nt][k2], sh);
-                    off[nt][k2] += __shfl_xor_sync(0xffffffffu, off[nt][k2], sh);
+                    R.l[nt][k] += __shfl_xor_sync(0xffffffffu, R.l[nt][k], sh);
+                    R.off[nt][k] += __shfl_xor_sync(0xffffffffu, R.off[nt][k], sh);
                 }
-                const int col = nt * 8 + 2 * t4 + k2;
+                const int col = nt * 8 + 2 * t4 + k;
                 if (g8 == 0) {
-                    sm_m[warp][col] = m[nt][k2];
-                    sm_l[warp][col] = l[nt][k2];
-                    sm_o[warp][col] = off[nt][k2];
+                    sm_m[warp][col] = R.m[nt][k];
+                    sm_l[warp][col] = R.l[nt][k];
+                    sm_o[warp][col] = R.off[nt][k];
                 }
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i)
                     *reinterpret_cast<float2*>(merge + (warp * kRows + col) * D + g8 * (D / 8) + 2 * i) =
-                        make_float2(o[nt][i][k2], o[nt][i][2 + k2] * (kSplit ? 1.0f : 0.0625f));
+                        make_float2(R.o[nt][i][k], R.o[nt][i][2 + k] * (kSplit ? 1.0f : 0.0625f));
             }
-        if (lane == 0) sm_e[warp] = ev - (kSplit ? 140 : 116);   // 2^24 of subnormal codes, 2^-14 2^(ev + 1 - 127) of the weights
+        if (lane == 0) sm_e[warp] = R.ev - (kSplit ? 132 : 108);   // 2^24 of subnormal codes, 2^-6 2^(ev + 1 - 127) of the weights
         asm volatile("bar.sync 1, 128;" ::: "memory");
         const bool whole = seg == at.s.tiles;
         float* part = p.part + (2 * static_cast<int64_t>(blockIdx.x) + (at.tile == 0 && w > w0 ? 1 : 0)) * (kRows * (D + 2));
