@@ -126,9 +126,17 @@ struct Attend {
     float* scores;                     // [T][kv_heads][S][group], in units of ln 2, or nullptr
     int64_t S;
     int64_t cap;                       // slots a sequence may have: the table's, and S with weights
-    int64_t* base;                     // [batch + 1] first tile of each sequence in the list of work, then the CTAs
+    struct Joint* joint;               // [CTAs]
     float* part;                       // [2 CTAs][rows][D + 2]: sums, maximum, sum of weights
     int* info;
+};
+
+// What CTA c leaves to kv_combine_kernel when it is the first to go on with rows that CTA c - 1 began.
+struct Joint {
+    int32_t last;            // the last CTA of these rows, or 0: nothing to join
+    int32_t first_slot;      // which of CTA c - 1's two partial results
+    int32_t h, row, rows;    // head, first query row of the sequence, number of rows
+    int32_t token;           // the sequence's first token
 };
 
 // Sequence b's share of the work.
@@ -161,6 +169,27 @@ __device__ __forceinline__ int32_t visible(int32_t n, int32_t nq, int32_t i) { r
 __device__ __forceinline__ int64_t first_tile(int64_t W, int64_t c, int64_t C) { return W * c / C; }
 __device__ __forceinline__ int64_t cta_of(int64_t W, int64_t w, int64_t C) { return ((w + 1) * C - 1) / W; }
 
+// lead = base + the sum of v over the threads before this one; returns base + the sum over all.
+__device__ __forceinline__ int64_t scan_add(int64_t v, int64_t base, int64_t* tmp, int64_t& lead) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int64_t x = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+    }
+    __syncthreads();
+    if (lane == 31) tmp[warp] = x;
+    __syncthreads();
+    lead = base + x - v;
+#pragma unroll
+    for (int i = 0; i < kThreads / 32; ++i) {
+        if (i < warp) lead += tmp[i];
+        base += tmp[i];
+    }
+    return base;
+}
+
 // A position in the list of work: tile `tile` of row group `rt` of head h of sequence b.
 struct Place {
     int b, h, rt, tile;
@@ -190,7 +219,8 @@ struct Shape {
     static constexpr int kRows = 8 * NT;
     static constexpr int kGranuleBytes = kGranule * (D + 8);
     static constexpr int kStageBytes = kTile / kGranule * kGranuleBytes;
-    static constexpr int kMergeFloats = kWarps * kRows * D;
+    static constexpr int kMergeRow = D + 4;   // with the rotation by g8 below: no bank conflicts
+    static constexpr int kMergeFloats = kWarps * kRows * kMergeRow;
     static constexpr int kStages = D == 128 ? 3 : 5;
     static constexpr size_t kSmem = kStages * kStageBytes + kMergeFloats * sizeof(float);
 };
@@ -429,7 +459,7 @@ struct Rows {
 };
 
 template <typename T, int D, int NT>
-__global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) kv_attend_kernel(const Attend p, const int min_tiles) {
+__global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) kv_attend_kernel(const Attend p) {
     using Sh = Shape<D, NT>;
     constexpr int kRows = Sh::kRows, kStages = Sh::kStages;
     constexpr bool kSplit = Rows<T, D, NT>::kSplit;
@@ -441,7 +471,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) kv_attend_kernel(co
     __shared__ int64_t scan_tmp[kThreads / 32], found_base;
     __shared__ int found_b;
     __shared__ float sm_m[kWarps][kRows], sm_l[kWarps][kRows], sm_o[kWarps][kRows];
-    __shared__ int sm_e[kWarps];
+    __shared__ float sm_e[kWarps];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const KvView& c = p.c;
 
@@ -456,51 +486,29 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) kv_attend_kernel(co
         fence_mbar_init();
         if (blockIdx.x == 0 && (p.start[0] != 0 || p.start[c.batch] != p.tokens)) record_error(p.info, -KQ_ERR_INVALID_ARG);
     }
-    int64_t W = 0;
-    {
-        int64_t mine = 0;
-        for (int b = tid; b < c.batch; b += kThreads) mine += work_of(p, sequence<kRows>(p, b, blockIdx.x ? nullptr : p.info));
-        for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
-        if (lane == 0) scan_tmp[warp] = mine;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kThreads / 32; ++i) W += scan_tmp[i];
+    // The sequences' tiles, kThreads of them at a time: the total, then the one that holds this CTA's first.
+    int64_t W = 0, v = 0, lead = 0;
+    for (int b0 = 0; b0 < c.batch; b0 += kThreads) {
+        v = b0 + tid < c.batch ? work_of(p, sequence<kRows>(p, b0 + tid, blockIdx.x ? nullptr : p.info)) : 0;
+        W = scan_add(v, W, scan_tmp, lead);
     }
-    const int64_t C = max(static_cast<int64_t>(1), min(static_cast<int64_t>(gridDim.x), (W + min_tiles - 1) / min_tiles));
+    const int64_t C = max(static_cast<int64_t>(1), min(static_cast<int64_t>(gridDim.x), W));
     const int64_t w0 = first_tile(W, blockIdx.x, C), w1 = blockIdx.x < C ? first_tile(W, blockIdx.x + 1, C) : w0;
-    if (blockIdx.x != 0 && w0 >= w1) return;
+    if (tid == 0) p.joint[blockIdx.x].last = 0;
+    if (w0 >= w1) return;
     int64_t before = 0;
     for (int b0 = 0; b0 < c.batch; b0 += kThreads) {
-        const int b = b0 + tid;
-        const int64_t v = b < c.batch ? work_of(p, sequence<kRows>(p, b, nullptr)) : 0;
-        int64_t x = v;
-        for (int o = 1; o < 32; o <<= 1) {
-            const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
-            if (lane >= o) x += y;
+        if (c.batch > kThreads) {
+            v = b0 + tid < c.batch ? work_of(p, sequence<kRows>(p, b0 + tid, nullptr)) : 0;
+            before = scan_add(v, before, scan_tmp, lead);
         }
-        __syncthreads();
-        if (lane == 31) scan_tmp[warp] = x;
-        __syncthreads();
-        int64_t lead = before, all = before;
-#pragma unroll
-        for (int i = 0; i < kThreads / 32; ++i) {
-            if (i < warp) lead += scan_tmp[i];
-            all += scan_tmp[i];
+        if (v > 0 && lead <= w0 && w0 < lead + v) {
+            found_b = b0 + tid;
+            found_base = lead;
         }
-        const int64_t at = lead + x - v;
-        if (b < c.batch && v > 0 && at <= w0 && w0 < at + v) {
-            found_b = b;
-            found_base = at;
-        }
-        if (blockIdx.x == 0 && b < c.batch) p.base[b] = at;
-        before = all;
-    }
-    if (blockIdx.x == 0 && tid == 0) {
-        p.base[c.batch] = W;
-        p.base[c.batch + 1] = C;
     }
     __syncthreads();
-    if (w0 >= w1 || found_b < 0) return;   // uniform: an empty list of work
+    if (found_b < 0) return;   // not reached: some sequence holds every tile
     pdl_launch_dependents();
     Place at;
     at.b = found_b;
@@ -510,6 +518,17 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) kv_attend_kernel(co
         at.h = static_cast<int>(rem / head);
         at.rt = static_cast<int>(rem % head / at.s.tiles);
         at.tile = static_cast<int>(rem % at.s.tiles);
+        const int64_t a = w0 - at.tile;   // the first tile of these rows
+        if (tid == 0 && blockIdx.x > 0 && at.tile > 0 && a >= first_tile(W, blockIdx.x - 1, C)) {
+            Joint j;
+            j.last = static_cast<int32_t>(cta_of(W, a + at.s.tiles - 1, C));
+            j.first_slot = a > first_tile(W, blockIdx.x - 1, C) ? 1 : 0;
+            j.h = at.h;
+            j.row = at.rt * kRows;
+            j.rows = min(kRows, at.s.nq * p.group - at.rt * kRows);
+            j.token = at.s.first;
+            p.joint[blockIdx.x] = j;
+        }
     }
 
     if (warp == kWarps) {
@@ -581,19 +600,18 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) kv_attend_kernel(co
             const bool real = nt * 8 + g8 < rows;
             const T* src = static_cast<const T*>(p.q) + (at.s.first + (real ? row / p.group : 0)) * p.q_token +
                            (static_cast<int64_t>(at.h) * p.group + (real ? row % p.group : 0)) * p.q_head + t4 * (D / 4);
-            float top = 0.0f, sum = 0.0f;
+            float xs[kWords][8], top = 0.0f, sum = 0.0f;
             bool fine = true;
 #pragma unroll
-            for (int i = 0; i < kWords; ++i) {
-                float x[8];
-                load8(src + 8 * i, p.q_vec, x);
+            for (int i = 0; i < kWords; ++i) load8(src + 8 * i, p.q_vec, xs[i]);
+#pragma unroll
+            for (int i = 0; i < kWords; ++i)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    top = fmaxf(top, fabsf(x[j]));
-                    sum += x[j];
-                    fine &= fabsf(x[j]) <= 3.402823466e38f;
+                    top = fmaxf(top, fabsf(xs[i][j]));
+                    sum += xs[i][j];
+                    fine &= fabsf(xs[i][j]) <= 3.402823466e38f;
                 }
-            }
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
             sum += __shfl_xor_sync(0xffffffffu, sum, 1);
@@ -612,8 +630,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) kv_attend_kernel(co
             const float gm = bad ? 0.0f : sum * unit;
 #pragma unroll
             for (int i = 0; i < kWords; ++i) {
-                float x[8];
-                load8(src + 8 * i, p.q_vec, x);
+                const float(&x)[8] = xs[i];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {   // nibbles j and j + 4
                     const float s = up * (!kSplit && (j & 1) ? 0.0625f : 1.0f);
@@ -674,15 +691,18 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) kv_attend_kernel(co
                 }
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i)
-                    *reinterpret_cast<float2*>(merge + (warp * kRows + col) * D + g8 * (D / 8) + 2 * i) =
+                    *reinterpret_cast<float2*>(merge + (warp * kRows + col) * Sh::kMergeRow + g8 * (D / 8) +
+                                               2 * ((i + g8) % (D / 16))) =
                         make_float2(R.o[nt][i][k], R.o[nt][i][2 + k] * (kSplit ? 1.0f : 0.0625f));
             }
-        if (lane == 0) sm_e[warp] = R.ev - (kSplit ? 132 : 108);   // 2^24 of subnormal codes, 2^-6 2^(ev + 1 - 127) of the weights
+        // 2^24 of subnormal codes, 2^-6 2^(ev + 1 - 127) of the weights
+        if (lane == 0) sm_e[warp] = __uint_as_float(static_cast<uint32_t>(min(R.ev - (kSplit ? 132 : 108), 127) + 127) << 23);
         asm volatile("bar.sync 1, 128;" ::: "memory");
         const bool whole = seg == at.s.tiles;
         float* part = p.part + (2 * static_cast<int64_t>(blockIdx.x) + (at.tile == 0 && w > w0 ? 1 : 0)) * (kRows * (D + 2));
+        const int d = tid % D, dg = d / (D / 8), di = d % (D / 8) / 2;
+        const float* mine = merge + dg * (D / 8) + 2 * ((di + dg) % (D / 16)) + (d & 1);
         for (int col = tid / D; col < rows; col += 128 / D) {
-            const int d = tid % D;
             float M = -INFINITY;
 #pragma unroll
             for (int i = 0; i < kWarps; ++i) M = fmaxf(M, sm_m[i][col]);
@@ -692,7 +712,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) kv_attend_kernel(co
             for (int i = 0; i < kWarps; ++i) {
                 const float f = ex2(sm_m[i][col] - ms);
                 L = fmaf(f, sm_l[i][col], L);
-                O = fmaf(f, ldexpf(merge[(i * kRows + col) * D + d], sm_e[i]) + sm_o[i][col], O);
+                O = fmaf(f, fmaf(mine[(i * kRows + col) * Sh::kMergeRow], sm_e[i], sm_o[i][col]), O);
             }
             if (whole) {
                 const int row = at.rt * kRows + col;
@@ -715,44 +735,49 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) kv_attend_kernel(co
     __syncthreads();
 }
 
-// Joins the partial results of rows that more than one CTA worked on. One block for a token and
-// key/value head, a thread for each dimension.
+// Joins the partial results of rows that more than one CTA worked on: block (c, column) for the rows that
+// CTA c went on with, its threads the D dimensions, in groups that share the partial results.
 template <typename T, int D, int NT>
-__global__ void __launch_bounds__(D) kv_combine_kernel(const Attend p) {
+__global__ void __launch_bounds__(512) kv_combine_kernel(const Attend p) {
     constexpr int kRows = 8 * NT;
+    __shared__ float sm[512], sl[512 / D];
     pdl_wait();
     pdl_launch_dependents();
-    const int64_t i = blockIdx.x / p.c.kv_heads;
-    const int h = static_cast<int>(blockIdx.x % p.c.kv_heads), d = threadIdx.x;
-    const int b = kv_sequence_of(p.start, p.c.batch, i);
-    if (b < 0) return;
-    const Seq s = sequence<kRows>(p, b, nullptr);
-    if (s.nq == 0) return;
-    const int64_t W = p.base[p.c.batch], C = p.base[p.c.batch + 1];
-    for (int g = 0; g < p.group; ++g) {
-        const int64_t row = (i - s.first) * p.group + g;
-        const int64_t a = p.base[b] + (static_cast<int64_t>(h) * s.rows_tiles + row / kRows) * s.tiles;
-        const int64_t c0 = cta_of(W, a, C), c1 = cta_of(W, a + s.tiles - 1, C);
-        if (c0 == c1) continue;
-        const int col = static_cast<int>(row % kRows);
-        const float* first = p.part + (2 * c0 + (a > first_tile(W, c0, C) ? 1 : 0)) * (kRows * (D + 2));
-        const float* rest = p.part + 2 * (c0 + 1) * (kRows * (D + 2));   // later CTAs begin with this item
-        const int64_t step = 2 * (kRows * (D + 2));
-        float M = first[kRows * D + col];
-        for (int64_t k = 0; k < c1 - c0; ++k) M = fmaxf(M, rest[k * step + kRows * D + col]);
-        const float ms = M == -INFINITY ? 0.0f : M;
-        float f = ex2(first[kRows * D + col] - ms);
-        float L = f * first[kRows * (D + 1) + col], O = f * first[col * D + d];
+    const Joint j = p.joint[blockIdx.x];
+    const int col = blockIdx.y;
+    if (j.last == 0 || col >= j.rows) return;
+    const int d = threadIdx.x % D, grp = threadIdx.x / D, groups = blockDim.x / D;
+    constexpr int64_t kPart = kRows * (D + 2);
+    const int64_t c = blockIdx.x;
+    const float* first = p.part + (2 * (c - 1) + j.first_slot) * kPart;
+    const float* rest = p.part + 2 * c * kPart;   // the others begin with these rows
+    const int64_t many = j.last - c + 1;
+    float M = first[kRows * D + col];
 #pragma unroll 4
-        for (int64_t k = 0; k < c1 - c0; ++k) {
-            f = ex2(rest[k * step + kRows * D + col] - ms);
-            L = fmaf(f, rest[k * step + kRows * (D + 1) + col], L);
-            O = fmaf(f, rest[k * step + col * D + d], O);
-        }
-        const int64_t r = i * p.q_heads + h * p.group + g;
-        static_cast<T*>(p.out)[r * D + d] = static_cast<T>(L == 0.0f ? 0.0f : O / L);
-        if (d == 0 && p.lse) p.lse[r] = L == 0.0f ? -INFINITY : (ms + log2f(L)) * kLn2;
+    for (int64_t k = 0; k < many; ++k) M = fmaxf(M, rest[2 * k * kPart + kRows * D + col]);
+    const float ms = M == -INFINITY ? 0.0f : M;
+    float L = 0.0f, O = 0.0f;
+#pragma unroll 4
+    for (int64_t k = grp - 1; k < many; k += groups) {
+        const float* q = k < 0 ? first : rest + 2 * k * kPart;
+        const float f = ex2(q[kRows * D + col] - ms);
+        L = fmaf(f, q[kRows * (D + 1) + col], L);
+        O = fmaf(f, q[col * D + d], O);
     }
+    if (groups > 1) {
+        sm[threadIdx.x] = O;
+        if (d == 0) sl[grp] = L;
+        __syncthreads();
+        if (grp > 0) return;
+        for (int g = 1; g < groups; ++g) {
+            O += sm[g * D + d];
+            L += sl[g];
+        }
+    }
+    const int row = j.row + col;
+    const int64_t r = (static_cast<int64_t>(j.token) + row / p.group) * p.q_heads + j.h * p.group + row % p.group;
+    static_cast<T*>(p.out)[r * D + d] = static_cast<T>(L == 0.0f ? 0.0f : O / L);
+    if (d == 0 && p.lse) p.lse[r] = L == 0.0f ? -INFINITY : (ms + log2f(L)) * kLn2;
 }
 
 // acc += the weights of the slots: a thread a slot, the rows of its sequence and head in order.
@@ -798,15 +823,18 @@ kq_status run_attend(const Attend& p, cudaStream_t stream) {
         return KQ_OK;
     }));
     const int grid = std::min(kMaxCtas, num_sms() * (NT == 1 ? 3 : 2));
-    kv_attend_kernel<T, D, NT><<<grid, kThreads, Sh::kSmem, stream>>>(p, 2);
+    kv_attend_kernel<T, D, NT><<<grid, kThreads, Sh::kSmem, stream>>>(p);
     KQ_LAUNCH_CHECK("kv_attend_kernel");
-    KQ_CUDA(launch_after(kv_combine_kernel<T, D, NT>, dim3(static_cast<unsigned>(p.tokens * p.c.kv_heads)), dim3(D), stream, p));
+    // few rows are split over many CTAs: more threads to go through their results
+    const int64_t share = grid / std::max<int64_t>(1, p.tokens * p.c.kv_heads);
+    const int threads = share >= 8 ? 512 : share >= 4 ? 256 : 128;
+    KQ_CUDA(launch_after(kv_combine_kernel<T, D, NT>, dim3(grid, Sh::kRows), dim3(threads), stream, p));
     count_launch();
     return KQ_OK;
 }
 
 size_t al256(size_t b) { return (b + 255) & ~static_cast<size_t>(255); }
-constexpr size_t kBaseBytes = (65536 + 2) * sizeof(int64_t);
+constexpr size_t kJointBytes = kMaxCtas * sizeof(Joint);
 size_t part_bytes(int64_t dim) { return al256(2ull * kMaxCtas * 16 * (dim + 2) * sizeof(float)); }
 
 }  // namespace
@@ -818,7 +846,7 @@ using namespace kq;
 
 extern "C" size_t kq_kv_attend_workspace(int64_t T, int64_t q_heads, int64_t kv_heads, int64_t dim, int64_t S) {
     if (T < 1 || q_heads < 1 || kv_heads < 1 || q_heads % kv_heads || dim < 1 || S < 0) return 0;
-    return al256(kBaseBytes) + part_bytes(dim) + al256(static_cast<size_t>(T) * q_heads * sizeof(float)) +
+    return al256(kJointBytes) + part_bytes(dim) + al256(static_cast<size_t>(T) * q_heads * sizeof(float)) +
            static_cast<size_t>(T) * q_heads * S * sizeof(float);
 }
 
@@ -862,9 +890,9 @@ extern "C" kq_status kq_kv_attend(const kq_kv_cache* cache, const void* q, int d
     p.lens = lens;
     p.scale = scale;
     p.out = out;
-    p.base = reinterpret_cast<int64_t*>(w);
-    p.part = reinterpret_cast<float*>(w + al256(kBaseBytes));
-    float* sums = reinterpret_cast<float*>(w + al256(kBaseBytes) + part_bytes(c.dim));
+    p.joint = reinterpret_cast<Joint*>(w);
+    p.part = reinterpret_cast<float*>(w + al256(kJointBytes));
+    float* sums = reinterpret_cast<float*>(w + al256(kJointBytes) + part_bytes(c.dim));
     p.lse = lse ? lse : acc ? sums : nullptr;
     p.scores = acc ? sums + al256(static_cast<size_t>(T) * q_heads * sizeof(float)) / sizeof(float) : nullptr;
     p.S = S;
