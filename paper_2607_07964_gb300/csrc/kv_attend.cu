@@ -27,9 +27,10 @@
 // each CTA takes an equal, contiguous part of it, so ragged lengths, few sequences and long ones
 // all fill the GPU evenly, without the host knowing the lengths. A CTA that covers a whole
 // (sequence, head) writes its output, parts of one are joined by kv_combine_kernel from at most two
-// partial results a CTA. One producer warp streams tiles through a ring of bulk copies; four
-// consumer warps take 32 tokens of a tile each, with their own running maximum and sums, joined at
-// the end of a segment. Accumulated weights need the finished log-sum, so the scores are kept
+// partial results a CTA. The four warps of a CTA take 32 tokens of a tile each, from a ring of bulk
+// copies of their own that they refill themselves, with their own running maximum and sums, joined
+// at the end of a segment. (A producer warp and a ring for the CTA left room for 12 working
+// warps on an SM instead of 16.) Accumulated weights need the finished log-sum, so the scores are kept
 // (they mostly stay in L2) and kv_weight_kernel turns them into weights.
 #include <algorithm>
 #include <atomic>
@@ -39,9 +40,11 @@
 namespace kq {
 namespace {
 
-constexpr int kWarps = 4;                        // consumer warps
+constexpr int kWarps = 4;
 constexpr int kTile = kWarps * 2 * kGranule;     // tokens of a tile: two granules to a warp
-constexpr int kThreads = 32 * (kWarps + 1);      // and the producer
+constexpr int kThreads = 32 * kWarps;
+constexpr int kStages = 2;                       // of a warp's ring
+constexpr int kAhead = 16;                       // steps whose addresses the lanes of a warp hold, a granule each
 constexpr int kMaxCtas = 640;                    // the workspace holds two partial results of each
 constexpr float kSlack = 8.0f;                   // how far, in powers of two, a weight may pass 1
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
@@ -218,14 +221,14 @@ template <int D, int NT>
 struct Shape {
     static constexpr int kRows = 8 * NT;
     static constexpr int kGranuleBytes = kGranule * (D + 8);
-    static constexpr int kStageBytes = kTile / kGranule * kGranuleBytes;
+    static constexpr int kStageBytes = 2 * kGranuleBytes;
     static constexpr int kMergeRow = D + 4;   // with the rotation by g8 below: no bank conflicts
     static constexpr int kMergeFloats = kWarps * kRows * kMergeRow;
-    static constexpr int kStages = D == 128 ? 3 : 5;
-    static constexpr size_t kSmem = kStages * kStageBytes + kMergeFloats * sizeof(float);
+    static constexpr size_t kSmem = kWarps * kStages * kStageBytes + kMergeFloats * sizeof(float);
+    static constexpr int kCtas = NT == 1 ? 4 : 2;   // on an SM: 128 registers a thread, or up to 255
 };
 
-// A consumer warp's state for a group of NT x 8 query rows. A lane (g8, t4) has columns 2 t4 and
+// A warp's state for a group of NT x 8 query rows. A lane (g8, t4) has columns 2 t4 and
 // 2 t4 + 1 of each 8 rows.
 template <typename T, int D, int NT>
 struct Rows {
@@ -458,17 +461,62 @@ struct Rows {
     }
 };
 
+// A warp's ring of staged granules. Lane l holds the address of granule l & 1 of step l / 2 of the
+// kAhead steps around the next load, and issues that granule's copy itself; the page numbers of the
+// kAhead steps after them are on their way. A warp refills a stage when its lanes have read it, so no
+// other warp is waited for.
+template <int D>
+struct Feed {
+    static constexpr int kBytes = kGranule * (D + 8);
+    const uint8_t* src;   // of this lane's granule, or nullptr
+    int32_t next;         // its page number kAhead steps later
+
+    __device__ __forceinline__ int slot_of(int tile, int64_t k, int warp, int lane) const {
+        return (tile + static_cast<int>(k) + (lane >> 1)) * kTile + warp * 2 * kGranule + (lane & 1) * kGranule;
+    }
+    // the page number of this lane's granule in the steps from k, of a segment of seg tiles
+    __device__ __forceinline__ int32_t fetch(const Attend& p, const Place& at, int64_t k, int64_t seg, int warp, int lane) const {
+        const int slot = slot_of(at.tile, k, warp, lane);
+        if (k + (lane >> 1) >= seg || slot >= at.s.n) return -1;
+        const int32_t id = p.c.table[static_cast<int64_t>(at.b) * p.c.table_ld + slot / p.c.page];
+        if (id >= 0 && id < p.c.pages) return id;
+        record_error(p.info, -KQ_ERR_INVALID_ARG);
+        return 0;
+    }
+    __device__ __forceinline__ void place(const Attend& p, const Place& at, int64_t k, int32_t id, int warp, int lane) {
+        const int slot = slot_of(at.tile, k, warp, lane);
+        src = id < 0 ? nullptr
+                     : p.c.data + (static_cast<int64_t>(id) * p.c.kv_heads + at.h) * kv_head_bytes(p.c) + slot % p.c.page * (D + 8);
+    }
+    // Step k's granules into a stage (k < seg).
+    __device__ __forceinline__ void load(const Attend& p, const Place& at, int64_t k, int64_t seg, uint8_t* stage, uint64_t* bar,
+                                         int warp, int lane) {
+        if (k % kAhead == 0 && k > 0) {
+            place(p, at, k, next, warp, lane);
+            next = fetch(p, at, k + kAhead, seg, warp, lane);
+        }
+        const bool mine = (lane >> 1) == k % kAhead && src != nullptr;
+        const uint32_t who = __ballot_sync(0xffffffffu, mine);
+        if (lane == 0) {
+            if (who) mbar_arrive_expect_tx(bar, __popc(who) * kBytes);
+            else mbar_arrive(bar);
+        }
+        __syncwarp();
+        if (mine) bulk_load(stage + (lane & 1) * kBytes, src, kBytes, bar);
+    }
+};
+
 template <typename T, int D, int NT>
-__global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) kv_attend_kernel(const Attend p) {
+__global__ void __launch_bounds__(kThreads, Shape<D, NT>::kCtas) kv_attend_kernel(const Attend p) {
     using Sh = Shape<D, NT>;
-    constexpr int kRows = Sh::kRows, kStages = Sh::kStages;
+    constexpr int kRows = Sh::kRows;
     constexpr bool kSplit = Rows<T, D, NT>::kSplit;
     constexpr int kWords = Rows<T, D, NT>::kWords;
     extern __shared__ __align__(128) uint8_t smem[];
-    float* const merge = reinterpret_cast<float*>(smem + kStages * Sh::kStageBytes);
-    __shared__ uint64_t full[kStages], empty[kStages];
+    float* const merge = reinterpret_cast<float*>(smem + kWarps * kStages * Sh::kStageBytes);
+    __shared__ uint64_t full[kWarps][kStages];
     __shared__ int abort_flag;
-    __shared__ int64_t scan_tmp[kThreads / 32], found_base;
+    __shared__ int64_t scan_tmp[kWarps], found_base;
     __shared__ int found_b;
     __shared__ float sm_m[kWarps][kRows], sm_l[kWarps][kRows], sm_o[kWarps][kRows];
     __shared__ float sm_e[kWarps];
@@ -476,14 +524,13 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) kv_attend_kernel(co
     const KvView& c = p.c;
 
     // ---- this CTA's part of the work
+    if (lane == 0) {
+        for (int i = 0; i < kStages; ++i) mbar_init(&full[warp][i], 1);
+        fence_mbar_init();
+    }
     if (tid == 0) {
-        for (int i = 0; i < kStages; ++i) {
-            mbar_init(&full[i], 1);
-            mbar_init(&empty[i], kWarps);
-        }
         abort_flag = 0;
         found_b = -1;
-        fence_mbar_init();
         if (blockIdx.x == 0 && (p.start[0] != 0 || p.start[c.batch] != p.tokens)) record_error(p.info, -KQ_ERR_INVALID_ARG);
     }
     // The sequences' tiles, kThreads of them at a time: the total, then the one that holds this CTA's first.
@@ -531,66 +578,25 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) kv_attend_kernel(co
         }
     }
 
-    if (warp == kWarps) {
-        // ---- producer: tiles into the ring; lane l holds the page of the l-th page ahead
-        int it = 0;
-        bool ok = true;
-        int page_b = -1, page_at = 0, page_id = 0;
-        for (int64_t w = w0; w < w1 && ok; ++w, ++it) {
-            const int slot0 = at.tile * kTile, grans = (min(kTile, at.s.n - slot0) + kGranule - 1) / kGranule;
-            const int stage = it % kStages;
-            if (it >= kStages) {
-                ok = lane != 0 || mbar_wait(&empty[stage], ((it / kStages) & 1) ^ 1, &abort_flag);
-                ok = __shfl_sync(0xffffffffu, ok, 0);
-                if (!ok) break;
-            }
-            if (lane == 0) {
-                if (grans > 0) mbar_arrive_expect_tx(&full[stage], grans * Sh::kGranuleBytes);
-                else mbar_arrive(&full[stage]);
-            }
-            for (int g = 0; g < grans;) {
-                const int slot = slot0 + g * kGranule, pg = slot / c.page;
-                if (page_b != at.b || pg < page_at || pg >= page_at + 32) {
-                    page_b = at.b;
-                    page_at = pg;
-                    page_id = 0;
-                    if (pg + lane <= (at.s.n - 1) / c.page) {
-                        page_id = c.table[static_cast<int64_t>(at.b) * c.table_ld + pg + lane];
-                        if (page_id < 0 || page_id >= c.pages) {
-                            record_error(p.info, -KQ_ERR_INVALID_ARG);
-                            page_id = 0;
-                        }
-                    }
-                }
-                const int id = __shfl_sync(0xffffffffu, page_id, pg - page_at);
-                const int in_page = slot - pg * c.page;
-                const int run = min(grans - g, (c.page - in_page) / kGranule);
-                if (lane == 0)
-                    bulk_load(smem + stage * Sh::kStageBytes + g * Sh::kGranuleBytes,
-                              c.data + (static_cast<int64_t>(id) * c.kv_heads + at.h) * kv_head_bytes(c) + in_page * (D + 8),
-                              run * Sh::kGranuleBytes, &full[stage]);
-                g += run;
-            }
-            if (++at.tile == at.s.tiles) next_item<kRows>(p, at);
-        }
-        // a wait gave up somewhere: leave only when this CTA's copies have landed
-        __syncthreads();
-        if (abort_flag && lane == 0) {
-            record_error(p.info, -KQ_ERR_TIMEOUT);
-            int none = 0;
-            for (int i = max(0, it - kStages); i < it; ++i) mbar_wait(&full[i % kStages], (i / kStages) & 1, &none);
-        }
-        return;
-    }
-
-    // ---- consumers
     const int g8 = lane >> 2, t4 = lane & 3;
-    int it = 0;
+    uint8_t* const ring = smem + warp * kStages * Sh::kStageBytes;
+    int it = 0;        // steps of this warp so far: its stage and the parity of its barrier
     // After a wait that gave up the warps go on through the same steps without waiting (the result is
     // reported as failed), so that none of them is left alone at a barrier.
+    bool fine_waits = true;
+    int issued = 0;
     for (int64_t w = w0; w < w1;) {
         const int64_t seg = min(w1 - w, static_cast<int64_t>(at.s.tiles - at.tile));
         const int rows = min(kRows, at.s.nq * p.group - at.rt * kRows);
+        Feed<D> feed;
+        feed.place(p, at, 0, feed.fetch(p, at, 0, seg, warp, lane), warp, lane);
+        feed.next = feed.fetch(p, at, kAhead, seg, warp, lane);
+#pragma unroll
+        for (int k = 0; k < kStages; ++k)
+            if (k < seg && fine_waits) {
+                const int stage = issued++ % kStages;
+                feed.load(p, at, k, seg, ring + stage * Sh::kStageBytes, &full[warp][stage], warp, lane);
+            }
         // q: lane (g8, t4) holds dimensions t4 D / 4 .. of row g8, each word of 8 as two k steps: (0, 4 | 1, 5) and
         // (2, 6 | 3, 7); the odd ones are divided by 16 where their nibbles sit four bits up
         Rows<T, D, NT> R;
@@ -600,28 +606,25 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) kv_attend_kernel(co
             const bool real = nt * 8 + g8 < rows;
             const T* src = static_cast<const T*>(p.q) + (at.s.first + (real ? row / p.group : 0)) * p.q_token +
                            (static_cast<int64_t>(at.h) * p.group + (real ? row % p.group : 0)) * p.q_head + t4 * (D / 4);
-            float xs[kWords][8], top = 0.0f, sum = 0.0f;
-            bool fine = true;
+            float xs[kWords][8], sum = 0.0f;
+            uint32_t top = 0;   // as bits: an infinity or a NaN is above every number
 #pragma unroll
             for (int i = 0; i < kWords; ++i) load8(src + 8 * i, p.q_vec, xs[i]);
 #pragma unroll
             for (int i = 0; i < kWords; ++i)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    top = fmaxf(top, fabsf(xs[i][j]));
+                    top = max(top, __float_as_uint(xs[i][j]) & 0x7FFFFFFFu);
                     sum += xs[i][j];
-                    fine &= fabsf(xs[i][j]) <= 3.402823466e38f;
                 }
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
             sum += __shfl_xor_sync(0xffffffffu, sum, 1);
             sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-            int bad = !fine;
-            bad |= __shfl_xor_sync(0xffffffffu, bad, 1);
-            bad |= __shfl_xor_sync(0xffffffffu, bad, 2);
+            const bool bad = top >= 0x7F800000u;
             // 2^e brings the largest below 2^14; both powers stay normal. The sign of the scale goes to q, so that
             // alpha > 0 and scores compare before they are scaled.
-            const int e = min(100, max(-113, 13 - static_cast<int>((__float_as_uint(top) >> 23) & 255) + 127));
+            const int e = min(100, max(-113, 13 - static_cast<int>(top >> 23) + 127));
             const float up = copysignf(__uint_as_float(static_cast<uint32_t>(e + 127) << 23), p.scale);
             const float f = fmaxf(fabsf(p.scale) * kLog2e, 0x1p-126f);
             // score / ln 2 = f (s sum(q c) + o sum(q)) with sum(q c) = S / unit
@@ -662,15 +665,19 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) kv_attend_kernel(co
 
         for (int64_t k = 0; k < seg; ++k, ++it) {
             const int stage = it % kStages;
-            const bool ok = __all_sync(0xffffffffu, mbar_wait(&full[stage], (it / kStages) & 1, &abort_flag));
+            uint8_t* gr = ring + stage * Sh::kStageBytes;
+            const bool ok = __all_sync(0xffffffffu, mbar_wait(&full[warp][stage], (it / kStages) & 1, &abort_flag));
             const int slot = (at.tile + static_cast<int>(k)) * kTile + warp * 2 * kGranule;
-            const uint8_t* gr = smem + stage * Sh::kStageBytes + warp * 2 * Sh::kGranuleBytes;
+            fine_waits &= ok;
             if (ok && slot < at.s.n) {   // uniform over the warp
                 if (slot + 2 * kGranule <= least) R.template step<false>(gr, slot, at.s.n, g8, t4, p.scores, p.group);
                 else R.template step<true>(gr, slot, at.s.n, g8, t4, p.scores, p.group);
             }
             __syncwarp();
-            if (lane == 0) mbar_arrive(&empty[stage]);
+            if (fine_waits && k + kStages < seg) {
+                feed.load(p, at, k + kStages, seg, gr, &full[warp][stage], warp, lane);
+                ++issued;
+            }
         }
 
         // ---- join the warps' sums
@@ -697,12 +704,12 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) kv_attend_kernel(co
             }
         // 2^24 of subnormal codes, 2^-6 2^(ev + 1 - 127) of the weights
         if (lane == 0) sm_e[warp] = __uint_as_float(static_cast<uint32_t>(min(R.ev - (kSplit ? 132 : 108), 127) + 127) << 23);
-        asm volatile("bar.sync 1, 128;" ::: "memory");
+        __syncthreads();
         const bool whole = seg == at.s.tiles;
         float* part = p.part + (2 * static_cast<int64_t>(blockIdx.x) + (at.tile == 0 && w > w0 ? 1 : 0)) * (kRows * (D + 2));
         const int d = tid % D, dg = d / (D / 8), di = d % (D / 8) / 2;
         const float* mine = merge + dg * (D / 8) + 2 * ((di + dg) % (D / 16)) + (d & 1);
-        for (int col = tid / D; col < rows; col += 128 / D) {
+        for (int col = tid / D; col < rows; col += kThreads / D) {
             float M = -INFINITY;
 #pragma unroll
             for (int i = 0; i < kWarps; ++i) M = fmaxf(M, sm_m[i][col]);
@@ -727,12 +734,16 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) kv_attend_kernel(co
                 }
             }
         }
-        asm volatile("bar.sync 1, 128;" ::: "memory");
+        __syncthreads();
         w += seg;
         at.tile += static_cast<int>(seg) - 1;
         if (++at.tile == at.s.tiles) next_item<kRows>(p, at);
     }
-    __syncthreads();
+    if (!fine_waits && lane == 0) {   // leave only when this warp's copies have landed
+        record_error(p.info, -KQ_ERR_TIMEOUT);
+        int none = 0;
+        for (int i = max(0, issued - kStages); i < issued; ++i) mbar_wait(&full[warp][i % kStages], (i / kStages) & 1, &none);
+    }
 }
 
 // Joins the partial results of rows that more than one CTA worked on: block (c, column) for the rows that
@@ -822,7 +833,7 @@ kq_status run_attend(const Attend& p, cudaStream_t stream) {
                                      static_cast<int>(Sh::kSmem)));
         return KQ_OK;
     }));
-    const int grid = std::min(kMaxCtas, num_sms() * (NT == 1 ? 3 : 2));
+    const int grid = std::min(kMaxCtas, num_sms() * Sh::kCtas);
     kv_attend_kernel<T, D, NT><<<grid, kThreads, Sh::kSmem, stream>>>(p);
     KQ_LAUNCH_CHECK("kv_attend_kernel");
     // few rows are split over many CTAs: more threads to go through their results
