@@ -34,6 +34,7 @@
 // (they mostly stay in L2) and kv_weight_kernel turns them into weights.
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "kv_common.cuh"
 
@@ -47,6 +48,8 @@ constexpr int kStages = 2;                       // of a warp's ring
 constexpr int kAhead = 16;                       // steps whose addresses the lanes of a warp hold, a granule each
 constexpr int kMaxCtas = 640;                    // the workspace holds two partial results of each
 constexpr float kSlack = 8.0f;                   // how far, in powers of two, a weight may pass 1
+constexpr float kNone = -3.0e38f;                // a maximum over nothing: finite, so that differences with it are numbers
+constexpr int kSettle = 8;                       // steps whose middle-code sums are taken off at once
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 __device__ __forceinline__ float ex2(float x) {
@@ -239,11 +242,26 @@ struct Rows {
     int32_t lim[NT][2];                              // slots seen
     int64_t put[NT][2];                              // where scores go
     float o[NT][D / 16][4], m[NT][2], l[NT][2], off[NT][2];
+    float mid[NT][4];                                // 8 times the sum of the weights in o (codes not centred)
     int ev;                                          // biased exponent that the value scales are held to
 
+    // o = corr (o - mid), mid = 0
+    __device__ __forceinline__ void settle_mid(int nt, const float (&corr)[2]) {
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (kSplit) o[nt][i][j] *= corr[j & 1];
+                else o[nt][i][j] = corr[j & 1] * fmaf(j < 2 ? -1.0f : -16.0f, mid[nt][j], o[nt][i][j]);
+            }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) mid[nt][j] = 0.0f;
+    }
+
     // Two granules: 32 tokens from slot `slot`, staged at gr. MASK: some slot may be unseen by some row.
+    // settle: take the middle code off the sums in any case.
     template <bool MASK>
-    __device__ __forceinline__ void step(const uint8_t* gr, int slot, int n, int g8, int t4, float* scores, int group) {
+    __device__ __forceinline__ void step(const uint8_t* gr, int slot, int n, int g8, int t4, float* scores, int group, bool settle) {
         // the token of A row g8 (and 8 more of row g8 + 8), chosen so that the tokens 2 t4, 2 t4 + 1, 2 t4 + 8 and
         // 2 t4 + 9 of the weights' fragment are rows t4, 7 - t4, 8 + t4, 15 - t4: neighbouring lanes
         // then read neighbouring rows of codes
@@ -347,36 +365,32 @@ struct Rows {
                 move |= mx[nt][k] > m[nt][k] + kSlack;
             }
         move |= static_cast<int>(__float_as_uint(vmax) >> 23) > ev;
-        float corr[NT][2];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) corr[nt][0] = corr[nt][1] = 1.0f;
-        if (__any_sync(0xffffffffu, move)) {
+        if (settle || __any_sync(0xffffffffu, move)) {
             const uint32_t vb = vmax < INFINITY ? __float_as_uint(vmax) : 0u;
             const int en = max(ev, static_cast<int>(__reduce_max_sync(0xffffffffu, vb) >> 23));
             const float drop = __uint_as_float(static_cast<uint32_t>(max(0, 127 + ev - en)) << 23);
             ev = en;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int nt = 0; nt < NT; ++nt) {
+                float corr[2];
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     float x = mx[nt][k];
 #pragma unroll
                     for (int sh = 4; sh < 32; sh <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, sh));
-                    const float mn = fmaxf(m[nt][k], x);
-                    const float r = mn == -INFINITY ? 1.0f : ex2(m[nt][k] - mn);
+                    const float mn = fmaxf(m[nt][k], x), r = ex2(m[nt][k] - mn);
                     m[nt][k] = mn;
                     l[nt][k] *= r;
                     off[nt][k] *= r;
-                    corr[nt][k] = r * drop;
+                    corr[k] = r * drop;
                 }
+                settle_mid(nt, corr);
+            }
         }
         const float inv = __uint_as_float(static_cast<uint32_t>(259 - ev) << 23);   // 2^6 / 2^(ev + 1 - 127)
         uint32_t b[2][NT][2], e[2][NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            float ms[2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) ms[k] = m[nt][k] == -INFINITY ? 0.0f : m[nt][k];
 #pragma unroll
             for (int gi = 0; gi < 2; ++gi)
 #pragma unroll
@@ -386,7 +400,7 @@ struct Rows {
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
                         const float x = s[gi][nt][2 * hf + k];
-                        const float pr = ex2(fmaf(alpha[nt][k], x, -ms[k]));
+                        const float pr = ex2(fmaf(alpha[nt][k], x, -m[nt][k]));
                         l[nt][k] += pr;
                         if (MASK) {
                             const bool in = slot + 16 * gi + tok + 8 * hf < lim[nt][k];
@@ -405,18 +419,10 @@ struct Rows {
                     }
                     b[gi][nt][hf] = transpose8(h);
                 }
-            if constexpr (!kSplit) {
-                // 8 times the weights' sum, in every row of the accumulator's layout
-                float mid[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            if constexpr (!kSplit) {   // in every row of the accumulator's layout
 #pragma unroll
                 for (int gi = 0; gi < 2; ++gi)
-                    mma_f16(mid, 0x00080008u, 0x00080008u, 0x00080008u, 0x00080008u, b[gi][nt][0], b[gi][nt][1]);
-                const float m16[2] = {16.0f * mid[0], 16.0f * mid[1]};
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        o[nt][i][j] = fmaf(o[nt][i][j], corr[nt][j & 1], j < 2 ? -mid[j] : -m16[j & 1]);
+                    mma_f16(mid[nt], 0x00080008u, 0x00080008u, 0x00080008u, 0x00080008u, b[gi][nt][0], b[gi][nt][1]);
             }
         }
         // values: words of dimensions 16 g8 .. (D = 128) or 8 g8 .. (D = 64) of four tokens
@@ -451,7 +457,7 @@ struct Rows {
                             mma_f16(u, a0, a1, a2, a3, e[gi][nt][0], e[gi][nt][1]);
                             mma_f16(u, a0, a1, a2, a3, b[gi][nt][0], b[gi][nt][1]);
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) ac[r] = gi == 0 ? fmaf(ac[r], corr[nt][r & 1], u[r]) : ac[r] + u[r];
+                            for (int r = 0; r < 4; ++r) ac[r] += u[r];
                         } else {
                             mma_f16(ac, a0, a1, a2, a3, b[gi][nt][0], b[gi][nt][1]);
                         }
@@ -462,47 +468,54 @@ struct Rows {
 };
 
 // A warp's ring of staged granules. Lane l holds the address of granule l & 1 of step l / 2 of the
-// kAhead steps around the next load, and issues that granule's copy itself; the page numbers of the
-// kAhead steps after them are on their way. A warp refills a stage when its lanes have read it, so no
+// kAhead steps around the next load; the page numbers of the kAhead steps after them are on their
+// way. A warp refills a stage when its lanes have read it, so no
 // other warp is waited for.
 template <int D>
 struct Feed {
     static constexpr int kBytes = kGranule * (D + 8);
-    const uint8_t* src;   // of this lane's granule, or nullptr
+    const uint8_t* src;   // of this lane's granule
     int32_t next;         // its page number kAhead steps later
 
-    __device__ __forceinline__ int slot_of(int tile, int64_t k, int warp, int lane) const {
-        return (tile + static_cast<int>(k) + (lane >> 1)) * kTile + warp * 2 * kGranule + (lane & 1) * kGranule;
+    __device__ __forceinline__ int slot_of(int tile, int k, int warp, int lane) const {
+        return (tile + k + (lane >> 1)) * kTile + warp * 2 * kGranule + (lane & 1) * kGranule;
     }
     // the page number of this lane's granule in the steps from k, of a segment of seg tiles
-    __device__ __forceinline__ int32_t fetch(const Attend& p, const Place& at, int64_t k, int64_t seg, int warp, int lane) const {
+    __device__ __forceinline__ int32_t fetch(const Attend& p, const Place& at, int k, int seg, int warp, int lane) const {
         const int slot = slot_of(at.tile, k, warp, lane);
-        if (k + (lane >> 1) >= seg || slot >= at.s.n) return -1;
+        if (k + (lane >> 1) >= seg || slot >= at.s.n) return 0;
         const int32_t id = p.c.table[static_cast<int64_t>(at.b) * p.c.table_ld + slot / p.c.page];
         if (id >= 0 && id < p.c.pages) return id;
         record_error(p.info, -KQ_ERR_INVALID_ARG);
         return 0;
     }
-    __device__ __forceinline__ void place(const Attend& p, const Place& at, int64_t k, int32_t id, int warp, int lane) {
+    __device__ __forceinline__ void place(const Attend& p, const Place& at, int k, int32_t id, int warp, int lane) {
         const int slot = slot_of(at.tile, k, warp, lane);
-        src = id < 0 ? nullptr
-                     : p.c.data + (static_cast<int64_t>(id) * p.c.kv_heads + at.h) * kv_head_bytes(p.c) + slot % p.c.page * (D + 8);
+        src = p.c.data + (static_cast<int64_t>(id) * p.c.kv_heads + at.h) * kv_head_bytes(p.c) + slot % p.c.page * (D + 8);
     }
-    // Step k's granules into a stage (k < seg).
-    __device__ __forceinline__ void load(const Attend& p, const Place& at, int64_t k, int64_t seg, uint8_t* stage, uint64_t* bar,
-                                         int warp, int lane) {
+    // Step k's granules into a stage (k < seg). Both are one run unless a page can end between them.
+    __device__ __forceinline__ void load(const Attend& p, const Place& at, int k, int seg, uint8_t* stage, uint64_t* bar, int warp,
+                                         int lane) {
         if (k % kAhead == 0 && k > 0) {
             place(p, at, k, next, warp, lane);
             next = fetch(p, at, k + kAhead, seg, warp, lane);
         }
-        const bool mine = (lane >> 1) == k % kAhead && src != nullptr;
-        const uint32_t who = __ballot_sync(0xffffffffu, mine);
+        const int left = at.s.n - (at.tile + k) * kTile - warp * 2 * kGranule;
+        const int many = left > kGranule ? 2 : left > 0 ? 1 : 0;
+        const uint64_t a = __shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(src), 2 * (k % kAhead));
+        uint64_t a2 = a + kBytes;
+        if (p.c.page % (2 * kGranule)) a2 = __shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(src), 2 * (k % kAhead) + 1);
         if (lane == 0) {
-            if (who) mbar_arrive_expect_tx(bar, __popc(who) * kBytes);
-            else mbar_arrive(bar);
+            if (many == 0) {
+                mbar_arrive(bar);
+            } else {
+                mbar_arrive_expect_tx(bar, many * kBytes);
+                const bool run = many == 1 || a2 == a + kBytes;
+                bulk_load(stage, reinterpret_cast<const void*>(a), run ? many * kBytes : kBytes, bar);
+                if (!run) bulk_load(stage + kBytes, reinterpret_cast<const void*>(a2), kBytes, bar);
+            }
         }
         __syncwarp();
-        if (mine) bulk_load(stage + (lane & 1) * kBytes, src, kBytes, bar);
     }
 };
 
@@ -586,7 +599,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT>::kCtas) kv_attend_kerne
     bool fine_waits = true;
     int issued = 0;
     for (int64_t w = w0; w < w1;) {
-        const int64_t seg = min(w1 - w, static_cast<int64_t>(at.s.tiles - at.tile));
+        const int seg = static_cast<int>(min(w1 - w, static_cast<int64_t>(at.s.tiles - at.tile)));
         const int rows = min(kRows, at.s.nq * p.group - at.rt * kRows);
         Feed<D> feed;
         feed.place(p, at, 0, feed.fetch(p, at, 0, seg, warp, lane), warp, lane);
@@ -653,36 +666,51 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT>::kCtas) kv_attend_kerne
                 const int i = crow / p.group;
                 R.lim[nt][k] = col < rows ? visible(at.s.n, at.s.nq, i) : 0;
                 R.put[nt][k] = ((static_cast<int64_t>(at.s.first + i) * c.kv_heads + at.h) * p.S) * p.group + crow % p.group;
-                R.m[nt][k] = -INFINITY, R.l[nt][k] = 0.0f, R.off[nt][k] = 0.0f;
+                R.m[nt][k] = kNone, R.l[nt][k] = 0.0f, R.off[nt][k] = 0.0f;
             }
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) R.o[nt][i][j] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) R.mid[nt][j] = 0.0f;
         }
         R.ev = 20;
         const int least = visible(at.s.n, at.s.nq, at.rt * kRows / p.group);   // what the first row sees, the others see
 
-        for (int64_t k = 0; k < seg; ++k, ++it) {
+        // The steps that every row sees in full, then those with an end: two loops, so that the first one
+        // carries its sums in place.
+        auto turn = [&](int k, auto masked) {
             const int stage = it % kStages;
             uint8_t* gr = ring + stage * Sh::kStageBytes;
-            const bool ok = __all_sync(0xffffffffu, mbar_wait(&full[warp][stage], (it / kStages) & 1, &abort_flag));
-            const int slot = (at.tile + static_cast<int>(k)) * kTile + warp * 2 * kGranule;
+            uint64_t* bar = &full[warp][stage];
+            bool ok = true;
+            if (__any_sync(0xffffffffu, !mbar_try_wait(bar, (it / kStages) & 1)))
+                ok = __all_sync(0xffffffffu, mbar_wait(bar, (it / kStages) & 1, &abort_flag));
             fine_waits &= ok;
-            if (ok && slot < at.s.n) {   // uniform over the warp
-                if (slot + 2 * kGranule <= least) R.template step<false>(gr, slot, at.s.n, g8, t4, p.scores, p.group);
-                else R.template step<true>(gr, slot, at.s.n, g8, t4, p.scores, p.group);
+            const int slot = (at.tile + k) * kTile + warp * 2 * kGranule;
+            if constexpr (decltype(masked)::value) {
+                if (ok && slot < at.s.n) R.template step<true>(gr, slot, at.s.n, g8, t4, p.scores, p.group, true);
+            } else {
+                R.template step<false>(gr, slot, at.s.n, g8, t4, p.scores, p.group, k % kSettle == 0);
             }
             __syncwarp();
             if (fine_waits && k + kStages < seg) {
-                feed.load(p, at, k + kStages, seg, gr, &full[warp][stage], warp, lane);
+                feed.load(p, at, k + kStages, seg, gr, bar, warp, lane);
                 ++issued;
             }
-        }
+            ++it;
+        };
+        const int whole_steps = min(seg, max(0, (least - warp * 2 * kGranule - 2 * kGranule) / kTile + 1 - at.tile));
+        int k = 0;
+        for (; k < whole_steps && (least >= (warp + 1) * 2 * kGranule); ++k) turn(k, std::false_type());
+        for (; k < seg; ++k) turn(k, std::true_type());
 
         // ---- join the warps' sums
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt) {
+            const float one[2] = {1.0f, 1.0f};
+            if constexpr (!kSplit) R.settle_mid(nt, one);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
 #pragma unroll
@@ -702,6 +730,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT>::kCtas) kv_attend_kerne
                                                2 * ((i + g8) % (D / 16))) =
                         make_float2(R.o[nt][i][k], R.o[nt][i][2 + k] * (kSplit ? 1.0f : 0.0625f));
             }
+        }
         // 2^24 of subnormal codes, 2^-6 2^(ev + 1 - 127) of the weights
         if (lane == 0) sm_e[warp] = __uint_as_float(static_cast<uint32_t>(min(R.ev - (kSplit ? 132 : 108), 127) + 127) << 23);
         __syncthreads();
@@ -710,14 +739,13 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT>::kCtas) kv_attend_kerne
         const int d = tid % D, dg = d / (D / 8), di = d % (D / 8) / 2;
         const float* mine = merge + dg * (D / 8) + 2 * ((di + dg) % (D / 16)) + (d & 1);
         for (int col = tid / D; col < rows; col += kThreads / D) {
-            float M = -INFINITY;
+            float M = kNone;
 #pragma unroll
             for (int i = 0; i < kWarps; ++i) M = fmaxf(M, sm_m[i][col]);
-            const float ms = M == -INFINITY ? 0.0f : M;
             float L = 0.0f, O = 0.0f;
 #pragma unroll
             for (int i = 0; i < kWarps; ++i) {
-                const float f = ex2(sm_m[i][col] - ms);
+                const float f = ex2(sm_m[i][col] - M);
                 L = fmaf(f, sm_l[i][col], L);
                 O = fmaf(f, fmaf(mine[(i * kRows + col) * Sh::kMergeRow], sm_e[i], sm_o[i][col]), O);
             }
@@ -725,7 +753,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT>::kCtas) kv_attend_kerne
                 const int row = at.rt * kRows + col;
                 const int64_t r = (static_cast<int64_t>(at.s.first) + row / p.group) * p.q_heads + at.h * p.group + row % p.group;
                 static_cast<T*>(p.out)[r * D + d] = static_cast<T>(L == 0.0f ? 0.0f : O / L);
-                if (d == 0 && p.lse) p.lse[r] = L == 0.0f ? -INFINITY : (ms + log2f(L)) * kLn2;
+                if (d == 0 && p.lse) p.lse[r] = L == 0.0f ? -INFINITY : (M + log2f(L)) * kLn2;
             } else {
                 part[col * D + d] = O;
                 if (d == 0) {
@@ -746,8 +774,8 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT>::kCtas) kv_attend_kerne
     }
 }
 
-// Joins the partial results of rows that more than one CTA worked on: block (c, column) for the rows that
-// CTA c went on with, its threads the D dimensions, in groups that share the partial results.
+// Joins the partial results of rows that more than one CTA worked on: blocks (c, i) for the rows that
+// CTA c went on with, columns i, i + gridDim.y ..; a thread for each dimension, in groups.
 template <typename T, int D, int NT>
 __global__ void __launch_bounds__(512) kv_combine_kernel(const Attend p) {
     constexpr int kRows = 8 * NT;
@@ -755,40 +783,43 @@ __global__ void __launch_bounds__(512) kv_combine_kernel(const Attend p) {
     pdl_wait();
     pdl_launch_dependents();
     const Joint j = p.joint[blockIdx.x];
-    const int col = blockIdx.y;
-    if (j.last == 0 || col >= j.rows) return;
+    if (j.last == 0) return;
     const int d = threadIdx.x % D, grp = threadIdx.x / D, groups = blockDim.x / D;
     constexpr int64_t kPart = kRows * (D + 2);
     const int64_t c = blockIdx.x;
     const float* first = p.part + (2 * (c - 1) + j.first_slot) * kPart;
     const float* rest = p.part + 2 * c * kPart;   // the others begin with these rows
-    const int64_t many = j.last - c + 1;
-    float M = first[kRows * D + col];
+    const int many = static_cast<int>(j.last - c) + 1;
+    // a few results: the groups of threads take a column each; many: they share a column's results
+    const bool share = many > 4 && groups > 1;
+    for (int col = blockIdx.y + (share ? 0 : grp * gridDim.y); col < j.rows; col += gridDim.y * (share ? 1 : groups)) {
+        float M = first[kRows * D + col];
 #pragma unroll 4
-    for (int64_t k = 0; k < many; ++k) M = fmaxf(M, rest[2 * k * kPart + kRows * D + col]);
-    const float ms = M == -INFINITY ? 0.0f : M;
-    float L = 0.0f, O = 0.0f;
+        for (int k = 0; k < many; ++k) M = fmaxf(M, rest[2 * k * kPart + kRows * D + col]);
+        float L = 0.0f, O = 0.0f;
 #pragma unroll 4
-    for (int64_t k = grp - 1; k < many; k += groups) {
-        const float* q = k < 0 ? first : rest + 2 * k * kPart;
-        const float f = ex2(q[kRows * D + col] - ms);
-        L = fmaf(f, q[kRows * (D + 1) + col], L);
-        O = fmaf(f, q[col * D + d], O);
-    }
-    if (groups > 1) {
-        sm[threadIdx.x] = O;
-        if (d == 0) sl[grp] = L;
-        __syncthreads();
-        if (grp > 0) return;
-        for (int g = 1; g < groups; ++g) {
-            O += sm[g * D + d];
-            L += sl[g];
+        for (int k = share ? grp - 1 : -1; k < many; k += share ? groups : 1) {
+            const float* q = k < 0 ? first : rest + 2 * k * kPart;
+            const float f = ex2(q[kRows * D + col] - M);
+            L = fmaf(f, q[kRows * (D + 1) + col], L);
+            O = fmaf(f, q[col * D + d], O);
         }
+        if (share) {
+            __syncthreads();
+            sm[threadIdx.x] = O;
+            if (d == 0) sl[grp] = L;
+            __syncthreads();
+            if (grp > 0) continue;
+            for (int g = 1; g < groups; ++g) {
+                O += sm[g * D + d];
+                L += sl[g];
+            }
+        }
+        const int row = j.row + col;
+        const int64_t r = (static_cast<int64_t>(j.token) + row / p.group) * p.q_heads + j.h * p.group + row % p.group;
+        static_cast<T*>(p.out)[r * D + d] = static_cast<T>(L == 0.0f ? 0.0f : O / L);
+        if (d == 0 && p.lse) p.lse[r] = L == 0.0f ? -INFINITY : (M + log2f(L)) * kLn2;
     }
-    const int row = j.row + col;
-    const int64_t r = (static_cast<int64_t>(j.token) + row / p.group) * p.q_heads + j.h * p.group + row % p.group;
-    static_cast<T*>(p.out)[r * D + d] = static_cast<T>(L == 0.0f ? 0.0f : O / L);
-    if (d == 0 && p.lse) p.lse[r] = L == 0.0f ? -INFINITY : (ms + log2f(L)) * kLn2;
 }
 
 // acc += the weights of the slots: a thread a slot, the rows of its sequence and head in order.
@@ -836,10 +867,9 @@ kq_status run_attend(const Attend& p, cudaStream_t stream) {
     const int grid = std::min(kMaxCtas, num_sms() * Sh::kCtas);
     kv_attend_kernel<T, D, NT><<<grid, kThreads, Sh::kSmem, stream>>>(p);
     KQ_LAUNCH_CHECK("kv_attend_kernel");
-    // few rows are split over many CTAs: more threads to go through their results
+    // few rows are split over many CTAs: a block for each column, to go through their results
     const int64_t share = grid / std::max<int64_t>(1, p.tokens * p.c.kv_heads);
-    const int threads = share >= 8 ? 512 : share >= 4 ? 256 : 128;
-    KQ_CUDA(launch_after(kv_combine_kernel<T, D, NT>, dim3(grid, Sh::kRows), dim3(threads), stream, p));
+    KQ_CUDA(launch_after(kv_combine_kernel<T, D, NT>, dim3(grid, share >= 4 ? Sh::kRows : 2), dim3(512), stream, p));
     count_launch();
     return KQ_OK;
 }
