@@ -23,15 +23,15 @@
 // lane take its operands straight from the staged bytes in the mma layout (a lane's 16 bytes of a
 // key row are its share of every k step; the order of the dimensions inside a product is free).
 //
-// Split. The work is the list of 128-token tiles of every (sequence, head, group of query rows), and
-// each CTA takes an equal, contiguous part of it, so ragged lengths, few sequences and long ones
-// all fill the GPU evenly, without the host knowing the lengths. A CTA that covers a whole
-// (sequence, head) writes its output, parts of one are joined by kv_combine_kernel from at most two
-// partial results a CTA. The four warps of a CTA take 32 tokens of a tile each, from a ring of bulk
-// copies of their own that they refill themselves, with their own running maximum and sums, joined
-// at the end of a segment. (A producer warp and a ring for the CTA left room for 12 working
-// warps on an SM instead of 16.) Accumulated weights need the finished log-sum, so the scores are kept
-// (they mostly stay in L2) and kv_weight_kernel turns them into weights.
+// Split. The work is the list of 32-token steps of every (sequence, head, group of query rows), and
+// each warp takes an equal, contiguous part of it, so ragged lengths, few sequences and long ones all
+// fill the GPU evenly, without the host knowing the lengths. A warp streams its tokens through a
+// ring of bulk copies that it refills itself and shares nothing with the other warps: 16 of them on
+// an SM, none waiting for another. One that covers all of a (sequence, head) writes its output;
+// parts are joined by kv_combine_kernel from at most two partial results a warp. (Four warps that
+// shared tiles and joined their sums in shared memory lost about 10 us at every change of sequence.)
+// Accumulated weights need the finished log-sum, so the scores are kept (they mostly stay in L2) and
+// kv_weight_kernel turns them into weights.
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -42,11 +42,12 @@ namespace kq {
 namespace {
 
 constexpr int kWarps = 4;
-constexpr int kTile = kWarps * 2 * kGranule;     // tokens of a tile: two granules to a warp
+constexpr int kStep = 2 * kGranule;             // tokens of a step
 constexpr int kThreads = 32 * kWarps;
-constexpr int kStages = 2;                       // of a warp's ring
+constexpr int kStages = 3;                       // steps in a warp's ring
 constexpr int kAhead = 16;                       // steps whose addresses the lanes of a warp hold, a granule each
-constexpr int kMaxCtas = 640;                    // the workspace holds two partial results of each
+constexpr int kMaxRows = 40960;                  // rows of all pieces together: the workspace holds two results of each
+constexpr int kMinSteps = 2;                     // of a piece, where there is little work
 constexpr float kSlack = 8.0f;                   // how far, in powers of two, a weight may pass 1
 constexpr float kNone = -3.0e38f;                // a maximum over nothing: finite, so that differences with it are numbers
 constexpr int kSettle = 8;                       // steps whose middle-code sums are taken off at once
@@ -132,22 +133,23 @@ struct Attend {
     float* scores;                     // [T][kv_heads][S][group], in units of ln 2, or nullptr
     int64_t S;
     int64_t cap;                       // slots a sequence may have: the table's, and S with weights
-    struct Joint* joint;               // [CTAs]
-    float* part;                       // [2 CTAs][rows][D + 2]: sums, maximum, sum of weights
+    struct Joint* joint;               // of each item in the list of work
+    int64_t* items;                    // how many there are
+    float* part;                       // [2 pieces][rows][D + 2]: sums, maximum, sum of weights
     int* info;
 };
 
-// What CTA c leaves to kv_combine_kernel when it is the first to go on with rows that CTA c - 1 began.
+// What the warp that begins the rows of an item leaves to kv_combine_kernel.
 struct Joint {
-    int32_t last;            // the last CTA of these rows, or 0: nothing to join
-    int32_t first_slot;      // which of CTA c - 1's two partial results
+    int32_t first, last;     // the pieces that share them; equal: nothing to join
+    int32_t slot;            // which of the first piece's two partial results
     int32_t h, row, rows;    // head, first query row of the sequence, number of rows
     int32_t token;           // the sequence's first token
 };
 
 // Sequence b's share of the work.
 struct Seq {
-    int32_t nq, rows_tiles, tiles;   // queries, groups of ROWS query rows, tiles (at least 1)
+    int32_t nq, rows_tiles, steps;   // queries, groups of ROWS query rows, steps (at least 1)
     int32_t n;                       // length
     int32_t first;                   // its first token
 };
@@ -163,42 +165,55 @@ __device__ __forceinline__ Seq sequence(const Attend& p, int b, int* info) {
         s.nq = 0;
     }
     s.rows_tiles = static_cast<int32_t>((static_cast<int64_t>(s.nq) * p.group + ROWS - 1) / ROWS);
-    s.tiles = max(1, (s.n + kTile - 1) / kTile);
+    s.steps = max(1, (s.n + kStep - 1) / kStep);
     return s;
 }
-__device__ __forceinline__ int64_t work_of(const Attend& p, const Seq& s) {
-    return static_cast<int64_t>(s.rows_tiles) * s.tiles * p.c.kv_heads;
+struct Work {
+    int64_t steps, items;
+};
+__device__ __forceinline__ Work work_of(const Attend& p, const Seq& s) {
+    const int64_t items = static_cast<int64_t>(s.rows_tiles) * p.c.kv_heads;
+    return {items * s.steps, items};
+}
+// Divisions of numbers that nearly always fit 32 bits.
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
+    return ((a | b) >> 32) == 0 ? static_cast<int64_t>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b)) : a / b;
 }
 // The slots that query token i (of nq) of a sequence with n slots sees.
 __device__ __forceinline__ int32_t visible(int32_t n, int32_t nq, int32_t i) { return max(0, n - (nq - 1 - i)); }
-// CTA c of C takes tiles W c / C .. W (c + 1) / C - 1 of W; the CTA that takes tile w.
-__device__ __forceinline__ int64_t first_tile(int64_t W, int64_t c, int64_t C) { return W * c / C; }
-__device__ __forceinline__ int64_t cta_of(int64_t W, int64_t w, int64_t C) { return ((w + 1) * C - 1) / W; }
+// W steps in C pieces, the first r of them one longer: the first step of piece c, the piece of step w.
+struct Pieces {
+    int64_t q, r;
+    __device__ Pieces(int64_t W, int64_t C) : q(divide(W, C)), r(W - q * C) {}
+    __device__ int64_t first(int64_t c) const { return c * q + min(c, r); }
+    __device__ int64_t of(int64_t w) const { return w < r * (q + 1) ? divide(w, q + 1) : r + divide(w - r * (q + 1), q); }
+};
 
 // lead = base + the sum of v over the threads before this one; returns base + the sum over all.
-__device__ __forceinline__ int64_t scan_add(int64_t v, int64_t base, int64_t* tmp, int64_t& lead) {
+__device__ __forceinline__ Work scan_add(const Work& v, Work base, Work* tmp, Work& lead) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int64_t x = v;
+    Work x = v;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
-        if (lane >= o) x += y;
+        const int64_t y = __shfl_up_sync(0xffffffffu, x.steps, o), z = __shfl_up_sync(0xffffffffu, x.items, o);
+        if (lane >= o) x.steps += y, x.items += z;
     }
     __syncthreads();
     if (lane == 31) tmp[warp] = x;
     __syncthreads();
-    lead = base + x - v;
+    lead = {base.steps + x.steps - v.steps, base.items + x.items - v.items};
 #pragma unroll
     for (int i = 0; i < kThreads / 32; ++i) {
-        if (i < warp) lead += tmp[i];
-        base += tmp[i];
+        if (i < warp) lead.steps += tmp[i].steps, lead.items += tmp[i].items;
+        base.steps += tmp[i].steps, base.items += tmp[i].items;
     }
     return base;
 }
 
-// A position in the list of work: tile `tile` of row group `rt` of head h of sequence b.
+// A position in the list of work: step `step` of row group `rt` of head h of sequence b.
 struct Place {
-    int b, h, rt, tile;
+    int b, h, rt, step;
+    int64_t item;   // its number in the list
     Seq s;
 };
 template <int ROWS>
@@ -212,7 +227,8 @@ __device__ __forceinline__ void next_sequence(const Attend& p, Place& at) {
 // Past the rest of this row group.
 template <int ROWS>
 __device__ __forceinline__ void next_item(const Attend& p, Place& at) {
-    at.tile = 0;
+    at.step = 0;
+    ++at.item;
     if (++at.rt < at.s.rows_tiles) return;
     at.rt = 0;
     if (++at.h < p.c.kv_heads) return;
@@ -220,15 +236,14 @@ __device__ __forceinline__ void next_item(const Attend& p, Place& at) {
     next_sequence<ROWS>(p, at);
 }
 
-template <int D, int NT>
+template <typename T, int D, int NT>
 struct Shape {
     static constexpr int kRows = 8 * NT;
     static constexpr int kGranuleBytes = kGranule * (D + 8);
     static constexpr int kStageBytes = 2 * kGranuleBytes;
-    static constexpr int kMergeRow = D + 4;   // with the rotation by g8 below: no bank conflicts
-    static constexpr int kMergeFloats = kWarps * kRows * kMergeRow;
-    static constexpr size_t kSmem = kWarps * kStages * kStageBytes + kMergeFloats * sizeof(float);
-    static constexpr int kCtas = NT == 1 ? 4 : 2;   // on an SM: 128 registers a thread, or up to 255
+    static constexpr size_t kSmem = kWarps * kStages * kStageBytes;
+    // CTAs on an SM: what the sums, twice as many with 16 rows or 128 dimensions, leave of the registers
+    static constexpr int kCtas = D == 64 ? (NT == 1 ? 5 : sizeof(T) == 4 ? 3 : 4) : (NT == 1 ? 4 : sizeof(T) == 4 ? 2 : 3);
 };
 
 // A warp's state for a group of NT x 8 query rows. A lane (g8, t4) has columns 2 t4 and
@@ -477,30 +492,29 @@ struct Feed {
     const uint8_t* src;   // of this lane's granule
     int32_t next;         // its page number kAhead steps later
 
-    __device__ __forceinline__ int slot_of(int tile, int k, int warp, int lane) const {
-        return (tile + k + (lane >> 1)) * kTile + warp * 2 * kGranule + (lane & 1) * kGranule;
+    __device__ __forceinline__ int slot_of(int step, int k, int lane) const {
+        return (step + k + (lane >> 1)) * kStep + (lane & 1) * kGranule;
     }
-    // the page number of this lane's granule in the steps from k, of a segment of seg tiles
-    __device__ __forceinline__ int32_t fetch(const Attend& p, const Place& at, int k, int seg, int warp, int lane) const {
-        const int slot = slot_of(at.tile, k, warp, lane);
+    // the page number of this lane's granule in the steps from k, of a segment of seg steps
+    __device__ __forceinline__ int32_t fetch(const Attend& p, const Place& at, int k, int seg, int lane) const {
+        const int slot = slot_of(at.step, k, lane);
         if (k + (lane >> 1) >= seg || slot >= at.s.n) return 0;
         const int32_t id = p.c.table[static_cast<int64_t>(at.b) * p.c.table_ld + slot / p.c.page];
         if (id >= 0 && id < p.c.pages) return id;
         record_error(p.info, -KQ_ERR_INVALID_ARG);
         return 0;
     }
-    __device__ __forceinline__ void place(const Attend& p, const Place& at, int k, int32_t id, int warp, int lane) {
-        const int slot = slot_of(at.tile, k, warp, lane);
+    __device__ __forceinline__ void place(const Attend& p, const Place& at, int k, int32_t id, int lane) {
+        const int slot = slot_of(at.step, k, lane);
         src = p.c.data + (static_cast<int64_t>(id) * p.c.kv_heads + at.h) * kv_head_bytes(p.c) + slot % p.c.page * (D + 8);
     }
     // Step k's granules into a stage (k < seg). Both are one run unless a page can end between them.
-    __device__ __forceinline__ void load(const Attend& p, const Place& at, int k, int seg, uint8_t* stage, uint64_t* bar, int warp,
-                                         int lane) {
+    __device__ __forceinline__ void load(const Attend& p, const Place& at, int k, int seg, uint8_t* stage, uint64_t* bar, int lane) {
         if (k % kAhead == 0 && k > 0) {
-            place(p, at, k, next, warp, lane);
-            next = fetch(p, at, k + kAhead, seg, warp, lane);
+            place(p, at, k, next, lane);
+            next = fetch(p, at, k + kAhead, seg, lane);
         }
-        const int left = at.s.n - (at.tile + k) * kTile - warp * 2 * kGranule;
+        const int left = at.s.n - (at.step + k) * kStep;
         const int many = left > kGranule ? 2 : left > 0 ? 1 : 0;
         const uint64_t a = __shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(src), 2 * (k % kAhead));
         uint64_t a2 = a + kBytes;
@@ -520,115 +534,130 @@ struct Feed {
 };
 
 template <typename T, int D, int NT>
-__global__ void __launch_bounds__(kThreads, Shape<D, NT>::kCtas) kv_attend_kernel(const Attend p) {
-    using Sh = Shape<D, NT>;
+__global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas) kv_attend_kernel(const Attend p) {
+    using Sh = Shape<T, D, NT>;
     constexpr int kRows = Sh::kRows;
     constexpr bool kSplit = Rows<T, D, NT>::kSplit;
     constexpr int kWords = Rows<T, D, NT>::kWords;
     extern __shared__ __align__(128) uint8_t smem[];
-    float* const merge = reinterpret_cast<float*>(smem + kWarps * kStages * Sh::kStageBytes);
     __shared__ uint64_t full[kWarps][kStages];
-    __shared__ int abort_flag;
-    __shared__ int64_t scan_tmp[kWarps], found_base;
-    __shared__ int found_b;
-    __shared__ float sm_m[kWarps][kRows], sm_l[kWarps][kRows], sm_o[kWarps][kRows];
-    __shared__ float sm_e[kWarps];
+    __shared__ int abort_flag[kWarps];
+    __shared__ Work scan_tmp[kWarps], found_base[kWarps];
+    __shared__ int found_b[kWarps];
+    __shared__ Seq found_s[kWarps];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const KvView& c = p.c;
 
-    // ---- this CTA's part of the work
+    // ---- this warp's part of the work
     if (lane == 0) {
         for (int i = 0; i < kStages; ++i) mbar_init(&full[warp][i], 1);
         fence_mbar_init();
+        abort_flag[warp] = 0;
+        found_b[warp] = -1;
     }
-    if (tid == 0) {
-        abort_flag = 0;
-        found_b = -1;
-        if (blockIdx.x == 0 && (p.start[0] != 0 || p.start[c.batch] != p.tokens)) record_error(p.info, -KQ_ERR_INVALID_ARG);
-    }
-    // The sequences' tiles, kThreads of them at a time: the total, then the one that holds this CTA's first.
-    int64_t W = 0, v = 0, lead = 0;
+    if (blockIdx.x == 0 && tid == 0 && (p.start[0] != 0 || p.start[c.batch] != p.tokens)) record_error(p.info, -KQ_ERR_INVALID_ARG);
+    // the sequences' steps, kThreads sequences at a time: the total, then the one that holds a warp's first
+    Seq s = {};
+    Work all = {0, 0}, v = {0, 0}, lead = {0, 0};
     for (int b0 = 0; b0 < c.batch; b0 += kThreads) {
-        v = b0 + tid < c.batch ? work_of(p, sequence<kRows>(p, b0 + tid, blockIdx.x ? nullptr : p.info)) : 0;
-        W = scan_add(v, W, scan_tmp, lead);
+        v = {0, 0};
+        if (b0 + tid < c.batch) {
+            s = sequence<kRows>(p, b0 + tid, blockIdx.x ? nullptr : p.info);
+            v = work_of(p, s);
+        }
+        all = scan_add(v, all, scan_tmp, lead);
     }
-    const int64_t C = max(static_cast<int64_t>(1), min(static_cast<int64_t>(gridDim.x), W));
-    const int64_t w0 = first_tile(W, blockIdx.x, C), w1 = blockIdx.x < C ? first_tile(W, blockIdx.x + 1, C) : w0;
-    if (tid == 0) p.joint[blockIdx.x].last = 0;
-    if (w0 >= w1) return;
-    int64_t before = 0;
+    const int64_t W = all.steps;
+    const int64_t C = max(static_cast<int64_t>(1), min(static_cast<int64_t>(gridDim.x) * kWarps, (W + kMinSteps - 1) / kMinSteps));
+    const Pieces pieces(W, C);
+    const int64_t me = warp * static_cast<int64_t>(gridDim.x) + blockIdx.x;   // neighbours in the list on different SMs
+    const int64_t w0 = me < C ? pieces.first(me) : W, w1 = me < C ? pieces.first(me + 1) : W;
+    if (blockIdx.x == 0 && tid == 0) *p.items = all.items;
+    Work before = {0, 0};
     for (int b0 = 0; b0 < c.batch; b0 += kThreads) {
         if (c.batch > kThreads) {
-            v = b0 + tid < c.batch ? work_of(p, sequence<kRows>(p, b0 + tid, nullptr)) : 0;
+            v = {0, 0};
+            if (b0 + tid < c.batch) {
+                s = sequence<kRows>(p, b0 + tid, nullptr);
+                v = work_of(p, s);
+            }
             before = scan_add(v, before, scan_tmp, lead);
         }
-        if (v > 0 && lead <= w0 && w0 < lead + v) {
-            found_b = b0 + tid;
-            found_base = lead;
+        for (int i = 0; i < kWarps; ++i) {
+            const int64_t other = i * static_cast<int64_t>(gridDim.x) + blockIdx.x;
+            const int64_t o0 = other < C ? pieces.first(other) : W;
+            if (v.steps > 0 && lead.steps <= o0 && o0 < lead.steps + v.steps) {
+                found_b[i] = b0 + tid;
+                found_base[i] = lead;
+                found_s[i] = s;
+            }
         }
     }
     __syncthreads();
-    if (found_b < 0) return;   // not reached: some sequence holds every tile
     pdl_launch_dependents();
+    if (w0 >= w1 || found_b[warp] < 0) return;   // from here on the warps are on their own
     Place at;
-    at.b = found_b;
-    at.s = sequence<kRows>(p, at.b, nullptr);
+    at.b = found_b[warp];
+    at.s = found_s[warp];
     {
-        const int64_t rem = w0 - found_base, head = static_cast<int64_t>(at.s.rows_tiles) * at.s.tiles;
-        at.h = static_cast<int>(rem / head);
-        at.rt = static_cast<int>(rem % head / at.s.tiles);
-        at.tile = static_cast<int>(rem % at.s.tiles);
-        const int64_t a = w0 - at.tile;   // the first tile of these rows
-        if (tid == 0 && blockIdx.x > 0 && at.tile > 0 && a >= first_tile(W, blockIdx.x - 1, C)) {
-            Joint j;
-            j.last = static_cast<int32_t>(cta_of(W, a + at.s.tiles - 1, C));
-            j.first_slot = a > first_tile(W, blockIdx.x - 1, C) ? 1 : 0;
-            j.h = at.h;
-            j.row = at.rt * kRows;
-            j.rows = min(kRows, at.s.nq * p.group - at.rt * kRows);
-            j.token = at.s.first;
-            p.joint[blockIdx.x] = j;
-        }
+        const int64_t rem = w0 - found_base[warp].steps, head = static_cast<int64_t>(at.s.rows_tiles) * at.s.steps;
+        at.h = static_cast<int>(divide(rem, head));
+        at.rt = static_cast<int>(divide(rem - at.h * head, at.s.steps));
+        at.step = static_cast<int>(rem - at.h * head - static_cast<int64_t>(at.rt) * at.s.steps);
+        at.item = found_base[warp].items + static_cast<int64_t>(at.h) * at.s.rows_tiles + at.rt;
     }
 
     const int g8 = lane >> 2, t4 = lane & 3;
     uint8_t* const ring = smem + warp * kStages * Sh::kStageBytes;
     int it = 0;        // steps of this warp so far: its stage and the parity of its barrier
-    // After a wait that gave up the warps go on through the same steps without waiting (the result is
-    // reported as failed), so that none of them is left alone at a barrier.
-    bool fine_waits = true;
+    bool fine_waits = true;   // a wait that gave up ends the warp's work
     int issued = 0;
-    for (int64_t w = w0; w < w1;) {
-        const int seg = static_cast<int>(min(w1 - w, static_cast<int64_t>(at.s.tiles - at.tile)));
+    for (int64_t w = w0; w < w1 && fine_waits;) {
+        const int seg = static_cast<int>(min(w1 - w, static_cast<int64_t>(at.s.steps - at.step)));
         const int rows = min(kRows, at.s.nq * p.group - at.rt * kRows);
+        if (at.step == 0 && lane == 0) {
+            Joint j;
+            j.first = static_cast<int32_t>(me);
+            j.last = seg == at.s.steps ? j.first : static_cast<int32_t>(pieces.of(w + at.s.steps - 1));
+            j.slot = w > w0 ? 1 : 0;
+            j.h = at.h;
+            j.row = at.rt * kRows;
+            j.rows = rows;
+            j.token = at.s.first;
+            p.joint[at.item] = j;
+        }
         Feed<D> feed;
-        feed.place(p, at, 0, feed.fetch(p, at, 0, seg, warp, lane), warp, lane);
-        feed.next = feed.fetch(p, at, kAhead, seg, warp, lane);
+        const int32_t page_id = feed.fetch(p, at, 0, seg, lane);
+        feed.next = feed.fetch(p, at, kAhead, seg, lane);
+        Rows<T, D, NT> R;
+        float xs[NT][kWords][8];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int r = at.rt * kRows + min(nt * 8 + g8, rows - 1);   // rows past the last repeat it; their results are not used
+            const T* src = static_cast<const T*>(p.q) + (at.s.first + r / p.group) * p.q_token +
+                           (static_cast<int64_t>(at.h) * p.group + r % p.group) * p.q_head + t4 * (D / 4);
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) load8(src + 8 * i, p.q_vec, xs[nt][i]);
+        }
+        feed.place(p, at, 0, page_id, lane);
 #pragma unroll
         for (int k = 0; k < kStages; ++k)
-            if (k < seg && fine_waits) {
+            if (k < seg) {
                 const int stage = issued++ % kStages;
-                feed.load(p, at, k, seg, ring + stage * Sh::kStageBytes, &full[warp][stage], warp, lane);
+                feed.load(p, at, k, seg, ring + stage * Sh::kStageBytes, &full[warp][stage], lane);
             }
         // q: lane (g8, t4) holds dimensions t4 D / 4 .. of row g8, each word of 8 as two k steps: (0, 4 | 1, 5) and
         // (2, 6 | 3, 7); the odd ones are divided by 16 where their nibbles sit four bits up
-        Rows<T, D, NT> R;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int row = at.rt * kRows + nt * 8 + g8;
-            const bool real = nt * 8 + g8 < rows;
-            const T* src = static_cast<const T*>(p.q) + (at.s.first + (real ? row / p.group : 0)) * p.q_token +
-                           (static_cast<int64_t>(at.h) * p.group + (real ? row % p.group : 0)) * p.q_head + t4 * (D / 4);
-            float xs[kWords][8], sum = 0.0f;
+            float sum = 0.0f;
             uint32_t top = 0;   // as bits: an infinity or a NaN is above every number
-#pragma unroll
-            for (int i = 0; i < kWords; ++i) load8(src + 8 * i, p.q_vec, xs[i]);
 #pragma unroll
             for (int i = 0; i < kWords; ++i)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    top = max(top, __float_as_uint(xs[i][j]) & 0x7FFFFFFFu);
-                    sum += xs[i][j];
+                    top = max(top, __float_as_uint(xs[nt][i][j]) & 0x7FFFFFFFu);
+                    sum += xs[nt][i][j];
                 }
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
@@ -646,11 +675,11 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT>::kCtas) kv_attend_kerne
             const float gm = bad ? 0.0f : sum * unit;
 #pragma unroll
             for (int i = 0; i < kWords; ++i) {
-                const float(&x)[8] = xs[i];
+                const float(&x)[8] = xs[nt][i];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {   // nibbles j and j + 4
                     const float s = up * (!kSplit && (j & 1) ? 0.0625f : 1.0f);
-                    const float x0 = real && !bad ? x[j] * s : 0.0f, x1 = real && !bad ? x[j + 4] * s : 0.0f;
+                    const float x0 = bad ? 0.0f : x[j] * s, x1 = bad ? 0.0f : x[j + 4] * s;
                     R.bq[nt][i][j] = pack_f16(x0, x1);
                     if constexpr (kSplit) {
                         const float2 h = unpack_f16(R.bq[nt][i][j]);
@@ -684,88 +713,71 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT>::kCtas) kv_attend_kerne
             const int stage = it % kStages;
             uint8_t* gr = ring + stage * Sh::kStageBytes;
             uint64_t* bar = &full[warp][stage];
-            bool ok = true;
             if (__any_sync(0xffffffffu, !mbar_try_wait(bar, (it / kStages) & 1)))
-                ok = __all_sync(0xffffffffu, mbar_wait(bar, (it / kStages) & 1, &abort_flag));
-            fine_waits &= ok;
-            const int slot = (at.tile + k) * kTile + warp * 2 * kGranule;
-            if constexpr (decltype(masked)::value) {
-                if (ok && slot < at.s.n) R.template step<true>(gr, slot, at.s.n, g8, t4, p.scores, p.group, true);
-            } else {
-                R.template step<false>(gr, slot, at.s.n, g8, t4, p.scores, p.group, k % kSettle == 0);
-            }
+                fine_waits = __all_sync(0xffffffffu, mbar_wait(bar, (it / kStages) & 1, &abort_flag[warp]));
+            const int slot = (at.step + k) * kStep;
+            if (fine_waits && (!decltype(masked)::value || slot < at.s.n))   // uniform over the warp
+                R.template step<decltype(masked)::value>(gr, slot, at.s.n, g8, t4, p.scores, p.group, k % kSettle == 0);
             __syncwarp();
             if (fine_waits && k + kStages < seg) {
-                feed.load(p, at, k + kStages, seg, gr, bar, warp, lane);
+                feed.load(p, at, k + kStages, seg, gr, bar, lane);
                 ++issued;
             }
             ++it;
         };
-        const int whole_steps = min(seg, max(0, (least - warp * 2 * kGranule - 2 * kGranule) / kTile + 1 - at.tile));
+        const int whole_steps = min(seg, least / kStep - at.step);
         int k = 0;
-        for (; k < whole_steps && (least >= (warp + 1) * 2 * kGranule); ++k) turn(k, std::false_type());
-        for (; k < seg; ++k) turn(k, std::true_type());
+        for (; k < whole_steps && fine_waits; ++k) turn(k, std::false_type());
+        for (; k < seg && fine_waits; ++k) turn(k, std::true_type());
+        if (!fine_waits) break;
 
-        // ---- join the warps' sums
+        // ---- the rows' result, or this piece's part of it
+        const bool whole = seg == at.s.steps;
+        float* part = p.part + (2 * me + (at.step == 0 && w > w0 ? 1 : 0)) * (kRows * (D + 2));
+        // 2^24 of subnormal codes, 2^-6 2^(ev + 1 - 127) of the weights
+        const float up = __uint_as_float(static_cast<uint32_t>(min(R.ev - (kSplit ? 132 : 108), 127) + 127) << 23);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const float one[2] = {1.0f, 1.0f};
             if constexpr (!kSplit) R.settle_mid(nt, one);
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
+            for (int k2 = 0; k2 < 2; ++k2) {
+                float L = R.l[nt][k2], off = R.off[nt][k2];
 #pragma unroll
                 for (int sh = 4; sh < 32; sh <<= 1) {
-                    R.l[nt][k] += __shfl_xor_sync(0xffffffffu, R.l[nt][k], sh);
-                    R.off[nt][k] += __shfl_xor_sync(0xffffffffu, R.off[nt][k], sh);
+                    L += __shfl_xor_sync(0xffffffffu, L, sh);
+                    off += __shfl_xor_sync(0xffffffffu, off, sh);
                 }
-                const int col = nt * 8 + 2 * t4 + k;
-                if (g8 == 0) {
-                    sm_m[warp][col] = R.m[nt][k];
-                    sm_l[warp][col] = R.l[nt][k];
-                    sm_o[warp][col] = R.off[nt][k];
+                const int col = nt * 8 + 2 * t4 + k2;
+                if (col >= rows) continue;
+                float x[D / 8];   // dimensions g8 D / 8 ..
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                    x[2 * i] = fmaf(R.o[nt][i][k2], up, off);
+                    x[2 * i + 1] = fmaf(R.o[nt][i][2 + k2], kSplit ? up : up * 0.0625f, off);
                 }
+                if (whole) {
+                    const int row = at.rt * kRows + col;
+                    const int64_t r = (static_cast<int64_t>(at.s.first) + row / p.group) * p.q_heads + at.h * p.group + row % p.group;
+                    T* dst = static_cast<T*>(p.out) + r * D + g8 * (D / 8);
+                    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
 #pragma unroll
-                for (int i = 0; i < D / 16; ++i)
-                    *reinterpret_cast<float2*>(merge + (warp * kRows + col) * Sh::kMergeRow + g8 * (D / 8) +
-                                               2 * ((i + g8) % (D / 16))) =
-                        make_float2(R.o[nt][i][k], R.o[nt][i][2 + k] * (kSplit ? 1.0f : 0.0625f));
-            }
-        }
-        // 2^24 of subnormal codes, 2^-6 2^(ev + 1 - 127) of the weights
-        if (lane == 0) sm_e[warp] = __uint_as_float(static_cast<uint32_t>(min(R.ev - (kSplit ? 132 : 108), 127) + 127) << 23);
-        __syncthreads();
-        const bool whole = seg == at.s.tiles;
-        float* part = p.part + (2 * static_cast<int64_t>(blockIdx.x) + (at.tile == 0 && w > w0 ? 1 : 0)) * (kRows * (D + 2));
-        const int d = tid % D, dg = d / (D / 8), di = d % (D / 8) / 2;
-        const float* mine = merge + dg * (D / 8) + 2 * ((di + dg) % (D / 16)) + (d & 1);
-        for (int col = tid / D; col < rows; col += kThreads / D) {
-            float M = kNone;
+                    for (int i = 0; i < D / 8; ++i) dst[i] = static_cast<T>(L == 0.0f ? 0.0f : x[i] * inv);
+                    if (g8 == 0 && p.lse) p.lse[r] = L == 0.0f ? -INFINITY : (R.m[nt][k2] + log2f(L)) * kLn2;
+                } else {
+                    float4* dst = reinterpret_cast<float4*>(part + col * D + g8 * (D / 8));
 #pragma unroll
-            for (int i = 0; i < kWarps; ++i) M = fmaxf(M, sm_m[i][col]);
-            float L = 0.0f, O = 0.0f;
-#pragma unroll
-            for (int i = 0; i < kWarps; ++i) {
-                const float f = ex2(sm_m[i][col] - M);
-                L = fmaf(f, sm_l[i][col], L);
-                O = fmaf(f, fmaf(mine[(i * kRows + col) * Sh::kMergeRow], sm_e[i], sm_o[i][col]), O);
-            }
-            if (whole) {
-                const int row = at.rt * kRows + col;
-                const int64_t r = (static_cast<int64_t>(at.s.first) + row / p.group) * p.q_heads + at.h * p.group + row % p.group;
-                static_cast<T*>(p.out)[r * D + d] = static_cast<T>(L == 0.0f ? 0.0f : O / L);
-                if (d == 0 && p.lse) p.lse[r] = L == 0.0f ? -INFINITY : (M + log2f(L)) * kLn2;
-            } else {
-                part[col * D + d] = O;
-                if (d == 0) {
-                    part[kRows * D + col] = M;
-                    part[kRows * (D + 1) + col] = L;
+                    for (int i = 0; i < D / 32; ++i) dst[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+                    if (g8 == 0) {
+                        part[kRows * D + col] = R.m[nt][k2];
+                        part[kRows * (D + 1) + col] = L;
+                    }
                 }
             }
         }
-        __syncthreads();
         w += seg;
-        at.tile += static_cast<int>(seg) - 1;
-        if (++at.tile == at.s.tiles) next_item<kRows>(p, at);
+        at.step += seg - 1;
+        if (++at.step == at.s.steps) next_item<kRows>(p, at);
     }
     if (!fine_waits && lane == 0) {   // leave only when this warp's copies have landed
         record_error(p.info, -KQ_ERR_TIMEOUT);
@@ -774,51 +786,82 @@ __global__ void __launch_bounds__(kThreads, Shape<D, NT>::kCtas) kv_attend_kerne
     }
 }
 
-// Joins the partial results of rows that more than one CTA worked on: blocks (c, i) for the rows that
-// CTA c went on with, columns i, i + gridDim.y ..; a thread for each dimension, in groups.
+// Joins the partial results of rows that more than one warp worked on: blocks (i, ..) for item i. A warp
+// takes a column, its lanes four dimensions each (D = 64: two); where the results are many, a block
+// takes a column and its warps share them.
 template <typename T, int D, int NT>
-__global__ void __launch_bounds__(512) kv_combine_kernel(const Attend p) {
-    constexpr int kRows = 8 * NT;
-    __shared__ float sm[512], sl[512 / D];
+__global__ void __launch_bounds__(256) kv_combine_kernel(const Attend p) {
+    constexpr int kRows = 8 * NT, kV = D / 32, kGroups = 8;
+    constexpr int64_t kPart = kRows * (D + 2);
+    __shared__ float sm[kGroups][D], sl[kGroups], sx[kGroups];
     pdl_wait();
     pdl_launch_dependents();
+    if (blockIdx.x >= *p.items) return;
     const Joint j = p.joint[blockIdx.x];
-    if (j.last == 0) return;
-    const int d = threadIdx.x % D, grp = threadIdx.x / D, groups = blockDim.x / D;
-    constexpr int64_t kPart = kRows * (D + 2);
-    const int64_t c = blockIdx.x;
-    const float* first = p.part + (2 * (c - 1) + j.first_slot) * kPart;
-    const float* rest = p.part + 2 * c * kPart;   // the others begin with these rows
-    const int many = static_cast<int>(j.last - c) + 1;
-    // a few results: the groups of threads take a column each; many: they share a column's results
-    const bool share = many > 4 && groups > 1;
-    for (int col = blockIdx.y + (share ? 0 : grp * gridDim.y); col < j.rows; col += gridDim.y * (share ? 1 : groups)) {
-        float M = first[kRows * D + col];
-#pragma unroll 4
-        for (int k = 0; k < many; ++k) M = fmaxf(M, rest[2 * k * kPart + kRows * D + col]);
-        float L = 0.0f, O = 0.0f;
-#pragma unroll 4
-        for (int k = share ? grp - 1 : -1; k < many; k += share ? groups : 1) {
-            const float* q = k < 0 ? first : rest + 2 * k * kPart;
-            const float f = ex2(q[kRows * D + col] - M);
-            L = fmaf(f, q[kRows * (D + 1) + col], L);
-            O = fmaf(f, q[col * D + d], O);
-        }
+    if (j.last == j.first) return;
+    const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5;
+    const int many = j.last - j.first + 1;
+    // the results after the first begin their pieces
+    auto result = [&](int k) { return p.part + (2 * static_cast<int64_t>(j.first + k) + (k == 0 ? j.slot : 0)) * kPart; };
+    const bool share = many > 32;
+    for (int col = share ? blockIdx.y : grp + blockIdx.y * kGroups; col < j.rows; col += gridDim.y * (share ? 1 : kGroups)) {
+        float M = kNone, L = 0.0f, O[kV];
+#pragma unroll
+        for (int i = 0; i < kV; ++i) O[i] = 0.0f;
+        for (int k = (share ? grp * 32 : 0) + lane; k < many; k += share ? 256 : 32) M = fmaxf(M, result(k)[kRows * D + col]);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
         if (share) {
             __syncthreads();
-            sm[threadIdx.x] = O;
-            if (d == 0) sl[grp] = L;
+            if (lane == 0) sx[grp] = M;
+            __syncthreads();
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) M = fmaxf(M, sx[g]);
+        }
+        for (int k0 = share ? grp * 32 : 0; k0 < many; k0 += share ? 256 : 32) {
+            const int here = min(32, many - k0);
+            float f = 0.0f;
+            if (lane < here) {
+                const float* q = result(k0 + lane);
+                f = ex2(q[kRows * D + col] - M);
+                L = fmaf(f, q[kRows * (D + 1) + col], L);
+            }
+#pragma unroll 8
+            for (int k = 0; k < here; ++k) {
+                const float fk = __shfl_sync(0xffffffffu, f, k);
+                const float* q = result(k0 + k) + col * D + lane * kV;
+                if constexpr (kV == 4) {
+                    const float4 x = *reinterpret_cast<const float4*>(q);
+                    O[0] = fmaf(fk, x.x, O[0]), O[1] = fmaf(fk, x.y, O[1]), O[2] = fmaf(fk, x.z, O[2]), O[3] = fmaf(fk, x.w, O[3]);
+                } else {
+                    const float2 x = *reinterpret_cast<const float2*>(q);
+                    O[0] = fmaf(fk, x.x, O[0]), O[1] = fmaf(fk, x.y, O[1]);
+                }
+            }
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
+        if (share) {
+#pragma unroll
+            for (int i = 0; i < kV; ++i) sm[grp][lane * kV + i] = O[i];
+            if (lane == 0) sl[grp] = L;
+            __syncthreads();
+            if (grp == 0)
+                for (int g = 1; g < kGroups; ++g) {
+                    L += sl[g];
+#pragma unroll
+                    for (int i = 0; i < kV; ++i) O[i] += sm[g][lane * kV + i];
+                }
             __syncthreads();
             if (grp > 0) continue;
-            for (int g = 1; g < groups; ++g) {
-                O += sm[g * D + d];
-                L += sl[g];
-            }
         }
         const int row = j.row + col;
         const int64_t r = (static_cast<int64_t>(j.token) + row / p.group) * p.q_heads + j.h * p.group + row % p.group;
-        static_cast<T*>(p.out)[r * D + d] = static_cast<T>(L == 0.0f ? 0.0f : O / L);
-        if (d == 0 && p.lse) p.lse[r] = L == 0.0f ? -INFINITY : (M + log2f(L)) * kLn2;
+        T* dst = static_cast<T*>(p.out) + r * D + lane * kV;
+        const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+#pragma unroll
+        for (int i = 0; i < kV; ++i) dst[i] = static_cast<T>(L == 0.0f ? 0.0f : O[i] * inv);
+        if (lane == 0 && p.lse) p.lse[r] = L == 0.0f ? -INFINITY : (M + log2f(L)) * kLn2;
     }
 }
 
@@ -855,28 +898,34 @@ cudaError_t launch_after(void (*kern)(Params...), dim3 grid, dim3 block, cudaStr
     return cudaLaunchKernelEx(&cfg, kern, static_cast<Params>(args)...);
 }
 
+int64_t most_items(int64_t tokens, int64_t batch, int64_t group, int64_t kv_heads, int64_t rows) {
+    return (tokens * group / rows + std::min(batch, tokens)) * kv_heads;
+}
+
 template <typename T, int D, int NT>
 kq_status run_attend(const Attend& p, cudaStream_t stream) {
-    using Sh = Shape<D, NT>;
+    using Sh = Shape<T, D, NT>;
     static std::atomic<uint64_t> done{0};
     KQ_TRY(once_per_device(done, [] {
         KQ_CUDA(cudaFuncSetAttribute(kv_attend_kernel<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                      static_cast<int>(Sh::kSmem)));
         return KQ_OK;
     }));
-    const int grid = std::min(kMaxCtas, num_sms() * Sh::kCtas);
+    const int grid = std::min(kMaxRows / Sh::kRows, num_sms() * Sh::kCtas * kWarps) / kWarps;
     kv_attend_kernel<T, D, NT><<<grid, kThreads, Sh::kSmem, stream>>>(p);
     KQ_LAUNCH_CHECK("kv_attend_kernel");
-    // few rows are split over many CTAs: a block for each column, to go through their results
-    const int64_t share = grid / std::max<int64_t>(1, p.tokens * p.c.kv_heads);
-    KQ_CUDA(launch_after(kv_combine_kernel<T, D, NT>, dim3(grid, share >= 4 ? Sh::kRows : 2), dim3(512), stream, p));
+    // a sequence has ceil(queries group / rows) items a head: at most this many, and few of them have many
+    // results each, with a block for each column to go through them
+    const int64_t items = most_items(p.tokens, p.c.batch, p.group, p.c.kv_heads, Sh::kRows);
+    const bool few = items * 32 < static_cast<int64_t>(grid) * kWarps;
+    KQ_CUDA(launch_after(kv_combine_kernel<T, D, NT>, dim3(static_cast<unsigned>(items), few ? Sh::kRows : NT), dim3(256), stream, p));
     count_launch();
     return KQ_OK;
 }
 
 size_t al256(size_t b) { return (b + 255) & ~static_cast<size_t>(255); }
-constexpr size_t kJointBytes = kMaxCtas * sizeof(Joint);
-size_t part_bytes(int64_t dim) { return al256(2ull * kMaxCtas * 16 * (dim + 2) * sizeof(float)); }
+size_t part_bytes(int64_t dim) { return al256(2ull * kMaxRows * (dim + 2) * sizeof(float)); }
+size_t joint_bytes(int64_t T, int64_t q_heads) { return al256(256 + 2ull * T * q_heads * sizeof(Joint)); }   // items: at most two a row
 
 }  // namespace
 
@@ -887,7 +936,7 @@ using namespace kq;
 
 extern "C" size_t kq_kv_attend_workspace(int64_t T, int64_t q_heads, int64_t kv_heads, int64_t dim, int64_t S) {
     if (T < 1 || q_heads < 1 || kv_heads < 1 || q_heads % kv_heads || dim < 1 || S < 0) return 0;
-    return al256(kJointBytes) + part_bytes(dim) + al256(static_cast<size_t>(T) * q_heads * sizeof(float)) +
+    return joint_bytes(T, q_heads) + part_bytes(dim) + al256(static_cast<size_t>(T) * q_heads * sizeof(float)) +
            static_cast<size_t>(T) * q_heads * S * sizeof(float);
 }
 
@@ -931,9 +980,10 @@ extern "C" kq_status kq_kv_attend(const kq_kv_cache* cache, const void* q, int d
     p.lens = lens;
     p.scale = scale;
     p.out = out;
-    p.joint = reinterpret_cast<Joint*>(w);
-    p.part = reinterpret_cast<float*>(w + al256(kJointBytes));
-    float* sums = reinterpret_cast<float*>(w + al256(kJointBytes) + part_bytes(c.dim));
+    p.items = reinterpret_cast<int64_t*>(w);
+    p.joint = reinterpret_cast<Joint*>(w + 256);
+    p.part = reinterpret_cast<float*>(w + joint_bytes(T, q_heads));
+    float* sums = reinterpret_cast<float*>(w + joint_bytes(T, q_heads) + part_bytes(c.dim));
     p.lse = lse ? lse : acc ? sums : nullptr;
     p.scores = acc ? sums + al256(static_cast<size_t>(T) * q_heads * sizeof(float)) / sizeof(float) : nullptr;
     p.S = S;
