@@ -1,7 +1,20 @@
-// kq_token_logprobs and its gradient. One block for a row: the maximum, then the sum of e^(x - m)
-// and of e^(x - m) (m - x), then the top tokens one after the other, each the largest below the one
-// before in the order (logit descending, index ascending).
-//   entropy = ln Z + sum e^(x - m) (m - x) / Z: both terms are at least 0, so nothing cancels.
+// kq_token_logprobs and kq_token_logprobs_grad: rows of logits, each read once.
+//
+// Mathematics. With t_v = log2(e) x_v - r for a reference r (in powers of two) near the maximum,
+//     Z = sum 2^t,  lse = (r + log2 Z) ln 2,  logp_v = (t_v - log2 Z) ln 2,
+//     entropy = (log2 Z - sum 2^t t / Z) ln 2.
+// A thread keeps a reference of its own, moved only when a value passes it by 2^kSlack, so Z and
+// sum 2^t t need no rescaling in the common step; r differs from the maximum by so little that the
+// entropy's two terms do not cancel beyond a few units. t is formed by one fma, the same for every
+// use, so a rounding of r cancels from logp and entropy, however large the logits are.
+//
+// The largest `top` values: the top-th largest of the threads' own maxima (by value, then index, so
+// that no two are equal) bounds the answer from below, and at most `top` threads have a value that
+// reaches it: only their share of the row, still in L2, is read again, for the few values above the bound.
+//
+// What bounds it: with V = 128000 in bf16 a row is 256 KB, 5.7 us of an SM's share of the memory
+// bandwidth, against about 6 instructions a value (3 us) and 1.5 us for the joint steps, which
+// other rows' blocks on the SM cover. The gradient reads and writes a row once.
 #include <algorithm>
 
 #include "kv_common.cuh"
@@ -10,15 +23,58 @@ namespace kq {
 namespace {
 
 constexpr int kThreads = 512;
+constexpr int kWarps = kThreads / 32;
+constexpr int kAhead = 4;                 // 16-byte loads of a thread in flight
+constexpr int kList = 1024;               // candidates for the top values
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kSlack = 4.0f;
+constexpr float kFloor = -2.0e38f;        // what a masked logit counts as: 2^t = 0 and t a number
+constexpr float kHuge = 1.0e38f;          // rows whose maximum is beyond this, or -infinity, go the careful way
 
 __device__ __forceinline__ float value(const float* p, int64_t i) { return p[i]; }
 __device__ __forceinline__ float value(const __nv_bfloat16* p, int64_t i) { return __bfloat162float(p[i]); }
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 
-// Larger for a larger logit, then for a smaller index; NaN above every number.
+// Larger for a larger logit, then for a smaller index; NaN above every number; never 0.
 __device__ __forceinline__ uint64_t rank_key(float x, uint32_t i) {
     uint32_t u = __float_as_uint(x == 0.0f ? 0.0f : x);
     u = isnan(x) ? 0xFFFFFFFFu : (u >> 31) ? ~u : (u | 0x80000000u);
     return (static_cast<uint64_t>(u) << 32) | (0xFFFFFFFFu - i);
+}
+__device__ __forceinline__ uint32_t key_index(uint64_t k) { return 0xFFFFFFFFu - static_cast<uint32_t>(k); }
+__device__ __forceinline__ float key_value(uint64_t k) {
+    const uint32_t u = static_cast<uint32_t>(k >> 32);
+    return __uint_as_float((u >> 31) ? u & 0x7FFFFFFFu : ~u);
+}
+
+// The values of a 16-byte vector, no lower than kFloor (a NaN stays one), and their true maximum
+// (NaN left out).
+template <typename T>
+__device__ __forceinline__ float unpack(const uint4& u, float (&x)[16 / sizeof(T)]) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    if constexpr (sizeof(T) == 2) {
+        constexpr uint32_t floor2 = 0xFF16FF16u;   // bf16(kFloor) twice
+        uint32_t a, b, m;
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(w[0]), "r"(w[1]));
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(b) : "r"(w[2]), "r"(w[3]));
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t c;
+            asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(c) : "r"(w[i]), "r"(floor2));
+            x[2 * i] = __uint_as_float(c << 16);
+            x[2 * i + 1] = __uint_as_float(c & 0xFFFF0000u);
+        }
+        return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm("max.NaN.f32 %0, %1, %2;" : "=f"(x[i]) : "f"(__uint_as_float(w[i])), "f"(kFloor));
+        return fmaxf(fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1])), fmaxf(__uint_as_float(w[2]), __uint_as_float(w[3])));
+    }
 }
 
 template <typename V, typename F>
@@ -28,22 +84,24 @@ __device__ __forceinline__ V block_reduce(V v, V* tmp, F f) {
     if ((threadIdx.x & 31) == 0) tmp[threadIdx.x >> 5] = v;
     __syncthreads();
     v = tmp[0];
-    for (int i = 1; i < kThreads / 32; ++i) v = f(v, tmp[i]);
+    for (int i = 1; i < kWarps; ++i) v = f(v, tmp[i]);
     return v;
 }
 
+struct Out {
+    float *logp, *entropy, *lse;
+    int32_t* top_id;
+    float* top_logp;
+    int* info;
+};
+
+// A row with a NaN or an infinite maximum, or whose values leave the range of the fast way: one value
+// at a time, the top values one after the other.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) logprob_kernel(const T* __restrict__ logits, int64_t V, int64_t ld,
-                                                           const int64_t* __restrict__ target, int top,
-                                                           float* __restrict__ logp, float* __restrict__ entropy,
-                                                           float* __restrict__ lse, int32_t* __restrict__ top_id,
-                                                           float* __restrict__ top_logp, int* info) {
-    __shared__ uint64_t tmp64[kThreads / 32];
+__device__ __noinline__ void careful_row(const T* x, int64_t r, int64_t V, int64_t y, int top, const Out& out, uint64_t* tmp64) {
     float* tmp = reinterpret_cast<float*>(tmp64);
-    const int64_t r = blockIdx.x;
-    const T* x = logits + r * ld;
     float m = -INFINITY;
-    bool bad = false;
+    int bad = 0;
     for (int64_t i = threadIdx.x; i < V; i += kThreads) {
         const float v = value(x, i);
         bad |= isnan(v) || v == INFINITY;
@@ -57,26 +115,17 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const T* __restrict__
         if (d > -INFINITY) {
             const float e = expf(d);
             z += e;
-            w -= e * d;
+            if (e > 0.0f) w -= e * d;
         }
     }
     z = block_reduce(z, tmp, [](float a, float b) { return a + b; });
     w = block_reduce(w, tmp, [](float a, float b) { return a + b; });
     const float lz = logf(z);
     const bool none = m == -INFINITY;
-    const float sum = bad ? NAN : none ? -INFINITY : m + lz;
     if (threadIdx.x == 0) {
-        const int64_t y = target[r];
-        float lp = 0.0f;
-        if (y >= V) {
-            record_error(info, -KQ_ERR_INVALID_ARG);
-            lp = NAN;
-        } else if (y >= 0) {
-            lp = bad ? NAN : none ? -INFINITY : value(x, y) - m - lz;
-        }
-        logp[r] = lp;
-        if (entropy) entropy[r] = bad ? NAN : none ? 0.0f : lz + w / z;
-        if (lse) lse[r] = sum;
+        out.logp[r] = y < 0 ? 0.0f : y >= V || bad ? NAN : none ? -INFINITY : value(x, y) - m - lz;
+        if (out.entropy) out.entropy[r] = bad ? NAN : none ? 0.0f : lz + w / z;
+        if (out.lse) out.lse[r] = bad ? NAN : none ? -INFINITY : m + lz;
     }
     uint64_t last = ~0ull;
     for (int k = 0; k < top; ++k) {
@@ -88,40 +137,252 @@ __global__ void __launch_bounds__(kThreads) logprob_kernel(const T* __restrict__
         best = block_reduce(best, tmp64, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
         last = best;
         if (threadIdx.x == 0) {
-            const int64_t i = 0xFFFFFFFFu - static_cast<uint32_t>(best);
-            top_id[r * top + k] = static_cast<int32_t>(i);
-            top_logp[r * top + k] = bad ? NAN : none ? -INFINITY : value(x, i) - m - lz;
+            out.top_id[r * top + k] = static_cast<int32_t>(key_index(best));
+            out.top_logp[r * top + k] = bad ? NAN : none ? -INFINITY : key_value(best) - m - lz;
         }
     }
 }
 
-__device__ __forceinline__ void put(float* p, float v) { *p = v; }
-__device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16(v); }
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 3) logprob_kernel(const T* __restrict__ logits, int64_t V, int64_t ld,
+                                                              const int64_t* __restrict__ target, int top, Out out) {
+    constexpr int E = 16 / sizeof(T);
+    __shared__ uint64_t tmp64[kWarps], list[kList];
+    __shared__ int chosen[KQ_LOGPROBS_MAX_TOP], n_chosen, n_list;
+    float* tmp = reinterpret_cast<float*>(tmp64);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int64_t r = blockIdx.x;
+    const T* x = logits + r * ld;
+    // vectors of 16 bytes between the first and the last aligned address, and the few values around them
+    const int head = static_cast<int>(min(V, static_cast<int64_t>((16 - (reinterpret_cast<uintptr_t>(x) & 15)) % 16 / sizeof(T))));
+    const uint4* xv = reinterpret_cast<const uint4*>(x + head);
+    const int nvec = static_cast<int>((V - head) / E);
+    const int tail = static_cast<int>(V - head) - nvec * E, edge = head + tail;
+    const int my_edge = tid < edge ? (tid < head ? tid : head + nvec * E + tid - head) : -1;
+
+    float ref = kFloor, ref2 = kFloor * kLog2e, z = 0.0f, w = 0.0f, best = -INFINITY;
+    int best_vec = -1;
+    auto take = [&](float top_value, const float* v, int n) {
+        if (top_value > ref + kSlack) {
+            const float nr2 = top_value * kLog2e, f = ex2(ref2 - nr2);
+            w = f > 0.0f ? f * fmaf(z, ref2 - nr2, w) : 0.0f;
+            z *= f;
+            ref = top_value;
+            ref2 = nr2;
+        }
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const float t = fmaf(v[i], kLog2e, -ref2), e = ex2(t);
+            z += e;
+            w = fmaf(e, t, w);
+        }
+    };
+    for (int j0 = tid; j0 < nvec; j0 += kThreads * kAhead) {
+        uint4 u[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int j = j0 + i * kThreads;
+            if (j < nvec) u[i] = __ldg(xv + j);
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int j = j0 + i * kThreads;
+            if (j >= nvec) break;
+            float v[E];
+            const float m = unpack<T>(u[i], v);
+            if (m > best) {
+                best = m;
+                best_vec = j;
+            }
+            take(m, v, E);
+        }
+    }
+    float ev = -INFINITY;
+    if (my_edge >= 0) {
+        ev = value(x, my_edge);
+        float c[1];
+        asm("max.NaN.f32 %0, %1, %2;" : "=f"(c[0]) : "f"(ev), "f"(kFloor));
+        take(ev, c, 1);
+    }
+    // ---- the sums about one reference
+    const float m = block_reduce(fmaxf(best, ev), tmp, [](float a, float b) { return fmaxf(a, b); });
+    const float r2 = block_reduce(ref2, tmp, [](float a, float b) { return fmaxf(a, b); });
+    {
+        const float f = ex2(ref2 - r2);
+        w = f > 0.0f ? f * fmaf(z, ref2 - r2, w) : 0.0f;
+        z = f > 0.0f || !(z == z) ? z * f : 0.0f;
+    }
+    z = block_reduce(z, tmp, [](float a, float b) { return a + b; });
+    w = block_reduce(w, tmp, [](float a, float b) { return a + b; });
+    const int64_t y = target[r];
+    if (y >= V && tid == 0) record_error(out.info, -KQ_ERR_INVALID_ARG);
+    if (!(m > -kHuge && m < kHuge && z < INFINITY)) {   // false for a NaN in z
+        careful_row(x, r, V, y, top, out, tmp64);
+        return;
+    }
+    const float lz2 = log2f(z);
+    if (tid == 0) {
+        out.logp[r] = y < 0 ? 0.0f : y >= V ? NAN : (fmaf(value(x, y), kLog2e, -r2) - lz2) * kLn2;
+        if (out.entropy) out.entropy[r] = fmaxf(0.0f, (lz2 - w / z) * kLn2);
+        if (out.lse) out.lse[r] = (r2 + lz2) * kLn2;
+    }
+    if (top == 0) return;
+
+    // ---- the top values
+    uint64_t key = my_edge >= 0 ? rank_key(ev, static_cast<uint32_t>(my_edge)) : 0;
+    if (tid < nvec) {
+        const T* p = reinterpret_cast<const T*>(xv + max(best_vec, tid));   // a thread of -infinities only: its first vector
+        const uint32_t at = static_cast<uint32_t>(p - x);
+#pragma unroll
+        for (int i = 0; i < E; ++i) key = max(key, rank_key(value(p, i), at + i));
+    }
+    // the top-th largest key, bit by bit: the value's (16 of bf16), then the index's
+    uint64_t bound = 0;
+    for (int bit = 63; bit >= 0; --bit) {
+        if (sizeof(T) == 2 && bit < 48 && bit >= 32) continue;
+        if (bit < 32 && bit >= 20) {
+            bound |= 1ull << bit;   // the index is below 2^20, its complement's upper bits are ones
+            continue;
+        }
+        const uint64_t cand = bound | (1ull << bit);
+        if (__syncthreads_count(key >= cand) >= top) bound = cand;
+    }
+    if (tid == 0) n_chosen = n_list = 0;
+    __syncthreads();
+    if (tid < nvec && key >= bound) {
+        const int at = atomicAdd(&n_chosen, 1);
+        if (at < KQ_LOGPROBS_MAX_TOP) chosen[at] = tid;
+    }
+    auto offer = [&](uint64_t k) {
+        if (k < bound) return;
+        const int at = atomicAdd(&n_list, 1);
+        if (at < kList) list[at] = k;
+    };
+    if (my_edge >= 0) offer(rank_key(ev, static_cast<uint32_t>(my_edge)));
+    __syncthreads();
+    const int many = min(n_chosen, KQ_LOGPROBS_MAX_TOP);
+    for (int s = warp; s < many; s += kWarps)
+        for (int j = chosen[s] + lane * kThreads; j < nvec; j += 32 * kThreads) {
+            const T* p = reinterpret_cast<const T*>(xv + j);
+            const uint32_t at = static_cast<uint32_t>(p - x);
+            const uint4 u = xv[j];
+            const T* q = reinterpret_cast<const T*>(&u);
+#pragma unroll
+            for (int i = 0; i < E; ++i) offer(rank_key(value(q, i), at + i));
+        }
+    __syncthreads();
+    const int n = n_list;
+    if (n > kList || n_chosen > KQ_LOGPROBS_MAX_TOP) {   // more near the bound than the list holds
+        careful_row(x, r, V, y, top, out, tmp64);
+        return;
+    }
+    for (int c = tid; c < n; c += kThreads) {
+        const uint64_t mine = list[c];
+        int rank = 0;
+        for (int i = 0; i < n; ++i) rank += list[i] > mine;
+        if (rank < top) {
+            out.top_id[r * top + rank] = static_cast<int32_t>(key_index(mine));
+            out.top_logp[r * top + rank] = (fmaf(key_value(mine), kLog2e, -r2) - lz2) * kLn2;
+        }
+    }
+}
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) logprob_grad_kernel(const T* logits, int64_t V, int64_t ld,
-                                                                const int64_t* __restrict__ target,
-                                                                const float* __restrict__ lse,
-                                                                const float* __restrict__ entropy,
-                                                                const float* __restrict__ g_logp,
-                                                                const float* __restrict__ g_entropy, T* grad,
-                                                                int64_t ld_grad, int* info) {
+struct Grad {
+    const T* logits;
+    T* grad;
+    int64_t V, ld, ld_grad;
+    const int64_t* target;
+    const float *lse, *entropy, *g_logp, *g_entropy;
+    int* info;
+};
+
+__device__ __forceinline__ float grad_of(float x, float sum, float g, float ge, float h) {
+    const float lp = x - sum, p = ex2(lp * kLog2e);
+    return p > 0.0f ? -p * fmaf(ge, lp + h, g) : p == p ? 0.0f : p;
+}
+
+// A block for kAhead x kThreads vectors of a row (VEC), or as many values.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kThreads) logprob_grad_kernel(const Grad<T> a) {
+    constexpr int E = VEC ? 16 / sizeof(T) : 1;
     const int64_t r = blockIdx.x;
-    const int64_t y = target[r];
-    if (y >= V && threadIdx.x == 0) record_error(info, -KQ_ERR_INVALID_ARG);
-    const float g = y >= 0 && y < V ? g_logp[r] : 0.0f;
-    const float ge = g_entropy ? g_entropy[r] : 0.0f, h = g_entropy ? entropy[r] : 0.0f, sum = lse[r];
-    for (int64_t i = threadIdx.x; i < V; i += kThreads) {
-        const float v = value(logits + r * ld, i);
-        float d = 0.0f;
-        if (sum != -INFINITY) {
-            const float lp = v - sum, p = expf(lp);
-            d = -g * p;
-            if (g_entropy && p != 0.0f) d -= ge * p * (lp + h);
-            if (i == y) d += g;
+    const int64_t y = a.target[r];
+    if (y >= a.V && threadIdx.x == 0 && blockIdx.y == 0) record_error(a.info, -KQ_ERR_INVALID_ARG);
+    const float sum = a.lse[r], g = y >= 0 && y < a.V ? a.g_logp[r] : 0.0f;
+    const float ge = a.g_entropy ? a.g_entropy[r] : 0.0f, h = a.g_entropy ? a.entropy[r] : 0.0f;
+    const bool none = sum == -INFINITY;
+    const T* x = a.logits + r * a.ld;
+    T* d = a.grad + r * a.ld_grad;
+    const int64_t n = (a.V + E - 1) / E;
+    for (int64_t j0 = static_cast<int64_t>(blockIdx.y) * kThreads * kAhead + threadIdx.x; j0 < n;
+         j0 += static_cast<int64_t>(gridDim.y) * kThreads * kAhead) {
+        if constexpr (VEC) {
+            uint4 u[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int64_t j = j0 + i * kThreads;
+                if ((j + 1) * E <= a.V) u[i] = reinterpret_cast<const uint4*>(x)[j];
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int64_t j = j0 + i * kThreads;
+                if (j >= n) break;
+                if ((j + 1) * E > a.V) {   // the row's last values
+                    for (int64_t v = j * E; v < a.V; ++v) {
+                        const float q = none ? 0.0f : grad_of(value(x, v), sum, g, ge, h);
+                        d[v] = static_cast<T>(v == y && !none ? q + g : q);
+                    }
+                    break;
+                }
+                float q[E];
+                const uint32_t w[4] = {u[i].x, u[i].y, u[i].z, u[i].w};
+#pragma unroll
+                for (int k = 0; k < E; ++k) {
+                    const float v = sizeof(T) == 4 ? __uint_as_float(w[k % 4])
+                                                   : __uint_as_float(k & 1 ? w[k / 2] & 0xFFFF0000u : w[k / 2] << 16);
+                    q[k] = none ? 0.0f : grad_of(v, sum, g, ge, h);
+                }
+                if (y / E == j && y >= 0 && !none) {
+#pragma unroll
+                    for (int k = 0; k < E; ++k)
+                        if (j * E + k == y) q[k] += g;
+                }
+                uint4 o;
+                if constexpr (sizeof(T) == 4) {
+                    o = make_uint4(__float_as_uint(q[0]), __float_as_uint(q[1]), __float_as_uint(q[2]), __float_as_uint(q[3]));
+                } else {
+                    uint32_t b[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const __nv_bfloat162 t = __floats2bfloat162_rn(q[2 * k], q[2 * k + 1]);
+                        b[k] = *reinterpret_cast<const uint32_t*>(&t);
+                    }
+                    o = make_uint4(b[0], b[1], b[2], b[3]);
+                }
+                reinterpret_cast<uint4*>(d)[j] = o;
+            }
+        } else {
+            for (int i = 0; i < kAhead; ++i) {
+                const int64_t v = j0 + i * kThreads;
+                if (v >= n) break;
+                const float q = none ? 0.0f : grad_of(value(x, v), sum, g, ge, h);
+                d[v] = static_cast<T>(v == y && !none ? q + g : q);
+            }
         }
-        put(grad + r * ld_grad + i, d);
     }
+}
+
+template <typename T>
+kq_status run_grad(const Grad<T>& a, int64_t rows, cudaStream_t stream) {
+    const bool vec = !((reinterpret_cast<uintptr_t>(a.logits) | reinterpret_cast<uintptr_t>(a.grad)) & 15u) &&
+                     !((a.ld * sizeof(T)) & 15u) && !((a.ld_grad * sizeof(T)) & 15u);
+    const int64_t n = vec ? cdiv(a.V, 16 / sizeof(T)) : a.V;
+    const dim3 grid(static_cast<unsigned>(rows), static_cast<unsigned>(std::min<int64_t>(cdiv(n, kThreads * kAhead), 65535)));
+    if (vec) logprob_grad_kernel<T, true><<<grid, kThreads, 0, stream>>>(a);
+    else logprob_grad_kernel<T, false><<<grid, kThreads, 0, stream>>>(a);
+    KQ_LAUNCH_CHECK("logprob_grad_kernel");
+    return KQ_OK;
 }
 
 }  // namespace
@@ -161,12 +422,12 @@ extern "C" kq_status kq_token_logprobs(const void* logits, int dtype, int64_t T,
     }
     if (T == 0) return KQ_OK;
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
+    const Out out = {logp, entropy, lse, top_id, top_logp, info};
     if (dtype == KQ_BF16)
         logprob_kernel<<<static_cast<unsigned>(T), kThreads, 0, stream>>>(static_cast<const __nv_bfloat16*>(logits), V, ld, target,
-                                                                        top, logp, entropy, lse, top_id, top_logp, info);
+                                                                        top, out);
     else
-        logprob_kernel<<<static_cast<unsigned>(T), kThreads, 0, stream>>>(static_cast<const float*>(logits), V, ld, target, top,
-                                                                        logp, entropy, lse, top_id, top_logp, info);
+        logprob_kernel<<<static_cast<unsigned>(T), kThreads, 0, stream>>>(static_cast<const float*>(logits), V, ld, target, top, out);
     KQ_LAUNCH_CHECK("logprob_kernel");
     return KQ_OK;
 }
@@ -186,13 +447,8 @@ extern "C" kq_status kq_token_logprobs_grad(const void* logits, int dtype, int64
     if (T == 0) return KQ_OK;
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
     if (dtype == KQ_BF16)
-        logprob_grad_kernel<<<static_cast<unsigned>(T), kThreads, 0, stream>>>(
-            static_cast<const __nv_bfloat16*>(logits), V, ld, target, lse, entropy, g_logp, g_entropy,
-            static_cast<__nv_bfloat16*>(grad), ld_grad, info);
-    else
-        logprob_grad_kernel<<<static_cast<unsigned>(T), kThreads, 0, stream>>>(static_cast<const float*>(logits), V, ld, target, lse,
-                                                                             entropy, g_logp, g_entropy,
-                                                                             static_cast<float*>(grad), ld_grad, info);
-    KQ_LAUNCH_CHECK("logprob_grad_kernel");
-    return KQ_OK;
+        return run_grad(Grad<__nv_bfloat16>{static_cast<const __nv_bfloat16*>(logits), static_cast<__nv_bfloat16*>(grad), V, ld,
+                                            ld_grad, target, lse, entropy, g_logp, g_entropy, info}, T, stream);
+    return run_grad(Grad<float>{static_cast<const float*>(logits), static_cast<float*>(grad), V, ld, ld_grad, target, lse, entropy,
+                                g_logp, g_entropy, info}, T, stream);
 }
