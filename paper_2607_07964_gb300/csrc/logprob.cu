@@ -22,10 +22,11 @@
 namespace kq {
 namespace {
 
-constexpr int kThreads = 512;
-constexpr int kWarps = kThreads / 32;
+constexpr int kThreads = 256;             // of a block where there are rows for every SM, and of the gradient's
+constexpr int kWide = 1024;               // where there are few
 constexpr int kAhead = 4;                 // 16-byte loads of a thread in flight
 constexpr int kList = 1024;               // candidates for the top values
+constexpr int kChosen = 64;               // threads whose values are looked through for them
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kSlack = 4.0f;
 constexpr float kFloor = -2.0e38f;        // what a masked logit counts as: 2^t = 0 and t a number
@@ -77,16 +78,17 @@ __device__ __forceinline__ float unpack(const uint4& u, float (&x)[16 / sizeof(T
     }
 }
 
-template <typename V, typename F>
+template <int NT, typename V, typename F>
 __device__ __forceinline__ V block_reduce(V v, V* tmp, F f) {
     for (int o = 16; o > 0; o >>= 1) v = f(v, __shfl_xor_sync(0xffffffffu, v, o));
     __syncthreads();
     if ((threadIdx.x & 31) == 0) tmp[threadIdx.x >> 5] = v;
     __syncthreads();
-    v = tmp[0];
-    for (int i = 1; i < kWarps; ++i) v = f(v, tmp[i]);
+    v = tmp[threadIdx.x % (NT / 32)];
+    for (int o = NT / 64; o > 0; o >>= 1) v = f(v, __shfl_xor_sync(0xffffffffu, v, o));
     return v;
 }
+__device__ __forceinline__ float sum2(float a, float b) { return a + b; }
 
 struct Out {
     float *logp, *entropy, *lse;
@@ -97,20 +99,20 @@ struct Out {
 
 // A row with a NaN or an infinite maximum, or whose values leave the range of the fast way: one value
 // at a time, the top values one after the other.
-template <typename T>
+template <typename T, int NT>
 __device__ __noinline__ void careful_row(const T* x, int64_t r, int64_t V, int64_t y, int top, const Out& out, uint64_t* tmp64) {
     float* tmp = reinterpret_cast<float*>(tmp64);
     float m = -INFINITY;
     int bad = 0;
-    for (int64_t i = threadIdx.x; i < V; i += kThreads) {
+    for (int64_t i = threadIdx.x; i < V; i += NT) {
         const float v = value(x, i);
         bad |= isnan(v) || v == INFINITY;
         m = fmaxf(m, v);
     }
-    m = block_reduce(m, tmp, [](float a, float b) { return fmaxf(a, b); });
+    m = block_reduce<NT>(m, tmp, [](float a, float b) { return fmaxf(a, b); });
     bad = __syncthreads_or(bad);
     float z = 0.0f, w = 0.0f;
-    for (int64_t i = threadIdx.x; i < V; i += kThreads) {
+    for (int64_t i = threadIdx.x; i < V; i += NT) {
         const float d = value(x, i) - m;
         if (d > -INFINITY) {
             const float e = expf(d);
@@ -118,8 +120,8 @@ __device__ __noinline__ void careful_row(const T* x, int64_t r, int64_t V, int64
             if (e > 0.0f) w -= e * d;
         }
     }
-    z = block_reduce(z, tmp, [](float a, float b) { return a + b; });
-    w = block_reduce(w, tmp, [](float a, float b) { return a + b; });
+    z = block_reduce<NT>(z, tmp, [](float a, float b) { return a + b; });
+    w = block_reduce<NT>(w, tmp, [](float a, float b) { return a + b; });
     const float lz = logf(z);
     const bool none = m == -INFINITY;
     if (threadIdx.x == 0) {
@@ -130,11 +132,11 @@ __device__ __noinline__ void careful_row(const T* x, int64_t r, int64_t V, int64
     uint64_t last = ~0ull;
     for (int k = 0; k < top; ++k) {
         uint64_t best = 0;
-        for (int64_t i = threadIdx.x; i < V; i += kThreads) {
+        for (int64_t i = threadIdx.x; i < V; i += NT) {
             const uint64_t key = rank_key(value(x, i), static_cast<uint32_t>(i));
             if (key < last && key > best) best = key;
         }
-        best = block_reduce(best, tmp64, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
+        best = block_reduce<NT>(best, tmp64, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
         last = best;
         if (threadIdx.x == 0) {
             out.top_id[r * top + k] = static_cast<int32_t>(key_index(best));
@@ -143,16 +145,17 @@ __device__ __noinline__ void careful_row(const T* x, int64_t r, int64_t V, int64
     }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads, 3) logprob_kernel(const T* __restrict__ logits, int64_t V, int64_t ld,
-                                                              const int64_t* __restrict__ target, int top, Out out) {
-    constexpr int E = 16 / sizeof(T);
+template <typename T, int NT>
+__global__ void __launch_bounds__(NT, 1536 / NT) logprob_kernel(const T* __restrict__ logits, int64_t V, int64_t ld,
+                                                                const int64_t* __restrict__ target, int top, Out out) {
+    constexpr int E = 16 / sizeof(T), kWarps = NT / 32;
     __shared__ uint64_t tmp64[kWarps], list[kList];
-    __shared__ int chosen[KQ_LOGPROBS_MAX_TOP], n_chosen, n_list;
-    float* tmp = reinterpret_cast<float*>(tmp64);
+    __shared__ float tmp[2][kWarps][4];
+    __shared__ int chosen[kChosen], n_chosen, n_list;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t r = blockIdx.x;
     const T* x = logits + r * ld;
+    const int64_t y = target[r];
     // vectors of 16 bytes between the first and the last aligned address, and the few values around them
     const int head = static_cast<int>(min(V, static_cast<int64_t>((16 - (reinterpret_cast<uintptr_t>(x) & 15)) % 16 / sizeof(T))));
     const uint4* xv = reinterpret_cast<const uint4*>(x + head);
@@ -160,11 +163,11 @@ __global__ void __launch_bounds__(kThreads, 3) logprob_kernel(const T* __restric
     const int tail = static_cast<int>(V - head) - nvec * E, edge = head + tail;
     const int my_edge = tid < edge ? (tid < head ? tid : head + nvec * E + tid - head) : -1;
 
-    float ref = kFloor, ref2 = kFloor * kLog2e, z = 0.0f, w = 0.0f, best = -INFINITY;
+    float ref = kFloor, ref2 = 0.0f, z = 0.0f, w = 0.0f, best = -INFINITY;
     int best_vec = -1;
     auto take = [&](float top_value, const float* v, int n) {
         if (top_value > ref + kSlack) {
-            const float nr2 = top_value * kLog2e, f = ex2(ref2 - nr2);
+            const float nr2 = top_value * kLog2e, f = ref == kFloor ? 0.0f : ex2(ref2 - nr2);
             w = f > 0.0f ? f * fmaf(z, ref2 - nr2, w) : 0.0f;
             z *= f;
             ref = top_value;
@@ -177,25 +180,31 @@ __global__ void __launch_bounds__(kThreads, 3) logprob_kernel(const T* __restric
             w = fmaf(e, t, w);
         }
     };
-    for (int j0 = tid; j0 < nvec; j0 += kThreads * kAhead) {
+    auto take_vec = [&](const uint4& u, int j) {
+        float v[E];
+        const float m = unpack<T>(u, v);
+        if (m > best) {
+            best = m;
+            best_vec = j;
+        }
+        take(m, v, E);
+    };
+    int j = tid;
+    for (; j + (kAhead - 1) * NT < nvec; j += kAhead * NT) {
         uint4 u[kAhead];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int j = j0 + i * kThreads;
-            if (j < nvec) u[i] = __ldg(xv + j);
-        }
+        for (int i = 0; i < kAhead; ++i) u[i] = __ldg(xv + j + i * NT);
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int j = j0 + i * kThreads;
-            if (j >= nvec) break;
-            float v[E];
-            const float m = unpack<T>(u[i], v);
-            if (m > best) {
-                best = m;
-                best_vec = j;
-            }
-            take(m, v, E);
-        }
+        for (int i = 0; i < kAhead; ++i) take_vec(u[i], j + i * NT);
+    }
+    {
+        uint4 u[kAhead - 1];
+#pragma unroll
+        for (int i = 0; i < kAhead - 1; ++i)
+            if (j + i * NT < nvec) u[i] = __ldg(xv + j + i * NT);
+#pragma unroll
+        for (int i = 0; i < kAhead - 1; ++i)
+            if (j + i * NT < nvec) take_vec(u[i], j + i * NT);
     }
     float ev = -INFINITY;
     if (my_edge >= 0) {
@@ -205,19 +214,48 @@ __global__ void __launch_bounds__(kThreads, 3) logprob_kernel(const T* __restric
         take(ev, c, 1);
     }
     // ---- the sums about one reference
-    const float m = block_reduce(fmaxf(best, ev), tmp, [](float a, float b) { return fmaxf(a, b); });
-    const float r2 = block_reduce(ref2, tmp, [](float a, float b) { return fmaxf(a, b); });
-    {
-        const float f = ex2(ref2 - r2);
-        w = f > 0.0f ? f * fmaf(z, ref2 - r2, w) : 0.0f;
-        z = f > 0.0f || !(z == z) ? z * f : 0.0f;
+    const bool has = tid < nvec || my_edge >= 0;
+    const float mine = fmaxf(best, ev);
+    float m = mine, low = has ? mine : INFINITY, r2 = ref == kFloor ? kFloor : ref2;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        low = fminf(low, __shfl_xor_sync(0xffffffffu, low, o));
+        r2 = fmaxf(r2, __shfl_xor_sync(0xffffffffu, r2, o));
     }
-    z = block_reduce(z, tmp, [](float a, float b) { return a + b; });
-    w = block_reduce(w, tmp, [](float a, float b) { return a + b; });
-    const int64_t y = target[r];
+    if (lane == 0) tmp[0][warp][0] = m, tmp[0][warp][1] = low, tmp[0][warp][2] = r2;
+    __syncthreads();
+    {
+        const float4 q = *reinterpret_cast<const float4*>(tmp[0][lane % kWarps]);
+        m = q.x, low = q.y, r2 = q.z;
+    }
+#pragma unroll
+    for (int o = kWarps / 2; o > 0; o >>= 1) {
+        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        low = fminf(low, __shfl_xor_sync(0xffffffffu, low, o));
+        r2 = fmaxf(r2, __shfl_xor_sync(0xffffffffu, r2, o));
+    }
+    {
+        const float f = ref == kFloor ? 0.0f : ex2(ref2 - r2);
+        w = f > 0.0f ? f * fmaf(z, ref2 - r2, w) : 0.0f;
+        z *= f;   // a NaN stays one
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        z += __shfl_xor_sync(0xffffffffu, z, o);
+        w += __shfl_xor_sync(0xffffffffu, w, o);
+    }
+    if (lane == 0) tmp[1][warp][0] = z, tmp[1][warp][1] = w;
+    __syncthreads();
+    z = tmp[1][lane % kWarps][0], w = tmp[1][lane % kWarps][1];
+#pragma unroll
+    for (int o = kWarps / 2; o > 0; o >>= 1) {
+        z += __shfl_xor_sync(0xffffffffu, z, o);
+        w += __shfl_xor_sync(0xffffffffu, w, o);
+    }
     if (y >= V && tid == 0) record_error(out.info, -KQ_ERR_INVALID_ARG);
     if (!(m > -kHuge && m < kHuge && z < INFINITY)) {   // false for a NaN in z
-        careful_row(x, r, V, y, top, out, tmp64);
+        careful_row<T, NT>(x, r, V, y, top, out, tmp64);
         return;
     }
     const float lz2 = log2f(z);
@@ -228,61 +266,79 @@ __global__ void __launch_bounds__(kThreads, 3) logprob_kernel(const T* __restric
     }
     if (top == 0) return;
 
-    // ---- the top values
+    // ---- the top values. The top-th largest of the threads' maxima, bit by bit from the first in which they
+    // differ; all of them and more are needed when there are fewer threads with values.
+    constexpr int kBits = 8 * sizeof(T);   // bf16 values order by their upper half
+    auto order = [](float v) { return static_cast<uint32_t>(rank_key(v, 0) >> 32) >> (32 - kBits); };
+    uint32_t bound_value = 0;
+    uint64_t bound = 0;
+    const uint32_t mine_order = has ? order(mine) : 0;
+    if (max(min(NT, nvec), edge) >= top) {
+        const uint32_t hi = order(m), differ = hi ^ order(low);
+        const int bits = 32 - __clz(differ);   // 0 when all are equal
+        bound_value = bits == 32 ? 0 : hi >> bits << bits;
+        for (int bit = bits - 1; bit >= 0; --bit) {
+            const uint32_t cand = bound_value | (1u << bit);
+            if (__syncthreads_count(mine_order >= cand) >= top) bound_value = cand;
+        }
+        const uint32_t full = kBits == 32 ? bound_value : bound_value << 16 | (bound_value >> 15 ? 0u : 0xFFFFu);
+        bound = static_cast<uint64_t>(full) << 32;
+    }
+    if (tid == 0) n_chosen = n_list = 0;
+    // a thread's largest key: the first of its largest values
     uint64_t key = my_edge >= 0 ? rank_key(ev, static_cast<uint32_t>(my_edge)) : 0;
-    if (tid < nvec) {
+    if (tid < nvec && best >= ev) {
         const T* p = reinterpret_cast<const T*>(xv + max(best_vec, tid));   // a thread of -infinities only: its first vector
         const uint32_t at = static_cast<uint32_t>(p - x);
 #pragma unroll
         for (int i = 0; i < E; ++i) key = max(key, rank_key(value(p, i), at + i));
     }
-    // the top-th largest key, bit by bit: the value's (16 of bf16), then the index's
-    uint64_t bound = 0;
-    for (int bit = 63; bit >= 0; --bit) {
-        if (sizeof(T) == 2 && bit < 48 && bit >= 32) continue;
-        if (bit < 32 && bit >= 20) {
-            bound |= 1ull << bit;   // the index is below 2^20, its complement's upper bits are ones
-            continue;
+    for (int pass = 0;; ++pass) {
+        __syncthreads();
+        if (tid < nvec && key >= bound) {
+            const int at = atomicAdd(&n_chosen, 1);
+            if (at < kChosen) chosen[at] = tid;
         }
-        const uint64_t cand = bound | (1ull << bit);
-        if (__syncthreads_count(key >= cand) >= top) bound = cand;
-    }
-    if (tid == 0) n_chosen = n_list = 0;
-    __syncthreads();
-    if (tid < nvec && key >= bound) {
-        const int at = atomicAdd(&n_chosen, 1);
-        if (at < KQ_LOGPROBS_MAX_TOP) chosen[at] = tid;
-    }
-    auto offer = [&](uint64_t k) {
-        if (k < bound) return;
-        const int at = atomicAdd(&n_list, 1);
-        if (at < kList) list[at] = k;
-    };
-    if (my_edge >= 0) offer(rank_key(ev, static_cast<uint32_t>(my_edge)));
-    __syncthreads();
-    const int many = min(n_chosen, KQ_LOGPROBS_MAX_TOP);
-    for (int s = warp; s < many; s += kWarps)
-        for (int j = chosen[s] + lane * kThreads; j < nvec; j += 32 * kThreads) {
-            const T* p = reinterpret_cast<const T*>(xv + j);
-            const uint32_t at = static_cast<uint32_t>(p - x);
-            const uint4 u = xv[j];
-            const T* q = reinterpret_cast<const T*>(&u);
+        auto offer = [&](uint64_t k) {
+            if (k < bound) return;
+            const int at = atomicAdd(&n_list, 1);
+            if (at < kList) list[at] = k;
+        };
+        if (my_edge >= 0) offer(rank_key(ev, static_cast<uint32_t>(my_edge)));
+        __syncthreads();
+        if (n_chosen <= kChosen) {
+            for (int s = warp; s < n_chosen; s += kWarps)
+                for (int i = chosen[s] + lane * NT; i < nvec; i += 32 * NT) {
+                    const uint32_t at = static_cast<uint32_t>(head + i * E);
+                    const uint4 u = xv[i];
+                    const T* q = reinterpret_cast<const T*>(&u);
 #pragma unroll
-            for (int i = 0; i < E; ++i) offer(rank_key(value(q, i), at + i));
+                    for (int e = 0; e < E; ++e) offer(rank_key(value(q, e), at + e));
+                }
         }
-    __syncthreads();
-    const int n = n_list;
-    if (n > kList || n_chosen > KQ_LOGPROBS_MAX_TOP) {   // more near the bound than the list holds
-        careful_row(x, r, V, y, top, out, tmp64);
-        return;
+        __syncthreads();
+        if (n_chosen <= kChosen && n_list <= kList) break;
+        if (pass == 1) {   // more near the bound than the list holds
+            careful_row<T, NT>(x, r, V, y, top, out, tmp64);
+            return;
+        }
+        // too many share the bound's value: of those, the ones with the lowest indices (complements, the largest
+        // first; an index is below 2^20)
+        bound |= 0xFFF00000ull;
+        for (int bit = 19; bit >= 0; --bit) {
+            const uint64_t cand = bound | (1ull << bit);
+            if (__syncthreads_count(key >= cand) >= top) bound = cand;
+        }
+        if (tid == 0) n_chosen = n_list = 0;
     }
-    for (int c = tid; c < n; c += kThreads) {
-        const uint64_t mine = list[c];
+    const int n = n_list;
+    for (int c = tid; c < n; c += NT) {
+        const uint64_t k = list[c];
         int rank = 0;
-        for (int i = 0; i < n; ++i) rank += list[i] > mine;
+        for (int i = 0; i < n; ++i) rank += list[i] > k;
         if (rank < top) {
-            out.top_id[r * top + rank] = static_cast<int32_t>(key_index(mine));
-            out.top_logp[r * top + rank] = (fmaf(key_value(mine), kLog2e, -r2) - lz2) * kLn2;
+            out.top_id[r * top + rank] = static_cast<int32_t>(key_index(k));
+            out.top_logp[r * top + rank] = (fmaf(key_value(k), kLog2e, -r2) - lz2) * kLn2;
         }
     }
 }
@@ -423,11 +479,18 @@ extern "C" kq_status kq_token_logprobs(const void* logits, int dtype, int64_t T,
     if (T == 0) return KQ_OK;
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
     const Out out = {logp, entropy, lse, top_id, top_logp, info};
-    if (dtype == KQ_BF16)
-        logprob_kernel<<<static_cast<unsigned>(T), kThreads, 0, stream>>>(static_cast<const __nv_bfloat16*>(logits), V, ld, target,
-                                                                        top, out);
-    else
-        logprob_kernel<<<static_cast<unsigned>(T), kThreads, 0, stream>>>(static_cast<const float*>(logits), V, ld, target, top, out);
+    // A row's joint steps take a block about as long as half a large row's values: many small blocks on an SM
+    // cover them for each other; a block with the SM to itself is shorter with more threads.
+    const bool many = T > 2 * num_sms();
+    if (dtype == KQ_BF16) {
+        const __nv_bfloat16* x = static_cast<const __nv_bfloat16*>(logits);
+        if (many) logprob_kernel<__nv_bfloat16, kThreads><<<static_cast<unsigned>(T), kThreads, 0, stream>>>(x, V, ld, target, top, out);
+        else logprob_kernel<__nv_bfloat16, kWide><<<static_cast<unsigned>(T), kWide, 0, stream>>>(x, V, ld, target, top, out);
+    } else {
+        const float* x = static_cast<const float*>(logits);
+        if (many) logprob_kernel<float, kThreads><<<static_cast<unsigned>(T), kThreads, 0, stream>>>(x, V, ld, target, top, out);
+        else logprob_kernel<float, kWide><<<static_cast<unsigned>(T), kWide, 0, stream>>>(x, V, ld, target, top, out);
+    }
     KQ_LAUNCH_CHECK("logprob_kernel");
     return KQ_OK;
 }
