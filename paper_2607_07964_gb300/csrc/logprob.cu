@@ -8,14 +8,16 @@
 // entropy's two terms do not cancel beyond a few units. t is formed by one fma, the same for every
 // use, so a rounding of r cancels from logp and entropy, however large the logits are.
 //
-// The largest `top` values: the top-th largest of the threads' own maxima (by value, then index, so
-// that no two are equal) bounds the answer from below, and at most `top` threads have a value that
-// reaches it: only their share of the row, still in L2, is read again, for the few values above the bound.
+// The largest `top` values: a bound that at least `top` of the threads' maxima reach, and the row's groups
+// of kAhead vectors whose own maximum, noted in 16 bits in shared memory along the way, reaches it
+// too: only those few are read again. (Going through all values of the threads that reach the bound
+// instead reads a third of the row a second time, when it has left L2.)
 //
 // What bounds it: with V = 128000 in bf16 a row is 256 KB, 5.7 us of an SM's share of the memory
 // bandwidth, against about 6 instructions a value (3 us) and 1.5 us for the joint steps, which
 // other rows' blocks on the SM cover. The gradient reads and writes a row once.
 #include <algorithm>
+#include <atomic>
 
 #include "kv_common.cuh"
 
@@ -26,7 +28,7 @@ constexpr int kThreads = 256;             // of a block where there are rows for
 constexpr int kWide = 1024;               // where there are few
 constexpr int kAhead = 4;                 // 16-byte loads of a thread in flight
 constexpr int kList = 1024;               // candidates for the top values
-constexpr int kChosen = 64;               // threads whose values are looked through for them
+constexpr int kGroups = 256;              // groups that are looked through for them
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kSlack = 4.0f;
 constexpr float kFloor = -2.0e38f;        // what a masked logit counts as: 2^t = 0 and t a number
@@ -151,7 +153,8 @@ __global__ void __launch_bounds__(NT, 1536 / NT) logprob_kernel(const T* __restr
     constexpr int E = 16 / sizeof(T), kWarps = NT / 32;
     __shared__ uint64_t tmp64[kWarps], list[kList];
     __shared__ float tmp[2][kWarps][4];
-    __shared__ int chosen[kChosen], n_chosen, n_list;
+    __shared__ int groups[kGroups], n_groups, n_list;
+    extern __shared__ uint16_t group_max[];   // [group of a thread][thread]: upper half of the maximum's order
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t r = blockIdx.x;
     const T* x = logits + r * ld;
@@ -164,7 +167,7 @@ __global__ void __launch_bounds__(NT, 1536 / NT) logprob_kernel(const T* __restr
     const int my_edge = tid < edge ? (tid < head ? tid : head + nvec * E + tid - head) : -1;
 
     float ref = kFloor, ref2 = 0.0f, z = 0.0f, w = 0.0f, best = -INFINITY;
-    int best_vec = -1;
+    int best_group = 0, n_mine = 0;   // of this thread's groups
     auto take = [&](float top_value, const float* v, int n) {
         if (top_value > ref + kSlack) {
             const float nr2 = top_value * kLog2e, f = ref == kFloor ? 0.0f : ex2(ref2 - nr2);
@@ -180,31 +183,48 @@ __global__ void __launch_bounds__(NT, 1536 / NT) logprob_kernel(const T* __restr
             w = fmaf(e, t, w);
         }
     };
-    auto take_vec = [&](const uint4& u, int j) {
-        float v[E];
-        const float m = unpack<T>(u, v);
-        if (m > best) {
-            best = m;
-            best_vec = j;
-        }
-        take(m, v, E);
-    };
+    // the values' order as whole numbers, and its upper half: all of a bf16 value's
+    auto order = [](float v) { return static_cast<uint32_t>(rank_key(v, 0) >> 32); };
     int j = tid;
     for (; j + (kAhead - 1) * NT < nvec; j += kAhead * NT) {
         uint4 u[kAhead];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) u[i] = __ldg(xv + j + i * NT);
+        float gm = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) take_vec(u[i], j + i * NT);
+        for (int i = 0; i < kAhead; ++i) {
+            float v[E];
+            const float m = unpack<T>(u[i], v);
+            gm = fmaxf(gm, m);
+            take(m, v, E);
+        }
+        if (gm > best) {
+            best = gm;
+            best_group = n_mine;
+        }
+        if (top) group_max[n_mine * NT + tid] = static_cast<uint16_t>(order(gm) >> 16);
+        ++n_mine;
     }
-    {
+    if (j < nvec) {
         uint4 u[kAhead - 1];
 #pragma unroll
         for (int i = 0; i < kAhead - 1; ++i)
             if (j + i * NT < nvec) u[i] = __ldg(xv + j + i * NT);
+        float gm = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < kAhead - 1; ++i)
-            if (j + i * NT < nvec) take_vec(u[i], j + i * NT);
+        for (int i = 0; i < kAhead - 1; ++i) {
+            if (j + i * NT >= nvec) break;
+            float v[E];
+            const float m = unpack<T>(u[i], v);
+            gm = fmaxf(gm, m);
+            take(m, v, E);
+        }
+        if (gm > best) {
+            best = gm;
+            best_group = n_mine;
+        }
+        if (top) group_max[n_mine * NT + tid] = static_cast<uint16_t>(order(gm) >> 16);
+        ++n_mine;
     }
     float ev = -INFINITY;
     if (my_edge >= 0) {
@@ -266,38 +286,34 @@ __global__ void __launch_bounds__(NT, 1536 / NT) logprob_kernel(const T* __restr
     }
     if (top == 0) return;
 
-    // ---- the top values. The top-th largest of the threads' maxima, bit by bit from the first in which they
-    // differ; all of them and more are needed when there are fewer threads with values.
-    constexpr int kBits = 8 * sizeof(T);   // bf16 values order by their upper half
-    auto order = [](float v) { return static_cast<uint32_t>(rank_key(v, 0) >> 32) >> (32 - kBits); };
-    uint32_t bound_value = 0;
+    // ---- the top values. A bound that at least `top` threads' maxima reach and not many more: bit by bit
+    // from the first in which they differ, towards the top-th largest. With fewer threads than that, all
+    // values are candidates.
     uint64_t bound = 0;
-    const uint32_t mine_order = has ? order(mine) : 0;
+    if (tid == 0) n_groups = n_list = 0;
     if (max(min(NT, nvec), edge) >= top) {
-        const uint32_t hi = order(m), differ = hi ^ order(low);
-        const int bits = 32 - __clz(differ);   // 0 when all are equal
-        bound_value = bits == 32 ? 0 : hi >> bits << bits;
+        constexpr int kShift = 32 - 8 * sizeof(T);   // bf16: the lower half says nothing
+        const uint32_t mine_order = has ? order(mine) >> kShift : 0, hi = order(m) >> kShift;
+        const int bits = 32 - __clz(hi ^ (order(low) >> kShift));   // 0 when all are equal
+        uint32_t b = bits == 32 ? 0 : hi >> bits << bits;
         for (int bit = bits - 1; bit >= 0; --bit) {
-            const uint32_t cand = bound_value | (1u << bit);
-            if (__syncthreads_count(mine_order >= cand) >= top) bound_value = cand;
+            const uint32_t cand = b | (1u << bit);
+            const int count = __syncthreads_count(mine_order >= cand);
+            if (count >= top) b = cand;
+            if (count >= top && count <= top + top / 2 + 4) break;
         }
-        const uint32_t full = kBits == 32 ? bound_value : bound_value << 16 | (bound_value >> 15 ? 0u : 0xFFFFu);
-        bound = static_cast<uint64_t>(full) << 32;
-    }
-    if (tid == 0) n_chosen = n_list = 0;
-    // a thread's largest key: the first of its largest values
-    uint64_t key = my_edge >= 0 ? rank_key(ev, static_cast<uint32_t>(my_edge)) : 0;
-    if (tid < nvec && best >= ev) {
-        const T* p = reinterpret_cast<const T*>(xv + max(best_vec, tid));   // a thread of -infinities only: its first vector
-        const uint32_t at = static_cast<uint32_t>(p - x);
-#pragma unroll
-        for (int i = 0; i < E; ++i) key = max(key, rank_key(value(p, i), at + i));
+        if (kShift) b = b << 16 | (b >> 15 ? 0u : 0xFFFFu);
+        bound = static_cast<uint64_t>(b) << 32;
     }
     for (int pass = 0;; ++pass) {
         __syncthreads();
-        if (tid < nvec && key >= bound) {
-            const int at = atomicAdd(&n_chosen, 1);
-            if (at < kChosen) chosen[at] = tid;
+        const uint32_t bound_half = static_cast<uint32_t>(bound >> 48), bound_index = key_index(bound);
+        for (int g = 0; g < n_mine; ++g) {
+            const uint32_t gm = group_max[g * NT + tid];
+            const int first = g * kAhead * NT + tid;   // its first vector
+            if (gm < bound_half || (gm == bound_half && static_cast<uint32_t>(head + first * E) > bound_index)) continue;
+            const int at = atomicAdd(&n_groups, 1);
+            if (at < kGroups) groups[at] = first;
         }
         auto offer = [&](uint64_t k) {
             if (k < bound) return;
@@ -306,30 +322,44 @@ __global__ void __launch_bounds__(NT, 1536 / NT) logprob_kernel(const T* __restr
         };
         if (my_edge >= 0) offer(rank_key(ev, static_cast<uint32_t>(my_edge)));
         __syncthreads();
-        if (n_chosen <= kChosen) {
-            for (int s = warp; s < n_chosen; s += kWarps)
-                for (int i = chosen[s] + lane * NT; i < nvec; i += 32 * NT) {
-                    const uint32_t at = static_cast<uint32_t>(head + i * E);
-                    const uint4 u = xv[i];
-                    const T* q = reinterpret_cast<const T*>(&u);
+        if (n_groups <= kGroups) {
+            for (int q = tid; q < n_groups * kAhead; q += NT) {
+                const int at = groups[q / kAhead] + q % kAhead * NT;
+                if (at >= nvec) continue;
+                const uint4 u = __ldg(xv + at);
+                const uint32_t w4[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-                    for (int e = 0; e < E; ++e) offer(rank_key(value(q, e), at + e));
+                for (int e = 0; e < E; ++e) {
+                    const uint32_t b = sizeof(T) == 4 ? w4[e % 4] : e & 1 ? w4[e / 2] & 0xFFFF0000u : w4[e / 2] << 16;
+                    offer(rank_key(__uint_as_float(b), static_cast<uint32_t>(head + at * E + e)));
                 }
+            }
         }
         __syncthreads();
-        if (n_chosen <= kChosen && n_list <= kList) break;
-        if (pass == 1) {   // more near the bound than the list holds
+        if (n_groups <= kGroups && n_list <= kList) break;
+        if (pass == 1) {   // more near the bound than the lists hold
             careful_row<T, NT>(x, r, V, y, top, out, tmp64);
             return;
         }
-        // too many share the bound's value: of those, the ones with the lowest indices (complements, the largest
-        // first; an index is below 2^20)
-        bound |= 0xFFF00000ull;
-        for (int bit = 19; bit >= 0; --bit) {
+        // Too many near the bound's value: the top-th largest of the threads' first largest values by value and index
+        // (complements, the largest first; an index is below 2^20).
+        uint64_t key = my_edge >= 0 ? rank_key(ev, static_cast<uint32_t>(my_edge)) : 0;
+        for (int i = 0; i < kAhead; ++i) {
+            const int at = best_group * kAhead * NT + tid + i * NT;
+            if (at >= nvec) break;
+            for (int e = 0; e < E; ++e)
+                key = max(key, rank_key(value(reinterpret_cast<const T*>(xv + at), e), static_cast<uint32_t>(head + at * E + e)));
+        }
+        bound = 0;
+        for (int bit = 63; bit >= 0; --bit) {
+            if (bit < 32 && bit >= 20) {
+                bound |= 1ull << bit;
+                continue;
+            }
             const uint64_t cand = bound | (1ull << bit);
             if (__syncthreads_count(key >= cand) >= top) bound = cand;
         }
-        if (tid == 0) n_chosen = n_list = 0;
+        if (tid == 0) n_groups = n_list = 0;
     }
     const int n = n_list;
     for (int c = tid; c < n; c += NT) {
@@ -341,6 +371,21 @@ __global__ void __launch_bounds__(NT, 1536 / NT) logprob_kernel(const T* __restr
             out.top_logp[r * top + rank] = (fmaf(key_value(k), kLog2e, -r2) - lz2) * kLn2;
         }
     }
+}
+
+template <typename T, int NT>
+kq_status run_logprob(const T* logits, int64_t rows, int64_t V, int64_t ld, const int64_t* target, int top, const Out& out,
+                      cudaStream_t stream) {
+    const int64_t group = kAhead * NT * (16 / sizeof(T));   // values of a group of every thread
+    const size_t smem = top ? static_cast<size_t>(cdiv(V, group)) * NT * sizeof(uint16_t) : 0;
+    static std::atomic<uint64_t> done{0};
+    KQ_TRY(once_per_device(done, [&] {
+        KQ_CUDA(cudaFuncSetAttribute(logprob_kernel<T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     static_cast<int>(cdiv(KQ_LOGPROBS_MAX_V, group) * NT * sizeof(uint16_t))));
+        return KQ_OK;
+    }));
+    logprob_kernel<T, NT><<<static_cast<unsigned>(rows), NT, smem, stream>>>(logits, V, ld, target, top, out);
+    return KQ_OK;
 }
 
 template <typename T>
@@ -358,51 +403,52 @@ __device__ __forceinline__ float grad_of(float x, float sum, float g, float ge, 
     return p > 0.0f ? -p * fmaf(ge, lp + h, g) : p == p ? 0.0f : p;
 }
 
-// A block for kAhead x kThreads vectors of a row (VEC), or as many values.
+// Blocks (row, part). VEC: logits and grad have the same place in 16 bytes, so a row is vectors with a few
+// values before and after them; else one value at a time.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads) logprob_grad_kernel(const Grad<T> a) {
-    constexpr int E = VEC ? 16 / sizeof(T) : 1;
+    constexpr int E = 16 / sizeof(T);
     const int64_t r = blockIdx.x;
+    const T* x = a.logits + r * a.ld;
+    T* d = a.grad + r * a.ld_grad;
     const int64_t y = a.target[r];
     if (y >= a.V && threadIdx.x == 0 && blockIdx.y == 0) record_error(a.info, -KQ_ERR_INVALID_ARG);
     const float sum = a.lse[r], g = y >= 0 && y < a.V ? a.g_logp[r] : 0.0f;
     const float ge = a.g_entropy ? a.g_entropy[r] : 0.0f, h = a.g_entropy ? a.entropy[r] : 0.0f;
     const bool none = sum == -INFINITY;
-    const T* x = a.logits + r * a.ld;
-    T* d = a.grad + r * a.ld_grad;
-    const int64_t n = (a.V + E - 1) / E;
-    for (int64_t j0 = static_cast<int64_t>(blockIdx.y) * kThreads * kAhead + threadIdx.x; j0 < n;
-         j0 += static_cast<int64_t>(gridDim.y) * kThreads * kAhead) {
-        if constexpr (VEC) {
+    auto one = [&](int64_t v) {
+        const float q = none ? 0.0f : grad_of(value(x, v), sum, g, ge, h);
+        d[v] = static_cast<T>(v == y && !none ? q + g : q);
+    };
+    if constexpr (VEC) {
+        const int64_t head = min(a.V, static_cast<int64_t>((16 - (reinterpret_cast<uintptr_t>(x) & 15)) % 16 / sizeof(T)));
+        const int64_t n = (a.V - head) / E, tail = a.V - head - n * E;
+        const uint4* xv = reinterpret_cast<const uint4*>(x + head);
+        uint4* dv = reinterpret_cast<uint4*>(d + head);
+        if (blockIdx.y == 0 && threadIdx.x < head + tail)
+            one(threadIdx.x < head ? threadIdx.x : n * E + threadIdx.x);
+        const int64_t ty = y >= head && !none ? (y - head) / E : -1;   // the target's vector
+        const int64_t step = static_cast<int64_t>(gridDim.y) * kThreads * kAhead;
+        for (int64_t j0 = static_cast<int64_t>(blockIdx.y) * kThreads * kAhead + threadIdx.x; j0 < n; j0 += step) {
             uint4 u[kAhead];
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const int64_t j = j0 + i * kThreads;
-                if ((j + 1) * E <= a.V) u[i] = reinterpret_cast<const uint4*>(x)[j];
-            }
+            for (int i = 0; i < kAhead; ++i)
+                if (j0 + i * kThreads < n) u[i] = __ldcs(xv + j0 + i * kThreads);
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
                 const int64_t j = j0 + i * kThreads;
                 if (j >= n) break;
-                if ((j + 1) * E > a.V) {   // the row's last values
-                    for (int64_t v = j * E; v < a.V; ++v) {
-                        const float q = none ? 0.0f : grad_of(value(x, v), sum, g, ge, h);
-                        d[v] = static_cast<T>(v == y && !none ? q + g : q);
-                    }
-                    break;
-                }
                 float q[E];
                 const uint32_t w[4] = {u[i].x, u[i].y, u[i].z, u[i].w};
 #pragma unroll
                 for (int k = 0; k < E; ++k) {
-                    const float v = sizeof(T) == 4 ? __uint_as_float(w[k % 4])
-                                                   : __uint_as_float(k & 1 ? w[k / 2] & 0xFFFF0000u : w[k / 2] << 16);
-                    q[k] = none ? 0.0f : grad_of(v, sum, g, ge, h);
+                    const uint32_t b = sizeof(T) == 4 ? w[k % 4] : k & 1 ? w[k / 2] & 0xFFFF0000u : w[k / 2] << 16;
+                    q[k] = none ? 0.0f : grad_of(__uint_as_float(b), sum, g, ge, h);
                 }
-                if (y / E == j && y >= 0 && !none) {
+                if (j == ty) {
 #pragma unroll
                     for (int k = 0; k < E; ++k)
-                        if (j * E + k == y) q[k] += g;
+                        if (head + j * E + k == y) q[k] += g;
                 }
                 uint4 o;
                 if constexpr (sizeof(T) == 4) {
@@ -416,25 +462,24 @@ __global__ void __launch_bounds__(kThreads) logprob_grad_kernel(const Grad<T> a)
                     }
                     o = make_uint4(b[0], b[1], b[2], b[3]);
                 }
-                reinterpret_cast<uint4*>(d)[j] = o;
-            }
-        } else {
-            for (int i = 0; i < kAhead; ++i) {
-                const int64_t v = j0 + i * kThreads;
-                if (v >= n) break;
-                const float q = none ? 0.0f : grad_of(value(x, v), sum, g, ge, h);
-                d[v] = static_cast<T>(v == y && !none ? q + g : q);
+                __stcs(dv + j, o);
             }
         }
+    } else {
+        for (int64_t v = static_cast<int64_t>(blockIdx.y) * kThreads + threadIdx.x; v < a.V;
+             v += static_cast<int64_t>(gridDim.y) * kThreads)
+            one(v);
     }
 }
 
 template <typename T>
 kq_status run_grad(const Grad<T>& a, int64_t rows, cudaStream_t stream) {
-    const bool vec = !((reinterpret_cast<uintptr_t>(a.logits) | reinterpret_cast<uintptr_t>(a.grad)) & 15u) &&
-                     !((a.ld * sizeof(T)) & 15u) && !((a.ld_grad * sizeof(T)) & 15u);
-    const int64_t n = vec ? cdiv(a.V, 16 / sizeof(T)) : a.V;
-    const dim3 grid(static_cast<unsigned>(rows), static_cast<unsigned>(std::min<int64_t>(cdiv(n, kThreads * kAhead), 65535)));
+    const bool vec = !((reinterpret_cast<uintptr_t>(a.logits) - reinterpret_cast<uintptr_t>(a.grad)) & 15u) &&
+                     !(((a.ld - a.ld_grad) * sizeof(T)) & 15u);
+    // a row to a block, cut in parts of at least one round of its threads while there are few rows
+    const int64_t rounds = cdiv(a.V, vec ? 16 / sizeof(T) * kThreads * kAhead : kThreads);
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(rounds, cdiv(static_cast<int64_t>(num_sms()) * 16, rows)));
+    const dim3 grid(static_cast<unsigned>(rows), static_cast<unsigned>(std::min<int64_t>(parts, 65535)));
     if (vec) logprob_grad_kernel<T, true><<<grid, kThreads, 0, stream>>>(a);
     else logprob_grad_kernel<T, false><<<grid, kThreads, 0, stream>>>(a);
     KQ_LAUNCH_CHECK("logprob_grad_kernel");
@@ -482,15 +527,17 @@ extern "C" kq_status kq_token_logprobs(const void* logits, int dtype, int64_t T,
     // A row's joint steps take a block about as long as half a large row's values: many small blocks on an SM
     // cover them for each other; a block with the SM to itself is shorter with more threads.
     const bool many = T > 2 * num_sms();
+    kq_status launched;
     if (dtype == KQ_BF16) {
         const __nv_bfloat16* x = static_cast<const __nv_bfloat16*>(logits);
-        if (many) logprob_kernel<__nv_bfloat16, kThreads><<<static_cast<unsigned>(T), kThreads, 0, stream>>>(x, V, ld, target, top, out);
-        else logprob_kernel<__nv_bfloat16, kWide><<<static_cast<unsigned>(T), kWide, 0, stream>>>(x, V, ld, target, top, out);
+        launched = many ? run_logprob<__nv_bfloat16, kThreads>(x, T, V, ld, target, top, out, stream)
+                        : run_logprob<__nv_bfloat16, kWide>(x, T, V, ld, target, top, out, stream);
     } else {
         const float* x = static_cast<const float*>(logits);
-        if (many) logprob_kernel<float, kThreads><<<static_cast<unsigned>(T), kThreads, 0, stream>>>(x, V, ld, target, top, out);
-        else logprob_kernel<float, kWide><<<static_cast<unsigned>(T), kWide, 0, stream>>>(x, V, ld, target, top, out);
+        launched = many ? run_logprob<float, kThreads>(x, T, V, ld, target, top, out, stream)
+                        : run_logprob<float, kWide>(x, T, V, ld, target, top, out, stream);
     }
+    KQ_TRY(launched);
     KQ_LAUNCH_CHECK("logprob_kernel");
     return KQ_OK;
 }
