@@ -7,9 +7,10 @@
 // instead of 8 (D = 128: 68 bytes a row, 4.25 bits a value).
 //
 // Both are bound by memory: append reads 2 D e and writes D + 8 bytes for each token and head
-// (e bytes a value), read the reverse. D / 8 lanes take a row, 8 values each, which is one 16-byte
-// load of bf16 (two of fp32) and one 4-byte word of codes; the minimum and maximum go through
-// shuffles inside those lanes, so nothing is staged.
+// (e bytes a value), read the reverse. A warp takes a token and a few of its heads, so that sequence,
+// slot and page are looked up once for all of them; half of it takes the key's row, half the
+// value's (D = 64: two heads at a time), 8 values to a lane, which is one 16-byte load of bf16 (two
+// of fp32) and one word of codes. The minimum and maximum go through shuffles inside those lanes.
 #include <algorithm>
 
 #include "kv_common.cuh"
@@ -73,15 +74,31 @@ struct RowSource {
     int64_t token[2], head[2];      // strides in elements
 };
 
-// One row per D / 8 lanes; rows are ordered (token, head, key then value).
+// How many heads of a token a warp takes, at most: kBatch at a time.
+constexpr int kBatch = 4;
+
+// A warp's token: its sequence, slot and the granule rows of head 0, or none.
+struct Token {
+    int b, t;            // sequence (-1: none), token in the granule
+    int64_t slot;
+    uint8_t* g;          // granule of head 0, or nullptr: no such slot or page
+};
+__device__ __forceinline__ Token locate(const KvView& c, int b, int64_t slot, int64_t most) {
+    Token k = {b, 0, slot, nullptr};
+    if (slot >= 0 && slot < most) {
+        k.g = kv_granule(c, b, 0, slot);
+        k.t = static_cast<int>(slot % kGranule);
+    }
+    return k;
+}
+
 template <typename T, int D, bool VEC>
-__global__ void __launch_bounds__(kThreads) kv_append_kernel(KvView c, RowSource src, int64_t tokens,
+__global__ void __launch_bounds__(kThreads) kv_append_kernel(KvView c, RowSource src, int64_t tokens, int groups, int per,
                                                              const int32_t* __restrict__ start,
                                                              const int32_t* __restrict__ lens, int32_t* lens_out,
                                                              float* __restrict__ acc, int32_t* __restrict__ pos, int64_t S,
                                                              const int32_t* __restrict__ seen, int32_t* seen_out, int* info) {
-    constexpr int kLanes = D / 8;
-    const int64_t tid = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
+    constexpr int kLanes = D / 8, kRowsAtOnce = 32 / kLanes;   // D = 128: a head's two rows; 64: two heads'
     const int64_t cap = kv_capacity(c);
     if (blockIdx.x == 0) {
         for (int b = threadIdx.x; b < c.batch; b += kThreads) {
@@ -93,124 +110,160 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(KvView c, RowSource
         }
         if (threadIdx.x == 0 && (start[0] != 0 || start[c.batch] != tokens)) record_error(info, -KQ_ERR_INVALID_ARG);
     }
-    const int lane = threadIdx.x % kLanes;
-    const uint32_t mask = (kLanes == 16 ? 0xFFFFu : 0xFFu) << (threadIdx.x % 32 - lane);
-    const int64_t rows = tokens * c.kv_heads * 2;
-    for (int64_t row = tid / kLanes; row < rows; row += static_cast<int64_t>(gridDim.x) * (kThreads / kLanes)) {
-        const int which = static_cast<int>(row & 1);
-        const int h = static_cast<int>((row >> 1) % c.kv_heads);
-        const int64_t i = (row >> 1) / c.kv_heads;
-        const int b = kv_sequence_of(start, c.batch, i);
-        if (b < 0) continue;   // uniform over the row's lanes; recorded by the first block
+    const int lane = threadIdx.x & 31, in_row = lane % kLanes, sub = lane / kLanes;
+    const int which = sub & 1;
+    const uint32_t mask = (kLanes == 16 ? 0xFFFFu : 0xFFu) << (lane - in_row);
+    const int64_t warps = static_cast<int64_t>(gridDim.x) * (kThreads / 32);
+    for (int64_t item = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5); item < tokens * groups;
+         item += warps) {
+        const int64_t i = groups == 1 ? item : item / groups;
+        const int h0 = static_cast<int>(item - i * groups) * per, h1 = min(h0 + per, c.kv_heads);
+        const int b = kv_sequence_of_warp(start, c.batch, i);
+        if (b < 0) continue;   // recorded by the first block
         const int64_t n = kv_length(lens, b, cap, info);
-        const int64_t slot = n + (i - start[b]);
-        uint8_t* g = slot < cap ? kv_granule(c, b, h, slot) : nullptr;
-        if (!g) {
+        const int64_t index = i - start[b];
+        const Token k = locate(c, b, n + index, cap);
+        if (!k.g) {
             record_error(info, -KQ_ERR_INVALID_ARG);
             continue;
         }
-        const T* p = static_cast<const T*>(src.p[which]) + i * src.token[which] + h * src.head[which] + lane * 8;
-        float x[8];
-        load8<T, VEC>(p, x);
-        float lo = x[0], hi = x[0];
-        bool fine = true;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            lo = fminf(lo, x[k]);
-            hi = fmaxf(hi, x[k]);
-            fine &= fabsf(x[k]) <= 3.402823466e38f;   // false for NaN as well
-        }
-#pragma unroll
-        for (int o = kLanes / 2; o > 0; o >>= 1) {
-            lo = fminf(lo, __shfl_xor_sync(mask, lo, o));
-            hi = fmaxf(hi, __shfl_xor_sync(mask, hi, o));
-        }
-        fine = __all_sync(mask, fine);
-        // down to bf16: negative values get a larger magnitude; up to bf16: the scale is >= 0
-        const uint32_t lb = __float_as_uint(lo);
-        const uint32_t ob = (lb + ((lb >> 31) ? 0xFFFFu : 0u)) & 0xFFFF0000u;
-        const float off = __uint_as_float(ob);
-        const uint32_t sb = (__float_as_uint(__fdiv_rn(__fsub_rn(hi, off), 15.0f)) + 0xFFFFu) & 0xFFFF0000u;
-        const float s = __uint_as_float(sb);
-        fine = fine && isfinite(off) && isfinite(s);
-        uint32_t word = 0;
-        if (fine && s > 0.0f) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float q = fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(x[k], off), s)), 0.0f), 15.0f);
-                word |= static_cast<uint32_t>(q) << (4 * k);
+        if (acc || pos) {
+            if (k.slot < S) {
+                for (int h = h0 + lane; h < h1; h += 32) {
+                    const int64_t at = (static_cast<int64_t>(b) * c.kv_heads + h) * S + k.slot;
+                    if (acc) acc[at] = 0.0f;
+                    if (pos) pos[at] = static_cast<int32_t>((seen ? seen[b] : n) + index);
+                }
+            } else {
+                record_error(info, -KQ_ERR_INVALID_ARG);
             }
         }
-        const int t = static_cast<int>(slot % kGranule);
-        reinterpret_cast<uint32_t*>(g + kv_code_at(D, which, t))[lane] = word;
-        if (lane == 0) {
-            *reinterpret_cast<uint32_t*>(g + kv_param_at(D, which, t)) = fine ? (sb >> 16) | ob : 0x7FC07FC0u;
-            if (which == 0 && (acc || pos)) {
-                if (slot < S) {
-                    const int64_t at = (static_cast<int64_t>(b) * c.kv_heads + h) * S + slot;
-                    if (acc) acc[at] = 0.0f;
-                    if (pos) pos[at] = static_cast<int32_t>((seen ? seen[b] : n) + (i - start[b]));
-                } else {
-                    record_error(info, -KQ_ERR_INVALID_ARG);
+        const T* p = static_cast<const T*>(src.p[which]) + i * src.token[which] + in_row * 8;
+        for (int hb = h0; hb < h1; hb += kBatch) {
+            float x[kBatch / (kRowsAtOnce / 2)][8];
+            constexpr int kRounds = kBatch / (kRowsAtOnce / 2);
+#pragma unroll
+            for (int u = 0; u < kRounds; ++u) {
+                const int h = hb + u * (kRowsAtOnce / 2) + (sub >> 1);
+                if (h < h1) load8<T, VEC>(p + h * src.head[which], x[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < kRounds; ++u) {
+                const int h = hb + u * (kRowsAtOnce / 2) + (sub >> 1);
+                if (h >= h1) continue;   // uniform over a row's lanes
+                float lo = x[u][0], hi = x[u][0];
+                uint32_t top = 0;        // as bits: an infinity or a NaN is above every number
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    lo = fminf(lo, x[u][j]);
+                    hi = fmaxf(hi, x[u][j]);
+                    top = max(top, __float_as_uint(x[u][j]) & 0x7FFFFFFFu);
                 }
+#pragma unroll
+                for (int o = kLanes / 2; o > 0; o >>= 1) {
+                    lo = fminf(lo, __shfl_xor_sync(mask, lo, o));
+                    hi = fmaxf(hi, __shfl_xor_sync(mask, hi, o));
+                }
+                bool fine = __all_sync(mask, top < 0x7F800000u);
+                // down to bf16: negative values get a larger magnitude; up to bf16: the scale is >= 0
+                const uint32_t lb = __float_as_uint(lo);
+                const uint32_t ob = (lb + ((lb >> 31) ? 0xFFFFu : 0u)) & 0xFFFF0000u;
+                const float off = __uint_as_float(ob);
+                const uint32_t sb = (__float_as_uint(__fdiv_rn(__fsub_rn(hi, off), 15.0f)) + 0xFFFFu) & 0xFFFF0000u;
+                const float s = __uint_as_float(sb);
+                fine = fine && isfinite(off) && isfinite(s);
+                uint32_t word = 0;
+                if (fine && s > 0.0f) {
+                    const float y = div_recip(s);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float q = fminf(fmaxf(rintf(div_rn(__fsub_rn(x[u][j], off), s, y)), 0.0f), 15.0f);
+                        word |= static_cast<uint32_t>(q) << (4 * j);
+                    }
+                }
+                uint8_t* g = k.g + h * kv_head_bytes(c);
+                reinterpret_cast<uint32_t*>(g + kv_code_at(D, which, k.t))[in_row] = word;
+                if (in_row == 0)
+                    *reinterpret_cast<uint32_t*>(g + kv_param_at(D, which, k.t)) = fine ? (sb >> 16) | ob : 0x7FC07FC0u;
             }
         }
     }
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) kv_read_kernel(KvView c, const int32_t* __restrict__ start,
+__global__ void __launch_bounds__(kThreads) kv_read_kernel(KvView c, int groups, int per, const int32_t* __restrict__ start,
                                                            const int32_t* __restrict__ first,
                                                            const int32_t* __restrict__ lens, int64_t tokens,
-                                                           T* __restrict__ k, T* __restrict__ v, int* info) {
-    constexpr int kLanes = D / 8;
-    const int64_t tid = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-    const int lane = threadIdx.x % kLanes;
+                                                           T* __restrict__ k_out, T* __restrict__ v_out, int* info) {
+    constexpr int kLanes = D / 8, kRowsAtOnce = 32 / kLanes, kRounds = kBatch / (kRowsAtOnce / 2);
+    const int lane = threadIdx.x & 31, in_row = lane % kLanes, sub = lane / kLanes, which = sub & 1;
     const int64_t cap = kv_capacity(c);
-    const int64_t rows = tokens * c.kv_heads * 2;
-    for (int64_t row = tid / kLanes; row < rows; row += static_cast<int64_t>(gridDim.x) * (kThreads / kLanes)) {
-        const int which = static_cast<int>(row & 1);
-        const int h = static_cast<int>((row >> 1) % c.kv_heads);
-        const int64_t i = (row >> 1) / c.kv_heads;
-        const int b = kv_sequence_of(start, c.batch, i);
-        const uint8_t* g = nullptr;
-        int64_t slot = 0;
+    const int64_t warps = static_cast<int64_t>(gridDim.x) * (kThreads / 32);
+    for (int64_t item = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5); item < tokens * groups;
+         item += warps) {
+        const int64_t i = groups == 1 ? item : item / groups;
+        const int h0 = static_cast<int>(item - i * groups) * per, h1 = min(h0 + per, c.kv_heads);
+        const int b = kv_sequence_of_warp(start, c.batch, i);
+        Token k = {-1, 0, 0, nullptr};
         if (b >= 0) {
-            slot = (first ? first[b] : 0) + (i - start[b]);
             const int64_t n = lens ? kv_length(lens, b, cap, info) : cap;
-            if (slot < 0) record_error(info, -KQ_ERR_INVALID_ARG);
-            if (slot >= 0 && slot < n) {
-                g = kv_granule(c, b, h, slot);
-                if (!g) record_error(info, -KQ_ERR_INVALID_ARG);
-            }
+            k = locate(c, b, (first ? first[b] : 0) + (i - start[b]), n);
+            if (k.slot < 0 || (k.slot < n && !k.g)) record_error(info, -KQ_ERR_INVALID_ARG);
         }
-        float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (g) {
-            const int t = static_cast<int>(slot % kGranule);
-            const uint32_t word = reinterpret_cast<const uint32_t*>(g + kv_code_at(D, which, t))[lane];
-            const uint32_t prm = *reinterpret_cast<const uint32_t*>(g + kv_param_at(D, which, t));
-            const float s = kv_scale(prm), off = kv_offset(prm);
+        T* out = (which ? v_out : k_out) + i * c.kv_heads * D + in_row * 8;
+        for (int hb = h0; hb < h1; hb += kBatch) {
+            uint32_t word[kRounds], prm[kRounds];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = fmaf(s, static_cast<float>((word >> (4 * j)) & 15u), off);
-        }
-        T* out = (which ? v : k) + (i * c.kv_heads + h) * D + lane * 8;
-        if constexpr (sizeof(T) == 2) {
-            uint32_t w[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const __nv_bfloat162 p = __floats2bfloat162_rn(x[2 * j], x[2 * j + 1]);
-                w[j] = *reinterpret_cast<const uint32_t*>(&p);
+            for (int u = 0; u < kRounds; ++u) {
+                const int h = hb + u * (kRowsAtOnce / 2) + (sub >> 1);
+                word[u] = prm[u] = 0;
+                if (k.g && h < h1) {
+                    const uint8_t* g = k.g + h * kv_head_bytes(c);
+                    word[u] = reinterpret_cast<const uint32_t*>(g + kv_code_at(D, which, k.t))[in_row];
+                    prm[u] = *reinterpret_cast<const uint32_t*>(g + kv_param_at(D, which, k.t));
+                }
             }
-            *reinterpret_cast<uint4*>(out) = make_uint4(w[0], w[1], w[2], w[3]);
-        } else {
-            reinterpret_cast<float4*>(out)[0] = make_float4(x[0], x[1], x[2], x[3]);
-            reinterpret_cast<float4*>(out)[1] = make_float4(x[4], x[5], x[6], x[7]);
+#pragma unroll
+            for (int u = 0; u < kRounds; ++u) {
+                const int h = hb + u * (kRowsAtOnce / 2) + (sub >> 1);
+                if (h >= h1) continue;
+                const float s = kv_scale(prm[u]), off = kv_offset(prm[u]);   // 0 where there is nothing to read
+                float x[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = fmaf(s, static_cast<float>((word[u] >> (4 * j)) & 15u), off);
+                T* dst = out + static_cast<int64_t>(h) * D;
+                if constexpr (sizeof(T) == 2) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const __nv_bfloat162 p = __floats2bfloat162_rn(x[2 * j], x[2 * j + 1]);
+                        w[j] = *reinterpret_cast<const uint32_t*>(&p);
+                    }
+                    *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+                } else {
+                    reinterpret_cast<float4*>(dst)[0] = make_float4(x[0], x[1], x[2], x[3]);
+                    reinterpret_cast<float4*>(dst)[1] = make_float4(x[4], x[5], x[6], x[7]);
+                }
+            }
         }
     }
 }
 
-int64_t row_blocks(int64_t rows, int dim) {
-    return std::max<int64_t>(1, std::min<int64_t>(cdiv(rows * (dim / 8), kThreads), static_cast<int64_t>(num_sms()) * 32));
+// Heads to a warp: all of a token's, unless that leaves SMs without work.
+struct Cut {
+    int groups, per;
+    unsigned grid;
+};
+Cut cut(int64_t tokens, int kv_heads) {
+    Cut k;
+    const int64_t want = cdiv(static_cast<int64_t>(num_sms()) * 16, std::max<int64_t>(1, tokens));
+    const int64_t most = cdiv(kv_heads, kBatch);
+    k.groups = static_cast<int>(std::max<int64_t>(1, std::min(want, most)));
+    k.per = static_cast<int>(cdiv(cdiv(kv_heads, k.groups), kBatch) * kBatch);
+    k.groups = static_cast<int>(cdiv(kv_heads, k.per));
+    k.grid = static_cast<unsigned>(std::max<int64_t>(
+        1, std::min<int64_t>(cdiv(tokens * k.groups, kThreads / 32), static_cast<int64_t>(num_sms()) * 16)));
+    return k;
 }
 
 }  // namespace
@@ -243,10 +296,11 @@ extern "C" kq_status kq_kv_append(const kq_kv_cache* cache, const void* k, const
     bool vec = true;
     for (int w = 0; w < 2; ++w)
         vec = vec && !(reinterpret_cast<uintptr_t>(src.p[w]) & 15u) && !((src.token[w] * es) & 15u) && !((src.head[w] * es) & 15u);
-    const unsigned grid = static_cast<unsigned>(row_blocks(T * c.kv_heads * 2, c.dim));
+    const Cut k_ = cut(T, c.kv_heads);
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
 #define KQ_APPEND(TY, DIM, VEC) \
-    kv_append_kernel<TY, DIM, VEC><<<grid, kThreads, 0, stream>>>(c, src, T, start, lens, lens_out, acc, pos, S, seen, seen_out, info)
+    kv_append_kernel<TY, DIM, VEC><<<k_.grid, kThreads, 0, stream>>>(c, src, T, k_.groups, k_.per, start, lens, lens_out, acc, pos, S, \
+                                                                      seen, seen_out, info)
     if (dtype == KQ_BF16) {
         if (c.dim == 128) vec ? KQ_APPEND(__nv_bfloat16, 128, true) : KQ_APPEND(__nv_bfloat16, 128, false);
         else vec ? KQ_APPEND(__nv_bfloat16, 64, true) : KQ_APPEND(__nv_bfloat16, 64, false);
@@ -274,11 +328,11 @@ extern "C" kq_status kq_kv_read(const kq_kv_cache* cache, const int32_t* start, 
         return KQ_ERR_INVALID_ARG;
     }
     if (T == 0) return KQ_OK;
-    const unsigned grid = static_cast<unsigned>(row_blocks(T * c.kv_heads * 2, c.dim));
+    const Cut k_ = cut(T, c.kv_heads);
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
 #define KQ_READ(TY, DIM)                                                                                         \
-    kv_read_kernel<TY, DIM><<<grid, kThreads, 0, stream>>>(c, start, first, lens, T, static_cast<TY*>(k), \
-                                                           static_cast<TY*>(v), info)
+    kv_read_kernel<TY, DIM><<<k_.grid, kThreads, 0, stream>>>(c, k_.groups, k_.per, start, first, lens, T, static_cast<TY*>(k), \
+                                                              static_cast<TY*>(v), info)
     if (dtype == KQ_BF16) c.dim == 128 ? KQ_READ(__nv_bfloat16, 128) : KQ_READ(__nv_bfloat16, 64);
     else c.dim == 128 ? KQ_READ(float, 128) : KQ_READ(float, 64);
 #undef KQ_READ

@@ -114,16 +114,18 @@ def _ok(st: int, where: str) -> None:
 
 
 def _ptr(t):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 def _stream(stream):
-    s = torch.cuda.current_stream() if stream is None else stream
-    return ctypes.c_void_p(s.cuda_stream)
+    if stream is None and torch.cuda.is_initialized():   # the current stream's handle, without an object around it
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
 
 
 def _need(t, name, dtype, shape=None, contiguous=True):
-    if t is None:
+    if t is None or (t.is_cuda and t.dtype is dtype and (shape is None or t.shape == shape) and
+                     (not contiguous or t.is_contiguous())):
         return
     if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
