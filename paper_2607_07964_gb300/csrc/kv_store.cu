@@ -69,6 +69,34 @@ __device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
     }
 }
 
+// The codes rint((x - off) / s) of 8 values, float32 with IEEE division, s > 0. The quotient is first
+// taken with a reciprocal; where the remainder shows it within 2^-17 of a tie (bf16 values often
+// sit on one) or the reciprocal leaves the normal numbers, it is divided.
+__device__ __forceinline__ uint32_t codes8(const float (&x)[8], float off, float s) {
+    constexpr float kRound = 12582912.0f;   // 1.5 * 2^23: adding it rounds to a whole number
+    const float y = div_recip(s);
+    const float edge = y == 0.0f ? -1.0f : s * (0.5f - 0x1p-17f);
+    float r[8], d[8];
+    uint32_t near = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        d[j] = __fsub_rn(x[j], off);
+        r[j] = __fsub_rn(__fmaf_rn(d[j], y, kRound), kRound);
+        if (fabsf(__fmaf_rn(-r[j], s, d[j])) >= edge) near |= 1u << j;
+    }
+    if (near) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (near >> j & 1) r[j] = fminf(fmaxf(rintf(__fdiv_rn(d[j], s)), 0.0f), 15.0f);
+    }
+    uint32_t half[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        half[i] = __float_as_uint(fmaf(fmaf(fmaf(r[4 * i + 3], 16.0f, r[4 * i + 2]), 16.0f, r[4 * i + 1]), 16.0f, r[4 * i]) +
+                                  8388608.0f);
+    return __byte_perm(half[0], half[1], 0x5410);
+}
+
 struct RowSource {
     const void* p[2];               // k, v
     int64_t token[2], head[2];      // strides in elements
@@ -151,20 +179,19 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(KvView c, RowSource
             for (int u = 0; u < kRounds; ++u) {
                 const int h = hb + u * (kRowsAtOnce / 2) + (sub >> 1);
                 if (h >= h1) continue;   // uniform over a row's lanes
-                float lo = x[u][0], hi = x[u][0];
-                uint32_t top = 0;        // as bits: an infinity or a NaN is above every number
+                float lo = x[u][0], hi = x[u][0], odd = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     lo = fminf(lo, x[u][j]);
                     hi = fmaxf(hi, x[u][j]);
-                    top = max(top, __float_as_uint(x[u][j]) & 0x7FFFFFFFu);
+                    odd = fmaf(x[u][j], 0.0f, odd);   // a NaN if one of them is not finite
                 }
 #pragma unroll
                 for (int o = kLanes / 2; o > 0; o >>= 1) {
                     lo = fminf(lo, __shfl_xor_sync(mask, lo, o));
                     hi = fmaxf(hi, __shfl_xor_sync(mask, hi, o));
                 }
-                bool fine = __all_sync(mask, top < 0x7F800000u);
+                bool fine = __all_sync(mask, odd == 0.0f);
                 // down to bf16: negative values get a larger magnitude; up to bf16: the scale is >= 0
                 const uint32_t lb = __float_as_uint(lo);
                 const uint32_t ob = (lb + ((lb >> 31) ? 0xFFFFu : 0u)) & 0xFFFF0000u;
@@ -172,15 +199,7 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(KvView c, RowSource
                 const uint32_t sb = (__float_as_uint(__fdiv_rn(__fsub_rn(hi, off), 15.0f)) + 0xFFFFu) & 0xFFFF0000u;
                 const float s = __uint_as_float(sb);
                 fine = fine && isfinite(off) && isfinite(s);
-                uint32_t word = 0;
-                if (fine && s > 0.0f) {
-                    const float y = div_recip(s);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float q = fminf(fmaxf(rintf(div_rn(__fsub_rn(x[u][j], off), s, y)), 0.0f), 15.0f);
-                        word |= static_cast<uint32_t>(q) << (4 * j);
-                    }
-                }
+                const uint32_t word = fine && s > 0.0f ? codes8(x[u], off, s) : 0u;
                 uint8_t* g = k.g + h * kv_head_bytes(c);
                 reinterpret_cast<uint32_t*>(g + kv_code_at(D, which, k.t))[in_row] = word;
                 if (in_row == 0)

@@ -428,7 +428,8 @@ def test_attend_records_bad_lengths_pages_and_tokens():
     (64, 32, 3, [257, 256], 1, 0, 1, "random"), (128, 16, 1, [500], 200, 200, 0, "random"),
     (64, 48, 2, [3000], 1500, 100, 3, "ties"), (64, 16, 1, [700], 64, 20, 2, "flat"),
     (128, 64, 1, [400], 100, 40, 4, "odd"), (64, 16, 1, [200], 50, 50, 0, "crowd"),
-    (64, 128, 1, [40000], 20011, 100, 4, "ties"), (64, 16, 2, [90], 200, 100, 4, "random")])
+    (64, 128, 1, [40000], 20011, 100, 4, "ties"), (64, 16, 2, [90], 200, 100, 4, "random"),
+    (64, 1024, 1, [420001], 900, 100, 4, "ties"), (128, 64, 1, [4096, 4097, 9000], 4095, 64, 4, "random")])
 @pytest.mark.parametrize("in_place", [False, True])
 def test_evict_keeps_and_moves_the_right_slots(dim, page, heads, lens, budget, recent, sink, kind, in_place):
     rng = np.random.default_rng(len(kind) + budget)
