@@ -285,10 +285,10 @@ extern "C" kq_status kq_kv_evict(const kq_kv_cache* cache, const int32_t* lens, 
         return KQ_OK;
     }));
     // CTAs of a head: one up to 4096 slots, where the exchanges between CTAs would cost more than
-    // they save; as many as keep 2048 slots each beyond, up to a cluster.
+    // they save, or where the heads fill the GPU; else as many as keep 2048 slots each, up to a cluster.
     const int64_t most = std::min(S, kv_capacity(c));
     int ctas = 1;
-    while (ctas < kCluster && most > 4096 && most > 2048 * ctas) ctas *= 2;
+    while (ctas < kCluster && most > 4096 && most > 2048 * ctas && c.batch * c.kv_heads * ctas < 2 * num_sms()) ctas *= 2;
     const Evict e = {c, lens, seen, acc, pos, S, budget, recent, sink, lens_out, acc_out, pos_out, static_cast<int32_t*>(ws), info,
                      static_cast<int32_t>(cdiv(cdiv(most, ctas), kThreads) * kThreads)};
     cudaLaunchConfig_t cfg = {};

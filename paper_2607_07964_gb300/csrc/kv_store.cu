@@ -49,30 +49,33 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// 8 consecutive values. VEC: 16-byte loads (the caller checked base and strides).
+// 8 consecutive values as they are loaded. VEC: 16 bytes at a time (the caller checked base and strides).
 template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
-    if constexpr (VEC && sizeof(T) == 2) {
-        const uint4 u = *reinterpret_cast<const uint4*>(p);
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[2 * i] = __uint_as_float(w[i] << 16);
-            x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-        }
-    } else if constexpr (VEC) {
-        const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = static_cast<float>(p[i]);
-    }
-}
+struct Eight {
+    uint32_t w[VEC && sizeof(T) == 2 ? 4 : 8];
 
-// The codes rint((x - off) / s) of 8 values, float32 with IEEE division, s > 0. The quotient is first
+    __device__ __forceinline__ void load(const T* p) {
+        if constexpr (VEC) {
+#pragma unroll
+            for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) {
+                const uint4 u = reinterpret_cast<const uint4*>(p)[i];
+                w[4 * i] = u.x, w[4 * i + 1] = u.y, w[4 * i + 2] = u.z, w[4 * i + 3] = u.w;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(static_cast<float>(p[i]));
+        }
+    }
+    __device__ __forceinline__ float get(int i) const {
+        if constexpr (VEC && sizeof(T) == 2) return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+        else return __uint_as_float(w[i]);
+    }
+};
+
+// The codes rint((x - off) / s) of 8 values of each lane of a warp, float32 with IEEE division. The quotient is first
 // taken with a reciprocal; where the remainder shows it within 2^-17 of a tie (bf16 values often
-// sit on one) or the reciprocal leaves the normal numbers, it is divided.
-__device__ __forceinline__ uint32_t codes8(const float (&x)[8], float off, float s) {
+// sit on one) or the reciprocal leaves the normal numbers, it is divided. Lanes without `use` get anything.
+__device__ __forceinline__ uint32_t codes8(const float (&x)[8], float off, float s, bool use) {
     constexpr float kRound = 12582912.0f;   // 1.5 * 2^23: adding it rounds to a whole number
     const float y = div_recip(s);
     const float edge = y == 0.0f ? -1.0f : s * (0.5f - 0x1p-17f);
@@ -82,12 +85,17 @@ __device__ __forceinline__ uint32_t codes8(const float (&x)[8], float off, float
     for (int j = 0; j < 8; ++j) {
         d[j] = __fsub_rn(x[j], off);
         r[j] = __fsub_rn(__fmaf_rn(d[j], y, kRound), kRound);
-        if (fabsf(__fmaf_rn(-r[j], s, d[j])) >= edge) near |= 1u << j;
+        if (use && fabsf(__fmaf_rn(-r[j], s, d[j])) >= edge) near |= 1u << j;
     }
-    if (near) {
+    while (__any_sync(0xffffffffu, near)) {   // one of a lane's at a time: few lanes have more than one
+        const int at = __ffs(near) - 1;
+        float q = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (near >> j & 1) r[j] = fminf(fmaxf(rintf(__fdiv_rn(d[j], s)), 0.0f), 15.0f);
+        for (int j = 0; j < 8; ++j) q = j == at ? d[j] : q;
+        q = fminf(fmaxf(rintf(__fdiv_rn(q, s)), 0.0f), 15.0f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) r[j] = j == at ? q : r[j];
+        near &= near - 1;
     }
     uint32_t half[2];
 #pragma unroll
@@ -121,7 +129,7 @@ __device__ __forceinline__ Token locate(const KvView& c, int b, int64_t slot, in
 }
 
 template <typename T, int D, bool VEC>
-__global__ void __launch_bounds__(kThreads) kv_append_kernel(KvView c, RowSource src, int64_t tokens, int groups, int per,
+__global__ void __launch_bounds__(kThreads, 3) kv_append_kernel(KvView c, RowSource src, int64_t tokens, int groups, int per,
                                                              const int32_t* __restrict__ start,
                                                              const int32_t* __restrict__ lens, int32_t* lens_out,
                                                              float* __restrict__ acc, int32_t* __restrict__ pos, int64_t S,
@@ -141,6 +149,8 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(KvView c, RowSource
     const int lane = threadIdx.x & 31, in_row = lane % kLanes, sub = lane / kLanes;
     const int which = sub & 1;
     const uint32_t mask = (kLanes == 16 ? 0xFFFFu : 0xFFu) << (lane - in_row);
+    const int head_bytes = c.page * (D + 8);
+    const int64_t stride = src.head[which];
     const int64_t warps = static_cast<int64_t>(gridDim.x) * (kThreads / 32);
     for (int64_t item = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5); item < tokens * groups;
          item += warps) {
@@ -166,32 +176,38 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(KvView c, RowSource
                 record_error(info, -KQ_ERR_INVALID_ARG);
             }
         }
-        const T* p = static_cast<const T*>(src.p[which]) + i * src.token[which] + in_row * 8;
-        for (int hb = h0; hb < h1; hb += kBatch) {
-            float x[kBatch / (kRowsAtOnce / 2)][8];
-            constexpr int kRounds = kBatch / (kRowsAtOnce / 2);
+        constexpr int kHeads = kRowsAtOnce / 2, kRounds = kBatch / kHeads;   // heads at once, rounds of a batch
+        const T* p = static_cast<const T*>(src.p[which]) + i * src.token[which] + (h0 + (sub >> 1)) * stride + in_row * 8;
+        uint8_t* g = k.g + (h0 + (sub >> 1)) * static_cast<int64_t>(head_bytes);
+        uint8_t* const code_at = g + kv_code_at(D, which, k.t) + in_row * 4;
+        uint8_t* const prm_at = g + kv_param_at(D, which, k.t);
+        int64_t moved = 0;
+        for (int h = h0 + (sub >> 1); h - (sub >> 1) < h1; h += kBatch) {
+            Eight<T, VEC> raw[kRounds];
 #pragma unroll
             for (int u = 0; u < kRounds; ++u) {
-                const int h = hb + u * (kRowsAtOnce / 2) + (sub >> 1);
-                if (h < h1) load8<T, VEC>(p + h * src.head[which], x[u]);
+                if (h + u * kHeads < h1) raw[u].load(p);
+                p += kHeads * stride;
             }
 #pragma unroll
-            for (int u = 0; u < kRounds; ++u) {
-                const int h = hb + u * (kRowsAtOnce / 2) + (sub >> 1);
-                if (h >= h1) continue;   // uniform over a row's lanes
-                float lo = x[u][0], hi = x[u][0], odd = 0.0f;
+            for (int u = 0; u < kRounds; ++u) {   // all lanes go along; rows past the last head are not written
+                const bool real = h + u * kHeads < h1;
+                float x[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = real ? raw[u].get(j) : 0.0f;
+                float lo = x[0], hi = x[0], odd = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    lo = fminf(lo, x[u][j]);
-                    hi = fmaxf(hi, x[u][j]);
-                    odd = fmaf(x[u][j], 0.0f, odd);   // a NaN if one of them is not finite
+                    lo = fminf(lo, x[j]);
+                    hi = fmaxf(hi, x[j]);
+                    odd = fmaf(x[j], 0.0f, odd);   // a NaN if one of them is not finite
                 }
 #pragma unroll
                 for (int o = kLanes / 2; o > 0; o >>= 1) {
-                    lo = fminf(lo, __shfl_xor_sync(mask, lo, o));
-                    hi = fmaxf(hi, __shfl_xor_sync(mask, hi, o));
+                    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+                    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
                 }
-                bool fine = __all_sync(mask, odd == 0.0f);
+                bool fine = (__ballot_sync(0xffffffffu, odd != 0.0f) & mask) == 0;
                 // down to bf16: negative values get a larger magnitude; up to bf16: the scale is >= 0
                 const uint32_t lb = __float_as_uint(lo);
                 const uint32_t ob = (lb + ((lb >> 31) ? 0xFFFFu : 0u)) & 0xFFFF0000u;
@@ -199,11 +215,13 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(KvView c, RowSource
                 const uint32_t sb = (__float_as_uint(__fdiv_rn(__fsub_rn(hi, off), 15.0f)) + 0xFFFFu) & 0xFFFF0000u;
                 const float s = __uint_as_float(sb);
                 fine = fine && isfinite(off) && isfinite(s);
-                const uint32_t word = fine && s > 0.0f ? codes8(x[u], off, s) : 0u;
-                uint8_t* g = k.g + h * kv_head_bytes(c);
-                reinterpret_cast<uint32_t*>(g + kv_code_at(D, which, k.t))[in_row] = word;
-                if (in_row == 0)
-                    *reinterpret_cast<uint32_t*>(g + kv_param_at(D, which, k.t)) = fine ? (sb >> 16) | ob : 0x7FC07FC0u;
+                const bool use = fine && s > 0.0f;
+                const uint32_t word = codes8(x, off, s, use);
+                if (real) {
+                    *reinterpret_cast<uint32_t*>(code_at + moved) = use ? word : 0u;
+                    if (in_row == 0) *reinterpret_cast<uint32_t*>(prm_at + moved) = fine ? (sb >> 16) | ob : 0x7FC07FC0u;
+                }
+                moved += kHeads * static_cast<int64_t>(head_bytes);
             }
         }
     }
