@@ -78,14 +78,19 @@ struct Eight {
 __device__ __forceinline__ uint32_t codes8(const float (&x)[8], float off, float s, bool use) {
     constexpr float kRound = 12582912.0f;   // 1.5 * 2^23: adding it rounds to a whole number
     const float y = div_recip(s);
-    const float edge = y == 0.0f ? -1.0f : s * (0.5f - 0x1p-17f);
-    float r[8], d[8];
-    uint32_t near = 0;
+    const float edge = !use ? INFINITY : y == 0.0f ? -1.0f : s * (0.5f - 0x1p-17f);
+    float r[8], d[8], most = 0.0f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         d[j] = __fsub_rn(x[j], off);
         r[j] = __fsub_rn(__fmaf_rn(d[j], y, kRound), kRound);
-        if (use && fabsf(__fmaf_rn(-r[j], s, d[j])) >= edge) near |= 1u << j;
+        most = fmaxf(most, fabsf(__fmaf_rn(-r[j], s, d[j])));
+    }
+    uint32_t near = 0;
+    if (most >= edge) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (fabsf(__fmaf_rn(-r[j], s, d[j])) >= edge) near |= 1u << j;
     }
     while (__any_sync(0xffffffffu, near)) {   // one of a lane's at a time: few lanes have more than one
         const int at = __ffs(near) - 1;
@@ -177,7 +182,7 @@ __global__ void __launch_bounds__(kThreads, 3) kv_append_kernel(KvView c, RowSou
             }
         }
         constexpr int kHeads = kRowsAtOnce / 2, kRounds = kBatch / kHeads;   // heads at once, rounds of a batch
-        const T* p = static_cast<const T*>(src.p[which]) + i * src.token[which] + (h0 + (sub >> 1)) * stride + in_row * 8;
+        const T* p = static_cast<const T*>(src.p[which]) + i * src.token[which] + min(h0 + (sub >> 1), h1 - 1) * stride + in_row * 8;
         uint8_t* g = k.g + (h0 + (sub >> 1)) * static_cast<int64_t>(head_bytes);
         uint8_t* const code_at = g + kv_code_at(D, which, k.t) + in_row * 4;
         uint8_t* const prm_at = g + kv_param_at(D, which, k.t);
@@ -186,15 +191,15 @@ __global__ void __launch_bounds__(kThreads, 3) kv_append_kernel(KvView c, RowSou
             Eight<T, VEC> raw[kRounds];
 #pragma unroll
             for (int u = 0; u < kRounds; ++u) {
-                if (h + u * kHeads < h1) raw[u].load(p);
-                p += kHeads * stride;
+                raw[u].load(p);
+                if (h + (u + 1) * kHeads < h1) p += kHeads * stride;   // past the last head: that one again
             }
 #pragma unroll
             for (int u = 0; u < kRounds; ++u) {   // all lanes go along; rows past the last head are not written
                 const bool real = h + u * kHeads < h1;
                 float x[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = real ? raw[u].get(j) : 0.0f;
+                for (int j = 0; j < 8; ++j) x[j] = raw[u].get(j);
                 float lo = x[0], hi = x[0], odd = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
