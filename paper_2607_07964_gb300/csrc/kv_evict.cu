@@ -27,7 +27,7 @@ constexpr int kKeys = 48 * 1024;               // keys that a CTA holds; beyond 
 constexpr int kMoves = 4;                      // moves of a warp in flight
 
 // Order-preserving key of a slot: protected above every weight, NaN below.
-__device__ __forceinline__ uint32_t evict_key(float w, int64_t pos, int64_t from, int64_t sink) {
+__device__ __forceinline__ uint32_t evict_key(float w, int32_t pos, int32_t from, int32_t sink) {
     if (pos >= from || pos < sink) return 0xFFFFFFFFu;
     if (isnan(w)) return 0u;
     const uint32_t u = __float_as_uint(w == 0.0f ? 0.0f : w);
@@ -67,71 +67,96 @@ struct Evict {
     const int32_t *lens, *seen;
     const float* acc;
     const int32_t* pos;
-    int64_t S, budget, recent, sink;
+    int64_t S;
+    int32_t budget, recent, sink;
     int32_t* lens_out;
     float* acc_out;
     int32_t *pos_out, *lists;
     int* info;
-    int32_t per;     // slots of a CTA, a multiple of kThreads
+    int32_t ctas, per;   // CTAs of a head, slots of each: a multiple of kThreads
 };
 
+// ONE: a head has one CTA, and nothing to exchange. FITS: a CTA's keys fit its shared memory.
+template <bool ONE, bool FITS>
 __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const Evict e) {
     extern __shared__ uint32_t keys[];
     __shared__ uint32_t hist[256], sum[256], picked[2], counts[3];
     __shared__ uint64_t tmp[kWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const uint32_t rank = cluster_ctarank();
-    uint32_t ctas;
-    asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(ctas));
-    const int64_t head = blockIdx.x / ctas;
-    const int b = static_cast<int>(head / e.c.kv_heads), h = static_cast<int>(head % e.c.kv_heads);
-    const int64_t n = kv_length(e.lens, b, min(kv_capacity(e.c), e.S), e.info);
-    const int64_t budget = e.budget;
-    if (h == 0 && rank == 0 && tid == 0) e.lens_out[b] = static_cast<int32_t>(min(n, budget));
+    const int rank = ONE ? 0 : static_cast<int>(cluster_ctarank()), ctas = ONE ? 1 : e.ctas;
+    auto sync = [] {
+        if constexpr (ONE) __syncthreads();
+        else cluster_barrier();
+    };
+    auto count_of = [&](int i, int r) { return ONE ? counts[i] : remote_u32(&counts[i], r); };
+    const int head = blockIdx.x / ctas;
+    const int b = head / e.c.kv_heads, h = head % e.c.kv_heads;
+    const int n = static_cast<int>(kv_length(e.lens, b, min(kv_capacity(e.c), e.S), e.info));
+    const int budget = e.budget;
+    if (h == 0 && rank == 0 && tid == 0) e.lens_out[b] = min(n, budget);
     const float* acc = e.acc + head * e.S;
     const int32_t* pos = e.pos + head * e.S;
     float* acc_out = e.acc_out + head * e.S;
     int32_t* pos_out = e.pos_out + head * e.S;
-    const int64_t first = static_cast<int64_t>(rank) * e.per;
-    const int64_t mine = max(static_cast<int64_t>(0), min(static_cast<int64_t>(e.per), n - first));
-    const int64_t kept = min(n, budget);
-    if (n <= budget) {   // the whole cluster leaves
-        for (int64_t j = first + tid; j < first + mine; j += kThreads) {
-            if (acc_out != acc) acc_out[j] = acc[j];
-            if (pos_out != pos) pos_out[j] = pos[j];
+    const int first = rank * e.per, mine = max(0, min(e.per, n - first));   // first < 2^31: no further than S and a part
+    // the front's weights and positions, holes among them, where the arrays differ
+    auto copy_front = [&] {
+        const int end = min(mine, max(0, min(n, budget) - first));
+        for (int j = tid; j < end; j += kThreads) {
+            if (acc_out != acc) acc_out[first + j] = acc[first + j];
+            if (pos_out != pos) pos_out[first + j] = pos[first + j];
         }
+    };
+    if (n <= budget) {   // the whole cluster leaves
+        copy_front();
         return;
     }
-    const int64_t from = static_cast<int64_t>(e.seen[b]) - e.recent;
-    for (int64_t j = tid; j < min(mine, static_cast<int64_t>(kKeys)); j += kThreads)
-        keys[j] = evict_key(acc[first + j], pos[first + j], from, e.sink);
-    auto key = [&](int64_t j) { return j < kKeys ? keys[j] : evict_key(acc[first + j], pos[first + j], from, e.sink); };
+    const int from = static_cast<int>(max(static_cast<int64_t>(INT32_MIN), static_cast<int64_t>(e.seen[b]) - e.recent));
+    auto made = [&](int j) { return evict_key(acc[first + j], pos[first + j], from, e.sink); };
+    {
+        const int held = FITS ? mine : min(mine, kKeys);
+        int j = tid;
+        for (; j + 3 * kThreads < held; j += 4 * kThreads) {
+            float w[4];
+            int32_t q[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = acc[first + j + i * kThreads], q[i] = pos[first + j + i * kThreads];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) keys[j + i * kThreads] = evict_key(w[i], q[i], from, e.sink);
+        }
+        for (; j < held; j += kThreads) keys[j] = made(j);
+    }
+    auto key = [&](int j) { return FITS || j < kKeys ? keys[j] : made(j); };
 
     // ---- the budget-th largest key: 8 bits at a time, from the top
-    uint32_t prefix = 0;
-    int64_t want = budget;   // how many of the keys that share the prefix stay
+    uint32_t prefix = 0, want = budget;   // want: how many of the keys that share the prefix stay
+#pragma unroll
     for (int shift = 24; shift >= 0; shift -= 8) {
         if (tid < 256) hist[tid] = 0;
         __syncthreads();
-        for (int64_t j0 = 0; j0 < mine; j0 += kThreads) {
-            const int64_t j = j0 + tid;
+        for (int j0 = 0; j0 < mine; j0 += kThreads) {
+            const int j = j0 + tid;
             const uint32_t k = j < mine ? key(j) : 0;
-            const bool in = j < mine && (shift == 24 || k >> (shift + 8) == prefix >> (shift + 8));
+            const bool in = j < mine && (shift == 24 || k >> (shift + 8 & 31) == prefix >> (shift + 8 & 31));
             // keys of a warp often share their upper bits: one count for all of them
             const uint32_t bin = in ? k >> shift & 255u : 256u, same = __match_any_sync(0xffffffffu, bin);
             if (in && (same & ((1u << lane) - 1)) == 0) atomicAdd(&hist[bin], __popc(same));
         }
-        cluster_barrier();
-        if (tid < 256) {
-            uint32_t s = 0;
-            for (uint32_t r = 0; r < ctas; ++r) s += remote_u32(&hist[tid], r);
-            sum[tid] = s;
+        sync();
+        if constexpr (!ONE) {
+            if (tid < 256) {
+                uint32_t s = 0;
+#pragma unroll
+                for (int r = 0; r < kCluster; ++r)
+                    if (r < ctas) s += remote_u32(&hist[tid], r);
+                sum[tid] = s;
+            }
+            __syncthreads();
         }
-        __syncthreads();
         if (warp == 0) {   // from the largest bin: the one in which the want-th key falls
             uint32_t v[8], s = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s += v[i] = sum[255 - (lane * 8 + i)];
+            for (int i = 0; i < 8; ++i) s += v[i] = (ONE ? hist : sum)[255 - (lane * 8 + i)];
             uint32_t x = s;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -141,74 +166,72 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const Evict e) {
             uint32_t before = x - s;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                if (before < want && want <= before + static_cast<int64_t>(v[i])) {
+                if (before < want && want <= before + v[i]) {
                     picked[0] = 255 - (lane * 8 + i);
                     picked[1] = before;
                 }
                 before += v[i];
             }
         }
-        cluster_barrier();   // hist is read by the others until here, picked written
+        sync();   // hist is read by the others until here, picked written
         prefix |= picked[0] << shift;
         want -= picked[1];
     }
     const uint32_t t = prefix;   // want: how many slots equal to it stay, the lowest
 
     // ---- ties before this CTA, then kept or not, slot by slot: a run of them to a thread
-    const int64_t run = (mine + kThreads - 1) / kThreads, j0 = min(tid * run, mine), j1 = min(j0 + run, mine);
+    const int run = (mine + kThreads - 1) / kThreads | 1;   // odd: neighbouring threads in different banks
+    const int j0 = min(tid * run, mine), j1 = min(j0 + run, mine);
     uint32_t eq = 0;
-    for (int64_t j = j0; j < j1; ++j) eq += key(j) == t;
+    for (int j = j0; j < j1; ++j) eq += key(j) == t;
     uint64_t total;
-    uint64_t ties = block_scan(eq, tmp, total);
-    if (tid == 0) counts[0] = static_cast<uint32_t>(total);
-    cluster_barrier();
-    for (uint32_t r = 0; r < rank; ++r) ties += remote_u32(&counts[0], r);
-    uint64_t both = 0;   // holes, and kept slots past the budget in the upper half
-    uint64_t tie = ties;
-    for (int64_t j = j0; j < j1; ++j) {
+    uint32_t ties = static_cast<uint32_t>(block_scan(eq, tmp, total));
+    if constexpr (!ONE) {
+        if (tid == 0) counts[0] = static_cast<uint32_t>(total);
+        sync();
+        for (int r = 0; r < rank; ++r) ties += count_of(0, r);
+    }
+    uint32_t holes_here = 0, tails_here = 0, tie = ties;
+    const int edge = budget - first;   // this CTA's slots below the budget
+    for (int j = j0; j < j1; ++j) {
         const uint32_t k = key(j);
-        const bool keep = k > t || (k == t && static_cast<int64_t>(tie++) < want);
-        if (first + j < budget) both += !keep;
-        else both += static_cast<uint64_t>(keep) << 32;
+        const bool keep = k > t || (k == t && tie++ < want);
+        holes_here += j < edge && !keep;
+        tails_here += j >= edge && keep;
     }
-    uint64_t at = block_scan(both, tmp, total);
-    if (tid == 0) {
-        counts[1] = static_cast<uint32_t>(total);
-        counts[2] = static_cast<uint32_t>(total >> 32);
-    }
-    cluster_barrier();
-    uint32_t hole_at = static_cast<uint32_t>(at), tail_at = static_cast<uint32_t>(at >> 32), holes = 0;
-    for (uint32_t r = 0; r < ctas; ++r) {
-        const uint32_t x = remote_u32(&counts[1], r);
-        if (r < rank) {
-            hole_at += x;
-            tail_at += remote_u32(&counts[2], r);
+    const uint64_t at = block_scan(holes_here | static_cast<uint64_t>(tails_here) << 32, tmp, total);
+    uint32_t hole_at = static_cast<uint32_t>(at), tail_at = static_cast<uint32_t>(at >> 32), holes = static_cast<uint32_t>(total);
+    if constexpr (!ONE) {
+        if (tid == 0) {
+            counts[1] = static_cast<uint32_t>(total);
+            counts[2] = static_cast<uint32_t>(total >> 32);
         }
-        holes += x;
+        sync();
+        holes = 0;
+        for (int r = 0; r < ctas; ++r) {
+            const uint32_t x = count_of(1, r);
+            if (r < rank) {
+                hole_at += x;
+                tail_at += count_of(2, r);
+            }
+            holes += x;
+        }
     }
-    int32_t* hole = e.lists + head * 2 * budget;
+    int32_t* hole = e.lists + static_cast<int64_t>(head) * 2 * budget;
     int32_t* tail = hole + budget;
     tie = ties;
-    for (int64_t j = j0; j < j1; ++j) {
+    for (int j = j0; j < j1; ++j) {
         const uint32_t k = key(j);
-        const bool keep = k > t || (k == t && static_cast<int64_t>(tie++) < want);
-        if (first + j < budget) {
-            if (!keep) hole[hole_at++] = static_cast<int32_t>(first + j);
-        } else if (keep) {
-            tail[tail_at++] = static_cast<int32_t>(first + j);
-        }
+        const bool keep = k > t || (k == t && tie++ < want);
+        if (j < edge && !keep) hole[hole_at++] = first + j;
+        if (j >= edge && keep) tail[tail_at++] = first + j;
     }
-    __threadfence();
-    cluster_barrier();   // the lists are complete, and no counts are read any more
+    copy_front();
+    sync();   // the lists and the fronts are complete, and no counts are read any more
 
-    // ---- weights and positions of the front, holes left out where the arrays differ; then the moves
-    for (int64_t j = first + tid; j < min(first + mine, kept); j += kThreads) {
-        if (acc_out != acc) acc_out[j] = acc[j];
-        if (pos_out != pos) pos_out[j] = pos[j];
-    }
-    cluster_barrier();
+    // ---- the moves
     const int words = e.c.dim / 8;   // of a row of codes
-    for (int64_t m0 = static_cast<int64_t>(warp * ctas + rank) * kMoves; m0 < holes; m0 += static_cast<int64_t>(kWarps) * ctas * kMoves) {
+    for (uint32_t m0 = (warp * ctas + rank) * kMoves; m0 < holes; m0 += kWarps * ctas * kMoves) {
         uint8_t* dst[kMoves];
         uint32_t code[kMoves], prm[kMoves], extra[kMoves];
         int32_t to[kMoves], td[kMoves];
@@ -268,11 +291,13 @@ extern "C" kq_status kq_kv_evict(const kq_kv_cache* cache, const int32_t* lens, 
     KvView c;
     KQ_TRY(kv_view(cache, "kq_kv_evict", &c));
     if (!lens || !acc || !pos || !seen || !lens_out || !acc_out || !pos_out || lens_out == lens || S < 1 ||
-        S > 0x7fffffffll || budget < 1 || recent < 0 || sink < 0 || recent > budget || sink > budget - recent) {
+        S > 0x7fffffffll - (1 << 20) || budget < 1 || recent < 0 || sink < 0 || recent > budget || sink > budget - recent) {
         set_error("kq_kv_evict: arrays must not be NULL, lens_out apart from lens, budget >= 1, recent + sink <= budget");
         return KQ_ERR_INVALID_ARG;
     }
     budget = std::min(budget, S);
+    recent = std::min<int64_t>(recent, 0x7fffffff);
+    sink = std::min<int64_t>(sink, 0x7fffffff);
     const size_t need = kq_kv_evict_workspace(c.batch, c.kv_heads, S, budget);
     if (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 255u)) {
         set_error("kq_kv_evict: workspace must be 256-byte aligned and hold %zu bytes", need);
@@ -280,8 +305,11 @@ extern "C" kq_status kq_kv_evict(const kq_kv_cache* cache, const int32_t* lens, 
     }
     static std::atomic<uint64_t> done{0};
     KQ_TRY(once_per_device(done, [] {
-        KQ_CUDA(cudaFuncSetAttribute(kv_evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                     static_cast<int>(kKeys * sizeof(uint32_t))));
+        const int most_smem = static_cast<int>(kKeys * sizeof(uint32_t));
+        KQ_CUDA(cudaFuncSetAttribute(kv_evict_kernel<true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most_smem));
+        KQ_CUDA(cudaFuncSetAttribute(kv_evict_kernel<true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most_smem));
+        KQ_CUDA(cudaFuncSetAttribute(kv_evict_kernel<false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most_smem));
+        KQ_CUDA(cudaFuncSetAttribute(kv_evict_kernel<false, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most_smem));
         return KQ_OK;
     }));
     // CTAs of a head: one up to 4096 slots, where the exchanges between CTAs would cost more than
@@ -289,7 +317,8 @@ extern "C" kq_status kq_kv_evict(const kq_kv_cache* cache, const int32_t* lens, 
     const int64_t most = std::min(S, kv_capacity(c));
     int ctas = 1;
     while (ctas < kCluster && most > 4096 && most > 2048 * ctas && c.batch * c.kv_heads * ctas < 2 * num_sms()) ctas *= 2;
-    const Evict e = {c, lens, seen, acc, pos, S, budget, recent, sink, lens_out, acc_out, pos_out, static_cast<int32_t*>(ws), info,
+    const Evict e = {c, lens, seen, acc, pos, S, static_cast<int32_t>(budget), static_cast<int32_t>(recent), static_cast<int32_t>(sink),
+                     lens_out, acc_out, pos_out, static_cast<int32_t*>(ws), info, ctas,
                      static_cast<int32_t>(cdiv(cdiv(most, ctas), kThreads) * kThreads)};
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(c.batch * c.kv_heads * ctas));
@@ -301,7 +330,9 @@ extern "C" kq_status kq_kv_evict(const kq_kv_cache* cache, const int32_t* lens, 
     at[0].val.clusterDim = {static_cast<unsigned>(ctas), 1, 1};
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    KQ_CUDA(cudaLaunchKernelEx(&cfg, kv_evict_kernel, e));
+    const bool fits = e.per <= kKeys;
+    KQ_CUDA(ctas == 1 ? (fits ? cudaLaunchKernelEx(&cfg, kv_evict_kernel<true, true>, e) : cudaLaunchKernelEx(&cfg, kv_evict_kernel<true, false>, e))
+                      : (fits ? cudaLaunchKernelEx(&cfg, kv_evict_kernel<false, true>, e) : cudaLaunchKernelEx(&cfg, kv_evict_kernel<false, false>, e)));
     KQ_LAUNCH_CHECK("kv_evict_kernel");
     return KQ_OK;
 }
