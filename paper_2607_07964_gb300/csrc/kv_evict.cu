@@ -24,7 +24,7 @@ constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
 constexpr int kCluster = 8;                    // CTAs of a head, at most
 constexpr int kKeys = 48 * 1024;               // keys that a CTA holds; beyond them they are made again from memory
-constexpr int kMoves = 4;                      // moves of a warp in flight
+constexpr int kMoves = 8;                      // moves of a warp in flight
 
 // Order-preserving key of a slot: protected above every weight, NaN below.
 __device__ __forceinline__ uint32_t evict_key(float w, int32_t pos, int32_t from, int32_t sink) {
@@ -229,44 +229,51 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const Evict e) {
     copy_front();
     sync();   // the lists and the fronts are complete, and no counts are read any more
 
-    // ---- the moves
-    const int words = e.c.dim / 8;   // of a row of codes
-    for (uint32_t m0 = (warp * ctas + rank) * kMoves; m0 < holes; m0 += kWarps * ctas * kMoves) {
-        uint8_t* dst[kMoves];
-        uint32_t code[kMoves], prm[kMoves], extra[kMoves];
-        int32_t to[kMoves], td[kMoves];
+    // ---- the moves: a lane finds both places of one and takes its parameters, weight and position; then the warp
+    // copies the code rows of one after the other
+    const int words = e.c.dim / 8, row = e.c.dim / 2;   // words and bytes of a row of codes
+    // lanes 0 .. words - 1 the key's codes, the next as many the value's
+    const int in_row = (lane >= words ? kGranule * row + (lane - words) * 4 : lane * 4);
+    const bool copies = lane < 2 * words;
+    const uint32_t chunk = min(32u, max(4u, (holes + kWarps * ctas - 1) / (kWarps * ctas)));
+    for (uint32_t m0 = (warp * ctas + rank) * chunk; m0 < holes; m0 += kWarps * ctas * chunk) {
+        const uint32_t here = min(chunk, holes - m0);
+        const uint8_t* src = nullptr;
+        uint8_t* dst = nullptr;
+        if (lane < here) {
+            const int to = hole[m0 + lane], at = tail[m0 + lane];
+            src = kv_granule(e.c, b, h, at);
+            dst = kv_granule(e.c, b, h, to);
+            if (src && dst) {
+                const int ts = at % kGranule, td = to % kGranule;
+                const float w = acc[at];
+                const int32_t q = pos[at];
+                uint32_t prm[2];
 #pragma unroll
-        for (int i = 0; i < kMoves; ++i) {
-            dst[i] = nullptr;
-            if (m0 + i >= holes) continue;
-            to[i] = hole[m0 + i];
-            const int32_t src_slot = tail[m0 + i];
-            const uint8_t* src = kv_granule(e.c, b, h, src_slot);
-            dst[i] = kv_granule(e.c, b, h, to[i]);
-            if (!src || !dst[i]) {
+                for (int i = 0; i < 2; ++i) prm[i] = *reinterpret_cast<const uint32_t*>(src + kv_param_at(e.c.dim, i, ts));
+#pragma unroll
+                for (int i = 0; i < 2; ++i) *reinterpret_cast<uint32_t*>(dst + kv_param_at(e.c.dim, i, td)) = prm[i];
+                acc_out[to] = w;
+                pos_out[to] = q;
+                src += ts * row;
+                dst += td * row;
+            } else {
                 record_error(e.info, -KQ_ERR_INVALID_ARG);
-                dst[i] = nullptr;
-                continue;
-            }
-            const int ts = src_slot % kGranule;
-            td[i] = to[i] % kGranule;
-            // lanes 0 .. words - 1 the key's codes, the next as many the value's
-            if (lane < 2 * words)
-                code[i] = reinterpret_cast<const uint32_t*>(src + kv_code_at(e.c.dim, lane >= words, ts))[lane % words];
-            if (lane < 2) {
-                prm[i] = *reinterpret_cast<const uint32_t*>(src + kv_param_at(e.c.dim, lane, ts));
-                extra[i] = lane ? static_cast<uint32_t>(pos[src_slot]) : __float_as_uint(acc[src_slot]);
+                dst = nullptr;
             }
         }
+        for (uint32_t k0 = 0; k0 < here; k0 += kMoves) {
+            uint32_t code[kMoves];
 #pragma unroll
-        for (int i = 0; i < kMoves; ++i) {
-            if (!dst[i]) continue;
-            if (lane < 2 * words)
-                reinterpret_cast<uint32_t*>(dst[i] + kv_code_at(e.c.dim, lane >= words, td[i]))[lane % words] = code[i];
-            if (lane < 2) {
-                *reinterpret_cast<uint32_t*>(dst[i] + kv_param_at(e.c.dim, lane, td[i])) = prm[i];
-                if (lane) pos_out[to[i]] = static_cast<int32_t>(extra[i]);
-                else acc_out[to[i]] = __uint_as_float(extra[i]);
+            for (int i = 0; i < kMoves; ++i) {
+                const uint64_t s = __shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(src), k0 + i & 31);
+                const uint64_t d = __shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(dst), k0 + i & 31);
+                if (k0 + i < here && d && copies) code[i] = *reinterpret_cast<const uint32_t*>(s + in_row);
+            }
+#pragma unroll
+            for (int i = 0; i < kMoves; ++i) {
+                const uint64_t d = __shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(dst), k0 + i & 31);
+                if (k0 + i < here && d && copies) *reinterpret_cast<uint32_t*>(d + in_row) = code[i];
             }
         }
     }
