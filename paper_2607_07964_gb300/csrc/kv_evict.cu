@@ -24,7 +24,7 @@ constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
 constexpr int kCluster = 8;                    // CTAs of a head, at most
 constexpr int kKeys = 48 * 1024;               // keys that a CTA holds; beyond them they are made again from memory
-constexpr int kMoves = 8;                      // moves of a warp in flight
+constexpr int kMoves = 16;                     // moves of a warp in flight
 
 // Order-preserving key of a slot: protected above every weight, NaN below.
 __device__ __forceinline__ uint32_t evict_key(float w, int32_t pos, int32_t from, int32_t sink) {
@@ -138,9 +138,22 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const Evict e) {
             const int j = j0 + tid;
             const uint32_t k = j < mine ? key(j) : 0;
             const bool in = j < mine && (shift == 24 || k >> (shift + 8 & 31) == prefix >> (shift + 8 & 31));
-            // keys of a warp often share their upper bits: one count for all of them
-            const uint32_t bin = in ? k >> shift & 255u : 256u, same = __match_any_sync(0xffffffffu, bin);
-            if (in && (same & ((1u << lane) - 1)) == 0) atomicAdd(&hist[bin], __popc(same));
+            const uint32_t bin = k >> shift & 255u;
+            bool left = in;
+            if (shift == 24) {   // weights share a few exponents: one count for all lanes of a bin, three bins a warp
+#pragma unroll
+                for (int i = 0; i < 3; ++i) {
+                    const uint32_t rest = __ballot_sync(0xffffffffu, left);
+                    if (rest == 0) break;
+                    const int lead = __ffs(rest) - 1;
+                    const uint32_t theirs = __shfl_sync(0xffffffffu, bin, lead);   // by all lanes, counted or not
+                    const bool same = left && bin == theirs;
+                    const uint32_t who = __ballot_sync(0xffffffffu, same);
+                    if (lane == lead) atomicAdd(&hist[bin], __popc(who));
+                    left = left && !same;
+                }
+            }
+            if (left) atomicAdd(&hist[bin], 1u);
         }
         sync();
         if constexpr (!ONE) {
@@ -323,7 +336,7 @@ extern "C" kq_status kq_kv_evict(const kq_kv_cache* cache, const int32_t* lens, 
     // they save, or where the heads fill the GPU; else as many as keep 2048 slots each, up to a cluster.
     const int64_t most = std::min(S, kv_capacity(c));
     int ctas = 1;
-    while (ctas < kCluster && most > 4096 && most > 2048 * ctas && c.batch * c.kv_heads * ctas < 2 * num_sms()) ctas *= 2;
+    while (ctas < kCluster && most > 4096 && most > 2048 * ctas && c.batch * c.kv_heads * ctas <= num_sms()) ctas *= 2;
     const Evict e = {c, lens, seen, acc, pos, S, static_cast<int32_t>(budget), static_cast<int32_t>(recent), static_cast<int32_t>(sink),
                      lens_out, acc_out, pos_out, static_cast<int32_t*>(ws), info, ctas,
                      static_cast<int32_t>(cdiv(cdiv(most, ctas), kThreads) * kThreads)};
