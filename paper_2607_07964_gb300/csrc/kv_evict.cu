@@ -1,8 +1,8 @@
 // kq_kv_evict: the slots of a sequence and head that stay, and the moves that bring them to the front.
 //
 // Selection: a slot's key is its weight as an order-preserving whole number, above all of them for
-// a protected slot. The budget-th largest key is found by four counts over 8 bits each; slots above
-// it stay, and of those equal to it the lowest. A kept slot at or beyond the budget moves into a
+// a protected slot. The budget-th largest key is found by up to four counts over 8 bits each; slots
+// above it stay, and of those equal to it the lowest. A kept slot at or beyond the budget moves into a
 // free one below it, i-th to i-th, so the two sides never overlap, nothing is copied that already has
 // its place, and cutting 64 of 4160 slots moves 64 rows, not 4096.
 //
@@ -80,7 +80,7 @@ struct Evict {
 template <bool ONE, bool FITS>
 __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const Evict e) {
     extern __shared__ uint32_t keys[];
-    __shared__ uint32_t hist[256], sum[256], picked[2], counts[3];
+    __shared__ uint32_t hist[4][256], sum[256], picked[2], counts[6];   // a count for each digit: none is cleared while read
     __shared__ uint64_t tmp[kWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = ONE ? 0 : static_cast<int>(cluster_ctarank()), ctas = ONE ? 1 : e.ctas;
@@ -113,6 +113,15 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const Evict e) {
     }
     const int from = static_cast<int>(max(static_cast<int64_t>(INT32_MIN), static_cast<int64_t>(e.seen[b]) - e.recent));
     auto made = [&](int j) { return evict_key(acc[first + j], pos[first + j], from, e.sink); };
+    for (int i = tid; i < 4 * 256; i += kThreads) hist[0][i] = 0;
+    if (tid == 0) counts[3] = 0xFFFFFFFFu, counts[4] = counts[5] = 0;
+    __syncthreads();
+    uint32_t low = 0xFFFFFFFFu, high = 0, safe = 0;   // of the keys that are not protected; how many are
+    auto note = [&](uint32_t k) {
+        safe += k == 0xFFFFFFFFu;
+        low = min(low, k);
+        if (k != 0xFFFFFFFFu) high = max(high, k);
+    };
     {
         const int held = FITS ? mine : min(mine, kKeys);
         int j = tid;
@@ -122,38 +131,47 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const Evict e) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) w[i] = acc[first + j + i * kThreads], q[i] = pos[first + j + i * kThreads];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) keys[j + i * kThreads] = evict_key(w[i], q[i], from, e.sink);
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t k = evict_key(w[i], q[i], from, e.sink);
+                keys[j + i * kThreads] = k;
+                note(k);
+            }
         }
-        for (; j < held; j += kThreads) keys[j] = made(j);
+        for (; j < held; j += kThreads) note(keys[j] = made(j));
+        if constexpr (!FITS)
+            for (; j < mine; j += kThreads) note(made(j));
+    }
+    low = __reduce_min_sync(0xffffffffu, low);
+    high = __reduce_max_sync(0xffffffffu, high);
+    safe = __reduce_add_sync(0xffffffffu, safe);
+    if (lane == 0) {
+        atomicMin(&counts[3], low);
+        atomicMax(&counts[4], high);
+        atomicAdd(&counts[5], safe);
+    }
+    sync();
+    low = 0xFFFFFFFFu, high = 0, safe = 0;
+    for (int r = 0; r < ctas; ++r) {
+        low = min(low, count_of(3, r));
+        high = max(high, count_of(4, r));
+        safe += count_of(5, r);
     }
     auto key = [&](int j) { return FITS || j < kKeys ? keys[j] : made(j); };
 
-    // ---- the budget-th largest key: 8 bits at a time, from the top
-    uint32_t prefix = 0, want = budget;   // want: how many of the keys that share the prefix stay
-#pragma unroll
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        if (tid < 256) hist[tid] = 0;
-        __syncthreads();
-        for (int j0 = 0; j0 < mine; j0 += kThreads) {
-            const int j = j0 + tid;
-            const uint32_t k = j < mine ? key(j) : 0;
-            const bool in = j < mine && (shift == 24 || k >> (shift + 8 & 31) == prefix >> (shift + 8 & 31));
-            const uint32_t bin = k >> shift & 255u;
-            bool left = in;
-            if (shift == 24) {   // weights share a few exponents: one count for all lanes of a bin, three bins a warp
-#pragma unroll
-                for (int i = 0; i < 3; ++i) {
-                    const uint32_t rest = __ballot_sync(0xffffffffu, left);
-                    if (rest == 0) break;
-                    const int lead = __ffs(rest) - 1;
-                    const uint32_t theirs = __shfl_sync(0xffffffffu, bin, lead);   // by all lanes, counted or not
-                    const bool same = left && bin == theirs;
-                    const uint32_t who = __ballot_sync(0xffffffffu, same);
-                    if (lane == lead) atomicAdd(&hist[bin], __popc(who));
-                    left = left && !same;
-                }
-            }
-            if (left) atomicAdd(&hist[bin], 1u);
+    // ---- the budget-th largest key: among the others once the protected slots have their places, by their distance
+    // from the smallest, 8 bits at a time from the first that any has (weights share a few exponents; their
+    // distances spread over the bins)
+    const bool crowd = safe >= static_cast<uint32_t>(budget);   // the protected alone fill the budget, the lowest first
+    uint32_t prefix = 0, want = crowd ? budget : budget - safe;   // want: how many of the keys that share the prefix stay
+    const int bits = crowd ? 0 : 32 - __clz(high - low);
+    for (int digit = 0, shift = bits - 8; shift > -8; ++digit, shift -= 8) {
+        uint32_t* const bins = hist[digit];
+        const int down = max(shift, 0), above = shift + 8;   // the last digit may have fewer than 8 bits
+        for (int j = tid; j < mine; j += kThreads) {
+            const uint32_t k = key(j) - low;
+            if (k > high - low) continue;   // protected
+            if (above < 32 && (k ^ prefix) >> above) continue;
+            atomicAdd(&bins[(k & (above < 32 ? (1u << above) - 1 : 0xFFFFFFFFu)) >> down], 1u);
         }
         sync();
         if constexpr (!ONE) {
@@ -161,7 +179,7 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const Evict e) {
                 uint32_t s = 0;
 #pragma unroll
                 for (int r = 0; r < kCluster; ++r)
-                    if (r < ctas) s += remote_u32(&hist[tid], r);
+                    if (r < ctas) s += remote_u32(&bins[tid], r);
                 sum[tid] = s;
             }
             __syncthreads();
@@ -169,7 +187,7 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const Evict e) {
         if (warp == 0) {   // from the largest bin: the one in which the want-th key falls
             uint32_t v[8], s = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s += v[i] = (ONE ? hist : sum)[255 - (lane * 8 + i)];
+            for (int i = 0; i < 8; ++i) s += v[i] = (ONE ? bins : sum)[255 - (lane * 8 + i)];
             uint32_t x = s;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -186,11 +204,11 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const Evict e) {
                 before += v[i];
             }
         }
-        sync();   // hist is read by the others until here, picked written
-        prefix |= picked[0] << shift;
+        __syncthreads();   // picked by each CTA for itself
+        prefix |= picked[0] << down;
         want -= picked[1];
     }
-    const uint32_t t = prefix;   // want: how many slots equal to it stay, the lowest
+    const uint32_t t = crowd ? 0xFFFFFFFFu : low + prefix;   // want: how many slots equal to it stay, the lowest
 
     // ---- ties before this CTA, then kept or not, slot by slot: a run of them to a thread
     const int run = (mine + kThreads - 1) / kThreads | 1;   // odd: neighbouring threads in different banks
