@@ -865,22 +865,54 @@ __global__ void __launch_bounds__(256) kv_combine_kernel(const Attend p) {
     }
 }
 
-// acc += the weights of the slots: a thread a slot, the rows of its sequence and head in order.
+// acc += the weights of the slots: a thread takes kSlots of them, the rows of their sequence and head in
+// order. Bound by the scores' bytes, 4 a row, so what counts is loads in flight: those of all the
+// slots, four rows at a time where the group allows it.
+template <bool QUADS>
 __global__ void __launch_bounds__(256) kv_weight_kernel(const Attend p, float* __restrict__ acc) {
+    constexpr int kSlots = 4;
     pdl_wait();
     const int b = blockIdx.x / p.c.kv_heads, h = blockIdx.x % p.c.kv_heads;
     const Seq s = sequence<8>(p, b, nullptr);
     if (s.nq == 0) return;
-    for (int slot = blockIdx.y * 256 + threadIdx.x; slot < s.n; slot += gridDim.y * 256) {
-        float sum = 0.0f;
-        for (int i = 0; i < s.nq; ++i) {
-            if (slot >= visible(s.n, s.nq, i)) continue;
-            const int64_t tk = s.first + i;
-            const float* sc = p.scores + ((tk * p.c.kv_heads + h) * p.S + slot) * p.group;
-            const float* ls = p.lse + tk * p.q_heads + h * p.group;
-            for (int g = 0; g < p.group; ++g) sum += ex2(sc[g] - ls[g] * kLog2e);
+    acc += (static_cast<int64_t>(b) * p.c.kv_heads + h) * p.S;
+    for (int64_t s0 = static_cast<int64_t>(blockIdx.y) * (256 * kSlots) + threadIdx.x; s0 - threadIdx.x < s.n;
+         s0 += static_cast<int64_t>(gridDim.y) * (256 * kSlots)) {
+        float sum[kSlots], old[kSlots];
+#pragma unroll
+        for (int u = 0; u < kSlots; ++u) {
+            sum[u] = 0.0f;
+            if (s0 + u * 256 < s.n) old[u] = acc[s0 + u * 256];
         }
-        acc[(static_cast<int64_t>(b) * p.c.kv_heads + h) * p.S + slot] += sum;
+        for (int i = 0; i < s.nq; ++i) {
+            const int64_t tk = s.first + i;
+            const int end = visible(s.n, s.nq, i);
+            const float* sc = p.scores + ((tk * p.c.kv_heads + h) * p.S + s0) * p.group;
+            const float* ls = p.lse + tk * p.q_heads + h * p.group;
+            if constexpr (QUADS) {
+                for (int g = 0; g < p.group; g += 4) {
+                    float4 x[kSlots];
+#pragma unroll
+                    for (int u = 0; u < kSlots; ++u)
+                        if (s0 + u * 256 < end) x[u] = __ldcs(reinterpret_cast<const float4*>(sc + static_cast<int64_t>(u) * 256 * p.group + g));
+                    const float l0 = ls[g] * kLog2e, l1 = ls[g + 1] * kLog2e, l2 = ls[g + 2] * kLog2e, l3 = ls[g + 3] * kLog2e;
+#pragma unroll
+                    for (int u = 0; u < kSlots; ++u)
+                        if (s0 + u * 256 < end)
+                            sum[u] += ex2(x[u].x - l0) + ex2(x[u].y - l1) + (ex2(x[u].z - l2) + ex2(x[u].w - l3));
+                }
+            } else {
+                for (int g = 0; g < p.group; ++g) {
+                    const float l0 = ls[g] * kLog2e;
+#pragma unroll
+                    for (int u = 0; u < kSlots; ++u)
+                        if (s0 + u * 256 < end) sum[u] += ex2(__ldcs(sc + static_cast<int64_t>(u) * 256 * p.group + g) - l0);
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kSlots; ++u)
+            if (s0 + u * 256 < s.n) acc[s0 + u * 256] = old[u] + sum[u];
     }
 }
 
@@ -1002,8 +1034,9 @@ extern "C" kq_status kq_kv_attend(const kq_kv_cache* cache, const void* q, int d
     KQ_TRY(st);
     if (acc) {
         const dim3 wg(static_cast<unsigned>(c.batch * c.kv_heads),
-                      static_cast<unsigned>(std::min<int64_t>(cdiv(p.cap, 256), 65535)));
-        KQ_CUDA(launch_after(kv_weight_kernel, wg, dim3(256), stream, p, acc));
+                      static_cast<unsigned>(std::min<int64_t>(cdiv(p.cap, 1024), 65535)));
+        KQ_CUDA(p.group % 4 ? launch_after(kv_weight_kernel<false>, wg, dim3(256), stream, p, acc)
+                            : launch_after(kv_weight_kernel<true>, wg, dim3(256), stream, p, acc));
         count_launch();
     }
     return KQ_OK;
