@@ -796,9 +796,9 @@ __global__ void __launch_bounds__(256) kv_combine_kernel(const Attend p) {
     __shared__ float sm[kGroups][D], sl[kGroups], sx[kGroups];
     pdl_wait();
     pdl_launch_dependents();
-    if (blockIdx.x >= *p.items) return;
-    const Joint j = p.joint[blockIdx.x];
-    if (j.last == j.first) return;
+    const int64_t items = *p.items;
+    const Joint j = p.joint[blockIdx.x];   // the array has room for every block
+    if (blockIdx.x >= items || j.last == j.first) return;
     const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5;
     const int many = j.last - j.first + 1;
     // the results after the first begin their pieces
@@ -826,16 +826,27 @@ __global__ void __launch_bounds__(256) kv_combine_kernel(const Attend p) {
                 f = ex2(q[kRows * D + col] - M);
                 L = fmaf(f, q[kRows * (D + 1) + col], L);
             }
-#pragma unroll 8
-            for (int k = 0; k < here; ++k) {
-                const float fk = __shfl_sync(0xffffffffu, f, k);
-                const float* q = result(k0 + k) + col * D + lane * kV;
-                if constexpr (kV == 4) {
-                    const float4 x = *reinterpret_cast<const float4*>(q);
-                    O[0] = fmaf(fk, x.x, O[0]), O[1] = fmaf(fk, x.y, O[1]), O[2] = fmaf(fk, x.z, O[2]), O[3] = fmaf(fk, x.w, O[3]);
-                } else {
-                    const float2 x = *reinterpret_cast<const float2*>(q);
-                    O[0] = fmaf(fk, x.x, O[0]), O[1] = fmaf(fk, x.y, O[1]);
+            constexpr int kAhead = 16;   // results in flight
+            for (int k1 = 0; k1 < here; k1 += kAhead) {
+                float x[kAhead][kV];
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) {
+                    if (k1 + k >= here) break;
+                    const float* q = result(k0 + k1 + k) + col * D + lane * kV;
+                    if constexpr (kV == 4) {
+                        const float4 y = *reinterpret_cast<const float4*>(q);
+                        x[k][0] = y.x, x[k][1] = y.y, x[k][2] = y.z, x[k][3] = y.w;
+                    } else {
+                        const float2 y = *reinterpret_cast<const float2*>(q);
+                        x[k][0] = y.x, x[k][1] = y.y;
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) {
+                    if (k1 + k >= here) break;
+                    const float fk = __shfl_sync(0xffffffffu, f, k1 + k);
+#pragma unroll
+                    for (int i = 0; i < kV; ++i) O[i] = fmaf(fk, x[k][i], O[i]);
                 }
             }
         }
@@ -1033,8 +1044,10 @@ extern "C" kq_status kq_kv_attend(const kq_kv_cache* cache, const void* q, int d
                           : (wide ? run_attend<float, 64, 2>(p, stream) : run_attend<float, 64, 1>(p, stream));
     KQ_TRY(st);
     if (acc) {
-        const dim3 wg(static_cast<unsigned>(c.batch * c.kv_heads),
-                      static_cast<unsigned>(std::min<int64_t>(cdiv(p.cap, 1024), 65535)));
+        // enough blocks for two rounds of a full GPU, each going through its slots in steps of 1024
+        const int64_t heads = static_cast<int64_t>(c.batch) * c.kv_heads;
+        const dim3 wg(static_cast<unsigned>(heads),
+                      static_cast<unsigned>(std::min<int64_t>(cdiv(p.cap, 1024), std::max<int64_t>(1, cdiv(num_sms() * 16, heads)))));
         KQ_CUDA(p.group % 4 ? launch_after(kv_weight_kernel<false>, wg, dim3(256), stream, p, acc)
                             : launch_after(kv_weight_kernel<true>, wg, dim3(256), stream, p, acc));
         count_launch();
