@@ -256,6 +256,52 @@ def test_attend_matches_64_bits(dim, page, heads, group, lens, counts, dtype, tr
     _check_attend(cache, q, counts, lens, heads, scale, dtype, out, lse, acc, acc0)
 
 
+@pytest.mark.parametrize("dim,heads,group,n,counts", [(128, 1, 8, 6000, 1), (64, 1, 3, 5011, 2), (128, 2, 12, 3100, 1)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attend_splits_few_rows_over_many_warps(dim, heads, group, n, counts, dtype):
+    """Long sequences of few heads: a row's result is joined from more parts than a warp has lanes."""
+    rng = np.random.default_rng(n)
+    cache = _pool(1, n, 64, heads, dim, rng)
+    _fill(cache, [n], heads, rng)
+    q = _rounded(rng.standard_normal((counts, heads * group, dim)) * 2, dtype)
+    acc0 = np.zeros((1, heads, n), np.float32)
+    out, lse, acc = _run_attend(cache, q.to(DEV), [counts], [n], heads, 1 / np.sqrt(dim), True, dtype, acc0, n)
+    _check_attend(cache, q, [counts], [n], heads, 1 / np.sqrt(dim), dtype, out, lse, acc, acc0)
+
+
+@pytest.mark.parametrize("batch", [129, 400])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_short_sequences(batch, dtype):
+    """More sequences than a block has threads, some without tokens and some without queries: append, read, attend."""
+    rng = np.random.default_rng(batch)
+    dim, heads, group = 64, 2, 3
+    lens = rng.integers(0, 40, batch)
+    counts = rng.integers(0, 3, batch)
+    lens = np.maximum(lens, counts)
+    lens[5] = 0
+    cache = _pool(batch, 40, 16, heads, dim, rng)
+    dc, dt = _to_dev(cache)
+    T = int(lens.sum())
+    k, v = (_rounded(rng.standard_normal((T, heads, dim)), dtype) for _ in range(2))
+    at = _starts(lens)
+    K().kq_kv_append(k.to(DEV), v.to(DEV), _i32(at), _i32(np.zeros(batch)), dc, dt)
+    for b in range(batch):
+        for j in range(lens[b]):
+            for h in range(heads):
+                cache.put(b, h, j, 0, k[at[b] + j, h].float().numpy())
+                cache.put(b, h, j, 1, v[at[b] + j, h].float().numpy())
+    assert np.array_equal(dc.cpu().numpy(), cache.data)
+    ko, vo = torch.empty(T, heads, dim, device=DEV), torch.empty(T, heads, dim, device=DEV)
+    K().kq_kv_read(dc, dt, _i32(at), None, _i32(lens), ko, vo)
+    want = np.concatenate([cache.rows(b, 1, lens[b], 1)[0] for b in range(batch)])
+    assert np.array_equal(vo[:, 1].cpu().numpy().astype(np.float64), want)
+    q = _rounded(rng.standard_normal((int(counts.sum()), heads * group, dim)), dtype)
+    acc0 = rng.random((batch, heads, 40)).astype(np.float32)
+    lens, counts = lens.tolist(), counts.tolist()
+    out, lse, acc = _run_attend(cache, q.to(DEV), counts, lens, heads, 0.2, True, dtype, acc0, 40)
+    _check_attend(cache, q, counts, lens, heads, 0.2, dtype, out, lse, acc, acc0)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attend_of_unaligned_and_strided_queries(dtype):
     rng = np.random.default_rng(3)
