@@ -8,9 +8,9 @@
 //
 // Both are bound by memory: append reads 2 D e and writes D + 8 bytes for each token and head
 // (e bytes a value), read the reverse. A warp takes a token and a few of its heads, so that sequence,
-// slot and page are looked up once for all of them; half of it takes the key's row, half the
-// value's (D = 64: two heads at a time), 8 values to a lane, which is one 16-byte load of bf16 (two
-// of fp32) and one word of codes. The minimum and maximum go through shuffles inside those lanes.
+// slot and page are looked up once for all of them. To append, four lanes take a row, so that what a
+// row costs once (two bounds, two divisions) is shared by 32 values of a lane (16 lanes a row spent
+// 2.5 times the time on it); to read, D / 8 lanes, a word of codes each, as there is nothing to share.
 #include <algorithm>
 
 #include "kv_common.cuh"
@@ -74,10 +74,10 @@ struct Eight {
 
 // The codes rint((x - off) / s) of 8 values of each lane of a warp, float32 with IEEE division. The quotient is first
 // taken with a reciprocal; where the remainder shows it within 2^-17 of a tie (bf16 values often
-// sit on one) or the reciprocal leaves the normal numbers, it is divided. Lanes without `use` get anything.
-__device__ __forceinline__ uint32_t codes8(const float (&x)[8], float off, float s, bool use) {
+// sit on one) or the reciprocal y = div_recip(s) leaves the normal numbers, it is divided. Lanes without
+// `use` get anything.
+__device__ __forceinline__ uint32_t codes8(const float (&x)[8], float off, float s, float y, bool use) {
     constexpr float kRound = 12582912.0f;   // 1.5 * 2^23: adding it rounds to a whole number
-    const float y = div_recip(s);
     const float edge = !use ? INFINITY : y == 0.0f ? -1.0f : s * (0.5f - 0x1p-17f);
     float r[8], d[8], most = 0.0f;
 #pragma unroll
@@ -139,7 +139,7 @@ __global__ void __launch_bounds__(kThreads, 3) kv_append_kernel(KvView c, RowSou
                                                              const int32_t* __restrict__ lens, int32_t* lens_out,
                                                              float* __restrict__ acc, int32_t* __restrict__ pos, int64_t S,
                                                              const int32_t* __restrict__ seen, int32_t* seen_out, int* info) {
-    constexpr int kLanes = D / 8, kRowsAtOnce = 32 / kLanes;   // D = 128: a head's two rows; 64: two heads'
+    constexpr int kChunks = D / 32;   // of 8 values, to each of a row's four lanes
     const int64_t cap = kv_capacity(c);
     if (blockIdx.x == 0) {
         for (int b = threadIdx.x; b < c.batch; b += kThreads) {
@@ -151,9 +151,7 @@ __global__ void __launch_bounds__(kThreads, 3) kv_append_kernel(KvView c, RowSou
         }
         if (threadIdx.x == 0 && (start[0] != 0 || start[c.batch] != tokens)) record_error(info, -KQ_ERR_INVALID_ARG);
     }
-    const int lane = threadIdx.x & 31, in_row = lane % kLanes, sub = lane / kLanes;
-    const int which = sub & 1;
-    const uint32_t mask = (kLanes == 16 ? 0xFFFFu : 0xFFu) << (lane - in_row);
+    const int lane = threadIdx.x & 31, in_row = lane & 3, which = (lane >> 2) & 1, in_batch = lane >> 3;
     const int head_bytes = c.page * (D + 8);
     const int64_t stride = src.head[which];
     const int64_t warps = static_cast<int64_t>(gridDim.x) * (kThreads / 32);
@@ -181,53 +179,52 @@ __global__ void __launch_bounds__(kThreads, 3) kv_append_kernel(KvView c, RowSou
                 record_error(info, -KQ_ERR_INVALID_ARG);
             }
         }
-        constexpr int kHeads = kRowsAtOnce / 2, kRounds = kBatch / kHeads;   // heads at once, rounds of a batch
-        const T* p = static_cast<const T*>(src.p[which]) + i * src.token[which] + min(h0 + (sub >> 1), h1 - 1) * stride + in_row * 8;
-        uint8_t* g = k.g + (h0 + (sub >> 1)) * static_cast<int64_t>(head_bytes);
-        uint8_t* const code_at = g + kv_code_at(D, which, k.t) + in_row * 4;
-        uint8_t* const prm_at = g + kv_param_at(D, which, k.t);
-        int64_t moved = 0;
-        for (int h = h0 + (sub >> 1); h - (sub >> 1) < h1; h += kBatch) {
-            Eight<T, VEC> raw[kRounds];
+        // lane in_row of a row takes its values 8 in_row + 32 i ..
+        const T* p = static_cast<const T*>(src.p[which]) + i * src.token[which] + in_row * 8;
+        uint8_t* const at = k.g + (h0 + in_batch) * static_cast<int64_t>(head_bytes);
+        uint32_t* codes = reinterpret_cast<uint32_t*>(at + kv_code_at(D, which, k.t)) + in_row;
+        uint32_t* params = reinterpret_cast<uint32_t*>(at + kv_param_at(D, which, k.t));
+        for (int hb = h0; hb < h1; hb += kBatch) {   // all lanes go along; rows past the last head are not written
+            const int h = hb + in_batch;
+            const T* row = p + min(h, h1 - 1) * stride;
+            Eight<T, VEC> raw[kChunks];
 #pragma unroll
-            for (int u = 0; u < kRounds; ++u) {
-                raw[u].load(p);
-                if (h + (u + 1) * kHeads < h1) p += kHeads * stride;   // past the last head: that one again
+            for (int u = 0; u < kChunks; ++u) raw[u].load(row + 32 * u);
+            float lo = raw[0].get(0), hi = lo, odd = 0.0f;
+#pragma unroll
+            for (int u = 0; u < kChunks; ++u)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float x = raw[u].get(j);
+                    lo = fminf(lo, x);
+                    hi = fmaxf(hi, x);
+                    odd = fmaf(x, 0.0f, odd);   // a NaN if one of them is not finite
+                }
+#pragma unroll
+            for (int o = 1; o < 4; o <<= 1) {
+                lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+                hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+                odd += __shfl_xor_sync(0xffffffffu, odd, o);
             }
+            // down to bf16: negative values get a larger magnitude; up to bf16: the scale is >= 0
+            const uint32_t lb = __float_as_uint(lo);
+            const uint32_t ob = (lb + ((lb >> 31) ? 0xFFFFu : 0u)) & 0xFFFF0000u;
+            const float off = __uint_as_float(ob);
+            const uint32_t sb = (__float_as_uint(__fdiv_rn(__fsub_rn(hi, off), 15.0f)) + 0xFFFFu) & 0xFFFF0000u;
+            const float s = __uint_as_float(sb);
+            const bool fine = odd == 0.0f && isfinite(off) && isfinite(s), use = fine && s > 0.0f;
+            const float y = div_recip(s);
 #pragma unroll
-            for (int u = 0; u < kRounds; ++u) {   // all lanes go along; rows past the last head are not written
-                const bool real = h + u * kHeads < h1;
+            for (int u = 0; u < kChunks; ++u) {
                 float x[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) x[j] = raw[u].get(j);
-                float lo = x[0], hi = x[0], odd = 0.0f;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    lo = fminf(lo, x[j]);
-                    hi = fmaxf(hi, x[j]);
-                    odd = fmaf(x[j], 0.0f, odd);   // a NaN if one of them is not finite
-                }
-#pragma unroll
-                for (int o = kLanes / 2; o > 0; o >>= 1) {
-                    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-                    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-                }
-                bool fine = (__ballot_sync(0xffffffffu, odd != 0.0f) & mask) == 0;
-                // down to bf16: negative values get a larger magnitude; up to bf16: the scale is >= 0
-                const uint32_t lb = __float_as_uint(lo);
-                const uint32_t ob = (lb + ((lb >> 31) ? 0xFFFFu : 0u)) & 0xFFFF0000u;
-                const float off = __uint_as_float(ob);
-                const uint32_t sb = (__float_as_uint(__fdiv_rn(__fsub_rn(hi, off), 15.0f)) + 0xFFFFu) & 0xFFFF0000u;
-                const float s = __uint_as_float(sb);
-                fine = fine && isfinite(off) && isfinite(s);
-                const bool use = fine && s > 0.0f;
-                const uint32_t word = codes8(x, off, s, use);
-                if (real) {
-                    *reinterpret_cast<uint32_t*>(code_at + moved) = use ? word : 0u;
-                    if (in_row == 0) *reinterpret_cast<uint32_t*>(prm_at + moved) = fine ? (sb >> 16) | ob : 0x7FC07FC0u;
-                }
-                moved += kHeads * static_cast<int64_t>(head_bytes);
+                const uint32_t word = codes8(x, off, s, y, use);
+                if (h < h1) codes[4 * u] = use ? word : 0u;
             }
+            if (h < h1 && in_row == 0) *params = fine ? (sb >> 16) | ob : 0x7FC07FC0u;
+            codes += kBatch * static_cast<int64_t>(head_bytes) / 4;
+            params += kBatch * static_cast<int64_t>(head_bytes) / 4;
         }
     }
 }
