@@ -134,7 +134,7 @@ __device__ __forceinline__ Token locate(const KvView& c, int b, int64_t slot, in
 }
 
 template <typename T, int D, bool VEC>
-__global__ void __launch_bounds__(kThreads, 3) kv_append_kernel(KvView c, RowSource src, int64_t tokens, int groups, int per,
+__global__ void __launch_bounds__(kThreads, VEC && sizeof(T) == 2 ? 4 : 3) kv_append_kernel(KvView c, RowSource src, int64_t tokens, int groups, int per,
                                                              const int32_t* __restrict__ start,
                                                              const int32_t* __restrict__ lens, int32_t* lens_out,
                                                              float* __restrict__ acc, int32_t* __restrict__ pos, int64_t S,
@@ -190,21 +190,21 @@ __global__ void __launch_bounds__(kThreads, 3) kv_append_kernel(KvView c, RowSou
             Eight<T, VEC> raw[kChunks];
 #pragma unroll
             for (int u = 0; u < kChunks; ++u) raw[u].load(row + 32 * u);
-            float lo = raw[0].get(0), hi = lo, odd = 0.0f;
+            // a NaN among the values stays in both
+            float lo = raw[0].get(0), hi = lo;
 #pragma unroll
             for (int u = 0; u < kChunks; ++u)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float x = raw[u].get(j);
-                    lo = fminf(lo, x);
-                    hi = fmaxf(hi, x);
-                    odd = fmaf(x, 0.0f, odd);   // a NaN if one of them is not finite
+                for (int j = 0; j < 8; j += 2) {
+                    const float x = raw[u].get(j), z = raw[u].get(j + 1);
+                    asm("min.NaN.f32 %0, %0, %1, %2;" : "+f"(lo) : "f"(x), "f"(z));
+                    asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(hi) : "f"(x), "f"(z));
                 }
 #pragma unroll
             for (int o = 1; o < 4; o <<= 1) {
-                lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-                hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-                odd += __shfl_xor_sync(0xffffffffu, odd, o);
+                const float l = __shfl_xor_sync(0xffffffffu, lo, o), t = __shfl_xor_sync(0xffffffffu, hi, o);
+                asm("min.NaN.f32 %0, %0, %1;" : "+f"(lo) : "f"(l));
+                asm("max.NaN.f32 %0, %0, %1;" : "+f"(hi) : "f"(t));
             }
             // down to bf16: negative values get a larger magnitude; up to bf16: the scale is >= 0
             const uint32_t lb = __float_as_uint(lo);
@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(kThreads, 3) kv_append_kernel(KvView c, RowSou
             const float off = __uint_as_float(ob);
             const uint32_t sb = (__float_as_uint(__fdiv_rn(__fsub_rn(hi, off), 15.0f)) + 0xFFFFu) & 0xFFFF0000u;
             const float s = __uint_as_float(sb);
-            const bool fine = odd == 0.0f && isfinite(off) && isfinite(s), use = fine && s > 0.0f;
+            const bool fine = isfinite(hi) && isfinite(off) && isfinite(s), use = fine && s > 0.0f;
             const float y = div_recip(s);
 #pragma unroll
             for (int u = 0; u < kChunks; ++u) {
