@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(NT, 1536 / NT) logprob_kernel(const T* __restr
     }
     const float lz2 = log2f(z);
     if (tid == 0) {
-        out.logp[r] = y < 0 ? 0.0f : y >= V ? NAN : (fmaf(value(x, y), kLog2e, -r2) - lz2) * kLn2;
+        out.logp[r] = y < 0 ? 0.0f : y >= V ? NAN : fminf(0.0f, (fmaf(value(x, y), kLog2e, -r2) - lz2) * kLn2);
         if (out.entropy) out.entropy[r] = fmaxf(0.0f, (lz2 - w / z) * kLn2);
         if (out.lse) out.lse[r] = (r2 + lz2) * kLn2;
     }
@@ -368,7 +368,7 @@ __global__ void __launch_bounds__(NT, 1536 / NT) logprob_kernel(const T* __restr
         for (int i = 0; i < n; ++i) rank += list[i] > k;
         if (rank < top) {
             out.top_id[r * top + rank] = static_cast<int32_t>(key_index(k));
-            out.top_logp[r * top + rank] = (fmaf(key_value(k), kLog2e, -r2) - lz2) * kLn2;
+            out.top_logp[r * top + rank] = fminf(0.0f, (fmaf(key_value(k), kLog2e, -r2) - lz2) * kLn2);
         }
     }
 }
