@@ -23,8 +23,9 @@
 // lane take its operands straight from the staged bytes in the mma layout (a lane's 16 bytes of a
 // key row are its share of every k step; the order of the dimensions inside a product is free).
 //
-// Split. The work is the list of 32-token steps of every (sequence, head, group of query rows), and
-// each warp takes an equal, contiguous part of it, so ragged lengths, few sequences and long ones all
+// Split. The work is the list of 32-token steps of every (sequence, head, group of query rows), an item,
+// each led by kItemCost steps that stand for its beginning and end (or the items of short sequences would
+// all fall to a few warps); each warp takes an equal, contiguous part of it, so ragged lengths, few sequences and long ones all
 // fill the GPU evenly, without the host knowing the lengths. A warp streams its tokens through a
 // ring of bulk copies that it refills itself and shares nothing with the other warps: 16 of them on
 // an SM, none waiting for another. One that covers all of a (sequence, head) writes its output;
@@ -48,6 +49,7 @@ constexpr int kStages = 3;                       // steps in a warp's ring
 constexpr int kAhead = 16;                       // steps whose addresses the lanes of a warp hold, a granule each
 constexpr int kMaxRows = 40960;                  // rows of all pieces together: the workspace holds two results of each
 constexpr int kMinSteps = 2;                     // of a piece, where there is little work
+constexpr int kItemCost = 4;                     // what beginning and ending an item costs, in steps
 constexpr float kSlack = 8.0f;                   // how far, in powers of two, a weight may pass 1
 constexpr float kNone = -3.0e38f;                // a maximum over nothing: finite, so that differences with it are numbers
 constexpr int kSettle = 8;                       // steps whose middle-code sums are taken off at once
@@ -142,7 +144,6 @@ struct Attend {
 // What the warp that begins the rows of an item leaves to kv_combine_kernel.
 struct Joint {
     int32_t first, last;     // the pieces that share them; equal: nothing to join
-    int32_t slot;            // which of the first piece's two partial results
     int32_t h, row, rows;    // head, first query row of the sequence, number of rows
     int32_t token;           // the sequence's first token
 };
@@ -173,7 +174,7 @@ struct Work {
 };
 __device__ __forceinline__ Work work_of(const Attend& p, const Seq& s) {
     const int64_t items = static_cast<int64_t>(s.rows_tiles) * p.c.kv_heads;
-    return {items * s.steps, items};
+    return {items * (s.steps + kItemCost), items};
 }
 // Divisions of numbers that nearly always fit 32 bits.
 __device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
@@ -212,7 +213,9 @@ __device__ __forceinline__ Work scan_add(const Work& v, Work base, Work* tmp, Wo
 
 // A position in the list of work: step `step` of row group `rt` of head h of sequence b.
 struct Place {
-    int b, h, rt, step;
+    int b, h, rt;
+    int v;          // place in the item's kItemCost + steps
+    int step;       // the step that the warp's part of the item begins with
     int64_t item;   // its number in the list
     Seq s;
 };
@@ -227,7 +230,7 @@ __device__ __forceinline__ void next_sequence(const Attend& p, Place& at) {
 // Past the rest of this row group.
 template <int ROWS>
 __device__ __forceinline__ void next_item(const Attend& p, Place& at) {
-    at.step = 0;
+    at.v = 0;
     ++at.item;
     if (++at.rt < at.s.rows_tiles) return;
     at.rt = 0;
@@ -600,10 +603,10 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas) kv_attend_ke
     at.b = found_b[warp];
     at.s = found_s[warp];
     {
-        const int64_t rem = w0 - found_base[warp].steps, head = static_cast<int64_t>(at.s.rows_tiles) * at.s.steps;
+        const int64_t rem = w0 - found_base[warp].steps, length = at.s.steps + kItemCost, head = at.s.rows_tiles * length;
         at.h = static_cast<int>(divide(rem, head));
-        at.rt = static_cast<int>(divide(rem - at.h * head, at.s.steps));
-        at.step = static_cast<int>(rem - at.h * head - static_cast<int64_t>(at.rt) * at.s.steps);
+        at.rt = static_cast<int>(divide(rem - at.h * head, length));
+        at.v = static_cast<int>(rem - at.h * head - at.rt * length);
         at.item = found_base[warp].items + static_cast<int64_t>(at.h) * at.s.rows_tiles + at.rt;
     }
 
@@ -613,13 +616,16 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas) kv_attend_ke
     bool fine_waits = true;   // a wait that gave up ends the warp's work
     int issued = 0;
     for (int64_t w = w0; w < w1 && fine_waits;) {
-        const int seg = static_cast<int>(min(w1 - w, static_cast<int64_t>(at.s.steps - at.step)));
+        // this warp's part of the item: steps from at.step, seg of them
+        const int length = at.s.steps + kItemCost, part_of = static_cast<int>(min(w1 - w, static_cast<int64_t>(length - at.v)));
+        at.step = max(at.v - kItemCost, 0);
+        const int seg = max(at.v + part_of - kItemCost, 0) - at.step;
+        if (seg == 0) break;   // the warp's last, and the next warp's item
         const int rows = min(kRows, at.s.nq * p.group - at.rt * kRows);
         if (at.step == 0 && lane == 0) {
             Joint j;
             j.first = static_cast<int32_t>(me);
-            j.last = seg == at.s.steps ? j.first : static_cast<int32_t>(pieces.of(w + at.s.steps - 1));
-            j.slot = w > w0 ? 1 : 0;
+            j.last = seg == at.s.steps ? j.first : static_cast<int32_t>(pieces.of(w - at.v + length - 1));
             j.h = at.h;
             j.row = at.rt * kRows;
             j.rows = rows;
@@ -733,7 +739,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas) kv_attend_ke
 
         // ---- the rows' result, or this piece's part of it
         const bool whole = seg == at.s.steps;
-        float* part = p.part + (2 * me + (at.step == 0 && w > w0 ? 1 : 0)) * (kRows * (D + 2));
+        float* part = p.part + (2 * me + (at.step == 0)) * (kRows * (D + 2));   // of an item begun here, of one gone on with
         // 2^24 of subnormal codes, 2^-6 2^(ev + 1 - 127) of the weights
         const float up = __uint_as_float(static_cast<uint32_t>(min(R.ev - (kSplit ? 132 : 108), 127) + 127) << 23);
 #pragma unroll
@@ -775,9 +781,9 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas) kv_attend_ke
                 }
             }
         }
-        w += seg;
-        at.step += seg - 1;
-        if (++at.step == at.s.steps) next_item<kRows>(p, at);
+        w += part_of;
+        at.v += part_of;
+        if (at.v == length) next_item<kRows>(p, at);
     }
     if (!fine_waits && lane == 0) {   // leave only when this warp's copies have landed
         record_error(p.info, -KQ_ERR_TIMEOUT);
@@ -801,8 +807,8 @@ __global__ void __launch_bounds__(256) kv_combine_kernel(const Attend p) {
     if (blockIdx.x >= items || j.last == j.first) return;
     const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5;
     const int many = j.last - j.first + 1;
-    // the results after the first begin their pieces
-    auto result = [&](int k) { return p.part + (2 * static_cast<int64_t>(j.first + k) + (k == 0 ? j.slot : 0)) * kPart; };
+    // the piece that begins the item has its result second, those that go on with it first
+    auto result = [&](int k) { return p.part + (2 * static_cast<int64_t>(j.first + k) + (k == 0)) * kPart; };
     const bool share = many > 32;
     for (int col = share ? blockIdx.y : grp + blockIdx.y * kGroups; col < j.rows; col += gridDim.y * (share ? 1 : kGroups)) {
         float M = kNone, L = 0.0f, O[kV];
