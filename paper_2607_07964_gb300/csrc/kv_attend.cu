@@ -190,25 +190,24 @@ struct Pieces {
     __device__ int64_t of(int64_t w) const { return w < r * (q + 1) ? divide(w, q + 1) : r + divide(w - r * (q + 1), q); }
 };
 
-// lead = base + the sum of v over the threads before this one; returns base + the sum over all.
-__device__ __forceinline__ Work scan_add(const Work& v, Work base, Work* tmp, Work& lead) {
+// lead: the sum of v over the threads before this one; returns the sum over all.
+__device__ __forceinline__ Work scan_add(const Work& v, Work* tmp, Work& lead) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    Work x = v;
+    Work x = v, all = {0, 0};
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const int64_t y = __shfl_up_sync(0xffffffffu, x.steps, o), z = __shfl_up_sync(0xffffffffu, x.items, o);
         if (lane >= o) x.steps += y, x.items += z;
     }
-    __syncthreads();
     if (lane == 31) tmp[warp] = x;
     __syncthreads();
-    lead = {base.steps + x.steps - v.steps, base.items + x.items - v.items};
+    lead = {x.steps - v.steps, x.items - v.items};
 #pragma unroll
     for (int i = 0; i < kThreads / 32; ++i) {
         if (i < warp) lead.steps += tmp[i].steps, lead.items += tmp[i].items;
-        base.steps += tmp[i].steps, base.items += tmp[i].items;
+        all.steps += tmp[i].steps, all.items += tmp[i].items;
     }
-    return base;
+    return all;
 }
 
 // A position in the list of work: step `step` of row group `rt` of head h of sequence b.
@@ -559,41 +558,35 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas) kv_attend_ke
         found_b[warp] = -1;
     }
     if (blockIdx.x == 0 && tid == 0 && (p.start[0] != 0 || p.start[c.batch] != p.tokens)) record_error(p.info, -KQ_ERR_INVALID_ARG);
-    // the sequences' steps, kThreads sequences at a time: the total, then the one that holds a warp's first
-    Seq s = {};
-    Work all = {0, 0}, v = {0, 0}, lead = {0, 0};
-    for (int b0 = 0; b0 < c.batch; b0 += kThreads) {
-        v = {0, 0};
-        if (b0 + tid < c.batch) {
-            s = sequence<kRows>(p, b0 + tid, blockIdx.x ? nullptr : p.info);
-            v = work_of(p, s);
-        }
-        all = scan_add(v, all, scan_tmp, lead);
+    // the sequences' steps, a run of sequences to a thread: the total, then the sequence that holds a warp's first
+    const int run = (c.batch + kThreads - 1) / kThreads, b0 = min(tid * run, c.batch), b1 = min(b0 + run, c.batch);
+    Work v = {0, 0}, lead;
+    for (int b = b0; b < b1; ++b) {
+        const Work one = work_of(p, sequence<kRows>(p, b, blockIdx.x ? nullptr : p.info));
+        v.steps += one.steps, v.items += one.items;
     }
+    const Work all = scan_add(v, scan_tmp, lead);
     const int64_t W = all.steps;
     const int64_t C = max(static_cast<int64_t>(1), min(static_cast<int64_t>(gridDim.x) * kWarps, (W + kMinSteps - 1) / kMinSteps));
     const Pieces pieces(W, C);
     const int64_t me = warp * static_cast<int64_t>(gridDim.x) + blockIdx.x;   // neighbours in the list on different SMs
     const int64_t w0 = me < C ? pieces.first(me) : W, w1 = me < C ? pieces.first(me + 1) : W;
     if (blockIdx.x == 0 && tid == 0) *p.items = all.items;
-    Work before = {0, 0};
-    for (int b0 = 0; b0 < c.batch; b0 += kThreads) {
-        if (c.batch > kThreads) {
-            v = {0, 0};
-            if (b0 + tid < c.batch) {
-                s = sequence<kRows>(p, b0 + tid, nullptr);
-                v = work_of(p, s);
-            }
-            before = scan_add(v, before, scan_tmp, lead);
-        }
-        for (int i = 0; i < kWarps; ++i) {
-            const int64_t other = i * static_cast<int64_t>(gridDim.x) + blockIdx.x;
-            const int64_t o0 = other < C ? pieces.first(other) : W;
-            if (v.steps > 0 && lead.steps <= o0 && o0 < lead.steps + v.steps) {
-                found_b[i] = b0 + tid;
-                found_base[i] = lead;
+    for (int i = 0; i < kWarps; ++i) {
+        const int64_t other = i * static_cast<int64_t>(gridDim.x) + blockIdx.x;
+        const int64_t o0 = other < C ? pieces.first(other) : W;
+        if (o0 < lead.steps || o0 >= lead.steps + v.steps) continue;
+        Work at = lead;
+        for (int b = b0; b < b1; ++b) {
+            const Seq s = sequence<kRows>(p, b, nullptr);
+            const Work one = work_of(p, s);
+            if (o0 < at.steps + one.steps) {
+                found_b[i] = b;
+                found_base[i] = at;
                 found_s[i] = s;
+                break;
             }
+            at.steps += one.steps, at.items += one.items;
         }
     }
     __syncthreads();
