@@ -900,23 +900,33 @@ __global__ void __launch_bounds__(256) kv_weight_kernel(const Attend p, float* _
             const float* sc = p.scores + ((tk * p.c.kv_heads + h) * p.S + s0) * p.group;
             const float* ls = p.lse + tk * p.q_heads + h * p.group;
             if constexpr (QUADS) {
-                for (int g = 0; g < p.group; g += 4) {
-                    float4 x[kSlots];
+                for (int g = 0; g < p.group; g += 8) {   // a 32-byte sector at a time where the group fills it
+                    float4 x[kSlots][2];
+                    const bool two = g + 4 < p.group;
 #pragma unroll
                     for (int u = 0; u < kSlots; ++u)
-                        if (s0 + u * 256 < end) x[u] = __ldcs(reinterpret_cast<const float4*>(sc + static_cast<int64_t>(u) * 256 * p.group + g));
-                    const float l0 = ls[g] * kLog2e, l1 = ls[g + 1] * kLog2e, l2 = ls[g + 2] * kLog2e, l3 = ls[g + 3] * kLog2e;
+                        if (s0 + u * 256 < end) {
+                            const float4* at = reinterpret_cast<const float4*>(sc + static_cast<int64_t>(u) * 256 * p.group + g);
+                            x[u][0] = at[0];
+                            if (two) x[u][1] = at[1];
+                        }
 #pragma unroll
-                    for (int u = 0; u < kSlots; ++u)
-                        if (s0 + u * 256 < end)
-                            sum[u] += ex2(x[u].x - l0) + ex2(x[u].y - l1) + (ex2(x[u].z - l2) + ex2(x[u].w - l3));
+                    for (int q = 0; q < 2; ++q) {
+                        if (q && !two) break;
+                        const float* l = ls + g + 4 * q;
+                        const float l0 = l[0] * kLog2e, l1 = l[1] * kLog2e, l2 = l[2] * kLog2e, l3 = l[3] * kLog2e;
+#pragma unroll
+                        for (int u = 0; u < kSlots; ++u)
+                            if (s0 + u * 256 < end)
+                                sum[u] += ex2(x[u][q].x - l0) + ex2(x[u][q].y - l1) + (ex2(x[u][q].z - l2) + ex2(x[u][q].w - l3));
+                    }
                 }
             } else {
                 for (int g = 0; g < p.group; ++g) {
                     const float l0 = ls[g] * kLog2e;
 #pragma unroll
                     for (int u = 0; u < kSlots; ++u)
-                        if (s0 + u * 256 < end) sum[u] += ex2(__ldcs(sc + static_cast<int64_t>(u) * 256 * p.group + g) - l0);
+                        if (s0 + u * 256 < end) sum[u] += ex2(sc[static_cast<int64_t>(u) * 256 * p.group + g] - l0);
                 }
             }
         }
