@@ -557,6 +557,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas) kv_attend_ke
         abort_flag[warp] = 0;
         found_b[warp] = -1;
     }
+    pdl_wait();   // nothing before this reads or writes global memory
     if (blockIdx.x == 0 && tid == 0 && (p.start[0] != 0 || p.start[c.batch] != p.tokens)) record_error(p.info, -KQ_ERR_INVALID_ARG);
     // the sequences' steps, a run of sequences to a thread: the total, then the sequence that holds a warp's first
     const int run = (c.batch + kThreads - 1) / kThreads, b0 = min(tid * run, c.batch), b1 = min(b0 + run, c.batch);
@@ -937,10 +938,11 @@ __global__ void __launch_bounds__(256) kv_weight_kernel(const Attend p, float* _
 }
 
 template <typename... Params, typename... Args>
-cudaError_t launch_after(void (*kern)(Params...), dim3 grid, dim3 block, cudaStream_t st, Args... args) {
+cudaError_t launch_after(void (*kern)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -964,13 +966,13 @@ kq_status run_attend(const Attend& p, cudaStream_t stream) {
         return KQ_OK;
     }));
     const int grid = std::min(kMaxRows / Sh::kRows, num_sms() * Sh::kCtas * kWarps) / kWarps;
-    kv_attend_kernel<T, D, NT><<<grid, kThreads, Sh::kSmem, stream>>>(p);
-    KQ_LAUNCH_CHECK("kv_attend_kernel");
+    KQ_CUDA(launch_after(kv_attend_kernel<T, D, NT>, dim3(grid), dim3(kThreads), Sh::kSmem, stream, p));
+    count_launch();
     // a sequence has ceil(queries group / rows) items a head: at most this many, and few of them have many
     // results each, with a block for each column to go through them
     const int64_t items = most_items(p.tokens, p.c.batch, p.group, p.c.kv_heads, Sh::kRows);
     const bool few = items * 32 < static_cast<int64_t>(grid) * kWarps;
-    KQ_CUDA(launch_after(kv_combine_kernel<T, D, NT>, dim3(static_cast<unsigned>(items), few ? Sh::kRows : NT), dim3(256), stream, p));
+    KQ_CUDA(launch_after(kv_combine_kernel<T, D, NT>, dim3(static_cast<unsigned>(items), few ? Sh::kRows : NT), dim3(256), 0, stream, p));
     count_launch();
     return KQ_OK;
 }
@@ -1057,8 +1059,8 @@ extern "C" kq_status kq_kv_attend(const kq_kv_cache* cache, const void* q, int d
         const int64_t heads = static_cast<int64_t>(c.batch) * c.kv_heads;
         const dim3 wg(static_cast<unsigned>(heads),
                       static_cast<unsigned>(std::min<int64_t>(cdiv(p.cap, 1024), std::max<int64_t>(1, cdiv(num_sms() * 16, heads)))));
-        KQ_CUDA(p.group % 4 ? launch_after(kv_weight_kernel<false>, wg, dim3(256), stream, p, acc)
-                            : launch_after(kv_weight_kernel<true>, wg, dim3(256), stream, p, acc));
+        KQ_CUDA(p.group % 4 ? launch_after(kv_weight_kernel<false>, wg, dim3(256), 0, stream, p, acc)
+                            : launch_after(kv_weight_kernel<true>, wg, dim3(256), 0, stream, p, acc));
         count_launch();
     }
     return KQ_OK;
