@@ -335,10 +335,10 @@ extern "C" kq_status kq_kv_append(const kq_kv_cache* cache, const void* k, const
     bool vec = true;
     for (int w = 0; w < 2; ++w)
         vec = vec && !(reinterpret_cast<uintptr_t>(src.p[w]) & 15u) && !((src.token[w] * es) & 15u) && !((src.head[w] * es) & 15u);
-    const Cut k_ = cut(T, c.kv_heads);
+    const Cut by = cut(T, c.kv_heads);
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
 #define KQ_APPEND(TY, DIM, VEC) \
-    kv_append_kernel<TY, DIM, VEC><<<k_.grid, kThreads, 0, stream>>>(c, src, T, k_.groups, k_.per, start, lens, lens_out, acc, pos, S, \
+    kv_append_kernel<TY, DIM, VEC><<<by.grid, kThreads, 0, stream>>>(c, src, T, by.groups, by.per, start, lens, lens_out, acc, pos, S, \
                                                                       seen, seen_out, info)
     if (dtype == KQ_BF16) {
         if (c.dim == 128) vec ? KQ_APPEND(__nv_bfloat16, 128, true) : KQ_APPEND(__nv_bfloat16, 128, false);
@@ -367,10 +367,10 @@ extern "C" kq_status kq_kv_read(const kq_kv_cache* cache, const int32_t* start, 
         return KQ_ERR_INVALID_ARG;
     }
     if (T == 0) return KQ_OK;
-    const Cut k_ = cut(T, c.kv_heads);
+    const Cut by = cut(T, c.kv_heads);
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
 #define KQ_READ(TY, DIM)                                                                                         \
-    kv_read_kernel<TY, DIM><<<k_.grid, kThreads, 0, stream>>>(c, k_.groups, k_.per, start, first, lens, T, static_cast<TY*>(k), \
+    kv_read_kernel<TY, DIM><<<by.grid, kThreads, 0, stream>>>(c, by.groups, by.per, start, first, lens, T, static_cast<TY*>(k), \
                                                               static_cast<TY*>(v), info)
     if (dtype == KQ_BF16) c.dim == 128 ? KQ_READ(__nv_bfloat16, 128) : KQ_READ(__nv_bfloat16, 64);
     else c.dim == 128 ? KQ_READ(float, 128) : KQ_READ(float, 64);

@@ -468,6 +468,24 @@ def test_attend_records_bad_lengths_pages_and_tokens():
     assert status([0, 1, 2], [20, 32], dt) == K().KQ_OK and torch.equal(out, good)
 
 
+def test_attend_of_overlapping_sequences_stays_in_its_workspace():
+    """start goes back and forth: more rows than tokens, reported, with nothing written past the workspace or out."""
+    rng = np.random.default_rng(10)
+    batch, T = 64, 9
+    cache = _pool(batch, 16, 16, 1, 64, rng)
+    _fill(cache, [16] * batch, 1, rng)
+    dc, dt = _to_dev(cache)
+    q = torch.randn(T, 1, 64, device=DEV)
+    out = torch.full((T + 64, 1, 64), 3.0, device=DEV)
+    need = K().kq_kv_attend_workspace(q, dc, dt, None)
+    ws = torch.full((need + 65536,), 0xAB, dtype=torch.uint8, device=DEV)
+    info = _i32([0])
+    start = _i32([0, T] * (batch // 2) + [0])
+    K().kq_kv_attend(q, start, _i32([16] * batch), dc, dt, out[:T], ws[:need], 0.1, info=info)
+    assert K().kq_check(info)[0] == K().KQ_ERR_INVALID_ARG
+    assert (ws[need:] == 0xAB).all() and (out[T:] == 3.0).all()
+
+
 # ------------------------------------------------------------------------------- eviction
 @pytest.mark.parametrize("dim,page,heads,lens,budget,recent,sink,kind", [
     (128, 64, 2, [300, 90, 0], 100, 10, 4, "random"), (64, 16, 1, [1000], 999, 0, 0, "random"),
