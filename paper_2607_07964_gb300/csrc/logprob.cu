@@ -9,7 +9,7 @@
 // use, so a rounding of r cancels from logp and entropy, however large the logits are.
 //
 // The largest `top` values: a bound that at least `top` of the threads' maxima reach, and the row's groups
-// of kAhead vectors whose own maximum, noted in 16 bits in shared memory along the way, reaches it
+// of kAhead (kWideAhead) vectors whose own maximum, noted in 16 bits in shared memory along the way, reaches it
 // too: only those few are read again. (Going through all values of the threads that reach the bound
 // instead reads a third of the row a second time, when it has left L2.)
 //
@@ -27,6 +27,7 @@ namespace {
 constexpr int kThreads = 256;             // of a block where there are rows for every SM, and of the gradient's
 constexpr int kWide = 1024;               // where there are few
 constexpr int kAhead = 4;                 // 16-byte loads of a thread in flight
+constexpr int kWideAhead = 8;             // of one in a block that has the SM to itself
 constexpr int kList = 1024;               // candidates for the top values
 constexpr int kGroups = 256;              // groups that are looked through for them
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
@@ -150,7 +151,7 @@ __device__ __noinline__ void careful_row(const T* x, int64_t r, int64_t V, int64
 template <typename T, int NT>
 __global__ void __launch_bounds__(NT, 1536 / NT) logprob_kernel(const T* __restrict__ logits, int64_t V, int64_t ld,
                                                                 const int64_t* __restrict__ target, int top, Out out) {
-    constexpr int E = 16 / sizeof(T), kWarps = NT / 32;
+    constexpr int E = 16 / sizeof(T), kWarps = NT / 32, A = NT == kWide ? kWideAhead : kAhead;
     __shared__ uint64_t tmp64[kWarps], list[kList];
     __shared__ float tmp[2][kWarps][4];
     __shared__ int groups[kGroups], n_groups, n_list;
@@ -186,13 +187,13 @@ __global__ void __launch_bounds__(NT, 1536 / NT) logprob_kernel(const T* __restr
     // the values' order as whole numbers, and its upper half: all of a bf16 value's
     auto order = [](float v) { return static_cast<uint32_t>(rank_key(v, 0) >> 32); };
     int j = tid;
-    for (; j + (kAhead - 1) * NT < nvec; j += kAhead * NT) {
-        uint4 u[kAhead];
+    for (; j + (A - 1) * NT < nvec; j += A * NT) {
+        uint4 u[A];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) u[i] = __ldg(xv + j + i * NT);
+        for (int i = 0; i < A; ++i) u[i] = __ldg(xv + j + i * NT);
         float gm = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
+        for (int i = 0; i < A; ++i) {
             float v[E];
             const float m = unpack<T>(u[i], v);
             gm = fmaxf(gm, m);
@@ -206,13 +207,13 @@ __global__ void __launch_bounds__(NT, 1536 / NT) logprob_kernel(const T* __restr
         ++n_mine;
     }
     if (j < nvec) {
-        uint4 u[kAhead - 1];
+        uint4 u[A - 1];
 #pragma unroll
-        for (int i = 0; i < kAhead - 1; ++i)
+        for (int i = 0; i < A - 1; ++i)
             if (j + i * NT < nvec) u[i] = __ldg(xv + j + i * NT);
         float gm = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < kAhead - 1; ++i) {
+        for (int i = 0; i < A - 1; ++i) {
             if (j + i * NT >= nvec) break;
             float v[E];
             const float m = unpack<T>(u[i], v);
@@ -310,7 +311,7 @@ __global__ void __launch_bounds__(NT, 1536 / NT) logprob_kernel(const T* __restr
         const uint32_t bound_half = static_cast<uint32_t>(bound >> 48), bound_index = key_index(bound);
         for (int g = 0; g < n_mine; ++g) {
             const uint32_t gm = group_max[g * NT + tid];
-            const int first = g * kAhead * NT + tid;   // its first vector
+            const int first = g * A * NT + tid;   // its first vector
             if (gm < bound_half || (gm == bound_half && static_cast<uint32_t>(head + first * E) > bound_index)) continue;
             const int at = atomicAdd(&n_groups, 1);
             if (at < kGroups) groups[at] = first;
@@ -323,8 +324,8 @@ __global__ void __launch_bounds__(NT, 1536 / NT) logprob_kernel(const T* __restr
         if (my_edge >= 0) offer(rank_key(ev, static_cast<uint32_t>(my_edge)));
         __syncthreads();
         if (n_groups <= kGroups) {
-            for (int q = tid; q < n_groups * kAhead; q += NT) {
-                const int at = groups[q / kAhead] + q % kAhead * NT;
+            for (int q = tid; q < n_groups * A; q += NT) {
+                const int at = groups[q / A] + q % A * NT;
                 if (at >= nvec) continue;
                 const uint4 u = __ldg(xv + at);
                 const uint32_t w4[4] = {u.x, u.y, u.z, u.w};
@@ -344,8 +345,8 @@ __global__ void __launch_bounds__(NT, 1536 / NT) logprob_kernel(const T* __restr
         // Too many near the bound's value: the top-th largest of the threads' first largest values by value and index
         // (complements, the largest first; an index is below 2^20).
         uint64_t key = my_edge >= 0 ? rank_key(ev, static_cast<uint32_t>(my_edge)) : 0;
-        for (int i = 0; i < kAhead; ++i) {
-            const int at = best_group * kAhead * NT + tid + i * NT;
+        for (int i = 0; i < A; ++i) {
+            const int at = best_group * A * NT + tid + i * NT;
             if (at >= nvec) break;
             for (int e = 0; e < E; ++e)
                 key = max(key, rank_key(value(reinterpret_cast<const T*>(xv + at), e), static_cast<uint32_t>(head + at * E + e)));
@@ -376,7 +377,7 @@ __global__ void __launch_bounds__(NT, 1536 / NT) logprob_kernel(const T* __restr
 template <typename T, int NT>
 kq_status run_logprob(const T* logits, int64_t rows, int64_t V, int64_t ld, const int64_t* target, int top, const Out& out,
                       cudaStream_t stream) {
-    const int64_t group = kAhead * NT * (16 / sizeof(T));   // values of a group of every thread
+    const int64_t group = (NT == kWide ? kWideAhead : kAhead) * NT * (16 / sizeof(T));   // values of a group of every thread
     const size_t smem = top ? static_cast<size_t>(cdiv(V, group)) * NT * sizeof(uint16_t) : 0;
     static std::atomic<uint64_t> done{0};
     KQ_TRY(once_per_device(done, [&] {
