@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(kThreads, VEC && sizeof(T) == 2 ? 4 : 3) kv_ap
     const int64_t cap = kv_capacity(c);
     if (blockIdx.x == 0) {
         for (int b = threadIdx.x; b < c.batch; b += kThreads) {
-            const int64_t add = max(0, start[b + 1] - start[b]);
+            const int64_t add = max(static_cast<int64_t>(0), static_cast<int64_t>(start[b + 1]) - start[b]);
             const int64_t n = kv_length(lens, b, cap, info);
             if (n + add > cap) record_error(info, -KQ_ERR_INVALID_ARG);
             if (lens_out) lens_out[b] = static_cast<int32_t>(min(n + add, cap));
