@@ -520,7 +520,8 @@ KQ_API kq_status kq_kv_evict(const kq_kv_cache* cache, const int32_t* lens, cons
  *     grad_v = g_logp (delta(v, target) - p_v) - g_entropy p_v (ln p_v + entropy)
  *   with lse and entropy from kq_token_logprobs (entropy and g_entropy may both be NULL). grad
  *   [T][V] in the logits' type, row stride ld_grad; it may be logits itself (same stride). A row
- *   with a negative target has no g_logp part, a row of -infinity only has grad 0. A target >= V
+ *   with a negative target has no g_logp part, a row of -infinity only has grad 0. p_v is taken from lse
+ *   as fp32 holds it: off by 2^-24 |lse| in proportion. A target >= V
  *   is recorded in info, its row's g_logp part left out.
  * ---------------------------------------------------------------------------------- */
 #define KQ_LOGPROBS_MAX_TOP 32

@@ -95,6 +95,11 @@ __device__ __forceinline__ V block_reduce(V v, V* tmp, F f) {
 }
 __device__ __forceinline__ float sum2(float a, float b) { return a + b; }
 
+// ln p of a logit; one masked with its type's lowest number would overflow in powers of two.
+__device__ __forceinline__ float logp_of(float x, float r2, float lz2) {
+    return x < kFloor ? x - (r2 + lz2) * kLn2 : fminf(0.0f, (fmaf(x, kLog2e, -r2) - lz2) * kLn2);
+}
+
 struct Out {
     float *logp, *entropy, *lse;
     int32_t* top_id;
@@ -283,7 +288,7 @@ __global__ void __launch_bounds__(NT, NT == kWide ? 1 : 1536 / NT) logprob_kerne
     }
     const float lz2 = log2f(z);
     if (tid == 0) {
-        out.logp[r] = y < 0 ? 0.0f : y >= V ? NAN : fminf(0.0f, (fmaf(value(x, y), kLog2e, -r2) - lz2) * kLn2);
+        out.logp[r] = y < 0 ? 0.0f : y >= V ? NAN : logp_of(value(x, y), r2, lz2);
         if (out.entropy) out.entropy[r] = fmaxf(0.0f, (lz2 - w / z) * kLn2);
         if (out.lse) out.lse[r] = (r2 + lz2) * kLn2;
     }
@@ -371,7 +376,7 @@ __global__ void __launch_bounds__(NT, NT == kWide ? 1 : 1536 / NT) logprob_kerne
         for (int i = 0; i < n; ++i) rank += list[i] > k;
         if (rank < top) {
             out.top_id[r * top + rank] = static_cast<int32_t>(key_index(k));
-            out.top_logp[r * top + rank] = fminf(0.0f, (fmaf(key_value(k), kLog2e, -r2) - lz2) * kLn2);
+            out.top_logp[r * top + rank] = logp_of(key_value(k), r2, lz2);
         }
     }
 }

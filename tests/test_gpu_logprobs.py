@@ -134,6 +134,42 @@ def test_logprobs_rows_without_a_distribution(V, dtype):
     assert not grad[0].any() and torch.isnan(grad[1]).any() and torch.isfinite(grad[3:].float()).all()
 
 
+@pytest.mark.parametrize("V", [7, 5000, 60000])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_logprobs_with_masks_of_the_lowest_value_and_huge_logits(V, dtype):
+    """Masks as the type's lowest number, alone, with a few allowed tokens (fewer than asked for), with -infinity, and
+    logits near the type's largest: the fast way's range ends at 1e38."""
+    lowest = torch.finfo(TYPES[dtype]).min
+    x = torch.full((6, V), lowest).to(TYPES[dtype])
+    x[1, 3] = 2.0
+    x[1, 5] = 1.0
+    x[2, ::2] = -float("inf")
+    x[3] = torch.linspace(-5, 5, V)
+    x[3, 1] = 3.0e38
+    x[4] = torch.linspace(-5, 5, V)
+    x[4, 0] = lowest
+    x[5, 2:5] = -float("inf")
+    x[5, 1] = -1.5
+    top = 4
+    target = np.array([2, 5, 1, 1, 0, 1])
+    want = _reference(x, target, top)
+    logp, h, lse, ids, tl = _run(x.to(DEV), torch.from_numpy(target).to(DEV), top)
+    for got, exact in ((lse, want[0]), (logp, want[1]), (h, want[2])):
+        got = got.cpu().numpy().astype(np.float64)
+        assert np.all(np.abs(got - exact) <= 2.0 ** -18 * (1 + np.abs(exact)) + 2.0 ** -18 * np.where(want[7] < 1e30, want[7], 0))
+    assert np.array_equal(ids.cpu().numpy(), want[3])
+    got, exact = tl.cpu().numpy().astype(np.float64), want[4]
+    inf = np.isinf(exact)
+    assert np.array_equal(got[inf], exact[inf]) and np.all(np.abs(got - exact)[~inf] <= (2.0 ** -18 * (1 + np.abs(exact)) + 2.0 ** -16)[~inf])
+    # the gradient of the rows whose log-sum fp32 can tell from the maximum
+    g = torch.ones(6, device=DEV)
+    grad = torch.empty_like(x, device=DEV)
+    K().kq_token_logprobs_grad(x.to(DEV), torch.from_numpy(target).to(DEV), lse, g, grad, entropy=h, g_entropy=g)
+    got = grad.float().cpu()
+    assert torch.isfinite(got).all()
+    assert (got[1, 6:] == 0).all() and (got[3, 2:] == 0).all()
+
+
 def test_logprobs_record_a_target_out_of_range():
     x = torch.randn(2, 10, device=DEV)
     info = torch.zeros(1, dtype=torch.int32, device=DEV)
