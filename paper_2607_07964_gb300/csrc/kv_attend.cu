@@ -629,7 +629,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas) kv_attend_ke
             j.row = at.rt * kRows;
             j.rows = rows;
             j.token = at.s.first;
-            if (at.item < p.most_items) p.joint[at.item] = j;
+            if (at.item < p.most_items && KQ_IN_RANGE(at.item, p.most_items)) p.joint[at.item] = j;
             else record_error(p.info, -KQ_ERR_INVALID_ARG);   // sequences that overlap
         }
         Feed<D> feed;
@@ -756,6 +756,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas) kv_attend_ke
                 }
                 const int col = nt * 8 + 2 * t4 + k2;
                 if (col >= rows) continue;
+                if (!KQ_IN_RANGE(part + kRows * (D + 2) - 1 - p.part, 2ll * kMaxRows * (D + 2))) continue;
                 float x[D / 8];   // dimensions g8 D / 8 ..
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i) {
@@ -765,6 +766,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas) kv_attend_ke
                 if (whole) {
                     const int row = at.rt * kRows + col;
                     const int64_t r = (static_cast<int64_t>(at.s.first) + row / p.group) * p.q_heads + at.h * p.group + row % p.group;
+                    if (!KQ_IN_RANGE(r, p.tokens * p.q_heads)) continue;
                     T* dst = static_cast<T*>(p.out) + r * D + g8 * (D / 8);
                     const float inv = L == 0.0f ? 0.0f : 1.0f / L;
 #pragma unroll
@@ -878,6 +880,7 @@ __global__ void __launch_bounds__(256) kv_combine_kernel(const Attend p) {
         }
         const int row = j.row + col;
         const int64_t r = (static_cast<int64_t>(j.token) + row / p.group) * p.q_heads + j.h * p.group + row % p.group;
+        if (!KQ_IN_RANGE(r, p.tokens * p.q_heads)) continue;
         T* dst = static_cast<T*>(p.out) + r * D + lane * kV;
         const float inv = L == 0.0f ? 0.0f : 1.0f / L;
 #pragma unroll
@@ -943,7 +946,7 @@ __global__ void __launch_bounds__(256) kv_weight_kernel(const Attend p, float* _
         }
 #pragma unroll
         for (int u = 0; u < kSlots; ++u)
-            if (s0 + u * 256 < s.n) acc[s0 + u * 256] = old[u] + sum[u];
+            if (s0 + u * 256 < s.n && KQ_IN_RANGE(s0 + u * 256, p.S)) acc[s0 + u * 256] = old[u] + sum[u];
     }
 }
 

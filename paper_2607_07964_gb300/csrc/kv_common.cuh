@@ -33,6 +33,7 @@ struct KvView {
 __host__ __device__ __forceinline__ int64_t kv_head_bytes(const KvView& c) {
     return static_cast<int64_t>(c.page) * (c.dim + 8);
 }
+__host__ __device__ __forceinline__ int64_t kv_pool_bytes(const KvView& c) { return c.pages * c.kv_heads * kv_head_bytes(c); }
 __host__ __device__ __forceinline__ int64_t kv_capacity(const KvView& c) { return c.table_ld * c.page; }
 
 // The granule of slot `slot` (0 <= slot < capacity) of sequence b and head h, or nullptr when

@@ -254,8 +254,8 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const Evict e) {
     for (int j = j0; j < j1; ++j) {
         const uint32_t k = key(j);
         const bool keep = k > t || (k == t && tie++ < want);
-        if (j < edge && !keep) hole[hole_at++] = first + j;
-        if (j >= edge && keep) tail[tail_at++] = first + j;
+        if (j < edge && !keep && KQ_IN_RANGE(hole_at, budget)) hole[hole_at++] = first + j;
+        if (j >= edge && keep && KQ_IN_RANGE(tail_at, budget)) tail[tail_at++] = first + j;
     }
     copy_front();
     sync();   // the lists and the fronts are complete, and no counts are read any more
@@ -284,8 +284,10 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const Evict e) {
                 for (int i = 0; i < 2; ++i) prm[i] = *reinterpret_cast<const uint32_t*>(src + kv_param_at(e.c.dim, i, ts));
 #pragma unroll
                 for (int i = 0; i < 2; ++i) *reinterpret_cast<uint32_t*>(dst + kv_param_at(e.c.dim, i, td)) = prm[i];
-                acc_out[to] = w;
-                pos_out[to] = q;
+                if (KQ_IN_RANGE(to, e.S)) {
+                    acc_out[to] = w;
+                    pos_out[to] = q;
+                }
                 src += ts * row;
                 dst += td * row;
             } else {
@@ -304,7 +306,8 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const Evict e) {
 #pragma unroll
             for (int i = 0; i < kMoves; ++i) {
                 const uint64_t d = __shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(dst), k0 + i & 31);
-                if (k0 + i < here && d && copies) *reinterpret_cast<uint32_t*>(d + in_row) = code[i];
+                if (k0 + i < here && d && copies && KQ_IN_RANGE(d + in_row - reinterpret_cast<uint64_t>(e.c.data), kv_pool_bytes(e.c) - 3))
+                    *reinterpret_cast<uint32_t*>(d + in_row) = code[i];
             }
         }
     }

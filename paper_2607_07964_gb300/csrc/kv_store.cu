@@ -172,6 +172,7 @@ __global__ void __launch_bounds__(kThreads, VEC && sizeof(T) == 2 ? 4 : 3) kv_ap
             if (k.slot < S) {
                 for (int h = h0 + lane; h < h1; h += 32) {
                     const int64_t at = (static_cast<int64_t>(b) * c.kv_heads + h) * S + k.slot;
+                    if (!KQ_IN_RANGE(at, static_cast<int64_t>(c.batch) * c.kv_heads * S)) continue;
                     if (acc) acc[at] = 0.0f;
                     if (pos) pos[at] = static_cast<int32_t>((seen ? seen[b] : n) + index);
                 }
@@ -220,9 +221,10 @@ __global__ void __launch_bounds__(kThreads, VEC && sizeof(T) == 2 ? 4 : 3) kv_ap
 #pragma unroll
                 for (int j = 0; j < 8; ++j) x[j] = raw[u].get(j);
                 const uint32_t word = codes8(x, off, s, y, use);
-                if (h < h1) codes[4 * u] = use ? word : 0u;
+                if (h < h1 && KQ_IN_RANGE(reinterpret_cast<uint8_t*>(codes + 4 * u) - c.data, kv_pool_bytes(c) - 3)) codes[4 * u] = use ? word : 0u;
             }
-            if (h < h1 && in_row == 0) *params = fine ? (sb >> 16) | ob : 0x7FC07FC0u;
+            if (h < h1 && in_row == 0 && KQ_IN_RANGE(reinterpret_cast<uint8_t*>(params) - c.data, kv_pool_bytes(c) - 3))
+                *params = fine ? (sb >> 16) | ob : 0x7FC07FC0u;
             codes += kBatch * static_cast<int64_t>(head_bytes) / 4;
             params += kBatch * static_cast<int64_t>(head_bytes) / 4;
         }
@@ -271,6 +273,7 @@ __global__ void __launch_bounds__(kThreads) kv_read_kernel(KvView c, int groups,
 #pragma unroll
                 for (int j = 0; j < 8; ++j) x[j] = fmaf(s, static_cast<float>((word[u] >> (4 * j)) & 15u), off);
                 T* dst = out + static_cast<int64_t>(h) * D;
+                if (!KQ_IN_RANGE(dst - (which ? v_out : k_out), tokens * c.kv_heads * D - 7)) continue;
                 if constexpr (sizeof(T) == 2) {
                     uint32_t w[4];
 #pragma unroll

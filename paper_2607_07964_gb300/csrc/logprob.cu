@@ -374,7 +374,7 @@ __global__ void __launch_bounds__(NT, NT == kWide ? 1 : 1536 / NT) logprob_kerne
         const uint64_t k = list[c];
         int rank = 0;
         for (int i = 0; i < n; ++i) rank += list[i] > k;
-        if (rank < top) {
+        if (rank < top && KQ_IN_RANGE(key_index(k), V)) {
             out.top_id[r * top + rank] = static_cast<int32_t>(key_index(k));
             out.top_logp[r * top + rank] = logp_of(key_value(k), r2, lz2);
         }
@@ -436,7 +436,7 @@ __global__ void __launch_bounds__(kThreads) logprob_grad_kernel(const Grad<T> a)
     const bool none = sum == -INFINITY;
     auto one = [&](int64_t v) {
         const float q = none ? 0.0f : grad_of(value(x, v), sum, g, ge, h);
-        d[v] = static_cast<T>(v == y && !none ? q + g : q);
+        if (KQ_IN_RANGE(v, a.V)) d[v] = static_cast<T>(v == y && !none ? q + g : q);
     };
     if constexpr (VEC) {
         const int64_t head = min(a.V, static_cast<int64_t>((16 - (reinterpret_cast<uintptr_t>(x) & 15)) % 16 / sizeof(T)));
@@ -480,7 +480,7 @@ __global__ void __launch_bounds__(kThreads) logprob_grad_kernel(const Grad<T> a)
                     }
                     o = make_uint4(b[0], b[1], b[2], b[3]);
                 }
-                __stcs(dv + j, o);
+                if (KQ_IN_RANGE(head + j * E + E - 1, a.V)) __stcs(dv + j, o);
             }
         }
     } else {
