@@ -28,6 +28,8 @@ constexpr int kThreads = 256;             // of a block where there are rows for
 constexpr int kNarrow = 64, kMedium = 128; // of one for a row of less than kShortRow, kMiddleRow bytes
 constexpr int kShortRow = 12288, kMiddleRow = 98304;
 constexpr int kWide = 1024;               // where there are few rows
+constexpr int kSplit = 512;               // where there are two to an SM, or so few that a cluster takes a row
+constexpr int kCluster = 8, kSplitBytes = 32768;   // of that many blocks at most, with no less than that of the row each
 constexpr int kAhead = 4;                 // 16-byte loads of a thread in flight
 constexpr int kWideAhead = 8;             // of one in a block that has the SM to itself
 constexpr int kList = 1024;               // candidates for the top values
@@ -95,6 +97,13 @@ __device__ __forceinline__ V block_reduce(V v, V* tmp, F f) {
 }
 __device__ __forceinline__ float sum2(float a, float b) { return a + b; }
 
+__device__ __forceinline__ uint32_t remote_u32(const void* p, uint32_t rank) {
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(mapa_shared(smem_u32(p), rank)) : "memory");
+    return v;
+}
+__device__ __forceinline__ float remote_f32(const float* p, uint32_t rank) { return __uint_as_float(remote_u32(p, rank)); }
+
 // ln p of a logit; one masked with its type's lowest number would overflow in powers of two.
 __device__ __forceinline__ float logp_of(float x, float r2, float lz2) {
     return x < kFloor ? x - (r2 + lz2) * kLn2 : fminf(0.0f, (fmaf(x, kLog2e, -r2) - lz2) * kLn2);
@@ -155,18 +164,26 @@ __device__ __noinline__ void careful_row(const T* x, int64_t r, int64_t V, int64
     }
 }
 
-template <typename T, int NT>
-__global__ void __launch_bounds__(NT, NT == kWide ? 1 : 1536 / NT) logprob_kernel(const T* __restrict__ logits, int64_t V, int64_t ld,
-                                                                const int64_t* __restrict__ target, int top, Out out) {
+// SPLIT: a cluster takes a row, each block an equal run of `part` values of it.
+template <typename T, int NT, bool SPLIT>
+__global__ void __launch_bounds__(NT, NT >= kSplit ? 1 : 1536 / NT) logprob_kernel(const T* __restrict__ logits, int64_t row_len,
+                                                                                   int64_t ld, const int64_t* __restrict__ target,
+                                                                                   int top, Out out, int parts, int part) {
     constexpr int E = 16 / sizeof(T), kWarps = NT / 32, A = NT == kWide ? kWideAhead : kAhead;
-    __shared__ uint64_t tmp64[kWarps], list[kList];
-    __shared__ float tmp[2][kWarps][4];
+    __shared__ uint64_t tmp64[kWarps], list[kList], mine_top[KQ_LOGPROBS_MAX_TOP];
+    __shared__ __align__(16) float tmp[2][kWarps][4];
+    __shared__ float stat[4];   // this block's maximum, reference and sums, and
+    __shared__ int failed;      // whether its top values went past its lists: read by the row's other blocks
     __shared__ int groups[kGroups], n_groups, n_list;
     extern __shared__ uint16_t group_max[];   // [group of a thread][thread]: upper half of the maximum's order
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int64_t r = blockIdx.x;
-    const T* x = logits + r * ld;
+    const int rank = SPLIT ? static_cast<int>(cluster_ctarank()) : 0;
+    const int64_t r = SPLIT ? blockIdx.x / parts : blockIdx.x;
     const int64_t y = target[r];
+    const uint32_t base = SPLIT ? static_cast<uint32_t>(rank) * part : 0;   // this block's first value in the row
+    const T* const row = logits + r * ld;
+    const T* x = row + base;
+    const int64_t V = SPLIT ? max(static_cast<int64_t>(0), min(static_cast<int64_t>(part), row_len - base)) : row_len;
     // vectors of 16 bytes between the first and the last aligned address, and the few values around them
     const int head = static_cast<int>(min(V, static_cast<int64_t>((16 - (reinterpret_cast<uintptr_t>(x) & 15)) % 16 / sizeof(T))));
     const uint4* xv = reinterpret_cast<const uint4*>(x + head);
@@ -281,18 +298,44 @@ __global__ void __launch_bounds__(NT, NT == kWide ? 1 : 1536 / NT) logprob_kerne
         z += __shfl_xor_sync(0xffffffffu, z, o);
         w += __shfl_xor_sync(0xffffffffu, w, o);
     }
-    if (y >= V && tid == 0) record_error(out.info, -KQ_ERR_INVALID_ARG);
-    if (!(m > -kHuge && m < kHuge && z < INFINITY)) {   // false for a NaN in z
-        careful_row<T, NT>(x, r, V, y, top, out, tmp64);
+    float row_max = m;
+    if constexpr (SPLIT) {   // the row's, from its blocks' in order
+        if (tid == 0) {
+            stat[0] = m, stat[1] = r2, stat[2] = z, stat[3] = w;
+            failed = 0;
+        }
+        if (tid < KQ_LOGPROBS_MAX_TOP) mine_top[tid] = 0;
+        cluster_barrier();
+        float all_r2 = kFloor;
+        for (int i = 0; i < parts; ++i) {
+            row_max = fmaxf(row_max, remote_f32(&stat[0], i));
+            all_r2 = fmaxf(all_r2, remote_f32(&stat[1], i));
+        }
+        z = w = 0.0f;
+        for (int i = 0; i < parts; ++i) {
+            const float ri = remote_f32(&stat[1], i), zi = remote_f32(&stat[2], i), wi = remote_f32(&stat[3], i);
+            const float f = ri == kFloor ? 0.0f : ex2(ri - all_r2);
+            z += zi * f;   // a NaN stays one
+            if (f > 0.0f) w += f * fmaf(zi, ri - all_r2, wi);
+        }
+        r2 = all_r2;
+    }
+    if (y >= row_len && tid == 0 && rank == 0) record_error(out.info, -KQ_ERR_INVALID_ARG);
+    if (!(row_max > -kHuge && row_max < kHuge && z < INFINITY)) {   // false for a NaN in z
+        if constexpr (SPLIT) cluster_barrier();   // no block leaves while another reads its part of the row's sums
+        if (rank == 0) careful_row<T, NT>(row, r, row_len, y, top, out, tmp64);
         return;
     }
     const float lz2 = log2f(z);
-    if (tid == 0) {
-        out.logp[r] = y < 0 ? 0.0f : y >= V ? NAN : logp_of(value(x, y), r2, lz2);
+    if (tid == 0 && rank == 0) {
+        out.logp[r] = y < 0 ? 0.0f : y >= row_len ? NAN : logp_of(value(row, y), r2, lz2);
         if (out.entropy) out.entropy[r] = fmaxf(0.0f, (lz2 - w / z) * kLn2);
         if (out.lse) out.lse[r] = (r2 + lz2) * kLn2;
     }
-    if (top == 0) return;
+    if (top == 0) {
+        if constexpr (SPLIT) cluster_barrier();
+        return;
+    }
 
     // ---- the top values. A bound that at least `top` threads' maxima reach and not many more: bit by bit
     // from the first in which they differ, towards the top-th largest. With fewer threads than that, all
@@ -319,7 +362,7 @@ __global__ void __launch_bounds__(NT, NT == kWide ? 1 : 1536 / NT) logprob_kerne
         for (int g = 0; g < n_mine; ++g) {
             const uint32_t gm = group_max[g * NT + tid];
             const int first = g * A * NT + tid;   // its first vector
-            if (gm < bound_half || (gm == bound_half && static_cast<uint32_t>(head + first * E) > bound_index)) continue;
+            if (gm < bound_half || (gm == bound_half && base + static_cast<uint32_t>(head + first * E) > bound_index)) continue;
             const int at = atomicAdd(&n_groups, 1);
             if (at < kGroups) groups[at] = first;
         }
@@ -328,7 +371,7 @@ __global__ void __launch_bounds__(NT, NT == kWide ? 1 : 1536 / NT) logprob_kerne
             const int at = atomicAdd(&n_list, 1);
             if (at < kList) list[at] = k;
         };
-        if (my_edge >= 0) offer(rank_key(ev, static_cast<uint32_t>(my_edge)));
+        if (my_edge >= 0) offer(rank_key(ev, base + static_cast<uint32_t>(my_edge)));
         __syncthreads();
         if (n_groups <= kGroups) {
             for (int q = tid; q < n_groups * A; q += NT) {
@@ -339,24 +382,29 @@ __global__ void __launch_bounds__(NT, NT == kWide ? 1 : 1536 / NT) logprob_kerne
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     const uint32_t b = sizeof(T) == 4 ? w4[e % 4] : e & 1 ? w4[e / 2] & 0xFFFF0000u : w4[e / 2] << 16;
-                    offer(rank_key(__uint_as_float(b), static_cast<uint32_t>(head + at * E + e)));
+                    offer(rank_key(__uint_as_float(b), base + static_cast<uint32_t>(head + at * E + e)));
                 }
             }
         }
         __syncthreads();
         if (n_groups <= kGroups && n_list <= kList) break;
         if (pass == 1) {   // more near the bound than the lists hold
-            careful_row<T, NT>(x, r, V, y, top, out, tmp64);
-            return;
+            if constexpr (SPLIT) {
+                if (tid == 0) failed = 1;
+                break;
+            } else {
+                careful_row<T, NT>(row, r, row_len, y, top, out, tmp64);
+                return;
+            }
         }
         // Too many near the bound's value: the top-th largest of the threads' first largest values by value and index
         // (complements, the largest first; an index is below 2^20).
-        uint64_t key = my_edge >= 0 ? rank_key(ev, static_cast<uint32_t>(my_edge)) : 0;
+        uint64_t key = my_edge >= 0 ? rank_key(ev, base + static_cast<uint32_t>(my_edge)) : 0;
         for (int i = 0; i < A; ++i) {
             const int at = best_group * A * NT + tid + i * NT;
             if (at >= nvec) break;
             for (int e = 0; e < E; ++e)
-                key = max(key, rank_key(value(reinterpret_cast<const T*>(xv + at), e), static_cast<uint32_t>(head + at * E + e)));
+                key = max(key, rank_key(value(reinterpret_cast<const T*>(xv + at), e), base + static_cast<uint32_t>(head + at * E + e)));
         }
         bound = 0;
         for (int bit = 63; bit >= 0; --bit) {
@@ -369,30 +417,65 @@ __global__ void __launch_bounds__(NT, NT == kWide ? 1 : 1536 / NT) logprob_kerne
         }
         if (tid == 0) n_groups = n_list = 0;
     }
-    const int n = n_list;
+    int n = min(n_list, kList);
+    if constexpr (SPLIT) {   // the block's own top values, then those of all, by the row's first block
+        for (int c = tid; c < n; c += NT) {
+            int place = 0;
+            for (int i = 0; i < n; ++i) place += list[i] > list[c];
+            if (place < top) mine_top[place] = list[c];
+        }
+        cluster_barrier();
+        if (rank == 0) {
+            bool lost = false;
+            for (int i = 0; i < parts; ++i) lost |= remote_u32(&failed, i) != 0;
+            n = parts * top;
+            if (tid < n) {   // parts * top <= 8 * 32
+                const uint64_t* at = &mine_top[tid % top];
+                list[tid] = remote_u32(at, tid / top) | static_cast<uint64_t>(remote_u32(reinterpret_cast<const uint32_t*>(at) + 1, tid / top)) << 32;
+            }
+            if (lost) {
+                __syncthreads();
+                careful_row<T, NT>(row, r, row_len, y, top, out, tmp64);
+                n = 0;
+            }
+        }
+        cluster_barrier();
+        if (rank != 0) return;
+    }
     for (int c = tid; c < n; c += NT) {
-        const uint64_t k = list[c];
-        int rank = 0;
-        for (int i = 0; i < n; ++i) rank += list[i] > k;
-        if (rank < top && KQ_IN_RANGE(key_index(k), V)) {
-            out.top_id[r * top + rank] = static_cast<int32_t>(key_index(k));
-            out.top_logp[r * top + rank] = logp_of(key_value(k), r2, lz2);
+        const uint64_t key = list[c];
+        int place = 0;
+        for (int i = 0; i < n; ++i) place += list[i] > key;
+        if (place < top && key && KQ_IN_RANGE(key_index(key), row_len)) {
+            out.top_id[r * top + place] = static_cast<int32_t>(key_index(key));
+            out.top_logp[r * top + place] = logp_of(key_value(key), r2, lz2);
         }
     }
 }
 
-template <typename T, int NT>
+template <typename T, int NT, bool SPLIT = false>
 kq_status run_logprob(const T* logits, int64_t rows, int64_t V, int64_t ld, const int64_t* target, int top, const Out& out,
-                      cudaStream_t stream) {
+                      cudaStream_t stream, int parts = 1) {
+    // runs of whole vectors, so that they all lie to 16 bytes as their row does
+    const int64_t part = cdiv(cdiv(V, parts), 64) * 64;
     const int64_t group = (NT == kWide ? kWideAhead : kAhead) * NT * (16 / sizeof(T));   // values of a group of every thread
-    const size_t smem = top ? static_cast<size_t>(cdiv(V, group)) * NT * sizeof(uint16_t) : 0;
     static std::atomic<uint64_t> done{0};
     KQ_TRY(once_per_device(done, [&] {
-        KQ_CUDA(cudaFuncSetAttribute(logprob_kernel<T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+        KQ_CUDA(cudaFuncSetAttribute(logprob_kernel<T, NT, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                      static_cast<int>(cdiv(KQ_LOGPROBS_MAX_V, group) * NT * sizeof(uint16_t))));
         return KQ_OK;
     }));
-    logprob_kernel<T, NT><<<static_cast<unsigned>(rows), NT, smem, stream>>>(logits, V, ld, target, top, out);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(rows * parts));
+    cfg.blockDim = dim3(NT);
+    cfg.dynamicSmemBytes = top ? static_cast<size_t>(cdiv(SPLIT ? part : V, group)) * NT * sizeof(uint16_t) : 0;
+    cfg.stream = stream;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim = {static_cast<unsigned>(parts), 1, 1};
+    cfg.attrs = at;
+    cfg.numAttrs = SPLIT ? 1 : 0;
+    KQ_CUDA(cudaLaunchKernelEx(&cfg, logprob_kernel<T, NT, SPLIT>, logits, V, ld, target, top, out, parts, static_cast<int>(part)));
     return KQ_OK;
 }
 
@@ -400,8 +483,12 @@ template <typename T>
 kq_status pick_logprob(const T* x, int64_t rows, int64_t V, int64_t ld, const int64_t* target, int top, const Out& out,
                        cudaStream_t stream) {
     const int64_t bytes = V * static_cast<int64_t>(sizeof(T));
+    int parts = 1;   // blocks of a row, a power of two
+    while (parts < kCluster && rows * parts * 2 <= num_sms() && bytes >= kSplitBytes * 2 * parts) parts *= 2;
+    if (parts > 1) return run_logprob<T, kSplit, true>(x, rows, V, ld, target, top, out, stream, parts);
     if (bytes < kShortRow) return run_logprob<T, kNarrow>(x, rows, V, ld, target, top, out, stream);
-    if (rows <= 2 * num_sms()) return run_logprob<T, kWide>(x, rows, V, ld, target, top, out, stream);
+    if (rows <= num_sms()) return run_logprob<T, kWide>(x, rows, V, ld, target, top, out, stream);
+    if (rows <= 2 * num_sms()) return run_logprob<T, kSplit>(x, rows, V, ld, target, top, out, stream);
     if (bytes < kMiddleRow) return run_logprob<T, kMedium>(x, rows, V, ld, target, top, out, stream);
     return run_logprob<T, kThreads>(x, rows, V, ld, target, top, out, stream);
 }
@@ -545,7 +632,9 @@ extern "C" kq_status kq_token_logprobs(const void* logits, int dtype, int64_t T,
     // A row's joint steps take a block about as long as half a large row's values: many small blocks on an SM
     // cover them for each other, the smaller the shorter the row (V = 32000 bf16: 128 threads 202 us, 256 226 us;
     // V = 128000: 216 and 190 us; V = 4000: 64 threads 69 us, 128 78 us, 256 120 us, each 16384 rows but 4096
-    // of the largest); a block with the SM to itself is shorter with more threads.
+    // of the largest); blocks alone or in
+    // twos on an SM are shorter with more threads (300 rows of 128000 bf16 27 us with 1024, 20 us with 512), and a few rows
+    // with a cluster each (8 rows: 12.3 us with one block a row, 10.3 us with eight).
     const kq_status launched =
         dtype == KQ_BF16 ? pick_logprob(static_cast<const __nv_bfloat16*>(logits), T, V, ld, target, top, out, stream)
                          : pick_logprob(static_cast<const float*>(logits), T, V, ld, target, top, out, stream);
