@@ -482,10 +482,12 @@ def _cache(cache, table, dim: int) -> _KvCache:
     _need(table, "table", torch.int32)
     if cache.dim() != 3 or table.dim() != 2:
         raise ValueError("cache must be [pages, kv_heads, page * (dim + 8)], table [batch, pages of a sequence]")
-    if cache.shape[2] % (dim + 8):
-        raise ValueError(f"cache's last dimension must be page * (dim + 8) with dim = {dim}, got {cache.shape[2]}")
-    return _KvCache(cache.data_ptr(), table.data_ptr(), cache.shape[0], cache.shape[2] // (dim + 8), cache.shape[1], dim,
-                    table.shape[0], table.shape[1])
+    pages, heads, size = cache.shape
+    page, rest = divmod(size, dim + 8)
+    if rest:
+        raise ValueError(f"cache's last dimension must be page * (dim + 8) with dim = {dim}, got {size}")
+    batch, table_ld = table.shape
+    return _KvCache(cache.data_ptr(), table.data_ptr(), pages, page, heads, dim, batch, table_ld)
 
 
 _DTYPES = {torch.bfloat16: KQ_BF16, torch.float32: KQ_F32}
@@ -519,19 +521,29 @@ def kq_kv_append(k, v, start, lens, cache, table, lens_out=None, acc=None, pos=N
         raise ValueError("k and v must have one shape and type")
     _need(v, "v", k.dtype, contiguous=False)
     c = _cache(cache, table, k.shape[2])
-    B, S = c.batch, 0
-    _need(start, "start", torch.int32, (B + 1,))
-    for t, name in ((lens, "lens"), (lens_out, "lens_out"), (seen, "seen"), (seen_out, "seen_out")):
-        _need(t, name, torch.int32, (B,))
-    for t, name, ty in ((acc, "acc", torch.float32), (pos, "pos", torch.int32)):
-        if t is not None:
-            S = t.shape[-1]
-            _need(t, name, ty, (B, c.kv_heads, S))
-    if acc is not None and pos is not None and acc.shape != pos.shape:
-        raise ValueError("acc and pos must have one shape")
-    _need(info, "info", torch.int32)
-    _ok(lib().kq_kv_append(ctypes.byref(c), _ptr(k), _ptr(v), dtype, k.shape[0], k.stride(0), k.stride(1), v.stride(0),
-                           v.stride(1), _ptr(start), _ptr(lens), _ptr(lens_out), _ptr(acc), _ptr(pos), S, _ptr(seen),
+    one, S = (c.batch,), 0
+    _need(start, "start", torch.int32, (c.batch + 1,))
+    _need(lens, "lens", torch.int32, one)
+    if lens_out is not None:
+        _need(lens_out, "lens_out", torch.int32, one)
+    if seen is not None:
+        _need(seen, "seen", torch.int32, one)
+    if seen_out is not None:
+        _need(seen_out, "seen_out", torch.int32, one)
+    if acc is not None:
+        S = acc.shape[-1]
+        _need(acc, "acc", torch.float32, (c.batch, c.kv_heads, S))
+    if pos is not None:
+        if acc is not None and pos.shape != acc.shape:
+            raise ValueError("acc and pos must have one shape")
+        S = pos.shape[-1]
+        _need(pos, "pos", torch.int32, (c.batch, c.kv_heads, S))
+    if info is not None:
+        _need(info, "info", torch.int32)
+    k0, k1, _ = k.stride()
+    v0, v1, _ = v.stride()
+    _ok(lib().kq_kv_append(ctypes.byref(c), k.data_ptr(), v.data_ptr(), dtype, k.shape[0], k0, k1, v0, v1,
+                           _ptr(start), _ptr(lens), _ptr(lens_out), _ptr(acc), _ptr(pos), S, _ptr(seen),
                            _ptr(seen_out), _ptr(info), _stream(stream)), "kq_kv_append")
 
 
