@@ -80,7 +80,7 @@ struct Evict {
 template <bool ONE, bool FITS>
 __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const Evict e) {
     extern __shared__ uint32_t keys[];
-    __shared__ uint32_t hist[4][256], sum[256], picked[2], counts[6];   // a count for each digit: none is cleared while read
+    __shared__ uint32_t hist[4][256], sum[256], picked[3], counts[6];   // a count for each digit: none is cleared while read
     __shared__ uint64_t tmp[kWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = ONE ? 0 : static_cast<int>(cluster_ctarank()), ctas = ONE ? 1 : e.ctas;
@@ -99,16 +99,14 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const Evict e) {
     float* acc_out = e.acc_out + head * e.S;
     int32_t* pos_out = e.pos_out + head * e.S;
     const int first = rank * e.per, mine = max(0, min(e.per, n - first));   // first < 2^31: no further than S and a part
-    // the front's weights and positions, holes among them, where the arrays differ
-    auto copy_front = [&] {
-        const int end = min(mine, max(0, min(n, budget) - first));
-        for (int j = tid; j < end; j += kThreads) {
-            if (acc_out != acc) acc_out[first + j] = acc[first + j];
-            if (pos_out != pos) pos_out[first + j] = pos[first + j];
-        }
+    // the front's weights and positions, free slots among them, where the arrays differ
+    auto copy = [&](int j, float w, int32_t q) {
+        if (first + j >= budget) return;
+        if (acc_out != acc) acc_out[first + j] = w;
+        if (pos_out != pos) pos_out[first + j] = q;
     };
     if (n <= budget) {   // the whole cluster leaves
-        copy_front();
+        for (int j = tid; j < mine; j += kThreads) copy(j, acc[first + j], pos[first + j]);
         return;
     }
     const int from = static_cast<int>(max(static_cast<int64_t>(INT32_MIN), static_cast<int64_t>(e.seen[b]) - e.recent));
@@ -134,12 +132,18 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const Evict e) {
             for (int i = 0; i < 4; ++i) {
                 const uint32_t k = evict_key(w[i], q[i], from, e.sink);
                 keys[j + i * kThreads] = k;
+                copy(j + i * kThreads, w[i], q[i]);
                 note(k);
             }
         }
-        for (; j < held; j += kThreads) note(keys[j] = made(j));
-        if constexpr (!FITS)
-            for (; j < mine; j += kThreads) note(made(j));
+        for (; j < mine; j += kThreads) {
+            const float w = acc[first + j];
+            const int32_t q = pos[first + j];
+            const uint32_t k = evict_key(w, q, from, e.sink);
+            if (FITS || j < kKeys) keys[j] = k;
+            copy(j, w, q);
+            note(k);
+        }
     }
     low = __reduce_min_sync(0xffffffffu, low);
     high = __reduce_max_sync(0xffffffffu, high);
@@ -200,6 +204,7 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const Evict e) {
                 if (before < want && want <= before + v[i]) {
                     picked[0] = 255 - (lane * 8 + i);
                     picked[1] = before;
+                    picked[2] = v[i];
                 }
                 before += v[i];
             }
@@ -208,19 +213,26 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const Evict e) {
         prefix |= picked[0] << down;
         want -= picked[1];
     }
+    // slots equal to the threshold: all of them stay, unless the last bin held more than that
+    const bool tied = bits <= 0 || picked[2] != want;
     const uint32_t t = crowd ? 0xFFFFFFFFu : low + prefix;   // want: how many slots equal to it stay, the lowest
 
     // ---- ties before this CTA, then kept or not, slot by slot: a run of them to a thread
     const int run = (mine + kThreads - 1) / kThreads | 1;   // odd: neighbouring threads in different banks
     const int j0 = min(tid * run, mine), j1 = min(j0 + run, mine);
-    uint32_t eq = 0;
-    for (int j = j0; j < j1; ++j) eq += key(j) == t;
     uint64_t total;
-    uint32_t ties = static_cast<uint32_t>(block_scan(eq, tmp, total));
-    if constexpr (!ONE) {
-        if (tid == 0) counts[0] = static_cast<uint32_t>(total);
-        sync();
-        for (int r = 0; r < rank; ++r) ties += count_of(0, r);
+    uint32_t ties = 0;
+    if (tied) {
+        uint32_t eq = 0;
+        for (int j = j0; j < j1; ++j) eq += key(j) == t;
+        ties = static_cast<uint32_t>(block_scan(eq, tmp, total));
+        if constexpr (!ONE) {
+            if (tid == 0) counts[0] = static_cast<uint32_t>(total);
+            sync();
+            for (int r = 0; r < rank; ++r) ties += count_of(0, r);
+        }
+    } else {
+        want = 0xFFFFFFFFu;
     }
     uint32_t holes_here = 0, tails_here = 0, tie = ties;
     const int edge = budget - first;   // this CTA's slots below the budget
@@ -257,7 +269,6 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const Evict e) {
         if (j < edge && !keep && KQ_IN_RANGE(hole_at, budget)) hole[hole_at++] = first + j;
         if (j >= edge && keep && KQ_IN_RANGE(tail_at, budget)) tail[tail_at++] = first + j;
     }
-    copy_front();
     sync();   // the lists and the fronts are complete, and no counts are read any more
 
     // ---- the moves: a lane finds both places of one and takes its parameters, weight and position; then the warp
