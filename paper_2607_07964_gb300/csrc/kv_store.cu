@@ -72,42 +72,56 @@ struct Eight {
     }
 };
 
-// The codes rint((x - off) / s) of 8 values of each lane of a warp, float32 with IEEE division. The quotient is first
-// taken with a reciprocal; where the remainder shows it within 2^-17 of a tie (bf16 values often
-// sit on one) or the reciprocal y = div_recip(s) leaves the normal numbers, it is divided. Lanes without
-// `use` get anything.
-__device__ __forceinline__ uint32_t codes8(const float (&x)[8], float off, float s, float y, bool use) {
-    constexpr float kRound = 12582912.0f;   // 1.5 * 2^23: adding it rounds to a whole number
-    const float edge = !use ? INFINITY : y == 0.0f ? -1.0f : s * (0.5f - 0x1p-17f);
-    float r[8], d[8], most = 0.0f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        d[j] = __fsub_rn(x[j], off);
-        r[j] = __fsub_rn(__fmaf_rn(d[j], y, kRound), kRound);
-        most = fmaxf(most, fabsf(__fmaf_rn(-r[j], s, d[j])));
+// Two floats in one 64-bit register, and the packed operations on them.
+struct Two {
+    uint64_t v;
+    __device__ __forceinline__ Two() {}
+    __device__ __forceinline__ Two(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+    __device__ __forceinline__ void bits(uint32_t& a, uint32_t& b) const {
+        asm("mov.b64 {%0, %1}, %2;" : "=r"(a), "=r"(b) : "l"(v));
     }
-    uint32_t near = 0;
-    if (most >= edge) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (fabsf(__fmaf_rn(-r[j], s, d[j])) >= edge) near |= 1u << j;
+};
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(a.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return a;
+}
+__device__ __forceinline__ Two mul2(Two a, Two b) {
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(a.v) : "l"(a.v), "l"(b.v));
+    return a;
+}
+__device__ __forceinline__ Two add2(Two a, Two b) {
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(a.v) : "l"(a.v), "l"(b.v));
+    return a;
+}
+
+// What turns a row's values into codes: codes8 computes rint(RN(RN(x - off) / s)), RN being the rounding to
+// float32, from y = 1 / s. q = RN(d y) is a few units u in the last place off d / s, and the scale has 8 bits, so
+// q s and d are both whole multiples of u ulp(s): the remainder d - q s is one of a few hundred of them and exact. RN(q +
+// (d - q s) y) then rounds a number within 2^-20 u of d / s; the nearest that d / s can be to the middle between two
+// floats is 2^-9 u (d minus such a middle times s is such a multiple again, halved, and not 0: the
+// product would need 25 bits), so it rounds to RN(d / s), ties of the codes included. x, off and s
+// are multiplied by a power of two z that brings s between 2^-69 and 2^64, where nothing that can
+// reach a code other than 0 is lost below the normal numbers.
+struct Scaler {
+    Two z, off, s, y;   // z, -off z, -s z, 1 / (s z)
+    __device__ __forceinline__ Scaler(float o, float step) {
+        const float f = step < 0x1p-64f ? 0x1p64f : step > 0x1p64f ? 0x1p-64f : 1.0f, t = step * f, r = __frcp_rn(t);
+        z = Two(f, f), off = Two(-o * f, -o * f), s = Two(-t, -t), y = Two(r, r);
     }
-    while (__any_sync(0xffffffffu, near)) {   // one of a lane's at a time: few lanes have more than one
-        const int at = __ffs(near) - 1;
-        float q = 0.0f;
+};
+// The codes of 8 values, the first in the lowest bits; of a row with scale 0, infinities or NaN, anything.
+__device__ __forceinline__ uint32_t codes8(const float (&x)[8], const Scaler& g) {
+    constexpr float kRound = 12582912.0f;   // 1.5 * 2^23: adding it rounds to a whole number, in the lowest bits
+    uint32_t t[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) q = j == at ? d[j] : q;
-        q = fminf(fmaxf(rintf(__fdiv_rn(q, s)), 0.0f), 15.0f);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) r[j] = j == at ? q : r[j];
-        near &= near - 1;
+    for (int j = 0; j < 8; j += 2) {
+        const Two d = fma2(Two(x[j], x[j + 1]), g.z, g.off);
+        const Two q = mul2(d, g.y);
+        add2(fma2(fma2(q, g.s, d), g.y, q), Two(kRound, kRound)).bits(t[j], t[j + 1]);
     }
-    uint32_t half[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-        half[i] = __float_as_uint(fmaf(fmaf(fmaf(r[4 * i + 3], 16.0f, r[4 * i + 2]), 16.0f, r[4 * i + 1]), 16.0f, r[4 * i]) +
-                                  8388608.0f);
-    return __byte_perm(half[0], half[1], 0x5410);
+    const uint32_t even = __byte_perm(__byte_perm(t[0], t[2], 0x0040), __byte_perm(t[4], t[6], 0x0040), 0x5410);
+    const uint32_t odd = __byte_perm(__byte_perm(t[1], t[3], 0x0040), __byte_perm(t[5], t[7], 0x0040), 0x5410);
+    return even | odd << 4;
 }
 
 struct RowSource {
@@ -214,13 +228,13 @@ __global__ void __launch_bounds__(kThreads, VEC && sizeof(T) == 2 ? 4 : 3) kv_ap
             const uint32_t sb = (__float_as_uint(__fdiv_rn(__fsub_rn(hi, off), 15.0f)) + 0xFFFFu) & 0xFFFF0000u;
             const float s = __uint_as_float(sb);
             const bool fine = isfinite(hi) && isfinite(off) && isfinite(s), use = fine && s > 0.0f;
-            const float y = div_recip(s);
+            const Scaler grid(off, s);
 #pragma unroll
             for (int u = 0; u < kChunks; ++u) {
                 float x[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) x[j] = raw[u].get(j);
-                const uint32_t word = codes8(x, off, s, y, use);
+                const uint32_t word = codes8(x, grid);
                 if (h < h1 && KQ_IN_RANGE(reinterpret_cast<uint8_t*>(codes + 4 * u) - c.data, kv_pool_bytes(c) - 3)) codes[4 * u] = use ? word : 0u;
             }
             if (h < h1 && in_row == 0 && KQ_IN_RANGE(reinterpret_cast<uint8_t*>(params) - c.data, kv_pool_bytes(c) - 3))

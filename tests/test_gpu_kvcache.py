@@ -161,6 +161,36 @@ def test_append_rows_at_the_edges_of_the_grid(dtype):
     assert np.array_equal(got[10], rows[10]) and np.isnan(got[3:7]).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("power", [-126, -110, -70, -66, -30, 0, 40, 63, 67, 100, 120])
+def test_append_codes_near_ties_at_every_scale(dtype, power):
+    """Quotients on ties, a float to either side of them and anywhere, from the smallest scales to the largest: the
+    bytes are those of the defining operations."""
+    dim, n = 128, 96
+    rng = np.random.default_rng(power + 200)
+    x = np.zeros((n, dim), np.float32)
+    for i in range(n):
+        m = 1 if i % 3 == 0 else rng.integers(128, 256) / 128     # of the scale: 8 bits, or a power of two
+        codes = rng.integers(0, 31, dim) / 2
+        codes[:2] = 0, 15
+        row = (codes * m * 2.0**power).astype(np.float32)
+        side = np.where(rng.random(dim) < 0.5, np.float32(np.inf), np.float32(0))
+        near = np.nextafter(row, side).astype(np.float32)
+        far = (rng.random(dim) * 15 * m * 2.0**power).astype(np.float32)
+        x[i] = np.where(codes == 15, row, np.choose(rng.integers(0, 3, dim), [row, near, far]))
+        x[i, :2] = 0, row[1]
+        if i % 4 == 1:   # an offset of about the range: values lose bits to it
+            x[i] += np.float32(-7.37 * 2.0**power)
+    x = _rounded(x, dtype)[:, None]
+    cache = _pool(1, n, 16, 1, dim, rng)
+    dc, dt = _to_dev(cache)
+    K().kq_kv_append(x.to(DEV), x.to(DEV), _i32([0, n]), _i32([0]), dc, dt)
+    for j in range(n):
+        for which in range(2):
+            cache.put(0, 0, j, which, x[j, 0].float().numpy())
+    assert np.array_equal(dc.cpu().numpy(), cache.data)
+
+
 def test_append_and_read_record_what_has_no_slot():
     rng = np.random.default_rng(1)
     cache = _pool(2, 32, 16, 2, 64, rng)
