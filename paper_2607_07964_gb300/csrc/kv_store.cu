@@ -6,11 +6,15 @@
 // rounding of s costs at most 2^-8 of the step, in exchange for 4 bytes of parameters a row
 // instead of 8 (D = 128: 68 bytes a row, 4.25 bits a value).
 //
-// Both are bound by memory: append reads 2 D e and writes D + 8 bytes for each token and head
-// (e bytes a value), read the reverse. A warp takes a token and a few of its heads, so that sequence,
-// slot and page are looked up once for all of them. To append, four lanes take a row, so that what a
-// row costs once (two bounds, two divisions) is shared by 32 values of a lane (16 lanes a row spent
-// 2.5 times the time on it); to read, D / 8 lanes, a word of codes each, as there is nothing to share.
+// Append reads 2 D e and writes D + 8 bytes for each token and head (e bytes a value), read the reverse. To
+// append, a warp takes 8 consecutive tokens and, one after the other, the key and value rows of a few heads: a token's
+// sequence, slot and page are looked up once for all of them, 8 parameters or positions fill a sector, and few heads
+// leave no lane idle (a warp to a token with its heads side by side: 41 instead of 14 us for 51k tokens of one head, 43
+// instead of 35 for four). Four lanes take a row, so that what a row costs once (two bounds, a division, a
+// reciprocal) is shared by 32 values of a lane. 51k tokens of 8 heads, D = 128, take 61 us in bf16 (0.64 of the measured
+// copy rate; about 420 instructions for 8 rows and the latency of their loads) and 85 us in fp32 (0.82). Copying the
+// rows ahead into shared memory was slower (82 and 125 us), prefetching them into L2 no faster. To read, a
+// warp takes a token and D / 8 lanes a row, a word of codes each, as there is nothing to share.
 #include <algorithm>
 
 #include "kv_common.cuh"
@@ -49,21 +53,22 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// 8 consecutive values as they are loaded. VEC: 16 bytes at a time (the caller checked base and strides).
+// 16 consecutive values as they are loaded. VEC: 16 bytes at a time (the caller checked base and strides; 32 at a
+// time were slower, 86 against 85 us for 51k tokens of 8 heads in fp32, 63 against 61 in bf16).
 template <typename T, bool VEC>
-struct Eight {
-    uint32_t w[VEC && sizeof(T) == 2 ? 4 : 8];
+struct Sixteen {
+    uint32_t w[VEC && sizeof(T) == 2 ? 8 : 16];
 
     __device__ __forceinline__ void load(const T* p) {
         if constexpr (VEC) {
 #pragma unroll
-            for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) {
+            for (int i = 0; i < static_cast<int>(sizeof(T)); ++i) {
                 const uint4 u = __ldcs(reinterpret_cast<const uint4*>(p) + i);
                 w[4 * i] = u.x, w[4 * i + 1] = u.y, w[4 * i + 2] = u.z, w[4 * i + 3] = u.w;
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(static_cast<float>(p[i]));
+            for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(static_cast<float>(p[i]));
         }
     }
     __device__ __forceinline__ float get(int i) const {
@@ -95,7 +100,8 @@ __device__ __forceinline__ Two add2(Two a, Two b) {
 }
 
 // What turns a row's values into codes: codes8 computes rint(RN(RN(x - off) / s)), RN being the rounding to
-// float32, from y = 1 / s. q = RN(d y) is a few units u in the last place off d / s, and the scale has 8 bits, so
+// float32, from y, about 1 / s, without a division or a branch (51k tokens of 8 heads, bf16: 63 us; with divisions where a
+// reciprocal came near a tie 100 us). q = RN(d y) is a few units u in the last place off d / s, and the scale has 8 bits, so
 // q s and d are both whole multiples of u ulp(s): the remainder d - q s is one of a few hundred of them and exact. RN(q +
 // (d - q s) y) then rounds a number within 2^-20 u of d / s; the nearest that d / s can be to the middle between two
 // floats is 2^-9 u (d minus such a middle times s is such a multiple again, halved, and not 0: the
@@ -103,9 +109,11 @@ __device__ __forceinline__ Two add2(Two a, Two b) {
 // are multiplied by a power of two z that brings s between 2^-69 and 2^64, where nothing that can
 // reach a code other than 0 is lost below the normal numbers.
 struct Scaler {
-    Two z, off, s, y;   // z, -off z, -s z, 1 / (s z)
+    Two z, off, s, y;   // z, -off z, -s z, about 1 / (s z)
     __device__ __forceinline__ Scaler(float o, float step) {
-        const float f = step < 0x1p-64f ? 0x1p64f : step > 0x1p64f ? 0x1p-64f : 1.0f, t = step * f, r = __frcp_rn(t);
+        const float f = step < 0x1p-64f ? 0x1p64f : step > 0x1p64f ? 0x1p-64f : 1.0f, t = step * f;
+        float r;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(t));   // within a unit in the last place
         z = Two(f, f), off = Two(-o * f, -o * f), s = Two(-t, -t), y = Two(r, r);
     }
 };
@@ -129,10 +137,10 @@ struct RowSource {
     int64_t token[2], head[2];      // strides in elements
 };
 
-// How many heads of a token a warp takes, at most: kBatch at a time.
-constexpr int kBatch = 4;
+constexpr int kRun = 8;     // consecutive tokens of a warp of append, one row of each at a time
+constexpr int kBatch = 4;   // heads of a token that a warp of read takes at a time
 
-// A warp's token: its sequence, slot and the granule rows of head 0, or none.
+// A token's place: its sequence, slot and the granule of head 0, or none.
 struct Token {
     int b, t;            // sequence (-1: none), token in the granule
     int64_t slot;
@@ -153,7 +161,7 @@ __global__ void __launch_bounds__(kThreads, VEC && sizeof(T) == 2 ? 4 : 3) kv_ap
                                                              const int32_t* __restrict__ lens, int32_t* lens_out,
                                                              float* __restrict__ acc, int32_t* __restrict__ pos, int64_t S,
                                                              const int32_t* __restrict__ seen, int32_t* seen_out, int* info) {
-    constexpr int kChunks = D / 32;   // of 8 values, to each of a row's four lanes
+    constexpr int kChunks = D / 64;   // of 16 values, to each of a row's four lanes
     const int64_t cap = kv_capacity(c);
     if (blockIdx.x == 0) {
         for (int b = threadIdx.x; b < c.batch; b += kThreads) {
@@ -165,52 +173,44 @@ __global__ void __launch_bounds__(kThreads, VEC && sizeof(T) == 2 ? 4 : 3) kv_ap
         }
         if (threadIdx.x == 0 && (start[0] != 0 || start[c.batch] != tokens)) record_error(info, -KQ_ERR_INVALID_ARG);
     }
-    const int lane = threadIdx.x & 31, in_row = lane & 3, which = (lane >> 2) & 1, in_batch = lane >> 3;
+    const int lane = threadIdx.x & 31, in_row = lane & 3;
     const int head_bytes = c.page * (D + 8);
-    const int64_t stride = src.head[which];
-    const int64_t warps = static_cast<int64_t>(gridDim.x) * (kThreads / 32);
-    for (int64_t item = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5); item < tokens * groups;
-         item += warps) {
-        const int64_t i = groups == 1 ? item : item / groups;
-        const int h0 = static_cast<int>(item - i * groups) * per, h1 = min(h0 + per, c.kv_heads);
-        const int b = kv_sequence_of_warp(start, c.batch, i);
-        if (b < 0) continue;   // recorded by the first block
-        const int64_t n = kv_length(lens, b, cap, info);
-        const int64_t index = i - start[b];
-        const Token k = locate(c, b, n + index, cap);
-        if (!k.g) {
-            record_error(info, -KQ_ERR_INVALID_ARG);
-            continue;
-        }
-        if (acc || pos) {
-            if (k.slot < S) {
-                for (int h = h0 + lane; h < h1; h += 32) {
-                    const int64_t at = (static_cast<int64_t>(b) * c.kv_heads + h) * S + k.slot;
-                    if (!KQ_IN_RANGE(at, static_cast<int64_t>(c.batch) * c.kv_heads * S)) continue;
-                    if (acc) acc[at] = 0.0f;
-                    if (pos) pos[at] = static_cast<int32_t>((seen ? seen[b] : n) + index);
-                }
-            } else {
-                record_error(info, -KQ_ERR_INVALID_ARG);
-            }
-        }
-        // lane in_row of a row takes its values 8 in_row + 32 i ..
-        const T* p = static_cast<const T*>(src.p[which]) + i * src.token[which] + in_row * 8;
-        uint8_t* const at = k.g + (h0 + in_batch) * static_cast<int64_t>(head_bytes);
-        uint32_t* codes = reinterpret_cast<uint32_t*>(at + kv_code_at(D, which, k.t)) + in_row;
-        uint32_t* params = reinterpret_cast<uint32_t*>(at + kv_param_at(D, which, k.t));
-        for (int hb = h0; hb < h1; hb += kBatch) {   // all lanes go along; rows past the last head are not written
-            const int h = hb + in_batch;
-            const T* row = p + min(h, h1 - 1) * stride;
-            Eight<T, VEC> raw[kChunks];
+    const int64_t warps = static_cast<int64_t>(gridDim.x) * (kThreads / 32), items = (tokens + kRun - 1) / kRun * groups;
+    for (int64_t item = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5); item < items; item += warps) {
+        const int64_t turn = groups == 1 ? item : item / groups, i = turn * kRun + (lane >> 2);   // the lane's token
+        const int u0 = static_cast<int>(item - turn * groups) * per, u1 = min(u0 + per, 2 * c.kv_heads);
+        // lane in_row of a row takes its values 16 in_row + 64 u ..; the first rows are asked for before their place is known
+        const int64_t in = min(i, tokens - 1);
+        Sixteen<T, VEC> raw[kChunks];
+        auto load = [&](int unit) {
+            const int which = unit & 1;
+            const T* row = static_cast<const T*>(src.p[which]) + in * src.token[which] + (unit >> 1) * src.head[which] + in_row * 16;
 #pragma unroll
-            for (int u = 0; u < kChunks; ++u) raw[u].load(row + 32 * u);
+            for (int u = 0; u < kChunks; ++u) raw[u].load(row + 64 * u);
+        };
+        load(u0);
+        const int b = i < tokens ? kv_sequence_of(start, c.batch, i) : -1;
+        Token k = {-1, 0, 0, nullptr};   // b < 0 is recorded by the first block
+        int32_t at_pos = 0;
+        if (b >= 0) {
+            const int64_t n = kv_length(lens, b, cap, info), index = i - start[b];
+            k = locate(c, b, n + index, cap);
+            if (!k.g || ((acc || pos) && k.slot >= S)) record_error(info, -KQ_ERR_INVALID_ARG);
+            if (pos) at_pos = static_cast<int32_t>((seen ? seen[b] : n) + index);
+        }
+        const bool there = k.g != nullptr;
+        for (int unit = u0; unit < u1; ++unit) {   // all lanes go along; what has no place is not written
+            const int which = unit & 1, h = unit >> 1;
+            if (unit > u0) load(unit);
+            uint8_t* const at = k.g + h * static_cast<int64_t>(head_bytes);
+            uint2* const codes = reinterpret_cast<uint2*>(at + kv_code_at(D, which, k.t)) + in_row;
+            uint32_t* const params = reinterpret_cast<uint32_t*>(at + kv_param_at(D, which, k.t));
             // a NaN among the values stays in both
             float lo = raw[0].get(0), hi = lo;
 #pragma unroll
             for (int u = 0; u < kChunks; ++u)
 #pragma unroll
-                for (int j = 0; j < 8; j += 2) {
+                for (int j = 0; j < 16; j += 2) {
                     const float x = raw[u].get(j), z = raw[u].get(j + 1);
                     asm("min.NaN.f32 %0, %0, %1, %2;" : "+f"(lo) : "f"(x), "f"(z));
                     asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(hi) : "f"(x), "f"(z));
@@ -225,22 +225,32 @@ __global__ void __launch_bounds__(kThreads, VEC && sizeof(T) == 2 ? 4 : 3) kv_ap
             const uint32_t lb = __float_as_uint(lo);
             const uint32_t ob = (lb + ((lb >> 31) ? 0xFFFFu : 0u)) & 0xFFFF0000u;
             const float off = __uint_as_float(ob);
-            const uint32_t sb = (__float_as_uint(__fdiv_rn(__fsub_rn(hi, off), 15.0f)) + 0xFFFFu) & 0xFFFF0000u;
+            const uint32_t qb = __float_as_uint(__fdiv_rn(__fsub_rn(hi, off), 15.0f)), sb = (qb + 0xFFFFu) & 0xFFFF0000u;
             const float s = __uint_as_float(sb);
-            const bool fine = isfinite(hi) && isfinite(off) && isfinite(s), use = fine && s > 0.0f;
+            const bool fine = qb <= 0x7F7F0000u, use = fine && sb;   // not NaN, not infinite, nor to become so
             const Scaler grid(off, s);
 #pragma unroll
             for (int u = 0; u < kChunks; ++u) {
-                float x[8];
+                uint32_t word[2];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = raw[u].get(j);
-                const uint32_t word = codes8(x, grid);
-                if (h < h1 && KQ_IN_RANGE(reinterpret_cast<uint8_t*>(codes + 4 * u) - c.data, kv_pool_bytes(c) - 3)) codes[4 * u] = use ? word : 0u;
+                for (int v = 0; v < 2; ++v) {
+                    float x[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[j] = raw[u].get(8 * v + j);
+                    word[v] = use ? codes8(x, grid) : 0u;
+                }
+                if (there && KQ_IN_RANGE(reinterpret_cast<uint8_t*>(codes + 4 * u) - c.data, kv_pool_bytes(c) - 7))
+                    codes[4 * u] = make_uint2(word[0], word[1]);
             }
-            if (h < h1 && in_row == 0 && KQ_IN_RANGE(reinterpret_cast<uint8_t*>(params) - c.data, kv_pool_bytes(c) - 3))
-                *params = fine ? (sb >> 16) | ob : 0x7FC07FC0u;
-            codes += kBatch * static_cast<int64_t>(head_bytes) / 4;
-            params += kBatch * static_cast<int64_t>(head_bytes) / 4;
+            if (there && in_row == 0) {
+                if (KQ_IN_RANGE(reinterpret_cast<uint8_t*>(params) - c.data, kv_pool_bytes(c) - 3))
+                    *params = fine ? (sb >> 16) | ob : 0x7FC07FC0u;
+                const int64_t slot = (static_cast<int64_t>(b) * c.kv_heads + h) * S + k.slot;
+                if (which == 0 && k.slot < S && KQ_IN_RANGE(slot, static_cast<int64_t>(c.batch) * c.kv_heads * S)) {
+                    if (acc) acc[slot] = 0.0f;
+                    if (pos) pos[slot] = at_pos;
+                }
+            }
         }
     }
 }
@@ -352,11 +362,17 @@ extern "C" kq_status kq_kv_append(const kq_kv_cache* cache, const void* k, const
     bool vec = true;
     for (int w = 0; w < 2; ++w)
         vec = vec && !(reinterpret_cast<uintptr_t>(src.p[w]) & 15u) && !((src.token[w] * es) & 15u) && !((src.head[w] * es) & 15u);
-    const Cut by = cut(T, c.kv_heads);
+    // four units to a warp, unless that leaves SMs without work: for 51k tokens of 8 heads, bf16, 61 us (one: 78, two: 66, eight
+    // and sixteen: 62 and 70); of 2 heads, where the rule takes two, 21 us (one: 24, four: 22)
+    const int64_t runs = cdiv(T, kRun), units = 2 * c.kv_heads;
+    const int per = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(4, runs * units / (num_sms() * 64))));
+    const int groups = static_cast<int>(cdiv(units, per));
+    const unsigned grid = static_cast<unsigned>(std::max<int64_t>(
+        1, std::min<int64_t>(cdiv(runs * groups, kThreads / 32), static_cast<int64_t>(num_sms()) * 16)));
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
-#define KQ_APPEND(TY, DIM, VEC) \
-    kv_append_kernel<TY, DIM, VEC><<<by.grid, kThreads, 0, stream>>>(c, src, T, by.groups, by.per, start, lens, lens_out, acc, pos, S, \
-                                                                      seen, seen_out, info)
+#define KQ_APPEND(TY, DIM, VEC)                                                                                            \
+    kv_append_kernel<TY, DIM, VEC><<<grid, kThreads, 0, stream>>>(c, src, T, groups, per, start, lens, lens_out, acc, pos, S, \
+                                                                  seen, seen_out, info)
     if (dtype == KQ_BF16) {
         if (c.dim == 128) vec ? KQ_APPEND(__nv_bfloat16, 128, true) : KQ_APPEND(__nv_bfloat16, 128, false);
         else vec ? KQ_APPEND(__nv_bfloat16, 64, true) : KQ_APPEND(__nv_bfloat16, 64, false);
