@@ -14,7 +14,7 @@
 // reciprocal) is shared by 32 values of a lane. 51k tokens of 8 heads, D = 128, take 61 us in bf16 (0.64 of the measured
 // copy rate; about 420 instructions for 8 rows and the latency of their loads) and 85 us in fp32 (0.82). Copying the
 // rows ahead into shared memory was slower (82 and 125 us), prefetching them into L2 no faster. To read, a
-// warp takes a token and D / 8 lanes a row, a word of codes each, as there is nothing to share.
+// warp takes a token (of one or two heads, several) and D / 8 lanes a row, a word of codes each, as there is nothing to share.
 #include <algorithm>
 
 #include "kv_common.cuh"
@@ -255,7 +255,9 @@ __global__ void __launch_bounds__(kThreads, VEC && sizeof(T) == 2 ? 4 : 3) kv_ap
     }
 }
 
-template <typename T, int D>
+// SHIFT: 1 << SHIFT tokens to a warp at a time, fewer heads of each. Otherwise few heads leave lanes
+// idle: 51k tokens of one head in 11 instead of 20 us, of two in 18 instead of 23.
+template <typename T, int D, int SHIFT>
 __global__ void __launch_bounds__(kThreads) kv_read_kernel(KvView c, int groups, int per, const int32_t* __restrict__ start,
                                                            const int32_t* __restrict__ first,
                                                            const int32_t* __restrict__ lens, int64_t tokens,
@@ -264,39 +266,51 @@ __global__ void __launch_bounds__(kThreads) kv_read_kernel(KvView c, int groups,
     const int lane = threadIdx.x & 31, in_row = lane % kLanes, sub = lane / kLanes, which = sub & 1;
     const int64_t cap = kv_capacity(c);
     const int64_t warps = static_cast<int64_t>(gridDim.x) * (kThreads / 32);
-    for (int64_t item = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5); item < tokens * groups;
-         item += warps) {
-        const int64_t i = groups == 1 ? item : item / groups;
-        const int h0 = static_cast<int>(item - i * groups) * per, h1 = min(h0 + per, c.kv_heads);
-        const int b = kv_sequence_of_warp(start, c.batch, i);
+    constexpr int kSide = kBatch >> SHIFT;   // heads of a token at a time
+    const int64_t items = ((tokens + (1 << SHIFT) - 1) >> SHIFT) * groups;
+    for (int64_t item = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5); item < items; item += warps) {
+        const int64_t turn = groups == 1 ? item : item / groups, i0 = turn << SHIFT;
+        const int h0 = static_cast<int>(item - turn * groups) * per, h1 = min(h0 + per, c.kv_heads);
+        // a lane looks up one of the tokens
+        const int64_t i = SHIFT ? i0 + (lane & ((1 << SHIFT) - 1)) : i0;
+        int b = -1;
+        if (SHIFT == 0) b = kv_sequence_of_warp(start, c.batch, i);
+        else if (i < tokens) b = kv_sequence_of(start, c.batch, i);
         Token k = {-1, 0, 0, nullptr};
         if (b >= 0) {
             const int64_t n = lens ? kv_length(lens, b, cap, info) : cap;
             k = locate(c, b, (first ? first[b] : 0) + (i - start[b]), n);
             if (k.slot < 0 || (k.slot < n && !k.g)) record_error(info, -KQ_ERR_INVALID_ARG);
         }
-        T* out = (which ? v_out : k_out) + i * c.kv_heads * D + in_row * 8;
-        for (int hb = h0; hb < h1; hb += kBatch) {
+        T* out = (which ? v_out : k_out) + i0 * c.kv_heads * D + in_row * 8;
+        for (int hb = h0; hb < h1; hb += kSide) {
             uint32_t word[kRounds], prm[kRounds];
 #pragma unroll
             for (int u = 0; u < kRounds; ++u) {
-                const int h = hb + u * (kRowsAtOnce / 2) + (sub >> 1);
+                const int at = u * (kRowsAtOnce / 2) + (sub >> 1), of = at >> (2 - SHIFT), h = hb + (SHIFT ? at & (kSide - 1) : at);
+                const uint8_t* g = k.g;
+                int t = k.t;
+                if (SHIFT) {
+                    g = reinterpret_cast<const uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(k.g), of));
+                    t = __shfl_sync(0xffffffffu, k.t, of);
+                }
                 word[u] = prm[u] = 0;
-                if (k.g && h < h1) {
-                    const uint8_t* g = k.g + h * kv_head_bytes(c);
-                    word[u] = reinterpret_cast<const uint32_t*>(g + kv_code_at(D, which, k.t))[in_row];
-                    prm[u] = *reinterpret_cast<const uint32_t*>(g + kv_param_at(D, which, k.t));
+                if (g && h < h1) {
+                    g += h * kv_head_bytes(c);
+                    word[u] = reinterpret_cast<const uint32_t*>(g + kv_code_at(D, which, t))[in_row];
+                    prm[u] = *reinterpret_cast<const uint32_t*>(g + kv_param_at(D, which, t));
                 }
             }
 #pragma unroll
             for (int u = 0; u < kRounds; ++u) {
-                const int h = hb + u * (kRowsAtOnce / 2) + (sub >> 1);
-                if (h >= h1) continue;
+                const int at = u * (kRowsAtOnce / 2) + (sub >> 1), h = hb + (SHIFT ? at & (kSide - 1) : at);
+                const int of = at >> (2 - SHIFT);
+                if (h >= h1 || (SHIFT && i0 + of >= tokens)) continue;
                 const float s = kv_scale(prm[u]), off = kv_offset(prm[u]);   // 0 where there is nothing to read
                 float x[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) x[j] = fmaf(s, static_cast<float>((word[u] >> (4 * j)) & 15u), off);
-                T* dst = out + static_cast<int64_t>(h) * D;
+                T* dst = out + static_cast<int64_t>(SHIFT ? of * c.kv_heads + h : h) * D;
                 if (!KQ_IN_RANGE(dst - (which ? v_out : k_out), tokens * c.kv_heads * D - 7)) continue;
                 if constexpr (sizeof(T) == 2) {
                     uint32_t w[4];
@@ -400,13 +414,21 @@ extern "C" kq_status kq_kv_read(const kq_kv_cache* cache, const int32_t* start, 
         return KQ_ERR_INVALID_ARG;
     }
     if (T == 0) return KQ_OK;
-    const Cut by = cut(T, c.kv_heads);
+    const int shift = c.kv_heads == 1 ? 2 : c.kv_heads == 2 ? 1 : 0;
+    const Cut by = cut((T + (1 << shift) - 1) >> shift, c.kv_heads);
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
-#define KQ_READ(TY, DIM)                                                                                         \
-    kv_read_kernel<TY, DIM><<<by.grid, kThreads, 0, stream>>>(c, by.groups, by.per, start, first, lens, T, static_cast<TY*>(k), \
-                                                              static_cast<TY*>(v), info)
-    if (dtype == KQ_BF16) c.dim == 128 ? KQ_READ(__nv_bfloat16, 128) : KQ_READ(__nv_bfloat16, 64);
-    else c.dim == 128 ? KQ_READ(float, 128) : KQ_READ(float, 64);
+#define KQ_READ_BY(TY, DIM, SHIFT)                                                                                             \
+    kv_read_kernel<TY, DIM, SHIFT><<<by.grid, kThreads, 0, stream>>>(c, by.groups, by.per, start, first, lens, T, \
+                                                                     static_cast<TY*>(k), static_cast<TY*>(v), info)
+#define KQ_READ(TY, DIM) shift == 0 ? KQ_READ_BY(TY, DIM, 0) : shift == 1 ? KQ_READ_BY(TY, DIM, 1) : KQ_READ_BY(TY, DIM, 2)
+    if (dtype == KQ_BF16) {
+        if (c.dim == 128) KQ_READ(__nv_bfloat16, 128);
+        else KQ_READ(__nv_bfloat16, 64);
+    } else {
+        if (c.dim == 128) KQ_READ(float, 128);
+        else KQ_READ(float, 64);
+    }
+#undef KQ_READ_BY
 #undef KQ_READ
     KQ_LAUNCH_CHECK("kv_read_kernel");
     return KQ_OK;
