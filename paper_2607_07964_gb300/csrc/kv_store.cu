@@ -11,8 +11,8 @@
 // sequence, slot and page are looked up once for all of them, 8 parameters or positions fill a sector, and few heads
 // leave no lane idle (a warp to a token with its heads side by side: 41 instead of 14 us for 51k tokens of one head, 43
 // instead of 35 for four). Four lanes take a row, so that what a row costs once (two bounds, a division, a
-// reciprocal) is shared by 32 values of a lane. 51k tokens of 8 heads, D = 128, take 61 us in bf16 (0.64 of the measured
-// copy rate; about 420 instructions for 8 rows and the latency of their loads) and 85 us in fp32 (0.82). Copying the
+// reciprocal) is shared by 32 values of a lane. 51k tokens of 8 heads, D = 128, take 58 us in bf16 (0.69 of the measured
+// copy rate; bound by instructions and the latency of the loads) and 81 us in fp32 (0.88). Copying the
 // rows ahead into shared memory was slower (82 and 125 us), prefetching them into L2 no faster. To read, a
 // warp takes a token (of one or two heads, several) and D / 8 lanes a row, a word of codes each, as there is nothing to share.
 #include <algorithm>
@@ -54,7 +54,7 @@ namespace {
 constexpr int kThreads = 256;
 
 // 16 consecutive values as they are loaded. VEC: 16 bytes at a time (the caller checked base and strides; 32 at a
-// time were slower, 86 against 85 us for 51k tokens of 8 heads in fp32, 63 against 61 in bf16).
+// time were 1 to 2 us slower for 51k tokens of 8 heads).
 template <typename T, bool VEC>
 struct Sixteen {
     uint32_t w[VEC && sizeof(T) == 2 ? 8 : 16];
@@ -100,8 +100,8 @@ __device__ __forceinline__ Two add2(Two a, Two b) {
 }
 
 // What turns a row's values into codes: codes8 computes rint(RN(RN(x - off) / s)), RN being the rounding to
-// float32, from y, about 1 / s, without a division or a branch (51k tokens of 8 heads, bf16: 63 us; with divisions where a
-// reciprocal came near a tie 100 us). q = RN(d y) is a few units u in the last place off d / s, and the scale has 8 bits, so
+// float32, from y, about 1 / s, without a division or a branch (51k tokens of 8 heads, bf16: 100 -> 63 us against
+// divisions where a reciprocal came near a tie). q = RN(d y) is a few units u in the last place off d / s, and the scale has 8 bits, so
 // q s and d are both whole multiples of u ulp(s): the remainder d - q s is one of a few hundred of them and exact. RN(q +
 // (d - q s) y) then rounds a number within 2^-20 u of d / s; the nearest that d / s can be to the middle between two
 // floats is 2^-9 u (d minus such a middle times s is such a multiple again, halved, and not 0: the
@@ -181,14 +181,12 @@ __global__ void __launch_bounds__(kThreads, VEC && sizeof(T) == 2 ? 4 : 3) kv_ap
         const int u0 = static_cast<int>(item - turn * groups) * per, u1 = min(u0 + per, 2 * c.kv_heads);
         // lane in_row of a row takes its values 16 in_row + 64 u ..; the first rows are asked for before their place is known
         const int64_t in = min(i, tokens - 1);
+        const T* const key = static_cast<const T*>(src.p[0]) + in * src.token[0] + in_row * 16;
+        const T* const value = static_cast<const T*>(src.p[1]) + in * src.token[1] + in_row * 16;
         Sixteen<T, VEC> raw[kChunks];
-        auto load = [&](int unit) {
-            const int which = unit & 1;
-            const T* row = static_cast<const T*>(src.p[which]) + in * src.token[which] + (unit >> 1) * src.head[which] + in_row * 16;
+        auto row_of = [&](int unit) { return unit & 1 ? value + (unit >> 1) * src.head[1] : key + (unit >> 1) * src.head[0]; };
 #pragma unroll
-            for (int u = 0; u < kChunks; ++u) raw[u].load(row + 64 * u);
-        };
-        load(u0);
+        for (int u = 0; u < kChunks; ++u) raw[u].load(row_of(u0) + 64 * u);
         const int b = i < tokens ? kv_sequence_of(start, c.batch, i) : -1;
         Token k = {-1, 0, 0, nullptr};   // b < 0 is recorded by the first block
         int32_t at_pos = 0;
@@ -199,12 +197,15 @@ __global__ void __launch_bounds__(kThreads, VEC && sizeof(T) == 2 ? 4 : 3) kv_ap
             if (pos) at_pos = static_cast<int32_t>((seen ? seen[b] : n) + index);
         }
         const bool there = k.g != nullptr;
+        uint8_t* const codes0 = k.g + kv_code_at(D, 0, k.t) + in_row * 8;   // of head 0's key
+        const int params0 = kv_param_at(D, 0, k.t) - kv_code_at(D, 0, k.t) - in_row * 8;
+        const int64_t slot0 = static_cast<int64_t>(b) * c.kv_heads * S + k.slot;
         for (int unit = u0; unit < u1; ++unit) {   // all lanes go along; what has no place is not written
             const int which = unit & 1, h = unit >> 1;
-            if (unit > u0) load(unit);
-            uint8_t* const at = k.g + h * static_cast<int64_t>(head_bytes);
-            uint2* const codes = reinterpret_cast<uint2*>(at + kv_code_at(D, which, k.t)) + in_row;
-            uint32_t* const params = reinterpret_cast<uint32_t*>(at + kv_param_at(D, which, k.t));
+            const T* const next = row_of(min(unit + 1, u1 - 1));
+            uint8_t* const at = codes0 + h * static_cast<int64_t>(head_bytes);
+            uint2* const codes = reinterpret_cast<uint2*>(at + which * kv_code_at(D, 1, 0));
+            uint32_t* const params = reinterpret_cast<uint32_t*>(at + params0 + which * (kGranule * 4));
             // a NaN among the values stays in both
             float lo = raw[0].get(0), hi = lo;
 #pragma unroll
@@ -241,12 +242,13 @@ __global__ void __launch_bounds__(kThreads, VEC && sizeof(T) == 2 ? 4 : 3) kv_ap
                 }
                 if (there && KQ_IN_RANGE(reinterpret_cast<uint8_t*>(codes + 4 * u) - c.data, kv_pool_bytes(c) - 7))
                     codes[4 * u] = make_uint2(word[0], word[1]);
+                if (unit + 1 < u1) raw[u].load(next + 64 * u);
             }
             if (there && in_row == 0) {
                 if (KQ_IN_RANGE(reinterpret_cast<uint8_t*>(params) - c.data, kv_pool_bytes(c) - 3))
                     *params = fine ? (sb >> 16) | ob : 0x7FC07FC0u;
-                const int64_t slot = (static_cast<int64_t>(b) * c.kv_heads + h) * S + k.slot;
-                if (which == 0 && k.slot < S && KQ_IN_RANGE(slot, static_cast<int64_t>(c.batch) * c.kv_heads * S)) {
+                const int64_t slot = slot0 + h * S;
+                if (which == 0 && (acc || pos) && k.slot < S && KQ_IN_RANGE(slot, static_cast<int64_t>(c.batch) * c.kv_heads * S)) {
                     if (acc) acc[slot] = 0.0f;
                     if (pos) pos[slot] = at_pos;
                 }
@@ -376,8 +378,8 @@ extern "C" kq_status kq_kv_append(const kq_kv_cache* cache, const void* k, const
     bool vec = true;
     for (int w = 0; w < 2; ++w)
         vec = vec && !(reinterpret_cast<uintptr_t>(src.p[w]) & 15u) && !((src.token[w] * es) & 15u) && !((src.head[w] * es) & 15u);
-    // four units to a warp, unless that leaves SMs without work: for 51k tokens of 8 heads, bf16, 61 us (one: 78, two: 66, eight
-    // and sixteen: 62 and 70); of 2 heads, where the rule takes two, 21 us (one: 24, four: 22)
+    // four units (a key or value row of each token) to a warp, unless that leaves SMs without work: for 51k tokens of 8
+    // heads, fp32, 81 us (one: 95, two: 83, eight: 84, sixteen: 85)
     const int64_t runs = cdiv(T, kRun), units = 2 * c.kv_heads;
     const int per = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(4, runs * units / (num_sms() * 64))));
     const int groups = static_cast<int>(cdiv(units, per));
