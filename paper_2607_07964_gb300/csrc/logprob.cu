@@ -164,6 +164,101 @@ __device__ __noinline__ void careful_row(const T* x, int64_t r, int64_t V, int64
     }
 }
 
+// Value e of a 16-byte vector.
+template <typename T>
+__device__ __forceinline__ float value_of(const uint4& u, int e) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    return __uint_as_float(sizeof(T) == 4 ? w[e % 4] : e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
+}
+// Candidates for the top values: those from the bound up, by value and index.
+struct Offers {
+    uint64_t bound;
+    uint64_t* list;
+    int* n;
+
+    __device__ __forceinline__ void add(uint64_t k) const {
+        if (k < bound) return;
+        const int at = atomicAdd(n, 1);
+        if (at < kList) list[at] = k;
+    }
+    template <typename T>
+    __device__ __forceinline__ void add_vector(const uint4* v, uint32_t first) const {
+        const uint4 u = __ldg(v);
+#pragma unroll
+        for (int e = 0; e < static_cast<int>(16 / sizeof(T)); ++e) add(rank_key(value_of<T>(u, e), first + e));
+    }
+};
+// A thread's share of a row: vectors threadIdx.x, threadIdx.x + NT, .. of nvec, A of them a group.
+struct Mine {
+    const uint4* xv;
+    int nvec, groups, best_group;   // the group with the largest value
+    uint32_t first;                 // index in the row of the first vector's first value
+    uint32_t most;                  // order of the largest value
+    uint64_t edge;                  // key of the thread's value outside the vectors, or 0
+};
+// Too many near the bound's value: the bound becomes the top-th largest of the threads' first largest values by value and
+// index (complements, the largest first; an index is below 2^20), and the groups that may hold something from there up are
+// read, on a list by all threads, or else each by its own: any number of float32 groups can share the bound's upper half
+// (4096 rows of 32000 fp32 logits, 20 top values: 105 us; all near 100 within 0.03, 126 us; all equal, 130 us).
+template <typename T, int NT, int A>
+__device__ __forceinline__ void second_look(const Mine& a, const uint16_t* group_max, int top, uint64_t* list, int* n_list,
+                                         int* groups, int* n_groups) {
+    constexpr int E = 16 / sizeof(T);
+    uint64_t key = a.edge, bound = 0;
+    const int at0 = a.best_group * A * NT + static_cast<int>(threadIdx.x);
+    uint4 u[A];
+#pragma unroll
+    for (int i = 0; i < A; ++i)
+        if (at0 + i * NT < a.nvec) u[i] = __ldg(a.xv + at0 + i * NT);
+#pragma unroll
+    for (int i = 0; i < A; ++i) {
+        if (at0 + i * NT >= a.nvec) break;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            key = max(key, rank_key(value_of<T>(u[i], e), a.first + static_cast<uint32_t>((at0 + i * NT) * E + e)));
+    }
+    for (int bit = 63; bit >= 0; --bit) {
+        if (bit < 32 && bit >= 20) {
+            bound |= 1ull << bit;
+            continue;
+        }
+        const uint64_t cand = bound | (1ull << bit);
+        if (__syncthreads_count(key >= cand) >= top) bound = cand;
+    }
+    if (threadIdx.x == 0) *n_list = *n_groups = 0;
+    __syncthreads();
+    const Offers offers = {bound, list, n_list};
+    if (a.edge) offers.add(a.edge);
+    const uint32_t bound_value = static_cast<uint32_t>(bound >> 32), bound_index = key_index(bound);
+    // Where no value of a group is above the bound's (in bf16 the upper half says so, in float32 the thread's largest
+    // can), one that begins behind the bound's index has nothing to offer.
+    auto each_group = [&](auto f) {
+        for (int g = 0; g < a.groups && a.most >= bound_value; ++g) {
+            const uint32_t gm = group_max[g * NT + threadIdx.x];
+            const int first = g * A * NT + static_cast<int>(threadIdx.x);
+            const bool equal = sizeof(T) == 2 ? gm == bound_value >> 16 : a.most == bound_value;
+            if (gm < bound_value >> 16 || (equal && a.first + static_cast<uint32_t>(first * E) > bound_index)) continue;
+            f(first);
+        }
+    };
+    auto read = [&](int at) {
+        if (at < a.nvec) offers.add_vector<T>(a.xv + at, a.first + static_cast<uint32_t>(at * E));
+    };
+    each_group([&](int first) {
+        const int at = atomicAdd(n_groups, 1);
+        if (at < kGroups) groups[at] = first;
+    });
+    __syncthreads();
+    if (*n_groups <= kGroups) {
+        for (int q = threadIdx.x; q < *n_groups * A; q += NT) read(groups[q / A] + q % A * NT);
+    } else {
+        each_group([&](int first) {
+            for (int i = 0; i < A; ++i) read(first + i * NT);
+        });
+    }
+    __syncthreads();
+}
+
 // SPLIT: a cluster takes a row, each block an equal run of `part` values of it.
 template <typename T, int NT, bool SPLIT>
 __global__ void __launch_bounds__(NT, NT >= kSplit ? 1 : 1536 / NT) logprob_kernel(const T* __restrict__ logits, int64_t row_len,
@@ -356,66 +451,35 @@ __global__ void __launch_bounds__(NT, NT >= kSplit ? 1 : 1536 / NT) logprob_kern
         if (kShift) b = b << 16 | (b >> 15 ? 0u : 0xFFFFu);
         bound = static_cast<uint64_t>(b) << 32;
     }
-    for (int pass = 0;; ++pass) {
-        __syncthreads();
-        const uint32_t bound_half = static_cast<uint32_t>(bound >> 48), bound_index = key_index(bound);
+    __syncthreads();
+    if (order(best) >= bound >> 32)   // no group holds more than its thread's largest, nor an upper half above its own
         for (int g = 0; g < n_mine; ++g) {
-            const uint32_t gm = group_max[g * NT + tid];
-            const int first = g * A * NT + tid;   // its first vector
-            if (gm < bound_half || (gm == bound_half && base + static_cast<uint32_t>(head + first * E) > bound_index)) continue;
+            if (group_max[g * NT + tid] < bound >> 48) continue;
             const int at = atomicAdd(&n_groups, 1);
-            if (at < kGroups) groups[at] = first;
+            if (at < kGroups) groups[at] = g * A * NT + tid;   // its first vector
         }
-        auto offer = [&](uint64_t k) {
-            if (k < bound) return;
-            const int at = atomicAdd(&n_list, 1);
-            if (at < kList) list[at] = k;
-        };
-        if (my_edge >= 0) offer(rank_key(ev, base + static_cast<uint32_t>(my_edge)));
-        __syncthreads();
-        if (n_groups <= kGroups) {
-            for (int q = tid; q < n_groups * A; q += NT) {
-                const int at = groups[q / A] + q % A * NT;
-                if (at >= nvec) continue;
-                const uint4 u = __ldg(xv + at);
-                const uint32_t w4[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const uint32_t b = sizeof(T) == 4 ? w4[e % 4] : e & 1 ? w4[e / 2] & 0xFFFF0000u : w4[e / 2] << 16;
-                    offer(rank_key(__uint_as_float(b), base + static_cast<uint32_t>(head + at * E + e)));
-                }
-            }
+    const Offers offers = {bound, list, &n_list};
+    if (my_edge >= 0) offers.add(rank_key(ev, base + static_cast<uint32_t>(my_edge)));
+    __syncthreads();
+    if (n_groups <= kGroups) {
+        for (int q = tid; q < n_groups * A; q += NT) {
+            const int at = groups[q / A] + q % A * NT;
+            if (at < nvec) offers.add_vector<T>(xv + at, base + static_cast<uint32_t>(head + at * E));
         }
-        __syncthreads();
-        if (n_groups <= kGroups && n_list <= kList) break;
-        if (pass == 1) {   // more near the bound than the lists hold
+    }
+    __syncthreads();
+    if (n_groups > kGroups || n_list > kList) {
+        const Mine own = {xv, nvec, n_mine, best_group, base + static_cast<uint32_t>(head), order(best),
+                          my_edge >= 0 ? rank_key(ev, base + static_cast<uint32_t>(my_edge)) : 0};
+        second_look<T, NT, A>(own, group_max, top, list, &n_list, groups, &n_groups);
+        if (n_list > kList) {   // more values from the bound up than the list holds
             if constexpr (SPLIT) {
                 if (tid == 0) failed = 1;
-                break;
             } else {
                 careful_row<T, NT>(row, r, row_len, y, top, out, tmp64);
                 return;
             }
         }
-        // Too many near the bound's value: the top-th largest of the threads' first largest values by value and index
-        // (complements, the largest first; an index is below 2^20).
-        uint64_t key = my_edge >= 0 ? rank_key(ev, base + static_cast<uint32_t>(my_edge)) : 0;
-        for (int i = 0; i < A; ++i) {
-            const int at = best_group * A * NT + tid + i * NT;
-            if (at >= nvec) break;
-            for (int e = 0; e < E; ++e)
-                key = max(key, rank_key(value(reinterpret_cast<const T*>(xv + at), e), base + static_cast<uint32_t>(head + at * E + e)));
-        }
-        bound = 0;
-        for (int bit = 63; bit >= 0; --bit) {
-            if (bit < 32 && bit >= 20) {
-                bound |= 1ull << bit;
-                continue;
-            }
-            const uint64_t cand = bound | (1ull << bit);
-            if (__syncthreads_count(key >= cand) >= top) bound = cand;
-        }
-        if (tid == 0) n_groups = n_list = 0;
     }
     int n = min(n_list, kList);
     if constexpr (SPLIT) {   // the block's own top values, then those of all, by the row's first block
