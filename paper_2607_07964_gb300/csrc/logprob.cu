@@ -6,7 +6,7 @@
 // A thread keeps a reference of its own, moved only when a value passes it by 2^kSlack, so Z and
 // sum 2^t t need no rescaling in the common step; r differs from the maximum by so little that the
 // entropy's two terms do not cancel beyond a few units. t is formed by one fma, the same for every
-// use, so a rounding of r cancels from logp and entropy, however large the logits are.
+// use, so a rounding of r (kHuge bounds it) cancels from logp and entropy.
 //
 // The largest `top` values: a bound that at least `top` of the threads' maxima reach, and the row's groups
 // of kAhead (kWideAhead) vectors whose own maximum, noted in 16 bits in shared memory along the way, reaches it
@@ -37,7 +37,10 @@ constexpr int kGroups = 256;              // groups that are looked through for 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kSlack = 4.0f;
 constexpr float kFloor = -2.0e38f;        // what a masked logit counts as: 2^t = 0 and t a number
-constexpr float kHuge = 1.0e38f;          // rows whose maximum is beyond this, or -infinity, go the careful way
+// Rows whose maximum is beyond this, or -infinity, go the careful way. The reference's rounding, in every t alike, is
+// at most 2^6 here, so that neither 2^t nor Z leaves the range and the terms that cancel stay below 2^7; and log2(e)
+// kFloor less a reference is a number, whose share 0 t is 0. (2^30 leaves rows shifted by -1e9 to the fast way.)
+constexpr float kHuge = 0x1p30f;
 
 __device__ __forceinline__ float value(const float* p, int64_t i) { return p[i]; }
 __device__ __forceinline__ float value(const __nv_bfloat16* p, int64_t i) { return __bfloat162float(p[i]); }
@@ -202,7 +205,7 @@ struct Mine {
 // (4096 rows of 32000 fp32 logits, 20 top values: 105 us; all near 100 within 0.03, 126 us; all equal, 130 us).
 template <typename T, int NT, int A>
 __device__ __forceinline__ void second_look(const Mine& a, const uint16_t* group_max, int top, uint64_t* list, int* n_list,
-                                         int* groups, int* n_groups) {
+                                            int* groups, int* n_groups) {
     constexpr int E = 16 / sizeof(T);
     uint64_t key = a.edge, bound = 0;
     const int at0 = a.best_group * A * NT + static_cast<int>(threadIdx.x);

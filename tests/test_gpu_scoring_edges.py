@@ -62,3 +62,50 @@ def test_top_values_that_share_their_leading_bits(T, V, dtype, kind, top):
     lp = torch.log_softmax(x.double(), 1)
     exact = lp.gather(1, want)
     assert ((tl - exact).abs() <= 2.0 ** -18 * (1 + x.double().amax(1, keepdim=True).abs() + exact.abs())).all()
+
+
+@pytest.mark.parametrize("V", [50, 9001, 60000])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("mask", ["infinite", "lowest"])
+@pytest.mark.parametrize("rows", [8, 200, 400])
+def test_entropy_of_rows_with_a_huge_maximum_and_masked_tokens(V, dtype, mask, rows):
+    """Row i: i % 4 + 1 tokens share a maximum between 1e37 and 3e38, most others are masked, some 0. The maximum's
+    tokens have differences of exactly 0 and the others probability 0, so logp is -ln k and the entropy ln k, each one
+    logarithm of a small whole number: within 2^-19 (1 + the value)."""
+    ty = torch.bfloat16 if dtype == "bf16" else torch.float32
+    x = torch.full((rows, V), -math.inf if mask == "infinite" else torch.finfo(ty).min, dtype=ty, device=DEV)
+    x[:, 1::7] = 0
+    tops = [1e37, 2.9e37, 3.1e37, 3.7e37, 5e37, 9.9e37, 1.01e38, 3e38]
+    k = [1 + i % 4 for i in range(rows)]
+    for i in range(rows):
+        x[i, 5:5 + 3 * k[i]:3] = tops[i % 8]
+    logp, h, lse, ids, tl = _run(x, torch.full((rows,), 5, device=DEV), 2)
+    want = torch.tensor(k, dtype=torch.float64, device=DEV).log()
+    tol = 2.0 ** -19 * (1 + want)
+    assert ((logp + want).abs() <= tol).all() and ((h - want).abs() <= tol).all()
+    assert ((lse - x[:, 5].double()).abs() <= 2.0 ** -22 * x[:, 5].double()).all()
+    assert (ids[:, 0] == 5).all() and ((tl[:, 0] + want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("V", [50, 9001, 60000])
+@pytest.mark.parametrize("rows", [14, 210, 420])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_whose_logits_are_all_large(V, rows, dtype):
+    """Row i: i % 4 + 1 tokens share a maximum of either sign, the others lie at least 2^-7 of it lower, which is more than
+    a thousand: probability 0. Up to 2^30 the reference is off by up to 64 powers of two, so terms of that size are
+    rounded (2^-18 each, three of them) where they cancel; beyond, differences are exact: within 2^-16 (1 + the value)."""
+    ty = torch.bfloat16 if dtype == "bf16" else torch.float32
+    tops = torch.tensor([2e5, -3e7, 2e8, -1e9, 1.05e9, 1.2e9, -3e9, 7e9, 1e10, -1e12, 1e15, 1e20, -1e30, 2.5e37], device=DEV)
+    k = [1 + i % 4 for i in range(rows)]
+    m = tops.repeat(rows // 14)[:, None]
+    x = (m - m.abs() * (0.01 + torch.rand(rows, V, device=DEV, generator=torch.Generator(DEV).manual_seed(V)))).to(ty)
+    m = m.to(ty)
+    for i in range(rows):
+        x[i, 5:5 + 3 * k[i]:3] = m[i, 0]
+    logp, h, lse, ids, tl = _run(x, torch.full((rows,), 5, device=DEV), 1)
+    want = torch.tensor(k, dtype=torch.float64, device=DEV).log()
+    tol = 2.0 ** -16 * (1 + want)
+    assert ((logp + want).abs() <= tol).all() and ((h - want).abs() <= tol).all()
+    exact = m[:, 0].double() + want
+    assert ((lse - exact).abs() <= 2.0 ** -22 * exact.abs()).all()
+    assert (ids[:, 0] == 5).all() and ((tl[:, 0] + want).abs() <= tol).all()
