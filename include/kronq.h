@@ -470,6 +470,8 @@ KQ_API kq_status kq_kv_read(const kq_kv_cache* cache, const int32_t* start, cons
  *     s_j = scale <q, k_j>,  out = sum_j e^(s_j) v_j / sum_j e^(s_j),  lse = ln sum_j e^(s_j)
  *   out [T][q_heads][dim] contiguous in q's type, lse (nullable) [T][q_heads] fp32. A token that
  *   sees no slot gives out = 0, lse = -infinity. Sums and softmax are fp32 over exact codes.
+ *   A sum of values carries weights of up to 2^8: it stays in range while the largest |value|
+ *   times the slots seen is below 2^120, and is infinite or NaN where it does not.
  *   acc (nullable, [batch][kv_heads][S] fp32): each slot's weight e^(s_j - lse), summed over the
  *   query heads of its head and over the sequence's tokens of this call, is added to it; then
  *   lens <= S. Results do not depend on the order in which blocks run.

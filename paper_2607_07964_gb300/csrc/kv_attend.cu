@@ -740,8 +740,11 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas) kv_attend_ke
         // ---- the rows' result, or this piece's part of it
         const bool whole = seg == at.s.steps;
         float* part = p.part + (2 * me + (at.step == 0)) * (kRows * (D + 2));   // of an item begun here, of one gone on with
-        // 2^24 of subnormal codes, 2^-6 2^(ev + 1 - 127) of the weights
-        const float up = __uint_as_float(static_cast<uint32_t>(min(R.ev - (kSplit ? 132 : 108), 127) + 127) << 23);
+        // 2^24 of subnormal codes, 2^-6 2^(ev + 1 - 127) of the weights; what float32 cannot hold of it, for scales
+        // of 2^109 and more, goes to the sums first
+        const int power = R.ev - (kSplit ? 132 : 108), past = max(0, power - 127);
+        const float up = __uint_as_float(static_cast<uint32_t>(power - past + 127) << 23);
+        const float first = __uint_as_float(static_cast<uint32_t>(past + 127) << 23);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const float one[2] = {1.0f, 1.0f};
@@ -760,8 +763,8 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas) kv_attend_ke
                 float x[D / 8];   // dimensions g8 D / 8 ..
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i) {
-                    x[2 * i] = fmaf(R.o[nt][i][k2], up, off);
-                    x[2 * i + 1] = fmaf(R.o[nt][i][2 + k2], kSplit ? up : up * 0.0625f, off);
+                    x[2 * i] = fmaf(R.o[nt][i][k2] * first, up, off);
+                    x[2 * i + 1] = fmaf(R.o[nt][i][2 + k2] * first, kSplit ? up : up * 0.0625f, off);
                 }
                 if (whole) {
                     const int row = at.rt * kRows + col;
