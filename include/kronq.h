@@ -442,7 +442,7 @@ KQ_API kq_status kq_infer(const uint32_t* packed, const float* scale, const int3
  *   (nullable, int32, same shape) the token's position seen[b] + its index in the call at the
  *   slots written (seen [batch] int32: tokens the sequence has had so far, evicted ones among
  *   them; seen = NULL counts from lens); seen_out (nullable) receives seen plus the new tokens.
- *   lens_out and seen_out must not be lens or seen.
+ *   Neither lens_out nor seen_out may share memory with start, lens or seen, nor with the other.
  * kq_kv_read: the values of cached tokens, k, v [T][kv_heads][dim] contiguous: token i of
  *   sequence b is slot first[b] + i - start[b] (first = NULL: 0). Slots at or beyond lens[b] (lens =
  *   NULL: the capacity) and tokens of no sequence read 0.

@@ -89,6 +89,12 @@ __device__ __forceinline__ int64_t kv_length(const int32_t* __restrict__ lens, i
     return n < 0 ? 0 : most;
 }
 
+// Host side: whether an output of n integers shares memory with m integers that blocks still read while it is written.
+inline bool kv_overlap(const int32_t* out, int64_t n, const int32_t* in, int64_t m) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(out), b = reinterpret_cast<uintptr_t>(in);
+    return out && in && a < b + static_cast<uintptr_t>(m) * sizeof(int32_t) && b < a + static_cast<uintptr_t>(n) * sizeof(int32_t);
+}
+
 // Host side: checks a cache description and makes the kernels' view of it.
 kq_status kv_view(const kq_kv_cache* c, const char* who, KvView* v);
 

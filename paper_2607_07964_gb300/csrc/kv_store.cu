@@ -367,11 +367,16 @@ extern "C" kq_status kq_kv_append(const kq_kv_cache* cache, const void* k, const
         return KQ_ERR_UNSUPPORTED;
     }
     const uintptr_t es = dtype == KQ_BF16 ? 2 : 4;
+    // the first block writes its outputs while the others read these
+    auto read_too = [&](const int32_t* out) {
+        return kv_overlap(out, c.batch, start, c.batch + 1) || kv_overlap(out, c.batch, lens, c.batch) ||
+               kv_overlap(out, c.batch, seen, c.batch);
+    };
     if (T < 0 || T > 0x7fffffffll || !start || !lens || (T > 0 && (!k || !v)) || ((acc || pos) && S < 1) ||
-        lens_out == lens || (seen_out && seen_out == seen) || (lens_out && lens_out == seen_out) ||
+        read_too(lens_out) || read_too(seen_out) || kv_overlap(lens_out, c.batch, seen_out, c.batch) ||
         ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & (es - 1))) {
         set_error("kq_kv_append: start, lens, k, v must not be NULL, 0 <= T < 2^31, S >= 1 with acc or pos, lens_out and "
-                  "seen_out apart from lens and seen");
+                  "seen_out apart from each other and from start, lens and seen");
         return KQ_ERR_INVALID_ARG;
     }
     RowSource src = {{k, v}, {k_token_stride, v_token_stride}, {k_head_stride, v_head_stride}};

@@ -100,3 +100,23 @@ def test_numpy_eviction_by_hand():
     pos = np.arange(6)
     assert ref.evict(acc, pos, 6, 6, 4, 1, 1) == [0, 4, 5, 3]       # 0 (sink), 5 (recent), .9, .2: slots 4 and 5 move into 1 and 2
     assert ref.evict(acc, pos, 6, 6, 3, 0, 0) == [0, 3, 4]          # .5, .9, .2: slots 3 and 4 move into 1 and 2, in order
+
+
+def test_append_refuses_outputs_that_its_blocks_still_read(K):
+    """lens, seen and start are read by every block while the first one writes lens_out and seen_out."""
+    lib, c = K.lib(), _cache(K)
+    start, lens, seen, out, out2 = (P(256 * i) for i in range(1, 6))
+    arg = [c, FAKE, FAKE, 0, 1, 256, 128, 256, 128, start, lens, None, None, None, 0, seen, None, None, None]
+    for lens_out, seen_out in ((lens, None), (seen, None), (start, None), (None, lens), (None, seen), (None, start),
+                               (out, out), (out, lens), (seen, out2)):
+        arg[11], arg[16] = lens_out, seen_out
+        assert lib.kq_kv_append(*arg) == K.KQ_ERR_INVALID_ARG, (lens_out, seen_out)
+        assert "apart" in K.last_error()
+    arg[11], arg[15], arg[16] = None, None, lens   # seen = NULL counts from lens
+    assert lib.kq_kv_append(*arg) == K.KQ_ERR_INVALID_ARG
+    many = _cache(K, batch=8)
+    arg[0], arg[15], arg[16] = many, seen, None
+    for near in (lens, seen, start):   # parts of one array
+        for off in (-28, 4, 28):
+            arg[11] = P(near.value + off)
+            assert lib.kq_kv_append(*arg) == K.KQ_ERR_INVALID_ARG, off
