@@ -494,7 +494,7 @@ KQ_API kq_status kq_kv_attend(const kq_kv_cache* cache, const void* q, int dtype
  *   pos). Only what moves is read and written.
  *   acc_out, pos_out ([batch][kv_heads][S], S as acc and pos) receive the weights and
  *   positions of the slots kept; they may be acc and pos themselves. Entries beyond the new length
- *   are left as they are. lens_out (not lens) receives min(lens, budget). Slots at and beyond
+ *   are left as they are. lens_out (apart from lens and seen) receives min(lens, budget). Slots at and beyond
  *   the new length keep stale contents. Pages must not be shared. recent + sink <= budget, budget >= 1.
  *   ws: kq_kv_evict_workspace(batch, kv_heads, S, budget) bytes, 256-byte aligned.
  */

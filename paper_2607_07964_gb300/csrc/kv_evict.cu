@@ -342,9 +342,10 @@ extern "C" kq_status kq_kv_evict(const kq_kv_cache* cache, const int32_t* lens, 
                                  size_t ws_bytes, kq_stream_t stream_) {
     KvView c;
     KQ_TRY(kv_view(cache, "kq_kv_evict", &c));
-    if (!lens || !acc || !pos || !seen || !lens_out || !acc_out || !pos_out || lens_out == lens || S < 1 ||
+    if (!lens || !acc || !pos || !seen || !lens_out || !acc_out || !pos_out || S < 1 ||
+        kv_overlap(lens_out, c.batch, lens, c.batch) || kv_overlap(lens_out, c.batch, seen, c.batch) ||   // other blocks read them
         S > 0x7fffffffll - (1 << 20) || budget < 1 || recent < 0 || sink < 0 || recent > budget || sink > budget - recent) {
-        set_error("kq_kv_evict: arrays must not be NULL, lens_out apart from lens, budget >= 1, recent + sink <= budget");
+        set_error("kq_kv_evict: arrays must not be NULL, lens_out apart from lens and seen, budget >= 1, recent + sink <= budget");
         return KQ_ERR_INVALID_ARG;
     }
     budget = std::min(budget, S);

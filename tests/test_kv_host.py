@@ -120,3 +120,13 @@ def test_append_refuses_outputs_that_its_blocks_still_read(K):
         for off in (-28, 4, 28):
             arg[11] = P(near.value + off)
             assert lib.kq_kv_append(*arg) == K.KQ_ERR_INVALID_ARG, off
+
+
+def test_evict_refuses_a_length_output_that_its_blocks_still_read(K):
+    """A sequence's lens and seen are read by the blocks of all its heads while one of them writes lens_out."""
+    lens, acc, pos, seen, lib = *(P(256 * i) for i in range(1, 5)), K.lib()
+    c = _cache(K, batch=8)
+    for lens_out in (lens, seen, P(lens.value + 4), P(seen.value - 28)):
+        assert lib.kq_kv_evict(c, lens, acc, pos, seen, 64, 8, 4, 2, lens_out, acc, pos, None, FAKE, 1 << 20,
+                               None) == K.KQ_ERR_INVALID_ARG
+        assert "apart" in K.last_error()
