@@ -66,20 +66,58 @@ class KvCache:
             self.pos = torch.zeros(batch, kv_heads, slots, **i32)
             self._evict_ws = torch.empty(kq.kq_kv_evict_workspace(self.acc, budget), dtype=torch.uint8, device=device)
         self._ws = None
-        self.most = 0   # slots that the longest sequence may hold
+        # what the host knows of the lengths: a sequence holds at most its entry and what all may have got since
+        self._each, self._peak, self._all = [0] * batch, 0, 0
+        self._sure = True   # exactly that
 
-    def append(self, k, v, start, most: int) -> None:
+    @property
+    def most(self) -> int:
+        """Slots that the longest sequence may hold."""
+        return self._peak + self._all
+
+    def _account(self, each) -> None:
+        self._each, self._peak, self._all = each, max(each), 0
+
+    def _longest(self, more, cap: int | None = None) -> int:
+        """The longest sequence's slots after `more` tokens, a number for all or a list, first cut back to `cap`."""
+        def left(n):
+            return n if cap is None else min(n, cap)
+        if not isinstance(more, list):
+            return left(self.most) + more
+        return max(left(n + self._all) + m for n, m in zip(self._each, more))
+
+    def measure(self) -> None:
+        """Reads the lengths from the device."""
+        self._account(self.lens.tolist())
+        self._sure = True
+
+    def append(self, k, v, start, most) -> None:
         """k, v [T, kv_heads, dim] of the sequences' next tokens; start [batch + 1] on the device; most: the
-        largest number of tokens that a sequence gets."""
-        if self.most + most > self.slots:
-            if self.budget is None or min(self.most, self.budget) + most > self.slots:
-                raise ValueError(f"{most} more tokens do not fit {self.slots} slots")
-            self.evict()
+        largest number of tokens that a sequence gets, or a list of the number that each gets. Where the largest
+        number leaves open whether the tokens fit, the lengths are read from the device."""
+        batch, T = len(self._each), k.shape[0]
+        more = list(most) if isinstance(most, (list, tuple)) else most
+        sure = isinstance(more, list) or T == batch * more
+        if isinstance(more, list) and (len(more) != batch or min(more) < 0 or sum(more) != T):
+            raise ValueError(f"most must be a number or {batch} counts that add up to the {T} tokens of k, got {most}")
+        if self._longest(more) > self.slots:
+            if not (self._sure and sure):
+                self.measure()
+                ends = start.tolist()
+                more, sure = [b - a for a, b in zip(ends, ends[1:])], True
+            if self._longest(more) > self.slots:
+                if self.budget is None or self._longest(more, self.budget) > self.slots:
+                    raise ValueError(f"{most} more tokens do not fit {self.slots} slots")
+                self.evict()
         kq.kq_kv_append(k, v, start, self.lens, self.data, self.table, lens_out=self._lens, acc=self.acc, pos=self.pos,
                         seen=self.seen, seen_out=self._seen, info=self.info)
         self.lens, self._lens = self._lens, self.lens
         self.seen, self._seen = self._seen, self.seen
-        self.most += most
+        self._sure = self._sure and sure
+        if isinstance(more, list):
+            self._account([n + self._all + m for n, m in zip(self._each, more)])
+        else:
+            self._all += more
 
     def attend(self, q, start, scale: float | None = None, lse=None):
         """Attention of q [T, q_heads, dim] of the tokens appended last over their sequences."""
@@ -96,7 +134,7 @@ class KvCache:
         kq.kq_kv_evict(self.data, self.table, self.lens, self.acc, self.pos, self.seen, self.dim, self.budget, self.recent,
                        self.sink, self._lens, self.acc, self.pos, self._evict_ws, info=self.info)
         self.lens, self._lens = self._lens, self.lens
-        self.most = min(self.most, self.budget)
+        self._account([min(n + self._all, self.budget) for n in self._each])
 
     def read(self, dtype=torch.float32):
         """The cached keys and values, [batch, slots, kv_heads, dim], zeros past each length."""
@@ -118,7 +156,7 @@ class AttentionBlock:
     def __init__(self, proj: dict, heads: int, cache: KvCache):
         self.proj, self.heads, self.cache = proj, heads, cache
 
-    def __call__(self, x, start, most: int):
+    def __call__(self, x, start, most):
         c, T = self.cache, x.shape[0]
         q, k, v = (self.proj[n](x) for n in ("q", "k", "v"))
         c.append(k.view(T, c.kv_heads, c.dim), v.view(T, c.kv_heads, c.dim), start, most)
@@ -161,7 +199,7 @@ def example(steps: int = 24, prompts=(40, 7, 23), vocab: int = 1000, heads: int 
     embed, head = (torch.randn(vocab, d, device="cuda", generator=g) for _ in range(2))
     tokens = torch.randint(0, vocab, (sum(prompts),), device="cuda", generator=g)
     ends = torch.tensor((0,) + tuple(prompts), device="cuda").cumsum(0).to(torch.int32)
-    x = block(embed[tokens], ends, max(prompts))[(ends[1:] - 1).long()]
+    x = block(embed[tokens], ends, prompts)[(ends[1:] - 1).long()]
     one = torch.arange(batch + 1, dtype=torch.int32, device="cuda")
     ids, logps = [], []
     for _ in range(steps):
