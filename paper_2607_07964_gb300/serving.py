@@ -45,7 +45,11 @@ class KvCache:
     """The 4-bit cache of `batch` sequences with up to `slots` cached tokens each. With a budget, append
     first cuts the sequences back to `budget` slots when the new tokens would not fit: the last `recent` and
     first `sink` positions stay, and those that drew the most attention weight since they were
-    cached, each head on its own."""
+    cached, each head on its own.
+
+    Its calls can be captured in CUDA graphs and replayed on the lengths as they then are. The host does not see
+    replays: once an append has been captured, the others read the lengths from the device first, and replays past the
+    last slot are up to the caller (a captured `evict` keeps away from it; tokens without a slot are reported by `check`)."""
 
     def __init__(self, batch: int, kv_heads: int, dim: int, slots: int, page: int = 64, budget: int | None = None,
                  recent: int = 0, sink: int = 0, device: str = "cuda"):
@@ -65,10 +69,12 @@ class KvCache:
             self.acc = torch.zeros(batch, kv_heads, slots, device=device)
             self.pos = torch.zeros(batch, kv_heads, slots, **i32)
             self._evict_ws = torch.empty(kq.kq_kv_evict_workspace(self.acc, budget), dtype=torch.uint8, device=device)
-        self._ws = None
+        self._ws, self._held = None, []   # workspaces that a graph may write to stay
         # what the host knows of the lengths: a sequence holds at most its entry and what all may have got since
         self._each, self._peak, self._all = [0] * batch, 0, 0
         self._sure = True   # exactly that
+        self._fixed = False     # a graph holds the arrays
+        self._replayed = False   # and may have appended since
 
     @property
     def most(self) -> int:
@@ -86,6 +92,23 @@ class KvCache:
             return left(self.most) + more
         return max(left(n + self._all) + m for n, m in zip(self._each, more))
 
+    def _capturing(self) -> bool:
+        now = self.lens.is_cuda and torch.cuda.is_current_stream_capturing()
+        self._fixed = self._fixed or now
+        return now
+
+    def _take(self, seen: bool) -> None:
+        """The lengths (and counts) that a call has written become the current ones: they change places, which costs
+        nothing, or are copied where a graph holds the arrays."""
+        if self._fixed:
+            self.lens.copy_(self._lens)
+            if seen:
+                self.seen.copy_(self._seen)
+            return
+        self.lens, self._lens = self._lens, self.lens
+        if seen:
+            self.seen, self._seen = self._seen, self.seen
+
     def measure(self) -> None:
         """Reads the lengths from the device."""
         self._account(self.lens.tolist())
@@ -100,8 +123,12 @@ class KvCache:
         sure = isinstance(more, list) or T == batch * more
         if isinstance(more, list) and (len(more) != batch or min(more) < 0 or sum(more) != T):
             raise ValueError(f"most must be a number or {batch} counts that add up to the {T} tokens of k, got {most}")
+        capturing = self._capturing()
+        if self._replayed and not capturing:
+            self.measure()
+        self._replayed = self._replayed or capturing
         if self._longest(more) > self.slots:
-            if not (self._sure and sure):
+            if not (self._sure and sure) and not capturing:
                 self.measure()
                 ends = start.tolist()
                 more, sure = [b - a for a, b in zip(ends, ends[1:])], True
@@ -111,8 +138,7 @@ class KvCache:
                 self.evict()
         kq.kq_kv_append(k, v, start, self.lens, self.data, self.table, lens_out=self._lens, acc=self.acc, pos=self.pos,
                         seen=self.seen, seen_out=self._seen, info=self.info)
-        self.lens, self._lens = self._lens, self.lens
-        self.seen, self._seen = self._seen, self.seen
+        self._take(seen=True)
         self._sure = self._sure and sure
         if isinstance(more, list):
             self._account([n + self._all + m for n, m in zip(self._each, more)])
@@ -121,8 +147,11 @@ class KvCache:
 
     def attend(self, q, start, scale: float | None = None, lse=None):
         """Attention of q [T, q_heads, dim] of the tokens appended last over their sequences."""
+        self._capturing()
         need = kq.kq_kv_attend_workspace(q, self.data, self.table, self.acc)
         if self._ws is None or self._ws.numel() < need:
+            if self._fixed:
+                self._held.append(self._ws)
             self._ws = torch.empty(need, dtype=torch.uint8, device=q.device)
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         kq.kq_kv_attend(q, start, self.lens, self.data, self.table, out, self._ws,
@@ -131,13 +160,15 @@ class KvCache:
 
     def evict(self) -> None:
         """Cuts every sequence with more than `budget` slots back to it."""
+        self._capturing()
         kq.kq_kv_evict(self.data, self.table, self.lens, self.acc, self.pos, self.seen, self.dim, self.budget, self.recent,
                        self.sink, self._lens, self.acc, self.pos, self._evict_ws, info=self.info)
-        self.lens, self._lens = self._lens, self.lens
+        self._take(seen=False)
         self._account([min(n + self._all, self.budget) for n in self._each])
 
     def read(self, dtype=torch.float32):
         """The cached keys and values, [batch, slots, kv_heads, dim], zeros past each length."""
+        self._capturing()
         batch = self.lens.shape[0]
         start = torch.arange(0, (batch + 1) * self.slots, self.slots, dtype=torch.int32, device=self.lens.device)
         k, v = (torch.empty(batch * self.slots, self.kv_heads, self.dim, dtype=dtype, device=self.lens.device) for _ in range(2))
