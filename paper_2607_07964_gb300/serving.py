@@ -152,6 +152,8 @@ class KvCache:
         if self._ws is None or self._ws.numel() < need:
             if self._fixed:
                 self._held.append(self._ws)
+            elif self._ws is not None:   # may have been made on another stream than the one that uses it last
+                self._ws.record_stream(torch.cuda.current_stream())
             self._ws = torch.empty(need, dtype=torch.uint8, device=q.device)
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         kq.kq_kv_attend(q, start, self.lens, self.data, self.table, out, self._ws,
