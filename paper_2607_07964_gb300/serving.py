@@ -162,6 +162,8 @@ class KvCache:
 
     def evict(self) -> None:
         """Cuts every sequence with more than `budget` slots back to it."""
+        if self.budget is None:
+            raise ValueError("a cache without a budget has nothing to cut back to")
         self._capturing()
         kq.kq_kv_evict(self.data, self.table, self.lens, self.acc, self.pos, self.seen, self.dim, self.budget, self.recent,
                        self.sink, self._lens, self.acc, self.pos, self._evict_ws, info=self.info)

@@ -76,3 +76,8 @@ def test_steps_of_all_sequences_do_not_wait_for_the_device(serving):
         _append(c, [1, 1, 1], [1, 2])
     with pytest.raises(ValueError, match="tokens of k"):
         _append(c, [1, 1, 1], [1, 1, 2])
+
+
+def test_eviction_without_a_budget_is_refused(serving):
+    with pytest.raises(ValueError, match="without a budget"):
+        serving.KvCache(1, 1, 64, 16, page=16, device="cpu").evict()
