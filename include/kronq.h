@@ -469,7 +469,10 @@ KQ_API kq_status kq_kv_read(const kq_kv_cache* cache, const int32_t* start, cons
  *   their sequence: token i of sequence b sees the slots below lens[b] - (start[b + 1] - 1 - i).
  *     s_j = scale <q, k_j>,  out = sum_j e^(s_j) v_j / sum_j e^(s_j),  lse = ln sum_j e^(s_j)
  *   out [T][q_heads][dim] contiguous in q's type, lse (nullable) [T][q_heads] fp32. A token that
- *   sees no slot gives out = 0, lse = -infinity. Sums and softmax are fp32 over exact codes.
+ *   sees no slot gives out = 0, lse = -infinity. The codes are exact; scores, softmax and sums are
+ *   fp32. With bf16 queries the weights enter the values' product in fp16 (11 bits) and the tensor
+ *   cores' sums run over the slots: 1e-4 of the output before it is rounded to bf16. With fp32 ones
+ *   queries and weights enter as two fp16 halves (22 bits): 1e-6.
  *   A sum of values carries weights of up to 2^8: it stays in range while the largest |value|
  *   times the slots seen is below 2^120, and is infinite or NaN where it does not.
  *   acc (nullable, [batch][kv_heads][S] fp32): each slot's weight e^(s_j - lse), summed over the
@@ -489,9 +492,9 @@ KQ_API kq_status kq_kv_attend(const kq_kv_cache* cache, const void* q, int dtype
  *   (pos >= seen[b] - recent) or the first `sink` (pos < sink), then those of the largest
  *   accumulated weight acc; equal weights, and more protected slots than the budget holds, go to
  *   the lowest slot first; a NaN weight ranks below every number. Kept slots below the budget stay
- *   where they are; kept slots beyond it move, in order, into the free slots, in order (keys are
- *   cached with their rotary position applied, so the order of slots carries no meaning beyond
- *   pos). Only what moves is read and written.
+ *   where they are; kept slots beyond it move, in order, into the free slots, in order (whatever the
+ *   caller does to keys for their position, a rotation for instance, it does before it appends
+ *   them, so the order of slots carries no meaning beyond pos). Only what moves is read and written.
  *   acc_out, pos_out ([batch][kv_heads][S], S as acc and pos) receive the weights and
  *   positions of the slots kept; they may be acc and pos themselves. Entries beyond the new length
  *   are left as they are. lens_out (apart from lens and seen) receives min(lens, budget). Slots at and beyond
@@ -517,7 +520,8 @@ KQ_API kq_status kq_kv_evict(const kq_kv_cache* cache, const int32_t* lens, cons
  *   recorded in info as -KQ_ERR_INVALID_ARG, with logp = NaN. A row of -infinity only has lse =
  *   logp = top_logp = -infinity and entropy 0. A row with a NaN or +infinity has NaN results
  *   (top_id then ranks NaN above every number).
- *   V <= 2^20. fp32 arithmetic; no workspace.
+ *   V <= 2^20. fp32 arithmetic with approximate powers of two (2^-22): results are off by about one
+ *   unit of fp32, terms that cancel in a row whose maximum is 2^24 to 2^30 by up to 2^-16. No workspace.
  * kq_token_logprobs_grad: the gradient of sum_t (g_logp_t logp_t + g_entropy_t entropy_t):
  *     grad_v = g_logp (delta(v, target) - p_v) - g_entropy p_v (ln p_v + entropy)
  *   with lse and entropy from kq_token_logprobs (entropy and g_entropy may both be NULL). grad

@@ -83,7 +83,8 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
 }
 __device__ __forceinline__ float2 unpack_f16(uint32_t x) { return __half22float2(*reinterpret_cast<const __half2*>(&x)); }
 // Two codes of a word, nibbles 0 and 4 of x (ODD: 1 and 5), as the A operand. Plain: the masked
-// bits, subnormals c 2^-24 (ODD: 16 c 2^-24). CENTRED: c - 8, through 1024 + c (ODD: 1024 + 16 c, over 16).
+// bits, subnormals c 2^-24 (ODD: 16 c 2^-24). CENTRED: c - 8, through 1024 + c (ODD: 1024 + 16 c, over 16): the well-known
+// way from small whole numbers to floats, their bits in the mantissa of a power of two that is then taken off.
 template <bool CENTRED, bool ODD>
 __device__ __forceinline__ uint32_t codes(uint32_t x) {
     constexpr uint32_t mask = ODD ? 0x00F000F0u : 0x000F000Fu;

@@ -101,7 +101,8 @@ __device__ __forceinline__ Two add2(Two a, Two b) {
 
 // What turns a row's values into codes: codes8 computes rint(RN(RN(x - off) / s)), RN being the rounding to
 // float32, from y, about 1 / s, without a division or a branch (51k tokens of 8 heads, bf16: 100 -> 63 us against
-// divisions where a reciprocal came near a tie). q = RN(d y) is a few units u in the last place off d / s, and the scale has 8 bits, so
+// divisions where a reciprocal came near a tie). It is Markstein's correction of a quotient by its exact remainder
+// (kq_common.cuh names the paper), with an argument of its own for scales of 8 bits. q = RN(d y) is a few units u in the last place off d / s, and the scale has 8 bits, so
 // q s and d are both whole multiples of u ulp(s): the remainder d - q s is one of a few hundred of them and exact. RN(q +
 // (d - q s) y) then rounds a number within 2^-20 u of d / s; the nearest that d / s can be to the middle between two
 // floats is 2^-9 u (d minus such a middle times s is such a multiple again, halved, and not 0: the

@@ -2,9 +2,10 @@
 
 QuantizedLinear applies a layer that LayerPipeline quantized (kq_pack_codes, kq_infer);
 KvCache owns a pool of pages and strings together kq_kv_append, kq_kv_attend, kq_kv_evict and
-kq_kv_read for a batch of sequences; AttentionBlock is one attention sublayer over both. Every
-step of the computation runs in libkronq's kernels, on the current stream, without waiting for
-the device; `KvCache.check` reads the device error word.
+kq_kv_read for a batch of sequences; AttentionBlock is one attention sublayer over both, without the
+norm before it and the rotation of queries and keys, which a model puts around and between. Products,
+cache, attention and scoring run in libkronq's kernels, on the current stream, without waiting for the
+device (`KvCache.append` says when it has to); `KvCache.check` reads the device error word.
 
 `python -m paper_2607_07964_gb300.serving` quantizes the projections of a small random model,
 feeds prompts of different lengths, decodes greedily with eviction, and prints the log
@@ -186,7 +187,8 @@ class KvCache:
 
 
 class AttentionBlock:
-    """x + W_o attention(W_q x, W_k x, W_v x) with quantized projections, tokens of several sequences packed."""
+    """x + W_o attention(W_q x, W_k x, W_v x) with quantized projections, tokens of several sequences packed (start and
+    most as KvCache.append takes them). Queries and keys are not rotated."""
 
     def __init__(self, proj: dict, heads: int, cache: KvCache):
         self.proj, self.heads, self.cache = proj, heads, cache
