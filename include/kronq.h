@@ -521,7 +521,8 @@ KQ_API kq_status kq_kv_evict(const kq_kv_cache* cache, const int32_t* lens, cons
  *   logp = top_logp = -infinity and entropy 0. A row with a NaN or +infinity has NaN results
  *   (top_id then ranks NaN above every number).
  *   V <= 2^20. fp32 arithmetic with approximate powers of two (2^-22): results are off by about one
- *   unit of fp32, terms that cancel in a row whose maximum is 2^24 to 2^30 by up to 2^-16. No workspace.
+ *   unit of fp32, whatever the row's maximum, but log probabilities and entropy by up to 2^-12 where
+ *   that is between 2^24 and 2^30 in size (neighbouring logits then differ by 2 to 128). No workspace.
  * kq_token_logprobs_grad: the gradient of sum_t (g_logp_t logp_t + g_entropy_t entropy_t):
  *     grad_v = g_logp (delta(v, target) - p_v) - g_entropy p_v (ln p_v + entropy)
  *   with lse and entropy from kq_token_logprobs (entropy and g_entropy may both be NULL). grad

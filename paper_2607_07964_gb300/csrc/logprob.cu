@@ -293,7 +293,8 @@ __global__ void __launch_bounds__(NT, NT >= kSplit ? 1 : 1536 / NT) logprob_kern
     int best_group = 0, n_mine = 0;   // of this thread's groups
     auto take = [&](float top_value, const float* v, int n) {
         if (top_value > ref + kSlack) {
-            const float nr2 = top_value * kLog2e, f = ref == kFloor ? 0.0f : ex2(ref2 - nr2);
+            // the rounded product, in the difference as in t: not to be fused with the subtraction
+            const float nr2 = __fmul_rn(top_value, kLog2e), f = ref == kFloor ? 0.0f : ex2(ref2 - nr2);
             w = f > 0.0f ? f * fmaf(z, ref2 - nr2, w) : 0.0f;
             z *= f;
             ref = top_value;

@@ -109,3 +109,27 @@ def test_rows_whose_logits_are_all_large(V, rows, dtype):
     exact = m[:, 0].double() + want
     assert ((lse - exact).abs() <= 2.0 ** -22 * exact.abs()).all()
     assert (ids[:, 0] == 5).all() and ((tl[:, 0] + want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("T,V,top", [(1, 900, 3), (200, 5003, 3), (400, 28505, 5), (3, 60000, 2), (40, 128000, 0), (400, 128000, 20)])
+@pytest.mark.parametrize("shift", [0, 3e3, -3e5, 3e6, -1.5e7, -2e7, 1e8, -9e8])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_shift_of_all_logits_costs_no_precision(T, V, top, shift, dtype):
+    """Logits spread by some 30 about a common value: differences within a row are exact, so the bound does not grow
+    with the shift. A term is off by 2^-24 of its own size and a power of two by 2^-21: 2^-18 (1 + |value|) in all up to 2^24, and
+    up to 2^30, where the reference is off by up to 64 powers of two (2^-18 of rounding, three times), 2^-16 (1 + |value|).
+    Rounding the difference of a log-sum costs 2^-24 of it twice."""
+    g = torch.Generator(DEV).manual_seed(V)
+    x = (torch.randn(T, V, device=DEV, generator=g) * 30 + shift).to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    target = torch.randint(0, V, (T,), device=DEV, generator=g)
+    logp, h, lse, ids, tl = _run(x, target, max(top, 1))
+    lp = torch.log_softmax(x.double(), 1)
+    eps = 2.0 ** -18 if abs(shift) < 2 ** 24 else 2.0 ** -16
+    want = lp.gather(1, target[:, None])[:, 0]
+    entropy = -(lp.exp() * lp).sum(1)
+    tops = torch.sort(x, dim=1, descending=True, stable=True).indices[:, :max(top, 1)]
+    assert torch.equal(ids.long(), tops)
+    for got, exact in ((logp, want), (h, entropy), (tl, lp.gather(1, tops))):
+        assert ((got - exact).abs() <= eps * (1 + exact.abs())).all(), float(((got - exact).abs() / (1 + exact.abs())).max())
+    exact = torch.logsumexp(x.double(), 1)
+    assert ((lse - exact).abs() <= 2.0 ** -18 + 2.0 ** -22 * exact.abs()).all()
