@@ -44,3 +44,28 @@ def test_numpy_values_are_those_of_their_codes():
     row[:2] = -5, 10
     cache.put(0, 0, 0, 1, row * np.float32(1.25 * 2.0 ** 109))
     assert ref.quantize(row[None])[0][0, 2] == 12 and cache.rows(0, 0, 1, 1)[0][0, 2] == 8.75 * 2.0 ** 109
+
+
+@pytest.mark.parametrize("n", [9, 70, 333])
+@pytest.mark.parametrize("dim,group", [(64, 4), (128, 5), (64, 12), (128, 16)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("order", ["rising", "falling", "mixed"])
+def test_attend_over_values_whose_sizes_the_weights_even_out(n, dim, group, dtype, order):
+    """Value rows from 2^-50 to 2^50, and keys that give the larger ones the smaller weights: query 0 weighs them so that all
+    count alike, the next ones lean to the large or to the small, the last sees the keys reversed. A row's result is what its own
+    weights make of it, whatever lies beside."""
+    rng = np.random.default_rng(n + dim)
+    cache = kv._pool(1, n, 16, 1, dim, rng)
+    power = np.linspace(-50, 50, n)
+    power = power[::-1] if order == "falling" else rng.permutation(power) if order == "mixed" else power
+    for j in range(n):
+        key = 0.01 * rng.standard_normal(dim)
+        key[0] = -power[j] * np.log(2)
+        cache.put(0, 0, j, 0, key.astype(np.float32))
+        cache.put(0, 0, j, 1, (rng.standard_normal(dim) * 2.0 ** power[j]).astype(np.float32))
+    q = 0.01 * rng.standard_normal((1, group, dim))
+    q[0, :, 0] = np.resize([1, 1.5, 0.5, -1, 0.02, 2.5], group)
+    q = kv._rounded(q, dtype)
+    acc0 = np.zeros((1, 1, n), np.float32)
+    out, lse, acc = kv._run_attend(cache, q.to(kv.DEV), [1], [n], 1, 1.0, True, dtype, acc0, n)
+    kv._check_attend(cache, q, [1], [n], 1, 1.0, dtype, out, lse, acc, acc0)
