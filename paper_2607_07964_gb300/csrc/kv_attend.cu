@@ -38,9 +38,9 @@
 // scores are kept and kv_weight_kernel turns them into weights: 8 bytes a slot and row, written
 // and read, in exchange for not reading the keys twice.
 //
-// Measured, 64 query heads on 8, D = 128, bf16: 64 sequences of up to 8192 slots (360 MB) 77 us for
+// Measured, 64 query heads on 8, D = 128, bf16: 64 sequences of up to 8192 slots (360 MB) 78 us for
 // the kernel, of which the copies run 58 us at 6.2 TB/s and the rest is its start and the spread of the
-// warps' ends; 85 us with the joining. 16 of up to 131072 slots (1.5 GB) 264 us, 5.6 TB/s.
+// warps' ends; 85 us with the joining. 16 of up to 131072 slots (1.44 GB) 271 us, 5.3 TB/s; 286 us where it keeps scores.
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
