@@ -10,9 +10,10 @@
  *   4. column-wise OBS sweep with b-bit asymmetric grids      (kq_obs_quantize)
  * with the GPTAQ drift correction as an option (kq_accum_drift, kq_gptaq_p, and the Pt
  * argument of kq_obs_quantize), inference with the quantized layer (kq_pack_codes,
- * kq_infer), decoding with a 4-bit key/value cache (kq_kv_append, kq_kv_attend, kq_kv_evict,
- * kq_kv_read), scoring (kq_token_logprobs and its gradient), plus two check-only calls
- * (kq_dequant_revert, kq_proxy_loss).
+ * kq_infer), rotary positions and norms of queries and keys (kq_qk_rotate and its gradient),
+ * decoding with a 4-bit key/value cache (kq_kv_append, kq_kv_attend, kq_kv_attend_window,
+ * kq_kv_evict, kq_kv_read), scoring (kq_token_logprobs and its gradient, kq_linear_logprobs and
+ * its own), plus two check-only calls (kq_dequant_revert, kq_proxy_loss).
  *
  * Conventions shared by every call
  *   - Tokens are rows: X is [T x d_in], G is [T x d_out]; the paper stacks tokens as
@@ -109,8 +110,8 @@ KQ_API kq_status kq_selftest_timeout(int* info, int64_t limit_us, kq_stream_t st
  * kq_debug_build: 1 for the debug build, 0 otherwise.
  * kq_debug_status: synchronizes the device, then *unit = the first source file (0 api,
  *   1 syrk, 2 biip, 3 chol, 4 obs, 5 trail_tc, 6 gptaq, 7 infer, 8 check, 9 kv_store,
- *   10 kv_attend, 11 kv_evict, 12 logprob) whose checks
- *   failed and *line = its first failing line, or *unit = -1 and *line = 0 when none did
+ *   10 kv_attend, 11 kv_evict, 12 logprob, 13 rotate,
+ *   14 linear_logprob) whose checks failed and *line = its first failing line, or *unit = -1 and *line = 0 when none did
  *   (always so in the normal build); reset clears the recorded lines.
  * kq_selftest_bounds: writes buf[i] = i for i = 0 .. n under a check against n; buf must
  *   hold n + 1 floats, so every write stays inside it in either build. The debug build skips
@@ -410,6 +411,51 @@ KQ_API kq_status kq_infer(const uint32_t* packed, const float* scale, const int3
                           int* info, void* ws, size_t ws_bytes, kq_stream_t stream);
 
 /* ------------------------------------------------------------------------------------
+ * Norms and rotary positions of queries and keys, between the projections and the cache (no
+ * counterpart in the paper, whose layers end at their products).
+ *
+ * kq_qk_rotate: each row x of dim values (a token's head) becomes
+ *     n = x r w, r = (mean(x^2) + eps)^(-1/2)   where its side has a weight w [dim], else n = x;
+ *   then its first rot values are rotated in pairs (a, b): values (2 j, 2 j + 1) when interleaved,
+ *   else (j, j + rot / 2), by the angle of the token's position p and pair j,
+ *     (a', b') = scale (a cos - b sin, b cos + a sin),   angle = 2 pi p freq[j] / 2^64;
+ *   the others are n. freq [rot / 2]: the turns of one position as 64-bit fractions (theta radians:
+ *   theta 2^64 / (2 pi)), so that p freq, whole numbers that wrap at a turn, is exact for every p. scale
+ *   is what a rotation stretched for long contexts multiplies queries and keys by (else 1).
+ *   Positions: pos [T], or with start [batch + 1] and first [batch] (as kq_kv_append's start and seen):
+ *   first[b] + i - start[b] for token i of sequence b, tokens of no sequence being left as they were; or the
+ *   token's index in the call where all are NULL.
+ *   q, k and their outputs are of dtype KQ_BF16 or KQ_F32, [T][heads][dim] with token and head strides in
+ *   elements and unit stride in dim; an output may be its input. k and k_out may be NULL together. Weights
+ *   are of the same type and may each be NULL. dim <= 256, rot even, 0 <= rot <= dim. fp32 arithmetic, one rounding.
+ * kq_qk_rotate_grad: with gq, gk the gradients of the outputs, q_out and k_out receive those of q and k (an
+ *   output may be its gq or gk), gq_weight and gk_weight [dim] fp32 (nullable) those of the weights, summed over tokens and
+ *   heads in an order that depends on the sizes only. q and k themselves are read where there is a weight, and may
+ *   be NULL elsewhere.
+ *   ws: kq_qk_rotate_grad_workspace(T, dim) bytes, 256-byte aligned, needed with a weight's gradient.
+ * ---------------------------------------------------------------------------------- */
+typedef struct kq_rotation {
+    const int64_t* freq;
+    int64_t rot;
+    const int32_t *pos, *start, *first;
+    int64_t batch;
+    int interleaved;
+    float scale;
+} kq_rotation;
+typedef struct kq_heads {
+    void* data;
+    int64_t heads, token_stride, head_stride;
+} kq_heads;
+KQ_API kq_status kq_qk_rotate(const kq_rotation* r, int dtype, int64_t T, int64_t dim, const kq_heads* q, const kq_heads* k,
+                              const kq_heads* q_out, const kq_heads* k_out, const void* q_weight, const void* k_weight,
+                              float eps, kq_stream_t stream);
+KQ_API size_t kq_qk_rotate_grad_workspace(int64_t T, int64_t dim);
+KQ_API kq_status kq_qk_rotate_grad(const kq_rotation* r, int dtype, int64_t T, int64_t dim, const kq_heads* q,
+                                   const kq_heads* k, const kq_heads* gq, const kq_heads* gk, const kq_heads* q_out,
+                                   const kq_heads* k_out, const void* q_weight, const void* k_weight, float eps,
+                                   float* gq_weight, float* gk_weight, void* ws, size_t ws_bytes, kq_stream_t stream);
+
+/* ------------------------------------------------------------------------------------
  * Decoding with a 4-bit key/value cache (serving a quantized model; no counterpart in the
  * paper, whose inference ends at the layer products of kq_infer).
  *
@@ -487,6 +533,16 @@ KQ_API kq_status kq_kv_attend(const kq_kv_cache* cache, const void* q, int dtype
                               const int32_t* lens, float scale, void* out, float* lse, float* acc, int64_t S,
                               int* info, void* ws, size_t ws_bytes, kq_stream_t stream);
 
+/* kq_kv_attend_window: kq_kv_attend with a sliding window: a token that sees the slots below n there
+ *   sees those with n - window <= j < n, and j < sink, here (window >= 1, sink >= 0). Pages whose slots no token
+ *   of the call sees are neither looked up in the table nor read, so their entries may be stale; a slot's number is
+ *   its position, so not after an eviction. No accumulated weights. The workspace is kq_kv_attend_workspace's with S = 0.
+ */
+KQ_API kq_status kq_kv_attend_window(const kq_kv_cache* cache, const void* q, int dtype, int64_t T, int64_t q_heads,
+                                     int64_t q_token_stride, int64_t q_head_stride, const int32_t* start,
+                                     const int32_t* lens, float scale, int64_t window, int64_t sink, void* out, float* lse,
+                                     int* info, void* ws, size_t ws_bytes, kq_stream_t stream);
+
 /* kq_kv_evict: cuts every sequence and head with more than `budget` slots back to `budget`
  *   slots, each head on its own. Kept are the slots whose position is among the last `recent`
  *   (pos >= seen[b] - recent) or the first `sink` (pos < sink), then those of the largest
@@ -540,6 +596,37 @@ KQ_API kq_status kq_token_logprobs_grad(const void* logits, int dtype, int64_t T
                                         const int64_t* target, const float* lse, const float* entropy,
                                         const float* g_logp, const float* g_entropy, void* grad, int64_t ld_grad,
                                         int* info, kq_stream_t stream);
+
+/* ------------------------------------------------------------------------------------
+ * Log probabilities straight from hidden states: the head's product with them inside, so that no logits are kept
+ * (262144 tokens of a 128000 vocabulary would be 67 GB in bf16).
+ *
+ * kq_linear_logprobs: kq_token_logprobs's logp, entropy and lse (entropy, lse nullable) for the logits z = x W^T,
+ *   x [T][d] and W [V][d] bf16 (row strides ldx, ldw; 16-byte aligned, d and the strides multiples of 8). Products are
+ *   exact, sums fp32: the tensor cores' over 512 of d, then in registers, so a logit is off by 2^-18 of the
+ *   sum of its products' sizes at most (2^-22 is ordinary). target as there: a negative one is not scored, one >= V recorded in info with logp = NaN. A row
+ *   with a NaN or +infinite logit has NaN results. T <= KQ_LINEAR_MAX_T, V <= 2^20, d <= 65536.
+ *   ws: kq_linear_logprobs_workspace(T, V, d) bytes, 256-byte aligned.
+ * kq_linear_logprobs_grad: the gradients of sum_t (g_logp_t logp_t + g_entropy_t entropy_t) with respect to x and W,
+ *   bf16 gx [T][d] and gw [V][d] (row strides ldgx, ldgw; either may be NULL), from kq_linear_logprobs's lse
+ *   and entropy (entropy and g_entropy may both be NULL). The logits are computed again, a piece of the vocabulary at a time;
+ *   their gradient enters both products in bf16, as kq_token_logprobs_grad would give it, the sums are fp32 and rounded once.
+ *   A row with a negative target has no g_logp part; a target >= V is recorded in info, its row's g_logp part left
+ *   out. gx and gw must not overlap x, W or each other. Results do not depend on the order in which blocks run.
+ *   ws: kq_linear_logprobs_grad_workspace(T, V, d) bytes, 256-byte aligned (2 pieces of logits' gradients of about
+ *   2^25 values, fp32 gx).
+ * info (nullable): also -KQ_ERR_TIMEOUT where a kernel gave up a wait.
+ * ---------------------------------------------------------------------------------- */
+#define KQ_LINEAR_MAX_T (1 << 24)
+KQ_API size_t kq_linear_logprobs_workspace(int64_t T, int64_t V, int64_t d);
+KQ_API kq_status kq_linear_logprobs(const uint16_t* x, int64_t T, int64_t d, int64_t ldx, const uint16_t* w, int64_t V,
+                                    int64_t ldw, const int64_t* target, float* logp, float* entropy, float* lse, int* info,
+                                    void* ws, size_t ws_bytes, kq_stream_t stream);
+KQ_API size_t kq_linear_logprobs_grad_workspace(int64_t T, int64_t V, int64_t d);
+KQ_API kq_status kq_linear_logprobs_grad(const uint16_t* x, int64_t T, int64_t d, int64_t ldx, const uint16_t* w, int64_t V,
+                                         int64_t ldw, const int64_t* target, const float* lse, const float* entropy,
+                                         const float* g_logp, const float* g_entropy, uint16_t* gx, int64_t ldgx, uint16_t* gw,
+                                         int64_t ldgw, int* info, void* ws, size_t ws_bytes, kq_stream_t stream);
 
 /* ------------------------------------------------------------------------------------
  * Check-only calls (not part of the timed path).

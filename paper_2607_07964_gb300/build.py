@@ -22,7 +22,7 @@ LIB = os.path.join(HERE, "libkronq.so")
 BUILD_DEBUG = os.path.join(HERE, "_build_debug")
 LIB_DEBUG = os.path.join(HERE, "libkronq_debug.so")
 SOURCES = ["kq_api.cu", "syrk.cu", "biip.cu", "chol.cu", "obs.cu", "trail_tc.cu", "gptaq.cu", "infer.cu", "check.cu",
-           "kv_store.cu", "kv_attend.cu", "kv_evict.cu", "logprob.cu"]
+           "kv_store.cu", "kv_attend.cu", "kv_evict.cu", "logprob.cu", "rotate.cu", "linear_logprob.cu"]
 HEADERS = sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".cuh")) + [
     os.path.join(ROOT, "include", "kronq.h")]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]

@@ -233,6 +233,8 @@ int debug_read_kv_store(int);
 int debug_read_kv_attend(int);
 int debug_read_kv_evict(int);
 int debug_read_logprob(int);
+int debug_read_rotate(int);
+int debug_read_linear_logprob(int);
 }  // namespace kq
 
 extern "C" int kq_debug_build(void) {
@@ -249,7 +251,7 @@ extern "C" kq_status kq_debug_status(int* unit, int* line, int reset) {
                                      kq::debug_read_chol,     kq::debug_read_obs,   kq::debug_read_trail_tc,
                                      kq::debug_read_gptaq,    kq::debug_read_infer, kq::debug_read_check,
                                      kq::debug_read_kv_store, kq::debug_read_kv_attend, kq::debug_read_kv_evict,
-                                     kq::debug_read_logprob};
+                                     kq::debug_read_logprob,  kq::debug_read_rotate, kq::debug_read_linear_logprob};
     KQ_CUDA(cudaDeviceSynchronize());
     int u = -1, l = 0;
     for (int k = 0; k < static_cast<int>(sizeof(readers) / sizeof(readers[0])); ++k) {

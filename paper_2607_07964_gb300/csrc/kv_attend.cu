@@ -46,6 +46,7 @@
 #include <type_traits>
 
 #include "kv_common.cuh"
+#include "pdl.cuh"
 
 namespace kq {
 namespace {
@@ -109,8 +110,6 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
                  "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(smem_u32(bar))
                  : "memory");
 }
-__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // 8 consecutive values; vec: they can be read 16 bytes at a time.
 __device__ __forceinline__ void load8(const float* p, bool vec, float (&x)[8]) {
@@ -154,6 +153,7 @@ struct Attend {
     struct Joint* joint;               // of each item in the list of work
     int64_t* items;                    // how many there are
     int64_t most_items;                // as many as the sequences of an ordered start can make
+    int32_t window, sink;              // with a window: a token sees its last `window` slots and the first `sink`
     float* part;                       // [2 pieces][rows][D + 2]: sums, maximum, sum of weights
     int* info;
 };
@@ -165,13 +165,16 @@ struct Joint {
     int32_t token;           // the sequence's first token
 };
 
+// Steps that hold the slots that stay visible.
+__device__ __forceinline__ int64_t first_steps(const Attend& p) { return (static_cast<int64_t>(p.sink) + kStep - 1) / kStep; }
+
 // Sequence b's share of the work.
 struct Seq {
     int32_t nq, rows_tiles, steps;   // queries, groups of ROWS query rows, steps (at least 1)
     int32_t n;                       // length
     int32_t first;                   // its first token
 };
-template <int ROWS>
+template <int ROWS, bool WINDOW>
 __device__ __forceinline__ Seq sequence(const Attend& p, int b, int* info) {
     Seq s;
     const int64_t s0 = p.start[b], s1 = p.start[b + 1];
@@ -184,6 +187,13 @@ __device__ __forceinline__ Seq sequence(const Attend& p, int b, int* info) {
     }
     s.rows_tiles = static_cast<int32_t>((static_cast<int64_t>(s.nq) * p.group + ROWS - 1) / ROWS);
     s.steps = max(1, (s.n + kStep - 1) / kStep);
+    if constexpr (WINDOW) {
+        // ROWS rows are of at most this many tokens; their windows together, wherever they begin, and the first slots lie in
+        // `most` steps
+        const int64_t tokens = min(static_cast<int64_t>(s.nq), static_cast<int64_t>((ROWS - 2) / p.group + 2));
+        const int64_t most = first_steps(p) + (p.window + tokens - 1 + 2 * (kStep - 1)) / kStep;
+        s.steps = static_cast<int32_t>(min(static_cast<int64_t>(s.steps), most));
+    }
     return s;
 }
 struct Work {
@@ -232,19 +242,21 @@ struct Place {
     int b, h, rt;
     int v;          // place in the item's kItemCost + steps
     int step;       // the step that the warp's part of the item begins with
+    int skip, turn; // with a window: steps from `turn` on lie `skip` steps further on in the sequence
+    int low;        // and the first slot that a window of the item's rows holds
     int64_t item;   // its number in the list
     Seq s;
 };
-template <int ROWS>
+template <int ROWS, bool WINDOW>
 __device__ __forceinline__ void next_sequence(const Attend& p, Place& at) {
     do {
         ++at.b;
         if (at.b >= p.c.batch) return;
-        at.s = sequence<ROWS>(p, at.b, nullptr);
+        at.s = sequence<ROWS, WINDOW>(p, at.b, nullptr);
     } while (at.s.rows_tiles == 0);
 }
 // Past the rest of this row group.
-template <int ROWS>
+template <int ROWS, bool WINDOW>
 __device__ __forceinline__ void next_item(const Attend& p, Place& at) {
     at.v = 0;
     ++at.item;
@@ -252,7 +264,7 @@ __device__ __forceinline__ void next_item(const Attend& p, Place& at) {
     at.rt = 0;
     if (++at.h < p.c.kv_heads) return;
     at.h = 0;
-    next_sequence<ROWS>(p, at);
+    next_sequence<ROWS, WINDOW>(p, at);
 }
 
 template <typename T, int D, int NT>
@@ -267,18 +279,22 @@ struct Shape {
 
 // A warp's state for a group of NT x 8 query rows. A lane (g8, t4) has columns 2 t4 and
 // 2 t4 + 1 of each 8 rows.
-template <typename T, int D, int NT>
+template <typename T, int D, int NT, bool WINDOW>
 struct Rows {
     static constexpr bool kSplit = sizeof(T) == 4;   // fp32: two fp16 halves of q and of the weights
     static constexpr int kWords = D / 32;            // code words of a row that a lane of a quad takes
     uint32_t bq[NT][kWords][4], bl[NT][kSplit ? kWords : 1][4];   // q, and what fp16 left of it
     float alpha[NT][2], gamma[NT][2];                // score = alpha (s S + o gamma), S from the tensor cores
     int32_t lim[NT][2];                              // slots seen
+    int32_t low[NT][2], sink;                        // with a window: of them from low on, and the first `sink`
     int64_t put[NT][2];                              // where scores go
     float o[NT][D / 16][4], m[NT][2], l[NT][2], off[NT][2];
     float mid[NT][4];                                // 8 times the sum of the weights in o (codes not centred)
     uint32_t unit[NT][2];                            // biased exponent of the power of two that p s' enters o with
 
+    __device__ __forceinline__ bool sees(int nt, int k, int slot) const {
+        return slot < lim[nt][k] && (!WINDOW || slot >= low[nt][k] || slot < sink);
+    }
     // o = corr (o - mid), mid = 0
     __device__ __forceinline__ void settle_mid(int nt, const float (&corr)[2]) {
 #pragma unroll
@@ -361,7 +377,7 @@ struct Rows {
                         float& x = s[gi][nt][2 * hf + k];
                         if constexpr (kSplit) x += s2[nt][0][2 * hf + k] + s2[nt][1][2 * hf + k];
                         x = fmaf(ks, x, ko * gamma[nt][k]);
-                        if (MASK && slot + 16 * gi + tok + 8 * hf >= lim[nt][k]) x = -INFINITY;
+                        if (MASK && !sees(nt, k, slot + 16 * gi + tok + 8 * hf)) x = -INFINITY;
                     }
             }
         }
@@ -427,7 +443,7 @@ struct Rows {
                         const float pr = ex2(fmaf(alpha[nt][k], x, -m[nt][k]));
                         l[nt][k] += pr;
                         if (MASK) {
-                            const bool in = slot + 16 * gi + tok + 8 * hf < lim[nt][k];
+                            const bool in = sees(nt, k, slot + 16 * gi + tok + 8 * hf);
                             off[nt][k] += in ? pr * vo[gi][hf] : 0.0f;
                             x = in ? pr * vs[gi][hf] : 0.0f;
                         } else {
@@ -528,29 +544,39 @@ struct Rows {
     }
 };
 
+// The place in the sequence of an item's step.
+template <bool WINDOW>
+__device__ __forceinline__ int step_at(const Place& at, int step) {
+    return WINDOW && step >= at.turn ? step + at.skip : step;
+}
+
 // A warp's ring of staged granules. Lane l holds the address of granule l & 1 of step l / 2 of the
 // kAhead steps around the next load; the page numbers of the kAhead steps after them are on their
 // way. A warp refills a stage when its lanes have read it, so no other warp is waited for.
-template <int D>
+template <int D, bool WINDOW>
 struct Feed {
     static constexpr int kBytes = kGranule * (D + 8);
     const uint8_t* src;   // of this lane's granule
     int32_t next;         // its page number kAhead steps later
 
-    __device__ __forceinline__ int slot_of(int step, int k, int lane) const {
-        return (step + k + (lane >> 1)) * kStep + (lane & 1) * kGranule;
+    __device__ __forceinline__ int slot_of(const Place& at, int k, int lane) const {
+        return step_at<WINDOW>(at, at.step + k + (lane >> 1)) * kStep + (lane & 1) * kGranule;
+    }
+    // Whether a row may see a slot of the granule: others are not asked for, as their pages may be gone.
+    __device__ __forceinline__ bool seen(const Attend& p, const Place& at, int slot) const {
+        return slot < at.s.n && (!WINDOW || slot < p.sink || slot > at.low - kGranule);
     }
     // the page number of this lane's granule in the steps from k, of a segment of seg steps
     __device__ __forceinline__ int32_t fetch(const Attend& p, const Place& at, int k, int seg, int lane) const {
-        const int slot = slot_of(at.step, k, lane);
-        if (k + (lane >> 1) >= seg || slot >= at.s.n) return 0;
+        const int slot = slot_of(at, k, lane);
+        if (k + (lane >> 1) >= seg || !seen(p, at, slot)) return 0;
         const int32_t id = p.c.table[static_cast<int64_t>(at.b) * p.c.table_ld + slot / p.c.page];
         if (id >= 0 && id < p.c.pages) return id;
         record_error(p.info, -KQ_ERR_INVALID_ARG);
         return 0;
     }
     __device__ __forceinline__ void place(const Attend& p, const Place& at, int k, int32_t id, int lane) {
-        const int slot = slot_of(at.step, k, lane);
+        const int slot = slot_of(at, k, lane);
         src = p.c.data + (static_cast<int64_t>(id) * p.c.kv_heads + at.h) * kv_head_bytes(p.c) + slot % p.c.page * (D + 8);
     }
     // Step k's granules into a stage (k < seg). Both are one run unless a page can end between them.
@@ -559,31 +585,32 @@ struct Feed {
             place(p, at, k, next, lane);
             next = fetch(p, at, k + kAhead, seg, lane);
         }
-        const int left = at.s.n - (at.step + k) * kStep;
-        const int many = left > kGranule ? 2 : left > 0 ? 1 : 0;
+        const int slot = step_at<WINDOW>(at, at.step + k) * kStep;
+        const bool one = seen(p, at, slot), two = seen(p, at, slot + kGranule);
+        const int many = one + two;
         const uint64_t a = __shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(src), 2 * (k % kAhead));
         uint64_t a2 = a + kBytes;
-        if (p.c.page % (2 * kGranule)) a2 = __shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(src), 2 * (k % kAhead) + 1);
+        if (WINDOW || p.c.page % (2 * kGranule)) a2 = __shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(src), 2 * (k % kAhead) + 1);
         if (lane == 0) {
             if (many == 0) {
                 mbar_arrive(bar);
             } else {
                 mbar_arrive_expect_tx(bar, many * kBytes);
                 const bool run = many == 1 || a2 == a + kBytes;
-                bulk_load(stage, reinterpret_cast<const void*>(a), run ? many * kBytes : kBytes, bar);
-                if (!run) bulk_load(stage + kBytes, reinterpret_cast<const void*>(a2), kBytes, bar);
+                if (!WINDOW || one) bulk_load(stage, reinterpret_cast<const void*>(a), run ? many * kBytes : kBytes, bar);
+                if (!run || (WINDOW && !one)) bulk_load(stage + kBytes, reinterpret_cast<const void*>(a2), kBytes, bar);
             }
         }
         __syncwarp();
     }
 };
 
-template <typename T, int D, int NT>
+template <typename T, int D, int NT, bool WINDOW>
 __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas) kv_attend_kernel(const Attend p) {
     using Sh = Shape<T, D, NT>;
     constexpr int kRows = Sh::kRows;
-    constexpr bool kSplit = Rows<T, D, NT>::kSplit;
-    constexpr int kWords = Rows<T, D, NT>::kWords;
+    constexpr bool kSplit = Rows<T, D, NT, WINDOW>::kSplit;
+    constexpr int kWords = Rows<T, D, NT, WINDOW>::kWords;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ uint64_t full[kWarps][kStages];
     __shared__ int abort_flag[kWarps];
@@ -606,7 +633,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas) kv_attend_ke
     const int run = (c.batch + kThreads - 1) / kThreads, b0 = min(tid * run, c.batch), b1 = min(b0 + run, c.batch);
     Work v = {0, 0}, lead;
     for (int b = b0; b < b1; ++b) {
-        const Work one = work_of(p, sequence<kRows>(p, b, blockIdx.x ? nullptr : p.info));
+        const Work one = work_of(p, sequence<kRows, WINDOW>(p, b, blockIdx.x ? nullptr : p.info));
         v.steps += one.steps, v.items += one.items;
     }
     const Work all = scan_add(v, scan_tmp, lead);
@@ -622,7 +649,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas) kv_attend_ke
         if (o0 < lead.steps || o0 >= lead.steps + v.steps) continue;
         Work at = lead;
         for (int b = b0; b < b1; ++b) {
-            const Seq s = sequence<kRows>(p, b, nullptr);
+            const Seq s = sequence<kRows, WINDOW>(p, b, nullptr);
             const Work one = work_of(p, s);
             if (o0 < at.steps + one.steps) {
                 found_b[i] = b;
@@ -659,6 +686,12 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas) kv_attend_ke
         const int seg = max(at.v + part_of - kItemCost, 0) - at.step;
         if (seg == 0) break;   // the warp's last, and the next warp's item
         const int rows = min(kRows, at.s.nq * p.group - at.rt * kRows);
+        const int least = visible(at.s.n, at.s.nq, at.rt * kRows / p.group);   // what the first row's token has before it
+        if constexpr (WINDOW) {
+            at.low = max(0, least - p.window);
+            at.turn = static_cast<int>(min(first_steps(p), static_cast<int64_t>(at.s.steps)));
+            at.skip = max(0, min(at.low / kStep - at.turn, (at.s.n + kStep - 1) / kStep - at.s.steps));
+        }
         if (at.step == 0 && lane == 0) {
             Joint j;
             j.first = static_cast<int32_t>(me);
@@ -670,10 +703,10 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas) kv_attend_ke
             if (at.item < p.most_items && KQ_IN_RANGE(at.item, p.most_items)) p.joint[at.item] = j;
             else record_error(p.info, -KQ_ERR_INVALID_ARG);   // sequences that overlap
         }
-        Feed<D> feed;
+        Feed<D, WINDOW> feed;
         const int32_t page_id = feed.fetch(p, at, 0, seg, lane);
         feed.next = feed.fetch(p, at, kAhead, seg, lane);
-        Rows<T, D, NT> R;
+        Rows<T, D, NT, WINDOW> R;
         float xs[NT][kWords][8];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -738,6 +771,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas) kv_attend_ke
                 R.gamma[nt][k] = __shfl_sync(0xffffffffu, gm, (2 * t4 + k) * 4);
                 const int i = crow / p.group;
                 R.lim[nt][k] = col < rows ? visible(at.s.n, at.s.nq, i) : 0;
+                if constexpr (WINDOW) R.low[nt][k] = R.lim[nt][k] - p.window, R.sink = p.sink;
                 R.put[nt][k] = ((static_cast<int64_t>(at.s.first + i) * c.kv_heads + at.h) * p.S) * p.group + crow % p.group;
                 R.m[nt][k] = kNone, R.l[nt][k] = 0.0f, R.off[nt][k] = 0.0f, R.unit[nt][k] = kTopUnit;
             }
@@ -748,8 +782,6 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas) kv_attend_ke
 #pragma unroll
             for (int j = 0; j < 4; ++j) R.mid[nt][j] = 0.0f;
         }
-        const int least = visible(at.s.n, at.s.nq, at.rt * kRows / p.group);   // what the first row sees, the others see
-
         // The steps that every row sees in full, then those with an end: two loops, so that the first one
         // carries its sums in place.
         auto turn = [&](int k, auto masked) {
@@ -758,7 +790,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas) kv_attend_ke
             uint64_t* bar = &full[warp][stage];
             if (__any_sync(0xffffffffu, !mbar_try_wait(bar, (it / kStages) & 1)))
                 fine_waits = __all_sync(0xffffffffu, mbar_wait(bar, (it / kStages) & 1, &abort_flag[warp]));
-            const int slot = (at.step + k) * kStep;
+            const int slot = step_at<WINDOW>(at, at.step + k) * kStep;
             if (fine_waits && (!decltype(masked)::value || slot < at.s.n))   // uniform over the warp
                 R.template step<decltype(masked)::value>(gr, slot, g8, t4, p.scores, p.group, k % kSettle == 0);
             __syncwarp();
@@ -768,8 +800,13 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas) kv_attend_ke
             }
             ++it;
         };
-        const int whole_steps = min(seg, least / kStep - at.step);
+        const int whole_steps = min(seg, least / kStep - at.step - (WINDOW ? at.skip : 0));
         int k = 0;
+        if constexpr (WINDOW) {   // before them those with first slots or a window's beginning, the last row's the latest
+            const int begin = visible(at.s.n, at.s.nq, (at.rt * kRows + rows - 1) / p.group) - p.window;
+            const int clear = begin <= 0 ? 0 : max(at.turn, (begin + kStep - 1) / kStep - at.skip) - at.step;
+            for (; k < min(seg, clear) && fine_waits; ++k) turn(k, std::true_type());
+        }
         for (; k < whole_steps && fine_waits; ++k) turn(k, std::false_type());
         for (; k < seg && fine_waits; ++k) turn(k, std::true_type());
         if (!fine_waits) break;
@@ -825,7 +862,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, D, NT>::kCtas) kv_attend_ke
         }
         w += part_of;
         at.v += part_of;
-        if (at.v == length) next_item<kRows>(p, at);
+        if (at.v == length) next_item<kRows, WINDOW>(p, at);
     }
     if (!fine_waits && lane == 0) {   // leave only when this warp's copies have landed
         record_error(p.info, -KQ_ERR_TIMEOUT);
@@ -937,7 +974,7 @@ __global__ void __launch_bounds__(256) kv_weight_kernel(const Attend p, float* _
     constexpr int kSlots = 4;
     pdl_wait();
     const int b = blockIdx.x / p.c.kv_heads, h = blockIdx.x % p.c.kv_heads;
-    const Seq s = sequence<8>(p, b, nullptr);
+    const Seq s = sequence<8, false>(p, b, nullptr);
     if (s.nq == 0) return;
     acc += (static_cast<int64_t>(b) * p.c.kv_heads + h) * p.S;
     for (int64_t s0 = static_cast<int64_t>(blockIdx.y) * (256 * kSlots) + threadIdx.x; s0 - threadIdx.x < s.n;
@@ -990,37 +1027,22 @@ __global__ void __launch_bounds__(256) kv_weight_kernel(const Attend p, float* _
     }
 }
 
-template <typename... Params, typename... Args>
-cudaError_t launch_after(void (*kern)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = block;
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kern, static_cast<Params>(args)...);
-}
-
 int64_t most_items(int64_t tokens, int64_t batch, int64_t group, int64_t kv_heads, int64_t rows) {
     return (tokens * group / rows + std::min(batch, tokens)) * kv_heads;
 }
 
-template <typename T, int D, int NT>
+template <typename T, int D, int NT, bool WINDOW>
 kq_status run_attend(Attend& p, cudaStream_t stream) {
     using Sh = Shape<T, D, NT>;
     p.most_items = most_items(p.tokens, p.c.batch, p.group, p.c.kv_heads, Sh::kRows);
     static std::atomic<uint64_t> done{0};
     KQ_TRY(once_per_device(done, [] {
-        KQ_CUDA(cudaFuncSetAttribute(kv_attend_kernel<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+        KQ_CUDA(cudaFuncSetAttribute(kv_attend_kernel<T, D, NT, WINDOW>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                      static_cast<int>(Sh::kSmem)));
         return KQ_OK;
     }));
     const int grid = std::min(kMaxRows / Sh::kRows, num_sms() * Sh::kCtas * kWarps) / kWarps;
-    KQ_CUDA(launch_after(kv_attend_kernel<T, D, NT>, dim3(grid), dim3(kThreads), Sh::kSmem, stream, p));
+    KQ_CUDA(launch_after(kv_attend_kernel<T, D, NT, WINDOW>, dim3(grid), dim3(kThreads), Sh::kSmem, stream, p));
     count_launch();
     // a sequence has ceil(queries group / rows) items a head: at most this many, and few of them have many
     // results each, with a block for each column to go through them
@@ -1048,14 +1070,16 @@ extern "C" size_t kq_kv_attend_workspace(int64_t T, int64_t q_heads, int64_t kv_
            static_cast<size_t>(T) * q_heads * S * sizeof(float);
 }
 
-extern "C" kq_status kq_kv_attend(const kq_kv_cache* cache, const void* q, int dtype, int64_t T, int64_t q_heads,
-                                  int64_t q_token_stride, int64_t q_head_stride, const int32_t* start,
-                                  const int32_t* lens, float scale, void* out, float* lse, float* acc, int64_t S, int* info,
-                                  void* ws, size_t ws_bytes, kq_stream_t stream_) {
+namespace {
+// Both calls; window 0: all slots.
+kq_status attend(const char* who, const kq_kv_cache* cache, const void* q, int dtype, int64_t T, int64_t q_heads,
+                 int64_t q_token_stride, int64_t q_head_stride, const int32_t* start, const int32_t* lens, float scale,
+                 int64_t window, int64_t sink, void* out, float* lse, float* acc, int64_t S, int* info, void* ws, size_t ws_bytes,
+                 kq_stream_t stream_) {
     KvView c;
-    KQ_TRY(kv_view(cache, "kq_kv_attend", &c));
+    KQ_TRY(kv_view(cache, who, &c));
     if (dtype != KQ_BF16 && dtype != KQ_F32) {
-        set_error("kq_kv_attend: dtype must be KQ_BF16 or KQ_F32");
+        set_error("%s: dtype must be KQ_BF16 or KQ_F32", who);
         return KQ_ERR_UNSUPPORTED;
     }
     const uintptr_t es = dtype == KQ_BF16 ? 2 : 4;
@@ -1063,14 +1087,14 @@ extern "C" kq_status kq_kv_attend(const kq_kv_cache* cache, const void* q, int d
         (T > 0 && (!q || !out)) || (acc && S < 1) || S > 0x7fffffffll || !(scale - scale == 0.0f) ||
         T * q_heads > 0x3fffffffll ||
         ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & (es - 1))) {
-        set_error("kq_kv_attend: q, out, start, lens must not be NULL, q_heads a multiple of kv_heads, T q_heads < 2^30, "
-                  "scale finite, S >= 1 with acc");
+        set_error("%s: q, out, start, lens must not be NULL, q_heads a multiple of kv_heads, T q_heads < 2^30, "
+                  "scale finite, S >= 1 with acc", who);
         return KQ_ERR_INVALID_ARG;
     }
     if (T == 0) return KQ_OK;
     const size_t need = kq_kv_attend_workspace(T, q_heads, c.kv_heads, c.dim, acc ? S : 0);
     if (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 255u)) {
-        set_error("kq_kv_attend: workspace must be 256-byte aligned and hold %zu bytes", need);
+        set_error("%s: workspace must be 256-byte aligned and hold %zu bytes", who, need);
         return KQ_ERR_WORKSPACE;
     }
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
@@ -1100,13 +1124,23 @@ extern "C" kq_status kq_kv_attend(const kq_kv_cache* cache, const void* q, int d
     // Up to 8 rows of a key/value head fill one accumulator tile; more take two, so that the cache is
     // read half as often (a tensor-core column costs the same whether a row fills it or not).
     const bool wide = p.group > 8 || T > c.batch;
-    kq_status st;
-    if (dtype == KQ_BF16)
-        st = c.dim == 128 ? (wide ? run_attend<__nv_bfloat16, 128, 2>(p, stream) : run_attend<__nv_bfloat16, 128, 1>(p, stream))
-                          : (wide ? run_attend<__nv_bfloat16, 64, 2>(p, stream) : run_attend<__nv_bfloat16, 64, 1>(p, stream));
-    else
-        st = c.dim == 128 ? (wide ? run_attend<float, 128, 2>(p, stream) : run_attend<float, 128, 1>(p, stream))
-                          : (wide ? run_attend<float, 64, 2>(p, stream) : run_attend<float, 64, 1>(p, stream));
+    constexpr int64_t kFar = 0x7fffffff;   // no sequence is longer
+    p.window = static_cast<int32_t>(std::min(window, kFar));
+    p.sink = static_cast<int32_t>(std::min(sink, kFar));
+    // a window that no sequence can outgrow is none
+    const bool limited = window > 0 && window < kv_capacity(c);
+    auto pick = [&](auto t, auto d, auto n) {
+        using E = decltype(t);
+        return limited ? run_attend<E, decltype(d)::value, decltype(n)::value, true>(p, stream)
+                       : run_attend<E, decltype(d)::value, decltype(n)::value, false>(p, stream);
+    };
+    auto pick_rows = [&](auto t, auto d) {
+        return wide ? pick(t, d, std::integral_constant<int, 2>()) : pick(t, d, std::integral_constant<int, 1>());
+    };
+    auto pick_dim = [&](auto t) {
+        return c.dim == 128 ? pick_rows(t, std::integral_constant<int, 128>()) : pick_rows(t, std::integral_constant<int, 64>());
+    };
+    const kq_status st = dtype == KQ_BF16 ? pick_dim(__nv_bfloat16()) : pick_dim(float());
     KQ_TRY(st);
     if (acc) {
         // enough blocks for two rounds of a full GPU, each going through its slots in steps of 1024
@@ -1118,4 +1152,25 @@ extern "C" kq_status kq_kv_attend(const kq_kv_cache* cache, const void* q, int d
         count_launch();
     }
     return KQ_OK;
+}
+}  // namespace
+
+extern "C" kq_status kq_kv_attend(const kq_kv_cache* cache, const void* q, int dtype, int64_t T, int64_t q_heads,
+                                  int64_t q_token_stride, int64_t q_head_stride, const int32_t* start,
+                                  const int32_t* lens, float scale, void* out, float* lse, float* acc, int64_t S, int* info,
+                                  void* ws, size_t ws_bytes, kq_stream_t stream) {
+    return attend("kq_kv_attend", cache, q, dtype, T, q_heads, q_token_stride, q_head_stride, start, lens, scale, 0, 0, out, lse,
+                  acc, S, info, ws, ws_bytes, stream);
+}
+
+extern "C" kq_status kq_kv_attend_window(const kq_kv_cache* cache, const void* q, int dtype, int64_t T, int64_t q_heads,
+                                         int64_t q_token_stride, int64_t q_head_stride, const int32_t* start,
+                                         const int32_t* lens, float scale, int64_t window, int64_t sink, void* out, float* lse,
+                                         int* info, void* ws, size_t ws_bytes, kq_stream_t stream) {
+    if (window < 1 || sink < 0) {
+        set_error("kq_kv_attend_window: window >= 1 and sink >= 0 needed");
+        return KQ_ERR_INVALID_ARG;
+    }
+    return attend("kq_kv_attend_window", cache, q, dtype, T, q_heads, q_token_stride, q_head_stride, start, lens, scale, window,
+                  sink, out, lse, nullptr, 0, info, ws, ws_bytes, stream);
 }

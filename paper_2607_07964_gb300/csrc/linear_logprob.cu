@@ -1,0 +1,745 @@
+// kq_linear_logprobs and kq_linear_logprobs_grad: log probabilities straight from hidden states, no logits kept.
+//
+// Mathematics. z = x W^T for T rows of hidden states x [T][d] and a head W [V][d]. For each row
+//     lse = ln sum_v e^(z_v),  logp = z_y - lse,  entropy = -sum_v p_v ln p_v,  p_v = e^(z_v - lse).
+// A tile of logits leaves, for each row and 128 columns, the maximum m, Z = sum 2^t and S = sum 2^t t with
+// t = log2(e) (z - m), and the target's logit where it has it. (The difference first: it is exact near the maximum, whatever
+// its size.) Joined: M = max m, lse = M + ln Z, entropy = (log2 Z - S / Z) ln 2.
+// Gradient of sum_t (g logp + h entropy): the logits' is
+//     D_v = g (delta(v, y) - p_v) - h p_v (ln p_v + entropy),   gx = D W,  gW = D^T x.
+// The vocabulary goes in pieces: D of a piece (logits computed again, from the log-sums) is held in bf16, read for
+// both products, and overwritten. bf16 has D's range and moves a sum of its terms by 2^-9 of the terms' size at
+// most, the size of the outputs' own rounding.
+//
+// What bounds it: the tensor cores where there are many rows (2 T V d operations a product), the bytes of W where there
+// are few. Layout: a cluster of two CTAs on two SMs holds a 256 x 256 tile (tcgen05 cta_group::2, each SM the
+// accumulator of 128 rows in tensor memory and half of each operand in shared memory); one warp issues the TMA
+// loads of 64-wide boxes into a ring, one the products, eight read accumulators and work on them while the
+// next chunk's products run into the other accumulator. Both operand layouts come from the same boxes: 64 of the
+// contiguous dimension by 64 rows, 128-byte swizzle, is 64 rows of 64 k for a K-major operand and 64 k of 64 rows for
+// an MN-major one. A launch carries the tiles of gx and gW of one piece and those of D of the next, so that the
+// clusters stay busy while the counts of each do not divide by the clusters.
+//   An accumulator is added to an fp32 sum in registers every kDrain slabs of 64: the tensor cores truncate their
+// sums, 2^-24.5 of them for each 16 products.
+#include <algorithm>
+#include <atomic>
+#include <cstring>
+
+#include <cuda_bf16.h>
+
+#include "kq_common.cuh"
+
+namespace kq {
+namespace {
+
+constexpr int BM = 256, BN = 256;                // tile of a pair
+constexpr int BK = 64;                           // of a slab
+constexpr int kBox = 64 * 64 * 2;                // bytes
+constexpr int kStage = 4 * kBox;                 // a CTA's 128 rows of A and 128 of B
+constexpr int kStages = 6;
+constexpr int kThreads = 384;                    // a warpgroup for loads and products, two for results
+// Registers of a thread: the launch gives all 168 (what 65536 leave 384 threads); results need a row's 128 sums and more.
+constexpr int kIssueRegs = 40, kResultRegs = 232;
+static_assert(128 * kIssueRegs + 256 * kResultRegs <= kThreads * 168, "more registers than the block was launched with");
+constexpr int kSmem = kStages * kStage + 1024 + 256;
+constexpr int kDrainLogits = 8, kDrainGrads = 32;   // slabs
+constexpr int kBand = 16;                        // row tiles that go through the vocabulary together
+constexpr int64_t kPiece = 1 << 25;              // elements of D that a piece holds, about
+constexpr int64_t kLeastPiece = 1024;            // columns
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kNone = -1.0e30f;                // t of a logit that cannot occur: 2^t = 0 and 0 t a number
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+__device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// 32 bytes, on a 32-byte boundary.
+__device__ __forceinline__ void store32(void* p, const uint32_t (&v)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
+                 "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    const __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&t);
+}
+
+enum Kind { kScore, kDelta, kGx, kGw };
+
+struct Job {
+    int64_t T, V, d;
+    const int64_t* target;
+    // score
+    float4* part;              // [T][parts]: m, Z, S of 128 columns
+    float* zt;                 // [T] the target's logit
+    int32_t parts;
+    // gradient
+    const float *lse, *entropy, *g_logp, *g_entropy;
+    __nv_bfloat16* delta;      // of the piece that this launch makes, [T][ld_delta]
+    int64_t ld_delta;
+    int64_t v_main, v_prod;    // the first column of the piece whose logits, whose products are computed
+    int64_t w_main, w_prod;    // and its width
+    float* sum;                // [splits][T][d]: gx so far
+    __nv_bfloat16 *gx, *gw;    // gx: nullptr unless this launch finishes it
+    int64_t ld_gx, ld_gw;
+    bool first;                // no gx so far
+    int32_t splits, split_slabs;
+    int32_t m_main, n_main, n_d, m_prod;   // tiles: rows, columns of the pieces and of d
+    int32_t t_gx, t_gw, tiles;             // tiles of each, in this order, and in all
+    int* info;
+};
+
+struct Tile {
+    int kind;
+    int m0, n0;      // of the tile, in its operands
+    int ka, kb;      // where K begins in A, in B
+    int slabs, split;
+};
+__device__ __forceinline__ Tile tile_at(const Job& j, int t, int main_kind) {
+    Tile a;
+    a.split = 0;
+    if (t < j.t_gx) {
+        const int mt = static_cast<int>((j.T + BM - 1) / BM), each = mt * j.n_d;
+        a.kind = kGx;
+        a.split = t / each;
+        t -= a.split * each;
+        a.m0 = t / j.n_d * BM;
+        a.n0 = t % j.n_d * BN;
+        a.ka = a.split * j.split_slabs * BK;
+        a.kb = static_cast<int>(j.v_prod) + a.ka;
+        const int all = static_cast<int>((j.w_prod + BK - 1) / BK);
+        a.slabs = min(j.split_slabs, all - a.split * j.split_slabs);
+        return a;
+    }
+    t -= j.t_gx;
+    if (t < j.t_gw) {
+        a.kind = kGw;
+        a.m0 = t / j.n_d * BM;
+        a.n0 = t % j.n_d * BN;
+        a.ka = a.kb = 0;
+        a.slabs = static_cast<int>((j.T + BK - 1) / BK);
+        return a;
+    }
+    t -= j.t_gw;
+    // bands of row tiles, each through all columns, rows first
+    a.kind = main_kind;
+    const int band = t / (kBand * j.n_main), rows = min(kBand, j.m_main - band * kBand);
+    t -= band * kBand * j.n_main;
+    a.m0 = (band * kBand + t % rows) * BM;
+    a.n0 = t / rows * BN;
+    a.ka = a.kb = 0;
+    a.slabs = static_cast<int>((j.d + BK - 1) / BK);
+    return a;
+}
+
+// Waits for a phase that the CTA's own earlier work ends, whatever has been given up.
+__device__ __forceinline__ void wait_quiet(uint64_t* bar, uint32_t parity) {
+    int none = 0;
+    mbar_wait(bar, parity, &none);
+}
+__device__ __forceinline__ int round_tile(int rd, int pair, int pairs) { return rd * pairs + ((rd & 1) ? pairs - 1 - pair : pair); }
+
+// m, Z and S of 128 logits of a row.
+__device__ __forceinline__ void score_row(const Job& j, float (&x)[128], int64_t row, int64_t col, int64_t at) {
+    const int64_t left = j.V - col;
+    if (row >= j.T || left <= 0) return;
+    if (left < 128) {
+#pragma unroll
+        for (int i = 0; i < 128; ++i)
+            if (i >= left) x[i] = -INFINITY;
+    }
+    const int64_t y = j.target[row] - col;
+    if (y >= 0 && y < min(left, static_cast<int64_t>(128))) {
+        float z = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 128; ++i)
+            if (i == y) z = x[i];
+        j.zt[row] = z;
+    }
+    float m = x[0];
+#pragma unroll
+    for (int i = 1; i < 128; ++i) m = max_nan(m, x[i]);
+    const float ref = m == -INFINITY ? 0.0f : m;
+    float z[2] = {0.0f, 0.0f}, s[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < 128; ++i) {
+        const float t = fmaxf((x[i] - ref) * kLog2e, kNone), e = ex2(t);
+        z[i & 1] += e;
+        s[i & 1] = fmaf(e, t, s[i & 1]);
+    }
+    if (KQ_IN_RANGE(at, j.parts)) j.part[row * j.parts + at] = make_float4(m, z[0] + z[1], s[0] + s[1], 0.0f);
+}
+
+// D of 128 logits of a row: to bf16, zeros from the vocabulary's end on.
+__device__ __forceinline__ void delta_row(const Job& j, float (&x)[128], int64_t row, int64_t col) {
+    if (row >= j.T || col >= j.ld_delta) return;
+    const int64_t left = j.V - j.v_main - col, y = j.target[row];
+    const float lse = j.lse[row], g = y >= 0 && y < j.V ? j.g_logp[row] : 0.0f;
+    const float ge = j.g_entropy ? j.g_entropy[row] : 0.0f, h = j.g_entropy ? j.entropy[row] : 0.0f;
+    const bool none = lse == -INFINITY;
+    const int64_t at = y - j.v_main - col;
+    __nv_bfloat16* out = j.delta + row * j.ld_delta + col;
+    const bool here = at >= 0 && at < 128 && y < j.V && !none;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+        uint32_t w[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            float q[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int i = 16 * c + 2 * k + e;
+                const float lp = x[i] - lse, p = ex2(lp * kLog2e);
+                q[e] = p > 0.0f ? -p * fmaf(ge, lp + h, g) : p == p ? 0.0f : p;
+                if (none || i >= left) q[e] = 0.0f;
+                if (here && i == at) q[e] += g;
+            }
+            w[k] = pack_bf16(q[0], q[1]);
+        }
+        if (KQ_IN_RANGE(row * j.ld_delta + col + 16 * c + 15, j.T * j.ld_delta)) store32(out + 16 * c, w);
+    }
+}
+
+// 128 values of a row to a bf16 matrix with n columns.
+__device__ __forceinline__ void put_bf16(const float (&x)[128], __nv_bfloat16* base, int64_t row, int64_t rows, int64_t ld, int64_t col,
+                                         int64_t n) {
+    if (row >= rows || col >= n) return;
+    __nv_bfloat16* out = base + row * ld + col;
+    const bool wide = !(reinterpret_cast<uintptr_t>(out) & 31u);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+        uint32_t w[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = pack_bf16(x[16 * c + 2 * k], x[16 * c + 2 * k + 1]);
+        if (wide && col + 16 * c + 16 <= n) {
+            store32(out + 16 * c, w);
+        } else {   // n is a multiple of 8, rows begin on 16 bytes
+            if (col + 16 * c + 8 <= n) *reinterpret_cast<uint4*>(out + 16 * c) = make_uint4(w[0], w[1], w[2], w[3]);
+            if (col + 16 * c + 16 <= n) *reinterpret_cast<uint4*>(out + 16 * c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+        }
+    }
+}
+
+// gx so far plus 128 values of a row.
+__device__ __forceinline__ void add_gx(const Job& j, float (&x)[128], int split, int64_t row, int64_t col) {
+    if (row >= j.T || col >= j.d) return;
+    float* sum = j.sum + (static_cast<int64_t>(split) * j.T + row) * j.d + col;
+    if (!j.first) {
+#pragma unroll
+        for (int c = 0; c < 32; ++c) {
+            if (col + 4 * c >= j.d) break;
+            const float4 o = *reinterpret_cast<const float4*>(sum + 4 * c);
+            x[4 * c] += o.x, x[4 * c + 1] += o.y, x[4 * c + 2] += o.z, x[4 * c + 3] += o.w;
+        }
+    }
+    if (j.gx) {
+        put_bf16(x, j.gx, row, j.T, j.ld_gx, col, j.d);
+        return;
+    }
+#pragma unroll
+    for (int c = 0; c < 16; ++c) {
+        if (col + 8 * c >= j.d) break;
+        uint32_t w[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(x[8 * c + k]);
+        store32(sum + 8 * c, w);
+    }
+}
+
+// Clusters walk the tiles of a job. MAIN: kScore or kDelta; only kDelta's launches have gradient tiles.
+template <int MAIN>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+linear_tile_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtensorMap mw,
+                   const __grid_constant__ CUtensorMap md, const __grid_constant__ Job j) {
+    const uint32_t rank = cluster_ctarank();
+    const int pair = static_cast<int>(blockIdx.x >> 1), pairs = static_cast<int>(gridDim.x >> 1);
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + kStages * kStage);
+    uint64_t* empty = full + kStages;
+    uint64_t* tfull = empty + kStages;
+    uint64_t* tempty = tfull + 2;
+    uint64_t* mma_done = tempty + 2;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(mma_done + 1);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(&full[s], 1);
+            mbar_init(&empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(&tfull[b], 1);
+            mbar_init(&tempty[b], 16);   // 8 epilogue warps in each CTA
+        }
+        mbar_init(mma_done, 1);
+        *abort_flag = 0;
+        fence_mbar_init();
+    }
+    if (warp == 1) {
+        tmem_alloc_pair(tmem_slot, 2 * BN);
+        tmem_relinquish_pair();
+    }
+    if (warp == 0 && lane == 0) {
+        tma_prefetch_desc(&mx);
+        tma_prefetch_desc(&mw);
+        if (MAIN == kDelta) tma_prefetch_desc(&md);
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_barrier();   // both CTAs' barriers are there before one is signalled from the other
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    const uint32_t full0 = mapa_shared(smem_u32(full), 0), tempty0 = mapa_shared(smem_u32(tempty), 0);   // CTA 0's
+
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssueRegs));
+        // ---- loads, each CTA its own half
+        if (warp == 0 && lane == 0) {
+            int k = 0;
+            bool ok = true;
+            for (int rd = 0; rd * pairs < j.tiles && ok; ++rd) {
+                const int t = round_tile(rd, pair, pairs);
+                if (t >= j.tiles) continue;
+                const Tile a = tile_at(j, t, MAIN);
+                const bool a_mn = a.kind == kGw, b_mn = a.kind == kGx || a.kind == kGw;
+                const CUtensorMap* ma = a.kind == kGx || a.kind == kGw ? &md : &mx;
+                const CUtensorMap* mb = a.kind == kGw ? &mx : &mw;
+                const int m = a.m0 + 128 * static_cast<int>(rank);
+                const int n = a.n0 + 128 * static_cast<int>(rank) + (a.kind == MAIN ? static_cast<int>(j.v_main) : 0);
+                for (int s = 0; s < a.slabs; ++s, ++k) {
+                    const int st = k % kStages;
+                    if (!mbar_wait(&empty[st], (static_cast<uint32_t>(k / kStages) & 1u) ^ 1u, abort_flag)) {
+                        ok = false;
+                        break;
+                    }
+                    if (rank == 0) mbar_arrive_expect_tx(&full[st], 2 * kStage);
+                    uint8_t* base = smem + st * kStage;
+                    const uint32_t bar = full0 + static_cast<uint32_t>(st * 8);
+                    const int ka = a.ka + s * BK, kb = a.kb + s * BK;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        tma_load_2d_pair(base + i * kBox, ma, bar, a_mn ? m + 64 * i : ka, a_mn ? ka : m + 64 * i);
+                        tma_load_2d_pair(base + (2 + i) * kBox, mb, bar, b_mn ? n + 64 * i : kb, b_mn ? kb : n + 64 * i);
+                    }
+                }
+            }
+            // the last slabs have been used by the products, so they have landed
+            for (int i = (k > kStages ? k - kStages : 0); i < k; ++i)
+                wait_quiet(&empty[i % kStages], static_cast<uint32_t>(i / kStages) & 1u);
+        }
+        // ---- products, CTA 0 for both
+        if (warp == 1 && lane == 0) {
+            if (rank == 0) {
+                int k = 0, cc = 0;
+                bool ok = true;
+                for (int rd = 0; rd * pairs < j.tiles && ok; ++rd) {
+                    const int t = round_tile(rd, pair, pairs);
+                    if (t >= j.tiles) continue;
+                    const Tile a = tile_at(j, t, MAIN);
+                    const bool a_mn = a.kind == kGw, b_mn = a.kind == kGx || a.kind == kGw;
+                    const uint32_t idesc = (idesc_bf16_mn_major(BM, BN) & ~(3u << 15)) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
+                    // to the next 16 of K: 32 bytes along swizzled rows, or 16 rows of 128 bytes
+                    const uint32_t a_step = a_mn ? 2048 : 32, b_step = b_mn ? 2048 : 32;
+                    const int drain = a.kind == MAIN ? kDrainLogits : kDrainGrads;
+                    for (int s0 = 0; s0 < a.slabs && ok; s0 += drain, ++cc) {
+                        const int buf = cc & 1;
+                        if (!mbar_wait_cl(&tempty[buf], ((static_cast<uint32_t>(cc) >> 1) & 1u) ^ 1u, abort_flag)) {
+                            ok = false;
+                            break;
+                        }
+                        tc_fence_after();
+                        const uint32_t dt = tmem + static_cast<uint32_t>(buf * BN);
+                        const int s1 = min(a.slabs, s0 + drain);
+                        for (int s = s0; s < s1; ++s, ++k) {
+                            const int st = k % kStages;
+                            if (!mbar_wait(&full[st], static_cast<uint32_t>(k / kStages) & 1u, abort_flag)) {
+                                ok = false;
+                                break;
+                            }
+                            tc_fence_after();
+                            const uint32_t sa = smem_u32(smem + st * kStage), sb = sa + 2 * kBox;
+#pragma unroll
+                            for (int q = 0; q < BK / 16; ++q)
+                                mma_pair(dt, smem_desc_sw128(sa + q * a_step, kBox, 1024), smem_desc_sw128(sb + q * b_step, kBox, 1024),
+                                         idesc, (s > s0 || q > 0) ? 1u : 0u);
+                            tc_commit_pair(&empty[st]);
+                        }
+                        if (ok) tc_commit_pair(&tfull[buf]);
+                    }
+                }
+                tc_commit_pair(mma_done);
+            }
+            wait_quiet(mma_done, 0);
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kResultRegs));
+        // ---- results: a thread has 128 columns (warps 4-7 the first half) of one of the CTA's 128 rows
+        const int q = warp & 3, h = (warp - 4) >> 2;
+        int cc = 0;
+        bool ok = true;
+        for (int rd = 0; rd * pairs < j.tiles && ok; ++rd) {
+            const int t = round_tile(rd, pair, pairs);
+            if (t >= j.tiles) continue;
+            const Tile a = tile_at(j, t, MAIN);
+            const int drain = a.kind == MAIN ? kDrainLogits : kDrainGrads;
+            float x[128];
+            for (int s0 = 0; s0 < a.slabs; s0 += drain, ++cc) {
+                const int buf = cc & 1;
+                ok = mbar_wait(&tfull[buf], (static_cast<uint32_t>(cc) >> 1) & 1u, abort_flag);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t at = tmem + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(buf * BN + h * 128);
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    float v[32];
+                    tmem_ld32(at + p * 32, v);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) x[p * 32 + i] = s0 ? x[p * 32 + i] + v[i] : v[i];
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_remote(tempty0 + static_cast<uint32_t>(buf * 8));
+            }
+            if (!ok) break;
+            const int64_t row = a.m0 + 128 * static_cast<int64_t>(rank) + q * 32 + lane, col = a.n0 + h * 128;
+            if (MAIN == kScore) {
+                score_row(j, x, row, col, a.n0 / 128 + h);
+            } else if (a.kind == kDelta) {
+                delta_row(j, x, row, col);
+            } else if (a.kind == kGx) {
+                add_gx(j, x, a.split, row, col);
+            } else {
+                put_bf16(x, j.gw + j.v_prod * j.ld_gw, row, min(j.w_prod, j.V - j.v_prod), j.ld_gw, col, j.d);
+            }
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (*abort_flag && threadIdx.x == 0) {
+        record_error(j.info, -KQ_ERR_TIMEOUT);
+        // copies that this CTA sent to the other's barriers have had time to land
+        const uint64_t t0 = global_timer_ns();
+        while (global_timer_ns() - t0 < 1000000ull) {
+        }
+    }
+    cluster_barrier();   // neither CTA leaves while the other may still signal it
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc_pair(tmem, 2 * BN);
+    }
+}
+
+// Joins the parts of a row: a block to a row.
+__global__ void __launch_bounds__(128) linear_join_kernel(const Job j, float* __restrict__ logp, float* __restrict__ entropy,
+                                                          float* __restrict__ lse) {
+    __shared__ float sm[4], sz[4], ss[4];
+    const int64_t row = blockIdx.x;
+    const float4* p = j.part + row * j.parts;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    float M = -INFINITY, Z = 0.0f, S = 0.0f;
+    auto join = [&](float m, float z, float s) {   // sums against m into those against M
+        const float top = max_nan(M, m);
+        if (top == -INFINITY) return;
+        const float a = (M - top) * kLog2e, b = (m - top) * kLog2e, fa = ex2(a), fb = ex2(b);
+        // 2^b (s + b z); a part against -infinity has none
+        S = (fa > 0.0f || a != a ? fa * fmaf(a, Z, S) : 0.0f) + (fb > 0.0f || b != b ? fb * fmaf(b, z, s) : 0.0f);
+        Z = fa * Z + fb * z;
+        M = top;
+    };
+    for (int i = threadIdx.x; i < j.parts; i += 128) {
+        const float4 v = p[i];
+        join(v.x, v.y, v.z);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const float m = __shfl_xor_sync(0xffffffffu, M, o), z = __shfl_xor_sync(0xffffffffu, Z, o), s = __shfl_xor_sync(0xffffffffu, S, o);
+        join(m, z, s);
+    }
+    if (lane == 0) sm[warp] = M, sz[warp] = Z, ss[warp] = S;
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int w = 1; w < 4; ++w) join(sm[w], sz[w], ss[w]);
+    const int64_t y = j.target[row];
+    const bool none = M == -INFINITY;
+    const float lz = log2f(Z), ln = lz * kLn2;
+    if (y >= j.V) record_error(j.info, -KQ_ERR_INVALID_ARG);
+    float lp = 0.0f;
+    if (y >= j.V) lp = NAN;
+    else if (y >= 0) lp = none ? -INFINITY : j.zt[row] - M - ln;
+    logp[row] = lp > 0.0f ? 0.0f : lp;
+    if (entropy) entropy[row] = none ? 0.0f : (lz - S / Z) * kLn2;
+    if (lse) lse[row] = none ? -INFINITY : M + ln;
+}
+
+// gx = the sum of the splits, in order.
+__global__ void __launch_bounds__(256) linear_gx_kernel(const float* __restrict__ sum, int splits, int64_t T, int64_t d,
+                                                        __nv_bfloat16* __restrict__ gx, int64_t ld) {
+    const int64_t each = T * d, per_row = d / 8;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < T * per_row; i += static_cast<int64_t>(gridDim.x) * 256) {
+        const int64_t row = i / per_row, col = (i - row * per_row) * 8;
+        float x[8] = {};
+        for (int s = 0; s < splits; ++s) {
+            const float4* p = reinterpret_cast<const float4*>(sum + s * each + row * d + col);
+            const float4 a = p[0], b = p[1];
+            x[0] += a.x, x[1] += a.y, x[2] += a.z, x[3] += a.w, x[4] += b.x, x[5] += b.y, x[6] += b.z, x[7] += b.w;
+        }
+        if (KQ_IN_RANGE(row * ld + col + 7, (T - 1) * ld + d))
+            *reinterpret_cast<uint4*>(gx + row * ld + col) =
+                make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+    }
+}
+// Targets past the vocabulary are reported; the gradient's tiles leave them out.
+__global__ void linear_targets_kernel(const int64_t* __restrict__ target, int64_t T, int64_t V, int* info) {
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < T; i += static_cast<int64_t>(gridDim.x) * blockDim.x)
+        if (target[i] >= V) record_error(info, -KQ_ERR_INVALID_ARG);
+}
+
+using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                   const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// 64 x 64 boxes of a row-major bf16 matrix, 128-byte swizzle, zeros outside.
+kq_status make_map(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int64_t ld, const char* who) {
+    static std::atomic<EncodeTiledFn> fn{nullptr};
+    EncodeTiledFn enc = fn.load();
+    if (!enc) {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess) {
+            set_error("%s: cuTensorMapEncodeTiled is unavailable", who);
+            return KQ_ERR_CUDA;
+        }
+        enc = reinterpret_cast<EncodeTiledFn>(p);
+        fn.store(enc);
+    }
+    std::memset(m, 0, sizeof(*m));
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
+    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld) * 2};
+    const cuuint32_t box[2] = {64, 64}, one[2] = {1, 1};
+    const CUresult r = enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, one,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) {
+        set_error("%s: cuTensorMapEncodeTiled failed (%d)", who, static_cast<int>(r));
+        return KQ_ERR_CUDA;
+    }
+    return KQ_OK;
+}
+
+int max_clusters() {
+    static std::atomic<int> kept[64] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return num_sms() / 2;
+    if (const int c = kept[dev].load()) return c;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(num_sms() / 2 * 2));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmem;
+    int c = 0;
+    if (cudaOccupancyMaxActiveClusters(&c, linear_tile_kernel<kScore>, &cfg) != cudaSuccess || c < 1) c = num_sms() / 2;
+    kept[dev].store(c);
+    return c;
+}
+
+template <int MAIN>
+kq_status run_tiles(const CUtensorMap& mx, const CUtensorMap& mw, const CUtensorMap& md, const Job& j, cudaStream_t stream) {
+    if (j.tiles == 0) return KQ_OK;
+    const int pairs = std::min(j.tiles, max_clusters());
+    linear_tile_kernel<MAIN><<<static_cast<unsigned>(2 * pairs), kThreads, kSmem, stream>>>(mx, mw, md, j);
+    KQ_LAUNCH_CHECK("linear_tile_kernel");
+    return KQ_OK;
+}
+kq_status set_up() {
+    static std::atomic<uint64_t> done{0};
+    return once_per_device(done, [] {
+        KQ_CUDA(cudaFuncSetAttribute(linear_tile_kernel<kScore>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
+        KQ_CUDA(cudaFuncSetAttribute(linear_tile_kernel<kDelta>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
+        return KQ_OK;
+    });
+}
+
+// How the gradient is cut; from the sizes alone, so that the workspace's size is the same on every device.
+struct Cut {
+    int64_t piece;        // columns
+    int64_t pieces;
+    int32_t splits, split_slabs;
+    size_t delta, sum;    // bytes of one of the two D, of gx so far
+};
+Cut cut_of(int64_t T, int64_t V, int64_t d) {
+    Cut c;
+    const int64_t columns = std::max(kLeastPiece, kPiece / T / BN * BN);
+    c.piece = std::min(columns, cdiv(V, BN) * BN);
+    c.pieces = cdiv(V, c.piece);
+    const int64_t tiles = cdiv(T, BM) * cdiv(d, BN), slabs = cdiv(std::min(c.piece, V), BK);   // of the first piece
+    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(76 / tiles, slabs / 4));
+    c.split_slabs = static_cast<int32_t>(cdiv(slabs, splits));
+    c.splits = static_cast<int32_t>(cdiv(slabs, c.split_slabs));
+    c.delta = static_cast<size_t>(T) * c.piece * 2;
+    c.sum = c.pieces * c.splits > 1 ? static_cast<size_t>(c.splits) * T * d * sizeof(float) : 0;
+    return c;
+}
+size_t al256(size_t b) { return (b + 255) & ~static_cast<size_t>(255); }
+
+kq_status check(const char* who, const uint16_t* x, int64_t T, int64_t d, int64_t ldx, const uint16_t* w, int64_t V, int64_t ldw,
+                const int64_t* target) {
+    if (V > KQ_LOGPROBS_MAX_V || d > 65536 || d % 8) {
+        set_error("%s: V must be at most %d, d a multiple of 8 up to 65536", who, KQ_LOGPROBS_MAX_V);
+        return KQ_ERR_UNSUPPORTED;
+    }
+    if (T < 0 || T > KQ_LINEAR_MAX_T || V < 1 || d < 1 || !w || ldw < d || ldx < d || ((ldx | ldw) & 7) || (T > 0 && (!x || !target)) ||
+        ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(w)) & 15u)) {
+        set_error("%s: x, w and target must not be NULL, x and w 16-byte aligned with row strides of at least d in multiples of 8, "
+                  "0 <= T <= %d, V >= 1", who, KQ_LINEAR_MAX_T);
+        return KQ_ERR_INVALID_ARG;
+    }
+    return KQ_OK;
+}
+
+}  // namespace
+
+KQ_DEBUG_UNIT(linear_logprob)
+}  // namespace kq
+
+using namespace kq;
+
+extern "C" size_t kq_linear_logprobs_workspace(int64_t T, int64_t V, int64_t d) {
+    if (T < 1 || V < 1 || d < 1) return 0;
+    return al256(static_cast<size_t>(T) * cdiv(V, 128) * sizeof(float4)) + al256(T * sizeof(float));
+}
+
+extern "C" kq_status kq_linear_logprobs(const uint16_t* x, int64_t T, int64_t d, int64_t ldx, const uint16_t* w, int64_t V, int64_t ldw,
+                                        const int64_t* target, float* logp, float* entropy, float* lse, int* info, void* ws,
+                                        size_t ws_bytes, kq_stream_t stream_) {
+    const char* who = "kq_linear_logprobs";
+    KQ_TRY(check(who, x, T, d, ldx, w, V, ldw, target));
+    if (T == 0) return KQ_OK;
+    if (!logp) {
+        set_error("%s: logp must not be NULL", who);
+        return KQ_ERR_INVALID_ARG;
+    }
+    const size_t need = kq_linear_logprobs_workspace(T, V, d);
+    if (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 255u)) {
+        set_error("%s: workspace must be 256-byte aligned and hold %zu bytes", who, need);
+        return KQ_ERR_WORKSPACE;
+    }
+    cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
+    KQ_TRY(set_up());
+    CUtensorMap mx, mw;
+    KQ_TRY(make_map(&mx, x, T, d, ldx, who));
+    KQ_TRY(make_map(&mw, w, V, d, ldw, who));
+    Job j = {};
+    j.T = T, j.V = V, j.d = d;
+    j.target = target;
+    j.parts = static_cast<int32_t>(cdiv(V, 128));
+    j.part = static_cast<float4*>(ws);
+    j.zt = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + al256(static_cast<size_t>(T) * j.parts * sizeof(float4)));
+    j.m_main = static_cast<int32_t>(cdiv(T, BM));
+    j.n_main = static_cast<int32_t>(cdiv(V, BN));
+    j.tiles = j.m_main * j.n_main;
+    j.info = info;
+    KQ_TRY(run_tiles<kScore>(mx, mw, mw, j, stream));
+    linear_join_kernel<<<static_cast<unsigned>(T), 128, 0, stream>>>(j, logp, entropy, lse);
+    KQ_LAUNCH_CHECK("linear_join_kernel");
+    return KQ_OK;
+}
+
+extern "C" size_t kq_linear_logprobs_grad_workspace(int64_t T, int64_t V, int64_t d) {
+    if (T < 1 || V < 1 || d < 1) return 0;
+    const Cut c = cut_of(T, V, d);
+    return al256(c.delta) * (c.pieces > 1 ? 2 : 1) + al256(c.sum);
+}
+
+extern "C" kq_status kq_linear_logprobs_grad(const uint16_t* x, int64_t T, int64_t d, int64_t ldx, const uint16_t* w, int64_t V,
+                                             int64_t ldw, const int64_t* target, const float* lse, const float* entropy,
+                                             const float* g_logp, const float* g_entropy, uint16_t* gx, int64_t ldgx, uint16_t* gw,
+                                             int64_t ldgw, int* info, void* ws, size_t ws_bytes, kq_stream_t stream_) {
+    const char* who = "kq_linear_logprobs_grad";
+    KQ_TRY(check(who, x, T, d, ldx, w, V, ldw, target));
+    if ((T > 0 && (!lse || !g_logp || (g_entropy && !entropy))) || (!gx && !gw) || (gx && (ldgx < d || (ldgx & 7))) ||
+        (gw && (ldgw < d || (ldgw & 7))) || ((reinterpret_cast<uintptr_t>(gx) | reinterpret_cast<uintptr_t>(gw)) & 15u)) {
+        set_error("%s: lse, g_logp (and entropy with g_entropy) and gx or gw must not be NULL, gx and gw 16-byte aligned with row "
+                  "strides of at least d in multiples of 8", who);
+        return KQ_ERR_INVALID_ARG;
+    }
+    cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
+    if (T == 0) {
+        if (gw) KQ_CUDA(cudaMemset2DAsync(gw, ldgw * 2, 0, d * 2, V, stream));
+        return KQ_OK;
+    }
+    const size_t need = kq_linear_logprobs_grad_workspace(T, V, d);
+    if (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 255u)) {
+        set_error("%s: workspace must be 256-byte aligned and hold %zu bytes", who, need);
+        return KQ_ERR_WORKSPACE;
+    }
+    KQ_TRY(set_up());
+    const Cut c = cut_of(T, V, d);
+    uint8_t* at = static_cast<uint8_t*>(ws);
+    __nv_bfloat16* delta[2] = {reinterpret_cast<__nv_bfloat16*>(at),
+                               reinterpret_cast<__nv_bfloat16*>(at + (c.pieces > 1 ? al256(c.delta) : 0))};
+    CUtensorMap mx, mw, md[2];
+    KQ_TRY(make_map(&mx, x, T, d, ldx, who));
+    KQ_TRY(make_map(&mw, w, V, d, ldw, who));
+    for (int i = 0; i < 2; ++i) KQ_TRY(make_map(&md[i], delta[i], T, c.piece, c.piece, who));
+    if (info) {
+        linear_targets_kernel<<<static_cast<unsigned>(std::min<int64_t>(cdiv(T, 256), 1024)), 256, 0, stream>>>(target, T, V, info);
+        KQ_LAUNCH_CHECK("linear_targets_kernel");
+    }
+    Job j = {};
+    j.T = T, j.V = V, j.d = d;
+    j.target = target;
+    j.lse = lse, j.entropy = entropy, j.g_logp = g_logp, j.g_entropy = g_entropy;
+    j.ld_delta = c.piece;
+    j.sum = reinterpret_cast<float*>(at + al256(c.delta) * (c.pieces > 1 ? 2 : 1));
+    j.gw = reinterpret_cast<__nv_bfloat16*>(gw);
+    j.ld_gx = ldgx, j.ld_gw = ldgw;
+    j.splits = c.splits, j.split_slabs = c.split_slabs;
+    j.m_main = static_cast<int32_t>(cdiv(T, BM));
+    j.n_d = static_cast<int32_t>(cdiv(d, BN));
+    j.info = info;
+    // launch i: D of piece i, the products with D of piece i - 1
+    for (int64_t i = 0; i <= c.pieces; ++i) {
+        j.v_main = i * c.piece;
+        j.w_main = std::min(c.piece, V - j.v_main);
+        j.n_main = i < c.pieces ? static_cast<int32_t>(cdiv(j.w_main, BN)) : 0;
+        j.delta = delta[i & 1];
+        j.t_gx = j.t_gw = 0;
+        if (i > 0) {
+            j.v_prod = (i - 1) * c.piece;
+            j.w_prod = std::min(c.piece, V - j.v_prod);
+            const int32_t splits = static_cast<int32_t>(cdiv(cdiv(j.w_prod, BK), c.split_slabs));
+            j.first = i == 1;
+            j.gx = c.splits == 1 && i == c.pieces ? reinterpret_cast<__nv_bfloat16*>(gx) : nullptr;
+            if (gx) j.t_gx = splits * j.m_main * j.n_d;
+            if (gw) j.t_gw = static_cast<int32_t>(cdiv(j.w_prod, BM)) * j.n_d;
+        }
+        j.tiles = j.t_gx + j.t_gw + j.m_main * j.n_main;
+        KQ_TRY(run_tiles<kDelta>(mx, mw, md[(i + 1) & 1], j, stream));
+    }
+    if (gx && c.splits > 1) {
+        const int64_t blocks = std::min<int64_t>(cdiv(T * (d / 8), 256), static_cast<int64_t>(num_sms()) * 8);
+        linear_gx_kernel<<<static_cast<unsigned>(blocks), 256, 0, stream>>>(j.sum, c.splits, T, d, reinterpret_cast<__nv_bfloat16*>(gx),
+                                                                            ldgx);
+        KQ_LAUNCH_CHECK("linear_gx_kernel");
+    }
+    return KQ_OK;
+}

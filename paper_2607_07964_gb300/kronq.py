@@ -6,6 +6,7 @@ or PyTorch fallback: if libkronq.so is missing or fails to load, every call rais
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 
 import torch
@@ -89,6 +90,14 @@ def lib() -> ctypes.CDLL:
             "kq_kv_evict": ([P, P, P, P, P, I64, I64, I64, I64, P, P, P, P, P, SZ, P], I),
             "kq_token_logprobs": ([P, I, I64, I64, I64, P, I, P, P, P, P, P, P, P], I),
             "kq_token_logprobs_grad": ([P, I, I64, I64, I64, P, P, P, P, P, P, I64, P, P], I),
+            "kq_qk_rotate": ([P, I, I64, I64, P, P, P, P, P, P, F, P], I),
+            "kq_qk_rotate_grad_workspace": ([I64, I64], SZ),
+            "kq_qk_rotate_grad": ([P, I, I64, I64, P, P, P, P, P, P, P, P, F, P, P, P, SZ, P], I),
+            "kq_kv_attend_window": ([P, P, I, I64, I64, I64, I64, P, P, F, I64, I64, P, P, P, P, SZ, P], I),
+            "kq_linear_logprobs_workspace": ([I64, I64, I64], SZ),
+            "kq_linear_logprobs": ([P, I64, I64, I64, P, I64, I64, P, P, P, P, P, P, SZ, P], I),
+            "kq_linear_logprobs_grad_workspace": ([I64, I64, I64], SZ),
+            "kq_linear_logprobs_grad": ([P, I64, I64, I64, P, I64, I64, P, P, P, P, P, P, I64, P, I64, P, P, SZ, P], I),
             "kq_proxy_loss_workspace": ([I64, I64], SZ),
             "kq_proxy_loss": ([P, P, I64, I64, P, P, P, P, SZ, P], I),
         }
@@ -509,6 +518,101 @@ def _rows3(t, name, heads=None, dim=None):
         raise ValueError(f"{name} must have {heads} heads of {dim}, got {tuple(t.shape)}")
 
 
+class _Rotation(ctypes.Structure):
+    _fields_ = [("freq", ctypes.c_void_p), ("rot", ctypes.c_int64), ("pos", ctypes.c_void_p), ("start", ctypes.c_void_p),
+                ("first", ctypes.c_void_p), ("batch", ctypes.c_int64), ("interleaved", ctypes.c_int), ("scale", ctypes.c_float)]
+
+
+class _Heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("heads", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64)]
+
+
+def kq_rotation_freq(theta, device="cuda"):
+    """freq of kq_qk_rotate: the radians that one position turns each pair by, as 64-bit fractions of a turn (int64)."""
+    turns = (round(float(t) / (2 * math.pi) * 2.0 ** 64) for t in theta)
+    return torch.tensor([((n + (1 << 63)) % (1 << 64)) - (1 << 63) for n in turns], dtype=torch.int64, device=device)
+
+
+def _heads(t, name, dtype, T, dim, heads=None):
+    if t is None:
+        return None
+    _rows3(t, name, heads, dim)
+    _need(t, name, dtype, contiguous=False)
+    if t.shape[0] != T:
+        raise ValueError(f"{name} must have {T} tokens, got {t.shape[0]}")
+    return ctypes.byref(_Heads(t.data_ptr(), t.shape[1], t.stride(0), t.stride(1)))
+
+
+def _rotation(freq, pos, start, first, interleaved, scale, T):
+    _need(freq, "freq", torch.int64)
+    _need(pos, "pos", torch.int32, (T,))
+    batch = 0
+    if first is not None or start is not None:
+        if first is None or start is None:
+            raise ValueError("start and first go together")
+        batch = first.shape[0]
+        _need(first, "first", torch.int32, (batch,))
+        _need(start, "start", torch.int32, (batch + 1,))
+    return _Rotation(freq.data_ptr(), 2 * freq.numel(), _ptr(pos), _ptr(start), _ptr(first), batch, int(interleaved), float(scale))
+
+
+def _no_empty(t, name):
+    if t is not None and t.shape[1] == 0:
+        raise ValueError(f"{name} must have at least one head")
+
+
+def kq_qk_rotate(q, k, q_out, k_out, freq, pos=None, start=None, first=None, interleaved: bool = False, scale: float = 1.0,
+                 q_weight=None, k_weight=None, eps: float = 1e-6, stream=None) -> None:
+    """q, k [T, heads, dim] (bf16 or fp32, any token and head strides; k, k_out may be None) normed over dim where a weight [dim]
+    is given, their first 2 freq.numel() values rotated by the tokens' positions: pos [T], or first[b] + index in sequence b
+    (start [batch + 1], first [batch]), or the index. freq: kq_rotation_freq. An output may be its input."""
+    dtype = _dtype(q, "q")
+    T, heads, dim = q.shape
+    for t, n in ((q, "q"), (k, "k")):
+        _no_empty(t, n)
+    for t, n in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        _need(t, n, q.dtype, (dim,))
+    if (k is None) != (k_out is None):
+        raise ValueError("k and k_out go together")
+    r = _rotation(freq, pos, start, first, interleaved, scale, T)
+    _ok(lib().kq_qk_rotate(ctypes.byref(r), dtype, T, dim, _heads(q, "q", q.dtype, T, dim), _heads(k, "k", q.dtype, T, dim),
+                           _heads(q_out, "q_out", q.dtype, T, dim, heads),
+                           _heads(k_out, "k_out", q.dtype, T, dim, None if k is None else k.shape[1]), _ptr(q_weight),
+                           _ptr(k_weight), float(eps), _stream(stream)), "kq_qk_rotate")
+
+
+def kq_qk_rotate_grad_workspace(q, k=None) -> int:
+    """Bytes of kq_qk_rotate_grad's workspace for these queries (its gq will do)."""
+    return int(lib().kq_qk_rotate_grad_workspace(q.shape[0], q.shape[2]))
+
+
+def kq_qk_rotate_grad(q, k, gq, gk, q_out, k_out, freq, pos=None, start=None, first=None, interleaved: bool = False,
+                      scale: float = 1.0, q_weight=None, k_weight=None, eps: float = 1e-6, gq_weight=None, gk_weight=None, ws=None,
+                      stream=None) -> None:
+    """The gradients of kq_qk_rotate's inputs, q_out and k_out, from those of its outputs, gq and gk, with those of the weights,
+    gq_weight and gk_weight [dim] fp32, where they are given (ws then). q and k may be None where there is no weight."""
+    dtype = _dtype(gq, "gq")
+    T, heads, dim = gq.shape
+    for t, n in ((gq, "gq"), (gk, "gk")):
+        _no_empty(t, n)
+    for t, n in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        _need(t, n, gq.dtype, (dim,))
+    for t, n in ((gq_weight, "gq_weight"), (gk_weight, "gk_weight")):
+        _need(t, n, torch.float32, (dim,))
+    if (gk is None) != (k_out is None):
+        raise ValueError("gk and k_out go together")
+    _need(ws, "ws", torch.uint8)
+    r = _rotation(freq, pos, start, first, interleaved, scale, T)
+    kv = None if gk is None else gk.shape[1]
+    _ok(lib().kq_qk_rotate_grad(ctypes.byref(r), dtype, T, dim, _heads(q, "q", gq.dtype, T, dim, heads),
+                                _heads(k, "k", gq.dtype, T, dim, kv), _heads(gq, "gq", gq.dtype, T, dim),
+                                _heads(gk, "gk", gq.dtype, T, dim), _heads(q_out, "q_out", gq.dtype, T, dim, heads),
+                                _heads(k_out, "k_out", gq.dtype, T, dim, kv), _ptr(q_weight), _ptr(k_weight), float(eps),
+                                _ptr(gq_weight), _ptr(gk_weight), _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)),
+        "kq_qk_rotate_grad")
+
+
 def kq_kv_append(k, v, start, lens, cache, table, lens_out=None, acc=None, pos=None, seen=None, seen_out=None, info=None,
                  stream=None) -> None:
     """k, v [T, kv_heads, dim] (bf16 or fp32, any token and head strides) into the 4-bit cache at the
@@ -592,6 +696,24 @@ def kq_kv_attend(q, start, lens, cache, table, out, ws, scale: float, lse=None, 
                            0 if ws is None else ws.numel(), _stream(stream)), "kq_kv_attend")
 
 
+def kq_kv_attend_window(q, start, lens, cache, table, out, ws, scale: float, window: int, sink: int = 0, lse=None, info=None,
+                        stream=None) -> None:
+    """kq_kv_attend where a token sees the last `window` of its slots and the first `sink` only."""
+    dtype = _dtype(q, "q")
+    _rows3(q, "q")
+    T, heads, dim = q.shape
+    c = _cache(cache, table, dim)
+    _need(out, "out", q.dtype, (T, heads, dim))
+    _need(lse, "lse", torch.float32, (T, heads))
+    _need(start, "start", torch.int32, (c.batch + 1,))
+    _need(lens, "lens", torch.int32, (c.batch,))
+    _need(ws, "ws", torch.uint8)
+    _need(info, "info", torch.int32)
+    _ok(lib().kq_kv_attend_window(ctypes.byref(c), _ptr(q), dtype, T, heads, q.stride(0), q.stride(1), _ptr(start), _ptr(lens),
+                                  float(scale), int(window), int(sink), _ptr(out), _ptr(lse), _ptr(info), _ptr(ws),
+                                  0 if ws is None else ws.numel(), _stream(stream)), "kq_kv_attend_window")
+
+
 def kq_kv_evict_workspace(acc, budget: int) -> int:
     """Bytes of kq_kv_evict's workspace for weights acc [batch, kv_heads, S]."""
     return int(lib().kq_kv_evict_workspace(acc.shape[0], acc.shape[1], acc.shape[2], int(budget)))
@@ -662,6 +784,59 @@ def kq_token_logprobs_grad(logits, target, lse, g_logp, grad, entropy=None, g_en
     _ok(lib().kq_token_logprobs_grad(_ptr(logits), dtype, T, V, _row_stride(logits), _ptr(target), _ptr(lse),
                                      _ptr(entropy), _ptr(g_logp), _ptr(g_entropy), _ptr(grad), _row_stride(grad),
                                      _ptr(info), _stream(stream)), "kq_token_logprobs_grad")
+
+
+def _matrix(t, name, cols=None, rows=None):
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1 and t.numel()):
+        raise ValueError(f"{name} must have two dimensions with unit column stride")
+    if (cols is not None and t.shape[1] != cols) or (rows is not None and t.shape[0] != rows):
+        raise ValueError(f"{name} must be {rows} x {cols}, got {tuple(t.shape)}")
+    _need(t, name, torch.bfloat16, contiguous=False)
+    # the one row of a matrix may have any stride
+    return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 8) * 8
+
+
+def kq_linear_logprobs_workspace(x, w) -> int:
+    """Bytes of kq_linear_logprobs's workspace for these tensors."""
+    return int(lib().kq_linear_logprobs_workspace(x.shape[0], w.shape[0], x.shape[1]))
+
+
+def kq_linear_logprobs(x, w, target, logp, ws, entropy=None, lse=None, info=None, stream=None) -> None:
+    """logp [T] of the target tokens [T] int64 (negative: not scored), with the entropy and log-sum of each row, for the logits
+    x w^T of hidden states x [T, d] and a head w [V, d] (bf16), which are not kept."""
+    ldx, ldw = _matrix(x, "x"), _matrix(w, "w", x.shape[1], w.shape[0])
+    T, d = x.shape
+    _need(target, "target", torch.int64, (T,))
+    for t, name in ((logp, "logp"), (entropy, "entropy"), (lse, "lse")):
+        _need(t, name, torch.float32, (T,))
+    _need(ws, "ws", torch.uint8)
+    _need(info, "info", torch.int32)
+    _ok(lib().kq_linear_logprobs(_ptr(x), T, d, ldx, _ptr(w), w.shape[0], ldw, _ptr(target), _ptr(logp), _ptr(entropy), _ptr(lse),
+                                 _ptr(info), _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)), "kq_linear_logprobs")
+
+
+def kq_linear_logprobs_grad_workspace(x, w) -> int:
+    """Bytes of kq_linear_logprobs_grad's workspace for these tensors."""
+    return int(lib().kq_linear_logprobs_grad_workspace(x.shape[0], w.shape[0], x.shape[1]))
+
+
+def kq_linear_logprobs_grad(x, w, target, lse, g_logp, ws, gx=None, gw=None, entropy=None, g_entropy=None, info=None,
+                            stream=None) -> None:
+    """gx [T, d], gw [V, d] (bf16; either may be None) = the gradients of sum(g_logp * logp + g_entropy * entropy) with respect
+    to x and w; lse and entropy from kq_linear_logprobs."""
+    ldx, ldw = _matrix(x, "x"), _matrix(w, "w", x.shape[1], w.shape[0])
+    T, d = x.shape
+    V = w.shape[0]
+    ldgx = d if gx is None else _matrix(gx, "gx", d, T)
+    ldgw = d if gw is None else _matrix(gw, "gw", d, V)
+    _need(target, "target", torch.int64, (T,))
+    for t, name in ((lse, "lse"), (g_logp, "g_logp"), (entropy, "entropy"), (g_entropy, "g_entropy")):
+        _need(t, name, torch.float32, (T,))
+    _need(ws, "ws", torch.uint8)
+    _need(info, "info", torch.int32)
+    _ok(lib().kq_linear_logprobs_grad(_ptr(x), T, d, ldx, _ptr(w), V, ldw, _ptr(target), _ptr(lse), _ptr(entropy), _ptr(g_logp),
+                                      _ptr(g_entropy), _ptr(gx), ldgx, _ptr(gw), ldgw, _ptr(info), _ptr(ws),
+                                      0 if ws is None else ws.numel(), _stream(stream)), "kq_linear_logprobs_grad")
 
 
 def kq_dequant_revert(codes, scale, zero, group: int, s_x, s_g, sign_u, sign_v, W_hat, stream=None):
