@@ -10,10 +10,10 @@
 // turn, so the angle of position 2^31 is as exact as that of position 1. Of the product's fraction of a turn the
 // upper 32 bits are used (1.5e-9 rad), rounded to fp32 (within 2^-25 of a turn): 2e-7 of the row's size.
 //
-// What bounds it: bytes, 2 elements moved for each forward, 3 backward, against about 10 instructions an
-// element. So: 16 bytes to a lane, G lanes to a row, cos and sin computed once a token (a table in shared memory, from
-// which each lane takes its own into registers for all the heads it goes through), partners exchanged by
-// shuffles, and kAhead rows of loads in flight to a lane.
+// What bounds it: bytes, 2 elements moved for each forward, 3 backward, against about 12 instructions an
+// element. So a warp takes a token and its heads by itself: it has the next kAhead rows' loads in flight while it works
+// on one (16 bytes to a lane, G lanes to a row), computes cos and sin of the token's pairs once, and exchanges
+// partners by shuffles. Backwards the warps stay and go from token to token, the weights' sums in registers.
 #include <algorithm>
 #include <atomic>
 
@@ -23,9 +23,12 @@
 namespace kq {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kAhead = 4;          // rows of a lane in flight
+constexpr int kThreads = 128;      // forwards
+constexpr int kGradThreads = 256;
+constexpr int kAhead = 4;          // rows of a lane in flight forwards
+constexpr int kGradAhead = 2;      // and backwards, of two inputs
 constexpr int kMaxDim = 256;
+constexpr int kMaxBlocks = 512;    // that a workspace has room for the sums of
 constexpr int kPairs = 0, kHalves = 1, kHalvesOdd = 2;   // layouts; odd: R / 2 is no multiple of a vector
 
 template <typename T>
@@ -44,25 +47,28 @@ struct Rotate {
     const uint64_t* freq;
     const int32_t *pos, *start, *first;
     int32_t batch, dim, half;        // half: pairs
-    int32_t per;       // tokens of a block at a time, a power of two
-    int32_t part;      // heads of a block
+    int32_t parts, part;   // of a token's rows, each of `part` looks at them
     float scale, eps;
-    bool vec;          // every row can be moved 16 bytes at a time
     float* sums;       // backward: [blocks][2][dim] of weight gradients, or nullptr
 };
 
-template <typename T>
+// FAST: every row can be moved 16 bytes at a time, and has whole vectors; n: how much of a vector there is.
+template <typename T, bool FAST>
 struct Lane {
     static constexpr int E = 16 / sizeof(T);
-    static __device__ __forceinline__ uint4 load(const T* p, bool vec, int n) {
+    static __device__ __forceinline__ uint4 load(const T* p, int n) {
         uint4 u = make_uint4(0, 0, 0, 0);
-        if (vec) {
+        if constexpr (FAST) {
             if (n > 0) u = *reinterpret_cast<const uint4*>(p);
         } else {
-            T* e = reinterpret_cast<T*>(&u);
+            uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
             for (int i = 0; i < E; ++i)
-                if (i < n) e[i] = p[i];
+                if (i < n) {
+                    if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(p[i]);
+                    else w[i / 2] |= static_cast<uint32_t>(__bfloat16_as_ushort(p[i])) << (16 * (i & 1));
+                }
+            u = make_uint4(w[0], w[1], w[2], w[3]);
         }
         return u;
     }
@@ -72,25 +78,23 @@ struct Lane {
         for (int i = 0; i < E; ++i)
             x[i] = __uint_as_float(sizeof(T) == 4 ? w[i % 4] : i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
     }
-    static __device__ __forceinline__ void store(T* p, bool vec, int n, const float (&x)[E]) {
-        uint32_t w[4];
+    static __device__ __forceinline__ void store(T* p, int n, const float (&x)[E]) {
+        if constexpr (FAST) {
+            uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (sizeof(T) == 4) {
-                w[i] = __float_as_uint(x[i]);
-            } else {
-                const __nv_bfloat162 t = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-                w[i] = *reinterpret_cast<const uint32_t*>(&t);
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (sizeof(T) == 4) {
+                    w[i] = __float_as_uint(x[i]);
+                } else {
+                    const __nv_bfloat162 t = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+                    w[i] = *reinterpret_cast<const uint32_t*>(&t);
+                }
             }
-        }
-        uint4 u = make_uint4(w[0], w[1], w[2], w[3]);
-        if (vec) {
-            if (n > 0) *reinterpret_cast<uint4*>(p) = u;
+            if (n > 0) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
         } else {
-            const T* e = reinterpret_cast<const T*>(&u);
 #pragma unroll
             for (int i = 0; i < E; ++i)
-                if (i < n) p[i] = e[i];
+                if (i < n) p[i] = static_cast<T>(x[i]);
         }
     }
 };
@@ -105,7 +109,7 @@ __device__ __forceinline__ float row_sum(float v) {
 // A lane's share of a row, NV vectors l, l + G, ..: cos and sin (of the sign that the partner enters with) of its dimensions.
 template <typename T, int G, int NV, int MODE>
 struct Share {
-    static constexpr int E = Lane<T>::E;
+    static constexpr int E = 16 / sizeof(T);
     float c[NV][E], s[NV][E];
     int n[NV], turned[NV];     // dimensions of a vector, and how many of them are rotated
     int l;
@@ -123,7 +127,7 @@ struct Share {
             for (int e = 0; e < E; ++e) {
                 const int i = dim_of(k, e);
                 const bool in = e < turned[k], second = MODE == kPairs ? e & 1 : i >= half;
-                const float2 t = table[in ? (MODE == kPairs ? i / 2 : second ? i - half : i) : 0];
+                const float2 t = in ? table[MODE == kPairs ? i / 2 : second ? i - half : i] : make_float2(1.0f, 0.0f);
                 c[k][e] = t.x;
                 s[k][e] = second ? t.y : -t.y;
             }
@@ -177,122 +181,136 @@ struct Share {
     }
 };
 
-// cos and sin of the block's tokens from t0 on; whether a token has a position.
+// cos and sin of a token's pairs, by a warp; whether the token has a position.
 template <typename T>
-__device__ __forceinline__ void fill_table(const Rotate<T>& p, int64_t t0, float2* table, int* known) {
-    for (int i = threadIdx.x; i < p.per * max(1, p.half); i += kThreads) {
-        const int a = i / max(1, p.half), j = i - a * max(1, p.half);
-        const int64_t t = t0 + a;
-        int64_t pos = t;
-        bool is = t < p.tokens;
-        if (is && p.pos) {
-            pos = p.pos[t];
-        } else if (is && p.start) {
-            const int b = kv_sequence_of(p.start, p.batch, t);
-            is = b >= 0;
-            if (is) pos = p.first[b] + (t - p.start[b]);
-        }
-        if (j == 0) known[a] = is;
-        if (j < p.half) {
-            const int32_t turn = static_cast<int32_t>((static_cast<uint64_t>(pos) * p.freq[j]) >> 32);
-            float s, c;
-            sincospif(static_cast<float>(turn) * 0x1p-31f, &s, &c);
-            table[i] = make_float2(c * p.scale, s * p.scale);
-        }
+__device__ __forceinline__ bool fill_table(const Rotate<T>& p, int64_t t, float2* table) {
+    int64_t pos = t;
+    bool is = true;
+    if (p.pos) {
+        pos = p.pos[t];
+    } else if (p.start) {
+        const int b = kv_sequence_of_warp(p.start, p.batch, t);
+        is = b >= 0;
+        if (is) pos = p.first[b] + (t - p.start[b]);
     }
+    __syncwarp();   // the table's last use
+    for (int j = threadIdx.x & 31; j < p.half; j += 32) {
+        const int32_t turn = static_cast<int32_t>((static_cast<uint64_t>(pos) * p.freq[j]) >> 32);
+        float s, c;
+        sincospif(static_cast<float>(turn) * 0x1p-31f, &s, &c);
+        table[j] = make_float2(c * p.scale, s * p.scale);
+    }
+    __syncwarp();
+    return is;
+}
+// A warp looks at 32 / G rows at a time, first of the queries, then of the keys.
+template <typename T, int G>
+struct Looks {
+    int queries, all;
+    __device__ __forceinline__ explicit Looks(const Rotate<T>& p) {
+        constexpr int R = 32 / G;
+        queries = (p.s[0].heads + R - 1) / R;
+        all = queries + (p.s[1].heads + R - 1) / R;
+    }
+};
+__host__ __device__ constexpr int warp_floats(int mode, int g, int half, int dim) {   // of shared memory
+    return 2 * half + (mode == kHalvesOdd ? 32 / g * dim : 0);
 }
 
-// Blocks (tokens, heads): `per` tokens, the slots of G lanes dealt to them in turn, each going through heads.
-template <typename T, int G, int NV, int MODE>
-__global__ void __launch_bounds__(kThreads) qk_rotate_kernel(const Rotate<T> p) {
-    constexpr int E = Lane<T>::E, kSlots = kThreads / G;
-    extern __shared__ __align__(16) uint8_t smem[];
-    float2* table = reinterpret_cast<float2*>(smem);
-    __shared__ int known[kSlots];
-    const int slot = threadIdx.x / G, mine = slot & (p.per - 1);
-    const int64_t t0 = static_cast<int64_t>(blockIdx.x) * p.per, t = t0 + mine;
-    float* xch = reinterpret_cast<float*>(table + p.per * max(1, p.half)) + slot * (MODE == kHalvesOdd ? p.dim : 0);
-    Share<T, G, NV, MODE> sh(threadIdx.x % G, p.dim);
-    const int heads = min(p.s[0].heads + p.s[1].heads - static_cast<int>(blockIdx.y) * p.part, p.part);
-    const int h0 = blockIdx.y * p.part, step = kSlots / p.per, turns = (heads + step - 1) / step;
+// A warp to a part of a token's rows.
+template <typename T, int G, int NV, int MODE, bool FAST>
+__global__ void __launch_bounds__(kThreads, FAST && NV == 1 ? 7 : 4) qk_rotate_kernel(const Rotate<T> p) {
+    using L = Lane<T, FAST>;
+    constexpr int E = L::E, R = 32 / G;
+    extern __shared__ __align__(16) float smem[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane / G;
+    const int64_t unit = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + warp;
+    const int64_t t = unit / p.parts;
+    if (t >= p.tokens) return;
+    float* mem = smem + warp * ((warp_floats(MODE, G, p.half, p.dim) + 1) & ~1);
+    float2* table = reinterpret_cast<float2*>(mem);
+    float* xch = mem + 2 * p.half + sub * p.dim;
+    Share<T, G, NV, MODE> sh(lane % G, p.dim);
+    const Looks<T, G> looks(p);
+    const int first = static_cast<int>(unit - t * p.parts) * p.part, last = min(first + p.part, looks.all);
     pdl_wait();
     pdl_launch_dependents();
-    uint4 raw[kAhead][NV], w[2][NV];
-    bool is = t < p.tokens;
-    const bool any = p.s[0].w || p.s[1].w;
-    auto head_of = [&](int i) { return slot / p.per + i * step; };   // among the block's heads
-    auto fetch = [&](int i0) {
+    const T* x0 = p.s[0].x + t * p.s[0].x_token + sh.dim_of(0, 0);
+    const T* x1 = p.s[1].x + t * p.s[1].x_token + sh.dim_of(0, 0);
+    uint4 raw[kAhead][NV];
+    auto fetch = [&](int i, uint4 (&u)[NV]) {
+        const bool key = i >= looks.queries;
+        const int h = (key ? i - looks.queries : i) * R + sub;
+        const bool here = i < last && h < (key ? p.s[1].heads : p.s[0].heads);
+        const T* src = key ? x1 + h * p.s[1].x_head : x0 + h * p.s[0].x_head;
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const int hh = head_of(i0 + u), h = h0 + hh, side = h >= p.s[0].heads;
-            const Rows<T>& s = p.s[side];
-            const T* src = s.x + t * s.x_token + static_cast<int64_t>(side ? h - p.s[0].heads : h) * s.x_head;
-#pragma unroll
-            for (int k = 0; k < NV; ++k)
-                if (is && hh < heads) raw[u][k] = Lane<T>::load(src + sh.dim_of(k, 0), p.vec, sh.n[k]);
-        }
+        for (int k = 0; k < NV; ++k) u[k] = here ? L::load(src + k * G * E, sh.n[k]) : make_uint4(0, 0, 0, 0);
     };
-    fetch(0);
 #pragma unroll
-    for (int side = 0; side < 2; ++side)
+    for (int u = 0; u < kAhead; ++u) fetch(first + u, raw[u]);
+    uint4 w[NV];
+    auto weights = [&](int side) {
 #pragma unroll
         for (int k = 0; k < NV; ++k)
-            w[side][k] = p.s[side].w ? Lane<T>::load(p.s[side].w + sh.dim_of(k, 0), p.vec, sh.n[k]) : make_uint4(0, 0, 0, 0);
-    fill_table(p, t0, table, known);
-    __syncthreads();
-    sh.take(table + mine * p.half, p.half);
-    is = is && known[mine];
-    for (int i0 = 0; i0 < turns; i0 += kAhead) {
-        if (i0 > 0) fetch(i0);
+            w[k] = p.s[side].w ? L::load(p.s[side].w + sh.dim_of(k, 0), sh.n[k]) : make_uint4(0, 0, 0, 0);
+    };
+    weights(first >= looks.queries);
+    const bool is = fill_table(p, t, table);
+    if (!is) return;
+    sh.take(table, p.half);
+    const float over = 1.0f / static_cast<float>(p.dim);
+    for (int i0 = first; i0 < last; i0 += kAhead) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            if (i0 + u >= turns) break;
-            const int hh = head_of(i0 + u), h = h0 + hh, side = h >= p.s[0].heads;
-            const Rows<T>& s = p.s[side];
-            const bool here = is && hh < heads;
+            const int i = i0 + u;
+            if (i >= last) break;
             float x[NV][E];
 #pragma unroll
-            for (int k = 0; k < NV; ++k) Lane<T>::unpack(here ? raw[u][k] : make_uint4(0, 0, 0, 0), x[k]);
-            float sum = 0.0f;
-            if (any) {
+            for (int k = 0; k < NV; ++k) L::unpack(raw[u][k], x[k]);
+            fetch(i + kAhead, raw[u]);
+            const int side = i >= looks.queries, h = (side ? i - looks.queries : i) * R + sub;
+            const Rows<T>& s = p.s[side];
+            if (i == looks.queries) weights(1);
+            if (s.w) {
+                float sum = 0.0f;
 #pragma unroll
                 for (int k = 0; k < NV; ++k)
 #pragma unroll
                     for (int e = 0; e < E; ++e) sum = fmaf(x[k][e], x[k][e], sum);
                 sum = row_sum<G>(sum);
-            }
-            if (s.w) {
-                const float r = __frsqrt_rn(sum / static_cast<float>(p.dim) + p.eps);
+                const float r = __frsqrt_rn(fmaf(sum, over, p.eps));
 #pragma unroll
                 for (int k = 0; k < NV; ++k) {
                     float g[E];
-                    Lane<T>::unpack(side ? w[1][k] : w[0][k], g);
+                    L::unpack(w[k], g);
 #pragma unroll
                     for (int e = 0; e < E; ++e) x[k][e] = x[k][e] * r * g[e];
                 }
             }
             sh.template turn<false>(x, p.half, xch);
-            if (here) {
-                T* dst = s.out + t * s.o_token + static_cast<int64_t>(side ? h - p.s[0].heads : h) * s.o_head;
+            if (h < s.heads) {
+                T* dst = s.out + t * s.o_token + h * s.o_head;
 #pragma unroll
-                for (int k = 0; k < NV; ++k) Lane<T>::store(dst + sh.dim_of(k, 0), p.vec, sh.n[k], x[k]);
+                for (int k = 0; k < NV; ++k) L::store(dst + sh.dim_of(k, 0), sh.n[k], x[k]);
             }
         }
     }
 }
 
-// The same backwards. Blocks stay and go through the tokens, so that the weights' gradients are summed in registers, then over
-// the block's slots in order, then (rotate_sums_kernel) over the blocks in order.
-template <typename T, int G, int NV, int MODE>
-__global__ void __launch_bounds__(kThreads) qk_rotate_grad_kernel(const Rotate<T> p) {
-    constexpr int E = Lane<T>::E, kSlots = kThreads / G;
-    extern __shared__ __align__(16) uint8_t smem[];
-    float2* table = reinterpret_cast<float2*>(smem);
-    __shared__ int known[kSlots];
-    const int slot = threadIdx.x / G, mine = slot & (p.per - 1);
-    float* xch = reinterpret_cast<float*>(table + p.per * max(1, p.half)) + slot * (MODE == kHalvesOdd ? p.dim : 0);
-    Share<T, G, NV, MODE> sh(threadIdx.x % G, p.dim);
-    const int heads = p.s[0].heads + p.s[1].heads, step = kSlots / p.per;
+// The same backwards. The warps go through units of a token's part in turn; the weights' gradients are summed in registers, then
+// over the block's slots in order, then (rotate_sums_kernel) over the blocks in order.
+template <typename T, int G, int NV, int MODE, bool FAST>
+__global__ void __launch_bounds__(kGradThreads, NV == 1 ? 2 : 1) qk_rotate_grad_kernel(const Rotate<T> p) {
+    using L = Lane<T, FAST>;
+    constexpr int E = L::E, R = 32 / G, kWarps = kGradThreads / 32, kSlots = kWarps * R;
+    extern __shared__ __align__(16) float smem[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane / G;
+    float* mem = smem + warp * ((warp_floats(MODE, G, p.half, p.dim) + 1) & ~1);
+    float2* table = reinterpret_cast<float2*>(mem);
+    float* xch = mem + 2 * p.half + sub * p.dim;
+    Share<T, G, NV, MODE> sh(lane % G, p.dim);
+    const Looks<T, G> looks(p);
+    const int64_t units = p.tokens * p.parts, step = static_cast<int64_t>(gridDim.x) * kWarps;
     pdl_wait();
     pdl_launch_dependents();
     uint4 w[2][NV];
@@ -301,87 +319,110 @@ __global__ void __launch_bounds__(kThreads) qk_rotate_grad_kernel(const Rotate<T
     for (int side = 0; side < 2; ++side)
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            w[side][k] = p.s[side].w ? Lane<T>::load(p.s[side].w + sh.dim_of(k, 0), p.vec, sh.n[k]) : make_uint4(0, 0, 0, 0);
+            w[side][k] = p.s[side].w ? L::load(p.s[side].w + sh.dim_of(k, 0), sh.n[k]) : make_uint4(0, 0, 0, 0);
 #pragma unroll
             for (int e = 0; e < E; ++e) gw[side][k][e] = 0.0f;
         }
     const float over = 1.0f / static_cast<float>(p.dim);
-    for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * p.per; t0 < p.tokens; t0 += static_cast<int64_t>(gridDim.x) * p.per) {
-        const int64_t t = t0 + mine;
-        __syncthreads();
-        fill_table(p, t0, table, known);
-        __syncthreads();
-        sh.take(table + mine * p.half, p.half);
-        const bool is = known[mine];
-        // queries, then keys, so that each side's sums stay where they are
+    // the look that is fetched next: kGradAhead before the one that is worked on, across units
+    int64_t next_unit = static_cast<int64_t>(blockIdx.x) * kWarps + warp, next_t = 0;
+    int next = 0, next_last = 0;
+    auto enter = [&] {
+        if (next_unit >= units) return;
+        next_t = next_unit / p.parts;
+        next = static_cast<int>(next_unit - next_t * p.parts) * p.part;
+        next_last = min(next + p.part, looks.all);
+    };
+    uint4 rx[kGradAhead][NV], rg[kGradAhead][NV];
+    auto fetch = [&](uint4 (&x)[NV], uint4 (&g)[NV]) {
+        if (next_unit >= units) return;
+        const int side = next >= looks.queries, h = (side ? next - looks.queries : next) * R + sub;
+        const Rows<T>& s = p.s[side];
+        const bool here = h < s.heads;
 #pragma unroll
-        for (int side = 0; side < 2; ++side) {
+        for (int k = 0; k < NV; ++k) {
+            x[k] = g[k] = make_uint4(0, 0, 0, 0);
+            if (here) g[k] = L::load(s.gy + next_t * s.g_token + h * s.g_head + sh.dim_of(k, 0), sh.n[k]);
+            if (here && s.w) x[k] = L::load(s.x + next_t * s.x_token + h * s.x_head + sh.dim_of(k, 0), sh.n[k]);
+        }
+        if (++next == next_last) {
+            next_unit += step;
+            enter();
+        }
+    };
+    int64_t unit = next_unit;
+    enter();
+#pragma unroll
+    for (int u = 0; u < kGradAhead; ++u) fetch(rx[u], rg[u]);
+    bool is = false;
+    int64_t t = 0;
+    int i = 0, last = 0;
+    auto begin = [&] {
+        t = unit / p.parts;
+        i = static_cast<int>(unit - t * p.parts) * p.part;
+        last = min(i + p.part, looks.all);
+        is = fill_table(p, t, table);
+        sh.take(table, p.half);
+    };
+    if (unit < units) begin();
+    while (unit < units) {
+#pragma unroll
+        for (int u = 0; u < kGradAhead; ++u) {
+            if (unit >= units) break;
+            float g[NV][E], x[NV][E];
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                L::unpack(rg[u][k], g[k]);
+                L::unpack(rx[u][k], x[k]);
+            }
+            fetch(rx[u], rg[u]);
+            const int side = i >= looks.queries, h = (side ? i - looks.queries : i) * R + sub;
             const Rows<T>& s = p.s[side];
-            const bool norm = s.w != nullptr;
-            for (int i0 = 0; i0 * step < s.heads; i0 += kAhead / 2) {
-                uint4 rx[kAhead / 2][NV], rg[kAhead / 2][NV];
+            const bool here = is && h < s.heads;
+            sh.template turn<true>(g, p.half, xch);
+            if (s.w) {
+                float sum = 0.0f, dot = 0.0f, y[NV][E];
 #pragma unroll
-                for (int u = 0; u < kAhead / 2; ++u) {
-                    const int h = slot / p.per + (i0 + u) * step;
-                    const bool here = is && h < s.heads;
-                    const T* gy = s.gy + t * s.g_token + static_cast<int64_t>(h) * s.g_head;
-                    const T* x = s.x + t * s.x_token + static_cast<int64_t>(h) * s.x_head;
+                for (int k = 0; k < NV; ++k) {
+                    L::unpack(side ? w[1][k] : w[0][k], y[k]);
 #pragma unroll
-                    for (int k = 0; k < NV; ++k) {
-                        rg[u][k] = rx[u][k] = make_uint4(0, 0, 0, 0);
-                        if (here) rg[u][k] = Lane<T>::load(gy + sh.dim_of(k, 0), p.vec, sh.n[k]);
-                        if (here && norm) rx[u][k] = Lane<T>::load(x + sh.dim_of(k, 0), p.vec, sh.n[k]);
+                    for (int e = 0; e < E; ++e) {
+                        y[k][e] *= g[k][e];
+                        sum = fmaf(x[k][e], x[k][e], sum);
+                        dot = fmaf(y[k][e], x[k][e], dot);
                     }
                 }
+                sum = row_sum<G>(sum);
+                dot = row_sum<G>(dot);
+                const float r = __frsqrt_rn(fmaf(sum, over, p.eps)), f = dot * over * r * r;
+                auto add = [&](float (&to)[NV][E]) {
 #pragma unroll
-                for (int u = 0; u < kAhead / 2; ++u) {
-                    if ((i0 + u) * step >= s.heads) break;
-                    const int h = slot / p.per + (i0 + u) * step;
-                    float g[NV][E], x[NV][E];
+                    for (int k = 0; k < NV; ++k)
 #pragma unroll
-                    for (int k = 0; k < NV; ++k) {
-                        Lane<T>::unpack(rg[u][k], g[k]);
-                        Lane<T>::unpack(rx[u][k], x[k]);
-                    }
-                    sh.template turn<true>(g, p.half, xch);
-                    if (norm) {
-                        float sum = 0.0f, dot = 0.0f;
-#pragma unroll
-                        for (int k = 0; k < NV; ++k) {
-                            float y[E];
-                            Lane<T>::unpack(w[side][k], y);
-#pragma unroll
-                            for (int e = 0; e < E; ++e) {
-                                sum = fmaf(x[k][e], x[k][e], sum);
-                                dot = fmaf(g[k][e] * y[e], x[k][e], dot);
-                            }
-                        }
-                        sum = row_sum<G>(sum);
-                        dot = row_sum<G>(dot);
-                        const float r = __frsqrt_rn(sum * over + p.eps), f = dot * over * r * r;
-#pragma unroll
-                        for (int k = 0; k < NV; ++k) {
-                            float y[E];
-                            Lane<T>::unpack(w[side][k], y);
-#pragma unroll
-                            for (int e = 0; e < E; ++e) {
-                                gw[side][k][e] = fmaf(g[k][e], x[k][e] * r, gw[side][k][e]);
-                                g[k][e] = r * fmaf(-f, x[k][e], g[k][e] * y[e]);
-                            }
-                        }
-                    }
-                    if (is && h < s.heads) {
-                        T* dst = s.out + t * s.o_token + static_cast<int64_t>(h) * s.o_head;
-#pragma unroll
-                        for (int k = 0; k < NV; ++k) Lane<T>::store(dst + sh.dim_of(k, 0), p.vec, sh.n[k], g[k]);
-                    }
+                        for (int e = 0; e < E; ++e) to[k][e] = fmaf(g[k][e], x[k][e] * r, to[k][e]);
+                };
+                if (is) {
+                    if (side) add(gw[1]);
+                    else add(gw[0]);
                 }
+#pragma unroll
+                for (int k = 0; k < NV; ++k)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) g[k][e] = r * fmaf(-f, x[k][e], y[k][e]);
+            }
+            if (here) {
+                T* dst = s.out + t * s.o_token + h * s.o_head;
+#pragma unroll
+                for (int k = 0; k < NV; ++k) L::store(dst + sh.dim_of(k, 0), sh.n[k], g[k]);
+            }
+            if (++i == last) {
+                unit += step;
+                if (unit < units) begin();
             }
         }
     }
     if (!p.sums) return;
-    // slots in order, one vector of a lane at a time
-    float* all = reinterpret_cast<float*>(smem);   // [kSlots][dim]
+    float* all = smem;   // [kSlots][dim]
 #pragma unroll
     for (int side = 0; side < 2; ++side) {
         __syncthreads();
@@ -389,12 +430,12 @@ __global__ void __launch_bounds__(kThreads) qk_rotate_grad_kernel(const Rotate<T
         for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int e = 0; e < E; ++e)
-                if (e < sh.n[k]) all[slot * p.dim + sh.dim_of(k, e)] = gw[side][k][e];
+                if (e < sh.n[k]) all[(warp * R + sub) * p.dim + sh.dim_of(k, e)] = gw[side][k][e];
         __syncthreads();
-        for (int i = threadIdx.x; i < p.dim; i += kThreads) {
+        for (int d = threadIdx.x; d < p.dim; d += kGradThreads) {
             float sum = 0.0f;
-            for (int q = 0; q < kSlots; ++q) sum += all[q * p.dim + i];
-            p.sums[(static_cast<int64_t>(blockIdx.x) * 2 + side) * p.dim + i] = sum;
+            for (int q = 0; q < kSlots; ++q) sum += all[q * p.dim + d];
+            if (KQ_IN_RANGE(blockIdx.x, kMaxBlocks)) p.sums[(static_cast<int64_t>(blockIdx.x) * 2 + side) * p.dim + d] = sum;
         }
     }
 }
@@ -416,30 +457,29 @@ __global__ void __launch_bounds__(1024) rotate_sums_kernel(const float* __restri
     out[i] = s;
 }
 
-constexpr int kMaxBlocks = 512;   // that a workspace has room for the sums of
 int64_t grad_blocks(int64_t tokens) { return std::min<int64_t>(tokens, kMaxBlocks); }
 
-template <typename T, int G, int NV, int MODE>
+template <typename T, int G, int NV, int MODE, bool FAST>
 kq_status launch(Rotate<T>& p, bool back, float* gqw, float* gkw, cudaStream_t stream) {
-    constexpr int kSlots = kThreads / G;
-    const int heads = p.s[0].heads + p.s[1].heads;
-    const int64_t sms = num_sms();
-    // several tokens to a block where there are many, so that the table costs little; the heads over several blocks
-    // where there are few
-    p.per = 1;
-    while (p.per < kSlots && p.per < 4 && p.tokens >= 2 * p.per * sms * 4) p.per *= 2;
-    p.part = heads;
-    if (p.tokens < 2 * sms) p.part = static_cast<int>(std::max<int64_t>(std::min(heads, kSlots), cdiv(heads, std::max<int64_t>(1, 2 * sms / p.tokens))));
-    size_t smem = p.per * std::max(1, p.half) * sizeof(float2) + (MODE == kHalvesOdd ? kSlots * p.dim * sizeof(float) : 0);
+    constexpr int R = 32 / G;
+    const int64_t looks = cdiv(p.s[0].heads, R) + cdiv(p.s[1].heads, R), warps = static_cast<int64_t>(num_sms()) * 16;
+    // a token's rows go to several warps where tokens are few; not below two looks each, which the table would outweigh
+    const int64_t parts = std::max<int64_t>(1, std::min(cdiv(looks, 2), warps / p.tokens));
+    p.part = static_cast<int32_t>(cdiv(looks, parts));
+    p.parts = static_cast<int32_t>(cdiv(looks, p.part));
+    const size_t floats = (warp_floats(MODE, G, p.half, p.dim) + 1) & ~1;
+    const int64_t units = p.tokens * p.parts;
     if (!back) {
-        const dim3 grid(static_cast<unsigned>(cdiv(p.tokens, p.per)), static_cast<unsigned>(cdiv(heads, p.part)));
-        KQ_CUDA(launch_after(qk_rotate_kernel<T, G, NV, MODE>, grid, dim3(kThreads), smem, stream, p));
+        KQ_CUDA(launch_after(qk_rotate_kernel<T, G, NV, MODE, FAST>, dim3(static_cast<unsigned>(cdiv(units, kThreads / 32))),
+                             dim3(kThreads), kThreads / 32 * floats * sizeof(float), stream, p));
         count_launch();
         return KQ_OK;
     }
-    const int blocks = static_cast<int>(std::min({grad_blocks(p.tokens), cdiv(p.tokens, p.per), sms * 3}));
-    if (p.sums) smem = std::max(smem, kSlots * p.dim * sizeof(float));
-    KQ_CUDA(launch_after(qk_rotate_grad_kernel<T, G, NV, MODE>, dim3(blocks), dim3(kThreads), smem, stream, p));
+    constexpr int kWarps = kGradThreads / 32;
+    const int blocks = static_cast<int>(std::min({grad_blocks(p.tokens), cdiv(units, kWarps), static_cast<int64_t>(num_sms()) * 2}));
+    size_t smem = kWarps * floats * sizeof(float);
+    if (p.sums) smem = std::max(smem, kWarps * R * p.dim * sizeof(float));
+    KQ_CUDA(launch_after(qk_rotate_grad_kernel<T, G, NV, MODE, FAST>, dim3(blocks), dim3(kGradThreads), smem, stream, p));
     count_launch();
     if (p.sums) {
         KQ_CUDA(launch_after(rotate_sums_kernel, dim3(static_cast<unsigned>(cdiv(p.dim, 32)), 2), dim3(1024), 0, stream,
@@ -450,20 +490,24 @@ kq_status launch(Rotate<T>& p, bool back, float* gqw, float* gkw, cudaStream_t s
 }
 
 template <typename T, int G, int NV>
-kq_status launch_mode(Rotate<T>& p, bool pairs, bool back, float* gqw, float* gkw, cudaStream_t stream) {
-    if (pairs) return launch<T, G, NV, kPairs>(p, back, gqw, gkw, stream);
-    if (p.half % Lane<T>::E == 0) return launch<T, G, NV, kHalves>(p, back, gqw, gkw, stream);
-    return launch<T, G, NV, kHalvesOdd>(p, back, gqw, gkw, stream);
+kq_status launch_mode(Rotate<T>& p, bool fast, bool pairs, bool back, float* gqw, float* gkw, cudaStream_t stream) {
+    if (!fast) {   // rows of any alignment: one value at a time, partners through shared memory where they are not neighbours
+        return pairs ? launch<T, G, NV, kPairs, false>(p, back, gqw, gkw, stream)
+                     : launch<T, G, NV, kHalvesOdd, false>(p, back, gqw, gkw, stream);
+    }
+    if (pairs) return launch<T, G, NV, kPairs, true>(p, back, gqw, gkw, stream);
+    if (p.half % (16 / sizeof(T)) == 0) return launch<T, G, NV, kHalves, true>(p, back, gqw, gkw, stream);
+    return launch<T, G, NV, kHalvesOdd, true>(p, back, gqw, gkw, stream);
 }
-kq_status launch_dim(Rotate<__nv_bfloat16>& p, bool pairs, bool back, float* gqw, float* gkw, cudaStream_t stream) {
-    if (p.dim <= 64) return launch_mode<__nv_bfloat16, 8, 1>(p, pairs, back, gqw, gkw, stream);
-    if (p.dim <= 128) return launch_mode<__nv_bfloat16, 16, 1>(p, pairs, back, gqw, gkw, stream);
-    return launch_mode<__nv_bfloat16, 32, 1>(p, pairs, back, gqw, gkw, stream);
+kq_status launch_dim(Rotate<__nv_bfloat16>& p, bool fast, bool pairs, bool back, float* gqw, float* gkw, cudaStream_t stream) {
+    if (p.dim <= 64) return launch_mode<__nv_bfloat16, 8, 1>(p, fast, pairs, back, gqw, gkw, stream);
+    if (p.dim <= 128) return launch_mode<__nv_bfloat16, 16, 1>(p, fast, pairs, back, gqw, gkw, stream);
+    return launch_mode<__nv_bfloat16, 32, 1>(p, fast, pairs, back, gqw, gkw, stream);
 }
-kq_status launch_dim(Rotate<float>& p, bool pairs, bool back, float* gqw, float* gkw, cudaStream_t stream) {
-    if (p.dim <= 64) return launch_mode<float, 16, 1>(p, pairs, back, gqw, gkw, stream);
-    if (p.dim <= 128) return launch_mode<float, 32, 1>(p, pairs, back, gqw, gkw, stream);
-    return launch_mode<float, 32, 2>(p, pairs, back, gqw, gkw, stream);
+kq_status launch_dim(Rotate<float>& p, bool fast, bool pairs, bool back, float* gqw, float* gkw, cudaStream_t stream) {
+    if (p.dim <= 64) return launch_mode<float, 16, 1>(p, fast, pairs, back, gqw, gkw, stream);
+    if (p.dim <= 128) return launch_mode<float, 32, 1>(p, fast, pairs, back, gqw, gkw, stream);
+    return launch_mode<float, 32, 2>(p, fast, pairs, back, gqw, gkw, stream);
 }
 
 // What both calls check of a set of rows.
@@ -512,9 +556,8 @@ kq_status run(const kq_rotation* r, int64_t tokens, int64_t dim, const kq_heads*
     p.half = static_cast<int32_t>(r->rot / 2);
     p.scale = r->scale;
     p.eps = eps;
-    p.vec = !((bits | dim * sizeof(T)) & 15u);
     p.sums = sums;
-    return launch_dim(p, r->interleaved != 0, gq != nullptr, gqw, gkw, stream);
+    return launch_dim(p, !((bits | dim * sizeof(T)) & 15u), r->interleaved != 0, gq != nullptr, gqw, gkw, stream);
 }
 
 // The arguments that both calls share. side i needs inputs where it has outputs.

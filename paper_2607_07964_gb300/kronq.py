@@ -8,6 +8,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
+import struct
 
 import torch
 
@@ -518,14 +519,9 @@ def _rows3(t, name, heads=None, dim=None):
         raise ValueError(f"{name} must have {heads} heads of {dim}, got {tuple(t.shape)}")
 
 
-class _Rotation(ctypes.Structure):
-    _fields_ = [("freq", ctypes.c_void_p), ("rot", ctypes.c_int64), ("pos", ctypes.c_void_p), ("start", ctypes.c_void_p),
-                ("first", ctypes.c_void_p), ("batch", ctypes.c_int64), ("interleaved", ctypes.c_int), ("scale", ctypes.c_float)]
-
-
-class _Heads(ctypes.Structure):
-    _fields_ = [("data", ctypes.c_void_p), ("heads", ctypes.c_int64), ("token_stride", ctypes.c_int64),
-                ("head_stride", ctypes.c_int64)]
+# kq_heads and kq_rotation as the library reads them
+_HEADS = struct.Struct("@Pqqq").pack
+_ROTATION = struct.Struct("@PqPPPqif").pack
 
 
 def kq_rotation_freq(theta, device="cuda"):
@@ -537,29 +533,31 @@ def kq_rotation_freq(theta, device="cuda"):
 def _heads(t, name, dtype, T, dim, heads=None):
     if t is None:
         return None
-    _rows3(t, name, heads, dim)
-    _need(t, name, dtype, contiguous=False)
-    if t.shape[0] != T:
-        raise ValueError(f"{name} must have {T} tokens, got {t.shape[0]}")
-    return ctypes.byref(_Heads(t.data_ptr(), t.shape[1], t.stride(0), t.stride(1)))
+    shape, stride = t.shape, t.stride()
+    if t.dtype is not dtype or not t.is_cuda or len(shape) != 3 or stride[2] != 1 or shape[2] != dim or shape[0] != T or (
+            heads is not None and shape[1] != heads):
+        _rows3(t, name, heads, dim)
+        _need(t, name, dtype, contiguous=False)
+        if shape[0] != T:
+            raise ValueError(f"{name} must have {T} tokens, got {shape[0]}")
+    if shape[1] == 0:
+        raise ValueError(f"{name} must have at least one head")
+    return _HEADS(t.data_ptr(), shape[1], stride[0], stride[1])
 
 
 def _rotation(freq, pos, start, first, interleaved, scale, T):
     _need(freq, "freq", torch.int64)
-    _need(pos, "pos", torch.int32, (T,))
-    batch = 0
-    if first is not None or start is not None:
-        if first is None or start is None:
-            raise ValueError("start and first go together")
-        batch = first.shape[0]
-        _need(first, "first", torch.int32, (batch,))
-        _need(start, "start", torch.int32, (batch + 1,))
-    return _Rotation(freq.data_ptr(), 2 * freq.numel(), _ptr(pos), _ptr(start), _ptr(first), batch, int(interleaved), float(scale))
-
-
-def _no_empty(t, name):
-    if t is not None and t.shape[1] == 0:
-        raise ValueError(f"{name} must have at least one head")
+    if first is None and start is None:
+        if pos is None:
+            return _ROTATION(freq.data_ptr(), 2 * freq.numel(), 0, 0, 0, 0, interleaved, scale)
+        _need(pos, "pos", torch.int32, (T,))
+        return _ROTATION(freq.data_ptr(), 2 * freq.numel(), pos.data_ptr(), 0, 0, 0, interleaved, scale)
+    if first is None or start is None or pos is not None:
+        raise ValueError("start and first go together, without pos")
+    batch = first.shape[0]
+    _need(first, "first", torch.int32, (batch,))
+    _need(start, "start", torch.int32, (batch + 1,))
+    return _ROTATION(freq.data_ptr(), 2 * freq.numel(), 0, start.data_ptr(), first.data_ptr(), batch, interleaved, scale)
 
 
 def kq_qk_rotate(q, k, q_out, k_out, freq, pos=None, start=None, first=None, interleaved: bool = False, scale: float = 1.0,
@@ -569,17 +567,15 @@ def kq_qk_rotate(q, k, q_out, k_out, freq, pos=None, start=None, first=None, int
     (start [batch + 1], first [batch]), or the index. freq: kq_rotation_freq. An output may be its input."""
     dtype = _dtype(q, "q")
     T, heads, dim = q.shape
-    for t, n in ((q, "q"), (k, "k")):
-        _no_empty(t, n)
-    for t, n in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        _need(t, n, q.dtype, (dim,))
+    ty = q.dtype
+    _need(q_weight, "q_weight", ty, (dim,))
+    _need(k_weight, "k_weight", ty, (dim,))
     if (k is None) != (k_out is None):
         raise ValueError("k and k_out go together")
-    r = _rotation(freq, pos, start, first, interleaved, scale, T)
-    _ok(lib().kq_qk_rotate(ctypes.byref(r), dtype, T, dim, _heads(q, "q", q.dtype, T, dim), _heads(k, "k", q.dtype, T, dim),
-                           _heads(q_out, "q_out", q.dtype, T, dim, heads),
-                           _heads(k_out, "k_out", q.dtype, T, dim, None if k is None else k.shape[1]), _ptr(q_weight),
-                           _ptr(k_weight), float(eps), _stream(stream)), "kq_qk_rotate")
+    _ok(lib().kq_qk_rotate(_rotation(freq, pos, start, first, interleaved, scale, T), dtype, T, dim, _heads(q, "q", ty, T, dim),
+                           _heads(k, "k", ty, T, dim), _heads(q_out, "q_out", ty, T, dim, heads),
+                           _heads(k_out, "k_out", ty, T, dim, None if k is None else k.shape[1]), _ptr(q_weight),
+                           _ptr(k_weight), eps, _stream(stream)), "kq_qk_rotate")
 
 
 def kq_qk_rotate_grad_workspace(q, k=None) -> int:
@@ -594,22 +590,20 @@ def kq_qk_rotate_grad(q, k, gq, gk, q_out, k_out, freq, pos=None, start=None, fi
     gq_weight and gk_weight [dim] fp32, where they are given (ws then). q and k may be None where there is no weight."""
     dtype = _dtype(gq, "gq")
     T, heads, dim = gq.shape
-    for t, n in ((gq, "gq"), (gk, "gk")):
-        _no_empty(t, n)
-    for t, n in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        _need(t, n, gq.dtype, (dim,))
-    for t, n in ((gq_weight, "gq_weight"), (gk_weight, "gk_weight")):
-        _need(t, n, torch.float32, (dim,))
+    ty, one = gq.dtype, (dim,)
+    _need(q_weight, "q_weight", ty, one)
+    _need(k_weight, "k_weight", ty, one)
+    _need(gq_weight, "gq_weight", torch.float32, one)
+    _need(gk_weight, "gk_weight", torch.float32, one)
     if (gk is None) != (k_out is None):
         raise ValueError("gk and k_out go together")
     _need(ws, "ws", torch.uint8)
-    r = _rotation(freq, pos, start, first, interleaved, scale, T)
     kv = None if gk is None else gk.shape[1]
-    _ok(lib().kq_qk_rotate_grad(ctypes.byref(r), dtype, T, dim, _heads(q, "q", gq.dtype, T, dim, heads),
-                                _heads(k, "k", gq.dtype, T, dim, kv), _heads(gq, "gq", gq.dtype, T, dim),
-                                _heads(gk, "gk", gq.dtype, T, dim), _heads(q_out, "q_out", gq.dtype, T, dim, heads),
-                                _heads(k_out, "k_out", gq.dtype, T, dim, kv), _ptr(q_weight), _ptr(k_weight), float(eps),
-                                _ptr(gq_weight), _ptr(gk_weight), _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)),
+    _ok(lib().kq_qk_rotate_grad(_rotation(freq, pos, start, first, interleaved, scale, T), dtype, T, dim,
+                                _heads(q, "q", ty, T, dim, heads), _heads(k, "k", ty, T, dim, kv), _heads(gq, "gq", ty, T, dim),
+                                _heads(gk, "gk", ty, T, dim), _heads(q_out, "q_out", ty, T, dim, heads),
+                                _heads(k_out, "k_out", ty, T, dim, kv), _ptr(q_weight), _ptr(k_weight), eps, _ptr(gq_weight),
+                                _ptr(gk_weight), _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)),
         "kq_qk_rotate_grad")
 
 

@@ -7,7 +7,16 @@ import pytest
 
 import rotate_reference as ref
 
-P = ctypes.c_void_p
+P, I64 = ctypes.c_void_p, ctypes.c_int64
+
+
+class Heads(ctypes.Structure):   # as include/kronq.h has them
+    _fields_ = [("data", P), ("heads", I64), ("token_stride", I64), ("head_stride", I64)]
+
+
+class Rotation(ctypes.Structure):
+    _fields_ = [("freq", P), ("rot", I64), ("pos", P), ("start", P), ("first", P), ("batch", I64), ("interleaved", ctypes.c_int),
+                ("scale", ctypes.c_float)]
 
 
 @pytest.fixture(scope="module")
@@ -57,13 +66,13 @@ def test_angles_of_far_positions():
 def _heads(K, **over):
     f = dict(data=256, heads=2, token_stride=256, head_stride=128)
     f.update(over)
-    return ctypes.byref(K._Heads(*f.values()))
+    return ctypes.byref(Heads(*f.values()))
 
 
 def _rotation(K, **over):
     f = dict(freq=256, rot=64, pos=256, start=None, first=None, batch=0, interleaved=0, scale=1.0)
     f.update(over)
-    return ctypes.byref(K._Rotation(*f.values()))
+    return ctypes.byref(Rotation(*f.values()))
 
 
 def test_arguments_are_refused_on_the_host(K):
@@ -87,6 +96,12 @@ def test_arguments_are_refused_on_the_host(K):
         args[at] = value
         assert lib.kq_qk_rotate_grad(*args) == status, (at, value)
     assert lib.kq_qk_rotate_grad_workspace(0, 128) == 0 and lib.kq_qk_rotate_grad_workspace(3, 128) == 3 * 2 * 128 * 4
+
+
+def test_the_binding_packs_the_structures_of_the_header(K):
+    assert len(K._HEADS(0, 0, 0, 0)) == ctypes.sizeof(Heads)
+    r = Rotation.from_buffer_copy(K._ROTATION(8, 64, 16, 24, 32, 5, True, 1.5))
+    assert [getattr(r, n) for n, _ in Rotation._fields_] == [8, 64, 16, 24, 32, 5, 1, 1.5]
 
 
 def test_binding_refuses_host_tensors_and_wrong_shapes(K):
