@@ -67,6 +67,31 @@ __device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uin
         "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
         : "memory");
 }
+// Whether p holds in all 256 threads of the eight result warps; a barrier for them.
+__device__ __forceinline__ bool named_all(bool p) {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred a, b;\n\t"
+        "setp.ne.u32 a, %1, 0;\n\t"
+        "barrier.red.and.pred b, 1, 256, a;\n\t"
+        "selp.u32 %0, 1, 0, b;\n\t}"
+        : "=r"(r)
+        : "r"(static_cast<uint32_t>(p))
+        : "memory");
+    return r != 0;
+}
+// 16 consecutive fp32 columns of the calling warp's 32 lanes of tensor memory.
+__device__ __forceinline__ void tmem_ld16(uint32_t at, float (&v)[16]) {
+    uint32_t r[16];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(at)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
 // 32 bytes, on a 32-byte boundary.
 __device__ __forceinline__ void store32(void* p, const uint32_t (&v)[8]) {
     asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
@@ -77,6 +102,20 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     const __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&t);
 }
+
+// The sums over one set of logits, against their maximum, joined with those over another: against the larger maximum.
+struct Sums {
+    float m, z, s;
+    __device__ __forceinline__ void join(float m2, float z2, float s2) {
+        const float top = max_nan(m, m2);
+        if (top == -INFINITY) return;
+        const float a = (m - top) * kLog2e, b = (m2 - top) * kLog2e, fa = ex2(a), fb = ex2(b);
+        // 2^b (s + b z); one against -infinity has none
+        s = (fa > 0.0f || a != a ? fa * fmaf(a, z, s) : 0.0f) + (fb > 0.0f || b != b ? fb * fmaf(b, z2, s2) : 0.0f);
+        z = fa * z + fb * z2;
+        m = top;
+    }
+};
 
 enum Kind { kScore, kDelta, kGx, kGw };
 
@@ -184,6 +223,12 @@ __device__ __forceinline__ void score_row(const Job& j, float (&x)[128], int64_t
     if (KQ_IN_RANGE(at, j.parts)) j.part[row * j.parts + at] = make_float4(m, z[0] + z[1], s[0] + s[1], 0.0f);
 }
 
+// What a logit z contributes to D but for the target's own share: -p (g + ge (ln p + h)).
+__device__ __forceinline__ float delta_of(float z, float lse, float g, float ge, float h) {
+    const float lp = z - lse, p = ex2(lp * kLog2e);
+    return p > 0.0f ? -p * fmaf(ge, lp + h, g) : p == p ? 0.0f : p;
+}
+
 // D of 128 logits of a row: to bf16, zeros from the vocabulary's end on.
 __device__ __forceinline__ void delta_row(const Job& j, float (&x)[128], int64_t row, int64_t col) {
     if (row >= j.T || col >= j.ld_delta) return;
@@ -203,8 +248,7 @@ __device__ __forceinline__ void delta_row(const Job& j, float (&x)[128], int64_t
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int i = 16 * c + 2 * k + e;
-                const float lp = x[i] - lse, p = ex2(lp * kLog2e);
-                q[e] = p > 0.0f ? -p * fmaf(ge, lp + h, g) : p == p ? 0.0f : p;
+                q[e] = delta_of(x[i], lse, g, ge, h);
                 if (none || i >= left) q[e] = 0.0f;
                 if (here && i == at) q[e] += g;
             }
@@ -448,6 +492,234 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
     }
 }
 
+// ---- few rows. The tiles above would take 256 of them whatever there are, and W would come in slower than memory can: here
+// W's rows are the product's rows, 128 to a CTA, and N >= T tokens its columns. The results are taken through shared memory,
+// so that a thread keeps the sums of one token from tile to tile.
+constexpr int kThinThreads = 320;                // loads, products, 8 warps for the results
+constexpr int kThinRows = 128, kThinMost = 128;  // rows of W of a tile, tokens
+constexpr int kThinLd = kThinRows + 4;           // floats between tokens in shared memory
+template <int N>
+struct Thin {
+    static constexpr int kStage = 2 * kBox + N * BK * 2;
+    static constexpr int kOut = N * kThinLd * 4;
+    static constexpr int kStages = (225 * 1024 - kOut - 5 * N * 4 - 1024) / kStage < 10 ? (225 * 1024 - kOut - 5 * N * 4 - 1024) / kStage : 10;
+    static constexpr int kBoxRows = N <= 64 ? N : N / 2;   // of x
+    static constexpr uint32_t kColumns = N == 32 ? 64 : N == 64 ? 128 : 256;   // two accumulators, a power of two
+    static constexpr int kSmem = kStages * kStage + kOut + 5 * N * 4 + 256 + 1024;
+};
+
+template <int MAIN, int N>
+__global__ void __launch_bounds__(kThinThreads, 1)
+linear_thin_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtensorMap mw, const __grid_constant__ Job j) {
+    using S = Thin<N>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    float* out = reinterpret_cast<float*>(smem + S::kStages * S::kStage);   // [N][kThinLd]
+    float* known = out + N * kThinLd;                                       // [5][N] of each token
+    __shared__ uint64_t full[S::kStages], empty[S::kStages], tfull[2], tempty[2], mma_done;
+    __shared__ uint32_t tmem_slot;
+    __shared__ volatile int abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S::kStages; ++s) {
+            mbar_init(&full[s], 1);
+            mbar_init(&empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(&tfull[b], 1);
+            mbar_init(&tempty[b], 8);
+        }
+        mbar_init(&mma_done, 1);
+        abort_flag = 0;
+        fence_mbar_init();
+    }
+    if (warp == 1) {
+        tmem_alloc(&tmem_slot, S::kColumns);
+        tmem_relinquish();
+    }
+    if (warp == 0 && lane == 0) {
+        tma_prefetch_desc(&mx);
+        tma_prefetch_desc(&mw);
+    }
+    if (MAIN == kDelta && threadIdx.x >= 64) {
+        for (int t = threadIdx.x - 64; t < N; t += 256) {
+            const bool is = t < j.T;
+            const int64_t y = is ? j.target[t] : -1;
+            const float lse = is ? j.lse[t] : -INFINITY;
+            known[t] = lse;
+            known[N + t] = y >= 0 && y < j.V ? j.g_logp[t] : 0.0f;
+            known[2 * N + t] = is && j.g_entropy ? j.g_entropy[t] : 0.0f;
+            known[3 * N + t] = is && j.g_entropy ? j.entropy[t] : 0.0f;
+            reinterpret_cast<int*>(known)[4 * N + t] = y >= 0 && y < j.V && lse != -INFINITY ? static_cast<int>(y) : -1;
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    const int tiles = static_cast<int>((j.w_main + kThinRows - 1) / kThinRows), slabs = static_cast<int>((j.d + BK - 1) / BK);
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int k = 0;
+            bool ok = true;
+            for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
+                const int v = static_cast<int>(j.v_main) + t * kThinRows;
+                for (int s = 0; s < slabs; ++s, ++k) {
+                    const int st = k % S::kStages;
+                    if (!mbar_wait(&empty[st], (static_cast<uint32_t>(k / S::kStages) & 1u) ^ 1u, &abort_flag)) {
+                        ok = false;
+                        break;
+                    }
+                    mbar_arrive_expect_tx(&full[st], S::kStage);
+                    uint8_t* base = smem + st * S::kStage;
+                    tma_load_2d(base, &mw, &full[st], s * BK, v);
+                    tma_load_2d(base + kBox, &mw, &full[st], s * BK, v + 64);
+#pragma unroll
+                    for (int i = 0; i < N / S::kBoxRows; ++i)
+                        tma_load_2d(base + 2 * kBox + i * S::kBoxRows * BK * 2, &mx, &full[st], s * BK, i * S::kBoxRows);
+                }
+            }
+            for (int i = (k > S::kStages ? k - S::kStages : 0); i < k; ++i)   // whatever is under way has landed
+                wait_quiet(&full[i % S::kStages], static_cast<uint32_t>(i / S::kStages) & 1u);
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            constexpr uint32_t idesc = idesc_bf16_mn_major(kThinRows, N) & ~(3u << 15);
+            int k = 0, cc = 0;
+            bool ok = true;
+            for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
+                for (int s0 = 0; s0 < slabs && ok; s0 += kDrainLogits, ++cc) {
+                    const int buf = cc & 1;
+                    if (!mbar_wait(&tempty[buf], ((static_cast<uint32_t>(cc) >> 1) & 1u) ^ 1u, &abort_flag)) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    const int s1 = min(slabs, s0 + kDrainLogits);
+                    for (int s = s0; s < s1; ++s, ++k) {
+                        const int st = k % S::kStages;
+                        if (!mbar_wait(&full[st], static_cast<uint32_t>(k / S::kStages) & 1u, &abort_flag)) {
+                            ok = false;
+                            break;
+                        }
+                        tc_fence_after();
+                        const uint32_t sa = smem_u32(smem + st * S::kStage), sb = sa + 2 * kBox;
+#pragma unroll
+                        for (int q = 0; q < BK / 16; ++q)
+                            tc_mma_f16(tmem + buf * N, smem_desc_sw128(sa + q * 32, 16, 1024), smem_desc_sw128(sb + q * 32, 16, 1024), idesc,
+                                       (s > s0 || q > 0) ? 1u : 0u);
+                        tc_commit(&empty[st]);
+                    }
+                    if (ok) tc_commit(&tfull[buf]);
+                }
+            }
+            tc_commit(&mma_done);
+            wait_quiet(&mma_done, 0);
+        }
+    } else {
+        // a thread takes half of the tokens of a row of W from tensor memory, then works on some rows of one token
+        constexpr int kHalf = N / 2, kShare = N == 32 ? 8 : N == 64 ? 4 : 2, kPart = kThinRows / kShare;
+        const int q = warp & 3, h = (warp - 2) >> 2, row = q * 32 + lane, id = threadIdx.x - 64;
+        const int token = id / kShare, from = id % kShare * kPart;
+        const bool mine = token < N && token < j.T;
+        const int64_t y = MAIN == kScore && mine ? j.target[token] : -1;
+        Sums sums = {-INFINITY, 0.0f, 0.0f};
+        int cc = 0;
+        bool ok = true;
+        for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
+            float x[kHalf];
+            for (int s0 = 0; s0 < slabs; s0 += kDrainLogits, ++cc) {
+                const int buf = cc & 1;
+                ok = mbar_wait(&tfull[buf], (static_cast<uint32_t>(cc) >> 1) & 1u, &abort_flag);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                tc_fence_after();
+#pragma unroll
+                for (int p = 0; p < kHalf / 16; ++p) {
+                    float v[16];
+                    tmem_ld16(tmem + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(buf * N + h * kHalf + p * 16), v);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[p * 16 + i] = s0 ? x[p * 16 + i] + v[i] : v[i];
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&tempty[buf]);
+            }
+            ok = named_all(ok);   // the others have read the last tile's, and none has given up
+            if (!ok) break;
+            const int64_t v0 = j.v_main + static_cast<int64_t>(t) * kThinRows;
+            // past the vocabulary: cannot occur
+#pragma unroll
+            for (int i = 0; i < kHalf; ++i) out[(h * kHalf + i) * kThinLd + row] = v0 + row < j.V ? x[i] : -INFINITY;
+            named_all(true);
+            if (MAIN == kDelta) {
+                // a warp takes every eighth token, a lane four rows of W
+                __nv_bfloat16* dst = j.delta + static_cast<int64_t>(t) * kThinRows + 4 * lane;
+#pragma unroll 3
+                for (int i = warp - 2; i < N; i += 8) {
+                    const float lse = known[i], g = known[N + i], ge = known[2 * N + i], hh = known[3 * N + i];
+                    const int at = reinterpret_cast<const int*>(known)[4 * N + i] - static_cast<int>(v0) - 4 * lane;
+                    const float4 a = *reinterpret_cast<const float4*>(out + i * kThinLd + 4 * lane);
+                    float d[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        d[k] = lse == -INFINITY ? 0.0f : delta_of(d[k], lse, g, ge, hh);
+                        if (k == at) d[k] += g;
+                    }
+                    if (i < j.T && KQ_IN_RANGE(t * kThinRows + 4 * lane + 3, j.ld_delta))
+                        *reinterpret_cast<uint2*>(dst + i * j.ld_delta) = make_uint2(pack_bf16(d[0], d[1]), pack_bf16(d[2], d[3]));
+                }
+                continue;
+            }
+            if (mine) {
+                const float4* at = reinterpret_cast<const float4*>(out + token * kThinLd + from);
+                float m = -INFINITY;
+#pragma unroll 8
+                for (int i = 0; i < kPart / 4; ++i) {
+                    const float4 a = at[i];
+                    m = max_nan(max_nan(m, max_nan(a.x, a.y)), max_nan(a.z, a.w));
+                }
+                const float ref = m == -INFINITY ? 0.0f : m;
+                float z[4] = {0.0f, 0.0f, 0.0f, 0.0f}, s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+                for (int i = 0; i < kPart / 4; ++i) {
+                    const float4 a = at[i];
+                    const float w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const float u = fmaxf((w[k] - ref) * kLog2e, kNone), e = ex2(u);
+                        z[k] += e;
+                        s[k] = fmaf(e, u, s[k]);
+                    }
+                }
+                sums.join(m, (z[0] + z[1]) + (z[2] + z[3]), (s[0] + s[1]) + (s[2] + s[3]));
+                const int64_t yr = y - v0 - from;
+                if (y >= 0 && y < j.V && yr >= 0 && yr < kPart) j.zt[token] = out[token * kThinLd + from + yr];
+            }
+            __syncwarp();
+        }
+        if (MAIN == kScore) {
+            if constexpr (kShare > 1) {
+#pragma unroll
+                for (int o = 1; o < kShare; o <<= 1)
+                    sums.join(__shfl_xor_sync(0xffffffffu, sums.m, o), __shfl_xor_sync(0xffffffffu, sums.z, o),
+                              __shfl_xor_sync(0xffffffffu, sums.s, o));
+            }
+            if (mine && from == 0 && KQ_IN_RANGE(blockIdx.x, j.parts))
+                j.part[static_cast<int64_t>(token) * j.parts + blockIdx.x] = make_float4(sums.m, sums.z, sums.s, 0.0f);
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (abort_flag && threadIdx.x == 0) record_error(j.info, -KQ_ERR_TIMEOUT);
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, S::kColumns);
+    }
+}
+
 // Joins the parts of a row: a block to a row.
 __global__ void __launch_bounds__(128) linear_join_kernel(const Job j, float* __restrict__ logp, float* __restrict__ entropy,
                                                           float* __restrict__ lse) {
@@ -455,29 +727,19 @@ __global__ void __launch_bounds__(128) linear_join_kernel(const Job j, float* __
     const int64_t row = blockIdx.x;
     const float4* p = j.part + row * j.parts;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    float M = -INFINITY, Z = 0.0f, S = 0.0f;
-    auto join = [&](float m, float z, float s) {   // sums against m into those against M
-        const float top = max_nan(M, m);
-        if (top == -INFINITY) return;
-        const float a = (M - top) * kLog2e, b = (m - top) * kLog2e, fa = ex2(a), fb = ex2(b);
-        // 2^b (s + b z); a part against -infinity has none
-        S = (fa > 0.0f || a != a ? fa * fmaf(a, Z, S) : 0.0f) + (fb > 0.0f || b != b ? fb * fmaf(b, z, s) : 0.0f);
-        Z = fa * Z + fb * z;
-        M = top;
-    };
+    Sums a = {-INFINITY, 0.0f, 0.0f};
     for (int i = threadIdx.x; i < j.parts; i += 128) {
         const float4 v = p[i];
-        join(v.x, v.y, v.z);
+        a.join(v.x, v.y, v.z);
     }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const float m = __shfl_xor_sync(0xffffffffu, M, o), z = __shfl_xor_sync(0xffffffffu, Z, o), s = __shfl_xor_sync(0xffffffffu, S, o);
-        join(m, z, s);
-    }
-    if (lane == 0) sm[warp] = M, sz[warp] = Z, ss[warp] = S;
+    for (int o = 16; o > 0; o >>= 1)
+        a.join(__shfl_xor_sync(0xffffffffu, a.m, o), __shfl_xor_sync(0xffffffffu, a.z, o), __shfl_xor_sync(0xffffffffu, a.s, o));
+    if (lane == 0) sm[warp] = a.m, sz[warp] = a.z, ss[warp] = a.s;
     __syncthreads();
     if (threadIdx.x) return;
-    for (int w = 1; w < 4; ++w) join(sm[w], sz[w], ss[w]);
+    for (int w = 1; w < 4; ++w) a.join(sm[w], sz[w], ss[w]);
+    const float M = a.m, Z = a.z, S = a.s;
     const int64_t y = j.target[row];
     const bool none = M == -INFINITY;
     const float lz = log2f(Z), ln = lz * kLn2;
@@ -517,8 +779,8 @@ using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t
                                    const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                    CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// 64 x 64 boxes of a row-major bf16 matrix, 128-byte swizzle, zeros outside.
-kq_status make_map(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int64_t ld, const char* who) {
+// Boxes of 64 columns and box_rows rows of a row-major bf16 matrix, 128-byte swizzle, zeros outside.
+kq_status make_map(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int64_t ld, const char* who, int box_rows = 64) {
     static std::atomic<EncodeTiledFn> fn{nullptr};
     EncodeTiledFn enc = fn.load();
     if (!enc) {
@@ -535,7 +797,7 @@ kq_status make_map(CUtensorMap* m, const void* base, int64_t rows, int64_t cols,
     std::memset(m, 0, sizeof(*m));
     const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
     const cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld) * 2};
-    const cuuint32_t box[2] = {64, 64}, one[2] = {1, 1};
+    const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(box_rows)}, one[2] = {1, 1};
     const CUresult r = enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, one,
                            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
@@ -568,6 +830,27 @@ kq_status run_tiles(const CUtensorMap& mx, const CUtensorMap& mw, const CUtensor
     linear_tile_kernel<MAIN><<<static_cast<unsigned>(2 * pairs), kThreads, kSmem, stream>>>(mx, mw, md, j);
     KQ_LAUNCH_CHECK("linear_tile_kernel");
     return KQ_OK;
+}
+template <int MAIN, int N>
+kq_status run_thin_of(const CUtensorMap& mx, const CUtensorMap& mw, Job& j, cudaStream_t stream) {
+    static std::atomic<uint64_t> done{0};
+    KQ_TRY(once_per_device(done, [] {
+        KQ_CUDA(cudaFuncSetAttribute(linear_thin_kernel<MAIN, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, Thin<N>::kSmem));
+        return KQ_OK;
+    }));
+    const int64_t blocks = std::min<int64_t>(cdiv(j.w_main, kThinRows), num_sms());
+    j.parts = static_cast<int32_t>(blocks);
+    linear_thin_kernel<MAIN, N><<<static_cast<unsigned>(blocks), kThinThreads, Thin<N>::kSmem, stream>>>(mx, mw, j);
+    KQ_LAUNCH_CHECK("linear_thin_kernel");
+    return KQ_OK;
+}
+int thin_box_rows(int64_t T) { return T <= 32 ? 32 : T <= 64 ? 64 : T <= 96 ? 48 : 64; }
+template <int MAIN>
+kq_status run_thin(const CUtensorMap& mx, const CUtensorMap& mw, Job& j, cudaStream_t stream) {
+    return j.T <= 32   ? run_thin_of<MAIN, 32>(mx, mw, j, stream)
+           : j.T <= 64 ? run_thin_of<MAIN, 64>(mx, mw, j, stream)
+           : j.T <= 96 ? run_thin_of<MAIN, 96>(mx, mw, j, stream)
+                       : run_thin_of<MAIN, 128>(mx, mw, j, stream);
 }
 kq_status set_up() {
     static std::atomic<uint64_t> done{0};
@@ -656,8 +939,14 @@ extern "C" kq_status kq_linear_logprobs(const uint16_t* x, int64_t T, int64_t d,
     j.m_main = static_cast<int32_t>(cdiv(T, BM));
     j.n_main = static_cast<int32_t>(cdiv(V, BN));
     j.tiles = j.m_main * j.n_main;
+    j.w_main = V;
     j.info = info;
-    KQ_TRY(run_tiles<kScore>(mx, mw, mw, j, stream));
+    if (T <= kThinMost) {
+        KQ_TRY(make_map(&mx, x, T, d, ldx, who, thin_box_rows(T)));
+        KQ_TRY(run_thin<kScore>(mx, mw, j, stream));
+    } else {
+        KQ_TRY(run_tiles<kScore>(mx, mw, mw, j, stream));
+    }
     linear_join_kernel<<<static_cast<unsigned>(T), 128, 0, stream>>>(j, logp, entropy, lse);
     KQ_LAUNCH_CHECK("linear_join_kernel");
     return KQ_OK;
@@ -716,12 +1005,16 @@ extern "C" kq_status kq_linear_logprobs_grad(const uint16_t* x, int64_t T, int64
     j.m_main = static_cast<int32_t>(cdiv(T, BM));
     j.n_d = static_cast<int32_t>(cdiv(d, BN));
     j.info = info;
-    // launch i: D of piece i, the products with D of piece i - 1
+    // launch i: D of piece i, the products with D of piece i - 1; few rows have a launch of their own for D
+    const bool thin = T <= kThinMost;
+    CUtensorMap mthin;
+    if (thin) KQ_TRY(make_map(&mthin, x, T, d, ldx, who, thin_box_rows(T)));
     for (int64_t i = 0; i <= c.pieces; ++i) {
         j.v_main = i * c.piece;
         j.w_main = std::min(c.piece, V - j.v_main);
-        j.n_main = i < c.pieces ? static_cast<int32_t>(cdiv(j.w_main, BN)) : 0;
+        j.n_main = i < c.pieces && !thin ? static_cast<int32_t>(cdiv(j.w_main, BN)) : 0;
         j.delta = delta[i & 1];
+        if (thin && i < c.pieces) KQ_TRY(run_thin<kDelta>(mthin, mw, j, stream));
         j.t_gx = j.t_gw = 0;
         if (i > 0) {
             j.v_prod = (i - 1) * c.piece;
