@@ -2,7 +2,7 @@
 //
 // Mathematics. z = x W^T for T rows of hidden states x [T][d] and a head W [V][d]. For each row
 //     lse = ln sum_v e^(z_v),  logp = z_y - lse,  entropy = -sum_v p_v ln p_v,  p_v = e^(z_v - lse).
-// A tile of logits leaves, for each row and 128 columns, the maximum m, Z = sum 2^t and S = sum 2^t t with
+// A tile of logits leaves, for each row and 64 columns, the maximum m, Z = sum 2^t and S = sum 2^t t with
 // t = log2(e) (z - m), and the target's logit where it has it. (The difference first: it is exact near the maximum, whatever
 // its size.) Joined: M = max m, lse = M + ln Z, entropy = (log2 Z - S / Z) ln 2.
 // Gradient of sum_t (g logp + h entropy): the logits' is
@@ -14,7 +14,7 @@
 // What bounds it: the tensor cores where there are many rows (2 T V d operations a product), the bytes of W where there
 // are few. Layout: a cluster of two CTAs on two SMs holds a 256 x 256 tile (tcgen05 cta_group::2, each SM the
 // accumulator of 128 rows in tensor memory and half of each operand in shared memory); one warp issues the TMA
-// loads of 64-wide boxes into a ring, one the products, eight read accumulators and work on them while the
+// loads of 64-wide boxes into a ring, one the products, 16 read accumulators and work on them while the
 // next chunk's products run into the other accumulator. Both operand layouts come from the same boxes: 64 of the
 // contiguous dimension by 64 rows, 128-byte swizzle, is 64 rows of 64 k for a K-major operand and 64 k of 64 rows for
 // an MN-major one. A launch carries the tiles of gx and gW of one piece and those of D of the next, so that the
@@ -28,6 +28,8 @@
 #include <cuda_bf16.h>
 
 #include "kq_common.cuh"
+#include "pdl.cuh"
+#include "trail_tc.cuh"
 
 namespace kq {
 namespace {
@@ -36,12 +38,13 @@ constexpr int BM = 256, BN = 256;                // tile of a pair
 constexpr int BK = 64;                           // of a slab
 constexpr int kBox = 64 * 64 * 2;                // bytes
 constexpr int kStage = 4 * kBox;                 // a CTA's 128 rows of A and 128 of B
-constexpr int kStages = 6;
-constexpr int kThreads = 384;                    // a warpgroup for loads and products, two for results
-// Registers of a thread: the launch gives all 168 (what 65536 leave 384 threads); results need a row's 128 sums and more.
-constexpr int kIssueRegs = 40, kResultRegs = 232;
-static_assert(128 * kIssueRegs + 256 * kResultRegs <= kThreads * 168, "more registers than the block was launched with");
-constexpr int kSmem = kStages * kStage + 1024 + 256;
+constexpr int kStages = 5;
+constexpr int kOutBox = 32 * 64 * 2;             // bytes of a warp's 32 rows by 64 columns of results
+constexpr int kThreads = 640;                    // a warpgroup for loads and products, 16 warps for results
+// Registers of a thread: the launch gives all 96 (what 65536 leave 640 threads); results need a row's 64 sums and more.
+constexpr int kIssueRegs = 64, kResultRegs = 104;
+static_assert(128 * kIssueRegs + 512 * kResultRegs <= kThreads * 96, "more registers than the block was launched with");
+constexpr int kSmem = kStages * kStage + 16 * kOutBox + 1024 + 256;
 constexpr int kDrainLogits = 8, kDrainGrads = 32;   // slabs
 constexpr int kBand = 16;                        // row tiles that go through the vocabulary together
 constexpr int64_t kPiece = 1 << 25;              // elements of D that a piece holds, about
@@ -123,7 +126,7 @@ struct Job {
     int64_t T, V, d;
     const int64_t* target;
     // score
-    float4* part;              // [T][parts]: m, Z, S of 128 columns
+    float4* part;              // [T][parts]: m, Z, S of 64 columns
     float* zt;                 // [T] the target's logit
     int32_t parts;
     // gradient
@@ -133,11 +136,10 @@ struct Job {
     int64_t v_main, v_prod;    // the first column of the piece whose logits, whose products are computed
     int64_t w_main, w_prod;    // and its width
     float* sum;                // [splits][T][d]: gx so far
-    __nv_bfloat16 *gx, *gw;    // gx: nullptr unless this launch finishes it
-    int64_t ld_gx, ld_gw;
-    bool first;                // no gx so far
+    bool first, last;          // no gx so far; this launch finishes it
     int32_t splits, split_slabs;
-    int32_t m_main, n_main, n_d, m_prod;   // tiles: rows, columns of the pieces and of d
+    int32_t m_main, n_main, m_prod, n_d;   // tiles of the rows, of the columns, of the rows again, of d
+    int32_t d_slabs, row_slabs, prod_slabs;   // slabs of d, of the rows, of the piece whose products are computed
     int32_t t_gx, t_gw, tiles;             // tiles of each, in this order, and in all
     int* info;
 };
@@ -152,25 +154,26 @@ __device__ __forceinline__ Tile tile_at(const Job& j, int t, int main_kind) {
     Tile a;
     a.split = 0;
     if (t < j.t_gx) {
-        const int mt = static_cast<int>((j.T + BM - 1) / BM), each = mt * j.n_d;
+        const int each = j.m_prod * j.n_d;
         a.kind = kGx;
         a.split = t / each;
         t -= a.split * each;
-        a.m0 = t / j.n_d * BM;
-        a.n0 = t % j.n_d * BN;
+        const int m = t / j.n_d;
+        a.m0 = m * BM;
+        a.n0 = (t - m * j.n_d) * BN;
         a.ka = a.split * j.split_slabs * BK;
         a.kb = static_cast<int>(j.v_prod) + a.ka;
-        const int all = static_cast<int>((j.w_prod + BK - 1) / BK);
-        a.slabs = min(j.split_slabs, all - a.split * j.split_slabs);
+        a.slabs = min(j.split_slabs, j.prod_slabs - a.split * j.split_slabs);
         return a;
     }
     t -= j.t_gx;
     if (t < j.t_gw) {
         a.kind = kGw;
-        a.m0 = t / j.n_d * BM;
-        a.n0 = t % j.n_d * BN;
+        const int m = t / j.n_d;
+        a.m0 = m * BM;
+        a.n0 = (t - m * j.n_d) * BN;
         a.ka = a.kb = 0;
-        a.slabs = static_cast<int>((j.T + BK - 1) / BK);
+        a.slabs = j.row_slabs;
         return a;
     }
     t -= j.t_gw;
@@ -178,10 +181,11 @@ __device__ __forceinline__ Tile tile_at(const Job& j, int t, int main_kind) {
     a.kind = main_kind;
     const int band = t / (kBand * j.n_main), rows = min(kBand, j.m_main - band * kBand);
     t -= band * kBand * j.n_main;
-    a.m0 = (band * kBand + t % rows) * BM;
-    a.n0 = t / rows * BN;
+    const int n = t / rows;
+    a.m0 = (band * kBand + t - n * rows) * BM;
+    a.n0 = n * BN;
     a.ka = a.kb = 0;
-    a.slabs = static_cast<int>((j.d + BK - 1) / BK);
+    a.slabs = j.d_slabs;
     return a;
 }
 
@@ -192,35 +196,38 @@ __device__ __forceinline__ void wait_quiet(uint64_t* bar, uint32_t parity) {
 }
 __device__ __forceinline__ int round_tile(int rd, int pair, int pairs) { return rd * pairs + ((rd & 1) ? pairs - 1 - pair : pair); }
 
-// m, Z and S of 128 logits of a row.
-__device__ __forceinline__ void score_row(const Job& j, float (&x)[128], int64_t row, int64_t col, int64_t at) {
+// m, Z and S of 64 logits of a row, and the target's logit.
+__device__ __forceinline__ Sums score_row(const Job& j, float (&x)[64], int64_t row, int64_t col) {
+    Sums a = {-INFINITY, 0.0f, 0.0f};
     const int64_t left = j.V - col;
-    if (row >= j.T || left <= 0) return;
-    if (left < 128) {
+    if (row >= j.T || left <= 0) return a;
+    if (left < 64) {
 #pragma unroll
-        for (int i = 0; i < 128; ++i)
+        for (int i = 0; i < 64; ++i)
             if (i >= left) x[i] = -INFINITY;
     }
     const int64_t y = j.target[row] - col;
-    if (y >= 0 && y < min(left, static_cast<int64_t>(128))) {
+    if (y >= 0 && y < min(left, static_cast<int64_t>(64))) {
         float z = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 128; ++i)
+        for (int i = 0; i < 64; ++i)
             if (i == y) z = x[i];
         j.zt[row] = z;
     }
-    float m = x[0];
+    a.m = x[0];
 #pragma unroll
-    for (int i = 1; i < 128; ++i) m = max_nan(m, x[i]);
-    const float ref = m == -INFINITY ? 0.0f : m;
+    for (int i = 1; i < 64; ++i) a.m = max_nan(a.m, x[i]);
+    const float ref = a.m == -INFINITY ? 0.0f : a.m;
     float z[2] = {0.0f, 0.0f}, s[2] = {0.0f, 0.0f};
 #pragma unroll
-    for (int i = 0; i < 128; ++i) {
+    for (int i = 0; i < 64; ++i) {
         const float t = fmaxf((x[i] - ref) * kLog2e, kNone), e = ex2(t);
         z[i & 1] += e;
         s[i & 1] = fmaf(e, t, s[i & 1]);
     }
-    if (KQ_IN_RANGE(at, j.parts)) j.part[row * j.parts + at] = make_float4(m, z[0] + z[1], s[0] + s[1], 0.0f);
+    a.z = z[0] + z[1];
+    a.s = s[0] + s[1];
+    return a;
 }
 
 // What a logit z contributes to D but for the target's own share: -p (g + ge (ln p + h)).
@@ -229,73 +236,70 @@ __device__ __forceinline__ float delta_of(float z, float lse, float g, float ge,
     return p > 0.0f ? -p * fmaf(ge, lp + h, g) : p == p ? 0.0f : p;
 }
 
-// D of 128 logits of a row: to bf16, zeros from the vocabulary's end on.
-__device__ __forceinline__ void delta_row(const Job& j, float (&x)[128], int64_t row, int64_t col) {
-    if (row >= j.T || col >= j.ld_delta) return;
-    const int64_t left = j.V - j.v_main - col, y = j.target[row];
-    const float lse = j.lse[row], g = y >= 0 && y < j.V ? j.g_logp[row] : 0.0f;
-    const float ge = j.g_entropy ? j.g_entropy[row] : 0.0f, h = j.g_entropy ? j.entropy[row] : 0.0f;
+// 64 columns of a warp's 32 rows to a bf16 matrix by way of shared memory: value(i) is this lane's column i. A box of
+// 128-byte lines, swizzled; what lies outside the matrix (rows x cols) is left out.
+template <typename F>
+__device__ __forceinline__ void put_rows(uint8_t* box, const CUtensorMap* map, int64_t row0, int64_t rows, int64_t col0, int64_t cols,
+                                         F value) {
+    const int lane = threadIdx.x & 31;
+    if (row0 >= rows || col0 >= cols) return;   // the same for the warp
+    if (lane == 0) bulk_wait_read0();           // the last results have left the box
+    __syncwarp();
+    uint4* line = reinterpret_cast<uint4*>(box + lane * 128);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = pack_bf16(value(8 * c + 2 * k), value(8 * c + 2 * k + 1));
+        line[c ^ (lane & 7)] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    fence_proxy_async();
+    __syncwarp();
+    if (lane == 0) {
+        tma_store_2d(map, box, static_cast<int>(col0), static_cast<int>(row0));
+        bulk_commit();
+    }
+}
+
+// D of 64 logits of a row, zeros from the vocabulary's end on.
+__device__ __forceinline__ void delta_rows(const Job& j, const float (&x)[64], uint8_t* box, const CUtensorMap* map, int64_t row0,
+                                           int64_t col) {
+    const int64_t row = row0 + (threadIdx.x & 31), left = j.V - j.v_main - col;
+    const bool is = row < j.T;
+    const int64_t y = is ? j.target[row] : -1;
+    const float lse = is ? j.lse[row] : -INFINITY, g = y >= 0 && y < j.V ? j.g_logp[row] : 0.0f;
+    const float ge = is && j.g_entropy ? j.g_entropy[row] : 0.0f, h = is && j.g_entropy ? j.entropy[row] : 0.0f;
     const bool none = lse == -INFINITY;
     const int64_t at = y - j.v_main - col;
-    __nv_bfloat16* out = j.delta + row * j.ld_delta + col;
-    const bool here = at >= 0 && at < 128 && y < j.V && !none;
-#pragma unroll
-    for (int c = 0; c < 8; ++c) {
-        uint32_t w[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            float q[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int i = 16 * c + 2 * k + e;
-                q[e] = delta_of(x[i], lse, g, ge, h);
-                if (none || i >= left) q[e] = 0.0f;
-                if (here && i == at) q[e] += g;
-            }
-            w[k] = pack_bf16(q[0], q[1]);
-        }
-        if (KQ_IN_RANGE(row * j.ld_delta + col + 16 * c + 15, j.T * j.ld_delta)) store32(out + 16 * c, w);
-    }
+    const int here = at >= 0 && at < 64 && y < j.V && !none ? static_cast<int>(at) : -1;
+    const int end = none ? 0 : static_cast<int>(max(static_cast<int64_t>(0), min(left, static_cast<int64_t>(64))));
+    put_rows(box, map, row0, j.T, col, j.ld_delta, [&](int i) {
+        const float q = i < end ? delta_of(x[i], lse, g, ge, h) : 0.0f;
+        return i == here ? q + g : q;
+    });
 }
 
-// 128 values of a row to a bf16 matrix with n columns.
-__device__ __forceinline__ void put_bf16(const float (&x)[128], __nv_bfloat16* base, int64_t row, int64_t rows, int64_t ld, int64_t col,
-                                         int64_t n) {
-    if (row >= rows || col >= n) return;
-    __nv_bfloat16* out = base + row * ld + col;
-    const bool wide = !(reinterpret_cast<uintptr_t>(out) & 31u);
-#pragma unroll
-    for (int c = 0; c < 8; ++c) {
-        uint32_t w[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) w[k] = pack_bf16(x[16 * c + 2 * k], x[16 * c + 2 * k + 1]);
-        if (wide && col + 16 * c + 16 <= n) {
-            store32(out + 16 * c, w);
-        } else {   // n is a multiple of 8, rows begin on 16 bytes
-            if (col + 16 * c + 8 <= n) *reinterpret_cast<uint4*>(out + 16 * c) = make_uint4(w[0], w[1], w[2], w[3]);
-            if (col + 16 * c + 16 <= n) *reinterpret_cast<uint4*>(out + 16 * c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
-        }
-    }
-}
-
-// gx so far plus 128 values of a row.
-__device__ __forceinline__ void add_gx(const Job& j, float (&x)[128], int split, int64_t row, int64_t col) {
-    if (row >= j.T || col >= j.d) return;
+// gx so far plus 64 values of a row.
+__device__ __forceinline__ void add_gx(const Job& j, float (&x)[64], int split, uint8_t* box, const CUtensorMap* map, int64_t row0,
+                                       int64_t col) {
+    const int64_t row = row0 + (threadIdx.x & 31);
+    const bool is = row < j.T && col < j.d;
     float* sum = j.sum + (static_cast<int64_t>(split) * j.T + row) * j.d + col;
-    if (!j.first) {
+    if (!j.first && is) {
 #pragma unroll
-        for (int c = 0; c < 32; ++c) {
+        for (int c = 0; c < 16; ++c) {
             if (col + 4 * c >= j.d) break;
             const float4 o = *reinterpret_cast<const float4*>(sum + 4 * c);
             x[4 * c] += o.x, x[4 * c + 1] += o.y, x[4 * c + 2] += o.z, x[4 * c + 3] += o.w;
         }
     }
-    if (j.gx) {
-        put_bf16(x, j.gx, row, j.T, j.ld_gx, col, j.d);
+    if (j.last) {
+        put_rows(box, map, row0, j.T, col, j.d, [&](int i) { return x[i]; });
         return;
     }
+    if (!is) return;
 #pragma unroll
-    for (int c = 0; c < 16; ++c) {
+    for (int c = 0; c < 8; ++c) {
         if (col + 8 * c >= j.d) break;
         uint32_t w[8];
 #pragma unroll
@@ -308,12 +312,14 @@ __device__ __forceinline__ void add_gx(const Job& j, float (&x)[128], int split,
 template <int MAIN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 linear_tile_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtensorMap mw,
-                   const __grid_constant__ CUtensorMap md, const __grid_constant__ Job j) {
+                   const __grid_constant__ CUtensorMap md, const __grid_constant__ CUtensorMap out_d,
+                   const __grid_constant__ CUtensorMap out_x, const __grid_constant__ CUtensorMap out_w, const __grid_constant__ Job j) {
     const uint32_t rank = cluster_ctarank();
     const int pair = static_cast<int>(blockIdx.x >> 1), pairs = static_cast<int>(gridDim.x >> 1);
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-    uint64_t* full = reinterpret_cast<uint64_t*>(smem + kStages * kStage);
+    uint8_t* boxes = smem + kStages * kStage;   // of the result warps
+    uint64_t* full = reinterpret_cast<uint64_t*>(boxes + 16 * kOutBox);
     uint64_t* empty = full + kStages;
     uint64_t* tfull = empty + kStages;
     uint64_t* tempty = tfull + 2;
@@ -329,7 +335,7 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(&tfull[b], 1);
-            mbar_init(&tempty[b], 16);   // 8 epilogue warps in each CTA
+            mbar_init(&tempty[b], 32);   // 16 result warps in each CTA
         }
         mbar_init(mma_done, 1);
         *abort_flag = 0;
@@ -349,6 +355,8 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
     cluster_barrier();   // both CTAs' barriers are there before one is signalled from the other
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
+    pdl_wait();   // nothing before this reads or writes global memory
+    pdl_launch_dependents();
     const uint32_t full0 = mapa_shared(smem_u32(full), 0), tempty0 = mapa_shared(smem_u32(tempty), 0);   // CTA 0's
 
     if (warp < 4) {
@@ -433,8 +441,9 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kResultRegs));
-        // ---- results: a thread has 128 columns (warps 4-7 the first half) of one of the CTA's 128 rows
+        // ---- results: a thread has 64 columns of one of the CTA's 128 rows
         const int q = warp & 3, h = (warp - 4) >> 2;
+        uint8_t* box = boxes + (warp - 4) * kOutBox;
         int cc = 0;
         bool ok = true;
         for (int rd = 0; rd * pairs < j.tiles && ok; ++rd) {
@@ -442,38 +451,47 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
             if (t >= j.tiles) continue;
             const Tile a = tile_at(j, t, MAIN);
             const int drain = a.kind == MAIN ? kDrainLogits : kDrainGrads;
-            float x[128];
+            float x[64];
             for (int s0 = 0; s0 < a.slabs; s0 += drain, ++cc) {
                 const int buf = cc & 1;
                 ok = mbar_wait(&tfull[buf], (static_cast<uint32_t>(cc) >> 1) & 1u, abort_flag);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t at = tmem + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(buf * BN + h * 128);
+                const uint32_t at = tmem + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(buf * BN + h * 64);
+                if (s0 == 0) {
 #pragma unroll
-                for (int p = 0; p < 4; ++p) {
-                    float v[32];
-                    tmem_ld32(at + p * 32, v);
+                    for (int p = 0; p < 2; ++p) tmem_ld32(at + p * 32, reinterpret_cast<float(&)[32]>(x[p * 32]));
                     tc_wait_ld();
+                } else {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) x[p * 32 + i] = s0 ? x[p * 32 + i] + v[i] : v[i];
+                    for (int p = 0; p < 4; ++p) {
+                        float v[16];
+                        tmem_ld16(at + p * 16, v);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) x[p * 16 + i] += v[i];
+                    }
                 }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive_remote(tempty0 + static_cast<uint32_t>(buf * 8));
             }
             if (!ok) break;
-            const int64_t row = a.m0 + 128 * static_cast<int64_t>(rank) + q * 32 + lane, col = a.n0 + h * 128;
+            const int64_t row0 = a.m0 + 128 * static_cast<int64_t>(rank) + q * 32, col = a.n0 + h * 64;
             if (MAIN == kScore) {
-                score_row(j, x, row, col, a.n0 / 128 + h);
+                const Sums sums = score_row(j, x, row0 + lane, col);
+                if (row0 + lane < j.T && KQ_IN_RANGE(a.n0 / 64 + h, j.parts))
+                    if (col < j.V) j.part[(row0 + lane) * j.parts + a.n0 / 64 + h] = make_float4(sums.m, sums.z, sums.s, 0.0f);
             } else if (a.kind == kDelta) {
-                delta_row(j, x, row, col);
+                delta_rows(j, x, box, &out_d, row0, col);
             } else if (a.kind == kGx) {
-                add_gx(j, x, a.split, row, col);
+                add_gx(j, x, a.split, box, &out_x, row0, col);
             } else {
-                put_bf16(x, j.gw + j.v_prod * j.ld_gw, row, min(j.w_prod, j.V - j.v_prod), j.ld_gw, col, j.d);
+                put_rows(box, &out_w, j.v_prod + row0, j.V, col, j.d, [&](int i) { return x[i]; });
             }
         }
+        if (MAIN == kDelta && lane == 0) bulk_wait_le<0>();   // the results have been written
     }
 
     tc_fence_before();
@@ -541,6 +559,8 @@ linear_thin_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
         tma_prefetch_desc(&mx);
         tma_prefetch_desc(&mw);
     }
+    pdl_wait();
+    pdl_launch_dependents();
     if (MAIN == kDelta && threadIdx.x >= 64) {
         for (int t = threadIdx.x - 64; t < N; t += 256) {
             const bool is = t < j.T;
@@ -725,6 +745,8 @@ __global__ void __launch_bounds__(128) linear_join_kernel(const Job j, float* __
                                                           float* __restrict__ lse) {
     __shared__ float sm[4], sz[4], ss[4];
     const int64_t row = blockIdx.x;
+    pdl_wait();
+    pdl_launch_dependents();
     const float4* p = j.part + row * j.parts;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     Sums a = {-INFINITY, 0.0f, 0.0f};
@@ -756,6 +778,8 @@ __global__ void __launch_bounds__(128) linear_join_kernel(const Job j, float* __
 __global__ void __launch_bounds__(256) linear_gx_kernel(const float* __restrict__ sum, int splits, int64_t T, int64_t d,
                                                         __nv_bfloat16* __restrict__ gx, int64_t ld) {
     const int64_t each = T * d, per_row = d / 8;
+    pdl_wait();
+    pdl_launch_dependents();
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < T * per_row; i += static_cast<int64_t>(gridDim.x) * 256) {
         const int64_t row = i / per_row, col = (i - row * per_row) * 8;
         float x[8] = {};
@@ -823,12 +847,17 @@ int max_clusters() {
     return c;
 }
 
+// The matrices of a launch: x, W, D that is read; D, gx and gw that are written.
+struct Maps {
+    CUtensorMap x, w, d, out_d, out_x, out_w;
+};
 template <int MAIN>
-kq_status run_tiles(const CUtensorMap& mx, const CUtensorMap& mw, const CUtensorMap& md, const Job& j, cudaStream_t stream) {
+kq_status run_tiles(const Maps& m, const Job& j, cudaStream_t stream) {
     if (j.tiles == 0) return KQ_OK;
     const int pairs = std::min(j.tiles, max_clusters());
-    linear_tile_kernel<MAIN><<<static_cast<unsigned>(2 * pairs), kThreads, kSmem, stream>>>(mx, mw, md, j);
-    KQ_LAUNCH_CHECK("linear_tile_kernel");
+    KQ_CUDA(launch_after(linear_tile_kernel<MAIN>, dim3(static_cast<unsigned>(2 * pairs)), dim3(kThreads), kSmem, stream, m.x, m.w, m.d,
+                         m.out_d, m.out_x, m.out_w, j));
+    count_launch();
     return KQ_OK;
 }
 template <int MAIN, int N>
@@ -840,8 +869,9 @@ kq_status run_thin_of(const CUtensorMap& mx, const CUtensorMap& mw, Job& j, cuda
     }));
     const int64_t blocks = std::min<int64_t>(cdiv(j.w_main, kThinRows), num_sms());
     j.parts = static_cast<int32_t>(blocks);
-    linear_thin_kernel<MAIN, N><<<static_cast<unsigned>(blocks), kThinThreads, Thin<N>::kSmem, stream>>>(mx, mw, j);
-    KQ_LAUNCH_CHECK("linear_thin_kernel");
+    KQ_CUDA(launch_after(linear_thin_kernel<MAIN, N>, dim3(static_cast<unsigned>(blocks)), dim3(kThinThreads), Thin<N>::kSmem, stream, mx,
+                         mw, j));
+    count_launch();
     return KQ_OK;
 }
 int thin_box_rows(int64_t T) { return T <= 32 ? 32 : T <= 64 ? 64 : T <= 96 ? 48 : 64; }
@@ -907,7 +937,7 @@ using namespace kq;
 
 extern "C" size_t kq_linear_logprobs_workspace(int64_t T, int64_t V, int64_t d) {
     if (T < 1 || V < 1 || d < 1) return 0;
-    return al256(static_cast<size_t>(T) * cdiv(V, 128) * sizeof(float4)) + al256(T * sizeof(float));
+    return al256(static_cast<size_t>(T) * cdiv(V, 64) * sizeof(float4)) + al256(T * sizeof(float));
 }
 
 extern "C" kq_status kq_linear_logprobs(const uint16_t* x, int64_t T, int64_t d, int64_t ldx, const uint16_t* w, int64_t V, int64_t ldw,
@@ -927,28 +957,25 @@ extern "C" kq_status kq_linear_logprobs(const uint16_t* x, int64_t T, int64_t d,
     }
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
     KQ_TRY(set_up());
-    CUtensorMap mx, mw;
-    KQ_TRY(make_map(&mx, x, T, d, ldx, who));
-    KQ_TRY(make_map(&mw, w, V, d, ldw, who));
+    Maps m;
+    KQ_TRY(make_map(&m.x, x, T, d, ldx, who, T <= kThinMost ? thin_box_rows(T) : 64));
+    KQ_TRY(make_map(&m.w, w, V, d, ldw, who));
+    m.d = m.out_d = m.out_x = m.out_w = m.w;   // not used
     Job j = {};
     j.T = T, j.V = V, j.d = d;
     j.target = target;
-    j.parts = static_cast<int32_t>(cdiv(V, 128));
+    j.parts = static_cast<int32_t>(cdiv(V, 64));
     j.part = static_cast<float4*>(ws);
     j.zt = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + al256(static_cast<size_t>(T) * j.parts * sizeof(float4)));
     j.m_main = static_cast<int32_t>(cdiv(T, BM));
     j.n_main = static_cast<int32_t>(cdiv(V, BN));
     j.tiles = j.m_main * j.n_main;
     j.w_main = V;
+    j.d_slabs = static_cast<int32_t>(cdiv(d, BK));
     j.info = info;
-    if (T <= kThinMost) {
-        KQ_TRY(make_map(&mx, x, T, d, ldx, who, thin_box_rows(T)));
-        KQ_TRY(run_thin<kScore>(mx, mw, j, stream));
-    } else {
-        KQ_TRY(run_tiles<kScore>(mx, mw, mw, j, stream));
-    }
-    linear_join_kernel<<<static_cast<unsigned>(T), 128, 0, stream>>>(j, logp, entropy, lse);
-    KQ_LAUNCH_CHECK("linear_join_kernel");
+    KQ_TRY(T <= kThinMost ? run_thin<kScore>(m.x, m.w, j, stream) : run_tiles<kScore>(m, j, stream));
+    KQ_CUDA(launch_after(linear_join_kernel, dim3(static_cast<unsigned>(T)), dim3(128), 0, stream, j, logp, entropy, lse));
+    count_launch();
     return KQ_OK;
 }
 
@@ -985,10 +1012,19 @@ extern "C" kq_status kq_linear_logprobs_grad(const uint16_t* x, int64_t T, int64
     uint8_t* at = static_cast<uint8_t*>(ws);
     __nv_bfloat16* delta[2] = {reinterpret_cast<__nv_bfloat16*>(at),
                                reinterpret_cast<__nv_bfloat16*>(at + (c.pieces > 1 ? al256(c.delta) : 0))};
-    CUtensorMap mx, mw, md[2];
-    KQ_TRY(make_map(&mx, x, T, d, ldx, who));
-    KQ_TRY(make_map(&mw, w, V, d, ldw, who));
-    for (int i = 0; i < 2; ++i) KQ_TRY(make_map(&md[i], delta[i], T, c.piece, c.piece, who));
+    Maps m;
+    CUtensorMap read[2], write[2], thin_x;
+    KQ_TRY(make_map(&m.x, x, T, d, ldx, who));
+    KQ_TRY(make_map(&m.w, w, V, d, ldw, who));
+    m.out_x = m.out_w = m.w;
+    if (gx) KQ_TRY(make_map(&m.out_x, gx, T, d, ldgx, who, 32));
+    if (gw) KQ_TRY(make_map(&m.out_w, gw, V, d, ldgw, who, 32));
+    for (int i = 0; i < 2; ++i) {
+        KQ_TRY(make_map(&read[i], delta[i], T, c.piece, c.piece, who));
+        KQ_TRY(make_map(&write[i], delta[i], T, c.piece, c.piece, who, 32));
+    }
+    const bool thin = T <= kThinMost;
+    if (thin) KQ_TRY(make_map(&thin_x, x, T, d, ldx, who, thin_box_rows(T)));
     if (info) {
         linear_targets_kernel<<<static_cast<unsigned>(std::min<int64_t>(cdiv(T, 256), 1024)), 256, 0, stream>>>(target, T, V, info);
         KQ_LAUNCH_CHECK("linear_targets_kernel");
@@ -999,40 +1035,39 @@ extern "C" kq_status kq_linear_logprobs_grad(const uint16_t* x, int64_t T, int64
     j.lse = lse, j.entropy = entropy, j.g_logp = g_logp, j.g_entropy = g_entropy;
     j.ld_delta = c.piece;
     j.sum = reinterpret_cast<float*>(at + al256(c.delta) * (c.pieces > 1 ? 2 : 1));
-    j.gw = reinterpret_cast<__nv_bfloat16*>(gw);
-    j.ld_gx = ldgx, j.ld_gw = ldgw;
     j.splits = c.splits, j.split_slabs = c.split_slabs;
-    j.m_main = static_cast<int32_t>(cdiv(T, BM));
+    j.m_main = j.m_prod = static_cast<int32_t>(cdiv(T, BM));
     j.n_d = static_cast<int32_t>(cdiv(d, BN));
+    j.d_slabs = static_cast<int32_t>(cdiv(d, BK));
+    j.row_slabs = static_cast<int32_t>(cdiv(T, BK));
     j.info = info;
     // launch i: D of piece i, the products with D of piece i - 1; few rows have a launch of their own for D
-    const bool thin = T <= kThinMost;
-    CUtensorMap mthin;
-    if (thin) KQ_TRY(make_map(&mthin, x, T, d, ldx, who, thin_box_rows(T)));
     for (int64_t i = 0; i <= c.pieces; ++i) {
         j.v_main = i * c.piece;
         j.w_main = std::min(c.piece, V - j.v_main);
         j.n_main = i < c.pieces && !thin ? static_cast<int32_t>(cdiv(j.w_main, BN)) : 0;
         j.delta = delta[i & 1];
-        if (thin && i < c.pieces) KQ_TRY(run_thin<kDelta>(mthin, mw, j, stream));
+        if (thin && i < c.pieces) KQ_TRY(run_thin<kDelta>(thin_x, m.w, j, stream));
         j.t_gx = j.t_gw = 0;
         if (i > 0) {
             j.v_prod = (i - 1) * c.piece;
             j.w_prod = std::min(c.piece, V - j.v_prod);
-            const int32_t splits = static_cast<int32_t>(cdiv(cdiv(j.w_prod, BK), c.split_slabs));
+            j.prod_slabs = static_cast<int32_t>(cdiv(j.w_prod, BK));
+            const int32_t splits = static_cast<int32_t>(cdiv(j.prod_slabs, c.split_slabs));
             j.first = i == 1;
-            j.gx = c.splits == 1 && i == c.pieces ? reinterpret_cast<__nv_bfloat16*>(gx) : nullptr;
+            j.last = c.splits == 1 && i == c.pieces;
             if (gx) j.t_gx = splits * j.m_main * j.n_d;
             if (gw) j.t_gw = static_cast<int32_t>(cdiv(j.w_prod, BM)) * j.n_d;
         }
         j.tiles = j.t_gx + j.t_gw + j.m_main * j.n_main;
-        KQ_TRY(run_tiles<kDelta>(mx, mw, md[(i + 1) & 1], j, stream));
+        m.d = read[(i + 1) & 1], m.out_d = write[i & 1];
+        KQ_TRY(run_tiles<kDelta>(m, j, stream));
     }
     if (gx && c.splits > 1) {
         const int64_t blocks = std::min<int64_t>(cdiv(T * (d / 8), 256), static_cast<int64_t>(num_sms()) * 8);
-        linear_gx_kernel<<<static_cast<unsigned>(blocks), 256, 0, stream>>>(j.sum, c.splits, T, d, reinterpret_cast<__nv_bfloat16*>(gx),
-                                                                            ldgx);
-        KQ_LAUNCH_CHECK("linear_gx_kernel");
+        KQ_CUDA(launch_after(linear_gx_kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream,
+                             static_cast<const float*>(j.sum), c.splits, T, d, reinterpret_cast<__nv_bfloat16*>(gx), ldgx));
+        count_launch();
     }
     return KQ_OK;
 }
