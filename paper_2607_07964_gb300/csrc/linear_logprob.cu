@@ -45,10 +45,12 @@ constexpr int kThreads = 640;                    // a warpgroup for loads and pr
 constexpr int kIssueRegs = 64, kResultRegs = 104;
 static_assert(128 * kIssueRegs + 512 * kResultRegs <= kThreads * 96, "more registers than the block was launched with");
 constexpr int kSmem = kStages * kStage + 16 * kOutBox + 1024 + 256;
-constexpr int kDrainLogits = 8, kDrainGrads = 32;   // slabs
+constexpr int kDrainLogits = 16, kDrainGrads = 32, kDrainThin = 8;   // slabs
+constexpr int kTileCost = 1;                     // what beginning and ending a tile costs, in slabs
 constexpr int kBand = 16;                        // row tiles that go through the vocabulary together
-constexpr int64_t kPiece = 1 << 25;              // elements of D that a piece holds, about
+constexpr int64_t kPiece = 1 << 26;              // elements of D that a piece holds, about
 constexpr int64_t kLeastPiece = 1024;            // columns
+constexpr int kMostPairs = 96;                   // clusters that a launch with tiles of several sizes has
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kNone = -1.0e30f;                // t of a logit that cannot occur: 2^t = 0 and 0 t a number
 
@@ -141,6 +143,7 @@ struct Job {
     int32_t m_main, n_main, m_prod, n_d;   // tiles of the rows, of the columns, of the rows again, of d
     int32_t d_slabs, row_slabs, prod_slabs;   // slabs of d, of the rows, of the piece whose products are computed
     int32_t t_gx, t_gw, tiles;             // tiles of each, in this order, and in all
+    int32_t first_main[kMostPairs + 1];    // with products: a pair's logits' tiles are from its entry to the next's
     int* info;
 };
 
@@ -194,7 +197,21 @@ __device__ __forceinline__ void wait_quiet(uint64_t* bar, uint32_t parity) {
     int none = 0;
     mbar_wait(bar, parity, &none);
 }
-__device__ __forceinline__ int round_tile(int rd, int pair, int pairs) { return rd * pairs + ((rd & 1) ? pairs - 1 - pair : pair); }
+__host__ __device__ __forceinline__ int round_tile(int rd, int pair, int pairs) {
+    return rd * pairs + ((rd & 1) ? pairs - 1 - pair : pair);
+}
+// A pair's tiles: of the products every pairs-th, back and forth; then of the logits a run that evens the pairs' work out. Where
+// there are no products every pairs-th of the logits, so that the pairs share rows of W.
+struct Walk {
+    int pair, pairs, dealt, run, count;
+    __device__ __forceinline__ Walk(const Job& j, int pair_, int pairs_) : pair(pair_), pairs(pairs_) {
+        const int deal = j.t_gx + j.t_gw ? j.t_gx + j.t_gw : j.tiles, whole = deal / pairs;
+        dealt = whole + (round_tile(whole, pair, pairs) < deal ? 1 : 0);
+        run = deal + (deal < j.tiles ? j.first_main[pair] : 0);
+        count = dealt + (deal < j.tiles ? j.first_main[pair + 1] - j.first_main[pair] : 0);
+    }
+    __device__ __forceinline__ int at(int n) const { return n < dealt ? round_tile(n, pair, pairs) : run + n - dealt; }
+};
 
 // m, Z and S of 64 logits of a row, and the target's logit.
 __device__ __forceinline__ Sums score_row(const Job& j, float (&x)[64], int64_t row, int64_t col) {
@@ -315,7 +332,7 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
                    const __grid_constant__ CUtensorMap md, const __grid_constant__ CUtensorMap out_d,
                    const __grid_constant__ CUtensorMap out_x, const __grid_constant__ CUtensorMap out_w, const __grid_constant__ Job j) {
     const uint32_t rank = cluster_ctarank();
-    const int pair = static_cast<int>(blockIdx.x >> 1), pairs = static_cast<int>(gridDim.x >> 1);
+    const Walk walk(j, static_cast<int>(blockIdx.x >> 1), static_cast<int>(gridDim.x >> 1));
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
     uint8_t* boxes = smem + kStages * kStage;   // of the result warps
@@ -365,10 +382,8 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
         if (warp == 0 && lane == 0) {
             int k = 0;
             bool ok = true;
-            for (int rd = 0; rd * pairs < j.tiles && ok; ++rd) {
-                const int t = round_tile(rd, pair, pairs);
-                if (t >= j.tiles) continue;
-                const Tile a = tile_at(j, t, MAIN);
+            for (int i = 0; i < walk.count && ok; ++i) {
+                const Tile a = tile_at(j, walk.at(i), MAIN);
                 const bool a_mn = a.kind == kGw, b_mn = a.kind == kGx || a.kind == kGw;
                 const CUtensorMap* ma = a.kind == kGx || a.kind == kGw ? &md : &mx;
                 const CUtensorMap* mb = a.kind == kGw ? &mx : &mw;
@@ -400,10 +415,8 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
             if (rank == 0) {
                 int k = 0, cc = 0;
                 bool ok = true;
-                for (int rd = 0; rd * pairs < j.tiles && ok; ++rd) {
-                    const int t = round_tile(rd, pair, pairs);
-                    if (t >= j.tiles) continue;
-                    const Tile a = tile_at(j, t, MAIN);
+                for (int i = 0; i < walk.count && ok; ++i) {
+                    const Tile a = tile_at(j, walk.at(i), MAIN);
                     const bool a_mn = a.kind == kGw, b_mn = a.kind == kGx || a.kind == kGw;
                     const uint32_t idesc = (idesc_bf16_mn_major(BM, BN) & ~(3u << 15)) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
                     // to the next 16 of K: 32 bytes along swizzled rows, or 16 rows of 128 bytes
@@ -446,10 +459,8 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
         uint8_t* box = boxes + (warp - 4) * kOutBox;
         int cc = 0;
         bool ok = true;
-        for (int rd = 0; rd * pairs < j.tiles && ok; ++rd) {
-            const int t = round_tile(rd, pair, pairs);
-            if (t >= j.tiles) continue;
-            const Tile a = tile_at(j, t, MAIN);
+        for (int i = 0; i < walk.count && ok; ++i) {
+            const Tile a = tile_at(j, walk.at(i), MAIN);
             const int drain = a.kind == MAIN ? kDrainLogits : kDrainGrads;
             float x[64];
             for (int s0 = 0; s0 < a.slabs; s0 += drain, ++cc) {
@@ -609,14 +620,14 @@ linear_thin_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
             int k = 0, cc = 0;
             bool ok = true;
             for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
-                for (int s0 = 0; s0 < slabs && ok; s0 += kDrainLogits, ++cc) {
+                for (int s0 = 0; s0 < slabs && ok; s0 += kDrainThin, ++cc) {
                     const int buf = cc & 1;
                     if (!mbar_wait(&tempty[buf], ((static_cast<uint32_t>(cc) >> 1) & 1u) ^ 1u, &abort_flag)) {
                         ok = false;
                         break;
                     }
                     tc_fence_after();
-                    const int s1 = min(slabs, s0 + kDrainLogits);
+                    const int s1 = min(slabs, s0 + kDrainThin);
                     for (int s = s0; s < s1; ++s, ++k) {
                         const int st = k % S::kStages;
                         if (!mbar_wait(&full[st], static_cast<uint32_t>(k / S::kStages) & 1u, &abort_flag)) {
@@ -649,7 +660,7 @@ linear_thin_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
         bool ok = true;
         for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
             float x[kHalf];
-            for (int s0 = 0; s0 < slabs; s0 += kDrainLogits, ++cc) {
+            for (int s0 = 0; s0 < slabs; s0 += kDrainThin, ++cc) {
                 const int buf = cc & 1;
                 ok = mbar_wait(&tfull[buf], (static_cast<uint32_t>(cc) >> 1) & 1u, &abort_flag);
                 ok = __all_sync(0xffffffffu, ok);
@@ -851,10 +862,47 @@ int max_clusters() {
 struct Maps {
     CUtensorMap x, w, d, out_d, out_x, out_w;
 };
+// The pairs' runs of the logits' tiles: as many to each as bring it up to a common level of work, counted in slabs.
+void even_out(Job& j, int pairs) {
+    const int deal = j.t_gx + j.t_gw, main = j.tiles - deal;
+    const int64_t cost = j.d_slabs + kTileCost;
+    int64_t load[kMostPairs] = {}, all = main * cost;
+    for (int t = 0, rd = 0; t < deal; t += pairs, ++rd)
+        for (int p = 0; p < pairs; ++p) {
+            const int at = round_tile(rd, p, pairs);
+            if (at >= deal) continue;
+            const int64_t slabs = at >= j.t_gx ? j.row_slabs
+                                               : std::min(j.split_slabs, j.prod_slabs - at / (j.m_prod * j.n_d) * j.split_slabs);
+            load[p] += slabs + kTileCost;
+            all += slabs + kTileCost;
+        }
+    // the lowest level that takes them all, within a tile of the mean or of the fullest pair
+    int64_t low = all / pairs, high = low + cost;
+    for (int p = 0; p < pairs; ++p) high = std::max(high, load[p] + cost);
+    auto room = [&](int64_t level, int p) { return level > load[p] ? (level - load[p]) / cost : 0; };
+    while (low < high) {
+        const int64_t mid = (low + high) / 2;
+        int64_t sum = 0;
+        for (int p = 0; p < pairs; ++p) sum += room(mid, p);
+        if (sum >= main) high = mid;
+        else low = mid + 1;
+    }
+    int64_t at = 0;
+    for (int p = 0; p < pairs; ++p) {
+        j.first_main[p] = static_cast<int32_t>(at);
+        at = std::min<int64_t>(main, at + room(low, p));
+    }
+    j.first_main[pairs] = static_cast<int32_t>(main);
+}
+
 template <int MAIN>
-kq_status run_tiles(const Maps& m, const Job& j, cudaStream_t stream) {
+kq_status run_tiles(const Maps& m, Job& j, cudaStream_t stream) {
     if (j.tiles == 0) return KQ_OK;
-    const int pairs = std::min(j.tiles, max_clusters());
+    int pairs = std::min(j.tiles, max_clusters());
+    if (j.t_gx + j.t_gw) {
+        pairs = std::min(pairs, kMostPairs);
+        even_out(j, pairs);
+    }
     KQ_CUDA(launch_after(linear_tile_kernel<MAIN>, dim3(static_cast<unsigned>(2 * pairs)), dim3(kThreads), kSmem, stream, m.x, m.w, m.d,
                          m.out_d, m.out_x, m.out_w, j));
     count_launch();
