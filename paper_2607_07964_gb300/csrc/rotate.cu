@@ -25,8 +25,7 @@ namespace {
 
 constexpr int kThreads = 128;      // forwards
 constexpr int kGradThreads = 256;
-constexpr int kAhead = 4;          // rows of a lane in flight forwards
-constexpr int kGradAhead = 2;      // and backwards, of two inputs
+constexpr int kAhead = 4;          // rows of a lane in flight forwards (backwards two, of two inputs)
 constexpr int kMaxDim = 256;
 constexpr int kMaxBlocks = 512;    // that a workspace has room for the sums of
 constexpr int kPairs = 0, kHalves = 1, kHalvesOdd = 2;   // layouts; odd: R / 2 is no multiple of a vector
@@ -106,44 +105,33 @@ __device__ __forceinline__ float row_sum(float v) {
     return v;
 }
 
-// A lane's share of a row, NV vectors l, l + G, ..: cos and sin (of the sign that the partner enters with) of its dimensions.
+// A lane's share of a row, NV vectors l, l + G, .., and what it makes of it: with x_p the partner of x_i,
+//     forwards  x_i c_i + x_p s_i,  c and s of cos, sin and the weights of the two,
+//     backwards g_i c_i + g_p s_i,  of cos and sin alone (the transposed rotation).
+// Values past the rotated ones have no partner: it counts as 0 whatever it holds.
 template <typename T, int G, int NV, int MODE>
 struct Share {
     static constexpr int E = 16 / sizeof(T);
     float c[NV][E], s[NV][E];
-    int n[NV], turned[NV];     // dimensions of a vector, and how many of them are rotated
-    int l;
+    int n[NV], turned[NV];     // values of a vector, and how many of them are rotated
+    int l, step;               // vectors between partners (halves)
 
-    __device__ __forceinline__ Share(int l_, int dim) : l(l_) {
-#pragma unroll
-        for (int k = 0; k < NV; ++k) n[k] = min(E, max(0, dim - (l + k * G) * E));
-    }
-    __device__ __forceinline__ int dim_of(int k, int e) const { return (l + k * G) * E + e; }
-    __device__ __forceinline__ void take(const float2* table, int half) {
+    __device__ __forceinline__ Share(int l_, int dim, int half) : l(l_), step(half / E) {
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
+            n[k] = min(E, max(0, dim - (l + k * G) * E));
             turned[k] = min(E, max(0, 2 * half - (l + k * G) * E));
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const int i = dim_of(k, e);
-                const bool in = e < turned[k], second = MODE == kPairs ? e & 1 : i >= half;
-                const float2 t = in ? table[MODE == kPairs ? i / 2 : second ? i - half : i] : make_float2(1.0f, 0.0f);
-                c[k][e] = t.x;
-                s[k][e] = second ? t.y : -t.y;
-            }
         }
     }
-    // y = rotated x; BACK: by the transposed matrix. xch: D floats of the row in shared memory (odd halves). Whole warps call it.
-    template <bool BACK>
-    __device__ __forceinline__ void turn(float (&x)[NV][E], int half, float* xch) const {
-        float y[NV][E];   // partners
+    __device__ __forceinline__ int dim_of(int k, int e) const { return (l + k * G) * E + e; }
+    // Whole warps call it. xch: the row in shared memory (odd halves).
+    __device__ __forceinline__ void partners(const float (&x)[NV][E], float (&y)[NV][E], int half, float* xch) const {
         if constexpr (MODE == kPairs) {
 #pragma unroll
             for (int k = 0; k < NV; ++k)
 #pragma unroll
                 for (int e = 0; e < E; ++e) y[k][e] = x[k][e ^ 1];
         } else if constexpr (MODE == kHalves) {
-            const int step = half / E;
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
                 const int v = l + k * G, from = v < step ? v + step : v - step;   // past R: not used
@@ -173,11 +161,33 @@ struct Share {
                 }
             __syncwarp();
         }
+    }
+    // c and s from a token's table; w: the weights, 1 where there are none, for what goes forwards.
+    template <bool BACK>
+    __device__ __forceinline__ void take(const float2* table, int half, const float (&w)[NV][E], float* xch) {
+        float wp[NV][E];
+        if constexpr (!BACK) partners(w, wp, half, xch);
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (e < turned[k]) x[k][e] = fmaf(BACK ? -s[k][e] : s[k][e], y[k][e], c[k][e] * x[k][e]);
+            for (int e = 0; e < E; ++e) {
+                const int i = dim_of(k, e);
+                const bool in = e < turned[k], second = MODE == kPairs ? e & 1 : i >= half;
+                const float2 t = in ? table[MODE == kPairs ? i / 2 : second ? i - half : i] : make_float2(1.0f, 0.0f);
+                c[k][e] = BACK ? t.x : t.x * w[k][e];
+                s[k][e] = second != BACK ? t.y : -t.y;
+                if constexpr (!BACK) s[k][e] = in ? s[k][e] * wp[k][e] : 0.0f;
+            }
+    }
+    // FULL: every value is rotated.
+    template <bool FULL>
+    __device__ __forceinline__ void turn(float (&x)[NV][E], int half, float* xch) const {
+        float y[NV][E];
+        partners(x, y, half, xch);
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[k][e] = fmaf(s[k][e], FULL || e < turned[k] ? y[k][e] : 0.0f, c[k][e] * x[k][e]);
     }
 };
 
@@ -203,95 +213,124 @@ __device__ __forceinline__ bool fill_table(const Rotate<T>& p, int64_t t, float2
     __syncwarp();
     return is;
 }
-// A warp looks at 32 / G rows at a time, first of the queries, then of the keys.
-template <typename T, int G>
-struct Looks {
-    int queries, all;
-    __device__ __forceinline__ explicit Looks(const Rotate<T>& p) {
-        constexpr int R = 32 / G;
-        queries = (p.s[0].heads + R - 1) / R;
-        all = queries + (p.s[1].heads + R - 1) / R;
-    }
-};
+// A warp looks at 32 / G rows at a time, first of the queries, then of the keys; an even number of looks at each, as it works
+// on two side by side.
+template <int G>
+__host__ __device__ constexpr int looks_at(int heads) {
+    return (heads + 2 * (32 / G) - 1) / (2 * (32 / G)) * 2;
+}
 __host__ __device__ constexpr int warp_floats(int mode, int g, int half, int dim) {   // of shared memory
-    return 2 * half + (mode == kHalvesOdd ? 32 / g * dim : 0);
+    return (2 * half + (mode == kHalvesOdd ? 32 / g * dim : 0) + 1) & ~1;
+}
+template <int NV, int E>
+__device__ __forceinline__ void square_sum(const float (&x)[NV][E], const float (&y)[NV][E], float& sum) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum = fmaf(x[k][e], y[k][e], sum);
+}
+template <typename T, int NV, bool FAST, typename S>
+__device__ __forceinline__ void unpack_weights(const T* w, const S& sh, float (&x)[NV][16 / sizeof(T)]) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        if (w) {
+            Lane<T, FAST>::unpack(Lane<T, FAST>::load(w + sh.dim_of(k, 0), sh.n[k]), x[k]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16 / static_cast<int>(sizeof(T)); ++e) x[k][e] = 1.0f;
+        }
+    }
 }
 
 // A warp to a part of a token's rows.
 template <typename T, int G, int NV, int MODE, bool FAST>
-__global__ void __launch_bounds__(kThreads, FAST && NV == 1 ? 7 : 4) qk_rotate_kernel(const Rotate<T> p) {
+__global__ void __launch_bounds__(kThreads) qk_rotate_kernel(const Rotate<T> p) {
     using L = Lane<T, FAST>;
     constexpr int E = L::E, R = 32 / G;
     extern __shared__ __align__(16) float smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane / G;
     const int64_t unit = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + warp;
-    const int64_t t = unit / p.parts;
+    const int64_t t = p.parts == 1 ? unit : unit / p.parts;
     if (t >= p.tokens) return;
-    float* mem = smem + warp * ((warp_floats(MODE, G, p.half, p.dim) + 1) & ~1);
+    float* mem = smem + warp * warp_floats(MODE, G, p.half, p.dim);
     float2* table = reinterpret_cast<float2*>(mem);
     float* xch = mem + 2 * p.half + sub * p.dim;
-    Share<T, G, NV, MODE> sh(lane % G, p.dim);
-    const Looks<T, G> looks(p);
-    const int first = static_cast<int>(unit - t * p.parts) * p.part, last = min(first + p.part, looks.all);
+    Share<T, G, NV, MODE> sh(lane % G, p.dim, p.half);
+    const int queries = looks_at<G>(p.s[0].heads), all = queries + looks_at<G>(p.s[1].heads);
+    const int first = static_cast<int>(unit - t * p.parts) * p.part, last = min(first + p.part, all);
     pdl_wait();
     pdl_launch_dependents();
-    const T* x0 = p.s[0].x + t * p.s[0].x_token + sh.dim_of(0, 0);
-    const T* x1 = p.s[1].x + t * p.s[1].x_token + sh.dim_of(0, 0);
+    const T* x0[2];
+    T* y0[2];
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+        x0[side] = p.s[side].x + t * p.s[side].x_token + sub * p.s[side].x_head + sh.dim_of(0, 0);
+        y0[side] = p.s[side].out + t * p.s[side].o_token + sub * p.s[side].o_head + sh.dim_of(0, 0);
+    }
     uint4 raw[kAhead][NV];
     auto fetch = [&](int i, uint4 (&u)[NV]) {
-        const bool key = i >= looks.queries;
-        const int h = (key ? i - looks.queries : i) * R + sub;
-        const bool here = i < last && h < (key ? p.s[1].heads : p.s[0].heads);
-        const T* src = key ? x1 + h * p.s[1].x_head : x0 + h * p.s[0].x_head;
-#pragma unroll
-        for (int k = 0; k < NV; ++k) u[k] = here ? L::load(src + k * G * E, sh.n[k]) : make_uint4(0, 0, 0, 0);
-    };
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) fetch(first + u, raw[u]);
-    uint4 w[NV];
-    auto weights = [&](int side) {
+        const bool key = i >= queries;
+        const int h = (key ? i - queries : i) * R;
+        const T* src = (key ? x0[1] : x0[0]) + h * (key ? p.s[1].x_head : p.s[0].x_head);
+        const bool here = i < last && h + sub < (key ? p.s[1].heads : p.s[0].heads);
 #pragma unroll
         for (int k = 0; k < NV; ++k)
-            w[k] = p.s[side].w ? L::load(p.s[side].w + sh.dim_of(k, 0), sh.n[k]) : make_uint4(0, 0, 0, 0);
+            if (here) u[k] = L::load(src + k * G * E, sh.n[k]);
     };
-    weights(first >= looks.queries);
-    const bool is = fill_table(p, t, table);
-    if (!is) return;
-    sh.take(table, p.half);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) raw[u][k] = make_uint4(0, 0, 0, 0);
+        fetch(first + u, raw[u]);
+    }
+    float w[NV][E];
+    unpack_weights<T, NV, FAST>(p.s[first >= queries].w, sh, w);
+    if (!fill_table(p, t, table)) return;
+    sh.template take<false>(table, p.half, w, xch);
     const float over = 1.0f / static_cast<float>(p.dim);
+    const bool full = 2 * p.half == p.dim;
     for (int i0 = first; i0 < last; i0 += kAhead) {
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const int i = i0 + u;
+        for (int u0 = 0; u0 < kAhead; u0 += 2) {
+            const int i = i0 + u0;
             if (i >= last) break;
-            float x[NV][E];
-#pragma unroll
-            for (int k = 0; k < NV; ++k) L::unpack(raw[u][k], x[k]);
-            fetch(i + kAhead, raw[u]);
-            const int side = i >= looks.queries, h = (side ? i - looks.queries : i) * R + sub;
+            if (i == queries && i > first) {
+                unpack_weights<T, NV, FAST>(p.s[1].w, sh, w);
+                sh.template take<false>(table, p.half, w, xch);
+            }
+            const int side = i >= queries, h0 = (side ? i - queries : i) * R;
             const Rows<T>& s = p.s[side];
-            if (i == looks.queries) weights(1);
+            float x[2][NV][E];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+#pragma unroll
+                for (int k = 0; k < NV; ++k) L::unpack(raw[u0 + u][k], x[u][k]);
+                fetch(i + u + kAhead, raw[u0 + u]);
+            }
+            float r[2] = {0.0f, 0.0f};
             if (s.w) {
-                float sum = 0.0f;
 #pragma unroll
-                for (int k = 0; k < NV; ++k)
-#pragma unroll
-                    for (int e = 0; e < E; ++e) sum = fmaf(x[k][e], x[k][e], sum);
-                sum = row_sum<G>(sum);
-                const float r = __frsqrt_rn(fmaf(sum, over, p.eps));
-#pragma unroll
-                for (int k = 0; k < NV; ++k) {
-                    float g[E];
-                    L::unpack(w[k], g);
-#pragma unroll
-                    for (int e = 0; e < E; ++e) x[k][e] = x[k][e] * r * g[e];
+                for (int u = 0; u < 2; ++u) {
+                    square_sum(x[u], x[u], r[u]);
+                    r[u] = rsqrtf(fmaf(row_sum<G>(r[u]), over, p.eps));
                 }
             }
-            sh.template turn<false>(x, p.half, xch);
-            if (h < s.heads) {
-                T* dst = s.out + t * s.o_token + h * s.o_head;
 #pragma unroll
-                for (int k = 0; k < NV; ++k) L::store(dst + sh.dim_of(k, 0), sh.n[k], x[k]);
+            for (int u = 0; u < 2; ++u) {
+                if (full) sh.template turn<true>(x[u], p.half, xch);
+                else sh.template turn<false>(x[u], p.half, xch);
+                if (s.w) {
+#pragma unroll
+                    for (int k = 0; k < NV; ++k)
+#pragma unroll
+                        for (int e = 0; e < E; ++e) x[u][k][e] *= r[u];
+                }
+                const int h = h0 + u * R;
+                T* dst = (side ? y0[1] : y0[0]) + h * s.o_head;
+                if (h + sub < s.heads) {
+#pragma unroll
+                    for (int k = 0; k < NV; ++k) L::store(dst + k * G * E, sh.n[k], x[u][k]);
+                }
             }
         }
     }
@@ -305,120 +344,123 @@ __global__ void __launch_bounds__(kGradThreads, NV == 1 ? 2 : 1) qk_rotate_grad_
     constexpr int E = L::E, R = 32 / G, kWarps = kGradThreads / 32, kSlots = kWarps * R;
     extern __shared__ __align__(16) float smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane / G;
-    float* mem = smem + warp * ((warp_floats(MODE, G, p.half, p.dim) + 1) & ~1);
+    float* mem = smem + warp * warp_floats(MODE, G, p.half, p.dim);
     float2* table = reinterpret_cast<float2*>(mem);
     float* xch = mem + 2 * p.half + sub * p.dim;
-    Share<T, G, NV, MODE> sh(lane % G, p.dim);
-    const Looks<T, G> looks(p);
+    Share<T, G, NV, MODE> sh(lane % G, p.dim, p.half);
+    const int queries = looks_at<G>(p.s[0].heads), looks = queries + looks_at<G>(p.s[1].heads);
     const int64_t units = p.tokens * p.parts, step = static_cast<int64_t>(gridDim.x) * kWarps;
+    const bool full = 2 * p.half == p.dim;
     pdl_wait();
     pdl_launch_dependents();
-    uint4 w[2][NV];
-    float gw[2][NV][E];
+    float w[NV][E], gw[2][NV][E];
 #pragma unroll
     for (int side = 0; side < 2; ++side)
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            w[side][k] = p.s[side].w ? L::load(p.s[side].w + sh.dim_of(k, 0), sh.n[k]) : make_uint4(0, 0, 0, 0);
+        for (int k = 0; k < NV; ++k)
 #pragma unroll
-            for (int e = 0; e < E; ++e) gw[side][k][e] = 0.0f;
-        }
+            for (int e = 0; e < E; ++e) gw[side][k][e] = w[k][e] = 0.0f;
+    int weights_of = -1;
     const float over = 1.0f / static_cast<float>(p.dim);
-    // the look that is fetched next: kGradAhead before the one that is worked on, across units
+    // the two looks that are fetched next, before the ones that are worked on, across units
     int64_t next_unit = static_cast<int64_t>(blockIdx.x) * kWarps + warp, next_t = 0;
     int next = 0, next_last = 0;
     auto enter = [&] {
         if (next_unit >= units) return;
-        next_t = next_unit / p.parts;
+        next_t = p.parts == 1 ? next_unit : next_unit / p.parts;
         next = static_cast<int>(next_unit - next_t * p.parts) * p.part;
-        next_last = min(next + p.part, looks.all);
+        next_last = min(next + p.part, looks);
     };
-    uint4 rx[kGradAhead][NV], rg[kGradAhead][NV];
-    auto fetch = [&](uint4 (&x)[NV], uint4 (&g)[NV]) {
+    uint4 rx[2][NV], rg[2][NV];
+    auto fetch = [&] {
         if (next_unit >= units) return;
-        const int side = next >= looks.queries, h = (side ? next - looks.queries : next) * R + sub;
+        const int side = next >= queries, h0 = (side ? next - queries : next) * R + sub;
         const Rows<T>& s = p.s[side];
-        const bool here = h < s.heads;
+        const T* gy = s.gy + next_t * s.g_token + h0 * s.g_head + sh.dim_of(0, 0);
+        const T* x = s.x + next_t * s.x_token + h0 * s.x_head + sh.dim_of(0, 0);
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            x[k] = g[k] = make_uint4(0, 0, 0, 0);
-            if (here) g[k] = L::load(s.gy + next_t * s.g_token + h * s.g_head + sh.dim_of(k, 0), sh.n[k]);
-            if (here && s.w) x[k] = L::load(s.x + next_t * s.x_token + h * s.x_head + sh.dim_of(k, 0), sh.n[k]);
+        for (int u = 0; u < 2; ++u) {
+            const bool here = h0 + u * R < s.heads;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                rx[u][k] = rg[u][k] = make_uint4(0, 0, 0, 0);
+                if (here) rg[u][k] = L::load(gy + u * R * s.g_head + k * G * E, sh.n[k]);
+                if (here && s.w) rx[u][k] = L::load(x + u * R * s.x_head + k * G * E, sh.n[k]);
+            }
         }
-        if (++next == next_last) {
+        next += 2;
+        if (next >= next_last) {
             next_unit += step;
             enter();
         }
     };
     int64_t unit = next_unit;
     enter();
+    fetch();
+    for (; unit < units; unit += step) {
+        const int64_t t = p.parts == 1 ? unit : unit / p.parts;
+        const int first = static_cast<int>(unit - t * p.parts) * p.part, last = min(first + p.part, looks);
+        const bool is = fill_table(p, t, table);
+        sh.template take<true>(table, p.half, w, xch);
+        for (int i = first; i < last; i += 2) {
+            float g[2][NV][E], x[2][NV][E];
 #pragma unroll
-    for (int u = 0; u < kGradAhead; ++u) fetch(rx[u], rg[u]);
-    bool is = false;
-    int64_t t = 0;
-    int i = 0, last = 0;
-    auto begin = [&] {
-        t = unit / p.parts;
-        i = static_cast<int>(unit - t * p.parts) * p.part;
-        last = min(i + p.part, looks.all);
-        is = fill_table(p, t, table);
-        sh.take(table, p.half);
-    };
-    if (unit < units) begin();
-    while (unit < units) {
-#pragma unroll
-        for (int u = 0; u < kGradAhead; ++u) {
-            if (unit >= units) break;
-            float g[NV][E], x[NV][E];
-#pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                L::unpack(rg[u][k], g[k]);
-                L::unpack(rx[u][k], x[k]);
-            }
-            fetch(rx[u], rg[u]);
-            const int side = i >= looks.queries, h = (side ? i - looks.queries : i) * R + sub;
-            const Rows<T>& s = p.s[side];
-            const bool here = is && h < s.heads;
-            sh.template turn<true>(g, p.half, xch);
-            if (s.w) {
-                float sum = 0.0f, dot = 0.0f, y[NV][E];
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int k = 0; k < NV; ++k) {
-                    L::unpack(side ? w[1][k] : w[0][k], y[k]);
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        y[k][e] *= g[k][e];
-                        sum = fmaf(x[k][e], x[k][e], sum);
-                        dot = fmaf(y[k][e], x[k][e], dot);
-                    }
+                    L::unpack(rg[u][k], g[u][k]);
+                    L::unpack(rx[u][k], x[u][k]);
                 }
-                sum = row_sum<G>(sum);
-                dot = row_sum<G>(dot);
-                const float r = __frsqrt_rn(fmaf(sum, over, p.eps)), f = dot * over * r * r;
-                auto add = [&](float (&to)[NV][E]) {
+            fetch();
+            const int side = i >= queries, h0 = (side ? i - queries : i) * R + sub;
+            const Rows<T>& s = p.s[side];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                if (full) sh.template turn<true>(g[u], p.half, xch);
+                else sh.template turn<false>(g[u], p.half, xch);
+            }
+            if (s.w) {
+                if (side != weights_of) {
+                    unpack_weights<T, NV, FAST>(s.w, sh, w);
+                    weights_of = side;
+                }
+                float sum[2] = {0.0f, 0.0f}, dot[2] = {0.0f, 0.0f};
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    square_sum(x[u], x[u], sum[u]);
 #pragma unroll
                     for (int k = 0; k < NV; ++k)
 #pragma unroll
-                        for (int e = 0; e < E; ++e) to[k][e] = fmaf(g[k][e], x[k][e] * r, to[k][e]);
-                };
-                if (is) {
-                    if (side) add(gw[1]);
-                    else add(gw[0]);
+                        for (int e = 0; e < E; ++e) dot[u] = fmaf(g[u][k][e] * w[k][e], x[u][k][e], dot[u]);
+                    sum[u] = row_sum<G>(sum[u]);
+                    dot[u] = row_sum<G>(dot[u]);
                 }
 #pragma unroll
-                for (int k = 0; k < NV; ++k)
+                for (int u = 0; u < 2; ++u) {
+                    const float r = rsqrtf(fmaf(sum[u], over, p.eps)), f = dot[u] * over * r * r, share = is ? r : 0.0f;
+                    auto add = [&](float (&to)[NV][E]) {
 #pragma unroll
-                    for (int e = 0; e < E; ++e) g[k][e] = r * fmaf(-f, x[k][e], y[k][e]);
-            }
-            if (here) {
-                T* dst = s.out + t * s.o_token + h * s.o_head;
+                        for (int k = 0; k < NV; ++k)
 #pragma unroll
-                for (int k = 0; k < NV; ++k) L::store(dst + sh.dim_of(k, 0), sh.n[k], g[k]);
+                            for (int e = 0; e < E; ++e) to[k][e] = fmaf(g[u][k][e], x[u][k][e] * share, to[k][e]);
+                    };
+                    if (is) {
+                        if (side) add(gw[1]);
+                        else add(gw[0]);
+                    }
+#pragma unroll
+                    for (int k = 0; k < NV; ++k)
+#pragma unroll
+                        for (int e = 0; e < E; ++e) g[u][k][e] = r * fmaf(-f, x[u][k][e], g[u][k][e] * w[k][e]);
+                }
             }
-            if (++i == last) {
-                unit += step;
-                if (unit < units) begin();
-            }
+            T* dst = s.out + t * s.o_token + h0 * s.o_head + sh.dim_of(0, 0);
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                if (is && h0 + u * R < s.heads) {
+#pragma unroll
+                    for (int k = 0; k < NV; ++k) L::store(dst + u * R * s.o_head + k * G * E, sh.n[k], g[u][k]);
+                }
         }
     }
     if (!p.sums) return;
@@ -462,12 +504,12 @@ int64_t grad_blocks(int64_t tokens) { return std::min<int64_t>(tokens, kMaxBlock
 template <typename T, int G, int NV, int MODE, bool FAST>
 kq_status launch(Rotate<T>& p, bool back, float* gqw, float* gkw, cudaStream_t stream) {
     constexpr int R = 32 / G;
-    const int64_t looks = cdiv(p.s[0].heads, R) + cdiv(p.s[1].heads, R), warps = static_cast<int64_t>(num_sms()) * 16;
-    // a token's rows go to several warps where tokens are few; not below two looks each, which the table would outweigh
-    const int64_t parts = std::max<int64_t>(1, std::min(cdiv(looks, 2), warps / p.tokens));
-    p.part = static_cast<int32_t>(cdiv(looks, parts));
+    const int64_t looks = looks_at<G>(p.s[0].heads) + looks_at<G>(p.s[1].heads), warps = static_cast<int64_t>(num_sms()) * 16;
+    // a token's rows go to several warps where tokens are few
+    const int64_t parts = std::max<int64_t>(1, std::min(looks / 2, warps / p.tokens));
+    p.part = static_cast<int32_t>(cdiv(looks / 2, parts) * 2);
     p.parts = static_cast<int32_t>(cdiv(looks, p.part));
-    const size_t floats = (warp_floats(MODE, G, p.half, p.dim) + 1) & ~1;
+    const size_t floats = warp_floats(MODE, G, p.half, p.dim);
     const int64_t units = p.tokens * p.parts;
     if (!back) {
         KQ_CUDA(launch_after(qk_rotate_kernel<T, G, NV, MODE, FAST>, dim3(static_cast<unsigned>(cdiv(units, kThreads / 32))),
