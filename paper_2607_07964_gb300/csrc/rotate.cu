@@ -11,8 +11,8 @@
 // upper 32 bits are used (1.5e-9 rad), rounded to fp32 (within 2^-25 of a turn): 2e-7 of the row's size.
 //
 // What bounds it: bytes, 2 elements moved for each forward, 3 backward, against about 12 instructions an
-// element. So a warp takes a token and its heads by itself: it has the next kAhead rows' loads in flight while it works
-// on one (16 bytes to a lane, G lanes to a row), computes cos and sin of the token's pairs once, and exchanges
+// element. So a warp takes a token and its heads by itself: it has the next two looks' loads in flight while it works
+// on two (16 bytes to a lane, G lanes to a row, 32 / G rows a look), computes cos and sin of the token's pairs once, and exchanges
 // partners by shuffles. Backwards the warps stay and go from token to token, the weights' sums in registers.
 #include <algorithm>
 #include <atomic>
@@ -25,7 +25,6 @@ namespace {
 
 constexpr int kThreads = 128;      // forwards
 constexpr int kGradThreads = 256;
-constexpr int kAhead = 4;          // rows of a lane in flight forwards (backwards two, of two inputs)
 constexpr int kMaxDim = 256;
 constexpr int kMaxBlocks = 512;    // that a workspace has room for the sums of
 constexpr int kPairs = 0, kHalves = 1, kHalvesOdd = 2;   // layouts; odd: R / 2 is no multiple of a vector
@@ -97,6 +96,31 @@ struct Lane {
         }
     }
 };
+
+// Two products, or products and sums, in one instruction.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y;\n\t"
+        "mov.b64 x, {%2, %3};\n\t"
+        "mov.b64 y, {%4, %5};\n\t"
+        "mul.rn.f32x2 x, x, y;\n\t"
+        "mov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, z;\n\t"
+        "mov.b64 x, {%2, %3};\n\t"
+        "mov.b64 y, {%4, %5};\n\t"
+        "mov.b64 z, {%6, %7};\n\t"
+        "fma.rn.f32x2 x, x, y, z;\n\t"
+        "mov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
 
 template <int G>
 __device__ __forceinline__ float row_sum(float v) {
@@ -187,7 +211,12 @@ struct Share {
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
-            for (int e = 0; e < E; ++e) x[k][e] = fmaf(s[k][e], FULL || e < turned[k] ? y[k][e] : 0.0f, c[k][e] * x[k][e]);
+            for (int e = 0; e < E; e += 2) {
+                const float2 a = make_float2(x[k][e], x[k][e + 1]), cc = make_float2(c[k][e], c[k][e + 1]);
+                const float2 b = make_float2(FULL || e < turned[k] ? y[k][e] : 0.0f, FULL || e + 1 < turned[k] ? y[k][e + 1] : 0.0f);
+                const float2 d = fma2(make_float2(s[k][e], s[k][e + 1]), b, mul2(cc, a));
+                x[k][e] = d.x, x[k][e + 1] = d.y;
+            }
     }
 };
 
@@ -222,12 +251,47 @@ __host__ __device__ constexpr int looks_at(int heads) {
 __host__ __device__ constexpr int warp_floats(int mode, int g, int half, int dim) {   // of shared memory
     return (2 * half + (mode == kHalvesOdd ? 32 / g * dim : 0) + 1) & ~1;
 }
+// sum of x y
 template <int NV, int E>
-__device__ __forceinline__ void square_sum(const float (&x)[NV][E], const float (&y)[NV][E], float& sum) {
+__device__ __forceinline__ float product_sum(const float (&x)[NV][E], const float (&y)[NV][E]) {
+    float2 sum = make_float2(0.0f, 0.0f);
 #pragma unroll
     for (int k = 0; k < NV; ++k)
 #pragma unroll
-        for (int e = 0; e < E; ++e) sum = fmaf(x[k][e], y[k][e], sum);
+        for (int e = 0; e < E; e += 2) sum = fma2(make_float2(x[k][e], x[k][e + 1]), make_float2(y[k][e], y[k][e + 1]), sum);
+    return sum.x + sum.y;
+}
+// x *= y
+template <int NV, int E>
+__device__ __forceinline__ void scale_by(float (&x)[NV][E], const float (&y)[NV][E]) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int e = 0; e < E; e += 2) {
+            const float2 d = mul2(make_float2(x[k][e], x[k][e + 1]), make_float2(y[k][e], y[k][e + 1]));
+            x[k][e] = d.x, x[k][e + 1] = d.y;
+        }
+}
+template <int NV, int E>
+__device__ __forceinline__ void scale_by(float (&x)[NV][E], float y) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int e = 0; e < E; e += 2) {
+            const float2 d = mul2(make_float2(x[k][e], x[k][e + 1]), make_float2(y, y));
+            x[k][e] = d.x, x[k][e + 1] = d.y;
+        }
+}
+// x = y a + x
+template <int NV, int E>
+__device__ __forceinline__ void add_scaled(float (&x)[NV][E], const float (&y)[NV][E], float a) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int e = 0; e < E; e += 2) {
+            const float2 d = fma2(make_float2(y[k][e], y[k][e + 1]), make_float2(a, a), make_float2(x[k][e], x[k][e + 1]));
+            x[k][e] = d.x, x[k][e + 1] = d.y;
+        }
 }
 template <typename T, int NV, bool FAST, typename S>
 __device__ __forceinline__ void unpack_weights(const T* w, const S& sh, float (&x)[NV][16 / sizeof(T)]) {
@@ -242,9 +306,10 @@ __device__ __forceinline__ void unpack_weights(const T* w, const S& sh, float (&
     }
 }
 
-// A warp to a part of a token's rows.
+// A warp to a part of a token's rows. 28 warps on an SM: 24 or 20 leave too few loads in flight (32768 tokens of 40 bf16 rows of
+// 128: 113, 118 and 118 us), 32 take too many registers (143).
 template <typename T, int G, int NV, int MODE, bool FAST>
-__global__ void __launch_bounds__(kThreads) qk_rotate_kernel(const Rotate<T> p) {
+__global__ void __launch_bounds__(kThreads, NV == 1 ? 7 : 4) qk_rotate_kernel(const Rotate<T> p) {
     using L = Lane<T, FAST>;
     constexpr int E = L::E, R = 32 / G;
     extern __shared__ __align__(16) float smem[];
@@ -260,76 +325,74 @@ __global__ void __launch_bounds__(kThreads) qk_rotate_kernel(const Rotate<T> p) 
     const int first = static_cast<int>(unit - t * p.parts) * p.part, last = min(first + p.part, all);
     pdl_wait();
     pdl_launch_dependents();
-    const T* x0[2];
-    T* y0[2];
+    // the two looks that are fetched next, before the ones that are worked on
+    int next = first;
+    const T* src[2];
 #pragma unroll
     for (int side = 0; side < 2; ++side) {
-        x0[side] = p.s[side].x + t * p.s[side].x_token + sub * p.s[side].x_head + sh.dim_of(0, 0);
-        y0[side] = p.s[side].out + t * p.s[side].o_token + sub * p.s[side].o_head + sh.dim_of(0, 0);
+        const int h = (side ? max(first - queries, 0) : first) * R + sub;
+        src[side] = p.s[side].x + t * p.s[side].x_token + h * p.s[side].x_head + sh.dim_of(0, 0);
     }
-    uint4 raw[kAhead][NV];
-    auto fetch = [&](int i, uint4 (&u)[NV]) {
-        const bool key = i >= queries;
-        const int h = (key ? i - queries : i) * R;
-        const T* src = (key ? x0[1] : x0[0]) + h * (key ? p.s[1].x_head : p.s[0].x_head);
-        const bool here = i < last && h + sub < (key ? p.s[1].heads : p.s[0].heads);
+    uint4 raw[2][NV];
 #pragma unroll
-        for (int k = 0; k < NV; ++k)
-            if (here) u[k] = L::load(src + k * G * E, sh.n[k]);
-    };
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int k = 0; k < NV; ++k) raw[u][k] = make_uint4(0, 0, 0, 0);
-        fetch(first + u, raw[u]);
-    }
-    float w[NV][E];
-    unpack_weights<T, NV, FAST>(p.s[first >= queries].w, sh, w);
+    auto fetch = [&] {
+        if (next >= last) return;
+        const bool key = next >= queries;
+        const int h = (key ? next - queries : next) * R + sub, heads = key ? p.s[1].heads : p.s[0].heads;
+        const int64_t head = key ? p.s[1].x_head : p.s[0].x_head;
+        const T* at = key ? src[1] : src[0];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+            if (h + u * R < heads) {
+#pragma unroll
+                for (int k = 0; k < NV; ++k) raw[u][k] = L::load(at + u * R * head + k * G * E, sh.n[k]);
+            }
+        next += 2;
+        if (key) src[1] = at + 2 * R * head;
+        else src[0] = at + 2 * R * head;
+    };
+    fetch();
     if (!fill_table(p, t, table)) return;
-    sh.template take<false>(table, p.half, w, xch);
     const float over = 1.0f / static_cast<float>(p.dim);
     const bool full = 2 * p.half == p.dim;
-    for (int i0 = first; i0 < last; i0 += kAhead) {
 #pragma unroll
-        for (int u0 = 0; u0 < kAhead; u0 += 2) {
-            const int i = i0 + u0;
-            if (i >= last) break;
-            if (i == queries && i > first) {
-                unpack_weights<T, NV, FAST>(p.s[1].w, sh, w);
-                sh.template take<false>(table, p.half, w, xch);
-            }
-            const int side = i >= queries, h0 = (side ? i - queries : i) * R;
-            const Rows<T>& s = p.s[side];
+    for (int side = 0; side < 2; ++side) {
+        const Rows<T>& s = p.s[side];
+        const int from = side ? max(first, queries) : first, to = side ? last : min(last, queries);
+        if (from >= to) continue;
+        const bool norm = s.w != nullptr;
+        {
+            float w[NV][E];
+            unpack_weights<T, NV, FAST>(s.w, sh, w);
+            sh.template take<false>(table, p.half, w, xch);
+        }
+        int h = (side ? from - queries : from) * R + sub;
+        T* dst = s.out + t * s.o_token + h * s.o_head + sh.dim_of(0, 0);
+        for (int i = from; i < to; i += 2, h += 2 * R, dst += 2 * R * s.o_head) {
             float x[2][NV][E];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int k = 0; k < NV; ++k) L::unpack(raw[u0 + u][k], x[u][k]);
-                fetch(i + u + kAhead, raw[u0 + u]);
-            }
-            float r[2] = {0.0f, 0.0f};
-            if (s.w) {
+                for (int k = 0; k < NV; ++k) L::unpack(raw[u][k], x[u][k]);
+            fetch();
+            float r[2] = {1.0f, 1.0f};
+            if (norm) {
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    square_sum(x[u], x[u], r[u]);
-                    r[u] = rsqrtf(fmaf(row_sum<G>(r[u]), over, p.eps));
-                }
+                for (int u = 0; u < 2; ++u) r[u] = product_sum(x[u], x[u]);
+#pragma unroll
+                for (int u = 0; u < 2; ++u) r[u] = rsqrtf(fmaf(row_sum<G>(r[u]), over, p.eps));
             }
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 if (full) sh.template turn<true>(x[u], p.half, xch);
                 else sh.template turn<false>(x[u], p.half, xch);
-                if (s.w) {
+                if (norm) scale_by(x[u], r[u]);
+                if (h + u * R < s.heads) {
 #pragma unroll
-                    for (int k = 0; k < NV; ++k)
-#pragma unroll
-                        for (int e = 0; e < E; ++e) x[u][k][e] *= r[u];
-                }
-                const int h = h0 + u * R;
-                T* dst = (side ? y0[1] : y0[0]) + h * s.o_head;
-                if (h + sub < s.heads) {
-#pragma unroll
-                    for (int k = 0; k < NV; ++k) L::store(dst + k * G * E, sh.n[k], x[u][k]);
+                    for (int k = 0; k < NV; ++k) L::store(dst + u * R * s.o_head + k * G * E, sh.n[k], x[u][k]);
                 }
             }
         }
@@ -424,34 +487,28 @@ __global__ void __launch_bounds__(kGradThreads, NV == 1 ? 2 : 1) qk_rotate_grad_
                     unpack_weights<T, NV, FAST>(s.w, sh, w);
                     weights_of = side;
                 }
-                float sum[2] = {0.0f, 0.0f}, dot[2] = {0.0f, 0.0f};
+                float sum[2], dot[2];
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    square_sum(x[u], x[u], sum[u]);
+                    // x g first, for the weights; its sum with w is the mean's
+                    sum[u] = product_sum(x[u], x[u]);
+                    float xg[NV][E];
 #pragma unroll
                     for (int k = 0; k < NV; ++k)
 #pragma unroll
-                        for (int e = 0; e < E; ++e) dot[u] = fmaf(g[u][k][e] * w[k][e], x[u][k][e], dot[u]);
+                        for (int e = 0; e < E; ++e) xg[k][e] = x[u][k][e];
+                    scale_by(xg, g[u]);
+                    dot[u] = product_sum(xg, w);
                     sum[u] = row_sum<G>(sum[u]);
                     dot[u] = row_sum<G>(dot[u]);
-                }
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const float r = rsqrtf(fmaf(sum[u], over, p.eps)), f = dot[u] * over * r * r, share = is ? r : 0.0f;
-                    auto add = [&](float (&to)[NV][E]) {
-#pragma unroll
-                        for (int k = 0; k < NV; ++k)
-#pragma unroll
-                            for (int e = 0; e < E; ++e) to[k][e] = fmaf(g[u][k][e], x[u][k][e] * share, to[k][e]);
-                    };
+                    const float r = rsqrtf(fmaf(sum[u], over, p.eps)), f = dot[u] * over * r * r;
                     if (is) {
-                        if (side) add(gw[1]);
-                        else add(gw[0]);
+                        if (side) add_scaled(gw[1], xg, r);
+                        else add_scaled(gw[0], xg, r);
                     }
-#pragma unroll
-                    for (int k = 0; k < NV; ++k)
-#pragma unroll
-                        for (int e = 0; e < E; ++e) g[u][k][e] = r * fmaf(-f, x[u][k][e], g[u][k][e] * w[k][e]);
+                    scale_by(g[u], w);
+                    add_scaled(g[u], x[u], -f);
+                    scale_by(g[u], r);
                 }
             }
             T* dst = s.out + t * s.o_token + h0 * s.o_head + sh.dim_of(0, 0);

@@ -1,10 +1,12 @@
 """Decoding with quantized layers over a 4-bit key/value cache, and scoring what was decoded.
 
 QuantizedLinear applies a layer that LayerPipeline quantized (kq_pack_codes, kq_infer);
-KvCache owns a pool of pages and strings together kq_kv_append, kq_kv_attend, kq_kv_evict and
-kq_kv_read for a batch of sequences; AttentionBlock is one attention sublayer over both, without the
-norm before it and the rotation of queries and keys, which a model puts around and between. Products,
-cache, attention and scoring run in libkronq's kernels, on the current stream, without waiting for the
+KvCache owns a pool of pages and strings together kq_kv_append, kq_kv_attend, kq_kv_attend_window,
+kq_kv_evict and kq_kv_read for a batch of sequences; Rotation holds the positions' frequencies and the
+norms of queries and keys (kq_qk_rotate); AttentionBlock is one attention sublayer over them, without the
+norm before it, which a model puts around it; score takes logits, score_hidden the hidden states and the
+head that they would come from, score_hidden_grad the gradients. Products, cache, attention and
+scoring run in libkronq's kernels, on the current stream, without waiting for the
 device (`KvCache.append` says when it has to); `KvCache.check` reads the device error word.
 
 `python -m paper_2607_07964_gb300.serving` quantizes the projections of a small random model,
@@ -146,8 +148,11 @@ class KvCache:
         else:
             self._all += more
 
-    def attend(self, q, start, scale: float | None = None, lse=None):
-        """Attention of q [T, q_heads, dim] of the tokens appended last over their sequences."""
+    def attend(self, q, start, scale: float | None = None, lse=None, window: int | None = None, sink: int = 0):
+        """Attention of q [T, q_heads, dim] of the tokens appended last over their sequences; with a window, over the last
+        `window` positions up to a token's own and the first `sink`."""
+        if window is not None and self.budget is not None:
+            raise ValueError("a cache that evicts does not hold its slots in the order of positions, so it has no window")
         self._capturing()
         need = kq.kq_kv_attend_workspace(q, self.data, self.table, self.acc)
         if self._ws is None or self._ws.numel() < need:
@@ -157,8 +162,12 @@ class KvCache:
                 self._ws.record_stream(torch.cuda.current_stream())
             self._ws = torch.empty(need, dtype=torch.uint8, device=q.device)
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        kq.kq_kv_attend(q, start, self.lens, self.data, self.table, out, self._ws,
-                        1 / math.sqrt(self.dim) if scale is None else scale, lse=lse, acc=self.acc, info=self.info)
+        scale = 1 / math.sqrt(self.dim) if scale is None else scale
+        if window is None:
+            kq.kq_kv_attend(q, start, self.lens, self.data, self.table, out, self._ws, scale, lse=lse, acc=self.acc, info=self.info)
+        else:
+            kq.kq_kv_attend_window(q, start, self.lens, self.data, self.table, out, self._ws, scale, window, sink, lse=lse,
+                                   info=self.info)
         return out
 
     def evict(self) -> None:
@@ -186,18 +195,60 @@ class KvCache:
             raise kq.KronqError(status, "KvCache", f"device error word {raw}")
 
 
+def rotation_theta(rot: int, base: float = 10000.0, stretch: float = 1.0, original: int = 8192):
+    """Radians that one position turns the pairs of `rot` dimensions by, base^(-2 j / rot), and the scale of queries and keys.
+    With stretch > 1, for texts of up to `stretch` times the `original` positions: waves that the original length
+    holds less than once are slowed by stretch, those that it holds four times or more are kept, those between in
+    proportion, and queries and keys are scaled by 1 + ln(stretch) / 10 each."""
+    theta = []
+    for j in range(rot // 2):
+        t = base ** (-2 * j / rot)
+        keep = min(1.0, max(0.0, (original * t / (2 * math.pi) - 1) / 3))
+        theta.append(t * (keep + (1 - keep) / stretch))
+    return theta, 1.0 + 0.1 * math.log(stretch)
+
+
+class Rotation:
+    """The rotation of queries and keys by their positions, and their norms before it where there are weights: theta and scale as
+    rotation_theta gives them."""
+
+    def __init__(self, theta, scale: float = 1.0, interleaved: bool = False, q_weight=None, k_weight=None, eps: float = 1e-6,
+                 device: str = "cuda"):
+        self.freq = kq.kq_rotation_freq(theta, device)
+        self.args = dict(scale=scale, interleaved=interleaved, q_weight=q_weight, k_weight=k_weight, eps=eps)
+
+    def __call__(self, q, k, **positions) -> None:
+        """q, k [T, heads, dim] in place; positions: pos [T], or start and first."""
+        kq.kq_qk_rotate(q, k, q, k, self.freq, **positions, **self.args)
+
+    def grad(self, q, k, gq, gk, **positions):
+        """(gradients of the weights, of queries and of keys, None without weights) for q, k as they were before the rotation; gq, gk,
+        the gradients of what it made of them, become those of q and k in place."""
+        sums = [None if self.args[n] is None else torch.empty(gq.shape[2], device=gq.device) for n in ("q_weight", "k_weight")]
+        ws = torch.empty(kq.kq_qk_rotate_grad_workspace(gq), dtype=torch.uint8, device=gq.device) if any(
+            s is not None for s in sums) else None
+        kq.kq_qk_rotate_grad(q, k, gq, gk, gq, gk, self.freq, gq_weight=sums[0], gk_weight=sums[1], ws=ws, **positions, **self.args)
+        return tuple(sums)
+
+
 class AttentionBlock:
     """x + W_o attention(W_q x, W_k x, W_v x) with quantized projections, tokens of several sequences packed (start and
-    most as KvCache.append takes them). Queries and keys are not rotated."""
+    most as KvCache.append takes them). Queries and keys are normed and rotated where a Rotation is given, by the number of
+    tokens that their sequence has had; with a window, attention sees the last `window` positions and the first `sink`."""
 
-    def __init__(self, proj: dict, heads: int, cache: KvCache):
+    def __init__(self, proj: dict, heads: int, cache: KvCache, rotation: Rotation | None = None, window: int | None = None,
+                 sink: int = 0):
         self.proj, self.heads, self.cache = proj, heads, cache
+        self.rotation, self.window, self.sink = rotation, window, sink
 
     def __call__(self, x, start, most):
         c, T = self.cache, x.shape[0]
         q, k, v = (self.proj[n](x) for n in ("q", "k", "v"))
-        c.append(k.view(T, c.kv_heads, c.dim), v.view(T, c.kv_heads, c.dim), start, most)
-        a = c.attend(q.view(T, self.heads, c.dim), start)
+        q, k, v = q.view(T, self.heads, c.dim), k.view(T, c.kv_heads, c.dim), v.view(T, c.kv_heads, c.dim)
+        if self.rotation is not None:
+            self.rotation(q, k, start=start, first=c.seen)
+        c.append(k, v, start, most)
+        a = c.attend(q, start, window=self.window, sink=self.sink)
         return x + self.proj["o"](a.view(T, -1))
 
 
@@ -209,6 +260,26 @@ def score(logits, target, top: int = 0):
     tops = torch.empty(T, top, device=dev) if top else None
     kq.kq_token_logprobs(logits, target, logp, entropy=entropy, top_id=ids, top_logp=tops)
     return logp, entropy, ids, tops
+
+
+def score_hidden(x, head, target, info=None):
+    """(logp, entropy, lse) of the target tokens under the logits x head^T of hidden states x [T, d] and a head [V, d] (bf16), as
+    score gives them for logits, which are not made here."""
+    T, dev = x.shape[0], x.device
+    logp, entropy, lse = (torch.empty(T, device=dev) for _ in range(3))
+    ws = torch.empty(kq.kq_linear_logprobs_workspace(x, head), dtype=torch.uint8, device=dev)
+    kq.kq_linear_logprobs(x, head, target, logp, ws, entropy=entropy, lse=lse, info=info)
+    return logp, entropy, lse
+
+
+def score_hidden_grad(x, head, target, lse, g_logp, entropy=None, g_entropy=None, of_head: bool = True, info=None):
+    """(gx, gradient of the head or None) of sum(g_logp * logp + g_entropy * entropy), from score_hidden's lse and entropy: with
+    g_logp = -1 / T what calibration starts its backward pass from."""
+    gx, gw = torch.empty_like(x), torch.empty_like(head) if of_head else None
+    ws = torch.empty(kq.kq_linear_logprobs_grad_workspace(x, head), dtype=torch.uint8, device=x.device)
+    kq.kq_linear_logprobs_grad(x, head, target, lse, g_logp, ws, gx=gx, gw=gw, entropy=entropy if g_entropy is not None else None,
+                               g_entropy=g_entropy, info=info)
+    return gx, gw
 
 
 def _quantized(name: str, d_out: int, d_in: int, bits: int, seed: int) -> QuantizedLinear:
@@ -225,13 +296,19 @@ def _quantized(name: str, d_out: int, d_in: int, bits: int, seed: int) -> Quanti
 
 
 def example(steps: int = 24, prompts=(40, 7, 23), vocab: int = 1000, heads: int = 4, kv_heads: int = 2, dim: int = 128,
-            budget: int = 32, bits: int = 4, seed: int = 0):
-    """Prompts of different lengths, then `steps` greedily decoded tokens of each under a cache budget. Returns
-    the decoded tokens and their log probabilities [steps, batch], and the block."""
+            budget: int | None = 32, bits: int = 4, seed: int = 0, window: int | None = None):
+    """Prompts of different lengths, then `steps` greedily decoded tokens of each: under a cache budget, or (budget None) with rotated
+    queries and keys and a window. Returns the decoded tokens and their log probabilities [steps, batch], and the block."""
     d, batch = heads * dim, len(prompts)
     proj = {n: _quantized(n, d if n in "qo" else kv_heads * dim, d, bits, seed + i) for i, n in enumerate("qkvo")}
-    cache = KvCache(batch, kv_heads, dim, max(max(prompts), budget) + 8, budget=budget, recent=budget // 4, sink=2)
-    block = AttentionBlock(proj, heads, cache)
+    if budget is None:
+        cache = KvCache(batch, kv_heads, dim, max(prompts) + steps)
+        one = torch.ones(dim, device="cuda")
+        theta, scale = rotation_theta(dim)
+        block = AttentionBlock(proj, heads, cache, Rotation(theta, scale, q_weight=one, k_weight=one), window, sink=2)
+    else:
+        cache = KvCache(batch, kv_heads, dim, max(max(prompts), budget) + 8, budget=budget, recent=budget // 4, sink=2)
+        block = AttentionBlock(proj, heads, cache)
     g = torch.Generator("cuda").manual_seed(seed)
     embed, head = (torch.randn(vocab, d, device="cuda", generator=g) for _ in range(2))
     tokens = torch.randint(0, vocab, (sum(prompts),), device="cuda", generator=g)
