@@ -139,6 +139,8 @@ struct Job {
     int64_t w_main, w_prod;    // and its width
     float* sum;                // [splits][T][d]: gx so far
     bool first, last;          // no gx so far; this launch finishes it
+    bool turned;               // D is by columns: a row of tokens for each row of W
+    bool gw;                   // few rows: gW is asked for
     int32_t splits, split_slabs;
     int32_t m_main, n_main, m_prod, n_d;   // tiles of the rows, of the columns, of the rows again, of d
     int32_t d_slabs, row_slabs, prod_slabs;   // slabs of d, of the rows, of the piece whose products are computed
@@ -384,7 +386,7 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
             bool ok = true;
             for (int i = 0; i < walk.count && ok; ++i) {
                 const Tile a = tile_at(j, walk.at(i), MAIN);
-                const bool a_mn = a.kind == kGw, b_mn = a.kind == kGx || a.kind == kGw;
+                const bool a_mn = a.kind == kGw || (a.kind == kGx && j.turned), b_mn = a.kind == kGx || a.kind == kGw;
                 const CUtensorMap* ma = a.kind == kGx || a.kind == kGw ? &md : &mx;
                 const CUtensorMap* mb = a.kind == kGw ? &mx : &mw;
                 const int m = a.m0 + 128 * static_cast<int>(rank);
@@ -417,7 +419,7 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
                 bool ok = true;
                 for (int i = 0; i < walk.count && ok; ++i) {
                     const Tile a = tile_at(j, walk.at(i), MAIN);
-                    const bool a_mn = a.kind == kGw, b_mn = a.kind == kGx || a.kind == kGw;
+                    const bool a_mn = a.kind == kGw || (a.kind == kGx && j.turned), b_mn = a.kind == kGx || a.kind == kGw;
                     const uint32_t idesc = (idesc_bf16_mn_major(BM, BN) & ~(3u << 15)) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
                     // to the next 16 of K: 32 bytes along swizzled rows, or 16 rows of 128 bytes
                     const uint32_t a_step = a_mn ? 2048 : 32, b_step = b_mn ? 2048 : 32;
@@ -531,20 +533,19 @@ template <int N>
 struct Thin {
     static constexpr int kStage = 2 * kBox + N * BK * 2;
     static constexpr int kOut = N * kThinLd * 4;
-    static constexpr int kStages = (225 * 1024 - kOut - 5 * N * 4 - 1024) / kStage < 10 ? (225 * 1024 - kOut - 5 * N * 4 - 1024) / kStage : 10;
+    static constexpr int kFit = (226 * 1024 - kOut - 1024) / kStage, kStages = kFit < 10 ? kFit : 10;
     static constexpr int kBoxRows = N <= 64 ? N : N / 2;   // of x
     static constexpr uint32_t kColumns = N == 32 ? 64 : N == 64 ? 128 : 256;   // two accumulators, a power of two
-    static constexpr int kSmem = kStages * kStage + kOut + 5 * N * 4 + 256 + 1024;
+    static constexpr int kSmem = kStages * kStage + kOut + 1024;
 };
 
-template <int MAIN, int N>
+template <int N>
 __global__ void __launch_bounds__(kThinThreads, 1)
 linear_thin_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtensorMap mw, const __grid_constant__ Job j) {
     using S = Thin<N>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
     float* out = reinterpret_cast<float*>(smem + S::kStages * S::kStage);   // [N][kThinLd]
-    float* known = out + N * kThinLd;                                       // [5][N] of each token
     __shared__ uint64_t full[S::kStages], empty[S::kStages], tfull[2], tempty[2], mma_done;
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int abort_flag;
@@ -572,18 +573,6 @@ linear_thin_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
     }
     pdl_wait();
     pdl_launch_dependents();
-    if (MAIN == kDelta && threadIdx.x >= 64) {
-        for (int t = threadIdx.x - 64; t < N; t += 256) {
-            const bool is = t < j.T;
-            const int64_t y = is ? j.target[t] : -1;
-            const float lse = is ? j.lse[t] : -INFINITY;
-            known[t] = lse;
-            known[N + t] = y >= 0 && y < j.V ? j.g_logp[t] : 0.0f;
-            known[2 * N + t] = is && j.g_entropy ? j.g_entropy[t] : 0.0f;
-            known[3 * N + t] = is && j.g_entropy ? j.entropy[t] : 0.0f;
-            reinterpret_cast<int*>(known)[4 * N + t] = y >= 0 && y < j.V && lse != -INFINITY ? static_cast<int>(y) : -1;
-        }
-    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -654,7 +643,7 @@ linear_thin_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
         const int q = warp & 3, h = (warp - 2) >> 2, row = q * 32 + lane, id = threadIdx.x - 64;
         const int token = id / kShare, from = id % kShare * kPart;
         const bool mine = token < N && token < j.T;
-        const int64_t y = MAIN == kScore && mine ? j.target[token] : -1;
+        const int64_t y = mine ? j.target[token] : -1;
         Sums sums = {-INFINITY, 0.0f, 0.0f};
         int cc = 0;
         bool ok = true;
@@ -685,25 +674,6 @@ linear_thin_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
 #pragma unroll
             for (int i = 0; i < kHalf; ++i) out[(h * kHalf + i) * kThinLd + row] = v0 + row < j.V ? x[i] : -INFINITY;
             named_all(true);
-            if (MAIN == kDelta) {
-                // a warp takes every eighth token, a lane four rows of W
-                __nv_bfloat16* dst = j.delta + static_cast<int64_t>(t) * kThinRows + 4 * lane;
-#pragma unroll 3
-                for (int i = warp - 2; i < N; i += 8) {
-                    const float lse = known[i], g = known[N + i], ge = known[2 * N + i], hh = known[3 * N + i];
-                    const int at = reinterpret_cast<const int*>(known)[4 * N + i] - static_cast<int>(v0) - 4 * lane;
-                    const float4 a = *reinterpret_cast<const float4*>(out + i * kThinLd + 4 * lane);
-                    float d[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        d[k] = lse == -INFINITY ? 0.0f : delta_of(d[k], lse, g, ge, hh);
-                        if (k == at) d[k] += g;
-                    }
-                    if (i < j.T && KQ_IN_RANGE(t * kThinRows + 4 * lane + 3, j.ld_delta))
-                        *reinterpret_cast<uint2*>(dst + i * j.ld_delta) = make_uint2(pack_bf16(d[0], d[1]), pack_bf16(d[2], d[3]));
-                }
-                continue;
-            }
             if (mine) {
                 const float4* at = reinterpret_cast<const float4*>(out + token * kThinLd + from);
                 float m = -INFINITY;
@@ -731,16 +701,267 @@ linear_thin_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
             }
             __syncwarp();
         }
-        if (MAIN == kScore) {
-            if constexpr (kShare > 1) {
 #pragma unroll
-                for (int o = 1; o < kShare; o <<= 1)
-                    sums.join(__shfl_xor_sync(0xffffffffu, sums.m, o), __shfl_xor_sync(0xffffffffu, sums.z, o),
-                              __shfl_xor_sync(0xffffffffu, sums.s, o));
-            }
-            if (mine && from == 0 && KQ_IN_RANGE(blockIdx.x, j.parts))
-                j.part[static_cast<int64_t>(token) * j.parts + blockIdx.x] = make_float4(sums.m, sums.z, sums.s, 0.0f);
+        for (int o = 1; o < kShare; o <<= 1)
+            sums.join(__shfl_xor_sync(0xffffffffu, sums.m, o), __shfl_xor_sync(0xffffffffu, sums.z, o),
+                      __shfl_xor_sync(0xffffffffu, sums.s, o));
+        if (mine && from == 0 && KQ_IN_RANGE(blockIdx.x, j.parts))
+            j.part[static_cast<int64_t>(token) * j.parts + blockIdx.x] = make_float4(sums.m, sums.z, sums.s, 0.0f);
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (abort_flag && threadIdx.x == 0) record_error(j.info, -KQ_ERR_TIMEOUT);
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, S::kColumns);
+    }
+}
+
+// ---- few rows, backwards. A CTA takes 128 rows of W at a time: their logits (the rows of W by N tokens), D, and the rows of gW:
+// D, rounded to bf16, goes to shared memory as the operand of D x, 128 columns of gW at a time, and to `delta` (a row of N tokens
+// for each row of W) for gx. One tile's products D x are issued between the next one's slabs, so that W's rows come in while gW's
+// go out; both are bytes that nothing else moves (W twice with gx).
+constexpr int kWide = 128;                       // columns of gW at a time
+template <int N>
+struct ThinGrad {
+    static constexpr int kBlocks = (N + 63) / 64;                       // of 64 tokens
+    static constexpr int kSlab = 2 * kBox + N * BK * 2, kColumnsOfX = 2 * kBlocks * kBox;
+    static constexpr int kStage = kSlab > kColumnsOfX ? kSlab : kColumnsOfX;
+    static constexpr int kD = kBlocks * 2 * kBox;                       // D of a tile
+    static constexpr int kKnown = N * 20;
+    static constexpr int kFit = (226 * 1024 - kD - 8 * kOutBox - kKnown - 1024) / kStage, kStages = kFit < 8 ? kFit : 8;
+    static constexpr uint32_t kColumns = 512;                           // two accumulators of N and two of kWide
+    static constexpr int kSmem = kStages * kStage + kD + 8 * kOutBox + kKnown + 1024;
+    static_assert(kStage % 1024 == 0 && kStages >= 3, "stages");
+};
+
+template <int N>
+__global__ void __launch_bounds__(kThinThreads, 1)
+linear_thin_grad_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtensorMap mw, const __grid_constant__ CUtensorMap mxt,
+                        const __grid_constant__ CUtensorMap out_w, const __grid_constant__ Job j) {
+    using S = ThinGrad<N>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    uint8_t* dop = smem + S::kStages * S::kStage;           // D as an operand: blocks of 64 tokens, 128-byte lines of a row of W
+    uint8_t* boxes = dop + S::kD;
+    float4* known = reinterpret_cast<float4*>(boxes + 8 * kOutBox);   // of each token: log-sum, the gradients, entropy
+    int* target = reinterpret_cast<int*>(known + N);
+    __shared__ uint64_t full[S::kStages], empty[S::kStages], zfull[2], zempty[2], gfull[2], gempty[2], dfull, mma_done;
+    __shared__ uint32_t tmem_slot;
+    __shared__ volatile int abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S::kStages; ++s) {
+            mbar_init(&full[s], 1);
+            mbar_init(&empty[s], 1);
         }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(&zfull[b], 1);
+            mbar_init(&zempty[b], 8);
+            mbar_init(&gfull[b], 1);
+            mbar_init(&gempty[b], 8);
+        }
+        mbar_init(&dfull, 8);
+        mbar_init(&mma_done, 1);
+        abort_flag = 0;
+        fence_mbar_init();
+    }
+    if (warp == 1) {
+        tmem_alloc(&tmem_slot, S::kColumns);
+        tmem_relinquish();
+    }
+    if (warp == 0 && lane == 0) {
+        tma_prefetch_desc(&mx);
+        tma_prefetch_desc(&mw);
+        tma_prefetch_desc(&mxt);
+        tma_prefetch_desc(&out_w);
+    }
+    pdl_wait();
+    pdl_launch_dependents();
+    if (threadIdx.x >= 64) {
+        for (int t = threadIdx.x - 64; t < N; t += 256) {
+            const bool is = t < j.T;
+            const int64_t y = is ? j.target[t] : -1;
+            const bool scored = y >= 0 && y < j.V;
+            const float lse = is ? j.lse[t] : -INFINITY;
+            known[t] = make_float4(lse, scored ? j.g_logp[t] : 0.0f, is && j.g_entropy ? j.g_entropy[t] : 0.0f,
+                                   is && j.g_entropy ? j.entropy[t] : 0.0f);
+            target[t] = scored && lse != -INFINITY ? static_cast<int>(y) : -1;
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    const int tiles = static_cast<int>((j.V + kThinRows - 1) / kThinRows), step = gridDim.x;
+    const int mine = (tiles - static_cast<int>(blockIdx.x) + step - 1) / step;     // tiles of this CTA; the grid has no more CTAs than tiles
+    const int slabs = j.d_slabs, turns = (slabs + 1) / 2;                          // a turn: kWide columns of gW, two slabs
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int k = 0;
+            bool ok = true;
+            auto room = [&](uint32_t bytes) {
+                const int st = k % S::kStages;
+                ok = ok && mbar_wait(&empty[st], (static_cast<uint32_t>(k / S::kStages) & 1u) ^ 1u, &abort_flag);
+                if (ok) mbar_arrive_expect_tx(&full[st], bytes);
+                return ok;
+            };
+            for (int r = 0; r <= mine && ok; ++r) {
+                const int v = (static_cast<int>(blockIdx.x) + r * step) * kThinRows;
+                for (int c = 0; c < turns && ok; ++c) {
+                    if (r > 0 && j.gw) {
+                        if (!room(S::kColumnsOfX)) break;
+                        uint8_t* base = smem + k % S::kStages * S::kStage;
+#pragma unroll
+                        for (int i = 0; i < 2 * S::kBlocks; ++i)
+                            tma_load_2d(base + i * kBox, &mxt, &full[k % S::kStages], c * kWide + (i & 1) * 64, (i >> 1) * 64);
+                        ++k;
+                    }
+                    for (int s = 2 * c; r < mine && s < min(2 * c + 2, slabs); ++s) {
+                        if (!room(S::kSlab)) break;
+                        uint8_t* base = smem + k % S::kStages * S::kStage;
+                        uint64_t* bar = &full[k % S::kStages];
+                        tma_load_2d(base, &mw, bar, s * BK, v);
+                        tma_load_2d(base + kBox, &mw, bar, s * BK, v + 64);
+#pragma unroll
+                        for (int i = 0; i < N / Thin<N>::kBoxRows; ++i)
+                            tma_load_2d(base + 2 * kBox + i * Thin<N>::kBoxRows * BK * 2, &mx, bar, s * BK, i * Thin<N>::kBoxRows);
+                        ++k;
+                    }
+                }
+            }
+            for (int i = (k > S::kStages ? k - S::kStages : 0); i < k; ++i)   // whatever is under way has landed
+                wait_quiet(&full[i % S::kStages], static_cast<uint32_t>(i / S::kStages) & 1u);
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            constexpr uint32_t z_idesc = idesc_bf16_mn_major(kThinRows, N) & ~(3u << 15);
+            constexpr uint32_t g_idesc = idesc_bf16_mn_major(kThinRows, kWide) & ~(1u << 15);   // x by columns
+            int k = 0, zc = 0, gc = 0;
+            bool ok = true;
+            auto landed = [&] {
+                ok = ok && mbar_wait(&full[k % S::kStages], static_cast<uint32_t>(k / S::kStages) & 1u, &abort_flag);
+                tc_fence_after();
+                return ok;
+            };
+            auto drained = [&](uint64_t* bars, int count) {
+                ok = ok && mbar_wait(&bars[count & 1], ((static_cast<uint32_t>(count) >> 1) & 1u) ^ 1u, &abort_flag);
+                tc_fence_after();
+                return ok;
+            };
+            for (int r = 0; r <= mine && ok; ++r) {
+                if (r > 0 && j.gw) {   // D of the last tile is there
+                    ok = mbar_wait(&dfull, static_cast<uint32_t>(r - 1) & 1u, &abort_flag);
+                    tc_fence_after();
+                }
+                for (int c = 0; c < turns && ok; ++c) {
+                    if (r > 0 && j.gw) {
+                        if (!drained(gempty, gc) || !landed()) break;
+                        const uint32_t sa = smem_u32(dop), sb = smem_u32(smem + k % S::kStages * S::kStage);
+#pragma unroll
+                        for (int q = 0; q < N / 16; ++q)
+                            tc_mma_f16(tmem + 2 * N + (gc & 1) * kWide, smem_desc_sw128(sa + q / 4 * 2 * kBox + q % 4 * 32, 16, 1024),
+                                       smem_desc_sw128(sb + q / 4 * 2 * kBox + q % 4 * 2048, kBox, 1024), g_idesc, q > 0 ? 1u : 0u);
+                        tc_commit(&empty[k % S::kStages]);
+                        tc_commit(&gfull[gc & 1]);
+                        ++k, ++gc;
+                    }
+                    for (int s = 2 * c; r < mine && s < min(2 * c + 2, slabs); ++s) {
+                        if (s % kDrainThin == 0 && !drained(zempty, zc)) break;
+                        if (!landed()) break;
+                        const uint32_t sa = smem_u32(smem + k % S::kStages * S::kStage), sb = sa + 2 * kBox;
+#pragma unroll
+                        for (int q = 0; q < BK / 16; ++q)
+                            tc_mma_f16(tmem + (zc & 1) * N, smem_desc_sw128(sa + q * 32, 16, 1024), smem_desc_sw128(sb + q * 32, 16, 1024),
+                                       z_idesc, (s % kDrainThin > 0 || q > 0) ? 1u : 0u);
+                        tc_commit(&empty[k % S::kStages]);
+                        ++k;
+                        if (s % kDrainThin == kDrainThin - 1 || s == slabs - 1) {
+                            tc_commit(&zfull[zc & 1]);
+                            ++zc;
+                        }
+                    }
+                }
+            }
+            tc_commit(&mma_done);
+            wait_quiet(&mma_done, 0);
+        }
+    } else {
+        constexpr int kHalf = N / 2;
+        const int q = warp & 3, h = (warp - 2) >> 2, row = q * 32 + lane;
+        const uint32_t lanes = tmem + (static_cast<uint32_t>(q * 32) << 16);
+        uint8_t* box = boxes + (warp - 2) * kOutBox;
+        int zc = 0, gc = 0;
+        bool ok = true;
+        auto filled = [&](uint64_t* bars, int count) {
+            const bool is = mbar_wait(&bars[count & 1], (static_cast<uint32_t>(count) >> 1) & 1u, &abort_flag);
+            ok = __all_sync(0xffffffffu, is);
+            tc_fence_after();
+            return ok;
+        };
+        auto drained = [&](uint64_t* bar) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar);
+        };
+        for (int r = 0; r <= mine && ok; ++r) {
+            const int tile = static_cast<int>(blockIdx.x) + r * step;
+            float x[kHalf];
+            for (int c = 0; c < turns; ++c) {
+                if (r > 0 && j.gw) {
+                    if (!filled(gfull, gc)) break;
+                    float y[64];
+#pragma unroll
+                    for (int p = 0; p < 2; ++p)
+                        tmem_ld32(lanes + static_cast<uint32_t>(2 * N + (gc & 1) * kWide + h * 64 + p * 32), reinterpret_cast<float(&)[32]>(y[p * 32]));
+                    tc_wait_ld();
+                    drained(&gempty[gc & 1]);
+                    ++gc;
+                    put_rows(box, &out_w, static_cast<int64_t>(tile - step) * kThinRows + q * 32, j.V, c * kWide + h * 64, j.d,
+                             [&](int i) { return y[i]; });
+                }
+                const int s = min(2 * c + 2, slabs);   // slabs that this turn ends with
+                if (r < mine && (s % kDrainThin == 0 || s == slabs)) {
+                    if (!filled(zfull, zc)) break;
+#pragma unroll
+                    for (int p = 0; p < kHalf / 16; ++p) {
+                        float v[16];
+                        tmem_ld16(lanes + static_cast<uint32_t>((zc & 1) * N + h * kHalf + p * 16), v);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) x[p * 16 + i] = s > kDrainThin ? x[p * 16 + i] + v[i] : v[i];
+                    }
+                    drained(&zempty[zc & 1]);
+                    ++zc;
+                }
+            }
+            if (!ok || r == mine) break;
+            // D; the last tile's products with it have been read out, so its operand may be written over
+            const int64_t v = static_cast<int64_t>(tile) * kThinRows + row;
+            __nv_bfloat16* dst = j.delta + v * N + h * kHalf;
+            const bool put = j.delta && KQ_IN_RANGE(v, j.ld_delta);
+#pragma unroll
+            for (int c = 0; c < kHalf / 8; ++c) {
+                float d[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int t = h * kHalf + 8 * c + e;
+                    const float4 a = known[t];
+                    d[e] = a.x != -INFINITY ? delta_of(x[8 * c + e], a.x, a.y, a.z, a.w) : 0.0f;
+                    if (target[t] == v) d[e] += a.y;
+                    if (v >= j.V) d[e] = 0.0f;
+                }
+                const uint4 w = make_uint4(pack_bf16(d[0], d[1]), pack_bf16(d[2], d[3]), pack_bf16(d[4], d[5]), pack_bf16(d[6], d[7]));
+                const int at = h * kHalf + 8 * c;
+                *reinterpret_cast<uint4*>(dop + at / 64 * 2 * kBox + row * 128 + ((at % 64 / 8) ^ (row & 7)) * 16) = w;
+                if (put) *reinterpret_cast<uint4*>(dst + 8 * c) = w;
+            }
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&dfull);
+        }
+        if (lane == 0) bulk_wait_le<0>();   // the results have been written
     }
     tc_fence_before();
     __syncthreads();
@@ -843,6 +1064,10 @@ kq_status make_map(CUtensorMap* m, const void* base, int64_t rows, int64_t cols,
     return KQ_OK;
 }
 
+// The matrices of a launch: x, W, D that is read; D, gx and gw that are written.
+struct Maps {
+    CUtensorMap x, w, d, out_d, out_x, out_w;
+};
 int max_clusters() {
     static std::atomic<int> kept[64] = {};
     int dev = 0;
@@ -858,10 +1083,6 @@ int max_clusters() {
     return c;
 }
 
-// The matrices of a launch: x, W, D that is read; D, gx and gw that are written.
-struct Maps {
-    CUtensorMap x, w, d, out_d, out_x, out_w;
-};
 // The pairs' runs of the logits' tiles: as many to each as bring it up to a common level of work, counted in slabs.
 void even_out(Job& j, int pairs) {
     const int deal = j.t_gx + j.t_gw, main = j.tiles - deal;
@@ -908,27 +1129,46 @@ kq_status run_tiles(const Maps& m, Job& j, cudaStream_t stream) {
     count_launch();
     return KQ_OK;
 }
-template <int MAIN, int N>
-kq_status run_thin_of(const CUtensorMap& mx, const CUtensorMap& mw, Job& j, cudaStream_t stream) {
-    static std::atomic<uint64_t> done{0};
-    KQ_TRY(once_per_device(done, [] {
-        KQ_CUDA(cudaFuncSetAttribute(linear_thin_kernel<MAIN, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, Thin<N>::kSmem));
+template <typename K, typename... Args>
+kq_status run_thin_kernel(K kernel, int smem, std::atomic<uint64_t>& done, int64_t blocks, cudaStream_t stream, const Args&... args) {
+    KQ_TRY(once_per_device(done, [&] {
+        KQ_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
         return KQ_OK;
     }));
-    const int64_t blocks = std::min<int64_t>(cdiv(j.w_main, kThinRows), num_sms());
-    j.parts = static_cast<int32_t>(blocks);
-    KQ_CUDA(launch_after(linear_thin_kernel<MAIN, N>, dim3(static_cast<unsigned>(blocks)), dim3(kThinThreads), Thin<N>::kSmem, stream, mx,
-                         mw, j));
+    KQ_CUDA(launch_after(kernel, dim3(static_cast<unsigned>(blocks)), dim3(kThinThreads), smem, stream, args...));
     count_launch();
     return KQ_OK;
 }
-int thin_box_rows(int64_t T) { return T <= 32 ? 32 : T <= 64 ? 64 : T <= 96 ? 48 : 64; }
-template <int MAIN>
-kq_status run_thin(const CUtensorMap& mx, const CUtensorMap& mw, Job& j, cudaStream_t stream) {
-    return j.T <= 32   ? run_thin_of<MAIN, 32>(mx, mw, j, stream)
-           : j.T <= 64 ? run_thin_of<MAIN, 64>(mx, mw, j, stream)
-           : j.T <= 96 ? run_thin_of<MAIN, 96>(mx, mw, j, stream)
-                       : run_thin_of<MAIN, 128>(mx, mw, j, stream);
+int64_t thin_blocks(int64_t V) { return std::min<int64_t>(cdiv(V, kThinRows), num_sms()); }
+// Tokens that a product has room for, and rows of a box of x.
+int thin_tokens(int64_t T, bool grad) { return T <= 32 ? 32 : T <= 64 ? 64 : T <= 96 && !grad ? 96 : 128; }
+int thin_box_rows(int n) { return n <= 64 ? n : n / 2; }
+
+template <int N>
+kq_status run_thin_of(const Maps& m, Job& j, cudaStream_t stream) {
+    static std::atomic<uint64_t> done{0};
+    j.parts = static_cast<int32_t>(thin_blocks(j.V));
+    return run_thin_kernel(linear_thin_kernel<N>, Thin<N>::kSmem, done, j.parts, stream, m.x, m.w, j);
+}
+kq_status run_thin(const Maps& m, Job& j, cudaStream_t stream) {
+    switch (thin_tokens(j.T, false)) {
+        case 32: return run_thin_of<32>(m, j, stream);
+        case 64: return run_thin_of<64>(m, j, stream);
+        case 96: return run_thin_of<96>(m, j, stream);
+        default: return run_thin_of<128>(m, j, stream);
+    }
+}
+template <int N>
+kq_status run_thin_grad_of(const Maps& m, const CUtensorMap& xt, const Job& j, cudaStream_t stream) {
+    static std::atomic<uint64_t> done{0};
+    return run_thin_kernel(linear_thin_grad_kernel<N>, ThinGrad<N>::kSmem, done, thin_blocks(j.V), stream, m.x, m.w, xt, m.out_w, j);
+}
+kq_status run_thin_grad(const Maps& m, const CUtensorMap& xt, const Job& j, cudaStream_t stream) {
+    switch (thin_tokens(j.T, true)) {
+        case 32: return run_thin_grad_of<32>(m, xt, j, stream);
+        case 64: return run_thin_grad_of<64>(m, xt, j, stream);
+        default: return run_thin_grad_of<128>(m, xt, j, stream);
+    }
 }
 kq_status set_up() {
     static std::atomic<uint64_t> done{0};
@@ -948,14 +1188,15 @@ struct Cut {
 };
 Cut cut_of(int64_t T, int64_t V, int64_t d) {
     Cut c;
-    const int64_t columns = std::max(kLeastPiece, kPiece / T / BN * BN);
-    c.piece = std::min(columns, cdiv(V, BN) * BN);
+    // few rows have D of the whole vocabulary, at most 2^27 values, by rows of W
+    const int64_t columns = T <= kThinMost ? V : std::max(kLeastPiece, kPiece / T / BN * BN);
+    c.piece = std::min(cdiv(columns, BN) * BN, cdiv(V, BN) * BN);
     c.pieces = cdiv(V, c.piece);
     const int64_t tiles = cdiv(T, BM) * cdiv(d, BN), slabs = cdiv(std::min(c.piece, V), BK);   // of the first piece
     const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(76 / tiles, slabs / 4));
     c.split_slabs = static_cast<int32_t>(cdiv(slabs, splits));
     c.splits = static_cast<int32_t>(cdiv(slabs, c.split_slabs));
-    c.delta = static_cast<size_t>(T) * c.piece * 2;
+    c.delta = static_cast<size_t>(T <= kThinMost ? thin_tokens(T, true) : T) * c.piece * 2;
     c.sum = c.pieces * c.splits > 1 ? static_cast<size_t>(c.splits) * T * d * sizeof(float) : 0;
     return c;
 }
@@ -1006,7 +1247,7 @@ extern "C" kq_status kq_linear_logprobs(const uint16_t* x, int64_t T, int64_t d,
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
     KQ_TRY(set_up());
     Maps m;
-    KQ_TRY(make_map(&m.x, x, T, d, ldx, who, T <= kThinMost ? thin_box_rows(T) : 64));
+    KQ_TRY(make_map(&m.x, x, T, d, ldx, who, T <= kThinMost ? thin_box_rows(thin_tokens(T, false)) : 64));
     KQ_TRY(make_map(&m.w, w, V, d, ldw, who));
     m.d = m.out_d = m.out_x = m.out_w = m.w;   // not used
     Job j = {};
@@ -1021,7 +1262,7 @@ extern "C" kq_status kq_linear_logprobs(const uint16_t* x, int64_t T, int64_t d,
     j.w_main = V;
     j.d_slabs = static_cast<int32_t>(cdiv(d, BK));
     j.info = info;
-    KQ_TRY(T <= kThinMost ? run_thin<kScore>(m.x, m.w, j, stream) : run_tiles<kScore>(m, j, stream));
+    KQ_TRY(T <= kThinMost ? run_thin(m, j, stream) : run_tiles<kScore>(m, j, stream));
     KQ_CUDA(launch_after(linear_join_kernel, dim3(static_cast<unsigned>(T)), dim3(128), 0, stream, j, logp, entropy, lse));
     count_launch();
     return KQ_OK;
@@ -1061,18 +1302,20 @@ extern "C" kq_status kq_linear_logprobs_grad(const uint16_t* x, int64_t T, int64
     __nv_bfloat16* delta[2] = {reinterpret_cast<__nv_bfloat16*>(at),
                                reinterpret_cast<__nv_bfloat16*>(at + (c.pieces > 1 ? al256(c.delta) : 0))};
     Maps m;
-    CUtensorMap read[2], write[2], thin_x;
+    CUtensorMap read[2], write[2];
+    const bool thin = T <= kThinMost;
+    const int n = thin_tokens(T, true);
     KQ_TRY(make_map(&m.x, x, T, d, ldx, who));
     KQ_TRY(make_map(&m.w, w, V, d, ldw, who));
     m.out_x = m.out_w = m.w;
     if (gx) KQ_TRY(make_map(&m.out_x, gx, T, d, ldgx, who, 32));
     if (gw) KQ_TRY(make_map(&m.out_w, gw, V, d, ldgw, who, 32));
     for (int i = 0; i < 2; ++i) {
-        KQ_TRY(make_map(&read[i], delta[i], T, c.piece, c.piece, who));
-        KQ_TRY(make_map(&write[i], delta[i], T, c.piece, c.piece, who, 32));
+        if (thin) KQ_TRY(make_map(&read[i], delta[i], V, n, n, who));
+        else KQ_TRY(make_map(&read[i], delta[i], T, c.piece, c.piece, who));
+        write[i] = read[i];
+        if (!thin) KQ_TRY(make_map(&write[i], delta[i], T, c.piece, c.piece, who, 32));
     }
-    const bool thin = T <= kThinMost;
-    if (thin) KQ_TRY(make_map(&thin_x, x, T, d, ldx, who, thin_box_rows(T)));
     if (info) {
         linear_targets_kernel<<<static_cast<unsigned>(std::min<int64_t>(cdiv(T, 256), 1024)), 256, 0, stream>>>(target, T, V, info);
         KQ_LAUNCH_CHECK("linear_targets_kernel");
@@ -1089,13 +1332,21 @@ extern "C" kq_status kq_linear_logprobs_grad(const uint16_t* x, int64_t T, int64
     j.d_slabs = static_cast<int32_t>(cdiv(d, BK));
     j.row_slabs = static_cast<int32_t>(cdiv(T, BK));
     j.info = info;
-    // launch i: D of piece i, the products with D of piece i - 1; few rows have a launch of their own for D
+    if (thin) {
+        Maps t = m;
+        KQ_TRY(make_map(&t.x, x, T, d, ldx, who, thin_box_rows(n)));
+        j.delta = gx ? delta[0] : nullptr;
+        j.gw = gw != nullptr;
+        KQ_TRY(run_thin_grad(t, m.x, j, stream));
+        if (!gx) return KQ_OK;
+    }
+    // launch i: D of piece i, the products with D of piece i - 1; of few rows gx alone is left
     for (int64_t i = 0; i <= c.pieces; ++i) {
         j.v_main = i * c.piece;
         j.w_main = std::min(c.piece, V - j.v_main);
         j.n_main = i < c.pieces && !thin ? static_cast<int32_t>(cdiv(j.w_main, BN)) : 0;
         j.delta = delta[i & 1];
-        if (thin && i < c.pieces) KQ_TRY(run_thin<kDelta>(thin_x, m.w, j, stream));
+        j.turned = thin;
         j.t_gx = j.t_gw = 0;
         if (i > 0) {
             j.v_prod = (i - 1) * c.piece;
@@ -1105,7 +1356,7 @@ extern "C" kq_status kq_linear_logprobs_grad(const uint16_t* x, int64_t T, int64
             j.first = i == 1;
             j.last = c.splits == 1 && i == c.pieces;
             if (gx) j.t_gx = splits * j.m_main * j.n_d;
-            if (gw) j.t_gw = static_cast<int32_t>(cdiv(j.w_prod, BM)) * j.n_d;
+            if (gw && !thin) j.t_gw = static_cast<int32_t>(cdiv(j.w_prod, BM)) * j.n_d;
         }
         j.tiles = j.t_gx + j.t_gw + j.m_main * j.n_main;
         m.d = read[(i + 1) & 1], m.out_d = write[i & 1];
