@@ -255,29 +255,39 @@ __device__ __forceinline__ float delta_of(float z, float lse, float g, float ge,
     return p > 0.0f ? -p * fmaf(ge, lp + h, g) : p == p ? 0.0f : p;
 }
 
-// 64 columns of a warp's 32 rows to a bf16 matrix by way of shared memory: value(i) is this lane's column i. A box of
-// 128-byte lines, swizzled; what lies outside the matrix (rows x cols) is left out.
-template <typename F>
-__device__ __forceinline__ void put_rows(uint8_t* box, const CUtensorMap* map, int64_t row0, int64_t rows, int64_t col0, int64_t cols,
-                                         F value) {
-    const int lane = threadIdx.x & 31;
-    if (row0 >= rows || col0 >= cols) return;   // the same for the warp
-    if (lane == 0) bulk_wait_read0();           // the last results have left the box
+// 64 columns of a warp's 32 rows to a bf16 matrix by way of shared memory: a box of 128-byte lines, swizzled, a line to a lane.
+// put_part: columns 8 FROM .. 8 TO, value(i) is this lane's column i. What lies outside the matrix (rows x cols) is left out.
+__device__ __forceinline__ void put_begin() {
+    if ((threadIdx.x & 31) == 0) bulk_wait_read0();   // the last results have left the box
     __syncwarp();
+}
+template <int FROM, int TO, typename F>
+__device__ __forceinline__ void put_part(uint8_t* box, F value) {
+    const int lane = threadIdx.x & 31;
     uint4* line = reinterpret_cast<uint4*>(box + lane * 128);
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
+    for (int c = FROM; c < TO; ++c) {
         uint32_t w[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) w[k] = pack_bf16(value(8 * c + 2 * k), value(8 * c + 2 * k + 1));
         line[c ^ (lane & 7)] = make_uint4(w[0], w[1], w[2], w[3]);
     }
+}
+__device__ __forceinline__ void put_end(uint8_t* box, const CUtensorMap* map, int64_t row0, int64_t rows, int64_t col0, int64_t cols) {
     fence_proxy_async();
     __syncwarp();
-    if (lane == 0) {
+    if ((threadIdx.x & 31) == 0 && row0 < rows && col0 < cols) {
         tma_store_2d(map, box, static_cast<int>(col0), static_cast<int>(row0));
         bulk_commit();
     }
+}
+template <typename F>
+__device__ __forceinline__ void put_rows(uint8_t* box, const CUtensorMap* map, int64_t row0, int64_t rows, int64_t col0, int64_t cols,
+                                         F value) {
+    if (row0 >= rows || col0 >= cols) return;   // the same for the warp
+    put_begin();
+    put_part<0, 8>(box, value);
+    put_end(box, map, row0, rows, col0, cols);
 }
 
 // D of 64 logits of a row, zeros from the vocabulary's end on.
@@ -784,7 +794,8 @@ linear_thin_grad_kernel(const __grid_constant__ CUtensorMap mx, const __grid_con
             const int64_t y = is ? j.target[t] : -1;
             const bool scored = y >= 0 && y < j.V;
             const float lse = is ? j.lse[t] : -INFINITY;
-            known[t] = make_float4(lse, scored ? j.g_logp[t] : 0.0f, is && j.g_entropy ? j.g_entropy[t] : 0.0f,
+            // a row of -infinity only, or none: p = 0 of every logit
+            known[t] = make_float4(lse == -INFINITY ? INFINITY : lse, scored ? j.g_logp[t] : 0.0f, is && j.g_entropy ? j.g_entropy[t] : 0.0f,
                                    is && j.g_entropy ? j.entropy[t] : 0.0f);
             target[t] = scored && lse != -INFINITY ? static_cast<int>(y) : -1;
         }
@@ -911,15 +922,18 @@ linear_thin_grad_kernel(const __grid_constant__ CUtensorMap mx, const __grid_con
             for (int c = 0; c < turns; ++c) {
                 if (r > 0 && j.gw) {
                     if (!filled(gfull, gc)) break;
-                    float y[64];
-#pragma unroll
-                    for (int p = 0; p < 2; ++p)
-                        tmem_ld32(lanes + static_cast<uint32_t>(2 * N + (gc & 1) * kWide + h * 64 + p * 32), reinterpret_cast<float(&)[32]>(y[p * 32]));
+                    const uint32_t at = lanes + static_cast<uint32_t>(2 * N + (gc & 1) * kWide + h * 64);
+                    float y[32];
+                    put_begin();
+                    tmem_ld32(at, y);
+                    tc_wait_ld();
+                    put_part<0, 4>(box, [&](int i) { return y[i]; });
+                    tmem_ld32(at + 32, y);
                     tc_wait_ld();
                     drained(&gempty[gc & 1]);
                     ++gc;
-                    put_rows(box, &out_w, static_cast<int64_t>(tile - step) * kThinRows + q * 32, j.V, c * kWide + h * 64, j.d,
-                             [&](int i) { return y[i]; });
+                    put_part<4, 8>(box, [&](int i) { return y[i - 32]; });
+                    put_end(box, &out_w, static_cast<int64_t>(tile - step) * kThinRows + q * 32, j.V, c * kWide + h * 64, j.d);
                 }
                 const int s = min(2 * c + 2, slabs);   // slabs that this turn ends with
                 if (r < mine && (s % kDrainThin == 0 || s == slabs)) {
@@ -941,19 +955,36 @@ linear_thin_grad_kernel(const __grid_constant__ CUtensorMap mx, const __grid_con
             const int64_t v = static_cast<int64_t>(tile) * kThinRows + row;
             __nv_bfloat16* dst = j.delta + v * N + h * kHalf;
             const bool put = j.delta && KQ_IN_RANGE(v, j.ld_delta);
+            // whether a target of this warp's tokens lies in the tile, which is rare
+            bool hit = false;
+#pragma unroll
+            for (int t = 0; t < kHalf; t += 32)
+                if (t + lane < kHalf) hit |= static_cast<unsigned>(target[h * kHalf + t + lane] - tile * kThinRows) < kThinRows;
+            hit = __any_sync(0xffffffffu, hit);
 #pragma unroll
             for (int c = 0; c < kHalf / 8; ++c) {
-                float d[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int t = h * kHalf + 8 * c + e;
-                    const float4 a = known[t];
-                    d[e] = a.x != -INFINITY ? delta_of(x[8 * c + e], a.x, a.y, a.z, a.w) : 0.0f;
-                    if (target[t] == v) d[e] += a.y;
-                    if (v >= j.V) d[e] = 0.0f;
-                }
-                const uint4 w = make_uint4(pack_bf16(d[0], d[1]), pack_bf16(d[2], d[3]), pack_bf16(d[4], d[5]), pack_bf16(d[6], d[7]));
                 const int at = h * kHalf + 8 * c;
+                float d[8];
+                if (j.g_entropy) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float4 a = known[at + e];
+                        d[e] = delta_of(x[8 * c + e], a.x, a.y, a.z, a.w);
+                    }
+                } else {   // the same without the entropy's part
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float2 a = *reinterpret_cast<const float2*>(known + at + e);
+                        d[e] = -a.y * ex2((x[8 * c + e] - a.x) * kLog2e);
+                    }
+                }
+                if (hit) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (target[at + e] == v) d[e] += known[at + e].y;
+                }
+                uint4 w = make_uint4(pack_bf16(d[0], d[1]), pack_bf16(d[2], d[3]), pack_bf16(d[4], d[5]), pack_bf16(d[6], d[7]));
+                if (v >= j.V) w = make_uint4(0, 0, 0, 0);
                 *reinterpret_cast<uint4*>(dop + at / 64 * 2 * kBox + row * 128 + ((at % 64 / 8) ^ (row & 7)) * 16) = w;
                 if (put) *reinterpret_cast<uint4*>(dst + 8 * c) = w;
             }
@@ -1007,22 +1038,22 @@ __global__ void __launch_bounds__(128) linear_join_kernel(const Job j, float* __
 }
 
 // gx = the sum of the splits, in order.
-__global__ void __launch_bounds__(256) linear_gx_kernel(const float* __restrict__ sum, int splits, int64_t T, int64_t d,
+__global__ void __launch_bounds__(64) linear_gx_kernel(const float* __restrict__ sum, int splits, int64_t T, int64_t d,
                                                         __nv_bfloat16* __restrict__ gx, int64_t ld) {
-    const int64_t each = T * d, per_row = d / 8;
+    const int64_t each = T * d, per_row = d / 4;
     pdl_wait();
     pdl_launch_dependents();
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < T * per_row; i += static_cast<int64_t>(gridDim.x) * 256) {
-        const int64_t row = i / per_row, col = (i - row * per_row) * 8;
-        float x[8] = {};
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < T * per_row;
+         i += static_cast<int64_t>(gridDim.x) * blockDim.x) {
+        const int64_t row = i / per_row, col = (i - row * per_row) * 4;
+        float x[4] = {};
+#pragma unroll 8
         for (int s = 0; s < splits; ++s) {
-            const float4* p = reinterpret_cast<const float4*>(sum + s * each + row * d + col);
-            const float4 a = p[0], b = p[1];
-            x[0] += a.x, x[1] += a.y, x[2] += a.z, x[3] += a.w, x[4] += b.x, x[5] += b.y, x[6] += b.z, x[7] += b.w;
+            const float4 a = *reinterpret_cast<const float4*>(sum + s * each + row * d + col);
+            x[0] += a.x, x[1] += a.y, x[2] += a.z, x[3] += a.w;
         }
-        if (KQ_IN_RANGE(row * ld + col + 7, (T - 1) * ld + d))
-            *reinterpret_cast<uint4*>(gx + row * ld + col) =
-                make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+        if (KQ_IN_RANGE(row * ld + col + 3, (T - 1) * ld + d))
+            *reinterpret_cast<uint2*>(gx + row * ld + col) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
     }
 }
 // Targets past the vocabulary are reported; the gradient's tiles leave them out.
@@ -1141,7 +1172,7 @@ kq_status run_thin_kernel(K kernel, int smem, std::atomic<uint64_t>& done, int64
 }
 int64_t thin_blocks(int64_t V) { return std::min<int64_t>(cdiv(V, kThinRows), num_sms()); }
 // Tokens that a product has room for, and rows of a box of x.
-int thin_tokens(int64_t T, bool grad) { return T <= 32 ? 32 : T <= 64 ? 64 : T <= 96 && !grad ? 96 : 128; }
+int thin_tokens(int64_t T) { return T <= 32 ? 32 : T <= 64 ? 64 : T <= 96 ? 96 : 128; }
 int thin_box_rows(int n) { return n <= 64 ? n : n / 2; }
 
 template <int N>
@@ -1151,7 +1182,7 @@ kq_status run_thin_of(const Maps& m, Job& j, cudaStream_t stream) {
     return run_thin_kernel(linear_thin_kernel<N>, Thin<N>::kSmem, done, j.parts, stream, m.x, m.w, j);
 }
 kq_status run_thin(const Maps& m, Job& j, cudaStream_t stream) {
-    switch (thin_tokens(j.T, false)) {
+    switch (thin_tokens(j.T)) {
         case 32: return run_thin_of<32>(m, j, stream);
         case 64: return run_thin_of<64>(m, j, stream);
         case 96: return run_thin_of<96>(m, j, stream);
@@ -1164,9 +1195,10 @@ kq_status run_thin_grad_of(const Maps& m, const CUtensorMap& xt, const Job& j, c
     return run_thin_kernel(linear_thin_grad_kernel<N>, ThinGrad<N>::kSmem, done, thin_blocks(j.V), stream, m.x, m.w, xt, m.out_w, j);
 }
 kq_status run_thin_grad(const Maps& m, const CUtensorMap& xt, const Job& j, cudaStream_t stream) {
-    switch (thin_tokens(j.T, true)) {
+    switch (thin_tokens(j.T)) {
         case 32: return run_thin_grad_of<32>(m, xt, j, stream);
         case 64: return run_thin_grad_of<64>(m, xt, j, stream);
+        case 96: return run_thin_grad_of<96>(m, xt, j, stream);
         default: return run_thin_grad_of<128>(m, xt, j, stream);
     }
 }
@@ -1196,7 +1228,7 @@ Cut cut_of(int64_t T, int64_t V, int64_t d) {
     const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(76 / tiles, slabs / 4));
     c.split_slabs = static_cast<int32_t>(cdiv(slabs, splits));
     c.splits = static_cast<int32_t>(cdiv(slabs, c.split_slabs));
-    c.delta = static_cast<size_t>(T <= kThinMost ? thin_tokens(T, true) : T) * c.piece * 2;
+    c.delta = static_cast<size_t>(T <= kThinMost ? thin_tokens(T) : T) * c.piece * 2;
     c.sum = c.pieces * c.splits > 1 ? static_cast<size_t>(c.splits) * T * d * sizeof(float) : 0;
     return c;
 }
@@ -1247,7 +1279,7 @@ extern "C" kq_status kq_linear_logprobs(const uint16_t* x, int64_t T, int64_t d,
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
     KQ_TRY(set_up());
     Maps m;
-    KQ_TRY(make_map(&m.x, x, T, d, ldx, who, T <= kThinMost ? thin_box_rows(thin_tokens(T, false)) : 64));
+    KQ_TRY(make_map(&m.x, x, T, d, ldx, who, T <= kThinMost ? thin_box_rows(thin_tokens(T)) : 64));
     KQ_TRY(make_map(&m.w, w, V, d, ldw, who));
     m.d = m.out_d = m.out_x = m.out_w = m.w;   // not used
     Job j = {};
@@ -1304,7 +1336,7 @@ extern "C" kq_status kq_linear_logprobs_grad(const uint16_t* x, int64_t T, int64
     Maps m;
     CUtensorMap read[2], write[2];
     const bool thin = T <= kThinMost;
-    const int n = thin_tokens(T, true);
+    const int n = thin_tokens(T);
     KQ_TRY(make_map(&m.x, x, T, d, ldx, who));
     KQ_TRY(make_map(&m.w, w, V, d, ldw, who));
     m.out_x = m.out_w = m.w;
@@ -1363,8 +1395,8 @@ extern "C" kq_status kq_linear_logprobs_grad(const uint16_t* x, int64_t T, int64
         KQ_TRY(run_tiles<kDelta>(m, j, stream));
     }
     if (gx && c.splits > 1) {
-        const int64_t blocks = std::min<int64_t>(cdiv(T * (d / 8), 256), static_cast<int64_t>(num_sms()) * 8);
-        KQ_CUDA(launch_after(linear_gx_kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream,
+        const int64_t blocks = std::min<int64_t>(cdiv(T * (d / 4), 64), static_cast<int64_t>(num_sms()) * 16);
+        KQ_CUDA(launch_after(linear_gx_kernel, dim3(static_cast<unsigned>(blocks)), dim3(64), 0, stream,
                              static_cast<const float*>(j.sum), c.splits, T, d, reinterpret_cast<__nv_bfloat16*>(gx), ldgx));
         count_launch();
     }
