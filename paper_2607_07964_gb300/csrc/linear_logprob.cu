@@ -504,8 +504,8 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
             const int64_t row0 = a.m0 + 128 * static_cast<int64_t>(rank) + q * 32, col = a.n0 + h * 64;
             if (MAIN == kScore) {
                 const Sums sums = score_row(j, x, row0 + lane, col);
-                if (row0 + lane < j.T && KQ_IN_RANGE(a.n0 / 64 + h, j.parts))
-                    if (col < j.V) j.part[(row0 + lane) * j.parts + a.n0 / 64 + h] = make_float4(sums.m, sums.z, sums.s, 0.0f);
+                if (row0 + lane < j.T && col < j.V && KQ_IN_RANGE(a.n0 / 64 + h, j.parts))
+                    j.part[(row0 + lane) * j.parts + a.n0 / 64 + h] = make_float4(sums.m, sums.z, sums.s, 0.0f);
             } else if (a.kind == kDelta) {
                 delta_rows(j, x, box, &out_d, row0, col);
             } else if (a.kind == kGx) {

@@ -168,7 +168,7 @@ def kq_debug_build() -> bool:
 
 
 DEBUG_UNITS = ("api", "syrk", "biip", "chol", "obs", "trail_tc", "gptaq", "infer", "check", "kv_store",
-               "kv_attend", "kv_evict", "logprob")
+               "kv_attend", "kv_evict", "logprob", "rotate", "linear_logprob")
 
 
 def kq_debug_status(reset: bool = True) -> tuple[str | None, int]:
