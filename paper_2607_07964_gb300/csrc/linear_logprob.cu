@@ -85,6 +85,42 @@ __device__ __forceinline__ bool named_all(bool p) {
         : "memory");
     return r != 0;
 }
+// The bounded waits of kq_common.cuh in which the hardware holds the thread back for up to kHold at a time, not for its
+// own short while: the result warps wait for most of a tile, and polling takes issue slots and power from the products.
+constexpr uint32_t kHold = 20000;   // ns
+template <bool CLUSTER>
+__device__ __forceinline__ bool held_try(uint64_t* bar, uint32_t parity) {
+    uint32_t ok;
+    if constexpr (CLUSTER)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(smem_u32(bar)), "r"(parity), "r"(kHold)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(smem_u32(bar)), "r"(parity), "r"(kHold)
+            : "memory");
+    return ok != 0;
+}
+template <bool CLUSTER = false>
+__device__ __forceinline__ bool held_wait(uint64_t* bar, uint32_t parity, volatile int* abort) {
+    if (held_try<CLUSTER>(bar, parity)) return true;
+    const uint64_t t0 = global_timer_ns();
+    for (uint32_t it = 0; it < kWaitLimitIters; ++it) {
+        if (held_try<CLUSTER>(bar, parity)) return true;
+        if (*abort) return false;
+        if (global_timer_ns() - t0 > kWaitLimitNs) break;
+    }
+    *abort = 1;
+    return false;
+}
 // 16 consecutive fp32 columns of the calling warp's 32 lanes of tensor memory.
 __device__ __forceinline__ void tmem_ld16(uint32_t at, float (&v)[16]) {
     uint32_t r[16];
@@ -197,7 +233,7 @@ __device__ __forceinline__ Tile tile_at(const Job& j, int t, int main_kind) {
 // Waits for a phase that the CTA's own earlier work ends, whatever has been given up.
 __device__ __forceinline__ void wait_quiet(uint64_t* bar, uint32_t parity) {
     int none = 0;
-    mbar_wait(bar, parity, &none);
+    held_wait(bar, parity, &none);
 }
 __host__ __device__ __forceinline__ int round_tile(int rd, int pair, int pairs) {
     return rd * pairs + ((rd & 1) ? pairs - 1 - pair : pair);
@@ -403,7 +439,7 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
                 const int n = a.n0 + 128 * static_cast<int>(rank) + (a.kind == MAIN ? static_cast<int>(j.v_main) : 0);
                 for (int s = 0; s < a.slabs; ++s, ++k) {
                     const int st = k % kStages;
-                    if (!mbar_wait(&empty[st], (static_cast<uint32_t>(k / kStages) & 1u) ^ 1u, abort_flag)) {
+                    if (!held_wait(&empty[st], (static_cast<uint32_t>(k / kStages) & 1u) ^ 1u, abort_flag)) {
                         ok = false;
                         break;
                     }
@@ -436,7 +472,7 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
                     const int drain = a.kind == MAIN ? kDrainLogits : kDrainGrads;
                     for (int s0 = 0; s0 < a.slabs && ok; s0 += drain, ++cc) {
                         const int buf = cc & 1;
-                        if (!mbar_wait_cl(&tempty[buf], ((static_cast<uint32_t>(cc) >> 1) & 1u) ^ 1u, abort_flag)) {
+                        if (!held_wait<true>(&tempty[buf], ((static_cast<uint32_t>(cc) >> 1) & 1u) ^ 1u, abort_flag)) {
                             ok = false;
                             break;
                         }
@@ -445,7 +481,7 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
                         const int s1 = min(a.slabs, s0 + drain);
                         for (int s = s0; s < s1; ++s, ++k) {
                             const int st = k % kStages;
-                            if (!mbar_wait(&full[st], static_cast<uint32_t>(k / kStages) & 1u, abort_flag)) {
+                            if (!held_wait(&full[st], static_cast<uint32_t>(k / kStages) & 1u, abort_flag)) {
                                 ok = false;
                                 break;
                             }
@@ -477,7 +513,7 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
             float x[64];
             for (int s0 = 0; s0 < a.slabs; s0 += drain, ++cc) {
                 const int buf = cc & 1;
-                ok = mbar_wait(&tfull[buf], (static_cast<uint32_t>(cc) >> 1) & 1u, abort_flag);
+                ok = held_wait(&tfull[buf], (static_cast<uint32_t>(cc) >> 1) & 1u, abort_flag);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
@@ -597,7 +633,7 @@ linear_thin_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
                 const int v = static_cast<int>(j.v_main) + t * kThinRows;
                 for (int s = 0; s < slabs; ++s, ++k) {
                     const int st = k % S::kStages;
-                    if (!mbar_wait(&empty[st], (static_cast<uint32_t>(k / S::kStages) & 1u) ^ 1u, &abort_flag)) {
+                    if (!held_wait(&empty[st], (static_cast<uint32_t>(k / S::kStages) & 1u) ^ 1u, &abort_flag)) {
                         ok = false;
                         break;
                     }
@@ -621,7 +657,7 @@ linear_thin_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
             for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
                 for (int s0 = 0; s0 < slabs && ok; s0 += kDrainThin, ++cc) {
                     const int buf = cc & 1;
-                    if (!mbar_wait(&tempty[buf], ((static_cast<uint32_t>(cc) >> 1) & 1u) ^ 1u, &abort_flag)) {
+                    if (!held_wait(&tempty[buf], ((static_cast<uint32_t>(cc) >> 1) & 1u) ^ 1u, &abort_flag)) {
                         ok = false;
                         break;
                     }
@@ -629,7 +665,7 @@ linear_thin_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
                     const int s1 = min(slabs, s0 + kDrainThin);
                     for (int s = s0; s < s1; ++s, ++k) {
                         const int st = k % S::kStages;
-                        if (!mbar_wait(&full[st], static_cast<uint32_t>(k / S::kStages) & 1u, &abort_flag)) {
+                        if (!held_wait(&full[st], static_cast<uint32_t>(k / S::kStages) & 1u, &abort_flag)) {
                             ok = false;
                             break;
                         }
@@ -661,7 +697,7 @@ linear_thin_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
             float x[kHalf];
             for (int s0 = 0; s0 < slabs; s0 += kDrainThin, ++cc) {
                 const int buf = cc & 1;
-                ok = mbar_wait(&tfull[buf], (static_cast<uint32_t>(cc) >> 1) & 1u, &abort_flag);
+                ok = held_wait(&tfull[buf], (static_cast<uint32_t>(cc) >> 1) & 1u, &abort_flag);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
@@ -814,7 +850,7 @@ linear_thin_grad_kernel(const __grid_constant__ CUtensorMap mx, const __grid_con
             bool ok = true;
             auto room = [&](uint32_t bytes) {
                 const int st = k % S::kStages;
-                ok = ok && mbar_wait(&empty[st], (static_cast<uint32_t>(k / S::kStages) & 1u) ^ 1u, &abort_flag);
+                ok = ok && held_wait(&empty[st], (static_cast<uint32_t>(k / S::kStages) & 1u) ^ 1u, &abort_flag);
                 if (ok) mbar_arrive_expect_tx(&full[st], bytes);
                 return ok;
             };
@@ -852,18 +888,18 @@ linear_thin_grad_kernel(const __grid_constant__ CUtensorMap mx, const __grid_con
             int k = 0, zc = 0, gc = 0;
             bool ok = true;
             auto landed = [&] {
-                ok = ok && mbar_wait(&full[k % S::kStages], static_cast<uint32_t>(k / S::kStages) & 1u, &abort_flag);
+                ok = ok && held_wait(&full[k % S::kStages], static_cast<uint32_t>(k / S::kStages) & 1u, &abort_flag);
                 tc_fence_after();
                 return ok;
             };
             auto drained = [&](uint64_t* bars, int count) {
-                ok = ok && mbar_wait(&bars[count & 1], ((static_cast<uint32_t>(count) >> 1) & 1u) ^ 1u, &abort_flag);
+                ok = ok && held_wait(&bars[count & 1], ((static_cast<uint32_t>(count) >> 1) & 1u) ^ 1u, &abort_flag);
                 tc_fence_after();
                 return ok;
             };
             for (int r = 0; r <= mine && ok; ++r) {
                 if (r > 0 && j.gw) {   // D of the last tile is there
-                    ok = mbar_wait(&dfull, static_cast<uint32_t>(r - 1) & 1u, &abort_flag);
+                    ok = held_wait(&dfull, static_cast<uint32_t>(r - 1) & 1u, &abort_flag);
                     tc_fence_after();
                 }
                 for (int c = 0; c < turns && ok; ++c) {
@@ -906,7 +942,7 @@ linear_thin_grad_kernel(const __grid_constant__ CUtensorMap mx, const __grid_con
         int zc = 0, gc = 0;
         bool ok = true;
         auto filled = [&](uint64_t* bars, int count) {
-            const bool is = mbar_wait(&bars[count & 1], (static_cast<uint32_t>(count) >> 1) & 1u, &abort_flag);
+            const bool is = held_wait(&bars[count & 1], (static_cast<uint32_t>(count) >> 1) & 1u, &abort_flag);
             ok = __all_sync(0xffffffffu, is);
             tc_fence_after();
             return ok;
