@@ -1354,6 +1354,11 @@ extern "C" kq_status kq_linear_logprobs_grad(const uint16_t* x, int64_t T, int64
                   "strides of at least d in multiples of 8", who);
         return KQ_ERR_INVALID_ARG;
     }
+    // later pieces read x and W again
+    if (T > 0 && ((gx && (gx == x || gx == w)) || (gw && (gw == w || gw == x)) || (gx && gx == gw))) {
+        set_error("%s: gx and gw must not be x, w or each other", who);
+        return KQ_ERR_INVALID_ARG;
+    }
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
     if (T == 0) {
         if (gw) KQ_CUDA(cudaMemset2DAsync(gw, ldgw * 2, 0, d * 2, V, stream));

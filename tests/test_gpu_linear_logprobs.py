@@ -201,6 +201,42 @@ def test_logits_of_a_huge_size():
     assert (ent == 0).all() and (logp <= 0).all() and torch.isfinite(logp).all()
 
 
+@pytest.mark.parametrize("T,V,d", [(3, 200, 72), (90, 513, 136), (129, 257, 64), (300, 1000, 200)])
+def test_gradients_between_other_columns_leave_them(T, V, d):
+    x, w, y = _case(T, V, d)
+    logp, ent, ls = _score(x, w, y)
+    wide = [torch.full((t.shape[0], t.shape[1] + 24), 3.0, dtype=t.dtype, device=DEV) for t in (x, w)]
+    ws = torch.empty(K().kq_linear_logprobs_grad_workspace(x, w), dtype=torch.uint8, device=DEV)
+    K().kq_linear_logprobs_grad(x, w, y, ls, torch.ones(T, device=DEV), ws, gx=wide[0][:, 8:8 + d], gw=wide[1][:, 8:8 + d])
+    for t in wide:
+        assert (t[:, :8] == 3).all() and (t[:, 8 + d:] == 3).all() and not (t[:, 8:8 + d] == 3).all()
+
+
+def test_two_streams_at_once():
+    cases = [_case(T, V, d, "peaked") for T, V, d in ((64, 20000, 512), (400, 5000, 512))]
+
+    def run(x, w, y, ws, gs, outs):
+        K().kq_linear_logprobs(x, w, y, outs[0], ws, entropy=outs[1], lse=outs[2])
+        K().kq_linear_logprobs_grad(x, w, y, outs[2], outs[0], gs, gx=outs[3], gw=outs[4])
+
+    sets = []
+    for x, w, y in cases:
+        sets.append((x, w, y, torch.empty(K().kq_linear_logprobs_workspace(x, w), dtype=torch.uint8, device=DEV),
+                     torch.empty(K().kq_linear_logprobs_grad_workspace(x, w), dtype=torch.uint8, device=DEV)))
+    want, got = ([[torch.empty(len(x), device=DEV) for _ in range(3)] + [torch.empty_like(x), torch.empty_like(w)] for x, w, _ in cases]
+                 for _ in range(2))
+    for s, o in zip(sets, want):
+        run(*s, o)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(5):
+        for st, s, o in zip(streams, sets, got):
+            with torch.cuda.stream(st):
+                run(*s, o)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for x, y in zip(want, got) for a, b in zip(x, y))
+
+
 def test_no_rows():
     x, w, y = _case(4, 300, 64)
     K().kq_linear_logprobs(x[:0], w, y[:0], torch.empty(0, device=DEV), None)

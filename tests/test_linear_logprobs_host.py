@@ -33,10 +33,12 @@ def test_scoring_refuses(K):
 
 def test_gradient_refuses(K):
     # x, T, d, ldx, w, V, ldw, target, lse, entropy, g_logp, g_entropy, gx, ldgx, gw, ldgw, info, ws, bytes, stream
-    good = [A, 4, 64, 64, A, 100, 64, A, A, A, A, A, A, 64, A, 64, None, A, 1 << 40, None]
+    B, C, D = P(512), P(1024), P(2048)
+    good = [A, 4, 64, 64, B, 100, 64, A, A, A, A, A, C, 64, D, 64, None, A, 1 << 40, None]
     _refused(K.lib().kq_linear_logprobs_grad, good, [
         (0, None, 1), (1, -1, 1), (2, 4, 2), (7, None, 1), (8, None, 1), (9, None, 1), (10, None, 1), (12, P(264), 1), (13, 56, 1),
-        (13, 66, 1), (14, P(264), 1), (15, 56, 1), (15, 68, 1), (17, None, 6), (17, P(264), 6), (18, 64, 6)])
+        (13, 66, 1), (14, P(264), 1), (15, 56, 1), (15, 68, 1), (12, A, 1), (12, B, 1), (12, D, 1), (14, A, 1), (14, B, 1), (17, None, 6),
+        (17, P(264), 6), (18, 64, 6)])
     args = list(good)
     args[12] = args[14] = None
     assert K.lib().kq_linear_logprobs_grad(*args) == K.KQ_ERR_INVALID_ARG
