@@ -771,19 +771,19 @@ constexpr int kWide = 128;                       // columns of gW at a time
 template <int N>
 struct ThinGrad {
     static constexpr int kBlocks = (N + 63) / 64;                       // of 64 tokens
-    static constexpr int kSlab = 2 * kBox + N * BK * 2, kColumnsOfX = 2 * kBlocks * kBox;
-    static constexpr int kStage = kSlab > kColumnsOfX ? kSlab : kColumnsOfX;
+    static constexpr int kBoxRows = Thin<N>::kBoxRows, kXBox = kBoxRows * 128, kXBoxes = N / kBoxRows;   // tokens of a box of x, bytes, boxes
+    static constexpr int kStage = 2 * kBox + N * BK * 2, kColumnsOfX = 2 * kXBoxes * kXBox;   // a slab; kWide columns of x
     static constexpr int kD = kBlocks * 2 * kBox;                       // D of a tile
     static constexpr int kKnown = N * 20;
     static constexpr int kFit = (226 * 1024 - kD - 8 * kOutBox - kKnown - 1024) / kStage, kStages = kFit < 8 ? kFit : 8;
     static constexpr uint32_t kColumns = 512;                           // two accumulators of N and two of kWide
     static constexpr int kSmem = kStages * kStage + kD + 8 * kOutBox + kKnown + 1024;
-    static_assert(kStage % 1024 == 0 && kStages >= 3, "stages");
+    static_assert(kStage % 1024 == 0 && kStages >= 3 && kColumnsOfX <= kStage, "stages");
 };
 
 template <int N>
 __global__ void __launch_bounds__(kThinThreads, 1)
-linear_thin_grad_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtensorMap mw, const __grid_constant__ CUtensorMap mxt,
+linear_thin_grad_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtensorMap mw,
                         const __grid_constant__ CUtensorMap out_w, const __grid_constant__ Job j) {
     using S = ThinGrad<N>;
     extern __shared__ uint8_t smem_raw[];
@@ -819,7 +819,6 @@ linear_thin_grad_kernel(const __grid_constant__ CUtensorMap mx, const __grid_con
     if (warp == 0 && lane == 0) {
         tma_prefetch_desc(&mx);
         tma_prefetch_desc(&mw);
-        tma_prefetch_desc(&mxt);
         tma_prefetch_desc(&out_w);
     }
     pdl_wait();
@@ -861,19 +860,19 @@ linear_thin_grad_kernel(const __grid_constant__ CUtensorMap mx, const __grid_con
                         if (!room(S::kColumnsOfX)) break;
                         uint8_t* base = smem + k % S::kStages * S::kStage;
 #pragma unroll
-                        for (int i = 0; i < 2 * S::kBlocks; ++i)
-                            tma_load_2d(base + i * kBox, &mxt, &full[k % S::kStages], c * kWide + (i & 1) * 64, (i >> 1) * 64);
+                        for (int i = 0; i < 2 * S::kXBoxes; ++i)
+                            tma_load_2d(base + i * S::kXBox, &mx, &full[k % S::kStages], c * kWide + (i & 1) * 64, (i >> 1) * S::kBoxRows);
                         ++k;
                     }
                     for (int s = 2 * c; r < mine && s < min(2 * c + 2, slabs); ++s) {
-                        if (!room(S::kSlab)) break;
+                        if (!room(S::kStage)) break;
                         uint8_t* base = smem + k % S::kStages * S::kStage;
                         uint64_t* bar = &full[k % S::kStages];
                         tma_load_2d(base, &mw, bar, s * BK, v);
                         tma_load_2d(base + kBox, &mw, bar, s * BK, v + 64);
 #pragma unroll
-                        for (int i = 0; i < N / Thin<N>::kBoxRows; ++i)
-                            tma_load_2d(base + 2 * kBox + i * Thin<N>::kBoxRows * BK * 2, &mx, bar, s * BK, i * Thin<N>::kBoxRows);
+                        for (int i = 0; i < S::kXBoxes; ++i)
+                            tma_load_2d(base + 2 * kBox + i * S::kXBox, &mx, bar, s * BK, i * S::kBoxRows);
                         ++k;
                     }
                 }
@@ -909,7 +908,8 @@ linear_thin_grad_kernel(const __grid_constant__ CUtensorMap mx, const __grid_con
 #pragma unroll
                         for (int q = 0; q < N / 16; ++q)
                             tc_mma_f16(tmem + 2 * N + (gc & 1) * kWide, smem_desc_sw128(sa + q / 4 * 2 * kBox + q % 4 * 32, 16, 1024),
-                                       smem_desc_sw128(sb + q / 4 * 2 * kBox + q % 4 * 2048, kBox, 1024), g_idesc, q > 0 ? 1u : 0u);
+                                       smem_desc_sw128(sb + 16 * q / S::kBoxRows * 2 * S::kXBox + 16 * q % S::kBoxRows * 128, S::kXBox, 1024),
+                                       g_idesc, q > 0 ? 1u : 0u);
                         tc_commit(&empty[k % S::kStages]);
                         tc_commit(&gfull[gc & 1]);
                         ++k, ++gc;
@@ -1226,16 +1226,16 @@ kq_status run_thin(const Maps& m, Job& j, cudaStream_t stream) {
     }
 }
 template <int N>
-kq_status run_thin_grad_of(const Maps& m, const CUtensorMap& xt, const Job& j, cudaStream_t stream) {
+kq_status run_thin_grad_of(const Maps& m, const Job& j, cudaStream_t stream) {
     static std::atomic<uint64_t> done{0};
-    return run_thin_kernel(linear_thin_grad_kernel<N>, ThinGrad<N>::kSmem, done, thin_blocks(j.V), stream, m.x, m.w, xt, m.out_w, j);
+    return run_thin_kernel(linear_thin_grad_kernel<N>, ThinGrad<N>::kSmem, done, thin_blocks(j.V), stream, m.x, m.w, m.out_w, j);
 }
-kq_status run_thin_grad(const Maps& m, const CUtensorMap& xt, const Job& j, cudaStream_t stream) {
+kq_status run_thin_grad(const Maps& m, const Job& j, cudaStream_t stream) {
     switch (thin_tokens(j.T)) {
-        case 32: return run_thin_grad_of<32>(m, xt, j, stream);
-        case 64: return run_thin_grad_of<64>(m, xt, j, stream);
-        case 96: return run_thin_grad_of<96>(m, xt, j, stream);
-        default: return run_thin_grad_of<128>(m, xt, j, stream);
+        case 32: return run_thin_grad_of<32>(m, j, stream);
+        case 64: return run_thin_grad_of<64>(m, j, stream);
+        case 96: return run_thin_grad_of<96>(m, j, stream);
+        default: return run_thin_grad_of<128>(m, j, stream);
     }
 }
 kq_status set_up() {
@@ -1410,7 +1410,7 @@ extern "C" kq_status kq_linear_logprobs_grad(const uint16_t* x, int64_t T, int64
         KQ_TRY(make_map(&t.x, x, T, d, ldx, who, thin_box_rows(n)));
         j.delta = gx ? delta[0] : nullptr;
         j.gw = gw != nullptr;
-        KQ_TRY(run_thin_grad(t, m.x, j, stream));
+        KQ_TRY(run_thin_grad(t, j, stream));
         if (!gx) return KQ_OK;
     }
     // launch i: D of piece i, the products with D of piece i - 1; of few rows gx alone is left
