@@ -26,6 +26,12 @@ namespace {
 constexpr int kThreads = 128;      // forwards
 constexpr int kGradThreads = 256;
 constexpr int kMaxDim = 256;
+// Blocks of an SM backwards: three have 85 registers a thread, which fp32's four values to a lane do with (16384 tokens of 20 fp32
+// rows of 128: 103 us, with two 108) and bf16's eight do not (40 bf16 rows: 105 us with two, 270 with three).
+template <typename T>
+__host__ __device__ constexpr int grad_blocks_of(int nv) {
+    return nv > 1 ? 1 : sizeof(T) == 4 ? 3 : 2;
+}
 constexpr int kMaxBlocks = 512;    // that a workspace has room for the sums of
 constexpr int kPairs = 0, kHalves = 1, kHalvesOdd = 2;   // layouts; odd: R / 2 is no multiple of a vector
 
@@ -402,7 +408,7 @@ __global__ void __launch_bounds__(kThreads, NV == 1 ? 7 : 4) qk_rotate_kernel(co
 // The same backwards. The warps go through units of a token's part in turn; the weights' gradients are summed in registers, then
 // over the block's slots in order, then (rotate_sums_kernel) over the blocks in order.
 template <typename T, int G, int NV, int MODE, bool FAST>
-__global__ void __launch_bounds__(kGradThreads, NV == 1 ? 2 : 1) qk_rotate_grad_kernel(const Rotate<T> p) {
+__global__ void __launch_bounds__(kGradThreads, grad_blocks_of<T>(NV)) qk_rotate_grad_kernel(const Rotate<T> p) {
     using L = Lane<T, FAST>;
     constexpr int E = L::E, R = 32 / G, kWarps = kGradThreads / 32, kSlots = kWarps * R;
     extern __shared__ __align__(16) float smem[];
@@ -575,7 +581,8 @@ kq_status launch(Rotate<T>& p, bool back, float* gqw, float* gkw, cudaStream_t s
         return KQ_OK;
     }
     constexpr int kWarps = kGradThreads / 32;
-    const int blocks = static_cast<int>(std::min({grad_blocks(p.tokens), cdiv(units, kWarps), static_cast<int64_t>(num_sms()) * 2}));
+    const int64_t fit = static_cast<int64_t>(num_sms()) * grad_blocks_of<T>(NV);
+    const int blocks = static_cast<int>(std::min({grad_blocks(p.tokens), cdiv(units, kWarps), fit}));
     size_t smem = kWarps * floats * sizeof(float);
     if (p.sums) smem = std::max(smem, kWarps * R * p.dim * sizeof(float));
     KQ_CUDA(launch_after(qk_rotate_grad_kernel<T, G, NV, MODE, FAST>, dim3(blocks), dim3(kGradThreads), smem, stream, p));
