@@ -148,6 +148,42 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&t);
 }
 
+// Two sums, products, or products and sums, in one instruction.
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y;\n\t"
+        "mov.b64 x, {%2, %3};\n\t"
+        "mov.b64 y, {%4, %5};\n\t"
+        "add.rn.f32x2 x, x, y;\n\t"
+        "mov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y;\n\t"
+        "mov.b64 x, {%2, %3};\n\t"
+        "mov.b64 y, {%4, %5};\n\t"
+        "mul.rn.f32x2 x, x, y;\n\t"
+        "mov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, z;\n\t"
+        "mov.b64 x, {%2, %3};\n\t"
+        "mov.b64 y, {%4, %5};\n\t"
+        "mov.b64 z, {%6, %7};\n\t"
+        "fma.rn.f32x2 x, x, y, z;\n\t"
+        "mov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+
 // The sums over one set of logits, against their maximum, joined with those over another: against the larger maximum.
 struct Sums {
     float m, z, s;
@@ -277,15 +313,18 @@ __device__ __forceinline__ Sums score_row(const Job& j, float (&x)[64], int64_t 
 #pragma unroll
     for (int i = 1; i < 64; ++i) a.m = max_nan(a.m, x[i]);
     const float ref = a.m == -INFINITY ? 0.0f : a.m;
-    float z[2] = {0.0f, 0.0f}, s[2] = {0.0f, 0.0f};
+    float2 z[2] = {}, s[2] = {};
+    const float2 less = make_float2(-ref, -ref), log2e = make_float2(kLog2e, kLog2e);
 #pragma unroll
-    for (int i = 0; i < 64; ++i) {
-        const float t = fmaxf((x[i] - ref) * kLog2e, kNone), e = ex2(t);
-        z[i & 1] += e;
-        s[i & 1] = fmaf(e, t, s[i & 1]);
+    for (int i = 0; i < 64; i += 2) {
+        float2 t = mul2(add2(make_float2(x[i], x[i + 1]), less), log2e);
+        t.x = fmaxf(t.x, kNone), t.y = fmaxf(t.y, kNone);
+        const float2 e = make_float2(ex2(t.x), ex2(t.y));
+        z[i / 2 & 1] = add2(z[i / 2 & 1], e);
+        s[i / 2 & 1] = fma2(e, t, s[i / 2 & 1]);
     }
-    a.z = z[0] + z[1];
-    a.s = s[0] + s[1];
+    a.z = (z[0].x + z[0].y) + (z[1].x + z[1].y);
+    a.s = (s[0].x + s[0].y) + (s[1].x + s[1].y);
     return a;
 }
 
@@ -436,7 +475,7 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
             bool ok = true;
             for (int i = 0; i < walk.count && ok; ++i) {
                 const Tile a = tile_at(j, walk.at(i), MAIN);
-                const bool a_mn = a.kind == kGw || (a.kind == kGx && j.turned), b_mn = a.kind == kGx || a.kind == kGw;
+                const bool a_mn = a.kind == (j.turned ? kGx : kGw), b_mn = a.kind == kGx || a.kind == kGw;
                 const CUtensorMap* ma = a.kind == kGx || a.kind == kGw ? &md : &mx;
                 const CUtensorMap* mb = a.kind == kGw ? &mx : &mw;
                 const int m = a.m0 + 128 * static_cast<int>(rank);
@@ -469,7 +508,7 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
                 bool ok = true;
                 for (int i = 0; i < walk.count && ok; ++i) {
                     const Tile a = tile_at(j, walk.at(i), MAIN);
-                    const bool a_mn = a.kind == kGw || (a.kind == kGx && j.turned), b_mn = a.kind == kGx || a.kind == kGw;
+                    const bool a_mn = a.kind == (j.turned ? kGx : kGw), b_mn = a.kind == kGx || a.kind == kGw;
                     const uint32_t idesc = (idesc_bf16_mn_major(BM, BN) & ~(3u << 15)) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
                     // to the next 16 of K: 32 bytes along swizzled rows, or 16 rows of 128 bytes
                     const uint32_t a_step = a_mn ? 2048 : 32, b_step = b_mn ? 2048 : 32;
@@ -776,6 +815,10 @@ linear_thin_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
 // as two kernels, D and then its product. gx is left to the tiles above: with 64 columns of W and a share of its rows to a
 // CTA, joined in a cluster, it took half as long again.
 constexpr int kWide = 128;                       // columns of gW at a time
+// Rows of W from which on gW comes in the same pass, half a tile for each SM: with fewer the tiles of a launch with gx share it out
+// better (36 rows of d = 4064, both gradients: V = 8000 74 us in one pass and 62 apart, 16000 91 and 96, 32001 160 and 178; 96 rows
+// of 1024: 33 and 32, 36 and 39, 63 and 63).
+constexpr int64_t kFused = 10240;
 template <int N>
 struct ThinGrad {
     static constexpr int kBlocks = (N + 63) / 64;                       // of 64 tokens
@@ -1413,13 +1456,16 @@ extern "C" kq_status kq_linear_logprobs_grad(const uint16_t* x, int64_t T, int64
     j.d_slabs = static_cast<int32_t>(cdiv(d, BK));
     j.row_slabs = static_cast<int32_t>(cdiv(T, BK));
     j.info = info;
+    bool fused = false;   // few rows: gW is done with D
     if (thin) {
         Maps t = m;
         KQ_TRY(make_map(&t.x, x, T, d, ldx, who, thin_box_rows(n)));
-        j.delta = gx ? delta[0] : nullptr;
-        j.gw = gw != nullptr;
+        // with few tiles of W its gradient goes by the tiles of gx's launch, which there are more of
+        fused = gw && V >= kFused;
+        j.delta = gx || !fused ? delta[0] : nullptr;
+        j.gw = fused;
         KQ_TRY(run_thin_grad(t, j, stream));
-        if (!gx) return KQ_OK;
+        if (!gx && fused) return KQ_OK;
     }
     // launch i: D of piece i, the products with D of piece i - 1; of few rows gx alone is left
     for (int64_t i = 0; i <= c.pieces; ++i) {
@@ -1437,7 +1483,7 @@ extern "C" kq_status kq_linear_logprobs_grad(const uint16_t* x, int64_t T, int64
             j.first = i == 1;
             j.last = c.splits == 1 && i == c.pieces;
             if (gx) j.t_gx = splits * j.m_main * j.n_d;
-            if (gw && !thin) j.t_gw = static_cast<int32_t>(cdiv(j.w_prod, BM)) * j.n_d;
+            if (gw && !fused) j.t_gw = static_cast<int32_t>(cdiv(j.w_prod, BM)) * j.n_d;
         }
         j.tiles = j.t_gx + j.t_gw + j.m_main * j.n_main;
         m.d = read[(i + 1) & 1], m.out_d = write[i & 1];

@@ -72,7 +72,8 @@ def _score(x, w, y, info=None, poison=255):
 
 
 SIZES = [(1, 1, 8), (1, 1000, 64), (2, 127, 72), (3, 128, 520), (5, 129, 8), (17, 4097, 264), (127, 300, 1000), (128, 513, 512),
-         (129, 257, 1024), (256, 255, 136), (257, 1025, 2056), (300, 20000, 128), (1000, 5003, 320), (4100, 700, 64), (8, 33000, 4096)]
+         (129, 257, 1024), (256, 255, 136), (257, 1025, 2056), (300, 20000, 128), (1000, 5003, 320), (4100, 700, 64), (8, 33000, 4096),
+         (33, 10241, 72), (64, 20000, 136), (100, 12345, 328), (90, 11000, 520), (10, 10240, 8)]
 
 
 @pytest.mark.parametrize("T,V,d", SIZES)
