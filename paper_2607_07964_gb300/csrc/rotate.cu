@@ -11,11 +11,11 @@
 // upper 32 bits are used (1.5e-9 rad), rounded to fp32 (within 2^-25 of a turn): 2e-7 of the row's size.
 //
 // What bounds it: bytes, 2 elements moved for each forward, 3 backward, against about 12 instructions an
-// element. So a warp takes a token and its heads by itself: it has the next two looks' loads in flight while it works
-// on two (16 bytes to a lane, G lanes to a row, 32 / G rows a look), computes cos and sin of the token's pairs once, and exchanges
-// partners by shuffles. Backwards the warps stay and go from token to token, the weights' sums in registers.
-// Measured: 32768 tokens of 40 bf16 rows of 128, with norms, 121 us (5.5 TB/s, 141 instructions for two rows of a warp);
-// backwards 16384 tokens 105 us (4.8 TB/s, 215 instructions).
+// element. So a warp takes a token, or one for each of its groups of G lanes, by itself: it has the next two looks' loads in flight
+// while it works on two (16 bytes to a lane, G lanes to a row, 32 / G rows a look), computes cos and sin of the tokens' pairs
+// once, and exchanges partners by shuffles. Backwards the warps stay and go from token to token, the weights' sums in registers.
+// Measured: 32768 tokens of 40 bf16 rows of 128, with norms, 120 us (5.6 TB/s, about 140 instructions for two rows of a
+// warp); backwards 16384 tokens 105 us (4.8 TB/s, 215 instructions).
 #include <algorithm>
 #include <atomic>
 
@@ -34,6 +34,7 @@ template <typename T>
 __host__ __device__ constexpr int grad_blocks_of(int nv) {
     return nv > 1 ? 1 : sizeof(T) == 4 ? 3 : 2;
 }
+constexpr int kManyRows = 36;      // of a token, see launch_mode
 constexpr int kMaxBlocks = 512;    // that a workspace has room for the sums of
 constexpr int kPairs = 0, kHalves = 1, kHalvesOdd = 2;   // layouts; odd: R / 2 is no multiple of a vector
 
@@ -53,7 +54,7 @@ struct Rotate {
     const uint64_t* freq;
     const int32_t *pos, *start, *first;
     int32_t batch, dim, half;        // half: pairs
-    int32_t parts, part;   // of a token's rows, each of `part` looks at them
+    int32_t parts, part;   // of a warp's tokens' rows, each of `part` looks at them
     float scale, eps;
     float* sums;       // backward: [blocks][2][dim] of weight gradients, or nullptr
 };
@@ -228,36 +229,44 @@ struct Share {
     }
 };
 
-// cos and sin of a token's pairs, by a warp; whether the token has a position.
-template <typename T>
-__device__ __forceinline__ bool fill_table(const Rotate<T>& p, int64_t t, float2* table) {
-    int64_t pos = t;
-    bool is = true;
+// cos and sin of the pairs of A tokens from t0 on, by a warp; a bit for each of them that is there and has a position.
+template <int A, typename T>
+__device__ __forceinline__ uint32_t fill_tables(const Rotate<T>& p, int64_t t0, float2* table) {
+    const int lane = threadIdx.x & 31;
+    bool is = lane < A && t0 + lane < p.tokens;
+    int64_t mine = t0 + lane;   // position of token lane
     if (p.pos) {
-        pos = p.pos[t];
+        if (is) mine = p.pos[mine];
     } else if (p.start) {
-        const int b = kv_sequence_of_warp(p.start, p.batch, t);
-        is = b >= 0;
-        if (is) pos = p.first[b] + (t - p.start[b]);
+#pragma unroll
+        for (int a = 0; a < A; ++a) {
+            const int b = kv_sequence_of_warp(p.start, p.batch, t0 + a);
+            if (lane == a && is) {
+                is = b >= 0;
+                if (is) mine = p.first[b] + (mine - p.start[b]);
+            }
+        }
     }
-    __syncwarp();   // the table's last use
-    for (int j = threadIdx.x & 31; j < p.half; j += 32) {
-        const int32_t turn = static_cast<int32_t>((static_cast<uint64_t>(pos) * p.freq[j]) >> 32);
-        float s, c;
-        sincospif(static_cast<float>(turn) * 0x1p-31f, &s, &c);
-        table[j] = make_float2(c * p.scale, s * p.scale);
+    const uint32_t known = __ballot_sync(0xffffffffu, is);
+    __syncwarp();   // the tables have had their last use
+#pragma unroll
+    for (int a = 0; a < A; ++a) {
+        const uint64_t pos = static_cast<uint64_t>(__shfl_sync(0xffffffffu, mine, a));
+        for (int j = lane; j < p.half; j += 32) {
+            const int32_t turn = static_cast<int32_t>((pos * p.freq[j]) >> 32);
+            float s, c;
+            sincospif(static_cast<float>(turn) * 0x1p-31f, &s, &c);
+            table[a * p.half + j] = make_float2(c * p.scale, s * p.scale);
+        }
     }
     __syncwarp();
-    return is;
+    return known;
 }
-// A warp looks at 32 / G rows at a time, first of the queries, then of the keys; an even number of looks at each, as it works
-// on two side by side.
-template <int G>
-__host__ __device__ constexpr int looks_at(int heads) {
-    return (heads + 2 * (32 / G) - 1) / (2 * (32 / G)) * 2;
-}
+// The 32 / G groups of lanes of a warp are of A tokens, and of as many rows of each as that leaves (A = 1 or 32 / G). They go
+// through the rows together, queries, then keys, two looks at a time: an even number of looks at each.
+__host__ __device__ constexpr int looks_at(int heads, int rows) { return (heads + 2 * rows - 1) / (2 * rows) * 2; }
 __host__ __device__ constexpr int warp_floats(int mode, int g, int half, int dim) {   // of shared memory
-    return (2 * half + (mode == kHalvesOdd ? 32 / g * dim : 0) + 1) & ~1;
+    return (32 / g * 2 * half + (mode == kHalvesOdd ? 32 / g * dim : 0) + 1) & ~1;
 }
 // sum of x y
 template <int NV, int E>
@@ -316,21 +325,24 @@ __device__ __forceinline__ void unpack_weights(const T* w, const S& sh, float (&
 
 // A warp to a part of a token's rows. 28 warps on an SM: 24 or 20 leave too few loads in flight (32768 tokens of 40 bf16 rows of
 // 128: 113, 118 and 118 us), 32 take too many registers (143).
-template <typename T, int G, int NV, int MODE, bool FAST>
+template <typename T, int G, int NV, int MODE, bool FAST, int A>
 __global__ void __launch_bounds__(kThreads, NV == 1 ? 7 : 4) qk_rotate_kernel(const Rotate<T> p) {
     using L = Lane<T, FAST>;
     constexpr int E = L::E, R = 32 / G;
     extern __shared__ __align__(16) float smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane / G;
-    const int64_t unit = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + warp;
-    const int64_t t = p.parts == 1 ? unit : unit / p.parts;
-    if (t >= p.tokens) return;
+    const int64_t unit = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + warp, group = p.parts == 1 ? unit : unit / p.parts;
+    constexpr int H = R / A;   // rows of a token in a look
+    const int hsub = sub % H;
+    const int64_t t0 = group * A, t = t0 + sub / H;
+    if (t0 >= p.tokens) return;
+    const bool mine = t < p.tokens;
     float* mem = smem + warp * warp_floats(MODE, G, p.half, p.dim);
     float2* table = reinterpret_cast<float2*>(mem);
-    float* xch = mem + 2 * p.half + sub * p.dim;
+    float* xch = mem + R * 2 * p.half + sub * p.dim;
     Share<T, G, NV, MODE> sh(lane % G, p.dim, p.half);
-    const int queries = looks_at<G>(p.s[0].heads), all = queries + looks_at<G>(p.s[1].heads);
-    const int first = static_cast<int>(unit - t * p.parts) * p.part, last = min(first + p.part, all);
+    const int queries = looks_at(p.s[0].heads, H), all = queries + looks_at(p.s[1].heads, H);
+    const int first = static_cast<int>(unit - group * p.parts) * p.part, last = min(first + p.part, all);
     pdl_wait();
     pdl_launch_dependents();
     // the two looks that are fetched next, before the ones that are worked on
@@ -338,7 +350,7 @@ __global__ void __launch_bounds__(kThreads, NV == 1 ? 7 : 4) qk_rotate_kernel(co
     const T* src[2];
 #pragma unroll
     for (int side = 0; side < 2; ++side) {
-        const int h = (side ? max(first - queries, 0) : first) * R + sub;
+        const int h = (side ? max(first - queries, 0) : first) * H + hsub;
         src[side] = p.s[side].x + t * p.s[side].x_token + h * p.s[side].x_head + sh.dim_of(0, 0);
     }
     uint4 raw[2][NV];
@@ -349,21 +361,23 @@ __global__ void __launch_bounds__(kThreads, NV == 1 ? 7 : 4) qk_rotate_kernel(co
     auto fetch = [&] {
         if (next >= last) return;
         const bool key = next >= queries;
-        const int h = (key ? next - queries : next) * R + sub, heads = key ? p.s[1].heads : p.s[0].heads;
-        const int64_t head = key ? p.s[1].x_head : p.s[0].x_head;
+        const int h = (key ? next - queries : next) * H + hsub, heads = key ? p.s[1].heads : p.s[0].heads;
+        const int64_t head = H * (key ? p.s[1].x_head : p.s[0].x_head);
         const T* at = key ? src[1] : src[0];
 #pragma unroll
         for (int u = 0; u < 2; ++u)
-            if (h + u * R < heads) {
+            if (mine && h + u * H < heads) {
 #pragma unroll
-                for (int k = 0; k < NV; ++k) raw[u][k] = L::load(at + u * R * head + k * G * E, sh.n[k]);
+                for (int k = 0; k < NV; ++k) raw[u][k] = L::load(at + u * head + k * G * E, sh.n[k]);
             }
         next += 2;
-        if (key) src[1] = at + 2 * R * head;
-        else src[0] = at + 2 * R * head;
+        if (key) src[1] = at + 2 * head;
+        else src[0] = at + 2 * head;
     };
     fetch();
-    if (!fill_table(p, t, table)) return;
+    const uint32_t known = fill_tables<A>(p, t0, table);
+    if (known == 0) return;
+    const bool is = known >> (sub / H) & 1;
     const float over = 1.0f / static_cast<float>(p.dim);
     const bool full = 2 * p.half == p.dim;
 #pragma unroll
@@ -375,11 +389,12 @@ __global__ void __launch_bounds__(kThreads, NV == 1 ? 7 : 4) qk_rotate_kernel(co
         {
             float w[NV][E];
             unpack_weights<T, NV, FAST>(s.w, sh, w);
-            sh.template take<false>(table, p.half, w, xch);
+            sh.template take<false>(table + sub / H * p.half, p.half, w, xch);
         }
-        int h = (side ? from - queries : from) * R + sub;
-        T* dst = s.out + t * s.o_token + h * s.o_head + sh.dim_of(0, 0);
-        for (int i = from; i < to; i += 2, h += 2 * R, dst += 2 * R * s.o_head) {
+        int h = (side ? from - queries : from) * H;
+        const int64_t head = H * s.o_head;
+        T* dst = s.out + t * s.o_token + (h + hsub) * s.o_head + sh.dim_of(0, 0);
+        for (int i = from; i < to; i += 2, h += 2 * H, dst += 2 * head) {
             float x[2][NV][E];
 #pragma unroll
             for (int u = 0; u < 2; ++u)
@@ -395,12 +410,13 @@ __global__ void __launch_bounds__(kThreads, NV == 1 ? 7 : 4) qk_rotate_kernel(co
             }
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
+                if (h + u * H >= s.heads) break;
                 if (full) sh.template turn<true>(x[u], p.half, xch);
                 else sh.template turn<false>(x[u], p.half, xch);
                 if (norm) scale_by(x[u], r[u]);
-                if (h + u * R < s.heads) {
+                if (is && h + u * H + hsub < s.heads) {
 #pragma unroll
-                    for (int k = 0; k < NV; ++k) L::store(dst + u * R * s.o_head + k * G * E, sh.n[k], x[u][k]);
+                    for (int k = 0; k < NV; ++k) L::store(dst + u * head + k * G * E, sh.n[k], x[u][k]);
                 }
             }
         }
@@ -409,7 +425,7 @@ __global__ void __launch_bounds__(kThreads, NV == 1 ? 7 : 4) qk_rotate_kernel(co
 
 // The same backwards. The warps go through units of a token's part in turn; the weights' gradients are summed in registers, then
 // over the block's slots in order, then (rotate_sums_kernel) over the blocks in order.
-template <typename T, int G, int NV, int MODE, bool FAST>
+template <typename T, int G, int NV, int MODE, bool FAST, int A>
 __global__ void __launch_bounds__(kGradThreads, grad_blocks_of<T>(NV)) qk_rotate_grad_kernel(const Rotate<T> p) {
     using L = Lane<T, FAST>;
     constexpr int E = L::E, R = 32 / G, kWarps = kGradThreads / 32, kSlots = kWarps * R;
@@ -417,10 +433,12 @@ __global__ void __launch_bounds__(kGradThreads, grad_blocks_of<T>(NV)) qk_rotate
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane / G;
     float* mem = smem + warp * warp_floats(MODE, G, p.half, p.dim);
     float2* table = reinterpret_cast<float2*>(mem);
-    float* xch = mem + 2 * p.half + sub * p.dim;
+    float* xch = mem + R * 2 * p.half + sub * p.dim;
     Share<T, G, NV, MODE> sh(lane % G, p.dim, p.half);
-    const int queries = looks_at<G>(p.s[0].heads), looks = queries + looks_at<G>(p.s[1].heads);
-    const int64_t units = p.tokens * p.parts, step = static_cast<int64_t>(gridDim.x) * kWarps;
+    constexpr int H = R / A;   // rows of a token in a look
+    const int hsub = sub % H, tsub = sub / H;
+    const int queries = looks_at(p.s[0].heads, H), looks = queries + looks_at(p.s[1].heads, H);
+    const int64_t units = (p.tokens + A - 1) / A * p.parts, step = static_cast<int64_t>(gridDim.x) * kWarps;
     const bool full = 2 * p.half == p.dim;
     pdl_wait();
     pdl_launch_dependents();
@@ -438,25 +456,26 @@ __global__ void __launch_bounds__(kGradThreads, grad_blocks_of<T>(NV)) qk_rotate
     int next = 0, next_last = 0;
     auto enter = [&] {
         if (next_unit >= units) return;
-        next_t = p.parts == 1 ? next_unit : next_unit / p.parts;
-        next = static_cast<int>(next_unit - next_t * p.parts) * p.part;
+        const int64_t group = p.parts == 1 ? next_unit : next_unit / p.parts;
+        next_t = group * A + tsub;
+        next = static_cast<int>(next_unit - group * p.parts) * p.part;
         next_last = min(next + p.part, looks);
     };
     uint4 rx[2][NV], rg[2][NV];
     auto fetch = [&] {
         if (next_unit >= units) return;
-        const int side = next >= queries, h0 = (side ? next - queries : next) * R + sub;
+        const int side = next >= queries, h0 = (side ? next - queries : next) * H + hsub;
         const Rows<T>& s = p.s[side];
         const T* gy = s.gy + next_t * s.g_token + h0 * s.g_head + sh.dim_of(0, 0);
         const T* x = s.x + next_t * s.x_token + h0 * s.x_head + sh.dim_of(0, 0);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const bool here = h0 + u * R < s.heads;
+            const bool here = next_t < p.tokens && h0 + u * H < s.heads;
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
                 rx[u][k] = rg[u][k] = make_uint4(0, 0, 0, 0);
-                if (here) rg[u][k] = L::load(gy + u * R * s.g_head + k * G * E, sh.n[k]);
-                if (here && s.w) rx[u][k] = L::load(x + u * R * s.x_head + k * G * E, sh.n[k]);
+                if (here) rg[u][k] = L::load(gy + u * H * s.g_head + k * G * E, sh.n[k]);
+                if (here && s.w) rx[u][k] = L::load(x + u * H * s.x_head + k * G * E, sh.n[k]);
             }
         }
         next += 2;
@@ -469,10 +488,10 @@ __global__ void __launch_bounds__(kGradThreads, grad_blocks_of<T>(NV)) qk_rotate
     enter();
     fetch();
     for (; unit < units; unit += step) {
-        const int64_t t = p.parts == 1 ? unit : unit / p.parts;
-        const int first = static_cast<int>(unit - t * p.parts) * p.part, last = min(first + p.part, looks);
-        const bool is = fill_table(p, t, table);
-        sh.template take<true>(table, p.half, w, xch);
+        const int64_t group = p.parts == 1 ? unit : unit / p.parts, t = group * A + tsub;
+        const int first = static_cast<int>(unit - group * p.parts) * p.part, last = min(first + p.part, looks);
+        const bool is = fill_tables<A>(p, group * A, table) >> tsub & 1;
+        sh.template take<true>(table + tsub * p.half, p.half, w, xch);
         for (int i = first; i < last; i += 2) {
             float g[2][NV][E], x[2][NV][E];
 #pragma unroll
@@ -483,7 +502,7 @@ __global__ void __launch_bounds__(kGradThreads, grad_blocks_of<T>(NV)) qk_rotate
                     L::unpack(rx[u][k], x[u][k]);
                 }
             fetch();
-            const int side = i >= queries, h0 = (side ? i - queries : i) * R + sub;
+            const int side = i >= queries, h0 = (side ? i - queries : i) * H + hsub;
             const Rows<T>& s = p.s[side];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
@@ -510,7 +529,7 @@ __global__ void __launch_bounds__(kGradThreads, grad_blocks_of<T>(NV)) qk_rotate
                     sum[u] = row_sum<G>(sum[u]);
                     dot[u] = row_sum<G>(dot[u]);
                     const float r = rsqrtf(fmaf(sum[u], over, p.eps)), f = dot[u] * over * r * r;
-                    if (is) {
+                    if (is) {   // rows that are not there count as 0
                         if (side) add_scaled(gw[1], xg, r);
                         else add_scaled(gw[0], xg, r);
                     }
@@ -522,9 +541,9 @@ __global__ void __launch_bounds__(kGradThreads, grad_blocks_of<T>(NV)) qk_rotate
             T* dst = s.out + t * s.o_token + h0 * s.o_head + sh.dim_of(0, 0);
 #pragma unroll
             for (int u = 0; u < 2; ++u)
-                if (is && h0 + u * R < s.heads) {
+                if (is && h0 + u * H < s.heads) {
 #pragma unroll
-                    for (int k = 0; k < NV; ++k) L::store(dst + u * R * s.o_head + k * G * E, sh.n[k], g[u][k]);
+                    for (int k = 0; k < NV; ++k) L::store(dst + u * H * s.o_head + k * G * E, sh.n[k], g[u][k]);
                 }
         }
     }
@@ -566,18 +585,19 @@ __global__ void __launch_bounds__(1024) rotate_sums_kernel(const float* __restri
 
 int64_t grad_blocks(int64_t tokens) { return std::min<int64_t>(tokens, kMaxBlocks); }
 
-template <typename T, int G, int NV, int MODE, bool FAST>
+template <typename T, int G, int NV, int MODE, bool FAST, int A>
 kq_status launch(Rotate<T>& p, bool back, float* gqw, float* gkw, cudaStream_t stream) {
     constexpr int R = 32 / G;
-    const int64_t looks = looks_at<G>(p.s[0].heads) + looks_at<G>(p.s[1].heads), warps = static_cast<int64_t>(num_sms()) * 16;
+    const int64_t looks = looks_at(p.s[0].heads, R / A) + looks_at(p.s[1].heads, R / A), groups = cdiv(p.tokens, A);
+    const int64_t warps = static_cast<int64_t>(num_sms()) * 16;
     // a token's rows go to several warps where tokens are few
-    const int64_t parts = std::max<int64_t>(1, std::min(looks / 2, warps / p.tokens));
+    const int64_t parts = std::max<int64_t>(1, std::min(looks / 2, warps / groups));
     p.part = static_cast<int32_t>(cdiv(looks / 2, parts) * 2);
     p.parts = static_cast<int32_t>(cdiv(looks, p.part));
     const size_t floats = warp_floats(MODE, G, p.half, p.dim);
-    const int64_t units = p.tokens * p.parts;
+    const int64_t units = groups * p.parts;
     if (!back) {
-        KQ_CUDA(launch_after(qk_rotate_kernel<T, G, NV, MODE, FAST>, dim3(static_cast<unsigned>(cdiv(units, kThreads / 32))),
+        KQ_CUDA(launch_after(qk_rotate_kernel<T, G, NV, MODE, FAST, A>, dim3(static_cast<unsigned>(cdiv(units, kThreads / 32))),
                              dim3(kThreads), kThreads / 32 * floats * sizeof(float), stream, p));
         count_launch();
         return KQ_OK;
@@ -587,7 +607,7 @@ kq_status launch(Rotate<T>& p, bool back, float* gqw, float* gkw, cudaStream_t s
     const int blocks = static_cast<int>(std::min({grad_blocks(p.tokens), cdiv(units, kWarps), fit}));
     size_t smem = kWarps * floats * sizeof(float);
     if (p.sums) smem = std::max(smem, kWarps * R * p.dim * sizeof(float));
-    KQ_CUDA(launch_after(qk_rotate_grad_kernel<T, G, NV, MODE, FAST>, dim3(blocks), dim3(kGradThreads), smem, stream, p));
+    KQ_CUDA(launch_after(qk_rotate_grad_kernel<T, G, NV, MODE, FAST, A>, dim3(blocks), dim3(kGradThreads), smem, stream, p));
     count_launch();
     if (p.sums) {
         KQ_CUDA(launch_after(rotate_sums_kernel, dim3(static_cast<unsigned>(cdiv(p.dim, 32)), 2), dim3(1024), 0, stream,
@@ -599,13 +619,20 @@ kq_status launch(Rotate<T>& p, bool back, float* gqw, float* gkw, cudaStream_t s
 
 template <typename T, int G, int NV>
 kq_status launch_mode(Rotate<T>& p, bool fast, bool pairs, bool back, float* gqw, float* gkw, cudaStream_t stream) {
+    constexpr int R = 32 / G;
+    // A token to a warp where it has many rows (32768 tokens of 40 bf16 rows of 128: 119 us, two tokens abreast 123; 16384
+    // backwards 105 and 107), else a token to each group of lanes, which are all at work whatever the rows (30000 tokens of 16 rows: 48
+    // and 46 us, backwards 80 and 78; 52708 of 4 + 2 rows of 64: 45 and 19, 75 and 38; of 1 + 1 of 128: 47 and 26, 78 and 43).
+    const bool one = p.s[0].heads + p.s[1].heads >= kManyRows;
     if (!fast) {   // rows of any alignment: one value at a time, partners through shared memory where they are not neighbours
-        return pairs ? launch<T, G, NV, kPairs, false>(p, back, gqw, gkw, stream)
-                     : launch<T, G, NV, kHalvesOdd, false>(p, back, gqw, gkw, stream);
+        return pairs ? launch<T, G, NV, kPairs, false, R>(p, back, gqw, gkw, stream)
+                     : launch<T, G, NV, kHalvesOdd, false, R>(p, back, gqw, gkw, stream);
     }
-    if (pairs) return launch<T, G, NV, kPairs, true>(p, back, gqw, gkw, stream);
-    if (p.half % (16 / sizeof(T)) == 0) return launch<T, G, NV, kHalves, true>(p, back, gqw, gkw, stream);
-    return launch<T, G, NV, kHalvesOdd, true>(p, back, gqw, gkw, stream);
+    if (pairs)
+        return one ? launch<T, G, NV, kPairs, true, 1>(p, back, gqw, gkw, stream) : launch<T, G, NV, kPairs, true, R>(p, back, gqw, gkw, stream);
+    if (p.half % (16 / sizeof(T)) == 0)
+        return one ? launch<T, G, NV, kHalves, true, 1>(p, back, gqw, gkw, stream) : launch<T, G, NV, kHalves, true, R>(p, back, gqw, gkw, stream);
+    return launch<T, G, NV, kHalvesOdd, true, R>(p, back, gqw, gkw, stream);
 }
 kq_status launch_dim(Rotate<__nv_bfloat16>& p, bool fast, bool pairs, bool back, float* gqw, float* gkw, cudaStream_t stream) {
     if (p.dim <= 64) return launch_mode<__nv_bfloat16, 8, 1>(p, fast, pairs, back, gqw, gkw, stream);

@@ -64,7 +64,9 @@ CASES = [(1, 1, 1, 128, 128, False, True), (5, 4, 1, 64, 64, False, True), (3, 2
          (7, 3, 1, 96, 24, True, True), (130, 8, 2, 128, 64, False, False), (9, 7, 1, 256, 256, False, True),
          (9, 7, 1, 256, 34, False, True), (4, 5, 5, 65, 64, False, True), (4, 2, 1, 33, 22, True, False),
          (6, 3, 0, 128, 128, True, True), (2, 2, 1, 2, 2, False, True), (3, 2, 1, 100, 0, False, True),
-         (1, 70, 9, 128, 128, False, True), (1000, 8, 4, 128, 128, False, True), (700, 3, 1, 112, 66, False, True)]
+         (1, 70, 9, 128, 128, False, True), (1000, 8, 4, 128, 128, False, True), (700, 3, 1, 112, 66, False, True),
+         (20001, 1, 1, 64, 16, True, True), (10003, 4, 2, 64, 64, False, True), (20003, 1, 0, 128, 34, False, False),
+         (19999, 1, 1, 256, 256, False, True)]
 
 
 @pytest.mark.parametrize("T,hq,hk,dim,rot,interleaved,norm", CASES)
@@ -126,6 +128,32 @@ def test_in_place_and_positions_of_sequences_and_tokens_of_none():
                           gq_weight=sums[1], ws=ws)
     assert all(torch.equal(x, y) for x, y in zip(*outs))
     assert torch.allclose(sums[0], sums[1], rtol=1e-5, atol=1e-5)   # 2^-17 of at most 27 terms of size 10, in another split
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_sequences_over_many_tokens_of_few_heads(dtype):
+    """Several tokens to a warp, the last of them of no sequence: as by positions, and not written."""
+    dt = TYPES[dtype]
+    g = torch.Generator(DEV).manual_seed(2)
+    counts = [7000, 0, 1, 9001, 4000]
+    T, end = 20011, sum(counts)
+    start = torch.tensor([0] + counts, device=DEV).cumsum(0).to(torch.int32)
+    first = torch.tensor([5, 1, 100000, 0, 77], dtype=torch.int32, device=DEV)
+    pos = torch.cat([torch.arange(f, f + n) for f, n in zip(first.tolist(), counts)] + [torch.zeros(T - end)]).to(DEV).to(torch.int32)
+    q, k, gq, gk = (torch.randn(T, h, 64, device=DEV, generator=g).to(dt) for h in (1, 1, 1, 1))
+    w = torch.rand(64, device=DEV, generator=g).to(dt)
+    freq = K().kq_rotation_freq(_theta(32))
+    ws = torch.empty(K().kq_qk_rotate_grad_workspace(q), dtype=torch.uint8, device=DEV)
+    got = []
+    for how in (dict(pos=pos[:end]), dict(start=start, first=first)):
+        n = end if "pos" in how else T
+        outs = [torch.full((T, 1, 64), 7.0, dtype=dt, device=DEV) for _ in range(4)] + [torch.empty(64, device=DEV) for _ in range(2)]
+        K().kq_qk_rotate(q[:n], k[:n], outs[0][:n], outs[1][:n], freq, q_weight=w, k_weight=w, **how)
+        K().kq_qk_rotate_grad(q[:n], k[:n], gq[:n], gk[:n], outs[2][:n], outs[3][:n], freq, q_weight=w, k_weight=w, gq_weight=outs[4],
+                              gk_weight=outs[5], ws=ws, **how)
+        got.append(outs)
+    assert all(torch.equal(a, b) for a, b in zip(got[0][:4], got[1][:4])) and (got[1][0][end:] == 7).all()
+    assert all(torch.allclose(a, b, rtol=0, atol=2.0 ** -17 * 20000) for a, b in zip(got[0][4:], got[1][4:]))   # of about 16000 in all
 
 
 def test_no_positions_means_the_index():
