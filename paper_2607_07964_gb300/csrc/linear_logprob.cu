@@ -807,6 +807,20 @@ linear_thin_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant
     }
 }
 
+// What D of a token needs, for n tokens by 256 threads.
+__device__ __forceinline__ void fill_known(const Job& j, int n, int thread, float4* known, int* target) {
+    for (int t = thread; t < n; t += 256) {
+        const bool is = t < j.T;
+        const int64_t y = is ? j.target[t] : -1;
+        const bool scored = y >= 0 && y < j.V;
+        const float lse = is ? j.lse[t] : -INFINITY;
+        // a row of -infinity only, or none: p = 0 of every logit
+        known[t] = make_float4(lse == -INFINITY ? INFINITY : lse, scored ? j.g_logp[t] : 0.0f, is && j.g_entropy ? j.g_entropy[t] : 0.0f,
+                               is && j.g_entropy ? j.entropy[t] : 0.0f);
+        target[t] = scored && lse != -INFINITY ? static_cast<int>(y) : -1;
+    }
+}
+
 // ---- few rows, backwards. A CTA takes 128 rows of W at a time: their logits (the rows of W by N tokens), D, and the rows of gW:
 // D, rounded to bf16, goes to shared memory as the operand of D x, 128 columns of gW at a time, and to `delta` (a row of N tokens
 // for each row of W) for gx. One tile's products D x are issued between the next one's slabs, so that W's rows come in while gW's
@@ -874,18 +888,7 @@ linear_thin_grad_kernel(const __grid_constant__ CUtensorMap mx, const __grid_con
     }
     pdl_wait();
     pdl_launch_dependents();
-    if (threadIdx.x >= 64) {
-        for (int t = threadIdx.x - 64; t < N; t += 256) {
-            const bool is = t < j.T;
-            const int64_t y = is ? j.target[t] : -1;
-            const bool scored = y >= 0 && y < j.V;
-            const float lse = is ? j.lse[t] : -INFINITY;
-            // a row of -infinity only, or none: p = 0 of every logit
-            known[t] = make_float4(lse == -INFINITY ? INFINITY : lse, scored ? j.g_logp[t] : 0.0f, is && j.g_entropy ? j.g_entropy[t] : 0.0f,
-                                   is && j.g_entropy ? j.entropy[t] : 0.0f);
-            target[t] = scored && lse != -INFINITY ? static_cast<int>(y) : -1;
-        }
-    }
+    if (threadIdx.x >= 64) fill_known(j, N, threadIdx.x - 64, known, target);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -1090,6 +1093,202 @@ linear_thin_grad_kernel(const __grid_constant__ CUtensorMap mx, const __grid_con
     }
 }
 
+// ---- few rows and a small vocabulary: fewer tiles of W than SMs. A cluster takes a tile, its CTAs a share of d each; a CTA adds up
+// the shares of its part of the tile's rows, in their order, from what the others have put into its shared memory.
+// A CTA alone takes 0.28 us for each slab of a tile, whatever the other SMs do, so that a long d with few tiles is bound by one CTA:
+// 9 rows of 1900 x 6304 took 31 us and take 10.7 (24 MB, 4 us at the copy's rate), with both gradients 60 and 28.
+template <int N>
+struct Split {
+    static constexpr int kStage = Thin<N>::kStage, kBoxRows = Thin<N>::kBoxRows, kMail = N * (kThinRows + 8) * 4;
+    static constexpr uint32_t kColumns = Thin<N>::kColumns;
+    static constexpr int kFit = (226 * 1024 - kMail - N * 20 - 1024) / kStage, kStages = kFit < 10 ? kFit : 10;
+    static constexpr int kSmem = kStages * kStage + kMail + N * 20 + 1024;
+};
+
+template <int MAIN, int N>
+__global__ void __launch_bounds__(kThinThreads, 1)
+linear_split_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtensorMap mw, const __grid_constant__ Job j) {
+    using S = Split<N>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    float* mail = reinterpret_cast<float*>(smem + S::kStages * S::kStage);   // [shares][N][rows of this CTA and one]
+    float4* known = reinterpret_cast<float4*>(mail + N * (kThinRows + 8));    // of each token: log-sum, the gradients, entropy
+    int* target = reinterpret_cast<int*>(known + N);
+    __shared__ uint64_t full[S::kStages], empty[S::kStages], tfull[2], tempty[2], mma_done;
+    __shared__ uint32_t tmem_slot;
+    __shared__ volatile int abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S::kStages; ++s) {
+            mbar_init(&full[s], 1);
+            mbar_init(&empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(&tfull[b], 1);
+            mbar_init(&tempty[b], 8);
+        }
+        mbar_init(&mma_done, 1);
+        abort_flag = 0;
+        fence_mbar_init();
+    }
+    if (warp == 1) {
+        tmem_alloc(&tmem_slot, S::kColumns);
+        tmem_relinquish();
+    }
+    if (warp == 0 && lane == 0) {
+        tma_prefetch_desc(&mx);
+        tma_prefetch_desc(&mw);
+    }
+    pdl_wait();
+    pdl_launch_dependents();
+    if (MAIN == kDelta && threadIdx.x >= 64) fill_known(j, N, threadIdx.x - 64, known, target);
+    tc_fence_before();
+    __syncthreads();
+    cluster_barrier();   // every CTA's mail is there
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    const int shares = gridDim.x, share = blockIdx.x, tile = blockIdx.y, rows = kThinRows / shares;
+    const int each = (j.d_slabs + shares - 1) / shares, first = share * each, slabs = max(0, min(each, j.d_slabs - first));
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int k = 0;
+            for (; k < slabs; ++k) {
+                const int st = k % S::kStages, x = (first + k) * BK;
+                if (!held_wait(&empty[st], (static_cast<uint32_t>(k / S::kStages) & 1u) ^ 1u, &abort_flag)) break;
+                mbar_arrive_expect_tx(&full[st], S::kStage);
+                uint8_t* base = smem + st * S::kStage;
+                tma_load_2d(base, &mw, &full[st], x, tile * kThinRows);
+                tma_load_2d(base + kBox, &mw, &full[st], x, tile * kThinRows + 64);
+#pragma unroll
+                for (int i = 0; i < N / S::kBoxRows; ++i)
+                    tma_load_2d(base + 2 * kBox + i * S::kBoxRows * BK * 2, &mx, &full[st], x, i * S::kBoxRows);
+            }
+            for (int i = (k > S::kStages ? k - S::kStages : 0); i < k; ++i)   // whatever is under way has landed
+                wait_quiet(&full[i % S::kStages], static_cast<uint32_t>(i / S::kStages) & 1u);
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            constexpr uint32_t idesc = idesc_bf16_mn_major(kThinRows, N) & ~(3u << 15);
+            int k = 0, cc = 0;
+            bool ok = true;
+            for (int s0 = 0; s0 < slabs && ok; s0 += kDrainThin, ++cc) {
+                const int buf = cc & 1;
+                if (!held_wait(&tempty[buf], ((static_cast<uint32_t>(cc) >> 1) & 1u) ^ 1u, &abort_flag)) break;
+                tc_fence_after();
+                for (const int s1 = min(slabs, s0 + kDrainThin); k < s1; ++k) {
+                    const int st = k % S::kStages;
+                    ok = held_wait(&full[st], static_cast<uint32_t>(k / S::kStages) & 1u, &abort_flag);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t sa = smem_u32(smem + st * S::kStage), sb = sa + 2 * kBox;
+#pragma unroll
+                    for (int q = 0; q < BK / 16; ++q)
+                        tc_mma_f16(tmem + buf * N, smem_desc_sw128(sa + q * 32, 16, 1024), smem_desc_sw128(sb + q * 32, 16, 1024), idesc,
+                                   (k > s0 || q > 0) ? 1u : 0u);
+                    tc_commit(&empty[st]);
+                }
+                if (ok) tc_commit(&tfull[buf]);
+            }
+            tc_commit(&mma_done);
+            wait_quiet(&mma_done, 0);
+        }
+    } else {
+        constexpr int kHalf = N / 2;
+        const int q = warp & 3, h = (warp - 2) >> 2, row = q * 32 + lane;
+        float x[kHalf];
+#pragma unroll
+        for (int i = 0; i < kHalf; ++i) x[i] = 0.0f;
+        for (int s0 = 0, cc = 0; s0 < slabs; s0 += kDrainThin, ++cc) {
+            const int buf = cc & 1;
+            const bool is = held_wait(&tfull[buf], (static_cast<uint32_t>(cc) >> 1) & 1u, &abort_flag);
+            if (!__all_sync(0xffffffffu, is)) break;
+            tc_fence_after();
+#pragma unroll
+            for (int p = 0; p < kHalf / 16; ++p) {
+                float v[16];
+                tmem_ld16(tmem + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(buf * N + h * kHalf + p * 16), v);
+                tc_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[p * 16 + i] += v[i];
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&tempty[buf]);
+        }
+        // to the CTA that has this row of W
+        const int owner = row / rows;
+        const uint32_t at = mapa_shared(smem_u32(mail + (share * N + h * kHalf) * (rows + 1) + row % rows), owner);
+#pragma unroll
+        for (int i = 0; i < kHalf; ++i)
+            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + static_cast<uint32_t>(i * (rows + 1)) * 4), "f"(x[i]) : "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_barrier();
+    const int64_t v0 = static_cast<int64_t>(tile) * kThinRows + share * rows;
+    if (threadIdx.x >= 64) {
+        const int id = threadIdx.x - 64, pitch = rows + 1;
+        // the logits, in the place of the first share's; past the vocabulary: cannot occur
+        for (int i = id; i < j.T * rows; i += 256) {
+            const int token = i / rows, row = i - token * rows;
+            float z = 0.0f;
+            for (int o = 0; o < shares; ++o) z += mail[(o * N + token) * pitch + row];
+            mail[token * pitch + row] = v0 + row < j.V ? z : -INFINITY;
+        }
+        named_all(true);
+        if (MAIN == kScore) {
+            constexpr int kShare = N == 32 ? 8 : N == 64 ? 4 : 2;   // threads of a token, which take its rows in turn
+            const int token = id / kShare, from = id % kShare;
+            const bool mine = token < N && token < j.T;
+            Sums sums = {-INFINITY, 0.0f, 0.0f};
+            if (mine) {
+                const int64_t y = j.target[token] - v0;
+                const float* z = mail + token * pitch;
+                float m = -INFINITY;
+                for (int i = from; i < rows; i += kShare) {
+                    m = max_nan(m, z[i]);
+                    if (y == i && v0 + i < j.V) j.zt[token] = z[i];
+                }
+                sums.m = m;
+                const float ref = m == -INFINITY ? 0.0f : m;
+                for (int i = from; i < rows; i += kShare) {
+                    const float u = fmaxf((z[i] - ref) * kLog2e, kNone), e = ex2(u);
+                    sums.z += e;
+                    sums.s = fmaf(e, u, sums.s);
+                }
+            }
+            __syncwarp();
+#pragma unroll
+            for (int o = 1; o < kShare; o <<= 1)
+                sums.join(__shfl_xor_sync(0xffffffffu, sums.m, o), __shfl_xor_sync(0xffffffffu, sums.z, o),
+                          __shfl_xor_sync(0xffffffffu, sums.s, o));
+            if (mine && from == 0 && KQ_IN_RANGE(tile * shares + share, j.parts))
+                j.part[static_cast<int64_t>(token) * j.parts + tile * shares + share] = make_float4(sums.m, sums.z, sums.s, 0.0f);
+        } else {
+            for (int i = id; i < rows * (N / 8); i += 256) {
+                const int t0 = i / rows * 8, row = i - i / rows * rows;
+                const int64_t v = v0 + row;
+                float d[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float4 a = known[t0 + e];
+                    d[e] = t0 + e < j.T && v < j.V ? delta_of(mail[(t0 + e) * pitch + row], a.x, a.y, a.z, a.w) : 0.0f;
+                    if (target[t0 + e] == v) d[e] += a.y;
+                }
+                if (KQ_IN_RANGE(v, j.ld_delta))
+                    *reinterpret_cast<uint4*>(j.delta + v * N + t0) =
+                        make_uint4(pack_bf16(d[0], d[1]), pack_bf16(d[2], d[3]), pack_bf16(d[4], d[5]), pack_bf16(d[6], d[7]));
+            }
+        }
+    }
+    if (abort_flag && threadIdx.x == 0) record_error(j.info, -KQ_ERR_TIMEOUT);
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, S::kColumns);
+    }
+}
+
 // Joins the parts of a row: a block to a row.
 __global__ void __launch_bounds__(128) linear_join_kernel(const Job j, float* __restrict__ logp, float* __restrict__ entropy,
                                                           float* __restrict__ lse) {
@@ -1262,9 +1461,47 @@ int64_t thin_blocks(int64_t V) { return std::min<int64_t>(cdiv(V, kThinRows), nu
 int thin_tokens(int64_t T) { return T <= 32 ? 32 : T <= 64 ? 64 : T <= 96 ? 96 : 128; }
 int thin_box_rows(int n) { return n <= 64 ? n : n / 2; }
 
+// The shares of d that a tile of W is cut into: as many as there are SMs for (152 SMs hold 76 clusters of 2 such CTAs, 36 of 4 or 15
+// of 8; with one cluster more, 38 of 4, 120 rows of 4864 x 2048 took 25 us instead of 16). Sums between CTAs cost as much as some
+// slabs, more for more tokens, so a share has to leave that many to the others. Scores, whole and in shares: 12 x 2583 x 3040 18 and 10
+// us, 100 x 3900 x 4096 25 and 16, 30 x 8000 x 2048 14 and 13, but 60 x 8000 x 2048 14.8 and 15.1, 100 x 8000 x 2048 16 and 19, 20 x
+// 1000 x 512 7.0 and 8.6. D's kernel gains sooner (all of a gradient, 100 x 8000 x 2048: 46 and 42 us; 20 x 1000 x 512: 13.8 and 14.4).
+int split_shares(const Job& j, bool score) {
+    const int64_t tiles = cdiv(j.V, kThinRows);
+    int shares = 1;
+    while (shares < 8 && tiles * shares * 2 <= num_sms() - 8 * shares && j.d_slabs >= 8 * shares) shares *= 2;
+    return j.d_slabs - cdiv(j.d_slabs, shares) > (score ? thin_tokens(j.T) / 4 : 4) ? shares : 1;
+}
+template <int MAIN, int N>
+kq_status run_split(const Maps& m, Job& j, int shares, cudaStream_t stream) {
+    static std::atomic<uint64_t> done{0};
+    KQ_TRY(once_per_device(done, [] {
+        KQ_CUDA(cudaFuncSetAttribute(linear_split_kernel<MAIN, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, Split<N>::kSmem));
+        return KQ_OK;
+    }));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(shares), static_cast<unsigned>(cdiv(j.V, kThinRows)));
+    cfg.blockDim = dim3(kThinThreads);
+    cfg.dynamicSmemBytes = Split<N>::kSmem;
+    cfg.stream = stream;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = static_cast<unsigned>(shares);
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    j.parts = static_cast<int32_t>(cdiv(j.V, kThinRows) * shares);
+    KQ_CUDA(cudaLaunchKernelEx(&cfg, linear_split_kernel<MAIN, N>, m.x, m.w, static_cast<const Job>(j)));
+    count_launch();
+    return KQ_OK;
+}
+
 template <int N>
 kq_status run_thin_of(const Maps& m, Job& j, cudaStream_t stream) {
     static std::atomic<uint64_t> done{0};
+    if (const int shares = split_shares(j, true); shares > 1) return run_split<kScore, N>(m, j, shares, stream);
     j.parts = static_cast<int32_t>(thin_blocks(j.V));
     return run_thin_kernel(linear_thin_kernel<N>, Thin<N>::kSmem, done, j.parts, stream, m.x, m.w, j);
 }
@@ -1277,11 +1514,12 @@ kq_status run_thin(const Maps& m, Job& j, cudaStream_t stream) {
     }
 }
 template <int N>
-kq_status run_thin_grad_of(const Maps& m, const Job& j, cudaStream_t stream) {
+kq_status run_thin_grad_of(const Maps& m, Job& j, cudaStream_t stream) {
     static std::atomic<uint64_t> done{0};
+    if (const int shares = split_shares(j, false); shares > 1 && !j.gw) return run_split<kDelta, N>(m, j, shares, stream);
     return run_thin_kernel(linear_thin_grad_kernel<N>, ThinGrad<N>::kSmem, done, thin_blocks(j.V), stream, m.x, m.w, m.out_w, j);
 }
-kq_status run_thin_grad(const Maps& m, const Job& j, cudaStream_t stream) {
+kq_status run_thin_grad(const Maps& m, Job& j, cudaStream_t stream) {
     switch (thin_tokens(j.T)) {
         case 32: return run_thin_grad_of<32>(m, j, stream);
         case 64: return run_thin_grad_of<64>(m, j, stream);
@@ -1320,6 +1558,10 @@ Cut cut_of(int64_t T, int64_t V, int64_t d) {
     return c;
 }
 size_t al256(size_t b) { return (b + 255) & ~static_cast<size_t>(255); }
+// Parts of a row's sums: 64 columns of a tile, or the rows of W that a CTA has of one of few tiles.
+int64_t most_parts(int64_t T, int64_t V) {
+    return T <= kThinMost ? std::max(cdiv(V, 64), 8 * std::min<int64_t>(cdiv(V, kThinRows), 128)) : cdiv(V, 64);
+}
 
 kq_status check(const char* who, const uint16_t* x, int64_t T, int64_t d, int64_t ldx, const uint16_t* w, int64_t V, int64_t ldw,
                 const int64_t* target) {
@@ -1345,7 +1587,7 @@ using namespace kq;
 
 extern "C" size_t kq_linear_logprobs_workspace(int64_t T, int64_t V, int64_t d) {
     if (T < 1 || V < 1 || d < 1) return 0;
-    return al256(static_cast<size_t>(T) * cdiv(V, 64) * sizeof(float4)) + al256(T * sizeof(float));
+    return al256(static_cast<size_t>(T) * most_parts(T, V) * sizeof(float4)) + al256(T * sizeof(float));
 }
 
 extern "C" kq_status kq_linear_logprobs(const uint16_t* x, int64_t T, int64_t d, int64_t ldx, const uint16_t* w, int64_t V, int64_t ldw,
@@ -1374,7 +1616,7 @@ extern "C" kq_status kq_linear_logprobs(const uint16_t* x, int64_t T, int64_t d,
     j.target = target;
     j.parts = static_cast<int32_t>(cdiv(V, 64));
     j.part = static_cast<float4*>(ws);
-    j.zt = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + al256(static_cast<size_t>(T) * j.parts * sizeof(float4)));
+    j.zt = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + al256(static_cast<size_t>(T) * most_parts(T, V) * sizeof(float4)));
     j.m_main = static_cast<int32_t>(cdiv(T, BM));
     j.n_main = static_cast<int32_t>(cdiv(V, BN));
     j.tiles = j.m_main * j.n_main;

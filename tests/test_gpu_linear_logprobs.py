@@ -73,7 +73,8 @@ def _score(x, w, y, info=None, poison=255):
 
 SIZES = [(1, 1, 8), (1, 1000, 64), (2, 127, 72), (3, 128, 520), (5, 129, 8), (17, 4097, 264), (127, 300, 1000), (128, 513, 512),
          (129, 257, 1024), (256, 255, 136), (257, 1025, 2056), (300, 20000, 128), (1000, 5003, 320), (4100, 700, 64), (8, 33000, 4096),
-         (33, 10241, 72), (64, 20000, 136), (100, 12345, 328), (90, 11000, 520), (10, 10240, 8)]
+         (33, 10241, 72), (64, 20000, 136), (100, 12345, 328), (90, 11000, 520), (10, 10240, 8), (1, 1000, 4096),
+         (33, 2000, 2056), (96, 5000, 2800), (70, 9000, 1032), (128, 130, 6000), (40, 9729, 1024)]
 
 
 @pytest.mark.parametrize("T,V,d", SIZES)
@@ -174,8 +175,9 @@ def test_the_gradient_is_that_of_the_log_probabilities():
     assert ((got - diff).abs() <= 2.0 ** -6 * (step.abs() * gx.double().abs()).sum(1) + z ** 3 + 1e-3).all()
 
 
-def test_targets_out_of_range_infinities_and_nan():
-    x, w, y = _case(6, 300, 64)
+@pytest.mark.parametrize("d", [64, 2056])
+def test_targets_out_of_range_infinities_and_nan(d):
+    x, w, y = _case(6, 300, d)
     y = torch.tensor([3, -1, 300, 7, 5, 2 ** 40], device=DEV)
     x[3, 5], x[4, 0] = float("nan"), float("inf")
     info = torch.zeros(1, dtype=torch.int32, device=DEV)
@@ -192,8 +194,9 @@ def test_targets_out_of_range_infinities_and_nan():
     assert gx[0].any() and not gx[1:].any() and torch.isfinite(gw).all()
 
 
-def test_logits_of_a_huge_size():
-    x, w, y = _case(4, 500, 64)
+@pytest.mark.parametrize("d", [64, 2056])
+def test_logits_of_a_huge_size(d):
+    x, w, y = _case(4, 500, d)
     big = (x.float() * 2.0 ** 60).bfloat16(), (w.float() * 2.0 ** 40).bfloat16()
     logp, ent, ls = _score(*big, y.clamp(min=0))
     z = big[0].double() @ big[1].double().T

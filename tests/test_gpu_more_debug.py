@@ -45,7 +45,7 @@ for heads, dim, group, page, window, sink, dtype in ((2, 128, 4, 64, 100, 4, tor
         out += [c.attend(rand(T, heads * group, dim).to(dtype), start, lse=lse, window=window, sink=sink), lse]
     c.check()
     res[f"window {heads} {dim}"] = [digest(t) for t in out]
-for T, V, d in ((1, 1, 8), (5, 1001, 72), (90, 5003, 320), (128, 129, 1000), (129, 700, 64), (1000, 3001, 264), (40, 12001, 136)):
+for T, V, d in ((1, 1, 8), (5, 1001, 72), (90, 5003, 320), (128, 129, 1000), (129, 700, 64), (1000, 3001, 264), (40, 12001, 136), (20, 1000, 2048), (90, 3000, 1032)):
     x, w = rand(T, d).bfloat16(), (rand(V, d) / d ** 0.5).bfloat16()
     y = torch.arange(T, device="cuda") % (V + 1) - 1
     logp, h, lse = score_hidden(x, w, y)

@@ -71,7 +71,8 @@ def test_window(heads, group, dim, page, window, sink, dtype):
 
 
 @pytest.mark.parametrize("T,V,d", [(1, 1, 8), (2, 200, 72), (33, 1000, 264), (96, 4097, 136), (128, 129, 1000), (129, 257, 64), (700, 3001, 520),
-                                   (1, 10241, 8), (96, 12001, 136), (128, 20000, 264)])
+                                   (1, 10241, 8), (96, 12001, 136), (128, 20000, 264),
+                                   (1, 1000, 4096), (40, 2001, 2056), (100, 4000, 1032)])
 def test_linear(T, V, d):
     new = Guarded()
     x, w = torch.randn(T, d, device=DEV).bfloat16(), (torch.randn(V, d, device=DEV) / d ** 0.5).bfloat16()
