@@ -473,7 +473,10 @@ __global__ void __launch_bounds__(kGradThreads, grad_blocks_of<T>(NV)) qk_rotate
             const bool here = next_t < p.tokens && h0 + u * H < s.heads;
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                rx[u][k] = rg[u][k] = make_uint4(0, 0, 0, 0);
+                // a row that is not there: a gradient of 0, of a row of ones, whose r is finite
+                constexpr uint32_t kOne = sizeof(T) == 4 ? 0x3F800000u : 0x3F803F80u;
+                rx[u][k] = make_uint4(kOne, kOne, kOne, kOne);
+                rg[u][k] = make_uint4(0, 0, 0, 0);
                 if (here) rg[u][k] = L::load(gy + u * H * s.g_head + k * G * E, sh.n[k]);
                 if (here && s.w) rx[u][k] = L::load(x + u * H * s.x_head + k * G * E, sh.n[k]);
             }

@@ -191,6 +191,31 @@ def test_rows_of_zeros_and_no_tokens():
     assert not g.any()
 
 
+@pytest.mark.parametrize("T,hq,hk", [(5, 3, 1), (3, 9, 5), (9001, 1, 1), (700, 33, 4)])
+@pytest.mark.parametrize("dim", [64, 128, 200])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_norms_without_eps(T, hq, hk, dim, dtype):
+    """Heads that fill no whole number of a warp's rows: what is not there adds nothing, though its norm would be infinite."""
+    rng = np.random.default_rng(T + dim)
+    dt = TYPES[dtype]
+    q, gq = (_rows(rng, T, hq, dim, dt, "whole") for _ in range(2))
+    k, gk = (_rows(rng, T, hk, dim, dt, "whole") for _ in range(2))
+    w = torch.from_numpy(1 + 0.3 * rng.standard_normal(dim)).to(DEV).to(dt)
+    theta = _theta(dim // 2)
+    freq, angle = K().kq_rotation_freq(theta), ref.angles(np.arange(T), ref.fractions(theta))
+    out, back = ([torch.empty_like(t) for t in (q, k)] for _ in range(2))
+    sums = [torch.empty(dim, device=DEV) for _ in range(2)]
+    ws = torch.empty(K().kq_qk_rotate_grad_workspace(gq), dtype=torch.uint8, device=DEV)
+    K().kq_qk_rotate(q, k, *out, freq, q_weight=w, k_weight=w, eps=0.0)
+    K().kq_qk_rotate_grad(q, k, gq, gk, *back, freq, q_weight=w, k_weight=w, eps=0.0, gq_weight=sums[0], gk_weight=sums[1], ws=ws)
+    for x, g, o, b, s in ((q, gq, out[0], back[0], sums[0]), (k, gk, out[1], back[1], sums[1])):
+        y, size = ref.forward(np64(x), np64(w), 0.0, angle, dim, False, 1.0)
+        _close(o, y, size, dt, 2.0 ** -19)
+        gx, size, gw, wsize = ref.backward(np64(x), np64(w), 0.0, np64(g), angle, dim, False, 1.0)
+        _close(b, gx, size, dt, 2.0 ** -18)
+        _close(s, gw, wsize, torch.float32, 2.0 ** -16)
+
+
 def test_gradient_matches_differences_of_the_kernel():
     """In float32 along a direction v of size 1 an element: forward errors of 2^-19 of about 2 a value, over 2 e = 2^-4, summed
     over n values with signs of their own, against the difference's e^2 / 6 times the third derivative (below 20)."""
