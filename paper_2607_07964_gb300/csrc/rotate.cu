@@ -731,6 +731,10 @@ kq_status check(const char* who, const kq_rotation* r, int dtype, int64_t T, int
             set_error("%s: inputs and outputs must have the same heads, at most 65535", who);
             return KQ_ERR_INVALID_ARG;
         }
+        if ((out[i]->token_stride == 0 && T > 1) || (out[i]->head_stride == 0 && out[i]->heads > 1)) {
+            set_error("%s: rows of an output must not share their place", who);
+            return KQ_ERR_INVALID_ARG;
+        }
         if (w[i] && (!(eps >= 0.0f) || !(eps - eps == 0.0f) || (reinterpret_cast<uintptr_t>(w[i]) & (es - 1)))) {
             set_error("%s: norms need eps >= 0 and weights aligned to their type", who);
             return KQ_ERR_INVALID_ARG;

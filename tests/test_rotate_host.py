@@ -84,6 +84,7 @@ def test_arguments_are_refused_on_the_host(K):
                                                   dict(scale=float("inf")), dict(start=256), dict(first=256),
                                                   dict(start=256, first=256, batch=1), dict(pos=None, start=256, first=256, batch=0))]
     cases += [(i, _heads(K, **o), 1) for i in (4, 6) for o in (dict(data=None), dict(data=257), dict(heads=3), dict(heads=0))]
+    cases += [(i, _heads(K, **o), 1) for i in (6, 7) for o in (dict(token_stride=0), dict(head_stride=0))]   # rows in one place
     for at, value, status in cases:
         args = list(good)
         args[at] = value
