@@ -224,7 +224,8 @@ class Rotation:
     def grad(self, q, k, gq, gk, **positions):
         """(gradients of the weights, of queries and of keys, None without weights) for q, k as they were before the rotation; gq, gk,
         the gradients of what it made of them, become those of q and k in place."""
-        sums = [None if self.args[n] is None else torch.empty(gq.shape[2], device=gq.device) for n in ("q_weight", "k_weight")]
+        sums = [None if g is None or self.args[n] is None else torch.empty(gq.shape[2], device=gq.device)
+                for n, g in (("q_weight", gq), ("k_weight", gk))]
         ws = torch.empty(kq.kq_qk_rotate_grad_workspace(gq), dtype=torch.uint8, device=gq.device) if any(
             s is not None for s in sums) else None
         kq.kq_qk_rotate_grad(q, k, gq, gk, gq, gk, self.freq, gq_weight=sums[0], gk_weight=sums[1], ws=ws, **positions, **self.args)

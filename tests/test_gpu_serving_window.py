@@ -156,6 +156,15 @@ def test_rotation_gradient_in_place():
         assert np.all(np.abs(s.double().cpu().numpy() - gw) <= 2.0 ** -16 * wsize)
     r = Rotation(theta, scale)
     assert r.grad(None, None, gq, gk, pos=pos) == (None, None)
+    # queries alone, where the keys have a norm too
+    r = Rotation(theta, scale, q_weight=w, k_weight=w)
+    a, b = q.clone(), torch.empty_like(q)
+    r(a, None, pos=pos)
+    r(b.copy_(q), k.clone(), pos=pos)
+    assert torch.equal(a, b)
+    one, two = gq.clone(), gq.clone()
+    sums, both = r.grad(q, None, one, None, pos=pos), r.grad(q, k, two, gk, pos=pos)
+    assert sums[1] is None and torch.equal(one, two) and torch.allclose(sums[0], both[0], rtol=1e-5, atol=1e-5)   # 20 terms, another split
 
 
 def test_example_with_a_window_decodes_and_scores():
