@@ -603,7 +603,7 @@ KQ_API kq_status kq_token_logprobs_grad(const void* logits, int dtype, int64_t T
  *
  * kq_linear_logprobs: kq_token_logprobs's logp, entropy and lse (entropy, lse nullable) for the logits z = x W^T,
  *   x [T][d] and W [V][d] bf16 (row strides ldx, ldw; 16-byte aligned, d and the strides multiples of 8). Products are
- *   exact, sums fp32: the tensor cores' over 512 of d, then in registers, so a logit is off by 2^-18 of the
+ *   exact, sums fp32: the tensor cores' over 1024 of d at most, then in registers, so a logit is off by 2^-17 of the
  *   sum of its products' sizes at most (2^-22 is ordinary). target as there: a negative one is not scored, one >= V recorded in info with logp = NaN. A row
  *   with a NaN or +infinite logit has NaN results. T <= KQ_LINEAR_MAX_T, V <= 2^20, d <= 65536.
  *   ws: kq_linear_logprobs_workspace(T, V, d) bytes, 256-byte aligned.
@@ -614,7 +614,7 @@ KQ_API kq_status kq_token_logprobs_grad(const void* logits, int dtype, int64_t T
  *   A row with a negative target has no g_logp part; a target >= V is recorded in info, its row's g_logp part left
  *   out. gx and gw must not overlap x, W or each other. Results do not depend on the order in which blocks run.
  *   ws: kq_linear_logprobs_grad_workspace(T, V, d) bytes, 256-byte aligned (2 pieces of logits' gradients of about
- *   2^25 values, fp32 gx).
+ *   2^26 values, or all of up to 128 rows, and fp32 gx).
  * info (nullable): also -KQ_ERR_TIMEOUT where a kernel gave up a wait.
  * ---------------------------------------------------------------------------------- */
 #define KQ_LINEAR_MAX_T (1 << 24)

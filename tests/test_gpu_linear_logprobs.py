@@ -1,8 +1,8 @@
 """GPU checks of kq_linear_logprobs and its gradient against 64 bits.
 
-Bounds. Products of bf16 values are exact; over 512 of d the tensor cores add 16 products at a time and may drop a unit (2^-23)
-of the sum's size at each of the 32 steps, and at most 128 chunks are added in fp32: a logit is off by at most
-e = 2^-18 A, A = sum |x w|. With u = 2^-18 (1 + |m| + |value|) for the softmax's own arithmetic (as in kq_token_logprobs's
+Bounds. Products of bf16 values are exact; over 1024 of d (512 for few rows) the tensor cores add 16 products at a time and may drop a unit (2^-23)
+of the sum so far at each of the 64 steps, which is half of A = sum |x w| or less in the mean of products that come in no order,
+and at most 128 chunks are added in fp32: a logit is off by at most e = 2^-18 A. With u = 2^-18 (1 + |m| + |value|) for the softmax's own arithmetic (as in kq_token_logprobs's
 tests): |lse - exact| <= e + u, |logp - exact| <= 2 e + u, and the entropy, whose derivative is -p (ln p + H):
 |H - exact| <= sum_v p |ln p + H| 2 e_v + u. The logits' gradient D = g (delta - p) - h p (ln p + H) from given lse and H:
     |dD| <= p (|g| + |h| (|ln p + H| + 1)) (2 e + 2^-18 (1 + |z| + |lse|)) + 2^-8 |D|,
