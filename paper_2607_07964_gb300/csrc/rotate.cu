@@ -15,7 +15,7 @@
 // while it works on two (16 bytes to a lane, G lanes to a row, 32 / G rows a look), computes cos and sin of the tokens' pairs
 // once, and exchanges partners by shuffles. Backwards the warps stay and go from token to token, the weights' sums in registers.
 // Measured: 32768 tokens of 40 bf16 rows of 128, with norms, 120 us (5.6 TB/s, about 140 instructions for two rows of a
-// warp); backwards 16384 tokens 105 us (4.8 TB/s, 215 instructions).
+// warp); backwards 16384 tokens 106 us (4.8 TB/s, 215 instructions).
 #include <algorithm>
 #include <atomic>
 
