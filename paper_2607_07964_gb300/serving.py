@@ -44,6 +44,13 @@ class QuantizedLinear:
         return y
 
 
+def _check_window(cache, window: int, sink: int) -> None:
+    if cache.budget is not None:
+        raise ValueError("a cache that evicts does not hold its slots in the order of positions, so it has no window")
+    if window < 1 or sink < 0:
+        raise ValueError(f"window must be at least 1 and sink at least 0, got {window} and {sink}")
+
+
 class KvCache:
     """The 4-bit cache of `batch` sequences with up to `slots` cached tokens each. With a budget, append
     first cuts the sequences back to `budget` slots when the new tokens would not fit: the last `recent` and
@@ -150,9 +157,9 @@ class KvCache:
 
     def attend(self, q, start, scale: float | None = None, lse=None, window: int | None = None, sink: int = 0):
         """Attention of q [T, q_heads, dim] of the tokens appended last over their sequences; with a window, over the last
-        `window` positions up to a token's own and the first `sink`."""
-        if window is not None and self.budget is not None:
-            raise ValueError("a cache that evicts does not hold its slots in the order of positions, so it has no window")
+        `window` positions up to a token's own and the first `sink`, without one over all of them."""
+        if window is not None:
+            _check_window(self, window, sink)
         self._capturing()
         need = kq.kq_kv_attend_workspace(q, self.data, self.table, self.acc)
         if self._ws is None or self._ws.numel() < need:
@@ -235,10 +242,14 @@ class Rotation:
 class AttentionBlock:
     """x + W_o attention(W_q x, W_k x, W_v x) with quantized projections, tokens of several sequences packed (start and
     most as KvCache.append takes them). Queries and keys are normed and rotated where a Rotation is given, by the number of
-    tokens that their sequence has had; with a window, attention sees the last `window` positions and the first `sink`."""
+    tokens that their sequence has had; with a window, attention sees the last `window` positions and the first `sink`, without
+    one all of them."""
 
     def __init__(self, proj: dict, heads: int, cache: KvCache, rotation: Rotation | None = None, window: int | None = None,
                  sink: int = 0):
+        # here, as a step that fails in its attention has appended its tokens
+        if window is not None:
+            _check_window(cache, window, sink)
         self.proj, self.heads, self.cache = proj, heads, cache
         self.rotation, self.window, self.sink = rotation, window, sink
 
