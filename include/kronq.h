@@ -606,15 +606,16 @@ KQ_API kq_status kq_token_logprobs_grad(const void* logits, int dtype, int64_t T
  *   exact, sums fp32: the tensor cores' over 1024 of d at most, then in registers, so a logit is off by 2^-17 of the
  *   sum of its products' sizes at most (2^-22 is ordinary). target as there: a negative one is not scored, one >= V recorded in info with logp = NaN. A row
  *   with a NaN or +infinite logit has NaN results. T <= KQ_LINEAR_MAX_T, V <= 2^20, d <= 65536.
- *   ws: kq_linear_logprobs_workspace(T, V, d) bytes, 256-byte aligned.
+ *   ws: kq_linear_logprobs_workspace(T, V, d) bytes, 256-byte aligned: for T > 128 rows V / 4 bytes for each row, of at most as many rows
+ *   at once as make 268 MB, or 4096. (Fewer rows may need more than many do: ask for each T.)
  * kq_linear_logprobs_grad: the gradients of sum_t (g_logp_t logp_t + g_entropy_t entropy_t) with respect to x and W,
  *   bf16 gx [T][d] and gw [V][d] (row strides ldgx, ldgw; either may be NULL), from kq_linear_logprobs's lse
  *   and entropy (entropy and g_entropy may both be NULL). The logits are computed again, a piece of the vocabulary at a time;
  *   their gradient enters both products in bf16, as kq_token_logprobs_grad would give it, the sums are fp32 and rounded once.
  *   A row with a negative target has no g_logp part; a target >= V is recorded in info, its row's g_logp part left
  *   out. gx and gw must not overlap x, W or each other. Results do not depend on the order in which blocks run.
- *   ws: kq_linear_logprobs_grad_workspace(T, V, d) bytes, 256-byte aligned (2 pieces of logits' gradients of about
- *   2^26 values, or all of up to 128 rows, and fp32 gx).
+ *   ws: kq_linear_logprobs_grad_workspace(T, V, d) bytes, 256-byte aligned (2 pieces of logits' gradients in bf16, of
+ *   about 2^26 values each, 1024 for each row from 65536 rows on, or all of up to 128 rows; and fp32 gx).
  * info (nullable): also -KQ_ERR_TIMEOUT where a kernel gave up a wait.
  * ---------------------------------------------------------------------------------- */
 #define KQ_LINEAR_MAX_T (1 << 24)

@@ -54,6 +54,7 @@ constexpr int kTileCost = 1;                     // what beginning and ending a 
 constexpr int kBand = 16;                        // row tiles that go through the vocabulary together
 constexpr int64_t kPiece = 1 << 26;              // elements of D that a piece holds, about
 constexpr int64_t kLeastPiece = 1024;            // columns
+constexpr int64_t kMostParts = 1 << 24;          // sums of 64 logits that scoring holds at once, of 4096 rows at least
 constexpr int kMostPairs = 96;                   // clusters that a launch with tiles of several sizes has
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kNone = -1.0e30f;                // t of a logit that cannot occur: 2^t = 0 and 0 t a number
@@ -1558,6 +1559,18 @@ Cut cut_of(int64_t T, int64_t V, int64_t d) {
     return c;
 }
 size_t al256(size_t b) { return (b + 255) & ~static_cast<size_t>(255); }
+// Rows that scoring has room for at once, whole bands: their parts, 16 bytes for 64 logits, are joined before the next rows come, so
+// that the workspace does not grow with the rows. At 2^29 logits or more a time that costs 1 to 2 % (16384 rows of 131072 x 512 by 8192
+// 1.45 and 1.46 ms, of 131072 x 64 1.14 and 1.16; 65536 of 128000 x 2048 19.5 and 19.5).
+int64_t score_room(int64_t V) {
+    constexpr int64_t band = kBand * BM;
+    return std::max(band, kMostParts / cdiv(V, 64) / band * band);
+}
+// Rows of each time: as many times as the room asks for, evenly, as a time of a few rows reads W for them alone.
+int64_t score_rows(int64_t T, int64_t V) {
+    const int64_t times = cdiv(T, score_room(V));
+    return times == 1 ? T : cdiv(cdiv(T, times), BM) * BM;
+}
 // Parts of a row's sums: 64 columns of a tile, or the rows of W that a CTA has of one of few tiles.
 int64_t most_parts(int64_t T, int64_t V) {
     return T <= kThinMost ? std::max(cdiv(V, 64), 8 * std::min<int64_t>(cdiv(V, kThinRows), 128)) : cdiv(V, 64);
@@ -1587,7 +1600,8 @@ using namespace kq;
 
 extern "C" size_t kq_linear_logprobs_workspace(int64_t T, int64_t V, int64_t d) {
     if (T < 1 || V < 1 || d < 1) return 0;
-    return al256(static_cast<size_t>(T) * most_parts(T, V) * sizeof(float4)) + al256(T * sizeof(float));
+    const int64_t rows = std::min(T, score_room(V));
+    return al256(static_cast<size_t>(rows) * most_parts(T, V) * sizeof(float4)) + al256(rows * sizeof(float));
 }
 
 extern "C" kq_status kq_linear_logprobs(const uint16_t* x, int64_t T, int64_t d, int64_t ldx, const uint16_t* w, int64_t V, int64_t ldw,
@@ -1608,24 +1622,30 @@ extern "C" kq_status kq_linear_logprobs(const uint16_t* x, int64_t T, int64_t d,
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
     KQ_TRY(set_up());
     Maps m;
-    KQ_TRY(make_map(&m.x, x, T, d, ldx, who, T <= kThinMost ? thin_box_rows(thin_tokens(T)) : 64));
     KQ_TRY(make_map(&m.w, w, V, d, ldw, who));
     m.d = m.out_d = m.out_x = m.out_w = m.w;   // not used
+    const bool thin = T <= kThinMost;
+    const int64_t rows = score_rows(T, V), room = std::min(T, score_room(V));
     Job j = {};
-    j.T = T, j.V = V, j.d = d;
-    j.target = target;
-    j.parts = static_cast<int32_t>(cdiv(V, 64));
+    j.V = V, j.d = d;
     j.part = static_cast<float4*>(ws);
-    j.zt = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + al256(static_cast<size_t>(T) * most_parts(T, V) * sizeof(float4)));
-    j.m_main = static_cast<int32_t>(cdiv(T, BM));
+    j.zt = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + al256(static_cast<size_t>(room) * most_parts(T, V) * sizeof(float4)));
     j.n_main = static_cast<int32_t>(cdiv(V, BN));
-    j.tiles = j.m_main * j.n_main;
     j.w_main = V;
     j.d_slabs = static_cast<int32_t>(cdiv(d, BK));
     j.info = info;
-    KQ_TRY(T <= kThinMost ? run_thin(m, j, stream) : run_tiles<kScore>(m, j, stream));
-    KQ_CUDA(launch_after(linear_join_kernel, dim3(static_cast<unsigned>(T)), dim3(128), 0, stream, j, logp, entropy, lse));
-    count_launch();
+    for (int64_t r = 0; r < T; r += rows) {
+        j.T = std::min(rows, T - r);
+        KQ_TRY(make_map(&m.x, x + r * ldx, j.T, d, ldx, who, thin ? thin_box_rows(thin_tokens(T)) : 64));
+        j.target = target + r;
+        j.parts = static_cast<int32_t>(cdiv(V, 64));
+        j.m_main = static_cast<int32_t>(cdiv(j.T, BM));
+        j.tiles = j.m_main * j.n_main;
+        KQ_TRY(thin ? run_thin(m, j, stream) : run_tiles<kScore>(m, j, stream));
+        KQ_CUDA(launch_after(linear_join_kernel, dim3(static_cast<unsigned>(j.T)), dim3(128), 0, stream, j, logp + r,
+                             entropy ? entropy + r : nullptr, lse ? lse + r : nullptr));
+        count_launch();
+    }
     return KQ_OK;
 }
 
