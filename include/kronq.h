@@ -426,10 +426,10 @@ KQ_API kq_status kq_infer(const uint32_t* packed, const float* scale, const int3
  *   first[b] + i - start[b] for token i of sequence b, tokens of no sequence being left as they were; or the
  *   token's index in the call where all are NULL.
  *   q, k and their outputs are of dtype KQ_BF16 or KQ_F32, [T][heads][dim] with token and head strides in
- *   elements and unit stride in dim; an output may be its input, and each of its rows has a place of its own. k and
+ *   elements and unit stride in dim; an output may be its own input, and each row of both outputs has a place of its own. k and
  *   k_out may be NULL together. Weights are of the same type and may each be NULL. dim <= 256, rot even, 0 <= rot <= dim. fp32 arithmetic, one rounding.
  * kq_qk_rotate_grad: with gq, gk the gradients of the outputs, q_out and k_out receive those of q and k (an
- *   output may be its gq or gk), gq_weight and gk_weight [dim] fp32 (nullable) those of the weights, summed over tokens and
+ *   output may be its own gq or gk), gq_weight and gk_weight [dim] fp32 (nullable) those of the weights, summed over tokens and
  *   heads in an order that depends on the sizes only. q and k themselves are read where there is a weight, and may
  *   be NULL elsewhere.
  *   ws: kq_qk_rotate_grad_workspace(T, dim) bytes, 256-byte aligned, needed with a weight's gradient.

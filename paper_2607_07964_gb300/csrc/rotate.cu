@@ -743,6 +743,16 @@ kq_status check(const char* who, const kq_rotation* r, int dtype, int64_t T, int
     return KQ_OK;
 }
 
+// A side's warps do not wait for the other's: neither output may be the other one, nor what the other side reads (x, and backwards g).
+kq_status check_places(const char* who, const kq_heads* const (&out)[2], const kq_heads* const (&x)[2], const kq_heads* const (&g)[2]) {
+    if (!out[1]) return KQ_OK;
+    bool same = out[0]->data == out[1]->data;
+    for (int i = 0; i < 2; ++i) same = same || (x[1 - i] && out[i]->data == x[1 - i]->data) || (g[1 - i] && out[i]->data == g[1 - i]->data);
+    if (!same) return KQ_OK;
+    set_error("%s: the outputs must not be each other or an input of each other's", who);
+    return KQ_ERR_INVALID_ARG;
+}
+
 }  // namespace
 
 KQ_DEBUG_UNIT(rotate)
@@ -755,6 +765,7 @@ extern "C" kq_status kq_qk_rotate(const kq_rotation* r, int dtype, int64_t T, in
                                   float eps, kq_stream_t stream_) {
     KQ_TRY(check("kq_qk_rotate", r, dtype, T, dim, {q, k}, {q_out, k_out}, {q_weight, k_weight}, eps));
     if (T == 0) return KQ_OK;
+    KQ_TRY(check_places("kq_qk_rotate", {q_out, k_out}, {q, k}, {nullptr, nullptr}));
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
     if (dtype == KQ_BF16)
         return run<__nv_bfloat16>(r, T, dim, q, k, nullptr, nullptr, q_out, k_out, q_weight, k_weight, eps, nullptr,
@@ -800,6 +811,11 @@ extern "C" kq_status kq_qk_rotate_grad(const kq_rotation* r, int dtype, int64_t 
     if (sums && (!ws || ws_bytes < kq_qk_rotate_grad_workspace(T, dim) || (reinterpret_cast<uintptr_t>(ws) & 255u))) {
         set_error("%s: workspace must be 256-byte aligned and hold %zu bytes", who, kq_qk_rotate_grad_workspace(T, dim));
         return KQ_ERR_WORKSPACE;
+    }
+    KQ_TRY(check_places(who, {q_out, k_out}, {q_weight ? q : nullptr, k_weight ? k : nullptr}, {gq, gk}));
+    if (gq_weight && gq_weight == gk_weight) {
+        set_error("%s: the weights' gradients must not be each other", who);
+        return KQ_ERR_INVALID_ARG;
     }
     float* s = sums ? static_cast<float*>(ws) : nullptr;
     if (dtype == KQ_BF16)
