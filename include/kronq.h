@@ -613,7 +613,7 @@ KQ_API kq_status kq_token_logprobs_grad(const void* logits, int dtype, int64_t T
  *   and entropy (entropy and g_entropy may both be NULL). The logits are computed again, a piece of the vocabulary at a time;
  *   their gradient enters both products in bf16, as kq_token_logprobs_grad would give it, the sums are fp32 and rounded once.
  *   A row with a negative target has no g_logp part; a target >= V is recorded in info, its row's g_logp part left
- *   out. gx and gw must not overlap x, W or each other. Results do not depend on the order in which blocks run.
+ *   out. x must be finite in those rows too: a NaN or an infinity in a row of x reaches all of gw, as D^T x has it. gx and gw must not overlap x, W or each other. Results do not depend on the order in which blocks run.
  *   ws: kq_linear_logprobs_grad_workspace(T, V, d) bytes, 256-byte aligned (2 pieces of logits' gradients in bf16, of
  *   about 2^26 values each, 1024 for each row from 65536 rows on, or all of up to 128 rows; and fp32 gx).
  * info (nullable): also -KQ_ERR_TIMEOUT where a kernel gave up a wait.
